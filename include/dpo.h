@@ -409,6 +409,190 @@ int dpo_grad_norm_noalloc(const void *grad, int64_t numel, dpo_dtype grad_dtype,
                           void *cuda_stream);
 
 /*
+ * ---- The feed-forward half of a pipeline stage ----------------------------
+ *
+ * What a stage runs between two optimizer steps: the residual's addition and the
+ * root-mean-square norm, the gated feed-forward block, their backward passes
+ * into the gradient buffers that the next step reads, and the activations of
+ * the microbatches in flight kept in 8 bits until their backward. The weights
+ * are what dpo_read_weights(DPO_STALE) names (PipeDream-2BW, Sec. 2).
+ *
+ * These calls have no context. The caller owns every buffer, workspace included;
+ * all are device memory of the current device. Matrices are row-major with
+ * contiguous rows; ld is the pitch in elements between rows (>= the columns).
+ * No output may overlap an input or another output. Nothing is allocated and
+ * the host is never synchronized: the launches go to the stream passed in, and
+ * the buffers stay alive and in place until they are done. Two calls
+ * may share a workspace only on one stream. A call of zero rows launches
+ * nothing, except that a gradient of weights that is not accumulated is set to
+ * zero. Errors: a DPO_E* code, with the message of the calling thread's last
+ * failure in dpo_last_error(NULL).
+ */
+
+/*
+ * Activations in 8 bits. Each row is cut into groups of DPO_PACK8_GROUP
+ * elements (the last may be shorter); a group shares the scale 2^(s - 127), s
+ * its scale byte (1 .. 247), the smallest power of two >= 2^-126 with which its
+ * largest finite magnitude is at most 448. Codes are E4M3 (one sign, four
+ * exponent, three fraction bits), rounded to nearest even; infinities and NaN
+ * become NaN codes and do not take part in the scale.
+ */
+#define DPO_PACK8_GROUP 32
+
+typedef struct {
+    uint8_t *codes;             /* rows x cols */
+    uint8_t *scales;            /* rows x ceil(cols / DPO_PACK8_GROUP) */
+    int64_t ld_codes, ld_scales;
+} dpo_packed8;
+
+/* codes, scales := x (rows x cols; DPO_F32 or DPO_BF16). Returns DPO_OK,
+ * DPO_EINVAL, DPO_EALIGN (a pointer not aligned to its elements), DPO_EDTYPE
+ * or DPO_ECUDA. */
+int dpo_pack8(const void *x, dpo_dtype dtype, int64_t rows, int64_t cols, int64_t ld_x,
+              const dpo_packed8 *out, void *cuda_stream);
+
+/* out (rows x cols, DPO_F32 or DPO_BF16) := the values that the codes stand
+ * for, rounded to its type: both hold them exactly but at the ends of their
+ * range (a magnitude above 3.17e38 may decode to 2^128, an infinity). Errors
+ * as dpo_pack8. */
+int dpo_unpack8(const dpo_packed8 *in, int64_t rows, int64_t cols, void *out, dpo_dtype dtype,
+                int64_t ld_out, void *cuda_stream);
+
+/*
+ * Residual addition and root-mean-square norm, per row of cols elements:
+ *   s = x + residual,  rstd = 1 / sqrt(mean(s^2) + eps),
+ *   y = (s rstd) weight,  h = s,  x8 = the 8-bit form of s rstd
+ * in fp32, each output rounded once.
+ */
+typedef struct {
+    const void *x;              /* dtype */
+    const void *residual;       /* dtype, or NULL: s = x */
+    const void *weight;         /* weight_dtype, cols */
+    void *h;                    /* dtype, or NULL */
+    void *y;                    /* dtype, or NULL */
+    float *rstd;                /* rows */
+    dpo_packed8 x8;             /* codes NULL: not written */
+    int64_t rows, cols;         /* cols in [1, DPO_RMSNORM_MAX_COLS] */
+    int64_t ld_x, ld_residual, ld_h, ld_y;
+    float eps;                  /* >= 0 */
+    int dtype;                  /* DPO_F32 or DPO_BF16 */
+    int weight_dtype;           /* dtype or DPO_F32 */
+} dpo_rmsnorm_args;
+
+#define DPO_RMSNORM_MAX_COLS 16384
+
+/* Returns DPO_OK, DPO_EINVAL, DPO_EALIGN, DPO_EDTYPE or DPO_ECUDA. */
+int dpo_rmsnorm(const dpo_rmsnorm_args *args, void *cuda_stream);
+
+/*
+ * Its backward pass: with the normalised rows n = h rstd, or the values of x8
+ * (the forward's 8-bit output, in whose place h need not be kept),
+ *   g = dy weight,  dx = rstd (g - n mean(g n)) + dh,  dweight = sum over rows of dy n
+ * dx is the gradient of x and of residual alike. Sums are in fp32, in an order
+ * that depends on the sizes alone.
+ */
+typedef struct {
+    const void *dy;             /* dtype */
+    const void *h;              /* dtype, or NULL: from x8 */
+    dpo_packed8 x8;             /* read when h is NULL */
+    const float *rstd;
+    const void *weight;
+    const void *dh;             /* gradient that reaches s past the norm (dtype), or NULL */
+    void *dx;                   /* dtype, or NULL */
+    void *dweight;              /* dweight_dtype, cols, or NULL */
+    int64_t rows, cols;
+    int64_t ld_dy, ld_h, ld_dh, ld_dx;
+    int dtype, weight_dtype, dweight_dtype;
+    int accumulate;             /* add to dweight instead of replacing it */
+    void *workspace;            /* dpo_rmsnorm_workspace bytes, 16-byte aligned */
+    int64_t workspace_bytes;
+} dpo_rmsnorm_backward_args;
+
+int dpo_rmsnorm_backward(const dpo_rmsnorm_backward_args *args, void *cuda_stream);
+
+/* Bytes of workspace of dpo_rmsnorm_backward on the current device. */
+int dpo_rmsnorm_workspace(int64_t rows, int64_t cols, int64_t *bytes);
+
+/* Gate activations: z sigmoid(z), and z sigmoid(2 sqrt(2/pi) (z + 0.044715 z^3)),
+ * which is GELU's tanh form. */
+#define DPO_ACT_SILU 0
+#define DPO_ACT_GELU 1
+
+/* What the forward keeps of its two projections for the backward. */
+#define DPO_KEEP_NONE 0
+#define DPO_KEEP_8BIT 1
+#define DPO_KEEP_BF16 2
+
+/*
+ * Gated feed-forward block, bf16 operands and fp32 accumulation:
+ *   G = x w_gate^T,  U = x w_up^T,  A = act(G) U,  out = A w_down^T
+ * A is rounded once to bf16, the second product's operand type. keep says what
+ * is stored of G and U: their 8-bit form or bf16. dim and hidden are multiples
+ * of 8; pointers are 16-byte aligned, pitches of bf16 matrices multiples of 8,
+ * of codes of 16.
+ */
+typedef struct {
+    const void *x;              /* bf16, tokens x dim */
+    const void *w_gate, *w_up;  /* bf16, hidden x dim, pitch dim */
+    const void *w_down;         /* bf16, dim x hidden, pitch hidden */
+    void *out;                  /* bf16, tokens x dim */
+    void *gate, *up;            /* DPO_KEEP_BF16: bf16, tokens x hidden, pitch hidden */
+    dpo_packed8 gate8, up8;     /* DPO_KEEP_8BIT: tokens x hidden */
+    int64_t tokens, dim, hidden;
+    int64_t ld_x, ld_out;
+    int act, keep;
+    void *workspace;            /* 256-byte aligned; see dpo_ffn_workspace */
+    int64_t workspace_bytes;
+} dpo_ffn_args;
+
+int dpo_ffn_forward(const dpo_ffn_args *args, void *cuda_stream);
+
+/*
+ * Its backward pass, from what the forward kept:
+ *   dA = dout w_down,  dU = dA act(G),  dG = dA U act'(G)   (rounded once to bf16)
+ *   dx = dG w_gate + dU w_up
+ *   dw_gate = dG^T x,  dw_up = dU^T x,  dw_down = dout^T A
+ * The block's input is x, or the 8-bit rows x8 times gain along the columns
+ * (dpo_rmsnorm's x8 and weight): those values are bf16 ones, and the products
+ * dG^T x8 and dU^T x8 take the gain in fp32 before their one rounding.
+ */
+typedef struct {
+    const void *dout;           /* bf16, tokens x dim */
+    const void *x;              /* bf16, tokens x dim, or NULL: from x8 */
+    dpo_packed8 x8;
+    const void *gain;           /* with x8: dim factors, or NULL: ones */
+    const void *w_gate, *w_up, *w_down;
+    const void *gate, *up;
+    dpo_packed8 gate8, up8;
+    void *dx;                   /* bf16, tokens x dim, or NULL */
+    void *dw_gate, *dw_up;      /* grad_dtype, hidden x dim */
+    void *dw_down;              /* grad_dtype, dim x hidden */
+    int64_t tokens, dim, hidden;
+    int64_t ld_dout, ld_x, ld_dx;
+    int act, keep;              /* keep as in the forward, not DPO_KEEP_NONE */
+    int grad_dtype;             /* DPO_F32 or DPO_BF16 */
+    int gain_dtype;             /* DPO_F32 or DPO_BF16 */
+    int accumulate;             /* add to the dw buffers instead of replacing them */
+    void *workspace;
+    int64_t workspace_bytes;
+} dpo_ffn_backward_args;
+
+/* Both return DPO_OK, DPO_EINVAL, DPO_EALIGN, DPO_EDTYPE or DPO_ECUDA. */
+int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_stream);
+
+/* Bytes of workspace of the two calls (from_x8: the backward reads x8). */
+int dpo_ffn_workspace(int64_t tokens, int64_t dim, int64_t hidden, int from_x8,
+                      int64_t *forward_bytes, int64_t *backward_bytes);
+
+/*
+ * Error bits of the feed-forward kernels on the current device since the last
+ * clear (a wait inside a kernel that gave up after one second; 0 when healthy).
+ * Waits for the device. dpo_ffn_clear_status clears them on the stream.
+ */
+int dpo_ffn_get_status(uint32_t *bits);
+int dpo_ffn_clear_status(void *cuda_stream);
+
+/*
  * Test hook for the allocation-failure paths, process-wide: of the library's
  * next device allocations (dpo_init makes one, dpo_muon_init one or two: its
  * table, then its workspace), let `after` succeed and make the following
@@ -418,8 +602,8 @@ int dpo_grad_norm_noalloc(const void *grad, int64_t numel, dpo_dtype grad_dtype,
  */
 int dpo_test_fail_allocs(int after, int count);
 
-/* Message of the last failing call on ctx (NULL ctx: last dpo_init failure of
- * the calling thread). Never NULL; owned by the library. */
+/* Message of the last failing call on ctx (NULL ctx: the calling thread's last
+ * failure of dpo_init or of a feed-forward call). Never NULL; owned by the library. */
 const char *dpo_last_error(const dpo_ctx *ctx);
 
 /* Free the context and its device scratch (after the work enqueued on it has

@@ -31,12 +31,14 @@ LIBS = {
     "libdpo.so": {
         "sources": ["csrc/dpo_kernels.cu", "csrc/dpo_step_adamw.cu", "csrc/dpo_step_nadam.cu",
                     "csrc/dpo_step_lion.cu", "csrc/dpo_step_adan.cu", "csrc/dpo_abi.cpp",
-                    "csrc/dpo_noalloc.cu", "csrc/dpo_muon.cu"],
+                    "csrc/dpo_noalloc.cu", "csrc/dpo_muon.cu", "csrc/dpo_rmsnorm.cu",
+                    "csrc/dpo_ffn.cu"],
         "headers": ["csrc/dpo_internal.h", "csrc/dpo_device.cuh", "csrc/dpo_reduce.cuh",
                     "csrc/dpo_step.cuh",
-                    "csrc/dpo_gemm.cuh", "../include/dpo.h", "../include/dpo_muon.h"],
+                    "csrc/dpo_gemm.cuh", "csrc/dpo_pack8.cuh", "csrc/dpo_ffn_gemm.cuh",
+                    "../include/dpo.h", "../include/dpo_muon.h"],
         "includes": ["csrc"],
-        "ptxas_v": ["csrc/dpo_step_adamw.cu", "csrc/dpo_muon.cu"],
+        "ptxas_v": ["csrc/dpo_step_adamw.cu", "csrc/dpo_muon.cu", "csrc/dpo_ffn.cu"],
     },
     "libdpo_synth.so": {
         "sources": ["synth/synth.cu"],

@@ -91,6 +91,26 @@ int cuda_fail(dpo_ctx *c, cudaError_t e, const char *what)
     return fail(c, DPO_ECUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
+}  // namespace
+
+namespace dpo {
+int call_fail(int code, const char *fmt, ...)
+{
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    try {
+        g_init_err = buf;
+    } catch (const std::bad_alloc &) {   // the code still goes out
+    }
+    return code;
+}
+}  // namespace dpo
+
+namespace {
+
 bool valid_dtype(int d) { return d == DPO_F32 || d == DPO_BF16; }
 int64_t dt_size(dpo_dtype d) { return d == DPO_BF16 ? 2 : 4; }
 

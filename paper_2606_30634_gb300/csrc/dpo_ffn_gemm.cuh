@@ -1,0 +1,631 @@
+// dpo_ffn_gemm.cuh -- the products of the gated feed-forward block on the
+// sm_103a tensor cores (tcgen05, TMA, TMEM), with the block's element-wise work
+// in their epilogues.
+//
+//   D = sum over segments s of A_s B_s      (M x N, fp32 accumulation)
+//
+// Operands are bf16 and taken as they lie in memory: A_s is M x K row-major
+// (K contiguous) or K x M row-major (M contiguous), B_s is N x K or K x N
+// likewise, so no transposed copy of a weight, an activation or a gradient is
+// ever made. A product has one or two segments of K (dx = dG w_gate + dU w_up).
+// Boxes past the edge of a matrix read as zeros and stores past it are
+// clipped by TMA, so no size needs padding.
+//
+// Roles, rings and barriers are those of the Newton-Schulz GEMM (dpo_gemm.cuh,
+// whose primitives this kernel uses): a persistent grid of CTA pairs on 256 x 256
+// tiles with the 2-SM MMA (CG = 2), or of single CTAs on 128 x 128 tiles (CG = 1)
+// where there are few; warp 0 loads, warp 1 issues the MMAs, eight warps drain
+// one accumulator while the MMAs fill the other. Every wait is bounded.
+//
+// Epilogues:
+//   kGate      the tile's columns are T / 2 of G beside the same T / 2 of U (the B
+//              operand is half w_gate rows, half w_up rows), so act(G) U is formed
+//              where both are in registers; writes A and what is kept of G and U
+//   kGateBack  the tile is of dA; reads what was kept of G and U, writes dG, dU, A
+//   kStore     writes D in bf16 or fp32, with factors along the columns and the old
+//              contents added where asked for
+#pragma once
+
+#include "dpo_gemm.cuh"
+#include "dpo_pack8.cuh"
+
+namespace dpo {
+namespace ffn {
+
+using gemm::BH;
+using gemm::BK;
+using gemm::BM;
+using gemm::group_sync;
+using gemm::kABytes;
+using gemm::kBBytes;
+using gemm::kBoxK;
+using gemm::kChunkBytes;
+using gemm::kErrDrain;
+using gemm::kErrWaitDone;
+using gemm::kErrWaitEmpty;
+using gemm::kErrWaitFull;
+using gemm::kStageBytes;
+using gemm::kStages;
+using gemm::kTile;
+using gemm::map_to_rank;
+using gemm::mbar_arrive;
+using gemm::mbar_arrive_expect_tx;
+using gemm::mbar_init;
+using gemm::mbar_wait;
+using gemm::mma_bf16;
+using gemm::mma_commit;
+using gemm::smem_desc;
+using gemm::smem_desc_mn;
+using gemm::swz64;
+using gemm::tmem_ld32;
+
+enum Epilogue { kGate = 0, kGateBack = 1, kStore = 2 };
+enum Keep { kKeepNone = 0, kKeep8 = 1, kKeep16 = 2 };
+enum Act { kSilu = 0, kGelu = 1 };
+
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = 64 + 32 * kEpiWarps;
+constexpr int kStaging = 2 * kChunkBytes;                     // per epilogue warp
+constexpr int kSmemBytes = kStages * kStageBytes + 1024 + kEpiWarps * kStaging;
+
+constexpr int kMaxProducts = 4;
+constexpr int kBandRows = 16;   // block rows per band, as in dpo_gemm.cuh
+
+// One product of a launch.
+struct Product {
+    CUtensorMap a[2], b[2];       // operands per segment (kGate: b[0] w_gate, b[1] w_up)
+    CUtensorMap d0, d1, d2;       // stores: kGate A, G, U; kGateBack dG, dU, A; kStore D
+    int m, n;                     // kGate: n is one projection's columns
+    int k_blocks[2];              // K blocks of each segment (second 0: one segment)
+    int a_mn, b_mn;               // the operand is M- or N-contiguous
+    int m_tiles, n_tiles, first;  // tiles, and the launch's number of the first
+    // kStore
+    int f32, accumulate;
+    const void *old;              // accumulate: D itself
+    int64_t ld_old;
+    const void *gain;             // N factors, or nullptr
+    int gain_f32;
+    // kGate, kGateBack
+    uint8_t *scale_g, *scale_u;   // kKeep8
+    int64_t ld_scale;
+    const void *kept_g, *kept_u;  // kGateBack: codes or bf16
+    int64_t ld_kept;
+    int keep, act;                // Keep, Act
+};
+
+struct Launch {
+    Product p[kMaxProducts];
+    int n_products, n_tiles;
+    unsigned int *err;
+};
+
+// 2-D TMA load and store (see the 3-D ones in dpo_gemm.cuh).
+template <int CG>
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int x, int y,
+                                         uint32_t bar)
+{
+    if (CG == 2)
+        asm volatile(
+            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+            " [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+            "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes"
+            " [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+            "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
+            : "memory");
+}
+
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, uint32_t src, int x, int y)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                     reinterpret_cast<uint64_t>(map)),
+                 "r"(src), "r"(x), "r"(y)
+                 : "memory");
+}
+
+// kind::f16 with fp32 accumulation and bf16 operands, M = N = kTile(cg), operands
+// K-major, or MN-major with bits 15 (A) and 16 (B).
+__device__ __forceinline__ uint32_t idesc_of(int cg, int a_mn, int b_mn)
+{
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTile(cg) >> 3) << 17) |
+           ((uint32_t)(kTile(cg) >> 4) << 24) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16);
+}
+
+// Product and position of tile t: bands of kBandRows block rows, column by column.
+struct Tile {
+    int p, m, n;   // product, block row, block column
+};
+__device__ __forceinline__ Tile tile_at(const Launch &L, int t)
+{
+    int p = 0;
+    while (p + 1 < L.n_products && t >= L.p[p + 1].first)
+        ++p;
+    const Product &P = L.p[p];
+    const int i = t - P.first, band = kBandRows * P.n_tiles;
+    const int b = i / band, r = i - b * band;
+    const int rows = min(kBandRows, P.m_tiles - b * kBandRows);
+    const int n = r / rows;
+    return {p, b * kBandRows + r - n * rows, n};
+}
+
+// act(z) = z s(q(z)) with s the logistic function: SiLU with q = z, GELU's tanh form
+// with q = 2 sqrt(2/pi) (z + 0.044715 z^3), since (1 + tanh(q / 2)) / 2 = s(q).
+// act' = s + z q' s (1 - s).
+template <int ACT>
+__device__ __forceinline__ float logistic(float z, float &dq)
+{
+    float q = z;
+    dq = 1.0f;
+    if (ACT == kGelu) {
+        const float c = 1.5957691216057308f, k = 0.044715f * c, z2 = z * z;
+        q = z * fmaf(k, z2, c);
+        dq = fmaf(3.0f * k, z2, c);
+    }
+    return __fdividef(1.0f, 1.0f + __expf(-q));
+}
+
+// 32 fp32 values of one row from 64 bytes of bf16.
+__device__ __forceinline__ void load_bf16_row(const __nv_bfloat16 *p, float (&v)[32])
+{
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+        const uint4 q = gemm::load_c(p + 8 * h);
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[h * 8 + 2 * j] = __uint_as_float(w[j] << 16);
+            v[h * 8 + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+        }
+    }
+}
+
+// 32 values of one row from 32 codes and their scale.
+__device__ __forceinline__ void load_codes_row(const uint8_t *p, float scale, float (&v)[32])
+{
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint4 q = gemm::load_c(reinterpret_cast<const __nv_bfloat16 *>(p) + 8 * h);
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 lo = decode2(w[j]), hi = decode2(w[j] >> 16);
+            v[h * 16 + 4 * j] = lo.x * scale;
+            v[h * 16 + 4 * j + 1] = lo.y * scale;
+            v[h * 16 + 4 * j + 2] = hi.x * scale;
+            v[h * 16 + 4 * j + 3] = hi.y * scale;
+        }
+    }
+}
+
+__device__ __forceinline__ float load_scale_byte(const uint8_t *p)
+{
+    uint16_t v;
+    asm volatile("ld.global.u8 %0, [%1];" : "=h"(v) : "l"(p));
+    return scale_of(v);
+}
+
+// What one epilogue warp stages and stores: 32 x 32 chunks through two buffers in
+// turn. Each chunk is a bulk async-group of its own, so a buffer is free once all
+// groups but the last one have been read.
+struct Stager {
+    uint32_t buf;
+    int lane, turn;
+    __device__ __forceinline__ uint32_t begin()
+    {
+        if (lane == 0) {
+            if (turn == 0)   // the chunk before may have been fp32, in both buffers
+                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            else
+                asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        }
+        __syncwarp();
+        const uint32_t b = buf + (uint32_t)((turn & 1) * kChunkBytes);
+        ++turn;
+        return b;
+    }
+    __device__ __forceinline__ void end(const CUtensorMap *map, uint32_t b, int x, int y)
+    {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            tma_store(map, b, x, y);
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+    }
+    __device__ __forceinline__ void bf16(const CUtensorMap *map, const float (&v)[32], int x, int y)
+    {
+        const uint32_t b = begin();
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(b + swz64(lane, g)),
+                         "r"(gemm::pack_bf16(v[g * 8], v[g * 8 + 1])),
+                         "r"(gemm::pack_bf16(v[g * 8 + 2], v[g * 8 + 3])),
+                         "r"(gemm::pack_bf16(v[g * 8 + 4], v[g * 8 + 5])),
+                         "r"(gemm::pack_bf16(v[g * 8 + 6], v[g * 8 + 7]))
+                         : "memory");
+        end(map, b, x, y);
+    }
+    // one 4 KiB chunk in the 128-byte swizzle (granule index XOR row mod 8), in both
+    // buffers
+    __device__ __forceinline__ void f32(const CUtensorMap *map, const float (&v)[32], int x, int y)
+    {
+        if (lane == 0)
+            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
+#pragma unroll
+        for (int g = 0; g < 8; ++g)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
+                             buf + (uint32_t)(lane * 128 + ((g ^ (lane & 7)) << 4))),
+                         "r"(__float_as_uint(v[g * 4])), "r"(__float_as_uint(v[g * 4 + 1])),
+                         "r"(__float_as_uint(v[g * 4 + 2])), "r"(__float_as_uint(v[g * 4 + 3]))
+                         : "memory");
+        end(map, buf, x, y);
+        turn = 0;
+    }
+    // 32 rows of 32 codes; returns this row's scale byte
+    __device__ __forceinline__ uint32_t codes(const CUtensorMap *map, const float (&v)[32], int x,
+                                              int y)
+    {
+        float amax = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            amax = fmaxf(amax, finite_abs(v[j]));
+        const uint32_t s = scale_byte(amax);
+        const float inv = inv_scale_of(s);
+        const uint32_t b = begin();
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int i = g * 16 + 4 * j;
+                w[j] = encode4(inf_to_nan(v[i]) * inv, inf_to_nan(v[i + 1]) * inv,
+                               inf_to_nan(v[i + 2]) * inv, inf_to_nan(v[i + 3]) * inv);
+            }
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
+                             b + (uint32_t)(lane * 32 + g * 16)),
+                         "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
+                         : "memory");
+        }
+        end(map, b, x, y);
+        return s;
+    }
+};
+
+__device__ __forceinline__ void load_acc(uint32_t acc, float (&v)[32])
+{
+    uint32_t r[32];
+    tmem_ld32(acc, r);
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+        v[j] = __uint_as_float(r[j]);
+}
+
+// u := act(g) u
+template <int ACT> __device__ __forceinline__ void gate(const float (&g)[32], float (&u)[32])
+{
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+        float dq;
+        u[j] *= g[j] * logistic<ACT>(g[j], dq);
+    }
+}
+
+// g, u, d := dG, dU, A of the gate's g and u and dA = d
+template <int ACT>
+__device__ __forceinline__ void gate_back(float (&g)[32], float (&u)[32], float (&d)[32])
+{
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+        float dq;
+        const float s = logistic<ACT>(g[j], dq), da = d[j];
+        const float act = g[j] * s, slope = fmaf(act * dq, 1.0f - s, s);
+        d[j] = act * u[j];
+        g[j] = da * u[j] * slope;
+        u[j] = da * act;
+    }
+}
+
+// 32 values of one row of what was kept, from column col0; zeros from column n.
+// Rows and pitches are 16-byte aligned and col0 is a multiple of 32, so a whole chunk is
+// read in 16-byte pieces; one that the matrix ends in, element by element.
+__device__ __forceinline__ void load_kept(const Product &P, const void *kept,
+                                          const uint8_t *scales, int row, int col0, float (&v)[32])
+{
+    const int64_t at = row * P.ld_kept + col0;
+    const bool whole = col0 + 32 <= P.n;
+    if (P.keep == kKeep8) {
+        const float s = load_scale_byte(scales + row * P.ld_scale + col0 / kGroup);
+        const uint8_t *p = static_cast<const uint8_t *>(kept) + at;
+        if (whole) {
+            load_codes_row(p, s, v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                uint16_t c = 0;
+                if (col0 + j < P.n)
+                    asm volatile("ld.global.u8 %0, [%1];" : "=h"(c) : "l"(p + j));
+                v[j] = decode2(c).x * s;
+            }
+        }
+    } else {
+        const __nv_bfloat16 *p = static_cast<const __nv_bfloat16 *>(kept) + at;
+        if (whole) {
+            load_bf16_row(p, v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                v[j] = col0 + j < P.n ? ld1(p + j) : 0.0f;
+        }
+    }
+}
+
+// One 32 x 32 chunk of the tile: accumulator columns from acc (kGate: of G, U's
+// half_cols further), output rows from row0 and columns from col0. Called by the
+// whole warp with the same arguments; tcgen05.ld and the stores are the warp's.
+template <int EPI>
+__device__ __forceinline__ void drain(const Product &P, Stager &st, uint32_t acc, int half_cols,
+                                      int row0, int col0)
+{
+    if (row0 >= P.m || col0 >= P.n)
+        return;
+    const int row = min(row0 + st.lane, P.m - 1);   // rows past the end: the stores clip them
+    if constexpr (EPI == kGate) {
+        float g[32], u[32];
+        load_acc(acc, g);
+        load_acc(acc + (uint32_t)half_cols, u);
+        if (P.keep == kKeep16) {
+            st.bf16(&P.d1, g, col0, row0);
+            st.bf16(&P.d2, u, col0, row0);
+        } else if (P.keep == kKeep8) {
+            const uint32_t sg = st.codes(&P.d1, g, col0, row0);
+            const uint32_t su = st.codes(&P.d2, u, col0, row0);
+            if (row0 + st.lane < P.m) {
+                const int64_t at = row * P.ld_scale + col0 / kGroup;
+                P.scale_g[at] = (uint8_t)sg;
+                P.scale_u[at] = (uint8_t)su;
+            }
+        }
+        if (P.act == kGelu)
+            gate<kGelu>(g, u);
+        else
+            gate<kSilu>(g, u);
+        st.bf16(&P.d0, u, col0, row0);
+    } else if constexpr (EPI == kGateBack) {
+        float g[32], u[32], d[32];
+        load_kept(P, P.kept_g, P.scale_g, row, col0, g);
+        load_kept(P, P.kept_u, P.scale_u, row, col0, u);
+        load_acc(acc, d);
+        if (P.act == kGelu)
+            gate_back<kGelu>(g, u, d);
+        else
+            gate_back<kSilu>(g, u, d);
+        st.bf16(&P.d0, g, col0, row0);
+        st.bf16(&P.d1, u, col0, row0);
+        st.bf16(&P.d2, d, col0, row0);
+    } else {
+        float v[32];
+        load_acc(acc, v);
+        if (P.gain != nullptr) {
+            const int c = min(col0 + st.lane, P.n - 1);
+            const float f = P.gain_f32 ? ld1(static_cast<const float *>(P.gain) + c)
+                                       : ld1(static_cast<const __nv_bfloat16 *>(P.gain) + c);
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                v[j] *= __shfl_sync(0xFFFFFFFFu, f, j);
+        }
+        if (P.accumulate) {
+            const int64_t at = row * P.ld_old + col0;
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (col0 + j < P.n)
+                    v[j] += P.f32 ? ld1(static_cast<const float *>(P.old) + at + j)
+                                  : ld1(static_cast<const __nv_bfloat16 *>(P.old) + at + j);
+        }
+        if (P.f32)
+            st.f32(&P.d0, v, col0, row0);
+        else
+            st.bf16(&P.d0, v, col0, row0);
+    }
+}
+
+//   full[s]      (leader) both ranks' TMA bytes of stage s have landed
+//   empty[s]     (each)   the leader's MMAs have finished reading stage s
+//   acc_full[a]  (each)   accumulator a holds a finished tile
+//   acc_empty[a] (leader) all epilogue warps of the pair have read it
+template <int CG, int EPI>
+__global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
+    ffn_gemm_kernel(const __grid_constant__ Launch L)
+{
+    constexpr int T = kTile(CG);
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t bars[2 * kStages + 4];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int aborted;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? gemm::cluster_rank() : 0u;
+    const bool leader = rank == 0;
+    const int pair = blockIdx.x / CG, n_pairs = gridDim.x / CG;
+    const uint32_t raw = (uint32_t)__cvta_generic_to_shared(smem_raw);
+    const uint32_t ring = (raw + 1023u) & ~1023u;
+    const uint32_t sa = ring, sb = ring + kStages * kABytes;
+    const uint32_t bar0 = (uint32_t)__cvta_generic_to_shared(bars);
+    auto full = [&](int s) { return bar0 + 8u * (uint32_t)s; };
+    auto empty = [&](int s) { return bar0 + 8u * (uint32_t)(kStages + s); };
+    auto acc_full = [&](int a) { return bar0 + 8u * (uint32_t)(2 * kStages + a); };
+    auto acc_empty = [&](int a) { return bar0 + 8u * (uint32_t)(2 * kStages + 2 + a); };
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(acc_full(a), 1);
+            mbar_init(acc_empty(a), CG * kEpiWarps);
+        }
+        aborted = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1)
+        gemm::tmem_alloc<CG>((uint32_t)__cvta_generic_to_shared(&tmem_slot));
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    group_sync<CG>();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = tmem_slot;
+    const int n_tiles = L.n_tiles;
+    pdl_wait();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int it = 0;   // K blocks issued by this CTA
+            for (int t = pair; t < n_tiles && !*(volatile int *)&aborted; t += n_pairs) {
+                const Tile tile = tile_at(L, t);
+                const Product &P = L.p[tile.p];
+                const bool a_mn = P.a_mn, b_mn = P.b_mn;
+                const int ma = tile.m * T + (int)rank * BM;
+                // B rows of this CTA: T / CG of the tile's columns; kGate: a pair's CTAs
+                // hold one projection each, a single CTA half a box of either
+                const int nb = EPI == kGate ? tile.n * (T / 2) : tile.n * T + (int)rank * BH;
+                const int kb0 = P.k_blocks[0], kb_n = kb0 + P.k_blocks[1];
+                for (int kb = 0; kb < kb_n; ++kb, ++it) {
+                    const int s = it % kStages;
+                    const uint32_t ph = (uint32_t)(it / kStages) & 1u;
+                    if (!mbar_wait(empty(s), ph ^ 1u) || *(volatile int *)&aborted) {
+                        atomicOr(L.err, kErrWaitEmpty);
+                        aborted = 1;
+                        break;
+                    }
+                    const uint32_t fbar = CG == 2 ? map_to_rank(full(s), 0) : full(s);
+                    if (leader)
+                        mbar_arrive_expect_tx(full(s), (uint32_t)(CG * kStageBytes));
+                    const int seg = kb >= kb0, k = (kb - (seg ? kb0 : 0)) * BK;
+                    const CUtensorMap *ta = &P.a[seg];
+                    const CUtensorMap *tb = EPI == kGate ? &P.b[CG == 2 ? rank : 0] : &P.b[seg];
+#pragma unroll
+                    for (int h = 0; h < BK / kBoxK; ++h) {
+                        const int k0 = k + h * kBoxK;
+                        const uint32_t ah = sa + (uint32_t)(s * kABytes + h * (kABytes / 2));
+                        const uint32_t bh = sb + (uint32_t)(s * kBBytes + h * (kBBytes / 2));
+                        if (a_mn) {
+                            tma_load<CG>(ah, ta, ma, k0, fbar);
+                            tma_load<CG>(ah + kABytes / 4, ta, ma + 64, k0, fbar);
+                        } else {
+                            tma_load<CG>(ah, ta, k0, ma, fbar);
+                        }
+                        if (EPI == kGate && CG == 1) {   // 64 rows of each projection
+                            tma_load<CG>(bh, &P.b[0], k0, nb, fbar);
+                            tma_load<CG>(bh + kBBytes / 4, &P.b[1], k0, nb, fbar);
+                        } else if (b_mn) {
+                            tma_load<CG>(bh, tb, nb, k0, fbar);
+                            tma_load<CG>(bh + kBBytes / 4, tb, nb + 64, k0, fbar);
+                        } else {
+                            tma_load<CG>(bh, tb, k0, nb, fbar);
+                        }
+                    }
+                }
+            }
+            if (leader)   // no CTA leaves before the loads in flight have landed
+                for (int q = it - kStages < 0 ? 0 : it - kStages; q < it; ++q)
+                    if (!mbar_wait(full(q % kStages), (uint32_t)(q / kStages) & 1u))
+                        atomicOr(L.err, kErrDrain);
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && leader) {
+            int it = 0, lt = 0;
+            for (int t = pair; t < n_tiles && !*(volatile int *)&aborted; t += n_pairs, ++lt) {
+                const Product &P = L.p[tile_at(L, t).p];
+                const int kb_n = P.k_blocks[0] + P.k_blocks[1];
+                const bool a_mn = P.a_mn, b_mn = P.b_mn;
+                const uint32_t idesc = idesc_of(CG, a_mn, b_mn);
+                const int a = lt & 1;
+                const uint32_t aph = (uint32_t)(lt >> 1) & 1u;
+                if (!mbar_wait(acc_empty(a), aph ^ 1u)) {
+                    atomicOr(L.err, kErrWaitDone);
+                    aborted = 1;
+                    break;
+                }
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t d = tmem + (uint32_t)(a * T);
+                bool ok = true;
+                for (int kb = 0; kb < kb_n; ++kb, ++it) {
+                    const int s = it % kStages;
+                    const uint32_t ph = (uint32_t)(it / kStages) & 1u;
+                    if (!mbar_wait(full(s), ph) || *(volatile int *)&aborted) {
+                        atomicOr(L.err, kErrWaitFull);
+                        aborted = 1;
+                        ok = false;
+                        break;
+                    }
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                    for (int k = 0; k < BK / 16; ++k) {
+                        const int h = k / (kBoxK / 16), kk = k % (kBoxK / 16);
+                        const uint32_t ah = sa + (uint32_t)(s * kABytes + h * (kABytes / 2));
+                        const uint32_t bh = sb + (uint32_t)(s * kBBytes + h * (kBBytes / 2));
+                        const uint64_t ad = a_mn ? smem_desc_mn(ah + (uint32_t)(kk * 16 * 128))
+                                                 : smem_desc(ah + (uint32_t)(kk * 32));
+                        const uint64_t bd = b_mn ? smem_desc_mn(bh + (uint32_t)(kk * 16 * 128))
+                                                 : smem_desc(bh + (uint32_t)(kk * 32));
+                        mma_bf16<CG>(d, ad, bd, idesc, (kb | k) != 0 ? 1u : 0u);
+                    }
+                    mma_commit<CG>(empty(s));
+                }
+                mma_commit<CG>(acc_full(a));
+                if (!ok) {
+                    if (!mbar_wait(acc_full(a), aph))
+                        atomicOr(L.err, kErrDrain);
+                    break;
+                }
+            }
+        }
+    } else {
+        // Warp w reads TMEM lanes 32 (w % 4) .. +31, rows BM rank + 32 (w % 4) + lane of
+        // the tile, and the half of its columns that (w - 2) / 4 names.
+        const int q = warp & 3, half = (warp - 2) >> 2;
+        Stager st = {ring + (uint32_t)(kStages * kStageBytes + (warp - 2) * kStaging), lane, 0};
+        constexpr int kCols = EPI == kGate ? T / 2 : T;   // output columns of a tile
+        int lt = 0;
+        for (int t = pair; t < n_tiles; t += n_pairs, ++lt) {
+            const Tile tile = tile_at(L, t);
+            const Product &P = L.p[tile.p];
+            const int a = lt & 1;
+            bool seen = mbar_wait(acc_full(a), (uint32_t)(lt >> 1) & 1u);
+            if (!seen)
+                atomicOr(L.err, kErrWaitDone);
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            seen = __all_sync(0xFFFFFFFFu, seen && !*(volatile int *)&aborted);
+            if (!seen)
+                break;
+            const int row0 = tile.m * T + (int)rank * BM + q * 32;
+            const uint32_t acc =
+                tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * T + half * (kCols / 2));
+#pragma unroll 1
+            for (int ch = 0; ch < kCols / 64; ++ch)
+                drain<EPI>(P, st, acc + (uint32_t)(ch * 32), kCols, row0,
+                           tile.n * kCols + half * (kCols / 2) + ch * 32);
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive<CG>(acc_empty(a));
+        }
+        if (lane == 0)
+            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    }
+    __syncthreads();
+    if (CG == 2)
+        group_sync<CG>();
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        gemm::tmem_free<CG>(tmem);
+    }
+}
+
+}  // namespace ffn
+}  // namespace dpo

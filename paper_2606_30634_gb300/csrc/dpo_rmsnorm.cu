@@ -1,0 +1,903 @@
+// dpo_rmsnorm.cu -- residual addition with the root-mean-square norm, its
+// backward pass, and activations in 8 bits (dpo_rmsnorm, dpo_rmsnorm_backward,
+// dpo_pack8, dpo_unpack8 in include/dpo.h).
+//
+// All four move bytes: a few operations per element against 2 to 9 bytes of it,
+// so HBM bounds them, and launch latency where there are few rows.
+#include "dpo.h"
+#include "dpo_pack8.cuh"
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <math.h>
+
+namespace dpo {
+namespace {
+
+// ------------------------------------------------------------- vectors ----
+// V elements as one access of at most 16 bytes (codes: V bytes).
+
+template <int B> struct Bytes;
+template <> struct Bytes<1> {
+    static __device__ __forceinline__ void ld(const void *p, uint32_t (&w)[1])
+    {
+        uint16_t v;
+        asm volatile("ld.global.u8 %0, [%1];" : "=h"(v) : "l"(p));
+        w[0] = v;
+    }
+    static __device__ __forceinline__ void st(void *p, const uint32_t (&w)[1])
+    {
+        *static_cast<uint8_t *>(p) = (uint8_t)w[0];
+    }
+};
+template <> struct Bytes<2> {
+    static __device__ __forceinline__ void ld(const void *p, uint32_t (&w)[1])
+    {
+        uint16_t v;
+        asm volatile("ld.global.b16 %0, [%1];" : "=h"(v) : "l"(p));
+        w[0] = v;
+    }
+    static __device__ __forceinline__ void st(void *p, const uint32_t (&w)[1])
+    {
+        *static_cast<uint16_t *>(p) = (uint16_t)w[0];
+    }
+};
+template <> struct Bytes<4> {
+    static __device__ __forceinline__ void ld(const void *p, uint32_t (&w)[1])
+    {
+        asm volatile("ld.global.b32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+    }
+    static __device__ __forceinline__ void st(void *p, const uint32_t (&w)[1])
+    {
+        *static_cast<uint32_t *>(p) = w[0];
+    }
+};
+template <> struct Bytes<8> {
+    static __device__ __forceinline__ void ld(const void *p, uint32_t (&w)[2])
+    {
+        asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+    }
+    static __device__ __forceinline__ void st(void *p, const uint32_t (&w)[2])
+    {
+        *static_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+    }
+};
+template <> struct Bytes<16> {
+    static __device__ __forceinline__ void ld(const void *p, uint32_t (&w)[4])
+    {
+        asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                     : "l"(p));
+    }
+    static __device__ __forceinline__ void st(void *p, const uint32_t (&w)[4])
+    {
+        *static_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+
+__host__ __device__ constexpr int words(int bytes) { return bytes < 4 ? 1 : bytes / 4; }
+
+// V elements of T as loaded.
+template <class T, int V> struct Vec;
+template <int V> struct Vec<float, V> {
+    static constexpr int B = 4 * V;
+    uint32_t w[V];
+    __device__ __forceinline__ void load(const float *p) { Bytes<B>::ld(p, w); }
+    __device__ __forceinline__ float get(int i) const { return __uint_as_float(w[i]); }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            w[i] = 0u;
+    }
+    __device__ __forceinline__ void set(const float (&v)[V])
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            w[i] = __float_as_uint(v[i]);
+    }
+    __device__ __forceinline__ void store(float *p) const { Bytes<B>::st(p, w); }
+};
+template <int V> struct Vec<__nv_bfloat16, V> {
+    static constexpr int B = 2 * V;
+    uint32_t w[words(B)];
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { Bytes<B>::ld(p, w); }
+    __device__ __forceinline__ float get(int i) const
+    {
+        return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+    }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < words(B); ++i)
+            w[i] = 0u;
+    }
+    __device__ __forceinline__ void set(const float (&v)[V])
+    {
+        if (V == 1) {
+            w[0] = pack_bf16x2(v[0], 0.0f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i)
+                w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+        }
+    }
+    __device__ __forceinline__ void store(__nv_bfloat16 *p) const { Bytes<B>::st(p, w); }
+};
+
+// V codes.
+template <int V> struct Codes {
+    uint32_t w[words(V)];
+    __device__ __forceinline__ void load(const uint8_t *p) { Bytes<V>::ld(p, w); }
+    __device__ __forceinline__ void store(uint8_t *p) const { Bytes<V>::st(p, w); }
+    __device__ __forceinline__ void set(const float (&v)[V], float inv)
+    {
+        if constexpr (V == 1) {
+            w[0] = encode2(inf_to_nan(v[0]) * inv, 0.0f) & 0xFFu;
+        } else if constexpr (V == 2) {
+            w[0] = encode2(inf_to_nan(v[0]) * inv, inf_to_nan(v[1]) * inv);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V / 4; ++i)
+                w[i] = encode4(inf_to_nan(v[4 * i]) * inv, inf_to_nan(v[4 * i + 1]) * inv,
+                               inf_to_nan(v[4 * i + 2]) * inv, inf_to_nan(v[4 * i + 3]) * inv);
+        }
+    }
+    __device__ __forceinline__ void get(float (&v)[V], float scale) const
+    {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            const float2 f = decode2(w[i / 4] >> (8 * (i & 3)));
+            v[i] = f.x * scale;
+            if (i + 1 < V)
+                v[i + 1] = f.y * scale;
+        }
+    }
+};
+
+__device__ __forceinline__ float load_scale(const uint8_t *p)
+{
+    uint16_t v;
+    asm volatile("ld.global.u8 %0, [%1];" : "=h"(v) : "l"(p));
+    return scale_of(v);
+}
+
+// Largest finite magnitude of a group whose V-element pieces lie in adjacent lanes.
+template <int V>
+__device__ __forceinline__ float group_amax(const float (&v)[V])
+{
+    float a = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        a = fmaxf(a, finite_abs(v[i]));
+#pragma unroll
+    for (int off = 1; off < kGroup / V; off <<= 1)
+        a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, off));
+    return a;
+}
+
+__device__ __forceinline__ float warp_sum(float v)
+{
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1)
+        v += __shfl_xor_sync(0xFFFFFFFFu, v, off);
+    return v;
+}
+
+// ---------------------------------------------------------------- norm ----
+// A row is held in the registers of W warps, 32 elements a thread, so each
+// input is read once. Thread i of the row takes the V-element pieces i, i + 32 W, ...:
+// a group of 32 is in 32 / V adjacent lanes.
+
+constexpr int kRowElems = 32;                 // elements of a row per thread
+constexpr int kMinWarps = 4;                  // warps of a CTA, at least
+// Threads of a CTA, at most: rows of up to 8192 elements, and wider ones. The bound
+// sets the registers a thread may have.
+constexpr int kCta = 256, kWideCta = 512;
+
+struct NormForwardArgs {
+    dpo_rmsnorm_args a;
+    int warps;                                // per row, a power of two
+};
+
+// Sum over the threads of each row of a CTA (every warp calls it); red holds a
+// float per warp. The sum order is fixed.
+__device__ __forceinline__ float row_sum(float v, int warps, float *red)
+{
+    v = warp_sum(v);
+    if (warps == 1)
+        return v;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (lane == 0)
+        red[warp] = v;
+    __syncthreads();
+    const int first = warp & ~(warps - 1);
+    v = warp_sum(lane < warps ? red[first + lane] : 0.0f);
+    __syncthreads();
+    return v;
+}
+
+template <class T, class WT, int V, int TB>
+__global__ void __launch_bounds__(TB)
+rmsnorm_kernel(const NormForwardArgs args)
+{
+    constexpr int N = kRowElems / V;
+    __shared__ float red[32];
+    const dpo_rmsnorm_args &a = args.a;
+    const int warps = args.warps, tpr = warps * 32;
+    const int rows_cta = (int)blockDim.x / tpr;
+    const int i0 = threadIdx.x & (tpr - 1);
+    const int64_t row = (int64_t)blockIdx.x * rows_cta + threadIdx.x / tpr;
+    const bool live = row < a.rows;
+    const int cols = (int)a.cols;
+    pdl_wait();
+    float s[N][V];
+    float sum = 0.0f;
+    {
+        Vec<T, V> x[N], r[N];
+        const T *xp = static_cast<const T *>(a.x) + row * a.ld_x;
+        const T *rp = static_cast<const T *>(a.residual) + row * a.ld_residual;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int c = (i0 + n * tpr) * V;
+            x[n].zero();
+            r[n].zero();
+            if (live && c < cols) {
+                x[n].load(xp + c);
+                if (a.residual != nullptr)
+                    r[n].load(rp + c);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                s[n][j] = x[n].get(j) + r[n].get(j);
+                sum = fmaf(s[n][j], s[n][j], sum);
+            }
+    }
+    sum = row_sum(sum, warps, red);
+    const float rstd = 1.0f / sqrtf(sum / (float)cols + a.eps);
+    if (live && i0 == 0)
+        a.rstd[row] = rstd;
+    T *hp = static_cast<T *>(a.h) + row * a.ld_h;
+    T *yp = static_cast<T *>(a.y) + row * a.ld_y;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int c = (i0 + n * tpr) * V;
+        const bool in = live && c < cols;
+        Vec<T, V> o;
+        if (in && a.h != nullptr) {
+            o.set(s[n]);
+            o.store(hp + c);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            s[n][j] *= rstd;
+        if (in && a.y != nullptr) {
+            Vec<WT, V> w;
+            w.load(static_cast<const WT *>(a.weight) + c);
+            float y[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                y[j] = s[n][j] * w.get(j);
+            o.set(y);
+            o.store(yp + c);
+        }
+        if (a.x8.codes != nullptr) {   // uniform: every lane takes part in the shuffles
+            const uint32_t b = scale_byte(group_amax<V>(s[n]));
+            if (in) {
+                Codes<V> q;
+                q.set(s[n], inv_scale_of(b));
+                q.store(a.x8.codes + row * a.x8.ld_codes + c);
+                if (c % kGroup == 0)
+                    a.x8.scales[row * a.x8.ld_scales + c / kGroup] = (uint8_t)b;
+            }
+        }
+    }
+}
+
+// Backward: a persistent grid of CTAs walks the rows; a thread keeps the sums of
+// dy n of its columns in registers, so dweight costs one partial row per CTA,
+// which the second kernel adds up.
+struct NormBackArgs {
+    dpo_rmsnorm_backward_args a;
+    int warps;
+    float *partials;                          // one row of cols per CTA
+};
+
+template <class T, class WT, int V, int TB>
+__global__ void __launch_bounds__(TB)
+rmsnorm_backward_kernel(const NormBackArgs args)
+{
+    constexpr int N = kRowElems / V;
+    __shared__ float red[32];
+    extern __shared__ float dw_cta[];         // cols, with several rows per CTA
+    const dpo_rmsnorm_backward_args &a = args.a;
+    const int warps = args.warps, tpr = warps * 32;
+    const int rows_cta = (int)blockDim.x / tpr;
+    const int i0 = threadIdx.x & (tpr - 1), r0 = threadIdx.x / tpr;
+    const int cols = (int)a.cols;
+    pdl_wait();
+    float dw[N][V];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            dw[n][j] = 0.0f;
+    for (int64_t base = (int64_t)blockIdx.x * rows_cta; base < a.rows;
+         base += (int64_t)gridDim.x * rows_cta) {
+        const int64_t row = base + r0;
+        const bool live = row < a.rows;
+        const float rstd = live ? ld1(a.rstd + row) : 0.0f;
+        Vec<T, V> dy[N];
+        float nv[N][V];
+        const T *dyp = static_cast<const T *>(a.dy) + row * a.ld_dy;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int c = (i0 + n * tpr) * V;
+            dy[n].zero();
+            if (live && c < cols)
+                dy[n].load(dyp + c);
+        }
+        if (a.h != nullptr) {
+            const T *hp = static_cast<const T *>(a.h) + row * a.ld_h;
+            Vec<T, V> h[N];
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int c = (i0 + n * tpr) * V;
+                h[n].zero();
+                if (live && c < cols)
+                    h[n].load(hp + c);
+            }
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    nv[n][j] = h[n].get(j) * rstd;
+        } else {
+            Codes<V> q[N];
+            float sc[N];
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int c = (i0 + n * tpr) * V;
+#pragma unroll
+                for (int j = 0; j < words(V); ++j)
+                    q[n].w[j] = 0u;
+                sc[n] = 0.0f;
+                if (live && c < cols) {
+                    q[n].load(a.x8.codes + row * a.x8.ld_codes + c);
+                    sc[n] = load_scale(a.x8.scales + row * a.x8.ld_scales + c / kGroup);
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+                q[n].get(nv[n], sc[n]);
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int c = (i0 + n * tpr) * V;
+            if (c < cols) {
+                Vec<WT, V> w;
+                w.load(static_cast<const WT *>(a.weight) + c);
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    sum = fmaf(dy[n].get(j) * w.get(j), nv[n][j], sum);
+            }
+        }
+        sum = row_sum(sum, warps, red) / (float)cols;
+        T *dxp = static_cast<T *>(a.dx) + row * a.ld_dx;
+        const T *dhp = static_cast<const T *>(a.dh) + row * a.ld_dh;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int c = (i0 + n * tpr) * V;
+            if (live && c < cols) {
+                if (a.dx != nullptr) {
+                    Vec<WT, V> w;
+                    Vec<T, V> dh, o;
+                    dh.zero();
+                    w.load(static_cast<const WT *>(a.weight) + c);
+                    if (a.dh != nullptr)
+                        dh.load(dhp + c);
+                    float v[V];
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        v[j] = fmaf(rstd, dy[n].get(j) * w.get(j) - nv[n][j] * sum, dh.get(j));
+                    o.set(v);
+                    o.store(dxp + c);
+                }
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    dw[n][j] = fmaf(dy[n].get(j), nv[n][j], dw[n][j]);
+            }
+        }
+    }
+    if (a.dweight == nullptr)
+        return;
+    float *out = args.partials + (int64_t)blockIdx.x * cols;
+    if (rows_cta > 1) {   // the CTA's rows, in order
+        for (int r = 0; r < rows_cta; ++r) {
+            if (r0 == r)
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    const int c = (i0 + n * tpr) * V;
+                    if (c < cols)
+#pragma unroll
+                        for (int j = 0; j < V; ++j) {
+                            if (r > 0)
+                                dw[n][j] = dw_cta[c + j] + dw[n][j];
+                            dw_cta[c + j] = dw[n][j];
+                        }
+                }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < cols; c += blockDim.x)
+            out[c] = dw_cta[c];
+        return;
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int c = (i0 + n * tpr) * V;
+        if (c < cols)
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                out[c + j] = dw[n][j];
+    }
+}
+
+// dweight[c] = the sum of the n partial rows, in a fixed order: 32 columns per
+// CTA, 16 interleaved shares of the rows, added up in order.
+constexpr int kSumShares = 16;
+template <class GT>
+__global__ void __launch_bounds__(32 * kSumShares)
+rmsnorm_dweight_kernel(const float *partials, int n, int cols, GT *dweight, int accumulate)
+{
+    __shared__ float share[kSumShares][33];
+    const int lane = threadIdx.x & 31, k = threadIdx.x >> 5;
+    const int c = blockIdx.x * 32 + lane;
+    pdl_wait();
+    float sum = 0.0f;
+    if (c < cols)
+        for (int i = k; i < n; i += kSumShares)
+            sum += ld1(partials + (int64_t)i * cols + c);
+    share[k][lane] = sum;
+    __syncthreads();
+    if (k != 0 || c >= cols)
+        return;
+    sum = share[0][lane];
+#pragma unroll
+    for (int i = 1; i < kSumShares; ++i)
+        sum += share[i][lane];
+    if (accumulate)
+        sum += ld1(dweight + c);
+    st1(dweight + c, sum);
+}
+
+// ---------------------------------------------------------------- pack ----
+// A warp takes spans of kSpan elements of a row, V a lane at a time.
+
+constexpr int kSpan = 1024;
+constexpr int kPackThreads = 256;
+
+struct PackArgs {
+    const void *x;                            // pack: in; unpack: out
+    uint8_t *codes, *scales;
+    int64_t ld_x, ld_codes, ld_scales;
+    int64_t cols, spans, items;               // spans per row, rows * spans
+};
+
+template <class T, int V, bool Unpack>
+__global__ void __launch_bounds__(kPackThreads)
+pack8_kernel(const PackArgs a)
+{
+    constexpr int N = kSpan / 32 / V;
+    const int lane = threadIdx.x & 31;
+    const int64_t first = (int64_t)blockIdx.x * (kPackThreads / 32) + (threadIdx.x >> 5);
+    const int64_t step = (int64_t)gridDim.x * (kPackThreads / 32);
+    pdl_wait();
+    for (int64_t item = first; item < a.items; item += step) {
+        const int64_t row = item / a.spans, c0 = (item - row * a.spans) * kSpan;
+        T *const xp = const_cast<T *>(static_cast<const T *>(a.x)) + row * a.ld_x;
+        uint8_t *const qp = a.codes + row * a.ld_codes;
+        uint8_t *const sp = a.scales + row * a.ld_scales;
+        if (Unpack) {
+            Codes<V> q[N];
+            float sc[N];
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int64_t c = c0 + (lane + n * 32) * V;
+                if (c < a.cols) {
+                    q[n].load(qp + c);
+                    sc[n] = load_scale(sp + c / kGroup);
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int64_t c = c0 + (lane + n * 32) * V;
+                if (c < a.cols) {
+                    float v[V];
+                    q[n].get(v, sc[n]);
+                    Vec<T, V> o;
+                    o.set(v);
+                    o.store(xp + c);
+                }
+            }
+        } else {
+            Vec<T, V> x[N];
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int64_t c = c0 + (lane + n * 32) * V;
+                x[n].zero();
+                if (c < a.cols)
+                    x[n].load(xp + c);
+            }
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int64_t c = c0 + (lane + n * 32) * V;
+                float v[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    v[j] = x[n].get(j);
+                const uint32_t b = scale_byte(group_amax<V>(v));
+                if (c < a.cols) {
+                    Codes<V> q;
+                    q.set(v, inv_scale_of(b));
+                    q.store(qp + c);
+                    if (c % kGroup == 0)
+                        sp[c / kGroup] = (uint8_t)b;
+                }
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- host ----
+
+int64_t elem_size(int dt) { return dt == DPO_BF16 ? 2 : 4; }
+bool known(int dt) { return dt == DPO_F32 || dt == DPO_BF16; }
+
+// Whether a matrix can be accessed V elements of `size` bytes at a time.
+bool whole(const void *p, int64_t ld, int64_t size, int v)
+{
+    return p == nullptr || (reinterpret_cast<uintptr_t>(p) % (size * v) == 0 && ld % v == 0);
+}
+
+bool aligned_to(const void *p, int64_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+int sm_count()
+{
+    int device = 0, sms = 0;
+    if (cudaGetDevice(&device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)
+        return 0;
+    return sms;
+}
+
+int row_warps(int64_t cols)
+{
+    int w = 1;
+    while ((int64_t)w * 32 * kRowElems < cols)
+        w *= 2;
+    return w;
+}
+
+// CTAs of the backward's persistent grid, for row counts that fill it.
+int64_t backward_ctas(int64_t rows, int64_t cols, int sms)
+{
+    const int warps = row_warps(cols), cta = warps > kMinWarps ? warps : kMinWarps;
+    const int64_t want = (rows + cta / warps - 1) / (cta / warps);
+    const int64_t most = (int64_t)sms * (cta <= 4 ? 4 : cta <= 8 ? 2 : 1);
+    return want < most ? want : most;
+}
+
+struct Span {
+    uintptr_t lo, hi;
+};
+Span span_of(const void *p, int64_t rows, int64_t cols, int64_t ld, int64_t size)
+{
+    const uintptr_t b = reinterpret_cast<uintptr_t>(p);
+    if (p == nullptr || rows <= 0 || cols <= 0)
+        return {0, 0};
+    return {b, b + (uintptr_t)(((rows - 1) * ld + cols) * size)};
+}
+bool meet(Span a, Span b) { return a.lo < b.hi && b.lo < a.hi; }
+
+template <class... P, class... A>
+int launch(const char *what, void (*kernel)(P...), int64_t grid, int threads, size_t smem,
+           void *stream, A &&...args)
+{
+    const cudaError_t e = launch_pdl(kernel, dim3((unsigned)grid), threads, smem,
+                                     static_cast<cudaStream_t>(stream), static_cast<A &&>(args)...);
+    return e == cudaSuccess ? DPO_OK : call_fail(DPO_ECUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+
+int check_packed(const char *what, const dpo_packed8 &p, int64_t cols)
+{
+    if (p.codes == nullptr || p.scales == nullptr)
+        return call_fail(DPO_EINVAL, "%s: codes and scales are needed", what);
+    if (p.ld_codes < cols || p.ld_scales < groups_of(cols))
+        return call_fail(DPO_EINVAL, "%s: a pitch of the 8-bit matrix is below its row", what);
+    return DPO_OK;
+}
+
+constexpr int64_t kMaxRows = (int64_t)1 << 31;
+
+int check_matrix(const char *what, const char *name, const void *p, int64_t cols, int64_t ld,
+                 int64_t size)
+{
+    if (p == nullptr)
+        return call_fail(DPO_EINVAL, "%s: %s is NULL", what, name);
+    if (ld < cols)
+        return call_fail(DPO_EINVAL, "%s: pitch %lld of %s is below its %lld columns", what,
+                         (long long)ld, name, (long long)cols);
+    if (!aligned_to(p, size))
+        return call_fail(DPO_EALIGN, "%s: %s is not aligned to its elements", what, name);
+    return DPO_OK;
+}
+
+template <class T, bool Unpack>
+auto pack_kernel(int v) -> void (*)(PackArgs)
+{
+    if (sizeof(T) == 2 && v == 8)
+        return pack8_kernel<T, sizeof(T) == 2 ? 8 : 4, Unpack>;
+    if (sizeof(T) == 4 && v >= 4)
+        return pack8_kernel<T, 4, Unpack>;
+    if (sizeof(T) == 2 && v == 2)
+        return pack8_kernel<T, sizeof(T) == 2 ? 2 : 1, Unpack>;
+    return pack8_kernel<T, 1, Unpack>;
+}
+
+int pack_or_unpack(const char *what, const void *x, dpo_dtype dtype, int64_t rows, int64_t cols,
+                   int64_t ld_x, const dpo_packed8 *p, bool unpack, void *stream)
+{
+    if (!known(dtype))
+        return call_fail(DPO_EDTYPE, "%s: dtype %d", what, (int)dtype);
+    if (rows < 0 || cols < 0 || rows >= kMaxRows || cols >= kMaxRows)
+        return call_fail(DPO_EINVAL, "%s: %lld x %lld", what, (long long)rows, (long long)cols);
+    if (p == nullptr)
+        return call_fail(DPO_EINVAL, "%s: no 8-bit matrix", what);
+    if (rows == 0 || cols == 0)
+        return DPO_OK;
+    const int64_t size = elem_size(dtype);
+    int rc = check_matrix(what, unpack ? "out" : "x", x, cols, ld_x, size);
+    if (rc == DPO_OK)
+        rc = check_packed(what, *p, cols);
+    if (rc != DPO_OK)
+        return rc;
+    const Span sx = span_of(x, rows, cols, ld_x, size),
+               sc = span_of(p->codes, rows, cols, p->ld_codes, 1),
+               ss = span_of(p->scales, rows, groups_of(cols), p->ld_scales, 1);
+    if (meet(sx, sc) || meet(sx, ss) || (!unpack && meet(sc, ss)))
+        return call_fail(DPO_EINVAL, "%s: buffers overlap", what);
+    const int sms = sm_count();
+    if (sms == 0)
+        return call_fail(DPO_ECUDA, "%s: no device", what);
+    int v = dtype == DPO_BF16 ? 8 : 4;
+    while (v > 1 && !(cols % v == 0 && whole(x, ld_x, size, v) && whole(p->codes, p->ld_codes, 1, v)))
+        v = v == 8 ? 2 : 1;
+    PackArgs a = {x, p->codes, p->scales, ld_x, p->ld_codes, p->ld_scales, cols, 0, 0};
+    a.spans = (cols + kSpan - 1) / kSpan;
+    a.items = rows * a.spans;
+    const int64_t want = (a.items + kPackThreads / 32 - 1) / (kPackThreads / 32);
+    const int64_t grid = want < (int64_t)sms * 8 ? want : (int64_t)sms * 8;
+    void (*k)(PackArgs);
+    if (dtype == DPO_BF16)
+        k = unpack ? pack_kernel<__nv_bfloat16, true>(v) : pack_kernel<__nv_bfloat16, false>(v);
+    else
+        k = unpack ? pack_kernel<float, true>(v) : pack_kernel<float, false>(v);
+    return launch(what, k, grid, kPackThreads, 0, stream, a);
+}
+
+// The instance for these types, V elements an access and CTA size.
+template <template <class, class, int, int> class K, int TB>
+auto pick_vec(int dtype, int wdtype, int v)
+{
+    using B = __nv_bfloat16;
+    if (dtype == DPO_F32)
+        return v >= 4 ? K<float, float, 4, TB>::fn() : K<float, float, 1, TB>::fn();
+    if (wdtype == DPO_F32)
+        return v == 8 ? K<B, float, 4, TB>::fn()
+                      : v >= 2 ? K<B, float, 2, TB>::fn() : K<B, float, 1, TB>::fn();
+    return v == 8 ? K<B, B, 8, TB>::fn() : v >= 2 ? K<B, B, 2, TB>::fn() : K<B, B, 1, TB>::fn();
+}
+template <template <class, class, int, int> class K>
+auto pick(int dtype, int wdtype, int v, int threads)
+{
+    return threads <= kCta ? pick_vec<K, kCta>(dtype, wdtype, v)
+                           : pick_vec<K, kWideCta>(dtype, wdtype, v);
+}
+template <class T, class WT, int V, int TB> struct Fwd {
+    static auto fn() { return &rmsnorm_kernel<T, WT, V, TB>; }
+};
+template <class T, class WT, int V, int TB> struct Back {
+    static auto fn() { return &rmsnorm_backward_kernel<T, WT, V, TB>; }
+};
+
+int check_norm(const char *what, int64_t rows, int64_t cols, int dtype, int wdtype,
+               const void *weight)
+{
+    if (!known(dtype) || (wdtype != dtype && wdtype != DPO_F32))
+        return call_fail(DPO_EDTYPE, "%s: dtype %d, weight dtype %d", what, dtype, wdtype);
+    if (rows < 0 || rows >= kMaxRows || cols < 1 || cols > DPO_RMSNORM_MAX_COLS)
+        return call_fail(DPO_EINVAL, "%s: %lld x %lld", what, (long long)rows, (long long)cols);
+    return check_matrix(what, "weight", weight, cols, cols, elem_size(wdtype));
+}
+
+}  // namespace
+}  // namespace dpo
+
+using namespace dpo;
+
+extern "C" int dpo_pack8(const void *x, dpo_dtype dtype, int64_t rows, int64_t cols, int64_t ld_x,
+                         const dpo_packed8 *out, void *cuda_stream)
+{
+    return pack_or_unpack("dpo_pack8", x, dtype, rows, cols, ld_x, out, false, cuda_stream);
+}
+
+extern "C" int dpo_unpack8(const dpo_packed8 *in, int64_t rows, int64_t cols, void *out,
+                           dpo_dtype dtype, int64_t ld_out, void *cuda_stream)
+{
+    return pack_or_unpack("dpo_unpack8", out, dtype, rows, cols, ld_out, in, true, cuda_stream);
+}
+
+extern "C" int dpo_rmsnorm(const dpo_rmsnorm_args *args, void *cuda_stream)
+{
+    const char *what = "dpo_rmsnorm";
+    if (args == nullptr)
+        return call_fail(DPO_EINVAL, "%s: no arguments", what);
+    const dpo_rmsnorm_args &a = *args;
+    int rc = check_norm(what, a.rows, a.cols, a.dtype, a.weight_dtype, a.weight);
+    if (rc != DPO_OK)
+        return rc;
+    if (!(a.eps >= 0.0f) || !isfinite(a.eps))
+        return call_fail(DPO_EINVAL, "%s: eps", what);
+    if (a.rows == 0)
+        return DPO_OK;
+    const int64_t size = elem_size(a.dtype);
+    const struct { const char *name; const void *p; int64_t ld; bool needed; } mats[] = {
+        {"x", a.x, a.ld_x, true}, {"residual", a.residual, a.ld_residual, false},
+        {"h", a.h, a.ld_h, false}, {"y", a.y, a.ld_y, false}};
+    for (const auto &m : mats)
+        if ((m.needed || m.p != nullptr) &&
+            (rc = check_matrix(what, m.name, m.p, a.cols, m.ld, size)) != DPO_OK)
+            return rc;
+    if ((rc = check_matrix(what, "rstd", a.rstd, 1, 1, 4)) != DPO_OK)
+        return rc;
+    if (a.x8.codes != nullptr && (rc = check_packed(what, a.x8, a.cols)) != DPO_OK)
+        return rc;
+    const int64_t ng = groups_of(a.cols);
+    const Span in[] = {span_of(a.x, a.rows, a.cols, a.ld_x, size),
+                       span_of(a.residual, a.rows, a.cols, a.ld_residual, size),
+                       span_of(a.weight, 1, a.cols, a.cols, elem_size(a.weight_dtype))};
+    const Span out[] = {span_of(a.h, a.rows, a.cols, a.ld_h, size),
+                        span_of(a.y, a.rows, a.cols, a.ld_y, size),
+                        span_of(a.rstd, 1, a.rows, a.rows, 4),
+                        span_of(a.x8.codes, a.rows, a.cols, a.x8.ld_codes, 1),
+                        span_of(a.x8.codes ? a.x8.scales : nullptr, a.rows, ng, a.x8.ld_scales, 1)};
+    for (int i = 0; i < 5; ++i) {
+        for (const Span &s : in)
+            if (meet(out[i], s))
+                return call_fail(DPO_EINVAL, "%s: an output overlaps an input", what);
+        for (int j = 0; j < i; ++j)
+            if (meet(out[i], out[j]))
+                return call_fail(DPO_EINVAL, "%s: outputs overlap", what);
+    }
+    int v = a.dtype == DPO_BF16 ? 8 : 4;
+    while (v > 1 &&
+           !(a.cols % v == 0 && whole(a.x, a.ld_x, size, v) && whole(a.residual, a.ld_residual, size, v) &&
+             whole(a.h, a.ld_h, size, v) && whole(a.y, a.ld_y, size, v) &&
+             aligned_to(a.weight, a.weight_dtype == DPO_F32 ? (v == 2 ? 8 : 16) : 2 * v) &&
+             whole(a.x8.codes, a.x8.ld_codes, 1, v)))
+        v = v == 8 ? 2 : 1;
+    const NormForwardArgs k = {a, row_warps(a.cols)};
+    const int cta = k.warps > kMinWarps ? k.warps : kMinWarps;
+    const int64_t grid = (a.rows + cta / k.warps - 1) / (cta / k.warps);
+    return launch(what, pick<Fwd>(a.dtype, a.weight_dtype, v, cta * 32), grid, cta * 32, 0,
+                  cuda_stream, k);
+}
+
+extern "C" int dpo_rmsnorm_workspace(int64_t rows, int64_t cols, int64_t *bytes)
+{
+    const char *what = "dpo_rmsnorm_workspace";
+    if (bytes == nullptr || rows < 0 || rows >= kMaxRows || cols < 1 || cols > DPO_RMSNORM_MAX_COLS)
+        return call_fail(DPO_EINVAL, "%s: %lld x %lld", what, (long long)rows, (long long)cols);
+    const int sms = sm_count();
+    if (sms == 0)
+        return call_fail(DPO_ECUDA, "%s: no device", what);
+    *bytes = backward_ctas(rows, cols, sms) * cols * 4;
+    return DPO_OK;
+}
+
+extern "C" int dpo_rmsnorm_backward(const dpo_rmsnorm_backward_args *args, void *cuda_stream)
+{
+    const char *what = "dpo_rmsnorm_backward";
+    if (args == nullptr)
+        return call_fail(DPO_EINVAL, "%s: no arguments", what);
+    const dpo_rmsnorm_backward_args &a = *args;
+    int rc = check_norm(what, a.rows, a.cols, a.dtype, a.weight_dtype, a.weight);
+    if (rc != DPO_OK)
+        return rc;
+    if (a.dweight != nullptr) {
+        if (!known(a.dweight_dtype))
+            return call_fail(DPO_EDTYPE, "%s: dweight dtype %d", what, a.dweight_dtype);
+        if (!aligned_to(a.dweight, elem_size(a.dweight_dtype)))
+            return call_fail(DPO_EALIGN, "%s: dweight", what);
+    }
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (a.rows == 0) {
+        if (a.dweight == nullptr || a.accumulate)
+            return DPO_OK;
+        const cudaError_t e =
+            cudaMemsetAsync(a.dweight, 0, (size_t)(a.cols * elem_size(a.dweight_dtype)), stream);
+        return e == cudaSuccess ? DPO_OK : call_fail(DPO_ECUDA, "%s: %s", what, cudaGetErrorString(e));
+    }
+    if (a.dx == nullptr && a.dweight == nullptr)
+        return DPO_OK;
+    const int64_t size = elem_size(a.dtype);
+    const struct { const char *name; const void *p; int64_t ld; bool needed; } mats[] = {
+        {"dy", a.dy, a.ld_dy, true}, {"h", a.h, a.ld_h, false},
+        {"dh", a.dh, a.ld_dh, false}, {"dx", a.dx, a.ld_dx, false}};
+    for (const auto &m : mats)
+        if ((m.needed || m.p != nullptr) &&
+            (rc = check_matrix(what, m.name, m.p, a.cols, m.ld, size)) != DPO_OK)
+            return rc;
+    if ((rc = check_matrix(what, "rstd", a.rstd, 1, 1, 4)) != DPO_OK)
+        return rc;
+    if (a.h == nullptr && (rc = check_packed(what, a.x8, a.cols)) != DPO_OK)
+        return rc;
+    const int sms = sm_count();
+    if (sms == 0)
+        return call_fail(DPO_ECUDA, "%s: no device", what);
+    const int64_t grid = backward_ctas(a.rows, a.cols, sms);
+    if (a.dweight != nullptr) {
+        if (a.workspace == nullptr || a.workspace_bytes < grid * a.cols * 4)
+            return call_fail(DPO_EINVAL, "%s: workspace of %lld bytes, %lld needed", what,
+                             (long long)a.workspace_bytes, (long long)(grid * a.cols * 4));
+        if (!aligned_to(a.workspace, 16))
+            return call_fail(DPO_EALIGN, "%s: workspace", what);
+    }
+    const uint8_t *codes = a.h == nullptr ? a.x8.codes : nullptr;
+    const Span in[] = {span_of(a.dy, a.rows, a.cols, a.ld_dy, size),
+                       span_of(a.h, a.rows, a.cols, a.ld_h, size),
+                       span_of(a.dh, a.rows, a.cols, a.ld_dh, size),
+                       span_of(a.rstd, 1, a.rows, a.rows, 4),
+                       span_of(a.weight, 1, a.cols, a.cols, elem_size(a.weight_dtype)),
+                       span_of(codes, a.rows, a.cols, a.x8.ld_codes, 1),
+                       span_of(codes ? a.x8.scales : nullptr, a.rows, groups_of(a.cols),
+                               a.x8.ld_scales, 1)};
+    const Span out[] = {span_of(a.dx, a.rows, a.cols, a.ld_dx, size),
+                        span_of(a.dweight, 1, a.cols, a.cols, elem_size(a.dweight_dtype)),
+                        span_of(a.dweight ? a.workspace : nullptr, 1, grid * a.cols, grid * a.cols, 4)};
+    for (int i = 0; i < 3; ++i) {
+        for (const Span &s : in)
+            if (meet(out[i], s))
+                return call_fail(DPO_EINVAL, "%s: an output overlaps an input", what);
+        for (int j = 0; j < i; ++j)
+            if (meet(out[i], out[j]))
+                return call_fail(DPO_EINVAL, "%s: outputs overlap", what);
+    }
+    int v = a.dtype == DPO_BF16 ? 8 : 4;
+    while (v > 1 &&
+           !(a.cols % v == 0 && whole(a.dy, a.ld_dy, size, v) && whole(a.h, a.ld_h, size, v) &&
+             whole(a.dh, a.ld_dh, size, v) && whole(a.dx, a.ld_dx, size, v) &&
+             aligned_to(a.weight, a.weight_dtype == DPO_F32 ? (v == 2 ? 8 : 16) : 2 * v) &&
+             whole(codes, a.x8.ld_codes, 1, v)))
+        v = v == 8 ? 2 : 1;
+    const NormBackArgs k = {a, row_warps(a.cols), static_cast<float *>(a.workspace)};
+    const int cta = k.warps > kMinWarps ? k.warps : kMinWarps;
+    const size_t smem = cta > k.warps ? (size_t)a.cols * 4 : 0;
+    rc = launch(what, pick<Back>(a.dtype, a.weight_dtype, v, cta * 32), grid, cta * 32,
+                smem, cuda_stream, k);
+    if (rc != DPO_OK || a.dweight == nullptr)
+        return rc;
+    const int64_t sum_grid = (a.cols + 31) / 32;
+    if (a.dweight_dtype == DPO_F32)
+        return launch(what, rmsnorm_dweight_kernel<float>, sum_grid, 32 * kSumShares, 0, cuda_stream,
+                      static_cast<const float *>(k.partials), (int)grid, (int)a.cols,
+                      static_cast<float *>(a.dweight), a.accumulate);
+    return launch(what, rmsnorm_dweight_kernel<__nv_bfloat16>, sum_grid, 32 * kSumShares, 0,
+                  cuda_stream, static_cast<const float *>(k.partials), (int)grid, (int)a.cols,
+                  static_cast<__nv_bfloat16 *>(a.dweight), a.accumulate);
+}

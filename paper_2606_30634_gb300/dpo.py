@@ -29,13 +29,20 @@ DPO_FLAG_NONFINITE = 1
 DPO_CORR_EF, DPO_CORR_SAPIPE_SAME, DPO_CORR_SAPIPE_UPDATED = 0, 1, 2
 DPO_OPT_ADAMW, DPO_OPT_NADAM, DPO_OPT_LION, DPO_OPT_ADAN = 0, 1, 2, 3
 DPO_STASH_COPY, DPO_STASH_PINGPONG = 0, 1
+DPO_ACT_SILU, DPO_ACT_GELU = 0, 1
+DPO_KEEP_NONE, DPO_KEEP_8BIT, DPO_KEEP_BF16 = 0, 1, 2
+DPO_PACK8_GROUP = 32
+DPO_RMSNORM_MAX_COLS = 16384
 
 EXPORTS = ("dpo_init", "dpo_stash", "dpo_step", "dpo_read_weights", "dpo_get_step",
            "dpo_set_step", "dpo_get_flags", "dpo_algorithmic_bytes", "dpo_launch_config",
            "dpo_last_error", "dpo_destroy", "dpo_grad_norm_noalloc", "dpo_set_delay",
            "dpo_grad_sqnorm", "dpo_set_clip_source", "dpo_test_fail_allocs",
            "dpo_get_phase_start", "dpo_set_phase_start", "dpo_set_capturable",
-           "dpo_set_timing", "dpo_get_timing")
+           "dpo_set_timing", "dpo_get_timing", "dpo_pack8", "dpo_unpack8", "dpo_rmsnorm",
+           "dpo_rmsnorm_backward", "dpo_rmsnorm_workspace", "dpo_ffn_forward",
+           "dpo_ffn_backward", "dpo_ffn_workspace", "dpo_ffn_get_status",
+           "dpo_ffn_clear_status")
 
 DPO_NOALLOC_CHUNK_ELEMS = 1 << 20
 DPO_NOALLOC_MAX_CHUNKS = 16384
@@ -62,6 +69,45 @@ class dpo_tensor(ctypes.Structure):
                 ("v", ctypes.c_void_p), ("stash", ctypes.c_void_p), ("ef", ctypes.c_void_p),
                 ("grad", ctypes.c_void_p), ("n", ctypes.c_void_p), ("grad_prev", ctypes.c_void_p),
                 ("numel", ctypes.c_int64), ("flags", ctypes.c_uint32)]
+
+
+_P, _L, _I, _F = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_float
+
+
+class dpo_packed8(ctypes.Structure):
+    _fields_ = [("codes", _P), ("scales", _P), ("ld_codes", _L), ("ld_scales", _L)]
+
+
+class dpo_rmsnorm_args(ctypes.Structure):
+    _fields_ = [("x", _P), ("residual", _P), ("weight", _P), ("h", _P), ("y", _P), ("rstd", _P),
+                ("x8", dpo_packed8), ("rows", _L), ("cols", _L), ("ld_x", _L),
+                ("ld_residual", _L), ("ld_h", _L), ("ld_y", _L), ("eps", _F), ("dtype", _I),
+                ("weight_dtype", _I)]
+
+
+class dpo_rmsnorm_backward_args(ctypes.Structure):
+    _fields_ = [("dy", _P), ("h", _P), ("x8", dpo_packed8), ("rstd", _P), ("weight", _P),
+                ("dh", _P), ("dx", _P), ("dweight", _P), ("rows", _L), ("cols", _L),
+                ("ld_dy", _L), ("ld_h", _L), ("ld_dh", _L), ("ld_dx", _L), ("dtype", _I),
+                ("weight_dtype", _I), ("dweight_dtype", _I), ("accumulate", _I),
+                ("workspace", _P), ("workspace_bytes", _L)]
+
+
+class dpo_ffn_args(ctypes.Structure):
+    _fields_ = [("x", _P), ("w_gate", _P), ("w_up", _P), ("w_down", _P), ("out", _P),
+                ("gate", _P), ("up", _P), ("gate8", dpo_packed8), ("up8", dpo_packed8),
+                ("tokens", _L), ("dim", _L), ("hidden", _L), ("ld_x", _L), ("ld_out", _L),
+                ("act", _I), ("keep", _I), ("workspace", _P), ("workspace_bytes", _L)]
+
+
+class dpo_ffn_backward_args(ctypes.Structure):
+    _fields_ = [("dout", _P), ("x", _P), ("x8", dpo_packed8), ("gain", _P), ("w_gate", _P),
+                ("w_up", _P), ("w_down", _P), ("gate", _P), ("up", _P), ("gate8", dpo_packed8),
+                ("up8", dpo_packed8), ("dx", _P), ("dw_gate", _P), ("dw_up", _P),
+                ("dw_down", _P), ("tokens", _L), ("dim", _L), ("hidden", _L), ("ld_dout", _L),
+                ("ld_x", _L), ("ld_dx", _L), ("act", _I), ("keep", _I), ("grad_dtype", _I),
+                ("gain_dtype", _I), ("accumulate", _I), ("workspace", _P),
+                ("workspace_bytes", _L)]
 
 
 _lib = None
@@ -109,6 +155,16 @@ def load() -> ctypes.CDLL:
         "dpo_set_timing": (I, [P, I]),
         "dpo_get_timing": (I, [P, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double),
                                ctypes.POINTER(ctypes.c_int64)]),
+        "dpo_pack8": (I, [P, I, _L, _L, _L, P, P]),
+        "dpo_unpack8": (I, [P, _L, _L, P, I, _L, P]),
+        "dpo_rmsnorm": (I, [P, P]),
+        "dpo_rmsnorm_backward": (I, [P, P]),
+        "dpo_rmsnorm_workspace": (I, [_L, _L, P]),
+        "dpo_ffn_forward": (I, [P, P]),
+        "dpo_ffn_backward": (I, [P, P]),
+        "dpo_ffn_workspace": (I, [_L, _L, _L, I, P, P]),
+        "dpo_ffn_get_status": (I, [P]),
+        "dpo_ffn_clear_status": (I, [P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -293,6 +349,62 @@ def dpo_grad_norm_noalloc(grad, numel: int, grad_dtype: int, max_grad_norm: floa
                                       ptr(norm_out), ptr(clip_out), _stream(stream))
     if rc != DPO_OK:
         raise DpoError(rc, "dpo_grad_norm_noalloc rejected its arguments or failed")
+
+
+# ------------------------------------- the feed-forward half of a stage --
+# Argument structures as in include/dpo.h; ``ffn`` fills them from tensors.
+
+def dpo_pack8(x, dtype: int, rows: int, cols: int, ld_x: int, out: dpo_packed8,
+              stream=None) -> None:
+    _check(load().dpo_pack8(_dptr(x), dtype, rows, cols, ld_x, ctypes.byref(out),
+                            _stream(stream)), None)
+
+
+def dpo_unpack8(packed: dpo_packed8, rows: int, cols: int, out, dtype: int, ld_out: int,
+                stream=None) -> None:
+    _check(load().dpo_unpack8(ctypes.byref(packed), rows, cols, _dptr(out), dtype, ld_out,
+                              _stream(stream)), None)
+
+
+def dpo_rmsnorm(args: dpo_rmsnorm_args, stream=None) -> None:
+    _check(load().dpo_rmsnorm(ctypes.byref(args), _stream(stream)), None)
+
+
+def dpo_rmsnorm_backward(args: dpo_rmsnorm_backward_args, stream=None) -> None:
+    _check(load().dpo_rmsnorm_backward(ctypes.byref(args), _stream(stream)), None)
+
+
+def dpo_rmsnorm_workspace(rows: int, cols: int) -> int:
+    n = ctypes.c_int64()
+    _check(load().dpo_rmsnorm_workspace(rows, cols, ctypes.byref(n)), None)
+    return n.value
+
+
+def dpo_ffn_forward(args: dpo_ffn_args, stream=None) -> None:
+    _check(load().dpo_ffn_forward(ctypes.byref(args), _stream(stream)), None)
+
+
+def dpo_ffn_backward(args: dpo_ffn_backward_args, stream=None) -> None:
+    _check(load().dpo_ffn_backward(ctypes.byref(args), _stream(stream)), None)
+
+
+def dpo_ffn_workspace(tokens: int, dim: int, hidden: int, from_x8: bool = False):
+    """(forward bytes, backward bytes)."""
+    f, b = ctypes.c_int64(), ctypes.c_int64()
+    _check(load().dpo_ffn_workspace(tokens, dim, hidden, 1 if from_x8 else 0, ctypes.byref(f),
+                                    ctypes.byref(b)), None)
+    return f.value, b.value
+
+
+def dpo_ffn_get_status() -> int:
+    """Error bits of the feed-forward kernels (0: healthy); waits for the device."""
+    v = ctypes.c_uint32()
+    _check(load().dpo_ffn_get_status(ctypes.byref(v)), None)
+    return int(v.value)
+
+
+def dpo_ffn_clear_status(stream=None) -> None:
+    _check(load().dpo_ffn_clear_status(_stream(stream)), None)
 
 
 # ------------------------------------------------------------------ owner --
