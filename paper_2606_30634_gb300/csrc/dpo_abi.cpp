@@ -6,6 +6,7 @@
 // here in double and handed to the kernels by value; every per-element
 // operation runs in dpo_kernels.cu.
 #include "dpo.h"
+#include "dpo_call.h"
 #include "dpo_internal.h"
 
 #include <cuda_runtime.h>

@@ -8,6 +8,7 @@
 //                          dx, dw_gate, dw_up, dw_down, one list of tiles
 // (and one more to widen the 8-bit rows when the block's input was kept so).
 #include "dpo.h"
+#include "dpo_call.h"
 #include "dpo_ffn_gemm.cuh"
 
 #include <cuda_runtime.h>

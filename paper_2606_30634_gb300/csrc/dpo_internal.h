@@ -163,10 +163,6 @@ StepFn pick_step_adan(bool param_bf16, StashKind stash, bool grad_bf16, Correcti
 // through the hook of dpo_test_fail_allocs (dpo_abi.cpp).
 cudaError_t device_alloc(void **p, size_t bytes);
 
-// Sets the calling thread's message (dpo_last_error(NULL)) and returns code: the
-// entry points that have no context.
-int call_fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
-
 // A launch that may overlap the tail of the kernel before it on the stream
 // (programmatic stream serialization; the kernels' side is pdl_wait in
 // dpo_device.cuh). The gap between two dependent plain launches measured 1.3 to

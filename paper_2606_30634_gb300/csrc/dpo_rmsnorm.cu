@@ -5,6 +5,7 @@
 // All four move bytes: a few operations per element against 2 to 9 bytes of it,
 // so HBM bounds them, and launch latency where there are few rows.
 #include "dpo.h"
+#include "dpo_call.h"
 #include "dpo_pack8.cuh"
 
 #include <cuda_bf16.h>
