@@ -35,8 +35,8 @@ LIBS = {
                     "csrc/dpo_ffn.cu"],
         "headers": ["csrc/dpo_internal.h", "csrc/dpo_device.cuh", "csrc/dpo_reduce.cuh",
                     "csrc/dpo_step.cuh",
-                    "csrc/dpo_gemm.cuh", "csrc/dpo_call.h", "csrc/dpo_pack8.cuh", "csrc/dpo_ffn_gemm.cuh",
-                    "../include/dpo.h", "../include/dpo_muon.h"],
+                    "csrc/dpo_gemm.cuh", "csrc/dpo_call.h", "csrc/dpo_pack8.cuh",
+                    "csrc/dpo_ffn_gemm.cuh", "csrc/dpo_ffn_few.cuh", "../include/dpo.h", "../include/dpo_muon.h"],
         "includes": ["csrc"],
         "ptxas_v": ["csrc/dpo_step_adamw.cu", "csrc/dpo_muon.cu", "csrc/dpo_ffn.cu"],
     },

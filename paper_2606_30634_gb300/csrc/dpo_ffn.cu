@@ -9,11 +9,12 @@
 // (and one more to widen the 8-bit rows when the block's input was kept so).
 #include "dpo.h"
 #include "dpo_call.h"
-#include "dpo_ffn_gemm.cuh"
+#include "dpo_ffn_few.cuh"
 
 #include <cuda_runtime.h>
 
 #include <mutex>
+#include <type_traits>
 
 namespace {
 
@@ -39,23 +40,80 @@ constexpr int kForms = 3;   // epilogues
 // What the launches need to know of a device, found by its first call.
 struct Device {
     bool ready = false;
+    int sms = 0;
     unsigned int *err = nullptr;
-    int slots[2][kForms] = {};   // resident CTAs (0) and CTA pairs (1) of each kernel
+    // what is resident of each kernel at once: pairs, single CTAs, and clusters that split a
+    // tile's K by 1, 2, 4, 8
+    int pairs[kForms] = {}, singles[kForms] = {}, clusters[4][kForms] = {};
 };
 constexpr int kMaxDevices = 64;
 std::mutex g_mu;
 Device g_devices[kMaxDevices];
 EncodeTiled g_encode = nullptr;
 
-KernelFn kernel_of(int cg, int epi)
+// How a launch's tiles are taken: by CTA pairs (cg 2), by single CTAs (cg 1), or by
+// clusters of `ways` CTAs that split a tile's K (thin).
+struct Form {
+    int cg;
+    bool thin;
+    int ways, a_rows;
+    int cluster() const { return cg * ways; }
+    int bk() const { return thin ? Ring<true>::BK : Ring<false>::BK; }
+    int smem() const { return thin ? Ring<true>::smem(a_rows) : Ring<false>::smem(BM); }
+};
+constexpr Form kPairs = {2, false, 1, BM}, kSingles = {1, false, 1, BM};
+Form thin(int ways, int a_rows) { return {1, true, ways, a_rows}; }
+
+int slots_of(const Device &d, Form f, int epi)
 {
-    if (cg == 1)
-        return epi == kGate ? ffn_gemm_kernel<1, kGate>
-                            : epi == kGateBack ? ffn_gemm_kernel<1, kGateBack>
-                                               : ffn_gemm_kernel<1, kStore>;
-    return epi == kGate ? ffn_gemm_kernel<2, kGate>
-                        : epi == kGateBack ? ffn_gemm_kernel<2, kGateBack>
-                                           : ffn_gemm_kernel<2, kStore>;
+    return f.cg == 2 ? d.pairs[epi]
+           : f.thin  ? d.clusters[__builtin_ctz((unsigned)f.ways)][epi] : d.singles[epi];
+}
+
+KernelFn kernel_of(Form f, int epi)
+{
+    if (f.cg == 2)
+        return epi == kGate ? ffn_gemm_kernel<2, kGate, false>
+                            : epi == kGateBack ? ffn_gemm_kernel<2, kGateBack, false>
+                                               : ffn_gemm_kernel<2, kStore, false>;
+    if (f.thin)
+        return epi == kGate ? ffn_gemm_kernel<1, kGate, true>
+                            : epi == kGateBack ? ffn_gemm_kernel<1, kGateBack, true>
+                                               : ffn_gemm_kernel<1, kStore, true>;
+    return epi == kGate ? ffn_gemm_kernel<1, kGate, false>
+                        : epi == kGateBack ? ffn_gemm_kernel<1, kGateBack, false>
+                                           : ffn_gemm_kernel<1, kStore, false>;
+}
+
+cudaLaunchAttribute cluster_of(int n)
+{
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)n;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    return attr;
+}
+
+// A launch of `ctas` CTAs in clusters, overlapping the tail of the one before it
+// (launch_pdl of dpo_internal.h).
+template <class A>
+int launch_clusters(const char *what, void (*kernel)(A), int64_t ctas, int cluster, int threads,
+                    size_t smem, void *stream, const typename std::remove_const<A>::type &args)
+{
+    cudaLaunchAttribute attr[2] = {cluster_of(cluster), {}};
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args);
+    const cudaError_t last = cudaGetLastError();
+    e = e != cudaSuccess ? e : last;
+    return e == cudaSuccess ? DPO_OK : call_fail(DPO_ECUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
 cudaError_t prepare(Device &d)
@@ -71,33 +129,35 @@ cudaError_t prepare(Device &d)
             return cudaErrorNotSupported;
         g_encode = reinterpret_cast<EncodeTiled>(p);
     }
-    for (int cg = 1; cg <= 2; ++cg)
+    for (const Form f : {kPairs, kSingles, thin(1, BM), thin(2, BM), thin(4, BM), thin(8, BM)})
         for (int epi = 0; epi < kForms; ++epi) {
-            const KernelFn k = kernel_of(cg, epi);
-            cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(k),
-                                                 cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                 kSmemBytes);
+            const void *k = reinterpret_cast<const void *>(kernel_of(f, epi));
+            cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                 f.smem());
             if (e != cudaSuccess)
                 return e;
-            cudaLaunchAttribute attr{};
-            attr.id = cudaLaunchAttributeClusterDimension;
-            attr.val.clusterDim.x = (unsigned)cg;
-            attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+            cudaLaunchAttribute attr = cluster_of(f.cluster());
             cudaLaunchConfig_t cfg{};
             cfg.gridDim = dim3(1024);
             cfg.blockDim = dim3(kThreads);
-            cfg.dynamicSmemBytes = kSmemBytes;
+            cfg.dynamicSmemBytes = (size_t)f.smem();
             cfg.attrs = &attr;
             cfg.numAttrs = 1;
-            e = cudaOccupancyMaxActiveClusters(&d.slots[cg - 1][epi],
-                                               reinterpret_cast<const void *>(k), &cfg);
+            int &n = f.cg == 2 ? d.pairs[epi]
+                     : f.thin  ? d.clusters[__builtin_ctz((unsigned)f.ways)][epi] : d.singles[epi];
+            e = cudaOccupancyMaxActiveClusters(&n, k, &cfg);
             if (e != cudaSuccess)
                 return e;
-            if (d.slots[cg - 1][epi] < 1)
+            if (n < 1)
                 return cudaErrorInvalidConfiguration;
         }
     void *p = nullptr;
-    const cudaError_t e = cudaGetSymbolAddress(&p, g_ffn_err);
+    cudaError_t e = cudaGetSymbolAddress(&p, g_ffn_err);
+    int device = 0;
+    if (e == cudaSuccess)
+        e = cudaGetDevice(&device);
+    if (e == cudaSuccess)
+        e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, device);
     if (e != cudaSuccess)
         return e;
     d.err = static_cast<unsigned int *>(p);
@@ -165,7 +225,7 @@ struct Maps {
     }
 };
 
-int blocks_of(int64_t k) { return (int)((k + BK - 1) / BK); }
+int64_t blocks_of(int64_t k, int bk) { return (k + bk - 1) / bk; }
 
 // A product's sizes, before its operands.
 struct Shape {
@@ -179,38 +239,57 @@ int64_t tiles_of(const Shape &s, int cg, int epi)
     return (s.m + t - 1) / t * ((s.n + tn - 1) / tn);
 }
 
-// CTA pairs or single CTAs: the clocks the launch takes either way, its tiles dealt
-// round-robin (the estimate of the Newton-Schulz launches, launch_clocks in
-// dpo_muon.cu). More than four rounds of single CTAs go to the pairs unweighed.
-int form_of(const Device &d, const Shape *s, int n, int epi)
+// The form of a launch: the one with the smallest estimate of its time in ns, tiles dealt
+// round-robin. A K block costs what its stage of the ring waits for, about 2 us over the
+// stages, or on a pair the tensor core's 700 ns; all of them, the weights' way from HBM at
+// least. The exchange of a split tile's sums adds 2.5 us to each round, since the next
+// tile's MMAs hide only part of it. K is split only where a launch is one product, and more
+// than four rounds of single CTAs go to the pairs unweighed. Forward of GB300's measured
+// alternatives (all forms forced in turn, 17 to 1536 tokens, four pairs of widths): within
+// 3 us of the best form of either product but for a 7B gate at 17 and 128 tokens (4 and 1).
+Form form_of(const Device &d, const Shape *s, int n, int epi)
 {
-    int64_t clocks[2];
-    for (int cg = 1; cg <= 2; ++cg) {
-        const int64_t block = cg == 1 ? 700 : 1100, epilogue = cg == 1 ? 2600 : 5000;
-        const int64_t slots = d.slots[cg - 1][epi];
+    const int a_rows = s[0].m <= 32 ? 32 : s[0].m <= 64 ? 64 : BM;
+    const Form forms[] = {kSingles, thin(1, a_rows), thin(2, a_rows), thin(4, a_rows),
+                          thin(8, a_rows), kPairs};
+    Form best = kPairs;
+    double least = 1e30;
+    for (const Form &f : forms) {
+        const double block = f.cg == 2 ? 700.0 : 2000.0 / (f.thin ? Ring<true>::stages(f.a_rows) : 3);
+        const double epilogue = f.cg == 2 ? 3000.0 : f.thin ? 3000.0 : 1500.0;
+        const int64_t slots = slots_of(d, f, epi);
         int64_t tiles = 0;
+        double work = 0.0, longest = 0.0, weights = 0.0;
         for (int i = 0; i < n; ++i)
-            tiles += tiles_of(s[i], cg, epi);
-        if (cg == 1 && tiles > 4 * slots)
-            return 2;
-        int64_t work = 0, longest = 0;
+            tiles += tiles_of(s[i], f.cg, epi);
+        if (f.cg == 1 && !f.thin && tiles > 4 * slots)
+            return kPairs;
+        if (f.thin && (n > 1 || blocks_of(s[0].k, f.bk()) < 2 * f.ways))
+            continue;
         for (int i = 0; i < n; ++i) {
-            const int64_t c = blocks_of(s[i].k) * s[i].segments * block;
-            const int64_t each = c > epilogue ? c : epilogue;
-            work += tiles_of(s[i], cg, epi) * each;
+            const int64_t blocks = blocks_of(s[i].k, f.bk()) * s[i].segments;
+            const double c = (double)((blocks + f.ways - 1) / f.ways) * block;
+            const double each = f.thin ? c + 2500.0 : c > epilogue ? c : epilogue;
+            work += (double)tiles_of(s[i], f.cg, epi) * each;
             longest = longest > each ? longest : each;
+            weights += (double)(s[i].n * s[i].k * s[i].segments) * (epi == kGate ? 4.0 : 2.0) / 6500.0;
         }
         // whole rounds of equal tiles, or the longest one's end
-        const int64_t even = (work + slots - 1) / slots;
-        const int64_t rounds = n == 1 ? (tiles + slots - 1) / slots * longest : even;
-        clocks[cg - 1] = (rounds > longest ? rounds : longest) + epilogue;
+        double time = n == 1 ? (double)((tiles + slots - 1) / slots) * longest : work / (double)slots;
+        time = time > longest ? time : longest;
+        time = (time > weights ? time : weights) + epilogue + 0.1 * time;   // ties: the shorter
+        if (time < least) {
+            least = time;
+            best = f;
+        }
     }
-    return clocks[0] < clocks[1] ? 1 : 2;
+    return best;
 }
 
-int run(const char *what, const Device &d, Launch &L, const Shape *s, int n, int epi, int cg,
+int run(const char *what, const Device &d, Launch &L, const Shape *s, int n, int epi, Form f,
         bool maps_ok, void *stream)
 {
+    const int cg = f.cg;
     if (!maps_ok)
         return call_fail(DPO_ECUDA, "%s: a tensor map was refused", what);
     int64_t total = 0;
@@ -219,7 +298,7 @@ int run(const char *what, const Device &d, Launch &L, const Shape *s, int n, int
         Product &P = L.p[i];
         P.m = (int)s[i].m;
         P.n = (int)s[i].n;
-        P.k_blocks[0] = blocks_of(s[i].k);
+        P.k_blocks[0] = (int)blocks_of(s[i].k, f.bk());
         P.k_blocks[1] = s[i].segments == 2 ? P.k_blocks[0] : 0;
         P.m_tiles = (int)((s[i].m + t - 1) / t);
         P.n_tiles = (int)((s[i].n + tn - 1) / tn);
@@ -229,11 +308,24 @@ int run(const char *what, const Device &d, Launch &L, const Shape *s, int n, int
     L.n_products = n;
     L.n_tiles = (int)total;
     L.err = d.err;
-    const int64_t slots = d.slots[cg - 1][epi];
-    const int64_t ctas = (total < slots ? total : slots) * cg;
-    const cudaError_t e = launch_pdl(kernel_of(cg, epi), dim3((unsigned)ctas), kThreads, kSmemBytes,
-                                     static_cast<cudaStream_t>(stream), L);
-    return e == cudaSuccess ? DPO_OK : call_fail(DPO_ECUDA, "%s: %s", what, cudaGetErrorString(e));
+    L.a_rows = f.a_rows;
+    const int64_t slots = slots_of(d, f, epi);
+    return launch_clusters(what, kernel_of(f, epi), (total < slots ? total : slots) * f.cluster(),
+                           f.cluster(), kThreads, (size_t)f.smem(), stream, L);
+}
+
+// ---- few tokens ----
+
+// One product of the forward for at most kFewTokens tokens. K is split over a cluster
+// while the units alone do not fill the SMs and every warp keeps 64 of k.
+int run_few(const char *what, const FewArgs &a, int epi, int sms, void *stream)
+{
+    const int rows = epi == kGate ? 8 : 16;
+    const int64_t units = (a.rows + rows - 1) / rows;
+    int split = 1;
+    while (split < 8 && units * split < (int64_t)sms * kFewCtas && a.k > split * kFewWarps * 64)
+        split *= 2;
+    return launch_clusters(what, epi == kGate ? few_kernel<kGate> : few_kernel<kStore>, units * split, split, kFewThreads, 0, stream, a);
 }
 
 int64_t align_up(int64_t v) { return (v + 255) / 256 * 256; }
@@ -364,38 +456,80 @@ extern "C" int dpo_ffn_forward(const dpo_ffn_args *args, void *cuda_stream)
     if ((rc = device_info(what, &d)) != DPO_OK)
         return rc;
 
+    if (T <= kFewTokens && a.keep != DPO_KEEP_8BIT) {
+        using E = __nv_bfloat16;
+        FewArgs f{};
+        f.x = static_cast<const E *>(a.x);
+        f.w0 = static_cast<const E *>(a.w_gate);
+        f.w1 = static_cast<const E *>(a.w_up);
+        f.out = static_cast<E *>(a.workspace);
+        if (a.keep == DPO_KEEP_BF16) {
+            f.keep0 = static_cast<E *>(a.gate);
+            f.keep1 = static_cast<E *>(a.up);
+        }
+        f.ld_x = a.ld_x;
+        f.ld_out = F;
+        f.tokens = (int)T;
+        f.rows = (int)F;
+        f.k = (int)D;
+        f.act = a.act;
+        if ((rc = run_few(what, f, kGate, d->sms, cuda_stream)) != DPO_OK)
+            return rc;
+        FewArgs o{};
+        o.x = f.out;
+        o.w0 = static_cast<const E *>(a.w_down);
+        o.out = static_cast<E *>(a.out);
+        o.ld_x = F;
+        o.ld_out = a.ld_out;
+        o.tokens = (int)T;
+        o.rows = (int)D;
+        o.k = (int)F;
+        return run_few(what, o, kStore, d->sms, cuda_stream);
+    }
     {
         const Shape s = {T, F, D, 1};
-        const int cg = form_of(*d, &s, 1, kGate);
+        const Form form = form_of(*d, &s, 1, kGate);
+        const int cg = form.cg;
         Launch L{};
         Maps m;
         Product &P = L.p[0];
-        m.operand(&P.a[0], a.x, T, D, a.ld_x, BM);
+        m.operand(&P.a[0], a.x, T, D, a.ld_x, form.a_rows);
         m.operand(&P.b[0], a.w_gate, F, D, D, cg == 2 ? BH : BH / 2);
         m.operand(&P.b[1], a.w_up, F, D, D, cg == 2 ? BH : BH / 2);
         m.bf16(&P.d0, a.workspace, T, F, F);
+        P.o0 = static_cast<__nv_bfloat16 *>(a.workspace);
+        P.ld_o = F;
         if (a.keep == DPO_KEEP_8BIT) {
             m.codes(&P.d1, a.gate8.codes, T, F, a.gate8.ld_codes);
             m.codes(&P.d2, a.up8.codes, T, F, a.up8.ld_codes);
             P.scale_g = a.gate8.scales;
             P.scale_u = a.up8.scales;
             P.ld_scale = a.gate8.ld_scales;
+            P.codes_g = a.gate8.codes;
+            P.codes_u = a.up8.codes;
+            P.ld_codes_g = a.gate8.ld_codes;
+            P.ld_codes_u = a.up8.ld_codes;
         } else if (a.keep == DPO_KEEP_BF16) {
             m.bf16(&P.d1, a.gate, T, F, F);
             m.bf16(&P.d2, a.up, T, F, F);
+            P.o1 = static_cast<__nv_bfloat16 *>(a.gate);
+            P.o2 = static_cast<__nv_bfloat16 *>(a.up);
         }
         P.keep = a.keep;
         P.act = a.act;
-        if ((rc = run(what, *d, L, &s, 1, kGate, cg, m.ok, cuda_stream)) != DPO_OK)
+        if ((rc = run(what, *d, L, &s, 1, kGate, form, m.ok, cuda_stream)) != DPO_OK)
             return rc;
     }
     const Shape s = {T, D, F, 1};
     Launch L{};
     Maps m;
-    m.operand(&L.p[0].a[0], a.workspace, T, F, F, BM);
+    const Form form = form_of(*d, &s, 1, kStore);
+    m.operand(&L.p[0].a[0], a.workspace, T, F, F, form.a_rows);
     m.operand(&L.p[0].b[0], a.w_down, D, F, F, BH);
     m.bf16(&L.p[0].d0, a.out, T, D, a.ld_out);
-    return run(what, *d, L, &s, 1, kStore, form_of(*d, &s, 1, kStore), m.ok, cuda_stream);
+    L.p[0].o0 = static_cast<__nv_bfloat16 *>(a.out);
+    L.p[0].ld_o = a.ld_out;
+    return run(what, *d, L, &s, 1, kStore, form, m.ok, cuda_stream);
 }
 
 extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_stream)
@@ -480,15 +614,20 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
     }
     {
         const Shape s = {T, F, D, 1};
+        const Form form = form_of(*d, &s, 1, kGateBack);
         Launch L{};
         Maps m;
         Product &P = L.p[0];
-        m.operand(&P.a[0], a.dout, T, D, a.ld_dout, BM);
+        m.operand(&P.a[0], a.dout, T, D, a.ld_dout, form.a_rows);
         m.operand(&P.b[0], a.w_down, D, F, F, kBoxK);
         P.b_mn = 1;
         m.bf16(&P.d0, dg, T, F, F);
         m.bf16(&P.d1, du, T, F, F);
         m.bf16(&P.d2, act, T, F, F);
+        P.o0 = static_cast<__nv_bfloat16 *>(dg);
+        P.o1 = static_cast<__nv_bfloat16 *>(du);
+        P.o2 = static_cast<__nv_bfloat16 *>(act);
+        P.ld_o = F;
         if (a.keep == DPO_KEEP_8BIT) {
             P.kept_g = a.gate8.codes;
             P.kept_u = a.up8.codes;
@@ -503,8 +642,7 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
         }
         P.keep = a.keep;
         P.act = a.act;
-        if ((rc = run(what, *d, L, &s, 1, kGateBack, form_of(*d, &s, 1, kGateBack), m.ok,
-                      cuda_stream)) != DPO_OK)
+        if ((rc = run(what, *d, L, &s, 1, kGateBack, form, m.ok, cuda_stream)) != DPO_OK)
             return rc;
     }
     Launch L{};

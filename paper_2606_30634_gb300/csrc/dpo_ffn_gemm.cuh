@@ -16,6 +16,9 @@
 // tiles with the 2-SM MMA (CG = 2), or of single CTAs on 128 x 128 tiles (CG = 1)
 // where there are few; warp 0 loads, warp 1 issues the MMAs, eight warps drain
 // one accumulator while the MMAs fill the other. Every wait is bounded.
+// A product of few tiles has them split along K (SPLIT): the CTAs of a cluster take
+// a share of one tile's K blocks each and exchange their fp32 sums through the
+// cluster's shared memory, each finishing its share of the rows.
 //
 // Epilogues:
 //   kGate      the tile's columns are T / 2 of G beside the same T / 2 of U (the B
@@ -33,19 +36,14 @@ namespace dpo {
 namespace ffn {
 
 using gemm::BH;
-using gemm::BK;
 using gemm::BM;
 using gemm::group_sync;
-using gemm::kABytes;
-using gemm::kBBytes;
 using gemm::kBoxK;
 using gemm::kChunkBytes;
 using gemm::kErrDrain;
 using gemm::kErrWaitDone;
 using gemm::kErrWaitEmpty;
 using gemm::kErrWaitFull;
-using gemm::kStageBytes;
-using gemm::kStages;
 using gemm::kTile;
 using gemm::map_to_rank;
 using gemm::mbar_arrive;
@@ -65,8 +63,34 @@ enum Act { kSilu = 0, kGelu = 1 };
 
 constexpr int kEpiWarps = 8;
 constexpr int kThreads = 64 + 32 * kEpiWarps;
-constexpr int kStaging = 2 * kChunkBytes;                     // per epilogue warp
-constexpr int kSmemBytes = kStages * kStageBytes + 1024 + kEpiWarps * kStaging;
+// The ring of operand stages and the epilogue warps' staging behind it. Three stages of
+// 128 of K (six of 64 are slower, see dpo_gemm.cuh). Where K is split the time is the
+// operands' latency, about 2 us from request to MMA with the ring full, so the bytes in
+// flight count: stages of 64 of K, which leave room for more of them, and of A only the
+// 32, 64 or 128 rows that a product of so few tokens has. The MMA reads 128 rows all the
+// same; what lies behind a short box ends up in accumulator rows that nothing reads.
+constexpr int kRowBytes = kBoxK * 2;                          // of a box: the swizzle span
+constexpr int kMaxStages = 10;
+template <bool SPLIT> struct Ring {
+    static constexpr int BK = SPLIT ? 64 : 128;
+    static constexpr int box = BM * kRowBytes;                // of one box of 128 rows
+    static constexpr int staging = SPLIT ? 8192 : 2 * kChunkBytes;   // per epilogue warp
+    static __host__ __device__ constexpr int a_bytes(int rows) { return rows * BK * 2; }
+    static constexpr int b_bytes = BH * BK * 2;
+    // epilogue warps of tiles with so many rows
+    static __host__ __device__ constexpr int warps(int rows) { return kEpiWarps * rows / BM; }
+    static __host__ __device__ constexpr int stages(int rows)
+    {
+        return !SPLIT ? 3 : rows == 32 ? 10 : rows == 64 ? 8 : 5;
+    }
+    static __host__ __device__ constexpr int smem(int rows)
+    {
+        return stages(rows) * (a_bytes(rows) + b_bytes) + 1024 + warps(rows) * staging;
+    }
+};
+static_assert(Ring<true>::smem(32) <= 232448 && Ring<true>::smem(64) <= 232448 &&
+                  Ring<true>::smem(128) <= 232448 && Ring<false>::smem(BM) <= 232448,
+              "shared memory of a CTA");
 
 constexpr int kMaxProducts = 4;
 constexpr int kBandRows = 16;   // block rows per band, as in dpo_gemm.cuh
@@ -91,11 +115,17 @@ struct Product {
     const void *kept_g, *kept_u;  // kGateBack: codes or bf16
     int64_t ld_kept;
     int keep, act;                // Keep, Act
+    // split K: the same outputs as pointers (kStore: bf16, nothing added)
+    __nv_bfloat16 *o0, *o1, *o2;
+    int64_t ld_o;
+    uint8_t *codes_g, *codes_u;
+    int64_t ld_codes_g, ld_codes_u;
 };
 
 struct Launch {
     Product p[kMaxProducts];
     int n_products, n_tiles;
+    int a_rows;                   // rows of A in a stage (BM but where K is split)
     unsigned int *err;
 };
 
@@ -132,6 +162,13 @@ __device__ __forceinline__ uint32_t idesc_of(int cg, int a_mn, int b_mn)
 {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTile(cg) >> 3) << 17) |
            ((uint32_t)(kTile(cg) >> 4) << 24) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16);
+}
+
+// K blocks of shares 0 .. share of `split` (share -1: none); with split <= all, none is
+// empty.
+__device__ __forceinline__ int share_end(int all, uint32_t share, uint32_t split)
+{
+    return (int)((uint32_t)all * (share + 1u) / split);
 }
 
 // Product and position of tile t: bands of kBandRows block rows, column by column.
@@ -432,27 +469,267 @@ __device__ __forceinline__ void drain(const Product &P, Stager &st, uint32_t acc
     }
 }
 
+// ---- split K ----
+// Warp w of each of the S CTAs holds its K share's sums of the same 32 rows, in two
+// chunks of 32 columns. Rank j finishes rows 32/S j .. of them: each lane sends its row
+// of a chunk (128 bytes, granules XOR-ed with the row) to the buffer of the rank that
+// owns it, in the place of the rank it comes from, and the owner adds the S rows up in
+// rank order, so the result does not depend on timing. The stores are asynchronous ones
+// that complete on the owner's mbarrier, both chunks in one phase.
+//   xfull[w]   all S ranks' bytes have landed in this warp's buffer
+//   xempty[w]  all S ranks have read what this warp sent before
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity)
+{
+    unsigned long long t0 = 0;
+    for (;;) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (ok)
+            return true;
+        const unsigned long long now = gemm::globaltimer();
+        if (t0 == 0)
+            t0 = now;
+        if (now - t0 > gemm::kWaitNs)
+            return false;
+    }
+}
+
+constexpr int kSendBytes = 32 * 32 * 4;   // one chunk
+
+struct Exchange {
+    uint32_t buf, xfull, xempty;   // this CTA's, of this warp
+    uint32_t rank, ranks;
+    int lane, turn;
+    unsigned int *err;
+
+    __device__ __forceinline__ bool give_up(bool ok) const
+    {
+        if (__all_sync(0xFFFFFFFFu, ok))
+            return false;
+        if (lane == 0)
+            atomicOr(err, kErrWaitDone);
+        return true;
+    }
+    // Before a tile's `chunks` sends; false when the wait gave up.
+    __device__ __forceinline__ bool begin(int chunks)
+    {
+        if (give_up(mbar_wait_cluster(xempty, ((uint32_t)turn & 1u) ^ 1u)))
+            return false;
+        if (lane == 0)
+            mbar_arrive_expect_tx(xfull, (uint32_t)(chunks * kSendBytes));
+        return true;
+    }
+    __device__ __forceinline__ void send(int chunk, const float (&v)[32]) const
+    {
+        const int rows = 32 / (int)ranks;
+        const uint32_t owner = (uint32_t)(lane / rows);
+        const uint32_t to =
+            map_to_rank(buf + (uint32_t)(chunk * kSendBytes + ((int)rank * rows + lane % rows) * 128),
+                        owner);
+        const uint32_t bar = map_to_rank(xfull, owner);
+#pragma unroll
+        for (int g = 0; g < 8; ++g)
+            asm volatile(
+                "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], "
+                "{%1, %2, %3, %4}, [%5];" ::"r"(to + (uint32_t)((g ^ (lane & 7)) << 4)),
+                "f"(v[4 * g]), "f"(v[4 * g + 1]), "f"(v[4 * g + 2]), "f"(v[4 * g + 3]), "r"(bar)
+                : "memory");
+    }
+    // All ranks' sends have landed; false when the wait gave up.
+    __device__ __forceinline__ bool landed() const
+    {
+        return !give_up(mbar_wait_cluster(xfull, (uint32_t)turn & 1u));
+    }
+    // In lanes below 32 / ranks: the total of row 32 / ranks * rank + lane.
+    __device__ __forceinline__ void total(int chunk, float (&v)[32]) const
+    {
+        const int rows = 32 / (int)ranks;
+        if (lane >= rows)
+            return;
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            v[j] = 0.0f;
+        const int key = ((int)rank * rows + lane) & 7;   // of the sending lane
+        for (int r = 0; r < (int)ranks; ++r) {
+            const uint32_t from = buf + (uint32_t)(chunk * kSendBytes + (r * rows + lane) * 128);
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+                float4 f;
+                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w)
+                             : "r"(from + (uint32_t)((g ^ key) << 4))
+                             : "memory");
+                v[4 * g] += f.x;
+                v[4 * g + 1] += f.y;
+                v[4 * g + 2] += f.z;
+                v[4 * g + 3] += f.w;
+            }
+        }
+    }
+    // The buffer has been read: tell every rank.
+    __device__ __forceinline__ void end()
+    {
+        __syncwarp();
+        if (lane < (int)ranks)
+            asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+                             map_to_rank(xempty, (uint32_t)lane))
+                         : "memory");
+        ++turn;
+    }
+};
+
+// The first n of 32 values of a row, n a multiple of 8, rows 16-byte aligned.
+__device__ __forceinline__ void store_row(__nv_bfloat16 *p, const float (&v)[32], int n)
+{
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+        if (g * 8 < n)
+            *reinterpret_cast<uint4 *>(p + g * 8) =
+                make_uint4(gemm::pack_bf16(v[g * 8], v[g * 8 + 1]),
+                           gemm::pack_bf16(v[g * 8 + 2], v[g * 8 + 3]),
+                           gemm::pack_bf16(v[g * 8 + 4], v[g * 8 + 5]),
+                           gemm::pack_bf16(v[g * 8 + 6], v[g * 8 + 7]));
+}
+
+__device__ __forceinline__ void store_codes(uint8_t *p, uint8_t *scale, const float (&v)[32], int n)
+{
+    float amax = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+        if (j < n)
+            amax = fmaxf(amax, finite_abs(v[j]));
+    const uint32_t s = scale_byte(amax);
+    const float inv = inv_scale_of(s);
+    *scale = (uint8_t)s;
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+        if (g * 8 < n) {
+            const float *w = v + g * 8;
+            *reinterpret_cast<uint2 *>(p + g * 8) = make_uint2(
+                encode4(inf_to_nan(w[0]) * inv, inf_to_nan(w[1]) * inv, inf_to_nan(w[2]) * inv,
+                        inf_to_nan(w[3]) * inv),
+                encode4(inf_to_nan(w[4]) * inv, inf_to_nan(w[5]) * inv, inf_to_nan(w[6]) * inv,
+                        inf_to_nan(w[7]) * inv));
+        }
+}
+
+// A warp's part of a tile split along K: 32 rows of kGate: 32 columns of G and of U,
+// otherwise of 64 columns, from row0 and col0 on. bf16 outputs o0, o1, o2 (as d0, d1, d2),
+// written row by row. acc_empty is arrived on as soon as the accumulator is read.
+// False when a wait gave up.
+template <int EPI>
+__device__ __forceinline__ bool drain_split(const Product &P, Exchange &ex, uint32_t acc,
+                                            int half_cols, int row0, int col0, uint32_t acc_empty)
+{
+    const bool any = row0 < P.m && col0 < P.n;   // the same on every rank
+    const int chunks = !any ? 0 : EPI == kGate || col0 + 32 < P.n ? 2 : 1;
+    if (any && !ex.begin(chunks))
+        return false;
+    for (int c = 0; c < chunks; ++c) {
+        float v[32];
+        load_acc(acc + (uint32_t)(c * (EPI == kGate ? half_cols : 32)), v);
+        ex.send(c, v);
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncwarp();
+    if (ex.lane == 0)
+        mbar_arrive<1>(acc_empty);
+    if (!any)
+        return true;
+    if (!ex.landed())
+        return false;
+    const int rows = 32 / (int)ex.ranks;
+    const int row = row0 + (int)ex.rank * rows + ex.lane;
+    const bool mine = ex.lane < rows && row < P.m;
+    if constexpr (EPI == kGate) {
+        const int n = min(32, P.n - col0);
+        const int64_t at = row * P.ld_o + col0;
+        float g[32], u[32];
+        ex.total(0, g);
+        ex.total(1, u);
+        ex.end();
+        if (!mine)
+            return true;
+        if (P.keep == kKeep16) {
+            store_row(P.o1 + at, g, n);
+            store_row(P.o2 + at, u, n);
+        } else if (P.keep == kKeep8) {
+            const int64_t sat = row * P.ld_scale + col0 / kGroup;
+            store_codes(P.codes_g + row * P.ld_codes_g + col0, P.scale_g + sat, g, n);
+            store_codes(P.codes_u + row * P.ld_codes_u + col0, P.scale_u + sat, u, n);
+        }
+        if (P.act == kGelu)
+            gate<kGelu>(g, u);
+        else
+            gate<kSilu>(g, u);
+        store_row(P.o0 + at, u, n);
+    } else {
+        for (int c = 0; c < chunks; ++c) {
+            const int n = min(32, P.n - col0 - c * 32);
+            const int64_t at = row * P.ld_o + col0 + c * 32;
+            float v[32];
+            ex.total(c, v);
+            if (!mine)
+                continue;
+            if constexpr (EPI == kGateBack) {
+                float g[32], u[32];
+                load_kept(P, P.kept_g, P.scale_g, row, col0 + c * 32, g);
+                load_kept(P, P.kept_u, P.scale_u, row, col0 + c * 32, u);
+                if (P.act == kGelu)
+                    gate_back<kGelu>(g, u, v);
+                else
+                    gate_back<kSilu>(g, u, v);
+                store_row(P.o0 + at, g, n);
+                store_row(P.o1 + at, u, n);
+                store_row(P.o2 + at, v, n);
+            } else {
+                store_row(P.o0 + at, v, n);
+            }
+        }
+        ex.end();
+    }
+    return true;
+}
+
 //   full[s]      (leader) both ranks' TMA bytes of stage s have landed
 //   empty[s]     (each)   the leader's MMAs have finished reading stage s
 //   acc_full[a]  (each)   accumulator a holds a finished tile
 //   acc_empty[a] (leader) all epilogue warps of the pair have read it
-template <int CG, int EPI>
-__global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
-    ffn_gemm_kernel(const __grid_constant__ Launch L)
+// CG CTAs share a tile (a pair's 2-SM MMA); SPLIT (CG = 1): the CTAs of a cluster
+// share a tile's K blocks. The cluster's size comes with the launch.
+template <int CG, int EPI, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_constant__ Launch L)
 {
-    constexpr int T = kTile(CG);
+    static_assert(CG == 1 || !SPLIT, "pairs do not split K");
+    using R = Ring<SPLIT>;
+    constexpr int T = kTile(CG), BK = R::BK, kBBytes = R::b_bytes;
+    const int a_rows = SPLIT ? L.a_rows : BM;
+    const int n_stages = R::stages(a_rows), a_bytes = R::a_bytes(a_rows);
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * kStages + 4];
+    constexpr int kStages = SPLIT ? kMaxStages : R::stages(BM);   // barriers laid out for
+    __shared__ uint64_t bars[2 * kStages + 4 + (SPLIT ? 2 * kEpiWarps : 0)];
     __shared__ uint32_t tmem_slot;
     __shared__ int aborted;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? gemm::cluster_rank() : 0u;
     const bool leader = rank == 0;
-    const int pair = blockIdx.x / CG, n_pairs = gridDim.x / CG;
+    uint32_t split = 1, share = 0;   // CTAs on a tile's K blocks, and which this is
+    if (SPLIT) {
+        asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(split));
+        share = gemm::cluster_rank();
+    }
+    const int group = SPLIT ? (int)split : CG;
+    const int pair = blockIdx.x / group, n_pairs = gridDim.x / group;
     const uint32_t raw = (uint32_t)__cvta_generic_to_shared(smem_raw);
     const uint32_t ring = (raw + 1023u) & ~1023u;
-    const uint32_t sa = ring, sb = ring + kStages * kABytes;
+    const uint32_t sa = ring, sb = ring + (uint32_t)(n_stages * a_bytes);
     const uint32_t bar0 = (uint32_t)__cvta_generic_to_shared(bars);
     auto full = [&](int s) { return bar0 + 8u * (uint32_t)s; };
     auto empty = [&](int s) { return bar0 + 8u * (uint32_t)(kStages + s); };
@@ -468,21 +745,38 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
             mbar_init(acc_full(a), 1);
             mbar_init(acc_empty(a), CG * kEpiWarps);
         }
+        if (SPLIT)
+            for (int w = 0; w < kEpiWarps; ++w) {
+                mbar_init(bar0 + 8u * (uint32_t)(2 * kStages + 4 + 2 * w), 1);
+                mbar_init(bar0 + 8u * (uint32_t)(2 * kStages + 5 + 2 * w), split);
+            }
         aborted = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1)
         gemm::tmem_alloc<CG>((uint32_t)__cvta_generic_to_shared(&tmem_slot));
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    group_sync<CG>();
+    group_sync<SPLIT ? 2 : CG>();   // barriers of every CTA initialised before remote use
+    if (SPLIT)
+        __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_slot;
     const int n_tiles = L.n_tiles;
+    if (warp == 0 && lane < L.n_products) {   // the maps are parameters: read before the wait
+        for (int i = 0; i < 2; ++i) {
+            asm volatile("prefetch.tensormap [%0];"
+                         ::"l"(reinterpret_cast<uint64_t>(&L.p[lane].a[i])) : "memory");
+            asm volatile("prefetch.tensormap [%0];"
+                         ::"l"(reinterpret_cast<uint64_t>(&L.p[lane].b[i])) : "memory");
+        }
+    }
     pdl_wait();
 
     if (warp == 0) {
         if (lane == 0) {
-            int it = 0;   // K blocks issued by this CTA
+            int it = 0, s = 0;   // K blocks issued by this CTA, the ring's next stage
+            uint32_t ph = 1;     // parity of the stage's release
+            const uint32_t bytes = (uint32_t)(CG * (a_bytes + kBBytes));
             for (int t = pair; t < n_tiles && !*(volatile int *)&aborted; t += n_pairs) {
                 const Tile tile = tile_at(L, t);
                 const Product &P = L.p[tile.p];
@@ -491,55 +785,63 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
                 // B rows of this CTA: T / CG of the tile's columns; kGate: a pair's CTAs
                 // hold one projection each, a single CTA half a box of either
                 const int nb = EPI == kGate ? tile.n * (T / 2) : tile.n * T + (int)rank * BH;
-                const int kb0 = P.k_blocks[0], kb_n = kb0 + P.k_blocks[1];
-                for (int kb = 0; kb < kb_n; ++kb, ++it) {
-                    const int s = it % kStages;
-                    const uint32_t ph = (uint32_t)(it / kStages) & 1u;
-                    if (!mbar_wait(empty(s), ph ^ 1u) || *(volatile int *)&aborted) {
+                const int kb0 = P.k_blocks[0], kb_all = kb0 + P.k_blocks[1];
+                const int kb_n = SPLIT ? share_end(kb_all, share, split) : kb_all;
+                for (int kb = SPLIT ? share_end(kb_all, share - 1, split) : 0; kb < kb_n;
+                     ++kb, ++it) {
+                    if (!mbar_wait(empty(s), ph) || *(volatile int *)&aborted) {
                         atomicOr(L.err, kErrWaitEmpty);
                         aborted = 1;
                         break;
                     }
                     const uint32_t fbar = CG == 2 ? map_to_rank(full(s), 0) : full(s);
                     if (leader)
-                        mbar_arrive_expect_tx(full(s), (uint32_t)(CG * kStageBytes));
+                        mbar_arrive_expect_tx(full(s), bytes);
                     const int seg = kb >= kb0, k = (kb - (seg ? kb0 : 0)) * BK;
                     const CUtensorMap *ta = &P.a[seg];
                     const CUtensorMap *tb = EPI == kGate ? &P.b[CG == 2 ? rank : 0] : &P.b[seg];
 #pragma unroll
                     for (int h = 0; h < BK / kBoxK; ++h) {
                         const int k0 = k + h * kBoxK;
-                        const uint32_t ah = sa + (uint32_t)(s * kABytes + h * (kABytes / 2));
-                        const uint32_t bh = sb + (uint32_t)(s * kBBytes + h * (kBBytes / 2));
-                        if (a_mn) {
+                        const uint32_t ah = sa + (uint32_t)(s * a_bytes + h * R::box);
+                        const uint32_t bh = sb + (uint32_t)(s * kBBytes + h * R::box);
+                        if (!SPLIT && a_mn) {
                             tma_load<CG>(ah, ta, ma, k0, fbar);
-                            tma_load<CG>(ah + kABytes / 4, ta, ma + 64, k0, fbar);
+                            tma_load<CG>(ah + R::box / 2, ta, ma + 64, k0, fbar);
                         } else {
                             tma_load<CG>(ah, ta, k0, ma, fbar);
                         }
                         if (EPI == kGate && CG == 1) {   // 64 rows of each projection
                             tma_load<CG>(bh, &P.b[0], k0, nb, fbar);
-                            tma_load<CG>(bh + kBBytes / 4, &P.b[1], k0, nb, fbar);
+                            tma_load<CG>(bh + R::box / 2, &P.b[1], k0, nb, fbar);
                         } else if (b_mn) {
                             tma_load<CG>(bh, tb, nb, k0, fbar);
-                            tma_load<CG>(bh + kBBytes / 4, tb, nb + 64, k0, fbar);
+                            tma_load<CG>(bh + R::box / 2, tb, nb + 64, k0, fbar);
                         } else {
                             tma_load<CG>(bh, tb, k0, nb, fbar);
                         }
                     }
+                    if (++s == n_stages) {
+                        s = 0;
+                        ph ^= 1u;
+                    }
                 }
             }
             if (leader)   // no CTA leaves before the loads in flight have landed
-                for (int q = it - kStages < 0 ? 0 : it - kStages; q < it; ++q)
-                    if (!mbar_wait(full(q % kStages), (uint32_t)(q / kStages) & 1u))
+                for (int q = it - n_stages < 0 ? 0 : it - n_stages; q < it; ++q)
+                    if (!mbar_wait(full(q % n_stages), (uint32_t)(q / n_stages) & 1u))
                         atomicOr(L.err, kErrDrain);
         }
     } else if (warp == 1) {
         if (lane == 0 && leader) {
-            int it = 0, lt = 0;
+            int lt = 0, s = 0;
+            uint32_t ph = 0;
             for (int t = pair; t < n_tiles && !*(volatile int *)&aborted; t += n_pairs, ++lt) {
                 const Product &P = L.p[tile_at(L, t).p];
-                const int kb_n = P.k_blocks[0] + P.k_blocks[1];
+                const int kb_all = P.k_blocks[0] + P.k_blocks[1];
+                const int kb_n = SPLIT ? share_end(kb_all, share, split) -
+                                             share_end(kb_all, share - 1, split)
+                                       : kb_all;
                 const bool a_mn = P.a_mn, b_mn = P.b_mn;
                 const uint32_t idesc = idesc_of(CG, a_mn, b_mn);
                 const int a = lt & 1;
@@ -552,9 +854,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t d = tmem + (uint32_t)(a * T);
                 bool ok = true;
-                for (int kb = 0; kb < kb_n; ++kb, ++it) {
-                    const int s = it % kStages;
-                    const uint32_t ph = (uint32_t)(it / kStages) & 1u;
+                for (int kb = 0; kb < kb_n; ++kb) {
                     if (!mbar_wait(full(s), ph) || *(volatile int *)&aborted) {
                         atomicOr(L.err, kErrWaitFull);
                         aborted = 1;
@@ -565,8 +865,8 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int k = 0; k < BK / 16; ++k) {
                         const int h = k / (kBoxK / 16), kk = k % (kBoxK / 16);
-                        const uint32_t ah = sa + (uint32_t)(s * kABytes + h * (kABytes / 2));
-                        const uint32_t bh = sb + (uint32_t)(s * kBBytes + h * (kBBytes / 2));
+                        const uint32_t ah = sa + (uint32_t)(s * a_bytes + h * R::box);
+                        const uint32_t bh = sb + (uint32_t)(s * kBBytes + h * R::box);
                         const uint64_t ad = a_mn ? smem_desc_mn(ah + (uint32_t)(kk * 16 * 128))
                                                  : smem_desc(ah + (uint32_t)(kk * 32));
                         const uint64_t bd = b_mn ? smem_desc_mn(bh + (uint32_t)(kk * 16 * 128))
@@ -574,6 +874,10 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
                         mma_bf16<CG>(d, ad, bd, idesc, (kb | k) != 0 ? 1u : 0u);
                     }
                     mma_commit<CG>(empty(s));
+                    if (++s == n_stages) {
+                        s = 0;
+                        ph ^= 1u;
+                    }
                 }
                 mma_commit<CG>(acc_full(a));
                 if (!ok) {
@@ -587,7 +891,11 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
         // Warp w reads TMEM lanes 32 (w % 4) .. +31, rows BM rank + 32 (w % 4) + lane of
         // the tile, and the half of its columns that (w - 2) / 4 names.
         const int q = warp & 3, half = (warp - 2) >> 2;
-        Stager st = {ring + (uint32_t)(kStages * kStageBytes + (warp - 2) * kStaging), lane, 0};
+        // staging of the warps that have rows
+        const int slot = SPLIT ? half * (a_rows / 32) + q : warp - 2;
+        Stager st = {ring + (uint32_t)(n_stages * (a_bytes + kBBytes) + slot * R::staging), lane, 0};
+        const uint32_t xbar = bar0 + 8u * (uint32_t)(2 * kStages + 4 + (warp - 2) * 2);
+        Exchange ex = {st.buf, xbar, xbar + 8u, share, split, lane, 0, L.err};
         constexpr int kCols = EPI == kGate ? T / 2 : T;   // output columns of a tile
         int lt = 0;
         for (int t = pair; t < n_tiles; t += n_pairs, ++lt) {
@@ -605,9 +913,20 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
             const uint32_t acc =
                 tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * T + half * (kCols / 2));
 #pragma unroll 1
-            for (int ch = 0; ch < kCols / 64; ++ch)
-                drain<EPI>(P, st, acc + (uint32_t)(ch * 32), kCols, row0,
-                           tile.n * kCols + half * (kCols / 2) + ch * 32);
+            for (int ch = 0; ch < (SPLIT ? 1 : kCols / 64); ++ch) {
+                const uint32_t at = acc + (uint32_t)(ch * 32);
+                const int col0 = tile.n * kCols + half * (kCols / 2) + ch * 32;
+                if constexpr (SPLIT)
+                    seen = drain_split<EPI>(P, ex, at, kCols, row0, col0, acc_empty(a));
+                else
+                    drain<EPI>(P, st, at, kCols, row0, col0);
+            }
+            if (SPLIT) {
+                if (seen)
+                    continue;
+                aborted = 1;
+                break;
+            }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0)
@@ -619,8 +938,8 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     }
     __syncthreads();
-    if (CG == 2)
-        group_sync<CG>();
+    if (CG == 2 || SPLIT)
+        group_sync<2>();   // no CTA leaves while a peer may use its shared memory
     if (warp == 1) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         gemm::tmem_free<CG>(tmem);

@@ -301,117 +301,150 @@ rmsnorm_kernel(const NormForwardArgs args)
 
 // Backward: a persistent grid of CTAs walks the rows; a thread keeps the sums of
 // dy n of its columns in registers, so dweight costs one partial row per CTA,
-// which the second kernel adds up.
+// which the second kernel adds up. A row is one pass of loads, a sum over the
+// row's threads and the stores; the next row's loads are issued before the sum of
+// this one, or each row would wait for HBM by itself.
 struct NormBackArgs {
     dpo_rmsnorm_backward_args a;
     int warps;
     float *partials;                          // one row of cols per CTA
 };
 
-template <class T, class WT, int V, int TB>
-__global__ void __launch_bounds__(TB)
+// E elements of a row per thread: 16, so that this row's and the next one's inputs, the
+// weights and the sums fit its registers, or 32 where that would take more than 512
+// threads (cols above 8192; the next row is not loaded ahead then, nor in the narrow
+// forms, whose pieces are many).
+constexpr int kBackElems = 16, kBackThreads = 512;
+
+// What a row's thread loads: dy, h or the codes and scales, dh.
+template <class T, int V, int E, bool X8> struct RowIn {
+    static constexpr int N = E / V;
+    Vec<T, V> dy[N], dh[N];
+    Vec<T, X8 ? 1 : V> h[X8 ? 1 : N];
+    Codes<V> q[X8 ? N : 1];
+    float scale[X8 ? N : 1];
+    float rstd;
+
+    __device__ __forceinline__ void load(const dpo_rmsnorm_backward_args &a, int64_t row, int i0,
+                                         int tpr)
+    {
+        const bool live = row < a.rows;
+        rstd = live ? ld1(a.rstd + row) : 0.0f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int c = (i0 + n * tpr) * V;
+            const bool in = live && c < (int)a.cols;
+            dy[n].zero();
+            dh[n].zero();
+            if (in) {
+                dy[n].load(static_cast<const T *>(a.dy) + row * a.ld_dy + c);
+                if (a.dh != nullptr)
+                    dh[n].load(static_cast<const T *>(a.dh) + row * a.ld_dh + c);
+            }
+            if constexpr (X8) {
+#pragma unroll
+                for (int j = 0; j < words(V); ++j)
+                    q[n].w[j] = 0u;
+                scale[n] = 0.0f;
+                if (in) {
+                    q[n].load(a.x8.codes + row * a.x8.ld_codes + c);
+                    scale[n] = load_scale(a.x8.scales + row * a.x8.ld_scales + c / kGroup);
+                }
+            } else {
+                h[n].zero();
+                if (in)
+                    h[n].load(static_cast<const T *>(a.h) + row * a.ld_h + c);
+            }
+        }
+    }
+    // the normalised values of piece n
+    __device__ __forceinline__ void normalised(int n, float (&v)[V]) const
+    {
+        if constexpr (X8) {
+            q[n].get(v, scale[n]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                v[j] = h[n].get(j) * rstd;
+        }
+    }
+};
+
+template <class T, class WT, int V, int E, bool X8>
+__global__ void __launch_bounds__(kBackThreads)
 rmsnorm_backward_kernel(const NormBackArgs args)
 {
-    constexpr int N = kRowElems / V;
-    __shared__ float red[32];
+    constexpr int N = E / V;
+    constexpr bool kAhead = V >= 4 && E == kBackElems;
+    __shared__ float red[2][32];              // by the row's parity: one barrier a row
     extern __shared__ float dw_cta[];         // cols, with several rows per CTA
     const dpo_rmsnorm_backward_args &a = args.a;
     const int warps = args.warps, tpr = warps * 32;
     const int rows_cta = (int)blockDim.x / tpr;
     const int i0 = threadIdx.x & (tpr - 1), r0 = threadIdx.x / tpr;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int cols = (int)a.cols;
+    const int64_t stride = (int64_t)gridDim.x * rows_cta;
     pdl_wait();
+    Vec<WT, V> w[N];
     float dw[N][V];
 #pragma unroll
-    for (int n = 0; n < N; ++n)
+    for (int n = 0; n < N; ++n) {
+        const int c = (i0 + n * tpr) * V;
+        w[n].zero();
+        if (c < cols)
+            w[n].load(static_cast<const WT *>(a.weight) + c);
 #pragma unroll
         for (int j = 0; j < V; ++j)
             dw[n][j] = 0.0f;
-    for (int64_t base = (int64_t)blockIdx.x * rows_cta; base < a.rows;
-         base += (int64_t)gridDim.x * rows_cta) {
+    }
+    RowIn<T, V, E, X8> next;
+    int64_t base = (int64_t)blockIdx.x * rows_cta;
+    if (kAhead)
+        next.load(a, base + r0, i0, tpr);
+    for (int parity = 0; base < a.rows; base += stride, parity ^= 1) {
         const int64_t row = base + r0;
-        const bool live = row < a.rows;
-        const float rstd = live ? ld1(a.rstd + row) : 0.0f;
-        Vec<T, V> dy[N];
-        float nv[N][V];
-        const T *dyp = static_cast<const T *>(a.dy) + row * a.ld_dy;
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const int c = (i0 + n * tpr) * V;
-            dy[n].zero();
-            if (live && c < cols)
-                dy[n].load(dyp + c);
-        }
-        if (a.h != nullptr) {
-            const T *hp = static_cast<const T *>(a.h) + row * a.ld_h;
-            Vec<T, V> h[N];
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int c = (i0 + n * tpr) * V;
-                h[n].zero();
-                if (live && c < cols)
-                    h[n].load(hp + c);
-            }
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    nv[n][j] = h[n].get(j) * rstd;
-        } else {
-            Codes<V> q[N];
-            float sc[N];
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int c = (i0 + n * tpr) * V;
-#pragma unroll
-                for (int j = 0; j < words(V); ++j)
-                    q[n].w[j] = 0u;
-                sc[n] = 0.0f;
-                if (live && c < cols) {
-                    q[n].load(a.x8.codes + row * a.x8.ld_codes + c);
-                    sc[n] = load_scale(a.x8.scales + row * a.x8.ld_scales + c / kGroup);
-                }
-            }
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-                q[n].get(nv[n], sc[n]);
-        }
+        if (!kAhead)
+            next.load(a, row, i0, tpr);
+        const RowIn<T, V, E, X8> in = next;
+        if (kAhead && base + stride < a.rows)
+            next.load(a, row + stride, i0, tpr);
         float sum = 0.0f;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const int c = (i0 + n * tpr) * V;
-            if (c < cols) {
-                Vec<WT, V> w;
-                w.load(static_cast<const WT *>(a.weight) + c);
+            float v[V];
+            in.normalised(n, v);
 #pragma unroll
-                for (int j = 0; j < V; ++j)
-                    sum = fmaf(dy[n].get(j) * w.get(j), nv[n][j], sum);
+            for (int j = 0; j < V; ++j) {
+                const float dy = in.dy[n].get(j);
+                sum = fmaf(dy * w[n].get(j), v[j], sum);
+                dw[n][j] = fmaf(dy, v[j], dw[n][j]);
             }
         }
-        sum = row_sum(sum, warps, red) / (float)cols;
-        T *dxp = static_cast<T *>(a.dx) + row * a.ld_dx;
-        const T *dhp = static_cast<const T *>(a.dh) + row * a.ld_dh;
+        sum = warp_sum(sum);
+        if (warps > 1) {
+            if (lane == 0)
+                red[parity][warp] = sum;
+            __syncthreads();
+            sum = warp_sum(lane < warps ? red[parity][(warp & ~(warps - 1)) + lane] : 0.0f);
+        }
+        sum /= (float)cols;
+        if (a.dx != nullptr && row < a.rows) {
+            T *dxp = static_cast<T *>(a.dx) + row * a.ld_dx;
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const int c = (i0 + n * tpr) * V;
-            if (live && c < cols) {
-                if (a.dx != nullptr) {
-                    Vec<WT, V> w;
-                    Vec<T, V> dh, o;
-                    dh.zero();
-                    w.load(static_cast<const WT *>(a.weight) + c);
-                    if (a.dh != nullptr)
-                        dh.load(dhp + c);
+            for (int n = 0; n < N; ++n) {
+                const int c = (i0 + n * tpr) * V;
+                if (c < cols) {
                     float v[V];
+                    in.normalised(n, v);
 #pragma unroll
                     for (int j = 0; j < V; ++j)
-                        v[j] = fmaf(rstd, dy[n].get(j) * w.get(j) - nv[n][j] * sum, dh.get(j));
+                        v[j] = fmaf(in.rstd, in.dy[n].get(j) * w[n].get(j) - v[j] * sum,
+                                    in.dh[n].get(j));
+                    Vec<T, V> o;
                     o.set(v);
                     o.store(dxp + c);
                 }
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    dw[n][j] = fmaf(dy[n].get(j), nv[n][j], dw[n][j]);
             }
         }
     }
@@ -449,8 +482,9 @@ rmsnorm_backward_kernel(const NormBackArgs args)
 }
 
 // dweight[c] = the sum of the n partial rows, in a fixed order: 32 columns per
-// CTA, 16 interleaved shares of the rows, added up in order.
-constexpr int kSumShares = 16;
+// CTA, 16 interleaved shares of the rows, eight loads of each in flight, added up
+// in order.
+constexpr int kSumShares = 16, kSumLoads = 8;
 template <class GT>
 __global__ void __launch_bounds__(32 * kSumShares)
 rmsnorm_dweight_kernel(const float *partials, int n, int cols, GT *dweight, int accumulate)
@@ -461,8 +495,17 @@ rmsnorm_dweight_kernel(const float *partials, int n, int cols, GT *dweight, int 
     pdl_wait();
     float sum = 0.0f;
     if (c < cols)
-        for (int i = k; i < n; i += kSumShares)
-            sum += ld1(partials + (int64_t)i * cols + c);
+        for (int i = k; i < n; i += kSumShares * kSumLoads) {
+            float v[kSumLoads];
+#pragma unroll
+            for (int u = 0; u < kSumLoads; ++u) {
+                const int at = i + u * kSumShares;
+                v[u] = at < n ? ld1(partials + (int64_t)at * cols + c) : 0.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < kSumLoads; ++u)
+                sum += v[u];
+        }
     share[k][lane] = sum;
     __syncthreads();
     if (k != 0 || c >= cols)
@@ -576,21 +619,30 @@ int sm_count()
     return sms;
 }
 
-int row_warps(int64_t cols)
+// Warps of a row with so many elements a thread.
+int row_warps(int64_t cols, int elems)
 {
     int w = 1;
-    while ((int64_t)w * 32 * kRowElems < cols)
+    while ((int64_t)w * 32 * elems < cols)
         w *= 2;
     return w;
 }
 
-// CTAs of the backward's persistent grid, for row counts that fill it.
-int64_t backward_ctas(int64_t rows, int64_t cols, int sms)
+// The backward's shape: elements of a row per thread, warps of a row and of a CTA, CTAs.
+struct BackShape {
+    int elems, warps, cta;
+    int64_t grid;
+};
+BackShape back_shape(int64_t rows, int64_t cols, int sms)
 {
-    const int warps = row_warps(cols), cta = warps > kMinWarps ? warps : kMinWarps;
-    const int64_t want = (rows + cta / warps - 1) / (cta / warps);
-    const int64_t most = (int64_t)sms * (cta <= 4 ? 4 : cta <= 8 ? 2 : 1);
-    return want < most ? want : most;
+    BackShape b;
+    b.elems = cols <= (int64_t)kBackThreads * kBackElems ? kBackElems : kRowElems;
+    b.warps = row_warps(cols, b.elems);
+    b.cta = b.warps > kMinWarps ? b.warps : kMinWarps;
+    const int64_t want = (rows + b.cta / b.warps - 1) / (b.cta / b.warps);
+    const int64_t most = (int64_t)sms * (16 / b.cta);   // 16 warps an SM
+    b.grid = want < most ? want : most;
+    return b;
 }
 
 struct Span {
@@ -712,9 +764,18 @@ auto pick(int dtype, int wdtype, int v, int threads)
 template <class T, class WT, int V, int TB> struct Fwd {
     static auto fn() { return &rmsnorm_kernel<T, WT, V, TB>; }
 };
-template <class T, class WT, int V, int TB> struct Back {
-    static auto fn() { return &rmsnorm_backward_kernel<T, WT, V, TB>; }
+template <class T, class WT, int V, int E> struct BackH {
+    static auto fn() { return &rmsnorm_backward_kernel<T, WT, V, E, false>; }
 };
+template <class T, class WT, int V, int E> struct Back8 {
+    static auto fn() { return &rmsnorm_backward_kernel<T, WT, V, E, true>; }
+};
+template <template <class, class, int, int> class K>
+auto pick_back(int dtype, int wdtype, int v, int elems)
+{
+    return elems == kBackElems ? pick_vec<K, kBackElems>(dtype, wdtype, v)
+                               : pick_vec<K, kRowElems>(dtype, wdtype, v);
+}
 
 int check_norm(const char *what, int64_t rows, int64_t cols, int dtype, int wdtype,
                const void *weight)
@@ -792,7 +853,7 @@ extern "C" int dpo_rmsnorm(const dpo_rmsnorm_args *args, void *cuda_stream)
              aligned_to(a.weight, a.weight_dtype == DPO_F32 ? (v == 2 ? 8 : 16) : 2 * v) &&
              whole(a.x8.codes, a.x8.ld_codes, 1, v)))
         v = v == 8 ? 2 : 1;
-    const NormForwardArgs k = {a, row_warps(a.cols)};
+    const NormForwardArgs k = {a, row_warps(a.cols, kRowElems)};
     const int cta = k.warps > kMinWarps ? k.warps : kMinWarps;
     const int64_t grid = (a.rows + cta / k.warps - 1) / (cta / k.warps);
     return launch(what, pick<Fwd>(a.dtype, a.weight_dtype, v, cta * 32), grid, cta * 32, 0,
@@ -807,7 +868,7 @@ extern "C" int dpo_rmsnorm_workspace(int64_t rows, int64_t cols, int64_t *bytes)
     const int sms = sm_count();
     if (sms == 0)
         return call_fail(DPO_ECUDA, "%s: no device", what);
-    *bytes = backward_ctas(rows, cols, sms) * cols * 4;
+    *bytes = back_shape(rows, cols, sms).grid * cols * 4;
     return DPO_OK;
 }
 
@@ -851,7 +912,8 @@ extern "C" int dpo_rmsnorm_backward(const dpo_rmsnorm_backward_args *args, void 
     const int sms = sm_count();
     if (sms == 0)
         return call_fail(DPO_ECUDA, "%s: no device", what);
-    const int64_t grid = backward_ctas(a.rows, a.cols, sms);
+    const BackShape shape = back_shape(a.rows, a.cols, sms);
+    const int64_t grid = shape.grid;
     if (a.dweight != nullptr) {
         if (a.workspace == nullptr || a.workspace_bytes < grid * a.cols * 4)
             return call_fail(DPO_EINVAL, "%s: workspace of %lld bytes, %lld needed", what,
@@ -886,11 +948,11 @@ extern "C" int dpo_rmsnorm_backward(const dpo_rmsnorm_backward_args *args, void 
              aligned_to(a.weight, a.weight_dtype == DPO_F32 ? (v == 2 ? 8 : 16) : 2 * v) &&
              whole(codes, a.x8.ld_codes, 1, v)))
         v = v == 8 ? 2 : 1;
-    const NormBackArgs k = {a, row_warps(a.cols), static_cast<float *>(a.workspace)};
-    const int cta = k.warps > kMinWarps ? k.warps : kMinWarps;
-    const size_t smem = cta > k.warps ? (size_t)a.cols * 4 : 0;
-    rc = launch(what, pick<Back>(a.dtype, a.weight_dtype, v, cta * 32), grid, cta * 32,
-                smem, cuda_stream, k);
+    const NormBackArgs k = {a, shape.warps, static_cast<float *>(a.workspace)};
+    const size_t smem = shape.cta > shape.warps ? (size_t)a.cols * 4 : 0;
+    rc = launch(what, a.h != nullptr ? pick_back<BackH>(a.dtype, a.weight_dtype, v, shape.elems)
+                                     : pick_back<Back8>(a.dtype, a.weight_dtype, v, shape.elems),
+                grid, shape.cta * 32, smem, cuda_stream, k);
     if (rc != DPO_OK || a.dweight == nullptr)
         return rc;
     const int64_t sum_grid = (a.cols + 31) / 32;

@@ -16,15 +16,15 @@ gradients into ``opt.grads(i)``, which the next ``opt.step`` reads:
 Every step of it runs in libdpo.so's kernels; PyTorch provides memory and streams.
 Tensors are on the current CUDA device; their last dimension is contiguous and the
 others flatten to rows. Outputs are allocated unless given. Calls go to PyTorch's
-current stream, or to ``stream`` (a torch.cuda.Stream), on which the outputs and
+current stream, or to ``stream=`` (a torch.cuda.Stream), on which the outputs and
 workspaces are then allocated too; tensors last used on another stream need the usual
 event or ``wait_stream`` before the call. ValueError and TypeError for tensors that do
 not fit, DpoError for what the library refuses.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
+import functools
 from dataclasses import dataclass
 from typing import NamedTuple, Optional, Tuple
 
@@ -34,9 +34,12 @@ from . import dpo as _dpo
 from .dpo import (DPO_ACT_GELU, DPO_ACT_SILU, DPO_BF16, DPO_F32, DPO_KEEP_8BIT, DPO_KEEP_BF16,
                   DPO_KEEP_NONE, DPO_PACK8_GROUP as GROUP, dpo_packed8)
 
+_empty, _empty_like, _byref = torch.empty, torch.empty_like, ctypes.byref
+_f32, _bf16, _u8 = torch.float32, torch.bfloat16, torch.uint8
+
 ACTIVATIONS = {"silu": DPO_ACT_SILU, "gelu": DPO_ACT_GELU}
 KEEP = {"none": DPO_KEEP_NONE, "8bit": DPO_KEEP_8BIT, "bf16": DPO_KEEP_BF16}
-_DTYPES = {torch.float32: DPO_F32, torch.bfloat16: DPO_BF16}
+_DTYPES = {_f32: DPO_F32, _bf16: DPO_BF16}
 
 
 @dataclass(frozen=True)
@@ -78,35 +81,43 @@ class Kept:
 
 
 # ---------------------------------------------------------------- helpers --
+# Small calls are as long as their host side, so each check costs one attribute or two.
 
-def _on(stream):
-    """The context in which a call allocates."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+def _on_stream(call):
+    """``stream=`` of a call: it allocates and launches on that stream."""
+    @functools.wraps(call)
+    def on_stream(*args, stream=None, **kw):
+        if stream is None:
+            return call(*args, **kw)
+        with torch.cuda.stream(stream):
+            return call(*args, **kw)
+    return on_stream
+
+
+def _run(name: str, args) -> None:
+    _dpo._check(getattr(_dpo.load(), name)(_byref(args), _dpo._current_stream()), None)
 
 
 def _rows(t, name: str):
-    """t as (rows x cols) with contiguous rows, without a copy."""
+    """(pointer, rows, columns, pitch) of t as a matrix with contiguous rows, not copied."""
     if not t.is_cuda:
         raise ValueError(f"{name} is not a CUDA tensor")
-    if t.dim() == 2:
-        m = t
-    elif t.dim() == 0:
-        raise ValueError(f"{name} has no dimensions")
-    else:
+    if t.dim() != 2:
+        if t.dim() == 0:
+            raise ValueError(f"{name} has no dimensions")
         try:
-            m = t.view(-1, t.shape[-1])
+            t = t.view(-1, t.shape[-1])
         except RuntimeError:
             raise ValueError(f"{name}: leading dimensions do not flatten to rows") from None
-    if m.shape[1] > 1 and m.stride(1) != 1:
+    rows, cols = t.shape
+    if rows != 1 and t.is_contiguous():
+        return t.data_ptr(), rows, cols, cols
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         raise ValueError(f"{name}: the last dimension is not contiguous")
-    return m
-
-
-def _ld(m) -> int:
-    """Pitch. A single row may report any stride: one that no pitch can be is replaced."""
-    rows, cols = m.shape
-    ld = m.stride(0)
-    return ld if rows > 1 or (ld >= cols and ld % 16 == 0) else cols
+    if rows == 1 and not (ld >= cols and ld % 16 == 0):
+        ld = cols   # a single row may report any stride
+    return t.data_ptr(), rows, cols, ld
 
 
 def _dtype(t, name: str) -> int:
@@ -116,214 +127,216 @@ def _dtype(t, name: str) -> int:
     return d
 
 
-def _like(t, ref, name: str, shape=None, dtype=None):
-    if t.dtype != (dtype or ref.dtype):
-        raise TypeError(f"{name}: {t.dtype}, expected {dtype or ref.dtype}")
-    if tuple(t.shape) != tuple(ref.shape if shape is None else shape):
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected "
-                         f"{tuple(ref.shape if shape is None else shape)}")
-    if t.device != ref.device:
-        raise ValueError(f"{name} is on {t.device}, not {ref.device}")
-    return t
+def _fits(t, dtype, shape, device, name: str) -> None:
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: {t.dtype}, expected {dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not {device}")
 
 
-def _vector(t, n: int, ref, name: str):
-    if tuple(t.shape) != (n,) or (n > 1 and t.stride(0) != 1):
+def _vector(t, n: int, device, name: str) -> int:
+    """Pointer of n contiguous elements."""
+    if t.shape != (n,) or (n > 1 and t.stride(0) != 1):
         raise ValueError(f"{name}: expected {n} contiguous elements")
-    if t.device != ref.device:
-        raise ValueError(f"{name} is on {t.device}, not {ref.device}")
-    return t
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not {device}")
+    return t.data_ptr()
 
 
-def _matrix(t, rows: int, cols: int, ref, name: str, dtypes=(torch.bfloat16,)):
-    """A contiguous weight or gradient matrix."""
-    if t.dtype not in dtypes:
-        raise TypeError(f"{name}: {t.dtype}")
-    if tuple(t.shape) != (rows, cols) or not t.is_contiguous():
+def _matrix(t, rows: int, cols: int, dtype, device, name: str) -> int:
+    """Pointer of a contiguous weight or gradient matrix."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: {t.dtype}, expected {dtype}")
+    if t.shape != (rows, cols) or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous {rows} x {cols} matrix, "
                          f"got {tuple(t.shape)}")
-    if t.device != ref.device:
-        raise ValueError(f"{name} is on {t.device}, not {ref.device}")
-    return t
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not {device}")
+    return t.data_ptr()
 
 
-def _packed(p: Packed8, rows: int, cols: int, ref, name: str) -> dpo_packed8:
-    q, s = p.codes, p.scales
-    groups = -(-cols // GROUP)
-    for t, shape in ((q, (rows, cols)), (s, (rows, groups))):
-        if t.dtype != torch.uint8:
+def _packed(p: Packed8, rows: int, cols: int, device, name: str) -> dpo_packed8:
+    out = []
+    for t, n in ((p.codes, cols), (p.scales, -(-cols // GROUP))):
+        if t.dtype != _u8:
             raise TypeError(f"{name}: {t.dtype}, expected uint8")
-        if t.numel() != shape[0] * shape[1] or t.shape[-1] != shape[1]:
-            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
-        if t.device != ref.device:
-            raise ValueError(f"{name} is on {t.device}, not {ref.device}")
-    q, s = _rows(q, name), _rows(s, name)
-    return dpo_packed8(q.data_ptr(), s.data_ptr(), _ld(q), max(_ld(s), groups))
+        ptr, r, c, ld = _rows(t, name)
+        if r != rows or c != n:
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {(rows, n)}")
+        if t.device != device:
+            raise ValueError(f"{name} is on {t.device}, not {device}")
+        out += (ptr, ld)
+    return dpo_packed8(out[0], out[2], out[1], out[3])
 
 
-def _new_packed(rows: int, cols: int, device, pitch: int = 1) -> Packed8:
+def _new_packed(rows: int, cols: int, device, pitch: int = 1):
     """Buffers of a rows x cols matrix in 8 bits, the codes' pitch a multiple of ``pitch``."""
-    ld = -(-cols // pitch) * pitch
-    codes = torch.empty((rows, ld), dtype=torch.uint8, device=device)
-    return Packed8(codes if ld == cols else codes[:, :cols],
-                   torch.empty((rows, -(-cols // GROUP)), dtype=torch.uint8, device=device))
+    ld, groups = -(-cols // pitch) * pitch, -(-cols // GROUP)
+    codes = _empty((rows, ld), dtype=_u8, device=device)
+    scales = _empty((rows, groups), dtype=_u8, device=device)
+    return (Packed8(codes if ld == cols else codes[:, :cols], scales),
+            dpo_packed8(codes.data_ptr(), scales.data_ptr(), ld, groups))
+
+
+def _new(ref):
+    """An uninitialised tensor of ref's shape, contiguous."""
+    return (_empty_like(ref) if ref.is_contiguous()
+            else _empty(ref.shape, dtype=ref.dtype, device=ref.device))
+
+
+# Sizes alone decide these.
+_norm_workspace = functools.lru_cache(256)(
+    lambda device, rows, cols: _dpo.dpo_rmsnorm_workspace(rows, cols))
+_ffn_workspace = functools.lru_cache(256)(_dpo.dpo_ffn_workspace)
 
 
 # ----------------------------------------------------- activations, 8 bits --
 
-def pack8(x, *, stream=None) -> Packed8:
+@_on_stream
+def pack8(x) -> Packed8:
     """x (fp32 or bf16, any leading dimensions) in 8 bits."""
-    m = _rows(x, "x")
+    ptr, rows, cols, ld = _rows(x, "x")
     dt = _dtype(x, "x")
-    rows, cols = m.shape
-    with _on(stream):
-        p = _new_packed(rows, cols, x.device)
-        _dpo.dpo_pack8(m, dt, rows, cols, _ld(m),
-                       dpo_packed8(p.codes.data_ptr(), p.scales.data_ptr(), cols,
-                                   p.scales.shape[1]), stream)
+    p, q = _new_packed(rows, cols, x.device)
+    _dpo._check(_dpo.load().dpo_pack8(ptr, dt, rows, cols, ld, _byref(q), _dpo._current_stream()),
+                None)
     return p
 
 
-def unpack8(p: Packed8, *, dtype=torch.bfloat16, out=None, stream=None):
+@_on_stream
+def unpack8(p: Packed8, *, dtype=_bf16, out=None):
     """The values p stands for (bf16 holds them exactly)."""
     rows, cols = p.codes.shape
-    q = _packed(p, rows, cols, p.codes, "p")
-    with _on(stream):
-        if out is None:
-            out = torch.empty((rows, cols), dtype=dtype, device=p.codes.device)
-        else:
-            _like(out, p.codes, "out", dtype=out.dtype)
-        m = _rows(out, "out")
-        _dpo.dpo_unpack8(q, rows, cols, m, _dtype(out, "out"), _ld(m), stream)
+    q = _packed(p, rows, cols, p.codes.device, "p")
+    if out is None:
+        out = _empty((rows, cols), dtype=dtype, device=p.codes.device)
+    else:
+        _fits(out, out.dtype, p.codes.shape, p.codes.device, "out")
+    ptr, _, _, ld = _rows(out, "out")
+    _dpo._check(_dpo.load().dpo_unpack8(_byref(q), rows, cols, ptr, _dtype(out, "out"), ld,
+                                        _dpo._current_stream()), None)
     return out
 
 
 # -------------------------------------------------------------------- norm --
 
-def add_rms_norm(x, weight, residual=None, *, eps: float = 1e-5, save8: bool = False,
-                 stream=None) -> NormOut:
+@_on_stream
+def add_rms_norm(x, weight, residual=None, *, eps: float = 1e-5, save8: bool = False) -> NormOut:
     """s = x + residual, y = s / rms(s) * weight per row, with what the backward needs:
     rstd and either h (s in x's type) or, with ``save8``, the normalised rows in 8 bits."""
-    m = _rows(x, "x")
-    dt = _dtype(x, "x")
-    rows, cols = m.shape
-    _vector(weight, cols, x, "weight")
-    a = _dpo.dpo_rmsnorm_args()
-    r = None
+    px, rows, cols, ld_x = _rows(x, "x")
+    dt, device = _dtype(x, "x"), x.device
+    pw = _vector(weight, cols, device, "weight")
+    pr = ld_r = ph = None
+    h = x
     if residual is not None:
-        r = _rows(_like(residual, x, "residual"), "residual")
-        a.residual, a.ld_residual = r.data_ptr(), _ld(r)
-    with _on(stream):
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        h = x if r is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-        x8 = None
-        if save8:
-            x8 = _new_packed(rows, cols, x.device)
-            a.x8 = dpo_packed8(x8.codes.data_ptr(), x8.scales.data_ptr(), cols,
-                               x8.scales.shape[1])
-        a.x, a.weight, a.y, a.rstd = m.data_ptr(), weight.data_ptr(), y.data_ptr(), rstd.data_ptr()
-        a.ld_x, a.ld_y, a.ld_h = _ld(m), cols, cols
-        if r is not None:
-            a.h = h.data_ptr()
-        a.rows, a.cols, a.eps, a.dtype, a.weight_dtype = rows, cols, eps, dt, _dtype(weight, "weight")
-        _dpo.dpo_rmsnorm(a, stream)
+        _fits(residual, x.dtype, x.shape, device, "residual")
+        pr, _, _, ld_r = _rows(residual, "residual")
+        h = _new(x)
+        ph = h.data_ptr()
+    y = _new(x)
+    rstd = _empty(rows, dtype=_f32, device=device)
+    x8, q = _new_packed(rows, cols, device) if save8 else (None, _NO_PACKED)
+    _run("dpo_rmsnorm", _dpo.dpo_rmsnorm_args(
+        px, pr, pw, ph, y.data_ptr(), rstd.data_ptr(), q, rows, cols, ld_x, ld_r or cols, cols, cols,
+        eps, dt, _dtype(weight, "weight")))
     return NormOut(y, h, rstd, x8)
 
 
+_NO_PACKED = dpo_packed8()
+
+
+@_on_stream
 def add_rms_norm_backward(dy, weight, rstd, *, h=None, x8: Optional[Packed8] = None, dh=None,
-                          dweight=None, accumulate: bool = False, stream=None):
+                          dweight=None, accumulate: bool = False):
     """(dx, dweight) from the forward's h or x8; dx is the gradient of x and of residual
     alike. ``dh``: the gradient that reaches the sum past the norm. ``dweight``: the
     buffer to write (fp32 or bf16), or with ``accumulate`` to add to; fp32 by default."""
     if (h is None) == (x8 is None):
         raise ValueError("give one of h and x8")
-    m = _rows(dy, "dy")
-    dt = _dtype(dy, "dy")
-    rows, cols = m.shape
-    _vector(weight, cols, dy, "weight")
-    if rstd.dtype != torch.float32:
+    if accumulate and dweight is None:
+        raise ValueError("accumulate needs a dweight to add to")
+    pdy, rows, cols, ld_dy = _rows(dy, "dy")
+    dt, device = _dtype(dy, "dy"), dy.device
+    pw = _vector(weight, cols, device, "weight")
+    if rstd.dtype != _f32:
         raise TypeError(f"rstd: {rstd.dtype}, expected float32")
-    _vector(rstd, rows, dy, "rstd")
-    a = _dpo.dpo_rmsnorm_backward_args()
+    prstd = _vector(rstd, rows, device, "rstd")
+    ph = pdh = None
+    ld_h = ld_dh = cols
+    q = _NO_PACKED
     if h is not None:
-        hm = _rows(_like(h, dy, "h"), "h")
-        a.h, a.ld_h = hm.data_ptr(), _ld(hm)
+        _fits(h, dy.dtype, dy.shape, device, "h")
+        ph, _, _, ld_h = _rows(h, "h")
     else:
-        a.x8 = _packed(x8, rows, cols, dy, "x8")
+        q = _packed(x8, rows, cols, device, "x8")
     if dh is not None:
-        dm = _rows(_like(dh, dy, "dh"), "dh")
-        a.dh, a.ld_dh = dm.data_ptr(), _ld(dm)
-    with _on(stream):
-        dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
-        if dweight is None:
-            if accumulate:
-                raise ValueError("accumulate needs a dweight to add to")
-            dweight = torch.empty(cols, dtype=torch.float32, device=dy.device)
-        _vector(dweight, cols, dy, "dweight")
-        n = _dpo.dpo_rmsnorm_workspace(rows, cols)
-        ws = torch.empty(n, dtype=torch.uint8, device=dy.device)
-        a.dy, a.rstd, a.weight = m.data_ptr(), rstd.data_ptr(), weight.data_ptr()
-        a.dx, a.dweight = dx.data_ptr(), dweight.data_ptr()
-        a.rows, a.cols, a.ld_dy, a.ld_dx = rows, cols, _ld(m), cols
-        a.dtype, a.weight_dtype = dt, _dtype(weight, "weight")
-        a.dweight_dtype, a.accumulate = _dtype(dweight, "dweight"), 1 if accumulate else 0
-        a.workspace, a.workspace_bytes = ws.data_ptr(), n
-        _dpo.dpo_rmsnorm_backward(a, stream)
+        _fits(dh, dy.dtype, dy.shape, device, "dh")
+        pdh, _, _, ld_dh = _rows(dh, "dh")
+    if dweight is None:
+        dweight = _empty(cols, dtype=_f32, device=device)
+    pdw = _vector(dweight, cols, device, "dweight")
+    dx = _new(dy)
+    n = _norm_workspace(device, rows, cols)
+    ws = _empty(n, dtype=_u8, device=device)
+    _run("dpo_rmsnorm_backward", _dpo.dpo_rmsnorm_backward_args(
+        pdy, ph, q, prstd, pw, pdh, dx.data_ptr(), pdw, rows, cols, ld_dy, ld_h, ld_dh, cols, dt,
+        _dtype(weight, "weight"), _dtype(dweight, "dweight"), 1 if accumulate else 0,
+        ws.data_ptr(), n))
     return dx, dweight
 
 
 # ------------------------------------------------- gated feed-forward block --
 
 def _sizes(x, w_gate, w_up, w_down, name: str):
-    m = _rows(x, name)
-    if x.dtype != torch.bfloat16:
+    """(pointer, pitch, tokens, dim, hidden, the weights' pointers)."""
+    px, tokens, dim, ld = _rows(x, name)
+    if x.dtype != _bf16:
         raise TypeError(f"{name}: {x.dtype} (bfloat16)")
-    tokens, dim = m.shape
-    hidden = w_gate.shape[0]
-    _matrix(w_gate, hidden, dim, x, "w_gate")
-    _matrix(w_up, hidden, dim, x, "w_up")
-    _matrix(w_down, dim, hidden, x, "w_down")
-    return m, tokens, dim, hidden
+    device, hidden = x.device, w_gate.shape[0]
+    return px, ld, tokens, dim, hidden, (_matrix(w_gate, hidden, dim, _bf16, device, "w_gate"),
+                                         _matrix(w_up, hidden, dim, _bf16, device, "w_up"),
+                                         _matrix(w_down, dim, hidden, _bf16, device, "w_down"))
 
 
-def gated_ffn(x, w_gate, w_up, w_down, *, activation: str = "silu", keep: str = "8bit", out=None,
-              stream=None) -> Tuple[torch.Tensor, Optional[Kept]]:
+@_on_stream
+def gated_ffn(x, w_gate, w_up, w_down, *, activation: str = "silu", keep: str = "8bit",
+              out=None) -> Tuple[torch.Tensor, Optional[Kept]]:
     """(out, kept): out = (act(x w_gate^T) * (x w_up^T)) w_down^T in bf16, with fp32
     accumulation. ``keep``: what is kept of the two projections for the backward, "8bit",
     "bf16" or "none" (kept is then None)."""
     act, kp = ACTIVATIONS.get(activation), KEEP.get(keep)
     if act is None or kp is None:
         raise ValueError(f"activation {activation!r}, keep {keep!r}")
-    m, tokens, dim, hidden = _sizes(x, w_gate, w_up, w_down, "x")
-    a = _dpo.dpo_ffn_args()
-    kept = None
-    with _on(stream):
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        om = _rows(_like(out, x, "out"), "out")
-        if kp == DPO_KEEP_8BIT:
-            g, u = (_new_packed(tokens, hidden, x.device, 16) for _ in range(2))
-            a.gate8, a.up8 = (_packed(p, tokens, hidden, x, "kept") for p in (g, u))
-            kept = Kept(g, u, activation, keep)
-        elif kp == DPO_KEEP_BF16:
-            g, u = (torch.empty((tokens, hidden), dtype=x.dtype, device=x.device)
-                    for _ in range(2))
-            a.gate, a.up = g.data_ptr(), u.data_ptr()
-            kept = Kept(g, u, activation, keep)
-        n, _ = _dpo.dpo_ffn_workspace(tokens, dim, hidden)
-        ws = torch.empty(n, dtype=torch.uint8, device=x.device)
-        a.x, a.w_gate, a.w_up, a.w_down = (t.data_ptr() for t in (m, w_gate, w_up, w_down))
-        a.out, a.tokens, a.dim, a.hidden = om.data_ptr(), tokens, dim, hidden
-        a.ld_x, a.ld_out, a.act, a.keep = _ld(m), _ld(om), act, kp
-        a.workspace, a.workspace_bytes = ws.data_ptr(), n
-        _dpo.dpo_ffn_forward(a, stream)
+    px, ld, tokens, dim, hidden, w = _sizes(x, w_gate, w_up, w_down, "x")
+    n, _ = _ffn_workspace(tokens, dim, hidden)
+    device = x.device
+    if out is None:
+        out = _new(x)
+    else:
+        _fits(out, _bf16, x.shape, device, "out")
+    po, _, _, ld_out = _rows(out, "out")
+    kept, pg, pu, g8, u8 = None, None, None, _NO_PACKED, _NO_PACKED
+    if kp == DPO_KEEP_8BIT:
+        g, g8 = _new_packed(tokens, hidden, device, 16)
+        u, u8 = _new_packed(tokens, hidden, device, 16)
+        kept = Kept(g, u, activation, keep)
+    elif kp == DPO_KEEP_BF16:
+        g = _empty((tokens, hidden), dtype=_bf16, device=device)
+        u = _empty_like(g)
+        pg, pu = g.data_ptr(), u.data_ptr()
+        kept = Kept(g, u, activation, keep)
+    ws = _empty(n, dtype=_u8, device=device)
+    _run("dpo_ffn_forward", _dpo.dpo_ffn_args(px, *w, po, pg, pu, g8, u8, tokens, dim, hidden, ld,
+                                              ld_out, act, kp, ws.data_ptr(), n))
     return out, kept
 
 
+@_on_stream
 def gated_ffn_backward(dout, kept: Kept, w_gate, w_up, w_down, dw_gate, dw_up, dw_down, *, x=None,
-                       x8: Optional[Packed8] = None, gain=None, accumulate: bool = False,
-                       dx=None, stream=None):
+                       x8: Optional[Packed8] = None, gain=None, accumulate: bool = False, dx=None):
     """dx, and the weights' gradients written into dw_gate, dw_up and dw_down (all fp32 or
     all bf16, ``opt.grads(i)`` reshaped), or with ``accumulate`` added to them. The block's
     input is ``x``, or the 8-bit rows ``x8`` times ``gain`` (add_rms_norm's x8 and weight)."""
@@ -333,38 +346,38 @@ def gated_ffn_backward(dout, kept: Kept, w_gate, w_up, w_down, dw_gate, dw_up, d
         raise ValueError("gain goes with x8")
     if kept is None:
         raise ValueError("the forward kept nothing (keep='none')")
-    m, tokens, dim, hidden = _sizes(dout, w_gate, w_up, w_down, "dout")
-    a = _dpo.dpo_ffn_backward_args()
-    grads = (torch.bfloat16, torch.float32)
-    _matrix(dw_gate, hidden, dim, dout, "dw_gate", grads)
-    for t, shape, name in ((dw_up, (hidden, dim), "dw_up"), (dw_down, (dim, hidden), "dw_down")):
-        _matrix(t, *shape, dout, name, (dw_gate.dtype,))
+    pd, ld, tokens, dim, hidden, w = _sizes(dout, w_gate, w_up, w_down, "dout")
+    device, gdt = dout.device, dw_gate.dtype
+    dt = _dtype(dw_gate, "dw_gate")
+    dw = (_matrix(dw_gate, hidden, dim, gdt, device, "dw_gate"),
+          _matrix(dw_up, hidden, dim, gdt, device, "dw_up"),
+          _matrix(dw_down, dim, hidden, gdt, device, "dw_down"))
+    px = pgain = pg = pu = None
+    ld_x, gain_dt, q, g8, u8 = dim, 0, _NO_PACKED, _NO_PACKED, _NO_PACKED
     if x is not None:
-        xm = _rows(_like(x, dout, "x"), "x")
-        a.x, a.ld_x = xm.data_ptr(), _ld(xm)
+        _fits(x, _bf16, dout.shape, device, "x")
+        px, _, _, ld_x = _rows(x, "x")
     else:
-        a.x8 = _packed(x8, tokens, dim, dout, "x8")
+        q = _packed(x8, tokens, dim, device, "x8")
         if gain is not None:
-            a.gain, a.gain_dtype = _vector(gain, dim, dout, "gain").data_ptr(), _dtype(gain, "gain")
+            pgain, gain_dt = _vector(gain, dim, device, "gain"), _dtype(gain, "gain")
     if kept.keep == "8bit":
-        a.gate8, a.up8 = (_packed(p, tokens, hidden, dout, "kept") for p in (kept.gate, kept.up))
+        g8 = _packed(kept.gate, tokens, hidden, device, "kept")
+        u8 = _packed(kept.up, tokens, hidden, device, "kept")
     else:
-        a.gate, a.up = (_matrix(t, tokens, hidden, dout, "kept").data_ptr()
-                        for t in (kept.gate, kept.up))
-    with _on(stream):
-        if dx is None:
-            dx = torch.empty(dout.shape, dtype=dout.dtype, device=dout.device)
-        dxm = _rows(_like(dx, dout, "dx"), "dx")
-        _, n = _dpo.dpo_ffn_workspace(tokens, dim, hidden, x8 is not None)
-        ws = torch.empty(n, dtype=torch.uint8, device=dout.device)
-        a.dout, a.w_gate, a.w_up, a.w_down = (t.data_ptr() for t in (m, w_gate, w_up, w_down))
-        a.dx, a.dw_gate, a.dw_up, a.dw_down = (t.data_ptr() for t in (dxm, dw_gate, dw_up, dw_down))
-        a.tokens, a.dim, a.hidden = tokens, dim, hidden
-        a.ld_dout, a.ld_dx = _ld(m), _ld(dxm)
-        a.act, a.keep = ACTIVATIONS[kept.activation], KEEP[kept.keep]
-        a.grad_dtype, a.accumulate = _DTYPES[dw_gate.dtype], 1 if accumulate else 0
-        a.workspace, a.workspace_bytes = ws.data_ptr(), n
-        _dpo.dpo_ffn_backward(a, stream)
+        pg = _matrix(kept.gate, tokens, hidden, _bf16, device, "kept")
+        pu = _matrix(kept.up, tokens, hidden, _bf16, device, "kept")
+    _, n = _ffn_workspace(tokens, dim, hidden, x8 is not None)
+    if dx is None:
+        dx = _new(dout)
+    else:
+        _fits(dx, _bf16, dout.shape, device, "dx")
+    pdx, _, _, ld_dx = _rows(dx, "dx")
+    ws = _empty(n, dtype=_u8, device=device)
+    _run("dpo_ffn_backward", _dpo.dpo_ffn_backward_args(
+        pd, px, q, pgain, *w, pg, pu, g8, u8, pdx, *dw, tokens, dim, hidden, ld, ld_x, ld_dx,
+        ACTIVATIONS[kept.activation], KEEP[kept.keep], dt, gain_dt, 1 if accumulate else 0,
+        ws.data_ptr(), n))
     return dx
 
 
