@@ -244,6 +244,27 @@ __device__ __forceinline__ float load_scale_byte(const uint8_t *p)
     return scale_of(v);
 }
 
+// Scale byte of the first n of 32 values that one lane holds; infinities become NaN (rare:
+// looked for only where the maximum, which passes over NaN, found one).
+__device__ __forceinline__ uint32_t row_scale(float (&v)[32], int n)
+{
+    float a = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+        if (j < n)
+            a = fmaxf(a, fabsf(v[j]));
+    if (a > kMaxFinite) {
+        a = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            if (j < n)
+                a = fmaxf(a, finite_abs(v[j]));
+            v[j] = inf_to_nan(v[j]);
+        }
+    }
+    return scale_byte(a);
+}
+
 // What one epilogue warp stages and stores: 32 x 32 chunks through two buffers in
 // turn. Each chunk is a bulk async-group of its own, so a buffer is free once all
 // groups but the last one have been read.
@@ -302,15 +323,10 @@ struct Stager {
         end(map, buf, x, y);
         turn = 0;
     }
-    // 32 rows of 32 codes; returns this row's scale byte
-    __device__ __forceinline__ uint32_t codes(const CUtensorMap *map, const float (&v)[32], int x,
-                                              int y)
+    // 32 rows of 32 codes; returns this row's scale byte. v is taken over.
+    __device__ __forceinline__ uint32_t codes(const CUtensorMap *map, float (&v)[32], int x, int y)
     {
-        float amax = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-            amax = fmaxf(amax, finite_abs(v[j]));
-        const uint32_t s = scale_byte(amax);
+        const uint32_t s = row_scale(v, 32);
         const float inv = inv_scale_of(s);
         const uint32_t b = begin();
 #pragma unroll
@@ -319,8 +335,7 @@ struct Stager {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int i = g * 16 + 4 * j;
-                w[j] = encode4(inf_to_nan(v[i]) * inv, inf_to_nan(v[i + 1]) * inv,
-                               inf_to_nan(v[i + 2]) * inv, inf_to_nan(v[i + 3]) * inv);
+                w[j] = encode4(v[i] * inv, v[i + 1] * inv, v[i + 2] * inv, v[i + 3] * inv);
             }
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
                              b + (uint32_t)(lane * 32 + g * 16)),
@@ -418,8 +433,15 @@ __device__ __forceinline__ void drain(const Product &P, Stager &st, uint32_t acc
             st.bf16(&P.d1, g, col0, row0);
             st.bf16(&P.d2, u, col0, row0);
         } else if (P.keep == kKeep8) {
-            const uint32_t sg = st.codes(&P.d1, g, col0, row0);
-            const uint32_t su = st.codes(&P.d2, u, col0, row0);
+            float q[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                q[j] = g[j];
+            const uint32_t sg = st.codes(&P.d1, q, col0, row0);
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                q[j] = u[j];
+            const uint32_t su = st.codes(&P.d2, q, col0, row0);
             if (row0 + st.lane < P.m) {
                 const int64_t at = row * P.ld_scale + col0 / kGroup;
                 P.scale_g[at] = (uint8_t)sg;
@@ -599,23 +621,20 @@ __device__ __forceinline__ void store_row(__nv_bfloat16 *p, const float (&v)[32]
 
 __device__ __forceinline__ void store_codes(uint8_t *p, uint8_t *scale, const float (&v)[32], int n)
 {
-    float amax = 0.0f;
+    float q[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j)
-        if (j < n)
-            amax = fmaxf(amax, finite_abs(v[j]));
-    const uint32_t s = scale_byte(amax);
+        q[j] = v[j];
+    const uint32_t s = row_scale(q, n);
     const float inv = inv_scale_of(s);
     *scale = (uint8_t)s;
 #pragma unroll
     for (int g = 0; g < 4; ++g)
         if (g * 8 < n) {
-            const float *w = v + g * 8;
-            *reinterpret_cast<uint2 *>(p + g * 8) = make_uint2(
-                encode4(inf_to_nan(w[0]) * inv, inf_to_nan(w[1]) * inv, inf_to_nan(w[2]) * inv,
-                        inf_to_nan(w[3]) * inv),
-                encode4(inf_to_nan(w[4]) * inv, inf_to_nan(w[5]) * inv, inf_to_nan(w[6]) * inv,
-                        inf_to_nan(w[7]) * inv));
+            const float *w = q + g * 8;
+            *reinterpret_cast<uint2 *>(p + g * 8) =
+                make_uint2(encode4(w[0] * inv, w[1] * inv, w[2] * inv, w[3] * inv),
+                           encode4(w[4] * inv, w[5] * inv, w[6] * inv, w[7] * inv));
         }
 }
 

@@ -33,10 +33,11 @@ __device__ __forceinline__ float inv_scale_of(uint32_t byte)
 }
 
 // Magnitude that counts for the scale: 0 for infinities and NaN.
+constexpr float kMaxFinite = 3.402823466e38f;
 __device__ __forceinline__ float finite_abs(float v)
 {
     const float a = fabsf(v);
-    return a <= 3.402823466e38f ? a : 0.0f;
+    return a <= kMaxFinite ? a : 0.0f;
 }
 
 // What is encoded: an infinity, which E4M3 has no code for, as NaN.

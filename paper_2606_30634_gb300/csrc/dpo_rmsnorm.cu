@@ -135,14 +135,14 @@ template <int V> struct Codes {
     __device__ __forceinline__ void set(const float (&v)[V], float inv)
     {
         if constexpr (V == 1) {
-            w[0] = encode2(inf_to_nan(v[0]) * inv, 0.0f) & 0xFFu;
+            w[0] = encode2(v[0] * inv, 0.0f) & 0xFFu;
         } else if constexpr (V == 2) {
-            w[0] = encode2(inf_to_nan(v[0]) * inv, inf_to_nan(v[1]) * inv);
+            w[0] = encode2(v[0] * inv, v[1] * inv);
         } else {
 #pragma unroll
             for (int i = 0; i < V / 4; ++i)
-                w[i] = encode4(inf_to_nan(v[4 * i]) * inv, inf_to_nan(v[4 * i + 1]) * inv,
-                               inf_to_nan(v[4 * i + 2]) * inv, inf_to_nan(v[4 * i + 3]) * inv);
+                w[i] = encode4(v[4 * i] * inv, v[4 * i + 1] * inv, v[4 * i + 2] * inv,
+                               v[4 * i + 3] * inv);
         }
     }
     __device__ __forceinline__ void get(float (&v)[V], float scale) const
@@ -157,25 +157,39 @@ template <int V> struct Codes {
     }
 };
 
-__device__ __forceinline__ float load_scale(const uint8_t *p)
+__device__ __forceinline__ uint16_t load_byte(const uint8_t *p)
 {
     uint16_t v;
     asm volatile("ld.global.u8 %0, [%1];" : "=h"(v) : "l"(p));
-    return scale_of(v);
+    return v;
 }
+__device__ __forceinline__ float load_scale(const uint8_t *p) { return scale_of(load_byte(p)); }
 
-// Largest finite magnitude of a group whose V-element pieces lie in adjacent lanes.
+// Scale byte of a group whose V-element pieces lie in adjacent lanes; infinities become NaN
+// in v. The maximum passes over NaN by itself, and infinities, which must not count, are
+// looked for only where it found one.
 template <int V>
-__device__ __forceinline__ float group_amax(const float (&v)[V])
+__device__ __forceinline__ uint32_t group_scale(float (&v)[V])
 {
     float a = 0.0f;
 #pragma unroll
     for (int i = 0; i < V; ++i)
-        a = fmaxf(a, finite_abs(v[i]));
+        a = fmaxf(a, fabsf(v[i]));
 #pragma unroll
     for (int off = 1; off < kGroup / V; off <<= 1)
         a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, off));
-    return a;
+    if (__any_sync(0xFFFFFFFFu, a > kMaxFinite)) {
+        a = 0.0f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            a = fmaxf(a, finite_abs(v[i]));
+            v[i] = inf_to_nan(v[i]);
+        }
+#pragma unroll
+        for (int off = 1; off < kGroup / V; off <<= 1)
+            a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, off));
+    }
+    return scale_byte(a);
 }
 
 __device__ __forceinline__ float warp_sum(float v)
@@ -287,7 +301,7 @@ rmsnorm_kernel(const NormForwardArgs args)
             o.store(yp + c);
         }
         if (a.x8.codes != nullptr) {   // uniform: every lane takes part in the shuffles
-            const uint32_t b = scale_byte(group_amax<V>(s[n]));
+            const uint32_t b = group_scale<V>(s[n]);
             if (in) {
                 Codes<V> q;
                 q.set(s[n], inv_scale_of(b));
@@ -301,25 +315,41 @@ rmsnorm_kernel(const NormForwardArgs args)
 
 // Backward: a persistent grid of CTAs walks the rows; a thread keeps the sums of
 // dy n of its columns in registers, so dweight costs one partial row per CTA,
-// which the second kernel adds up. A row is one pass of loads, a sum over the
-// row's threads and the stores; the next row's loads are issued before the sum of
-// this one, or each row would wait for HBM by itself.
+// which the second kernel adds up. A row is its inputs' loads, a sum over the row's
+// threads and the stores; what bounds it is how many rows' inputs are on their way at
+// once, since HBM answers after about 2 us under load and a row is 12 to 24 bytes a
+// column. With 16-byte pieces (RING) each thread copies its own pieces of the next three
+// rows to shared memory with cp.async, in places that only it reads, so no barrier
+// guards them. GB300, 8192 x 4096 from 8-bit rows: one row ahead in registers 65 us.
 struct NormBackArgs {
     dpo_rmsnorm_backward_args a;
     int warps;
     float *partials;                          // one row of cols per CTA
 };
 
-// E elements of a row per thread: 16, so that this row's and the next one's inputs, the
-// weights and the sums fit its registers, or 32 where that would take more than 512
-// threads (cols above 8192; the next row is not loaded ahead then, nor in the narrow
-// forms, whose pieces are many).
+// E elements of a row per thread: 16, or 32 where that would take more than 512 threads
+// (cols above 8192).
 constexpr int kBackElems = 16, kBackThreads = 512;
+constexpr int kDepth = 4;                     // rows of the ring
 
-// What a row's thread loads: dy, h or the codes and scales, dh.
-template <class T, int V, int E, bool X8> struct RowIn {
+// B bytes from global to shared memory, or zeros.
+template <int B>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void *src, bool in)
+{
+    const int n = in ? B : 0;
+    if (B == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n)
+                     : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(B),
+                     "r"(n)
+                     : "memory");
+}
+
+// A row's inputs as one thread holds them: dy, dh, and h or the codes and scales.
+template <class T, int V, int E, bool X8> struct RowRegs {
     static constexpr int N = E / V;
-    Vec<T, V> dy[N], dh[N];
+    Vec<T, V> dy_[N], dh_[N];
     Vec<T, X8 ? 1 : V> h[X8 ? 1 : N];
     Codes<V> q[X8 ? N : 1];
     float scale[X8 ? N : 1];
@@ -334,12 +364,12 @@ template <class T, int V, int E, bool X8> struct RowIn {
         for (int n = 0; n < N; ++n) {
             const int c = (i0 + n * tpr) * V;
             const bool in = live && c < (int)a.cols;
-            dy[n].zero();
-            dh[n].zero();
+            dy_[n].zero();
+            dh_[n].zero();
             if (in) {
-                dy[n].load(static_cast<const T *>(a.dy) + row * a.ld_dy + c);
+                dy_[n].load(static_cast<const T *>(a.dy) + row * a.ld_dy + c);
                 if (a.dh != nullptr)
-                    dh[n].load(static_cast<const T *>(a.dh) + row * a.ld_dh + c);
+                    dh_[n].load(static_cast<const T *>(a.dh) + row * a.ld_dh + c);
             }
             if constexpr (X8) {
 #pragma unroll
@@ -357,7 +387,8 @@ template <class T, int V, int E, bool X8> struct RowIn {
             }
         }
     }
-    // the normalised values of piece n
+    __device__ __forceinline__ Vec<T, V> dy(int n) const { return dy_[n]; }
+    __device__ __forceinline__ Vec<T, V> dh(int n) const { return dh_[n]; }
     __device__ __forceinline__ void normalised(int n, float (&v)[V]) const
     {
         if constexpr (X8) {
@@ -370,14 +401,99 @@ template <class T, int V, int E, bool X8> struct RowIn {
     }
 };
 
-template <class T, class WT, int V, int E, bool X8>
+// The same from a slot of the ring: pieces of dy, dh, and h or the codes, each [n][thread].
+// rstd and the scales, single bytes, wait in registers.
+template <class T, int V, int E, bool X8> struct RowSlot {
+    static constexpr int N = E / V, B = V * (int)sizeof(T), BH = X8 ? V : B;
+    static __host__ __device__ constexpr int bytes(int threads) { return N * (2 * B + BH) * threads; }
+    uint8_t *slot;             // of this thread's first piece of dy
+    int threads;
+    float rstd;
+    uint16_t scale[X8 ? N : 1];   // as loaded: converting it here would wait for it
+
+    __device__ __forceinline__ const uint8_t *piece(int kind, int n) const
+    {
+        const uint8_t *base = slot + (int)threadIdx.x * (kind == 2 ? BH : B);
+        return base + threads * ((kind == 2 ? 2 * N * B + n * BH : (kind * N + n) * B));
+    }
+    __device__ __forceinline__ void load(const dpo_rmsnorm_backward_args &a, int64_t row, int i0,
+                                         int tpr)
+    {
+        const bool live = row < a.rows;
+        rstd = live ? ld1(a.rstd + row) : 0.0f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int c = (i0 + n * tpr) * V;
+            const bool in = live && c < (int)a.cols;
+            auto to = [&](int kind) { return (uint32_t)__cvta_generic_to_shared(piece(kind, n)); };
+            // nothing is read for a piece that is not there: its address is the matrix's
+            const int64_t r = in ? row : 0;
+            const int at = in ? c : 0;
+            copy_async<B>(to(0), static_cast<const T *>(a.dy) + r * a.ld_dy + at, in);
+            if (a.dh != nullptr)
+                copy_async<B>(to(1), static_cast<const T *>(a.dh) + r * a.ld_dh + at, in);
+            if constexpr (X8) {
+                copy_async<BH>(to(2), a.x8.codes + r * a.x8.ld_codes + at, in);
+                scale[n] = 0;
+                if (in)
+                    scale[n] = load_byte(a.x8.scales + row * a.x8.ld_scales + c / kGroup);
+            } else {
+                copy_async<BH>(to(2), static_cast<const T *>(a.h) + r * a.ld_h + at, in);
+            }
+        }
+    }
+    template <class P> __device__ __forceinline__ P get(int kind, int n) const
+    {
+        return *reinterpret_cast<const P *>(piece(kind, n));
+    }
+    struct alignas(B) Raw { uint32_t w[words(B)]; };
+    struct alignas(BH) RawH { uint32_t w[words(BH)]; };
+    __device__ __forceinline__ Vec<T, V> dy(int n) const
+    {
+        const Raw r = get<Raw>(0, n);
+        Vec<T, V> v;
+#pragma unroll
+        for (int i = 0; i < words(B); ++i)
+            v.w[i] = r.w[i];
+        return v;
+    }
+    __device__ __forceinline__ Vec<T, V> dh(int n) const
+    {
+        const Raw r = get<Raw>(1, n);
+        Vec<T, V> v;
+#pragma unroll
+        for (int i = 0; i < words(B); ++i)
+            v.w[i] = r.w[i];
+        return v;
+    }
+    __device__ __forceinline__ void normalised(int n, float (&v)[V]) const
+    {
+        const RawH r = get<RawH>(2, n);
+        if constexpr (X8) {
+            Codes<V> q;
+#pragma unroll
+            for (int i = 0; i < words(BH); ++i)
+                q.w[i] = r.w[i];
+            q.get(v, scale_of(scale[n]));
+        } else {
+            Vec<T, V> h;
+#pragma unroll
+            for (int i = 0; i < words(BH); ++i)
+                h.w[i] = r.w[i];
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                v[j] = h.get(j) * rstd;
+        }
+    }
+};
+
+template <class T, class WT, int V, int E, bool X8, bool RING>
 __global__ void __launch_bounds__(kBackThreads)
 rmsnorm_backward_kernel(const NormBackArgs args)
 {
     constexpr int N = E / V;
-    constexpr bool kAhead = V >= 4 && E == kBackElems;
     __shared__ float red[2][32];              // by the row's parity: one barrier a row
-    extern __shared__ float dw_cta[];         // cols, with several rows per CTA
+    extern __shared__ __align__(16) uint8_t smem[];   // the ring; at the end, cols floats
     const dpo_rmsnorm_backward_args &a = args.a;
     const int warps = args.warps, tpr = warps * 32;
     const int rows_cta = (int)blockDim.x / tpr;
@@ -398,27 +514,19 @@ rmsnorm_backward_kernel(const NormBackArgs args)
         for (int j = 0; j < V; ++j)
             dw[n][j] = 0.0f;
     }
-    RowIn<T, V, E, X8> next;
-    int64_t base = (int64_t)blockIdx.x * rows_cta;
-    if (kAhead)
-        next.load(a, base + r0, i0, tpr);
-    for (int parity = 0; base < a.rows; base += stride, parity ^= 1) {
-        const int64_t row = base + r0;
-        if (!kAhead)
-            next.load(a, row, i0, tpr);
-        const RowIn<T, V, E, X8> in = next;
-        if (kAhead && base + stride < a.rows)
-            next.load(a, row + stride, i0, tpr);
-        float sum = 0.0f;
+    int parity = 0;
+    auto one_row = [&](const auto &in, int64_t row) {
+        float sum = 0.0f, gk[N][V], vk[N][V];
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            float v[V];
-            in.normalised(n, v);
+            const Vec<T, V> dyv = in.dy(n);
+            in.normalised(n, vk[n]);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float dy = in.dy[n].get(j);
-                sum = fmaf(dy * w[n].get(j), v[j], sum);
-                dw[n][j] = fmaf(dy, v[j], dw[n][j]);
+                const float dy = dyv.get(j);
+                gk[n][j] = dy * w[n].get(j);
+                sum = fmaf(gk[n][j], vk[n][j], sum);
+                dw[n][j] = fmaf(dy, vk[n][j], dw[n][j]);
             }
         }
         sum = warp_sum(sum);
@@ -427,31 +535,73 @@ rmsnorm_backward_kernel(const NormBackArgs args)
                 red[parity][warp] = sum;
             __syncthreads();
             sum = warp_sum(lane < warps ? red[parity][(warp & ~(warps - 1)) + lane] : 0.0f);
+            parity ^= 1;
         }
         sum /= (float)cols;
-        if (a.dx != nullptr && row < a.rows) {
-            T *dxp = static_cast<T *>(a.dx) + row * a.ld_dx;
+        if (a.dx == nullptr || row >= a.rows)
+            return;
+        T *dxp = static_cast<T *>(a.dx) + row * a.ld_dx;
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int c = (i0 + n * tpr) * V;
-                if (c < cols) {
-                    float v[V];
-                    in.normalised(n, v);
+        for (int n = 0; n < N; ++n) {
+            const int c = (i0 + n * tpr) * V;
+            if (c < cols) {
+                float v[V];
+                if (a.dh != nullptr) {
+                    const Vec<T, V> dhv = in.dh(n);
 #pragma unroll
                     for (int j = 0; j < V; ++j)
-                        v[j] = fmaf(in.rstd, in.dy[n].get(j) * w[n].get(j) - v[j] * sum,
-                                    in.dh[n].get(j));
-                    Vec<T, V> o;
-                    o.set(v);
-                    o.store(dxp + c);
+                        v[j] = fmaf(in.rstd, fmaf(-vk[n][j], sum, gk[n][j]), dhv.get(j));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        v[j] = in.rstd * fmaf(-vk[n][j], sum, gk[n][j]);
                 }
+                Vec<T, V> o;
+                o.set(v);
+                o.store(dxp + c);
             }
+        }
+    };
+    int64_t base = (int64_t)blockIdx.x * rows_cta;
+    if constexpr (RING) {
+        using Slot = RowSlot<T, V, E, X8>;
+        Slot ring[kDepth];
+        auto fetch = [&](Slot &s, int64_t b) {
+            if (b < a.rows)
+                s.load(a, b + r0, i0, tpr);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+#pragma unroll
+        for (int d = 0; d < kDepth; ++d) {
+            ring[d].slot = smem + d * Slot::bytes((int)blockDim.x);
+            ring[d].threads = (int)blockDim.x;
+            if (d < kDepth - 1)
+                fetch(ring[d], base + d * stride);
+        }
+        while (base < a.rows) {
+#pragma unroll
+            for (int d = 0; d < kDepth; ++d) {
+                if (base >= a.rows)
+                    break;
+                fetch(ring[(d + kDepth - 1) % kDepth], base + (kDepth - 1) * stride);
+                asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+                one_row(ring[d], base + r0);
+                base += stride;
+            }
+        }
+    } else {
+        for (; base < a.rows; base += stride) {
+            RowRegs<T, V, E, X8> in;
+            in.load(a, base + r0, i0, tpr);
+            one_row(in, base + r0);
         }
     }
     if (a.dweight == nullptr)
         return;
     float *out = args.partials + (int64_t)blockIdx.x * cols;
     if (rows_cta > 1) {   // the CTA's rows, in order
+        float *dw_cta = reinterpret_cast<float *>(smem);
+        __syncthreads();   // nobody reads the ring any more
         for (int r = 0; r < rows_cta; ++r) {
             if (r0 == r)
 #pragma unroll
@@ -584,7 +734,7 @@ pack8_kernel(const PackArgs a)
 #pragma unroll
                 for (int j = 0; j < V; ++j)
                     v[j] = x[n].get(j);
-                const uint32_t b = scale_byte(group_amax<V>(v));
+                const uint32_t b = group_scale<V>(v);
                 if (c < a.cols) {
                     Codes<V> q;
                     q.set(v, inv_scale_of(b));
@@ -676,6 +826,7 @@ int check_packed(const char *what, const dpo_packed8 &p, int64_t cols)
 }
 
 constexpr int64_t kMaxRows = (int64_t)1 << 31;
+constexpr int kMaxSmem = 226 * 1024;   // dynamic, beside the kernel's own 256 bytes
 
 int check_matrix(const char *what, const char *name, const void *p, int64_t cols, int64_t ld,
                  int64_t size)
@@ -765,16 +916,26 @@ template <class T, class WT, int V, int TB> struct Fwd {
     static auto fn() { return &rmsnorm_kernel<T, WT, V, TB>; }
 };
 template <class T, class WT, int V, int E> struct BackH {
-    static auto fn() { return &rmsnorm_backward_kernel<T, WT, V, E, false>; }
+    static auto fn() { return &rmsnorm_backward_kernel<T, WT, V, E, false, false>; }
 };
 template <class T, class WT, int V, int E> struct Back8 {
-    static auto fn() { return &rmsnorm_backward_kernel<T, WT, V, E, true>; }
+    static auto fn() { return &rmsnorm_backward_kernel<T, WT, V, E, true, false>; }
 };
 template <template <class, class, int, int> class K>
 auto pick_back(int dtype, int wdtype, int v, int elems)
 {
     return elems == kBackElems ? pick_vec<K, kBackElems>(dtype, wdtype, v)
                                : pick_vec<K, kRowElems>(dtype, wdtype, v);
+}
+
+// The ring's instance and its shared memory for CTAs of so many threads.
+using BackFn = void (*)(NormBackArgs);
+template <class T, class WT, int V> BackFn ring_of(bool x8, int threads, int *smem)
+{
+    constexpr int E = kBackElems;
+    *smem = kDepth * (x8 ? RowSlot<T, V, E, true>::bytes(threads) : RowSlot<T, V, E, false>::bytes(threads));
+    return x8 ? rmsnorm_backward_kernel<T, WT, V, E, true, true>
+              : rmsnorm_backward_kernel<T, WT, V, E, false, true>;
 }
 
 int check_norm(const char *what, int64_t rows, int64_t cols, int dtype, int wdtype,
@@ -949,10 +1110,27 @@ extern "C" int dpo_rmsnorm_backward(const dpo_rmsnorm_backward_args *args, void 
              whole(codes, a.x8.ld_codes, 1, v)))
         v = v == 8 ? 2 : 1;
     const NormBackArgs k = {a, shape.warps, static_cast<float *>(a.workspace)};
-    const size_t smem = shape.cta > shape.warps ? (size_t)a.cols * 4 : 0;
-    rc = launch(what, a.h != nullptr ? pick_back<BackH>(a.dtype, a.weight_dtype, v, shape.elems)
-                                     : pick_back<Back8>(a.dtype, a.weight_dtype, v, shape.elems),
-                grid, shape.cta * 32, smem, cuda_stream, k);
+    // the ring where the pieces are the widest ones and it fits
+    const bool x8 = a.h == nullptr;
+    int smem = shape.cta > shape.warps ? (int)a.cols * 4 : 0, ring = 0;
+    BackFn fn = x8 ? pick_back<Back8>(a.dtype, a.weight_dtype, v, shape.elems)
+                   : pick_back<BackH>(a.dtype, a.weight_dtype, v, shape.elems);
+    if (v >= 4 && shape.elems == kBackElems) {
+        using B = __nv_bfloat16;
+        const int threads = shape.cta * 32;
+        const BackFn with = a.dtype == DPO_F32 ? ring_of<float, float, 4>(x8, threads, &ring)
+                            : a.weight_dtype == DPO_F32 ? ring_of<B, float, 4>(x8, threads, &ring)
+                                                        : ring_of<B, B, 8>(x8, threads, &ring);
+        if (ring <= kMaxSmem) {
+            fn = with;
+            smem = ring > smem ? ring : smem;
+            const cudaError_t e = cudaFuncSetAttribute(
+                reinterpret_cast<const void *>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+            if (e != cudaSuccess)
+                return call_fail(DPO_ECUDA, "%s: %s", what, cudaGetErrorString(e));
+        }
+    }
+    rc = launch(what, fn, grid, shape.cta * 32, (size_t)smem, cuda_stream, k);
     if (rc != DPO_OK || a.dweight == nullptr)
         return rc;
     const int64_t sum_grid = (a.cols + 31) / 32;
