@@ -157,10 +157,10 @@ template <int V> struct Codes {
     }
 };
 
-__device__ __forceinline__ uint16_t load_byte(const uint8_t *p)
+__device__ __forceinline__ uint32_t load_byte(const uint8_t *p)
 {
-    uint16_t v;
-    asm volatile("ld.global.u8 %0, [%1];" : "=h"(v) : "l"(p));
+    uint32_t v;
+    asm volatile("ld.global.u8 %0, [%1];" : "=r"(v) : "l"(p));
     return v;
 }
 __device__ __forceinline__ float load_scale(const uint8_t *p) { return scale_of(load_byte(p)); }
@@ -409,7 +409,7 @@ template <class T, int V, int E, bool X8> struct RowSlot {
     uint8_t *slot;             // of this thread's first piece of dy
     int threads;
     float rstd;
-    uint16_t scale[X8 ? N : 1];   // as loaded: converting it here would wait for it
+    uint32_t scale[X8 ? N : 1];   // as loaded: converting it here would wait for it
 
     __device__ __forceinline__ const uint8_t *piece(int kind, int n) const
     {
