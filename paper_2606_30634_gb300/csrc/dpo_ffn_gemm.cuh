@@ -171,25 +171,19 @@ __device__ __forceinline__ int share_end(int all, uint32_t share, uint32_t split
     return (int)((uint32_t)all * (share + 1u) / split);
 }
 
-// What the roles read of a product to find their tiles, in shared memory: from the
-// launch's parameters, each role's search took some 2 us a tile.
-struct Sched {
-    int first, m_tiles, n_tiles, kb0, kb_all, a_mn, b_mn;
-};
-
 // Product and position of tile t: bands of kBandRows block rows, column by column.
 struct Tile {
     int p, m, n;   // product, block row, block column
 };
-__device__ __forceinline__ Tile tile_at(const Sched *sched, int n_products, int t)
+__device__ __forceinline__ Tile tile_at(const Launch &L, int t)
 {
     int p = 0;
-    while (p + 1 < n_products && t >= sched[p + 1].first)
+    while (p + 1 < L.n_products && t >= L.p[p + 1].first)
         ++p;
-    const Sched &S = sched[p];
-    const int i = t - S.first, band = kBandRows * S.n_tiles;
+    const Product &P = L.p[p];
+    const int i = t - P.first, band = kBandRows * P.n_tiles;
     const int b = i / band, r = i - b * band;
-    const int rows = min(kBandRows, S.m_tiles - b * kBandRows);
+    const int rows = min(kBandRows, P.m_tiles - b * kBandRows);
     const int n = r / rows;
     return {p, b * kBandRows + r - n * rows, n};
 }
@@ -208,6 +202,46 @@ __device__ __forceinline__ float logistic(float z, float &dq)
         dq = fmaf(3.0f * k, z2, c);
     }
     return __fdividef(1.0f, 1.0f + __expf(-q));
+}
+
+// 32 fp32 values of one row from 64 bytes of bf16.
+__device__ __forceinline__ void load_bf16_row(const __nv_bfloat16 *p, float (&v)[32])
+{
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+        const uint4 q = gemm::load_c(p + 8 * h);
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[h * 8 + 2 * j] = __uint_as_float(w[j] << 16);
+            v[h * 8 + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+        }
+    }
+}
+
+// 32 values of one row from 32 codes and their scale.
+__device__ __forceinline__ void load_codes_row(const uint8_t *p, float scale, float (&v)[32])
+{
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint4 q = gemm::load_c(reinterpret_cast<const __nv_bfloat16 *>(p) + 8 * h);
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 lo = decode2(w[j]), hi = decode2(w[j] >> 16);
+            v[h * 16 + 4 * j] = lo.x * scale;
+            v[h * 16 + 4 * j + 1] = lo.y * scale;
+            v[h * 16 + 4 * j + 2] = hi.x * scale;
+            v[h * 16 + 4 * j + 3] = hi.y * scale;
+        }
+    }
+}
+
+__device__ __forceinline__ float load_scale_byte(const uint8_t *p)
+{
+    uint16_t v;
+    asm volatile("ld.global.u8 %0, [%1];" : "=h"(v) : "l"(p));
+    return scale_of(v);
 }
 
 // Scale byte of the first n of 32 values that one lane holds; infinities become NaN (rare:
@@ -261,20 +295,14 @@ struct Stager {
     }
     __device__ __forceinline__ void bf16(const CUtensorMap *map, const float (&v)[32], int x, int y)
     {
-        uint32_t w[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            w[i] = gemm::pack_bf16(v[2 * i], v[2 * i + 1]);
-        bf16(map, w, x, y);
-    }
-    __device__ __forceinline__ void bf16(const CUtensorMap *map, const uint32_t (&w)[16], int x,
-                                         int y)
-    {
         const uint32_t b = begin();
 #pragma unroll
         for (int g = 0; g < 4; ++g)
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(b + swz64(lane, g)),
-                         "r"(w[4 * g]), "r"(w[4 * g + 1]), "r"(w[4 * g + 2]), "r"(w[4 * g + 3])
+                         "r"(gemm::pack_bf16(v[g * 8], v[g * 8 + 1])),
+                         "r"(gemm::pack_bf16(v[g * 8 + 2], v[g * 8 + 3])),
+                         "r"(gemm::pack_bf16(v[g * 8 + 4], v[g * 8 + 5])),
+                         "r"(gemm::pack_bf16(v[g * 8 + 6], v[g * 8 + 7]))
                          : "memory");
         end(map, b, x, y);
     }
@@ -338,116 +366,61 @@ template <int ACT> __device__ __forceinline__ void gate(const float (&g)[32], fl
     }
 }
 
-// dG, dU, A in bf16 pairs of the gate's g and u and dA = da.
+// g, u, d := dG, dU, A of the gate's g and u and dA = d
 template <int ACT>
-__device__ __forceinline__ void gate_back(float2 g, float2 u, float2 da, uint32_t &dg, uint32_t &du,
-                                          uint32_t &a)
+__device__ __forceinline__ void gate_back(float (&g)[32], float (&u)[32], float (&d)[32])
 {
-    float q0, q1;
-    const float s0 = logistic<ACT>(g.x, q0), s1 = logistic<ACT>(g.y, q1);
-    const float a0 = g.x * s0, a1 = g.y * s1;
-    a = gemm::pack_bf16(a0 * u.x, a1 * u.y);
-    du = gemm::pack_bf16(da.x * a0, da.y * a1);
-    dg = gemm::pack_bf16(da.x * u.x * fmaf(a0 * q0, 1.0f - s0, s0),
-                         da.y * u.y * fmaf(a1 * q1, 1.0f - s1, s1));
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+        float dq;
+        const float s = logistic<ACT>(g[j], dq), da = d[j];
+        const float act = g[j] * s, slope = fmaf(act * dq, 1.0f - s, s);
+        d[j] = act * u[j];
+        g[j] = da * u[j] * slope;
+        u[j] = da * act;
+    }
 }
 
-// 32 columns of one row of what was kept of G and U, as loaded: codes with their scale
-// bytes, or bf16. Rows and pitches are 16-byte aligned and col0 is a multiple of 32, so a
-// chunk is read in 16-byte pieces; of one that the matrix ends in, whose last piece may
-// reach past the row, the elements before the end are read one by one. Rows past the end
-// read the last one.
-struct Kept {
-    uint32_t g[16], u[16];
-    uint32_t sg, su;   // whole registers: packing them would wait for the loads
-
-    __device__ __forceinline__ void load(const Product &P, int row, int col0)
-    {
-        if (col0 >= P.n)
-            return;
-        row = min(row, P.m - 1);
-        const int n = P.n - col0;
-        const bool codes = P.keep == kKeep8;
-        sg = su = 0;
-        if (codes) {
-            const int64_t sat = row * P.ld_scale + col0 / kGroup;
-            asm volatile("ld.global.u8 %0, [%1];" : "=r"(sg) : "l"(P.scale_g + sat));
-            asm volatile("ld.global.u8 %0, [%1];" : "=r"(su) : "l"(P.scale_u + sat));
-        }
-        const int64_t at = (row * P.ld_kept + col0) * (codes ? 1 : 2);
-        const uint8_t *gp = static_cast<const uint8_t *>(P.kept_g) + at;
-        const uint8_t *up = static_cast<const uint8_t *>(P.kept_u) + at;
-        if (n >= 32) {
-            const int pieces = codes ? 2 : 4;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i < pieces) {
-                    piece(gp + 16 * i, g, i);
-                    piece(up + 16 * i, u, i);
-                }
-        } else {   // four or two elements to a word
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                g[i] = u[i] = 0u;
-                if (i * (codes ? 4 : 2) < n) {   // n is a multiple of 8: words are whole
-                    asm volatile("ld.global.b32 %0, [%1];" : "=r"(g[i]) : "l"(gp + 4 * i));
-                    asm volatile("ld.global.b32 %0, [%1];" : "=r"(u[i]) : "l"(up + 4 * i));
-                }
-            }
-        }
-    }
-    static __device__ __forceinline__ void piece(const uint8_t *p, uint32_t (&w)[16], int i)
-    {
-        asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3])
-                     : "l"(p));
-    }
-    // dG, dU, A of the chunk from its dA
-    template <int ACT>
-    __device__ __forceinline__ void back(const Product &P, const float (&da)[32],
-                                         uint32_t (&dg)[16], uint32_t (&du)[16],
-                                         uint32_t (&a)[16]) const
-    {
-        const bool codes = P.keep == kKeep8;
-        const float fg = scale_of(sg), fu = scale_of(su);
-        if (codes) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float2 gv = decode2(g[i / 2] >> (16 * (i & 1)));
-                float2 uv = decode2(u[i / 2] >> (16 * (i & 1)));
-                gv.x *= fg;
-                gv.y *= fg;
-                uv.x *= fu;
-                uv.y *= fu;
-                gate_back<ACT>(gv, uv, make_float2(da[2 * i], da[2 * i + 1]), dg[i], du[i], a[i]);
-            }
+// 32 values of one row of what was kept, from column col0; zeros from column n.
+// Rows and pitches are 16-byte aligned and col0 is a multiple of 32, so a whole chunk is
+// read in 16-byte pieces; one that the matrix ends in, element by element.
+__device__ __forceinline__ void load_kept(const Product &P, const void *kept,
+                                          const uint8_t *scales, int row, int col0, float (&v)[32])
+{
+    const int64_t at = row * P.ld_kept + col0;
+    const bool whole = col0 + 32 <= P.n;
+    if (P.keep == kKeep8) {
+        const float s = load_scale_byte(scales + row * P.ld_scale + col0 / kGroup);
+        const uint8_t *p = static_cast<const uint8_t *>(kept) + at;
+        if (whole) {
+            load_codes_row(p, s, v);
         } else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                gate_back<ACT>(
-                    make_float2(__uint_as_float(g[i] << 16), __uint_as_float(g[i] & 0xFFFF0000u)),
-                    make_float2(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xFFFF0000u)),
-                    make_float2(da[2 * i], da[2 * i + 1]), dg[i], du[i], a[i]);
+            for (int j = 0; j < 32; ++j) {
+                uint16_t c = 0;
+                if (col0 + j < P.n)
+                    asm volatile("ld.global.u8 %0, [%1];" : "=h"(c) : "l"(p + j));
+                v[j] = decode2(c).x * s;
+            }
+        }
+    } else {
+        const __nv_bfloat16 *p = static_cast<const __nv_bfloat16 *>(kept) + at;
+        if (whole) {
+            load_bf16_row(p, v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                v[j] = col0 + j < P.n ? ld1(p + j) : 0.0f;
         }
     }
-    __device__ __forceinline__ void back(const Product &P, const float (&da)[32],
-                                         uint32_t (&dg)[16], uint32_t (&du)[16],
-                                         uint32_t (&a)[16]) const
-    {
-        if (P.act == kGelu)
-            back<kGelu>(P, da, dg, du, a);
-        else
-            back<kSilu>(P, da, dg, du, a);
-    }
-};
+}
 
 // One 32 x 32 chunk of the tile: accumulator columns from acc (kGate: of G, U's
-// half_cols further), output rows from row0 and columns from col0; kGateBack: kept holds
-// the chunk's G and U and is left with the next one's (more: there is one). Called by the
+// half_cols further), output rows from row0 and columns from col0. Called by the
 // whole warp with the same arguments; tcgen05.ld and the stores are the warp's.
 template <int EPI>
-__device__ __forceinline__ void drain(const Product &P, Stager &st, Kept &kept, uint32_t acc,
-                                      int half_cols, int row0, int col0, bool more)
+__device__ __forceinline__ void drain(const Product &P, Stager &st, uint32_t acc, int half_cols,
+                                      int row0, int col0)
 {
     if (row0 >= P.m || col0 >= P.n)
         return;
@@ -481,15 +454,17 @@ __device__ __forceinline__ void drain(const Product &P, Stager &st, Kept &kept, 
             gate<kSilu>(g, u);
         st.bf16(&P.d0, u, col0, row0);
     } else if constexpr (EPI == kGateBack) {
-        float d[32];
-        uint32_t dg[16], du[16], a[16];
+        float g[32], u[32], d[32];
+        load_kept(P, P.kept_g, P.scale_g, row, col0, g);
+        load_kept(P, P.kept_u, P.scale_u, row, col0, u);
         load_acc(acc, d);
-        kept.back(P, d, dg, du, a);
-        if (more)   // under way while this chunk is stored
-            kept.load(P, row, col0 + 32);
-        st.bf16(&P.d0, dg, col0, row0);
-        st.bf16(&P.d1, du, col0, row0);
-        st.bf16(&P.d2, a, col0, row0);
+        if (P.act == kGelu)
+            gate_back<kGelu>(g, u, d);
+        else
+            gate_back<kSilu>(g, u, d);
+        st.bf16(&P.d0, g, col0, row0);
+        st.bf16(&P.d1, u, col0, row0);
+        st.bf16(&P.d2, d, col0, row0);
     } else {
         float v[32];
         load_acc(acc, v);
@@ -632,21 +607,16 @@ struct Exchange {
 };
 
 // The first n of 32 values of a row, n a multiple of 8, rows 16-byte aligned.
-__device__ __forceinline__ void store_row(__nv_bfloat16 *p, const uint32_t (&w)[16], int n)
+__device__ __forceinline__ void store_row(__nv_bfloat16 *p, const float (&v)[32], int n)
 {
 #pragma unroll
     for (int g = 0; g < 4; ++g)
         if (g * 8 < n)
             *reinterpret_cast<uint4 *>(p + g * 8) =
-                make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
-}
-__device__ __forceinline__ void store_row(__nv_bfloat16 *p, const float (&v)[32], int n)
-{
-    uint32_t w[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-        w[i] = gemm::pack_bf16(v[2 * i], v[2 * i + 1]);
-    store_row(p, w, n);
+                make_uint4(gemm::pack_bf16(v[g * 8], v[g * 8 + 1]),
+                           gemm::pack_bf16(v[g * 8 + 2], v[g * 8 + 3]),
+                           gemm::pack_bf16(v[g * 8 + 4], v[g * 8 + 5]),
+                           gemm::pack_bf16(v[g * 8 + 6], v[g * 8 + 7]));
 }
 
 __device__ __forceinline__ void store_codes(uint8_t *p, uint8_t *scale, const float (&v)[32], int n)
@@ -727,13 +697,16 @@ __device__ __forceinline__ bool drain_split(const Product &P, Exchange &ex, uint
             if (!mine)
                 continue;
             if constexpr (EPI == kGateBack) {
-                Kept kept;
-                uint32_t dg[16], du[16], a[16];
-                kept.load(P, row, col0 + c * 32);
-                kept.back(P, v, dg, du, a);
-                store_row(P.o0 + at, dg, n);
-                store_row(P.o1 + at, du, n);
-                store_row(P.o2 + at, a, n);
+                float g[32], u[32];
+                load_kept(P, P.kept_g, P.scale_g, row, col0 + c * 32, g);
+                load_kept(P, P.kept_u, P.scale_u, row, col0 + c * 32, u);
+                if (P.act == kGelu)
+                    gate_back<kGelu>(g, u, v);
+                else
+                    gate_back<kSilu>(g, u, v);
+                store_row(P.o0 + at, g, n);
+                store_row(P.o1 + at, u, n);
+                store_row(P.o2 + at, v, n);
             } else {
                 store_row(P.o0 + at, v, n);
             }
@@ -762,7 +735,6 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
     __shared__ uint64_t bars[2 * kStages + 4 + (SPLIT ? 2 * kEpiWarps : 0)];
     __shared__ uint32_t tmem_slot;
     __shared__ int aborted;
-    __shared__ Sched sched[kMaxProducts];
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? gemm::cluster_rank() : 0u;
@@ -800,11 +772,6 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
         aborted = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 2 && lane < L.n_products) {
-        const Product &P = L.p[lane];
-        sched[lane] = {P.first, P.m_tiles, P.n_tiles, P.k_blocks[0], P.k_blocks[0] + P.k_blocks[1],
-                       P.a_mn, P.b_mn};
-    }
     if (warp == 1)
         gemm::tmem_alloc<CG>((uint32_t)__cvta_generic_to_shared(&tmem_slot));
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -813,8 +780,8 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
         __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_slot;
-    const int n_tiles = L.n_tiles, n_products = L.n_products;
-    if (warp == 0 && lane < n_products) {   // the maps are parameters: read before the wait
+    const int n_tiles = L.n_tiles;
+    if (warp == 0 && lane < L.n_products) {   // the maps are parameters: read before the wait
         for (int i = 0; i < 2; ++i) {
             asm volatile("prefetch.tensormap [%0];"
                          ::"l"(reinterpret_cast<uint64_t>(&L.p[lane].a[i])) : "memory");
@@ -829,19 +796,18 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
             int it = 0, s = 0;   // K blocks issued by this CTA, the ring's next stage
             uint32_t ph = 1;     // parity of the stage's release
             const uint32_t bytes = (uint32_t)(CG * (a_bytes + kBBytes));
-            Tile next = tile_at(sched, n_products, pair);
             for (int t = pair; t < n_tiles && !*(volatile int *)&aborted; t += n_pairs) {
-                const Tile tile = next;
+                const Tile tile = tile_at(L, t);
                 const Product &P = L.p[tile.p];
-                const Sched &S = sched[tile.p];
-                const bool a_mn = S.a_mn, b_mn = S.b_mn;
+                const bool a_mn = P.a_mn, b_mn = P.b_mn;
                 const int ma = tile.m * T + (int)rank * BM;
                 // B rows of this CTA: T / CG of the tile's columns; kGate: a pair's CTAs
                 // hold one projection each, a single CTA half a box of either
                 const int nb = EPI == kGate ? tile.n * (T / 2) : tile.n * T + (int)rank * BH;
-                const int kb0 = S.kb0, kb_n = SPLIT ? share_end(S.kb_all, share, split) : S.kb_all;
-                const int kb_first = SPLIT ? share_end(S.kb_all, share - 1, split) : 0;
-                for (int kb = kb_first; kb < kb_n; ++kb, ++it) {
+                const int kb0 = P.k_blocks[0], kb_all = kb0 + P.k_blocks[1];
+                const int kb_n = SPLIT ? share_end(kb_all, share, split) : kb_all;
+                for (int kb = SPLIT ? share_end(kb_all, share - 1, split) : 0; kb < kb_n;
+                     ++kb, ++it) {
                     if (!mbar_wait(empty(s), ph) || *(volatile int *)&aborted) {
                         atomicOr(L.err, kErrWaitEmpty);
                         aborted = 1;
@@ -878,8 +844,6 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                         s = 0;
                         ph ^= 1u;
                     }
-                    if (kb == kb_first && t + n_pairs < n_tiles)   // found while the ring is full
-                        next = tile_at(sched, n_products, t + n_pairs);
                 }
             }
             if (leader)   // no CTA leaves before the loads in flight have landed
@@ -891,13 +855,13 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
         if (lane == 0 && leader) {
             int lt = 0, s = 0;
             uint32_t ph = 0;
-            int next = tile_at(sched, n_products, pair).p;
             for (int t = pair; t < n_tiles && !*(volatile int *)&aborted; t += n_pairs, ++lt) {
-                const Sched S = sched[next];
-                const int kb_n = SPLIT ? share_end(S.kb_all, share, split) -
-                                             share_end(S.kb_all, share - 1, split)
-                                       : S.kb_all;
-                const bool a_mn = S.a_mn, b_mn = S.b_mn;
+                const Product &P = L.p[tile_at(L, t).p];
+                const int kb_all = P.k_blocks[0] + P.k_blocks[1];
+                const int kb_n = SPLIT ? share_end(kb_all, share, split) -
+                                             share_end(kb_all, share - 1, split)
+                                       : kb_all;
+                const bool a_mn = P.a_mn, b_mn = P.b_mn;
                 const uint32_t idesc = idesc_of(CG, a_mn, b_mn);
                 const int a = lt & 1;
                 const uint32_t aph = (uint32_t)(lt >> 1) & 1u;
@@ -933,8 +897,6 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                         s = 0;
                         ph ^= 1u;
                     }
-                    if (kb == 0 && t + n_pairs < n_tiles)   // while the tensor core works on it
-                        next = tile_at(sched, n_products, t + n_pairs).p;
                 }
                 mma_commit<CG>(acc_full(a));
                 if (!ok) {
@@ -956,13 +918,9 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
         constexpr int kCols = EPI == kGate ? T / 2 : T;   // output columns of a tile
         int lt = 0;
         for (int t = pair; t < n_tiles; t += n_pairs, ++lt) {
-            const Tile tile = tile_at(sched, n_products, t);
+            const Tile tile = tile_at(L, t);
             const Product &P = L.p[tile.p];
             const int a = lt & 1;
-            const int row0 = tile.m * T + (int)rank * BM + q * 32;
-            Kept kept;   // of the first chunk, requested before its accumulator is ready
-            if (EPI == kGateBack && !SPLIT)
-                kept.load(P, row0 + lane, tile.n * kCols + half * (kCols / 2));
             bool seen = mbar_wait(acc_full(a), (uint32_t)(lt >> 1) & 1u);
             if (!seen)
                 atomicOr(L.err, kErrWaitDone);
@@ -970,6 +928,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
             seen = __all_sync(0xFFFFFFFFu, seen && !*(volatile int *)&aborted);
             if (!seen)
                 break;
+            const int row0 = tile.m * T + (int)rank * BM + q * 32;
             const uint32_t acc =
                 tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * T + half * (kCols / 2));
 #pragma unroll 1
@@ -979,7 +938,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                 if constexpr (SPLIT)
                     seen = drain_split<EPI>(P, ex, at, kCols, row0, col0, acc_empty(a));
                 else
-                    drain<EPI>(P, st, kept, at, kCols, row0, col0, ch + 1 < kCols / 64);
+                    drain<EPI>(P, st, at, kCols, row0, col0);
             }
             if (SPLIT) {
                 if (seen)
