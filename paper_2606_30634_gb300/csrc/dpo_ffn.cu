@@ -35,7 +35,7 @@ using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t,
                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 using KernelFn = void (*)(const Launch);
-constexpr int kForms = 3;   // epilogues
+constexpr int kForms = 4;   // epilogues
 
 // What the launches need to know of a device, found by its first call.
 struct Device {
@@ -70,19 +70,16 @@ int slots_of(const Device &d, Form f, int epi)
            : f.thin  ? d.clusters[__builtin_ctz((unsigned)f.ways)][epi] : d.singles[epi];
 }
 
+template <int CG, bool SPLIT> KernelFn kernel_of(int epi)
+{
+    return epi == kGate         ? ffn_gemm_kernel<CG, kGate, SPLIT>
+           : epi == kGateBack8  ? ffn_gemm_kernel<CG, kGateBack8, SPLIT>
+           : epi == kGateBack16 ? ffn_gemm_kernel<CG, kGateBack16, SPLIT>
+                                : ffn_gemm_kernel<CG, kStore, SPLIT>;
+}
 KernelFn kernel_of(Form f, int epi)
 {
-    if (f.cg == 2)
-        return epi == kGate ? ffn_gemm_kernel<2, kGate, false>
-                            : epi == kGateBack ? ffn_gemm_kernel<2, kGateBack, false>
-                                               : ffn_gemm_kernel<2, kStore, false>;
-    if (f.thin)
-        return epi == kGate ? ffn_gemm_kernel<1, kGate, true>
-                            : epi == kGateBack ? ffn_gemm_kernel<1, kGateBack, true>
-                                               : ffn_gemm_kernel<1, kStore, true>;
-    return epi == kGate ? ffn_gemm_kernel<1, kGate, false>
-                        : epi == kGateBack ? ffn_gemm_kernel<1, kGateBack, false>
-                                           : ffn_gemm_kernel<1, kStore, false>;
+    return f.cg == 2 ? kernel_of<2, false>(epi) : f.thin ? kernel_of<1, true>(epi) : kernel_of<1, false>(epi);
 }
 
 cudaLaunchAttribute cluster_of(int n)
@@ -505,6 +502,8 @@ extern "C" int dpo_ffn_forward(const dpo_ffn_args *args, void *cuda_stream)
             P.scale_g = a.gate8.scales;
             P.scale_u = a.up8.scales;
             P.ld_scale = a.gate8.ld_scales;
+            P.wide = reinterpret_cast<uintptr_t>(P.scale_g) % 2 == 0 &&
+                     reinterpret_cast<uintptr_t>(P.scale_u) % 2 == 0 && P.ld_scale % 2 == 0;
             P.codes_g = a.gate8.codes;
             P.codes_u = a.up8.codes;
             P.ld_codes_g = a.gate8.ld_codes;
@@ -614,7 +613,8 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
     }
     {
         const Shape s = {T, F, D, 1};
-        const Form form = form_of(*d, &s, 1, kGateBack);
+        const int epi = a.keep == DPO_KEEP_8BIT ? kGateBack8 : kGateBack16;
+        const Form form = form_of(*d, &s, 1, epi);
         Launch L{};
         Maps m;
         Product &P = L.p[0];
@@ -642,7 +642,13 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
         }
         P.keep = a.keep;
         P.act = a.act;
-        if ((rc = run(what, *d, L, &s, 1, kGateBack, form, m.ok, cuda_stream)) != DPO_OK)
+        const int64_t size = a.keep == DPO_KEEP_8BIT ? 1 : 2;
+        P.wide = F % 128 == 0 && reinterpret_cast<uintptr_t>(P.kept_g) % 32 == 0 &&
+                 reinterpret_cast<uintptr_t>(P.kept_u) % 32 == 0 && P.ld_kept * size % 32 == 0 &&
+                 (a.keep != DPO_KEEP_8BIT ||
+                  (reinterpret_cast<uintptr_t>(P.scale_g) % 4 == 0 &&
+                   reinterpret_cast<uintptr_t>(P.scale_u) % 4 == 0 && P.ld_scale % 4 == 0));
+        if ((rc = run(what, *d, L, &s, 1, epi, form, m.ok, cuda_stream)) != DPO_OK)
             return rc;
     }
     Launch L{};

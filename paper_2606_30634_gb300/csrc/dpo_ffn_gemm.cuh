@@ -24,7 +24,7 @@
 //   kGate      the tile's columns are T / 2 of G beside the same T / 2 of U (the B
 //              operand is half w_gate rows, half w_up rows), so act(G) U is formed
 //              where both are in registers; writes A and what is kept of G and U
-//   kGateBack  the tile is of dA; reads what was kept of G and U, writes dG, dU, A
+//   kGateBack8, kGateBack16  the tile is of dA; reads what was kept of G and U, writes dG, dU, A
 //   kStore     writes D in bf16 or fp32, with factors along the columns and the old
 //              contents added where asked for
 #pragma once
@@ -57,7 +57,8 @@ using gemm::smem_desc_mn;
 using gemm::swz64;
 using gemm::tmem_ld32;
 
-enum Epilogue { kGate = 0, kGateBack = 1, kStore = 2 };
+enum Epilogue { kGate = 0, kGateBack8 = 1, kGateBack16 = 2, kStore = 3 };
+__host__ __device__ constexpr bool gate_back(int epi) { return epi == kGateBack8 || epi == kGateBack16; }
 enum Keep { kKeepNone = 0, kKeep8 = 1, kKeep16 = 2 };
 enum Act { kSilu = 0, kGelu = 1 };
 
@@ -115,6 +116,8 @@ struct Product {
     const void *kept_g, *kept_u;  // kGateBack: codes or bf16
     int64_t ld_kept;
     int keep, act;                // Keep, Act
+    int wide;                     // kGate: scale rows 2-byte aligned; kGateBack: kept values
+                                  // in whole, 32-byte aligned chunks
     // split K: the same outputs as pointers (kStore: bf16, nothing added)
     __nv_bfloat16 *o0, *o1, *o2;
     int64_t ld_o;
@@ -204,46 +207,6 @@ __device__ __forceinline__ float logistic(float z, float &dq)
     return __fdividef(1.0f, 1.0f + __expf(-q));
 }
 
-// 32 fp32 values of one row from 64 bytes of bf16.
-__device__ __forceinline__ void load_bf16_row(const __nv_bfloat16 *p, float (&v)[32])
-{
-#pragma unroll
-    for (int h = 0; h < 4; ++h) {
-        const uint4 q = gemm::load_c(p + 8 * h);
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[h * 8 + 2 * j] = __uint_as_float(w[j] << 16);
-            v[h * 8 + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-        }
-    }
-}
-
-// 32 values of one row from 32 codes and their scale.
-__device__ __forceinline__ void load_codes_row(const uint8_t *p, float scale, float (&v)[32])
-{
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const uint4 q = gemm::load_c(reinterpret_cast<const __nv_bfloat16 *>(p) + 8 * h);
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float2 lo = decode2(w[j]), hi = decode2(w[j] >> 16);
-            v[h * 16 + 4 * j] = lo.x * scale;
-            v[h * 16 + 4 * j + 1] = lo.y * scale;
-            v[h * 16 + 4 * j + 2] = hi.x * scale;
-            v[h * 16 + 4 * j + 3] = hi.y * scale;
-        }
-    }
-}
-
-__device__ __forceinline__ float load_scale_byte(const uint8_t *p)
-{
-    uint16_t v;
-    asm volatile("ld.global.u8 %0, [%1];" : "=h"(v) : "l"(p));
-    return scale_of(v);
-}
-
 // Scale byte of the first n of 32 values that one lane holds; infinities become NaN (rare:
 // looked for only where the maximum, which passes over NaN, found one).
 __device__ __forceinline__ uint32_t row_scale(float (&v)[32], int n)
@@ -295,14 +258,20 @@ struct Stager {
     }
     __device__ __forceinline__ void bf16(const CUtensorMap *map, const float (&v)[32], int x, int y)
     {
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            w[i] = gemm::pack_bf16(v[2 * i], v[2 * i + 1]);
+        bf16(map, w, x, y);
+    }
+    __device__ __forceinline__ void bf16(const CUtensorMap *map, const uint32_t (&w)[16], int x,
+                                         int y)
+    {
         const uint32_t b = begin();
 #pragma unroll
         for (int g = 0; g < 4; ++g)
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(b + swz64(lane, g)),
-                         "r"(gemm::pack_bf16(v[g * 8], v[g * 8 + 1])),
-                         "r"(gemm::pack_bf16(v[g * 8 + 2], v[g * 8 + 3])),
-                         "r"(gemm::pack_bf16(v[g * 8 + 4], v[g * 8 + 5])),
-                         "r"(gemm::pack_bf16(v[g * 8 + 6], v[g * 8 + 7]))
+                         "r"(w[4 * g]), "r"(w[4 * g + 1]), "r"(w[4 * g + 2]), "r"(w[4 * g + 3])
                          : "memory");
         end(map, b, x, y);
     }
@@ -366,61 +335,121 @@ template <int ACT> __device__ __forceinline__ void gate(const float (&g)[32], fl
     }
 }
 
-// g, u, d := dG, dU, A of the gate's g and u and dA = d
+// dG, dU, A in bf16 pairs of the gate's g and u and dA = da.
 template <int ACT>
-__device__ __forceinline__ void gate_back(float (&g)[32], float (&u)[32], float (&d)[32])
+__device__ __forceinline__ void back_pair(float2 g, float2 u, float2 da, uint32_t &dg, uint32_t &du,
+                                          uint32_t &a)
 {
-#pragma unroll
-    for (int j = 0; j < 32; ++j) {
-        float dq;
-        const float s = logistic<ACT>(g[j], dq), da = d[j];
-        const float act = g[j] * s, slope = fmaf(act * dq, 1.0f - s, s);
-        d[j] = act * u[j];
-        g[j] = da * u[j] * slope;
-        u[j] = da * act;
-    }
+    float q0, q1;
+    const float s0 = logistic<ACT>(g.x, q0), s1 = logistic<ACT>(g.y, q1);
+    const float a0 = g.x * s0, a1 = g.y * s1;
+    a = gemm::pack_bf16(a0 * u.x, a1 * u.y);
+    du = gemm::pack_bf16(da.x * a0, da.y * a1);
+    dg = gemm::pack_bf16(da.x * u.x * fmaf(a0 * q0, 1.0f - s0, s0),
+                         da.y * u.y * fmaf(a1 * q1, 1.0f - s1, s1));
 }
 
-// 32 values of one row of what was kept, from column col0; zeros from column n.
-// Rows and pitches are 16-byte aligned and col0 is a multiple of 32, so a whole chunk is
-// read in 16-byte pieces; one that the matrix ends in, element by element.
-__device__ __forceinline__ void load_kept(const Product &P, const void *kept,
-                                          const uint8_t *scales, int row, int col0, float (&v)[32])
-{
-    const int64_t at = row * P.ld_kept + col0;
-    const bool whole = col0 + 32 <= P.n;
-    if (P.keep == kKeep8) {
-        const float s = load_scale_byte(scales + row * P.ld_scale + col0 / kGroup);
-        const uint8_t *p = static_cast<const uint8_t *>(kept) + at;
-        if (whole) {
-            load_codes_row(p, s, v);
-        } else {
+// 32 columns of one row of what was kept of G and U, as loaded: codes with their scale
+// bytes (CODES), or bf16, zeros past the matrix. A lane holds a row, so every load of the
+// warp touches 32 lines whatever its width, and their number is what the loads cost (1B
+// layer, the whole launch: 8-byte pieces 142 us, 16-byte ones 125, no loads at all 112):
+// Product::wide says that all rows are 32-byte aligned and whole chunks of 128 columns, so
+// a row's chunk of codes is one load (past L1: 134 -> 124 us) and four chunks' scales another. Otherwise rows and
+// pitches are 16-byte aligned and hidden is a multiple of 8: pieces of 8 elements.
+// Rows past the end read the last one.
+template <bool CODES> struct Kept {
+    static constexpr int W = CODES ? 2 : 4;   // words of 8 elements
+    uint32_t g[4 * W], u[4 * W];
+    uint32_t sg, su;                          // scale bytes; wide: of four chunks
+
+    __device__ __forceinline__ void load(const Product &P, int row, int col0, bool first)
+    {
+        const int n = P.n - col0;
+        const int64_t at = (row * P.ld_kept + col0) * (CODES ? 1 : 2);
+        const uint8_t *gp = static_cast<const uint8_t *>(P.kept_g) + at;
+        const uint8_t *up = static_cast<const uint8_t *>(P.kept_u) + at;
+        const int64_t sat = row * P.ld_scale + col0 / kGroup;
+        if (P.wide) {
+            if (CODES && first) {   // col0 is a multiple of 64: bytes 0 or 2 of the four
+                asm volatile("ld.global.b32 %0, [%1];" : "=r"(sg) : "l"(P.scale_g + (sat & ~3ll)));
+                asm volatile("ld.global.b32 %0, [%1];" : "=r"(su) : "l"(P.scale_u + (sat & ~3ll)));
+            }
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                uint16_t c = 0;
-                if (col0 + j < P.n)
-                    asm volatile("ld.global.u8 %0, [%1];" : "=h"(c) : "l"(p + j));
-                v[j] = decode2(c).x * s;
+            for (int i = 0; i < W / 2; ++i) {
+                load32(gp + 32 * i, g + 8 * i);
+                load32(up + 32 * i, u + 8 * i);
+            }
+            return;
+        }
+        if (CODES) {
+            asm volatile("ld.global.u8 %0, [%1];" : "=r"(sg) : "l"(P.scale_g + sat));
+            asm volatile("ld.global.u8 %0, [%1];" : "=r"(su) : "l"(P.scale_u + sat));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                g[i * W + j] = u[i * W + j] = 0u;
+            if (i * 8 < n) {
+                piece(gp + i * 4 * W, g + i * W);
+                piece(up + i * 4 * W, u + i * W);
             }
         }
-    } else {
-        const __nv_bfloat16 *p = static_cast<const __nv_bfloat16 *>(kept) + at;
-        if (whole) {
-            load_bf16_row(p, v);
+    }
+    static __device__ __forceinline__ void load32(const uint8_t *p, uint32_t *w)
+    {
+        asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]),
+                       "=r"(w[6]), "=r"(w[7])
+                     : "l"(p));
+    }
+    static __device__ __forceinline__ void piece(const uint8_t *p, uint32_t *w)
+    {
+        if constexpr (CODES)
+            asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+        else
+            asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                         : "l"(p));
+    }
+    static __device__ __forceinline__ float2 pair(const uint32_t *w, int i, float scale)
+    {
+        if constexpr (CODES) {
+            const float2 v = decode2(w[i / 2] >> (16 * (i & 1)));
+            return make_float2(v.x * scale, v.y * scale);
         } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                v[j] = col0 + j < P.n ? ld1(p + j) : 0.0f;
+            return make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
         }
     }
-}
+    // dG, dU, A of the chunk from its dA
+    template <int ACT>
+    __device__ __forceinline__ void back(const float (&da)[32], int shift, uint32_t (&dg)[16],
+                                         uint32_t (&du)[16], uint32_t (&a)[16]) const
+    {
+        const float fg = scale_of(sg >> shift & 0xFFu), fu = scale_of(su >> shift & 0xFFu);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            back_pair<ACT>(pair(g, i, fg), pair(u, i, fu), make_float2(da[2 * i], da[2 * i + 1]),
+                           dg[i], du[i], a[i]);
+    }
+    __device__ __forceinline__ void back(const Product &P, const float (&da)[32], int col0,
+                                         uint32_t (&dg)[16], uint32_t (&du)[16],
+                                         uint32_t (&a)[16]) const
+    {
+        const int shift = P.wide ? col0 / kGroup % 4 * 8 : 0;
+        if (P.act == kGelu)
+            back<kGelu>(da, shift, dg, du, a);
+        else
+            back<kSilu>(da, shift, dg, du, a);
+    }
+};
 
 // One 32 x 32 chunk of the tile: accumulator columns from acc (kGate: of G, U's
 // half_cols further), output rows from row0 and columns from col0. Called by the
 // whole warp with the same arguments; tcgen05.ld and the stores are the warp's.
 template <int EPI>
-__device__ __forceinline__ void drain(const Product &P, Stager &st, uint32_t acc, int half_cols,
-                                      int row0, int col0)
+__device__ __forceinline__ void drain(const Product &P, Stager &st, Kept<EPI == kGateBack8> &kept,
+                                      uint32_t acc, int half_cols, int row0, int col0, bool first)
 {
     if (row0 >= P.m || col0 >= P.n)
         return;
@@ -442,8 +471,19 @@ __device__ __forceinline__ void drain(const Product &P, Stager &st, uint32_t acc
             for (int j = 0; j < 32; ++j)
                 q[j] = u[j];
             const uint32_t su = st.codes(&P.d2, q, col0, row0);
-            if (row0 + st.lane < P.m) {
-                const int64_t at = row * P.ld_scale + col0 / kGroup;
+            // scale bytes, two chunks' in one store where a pair's warp has both: single
+            // bytes were a third of the launch's writes to L2
+            const int64_t at = row * P.ld_scale + col0 / kGroup;
+            const bool in = row0 + st.lane < P.m, two = half_cols == 128 && P.wide;
+            if (two && first && col0 + 32 < P.n) {
+                kept.sg = sg;
+                kept.su = su;
+            } else if (two && !first) {
+                if (in) {
+                    *reinterpret_cast<uint16_t *>(P.scale_g + at - 1) = (uint16_t)(kept.sg | sg << 8);
+                    *reinterpret_cast<uint16_t *>(P.scale_u + at - 1) = (uint16_t)(kept.su | su << 8);
+                }
+            } else if (in) {
                 P.scale_g[at] = (uint8_t)sg;
                 P.scale_u[at] = (uint8_t)su;
             }
@@ -453,18 +493,15 @@ __device__ __forceinline__ void drain(const Product &P, Stager &st, uint32_t acc
         else
             gate<kSilu>(g, u);
         st.bf16(&P.d0, u, col0, row0);
-    } else if constexpr (EPI == kGateBack) {
-        float g[32], u[32], d[32];
-        load_kept(P, P.kept_g, P.scale_g, row, col0, g);
-        load_kept(P, P.kept_u, P.scale_u, row, col0, u);
+    } else if constexpr (gate_back(EPI)) {
+        float d[32];
+        uint32_t dg[16], du[16], a[16];
+        kept.load(P, row, col0, first);
         load_acc(acc, d);
-        if (P.act == kGelu)
-            gate_back<kGelu>(g, u, d);
-        else
-            gate_back<kSilu>(g, u, d);
-        st.bf16(&P.d0, g, col0, row0);
-        st.bf16(&P.d1, u, col0, row0);
-        st.bf16(&P.d2, d, col0, row0);
+        kept.back(P, d, col0, dg, du, a);
+        st.bf16(&P.d0, dg, col0, row0);
+        st.bf16(&P.d1, du, col0, row0);
+        st.bf16(&P.d2, a, col0, row0);
     } else {
         float v[32];
         load_acc(acc, v);
@@ -476,13 +513,26 @@ __device__ __forceinline__ void drain(const Product &P, Stager &st, uint32_t acc
             for (int j = 0; j < 32; ++j)
                 v[j] *= __shfl_sync(0xFFFFFFFFu, f, j);
         }
-        if (P.accumulate) {
-            const int64_t at = row * P.ld_old + col0;
+        if (P.accumulate) {   // in 16-byte pieces: rows are 16-byte aligned, n is a multiple of 8
+            const int size = P.f32 ? 4 : 2, left = P.n - col0;
+            const uint8_t *old = static_cast<const uint8_t *>(P.old) + (row * P.ld_old + col0) * size;
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (col0 + j < P.n)
-                    v[j] += P.f32 ? ld1(static_cast<const float *>(P.old) + at + j)
-                                  : ld1(static_cast<const __nv_bfloat16 *>(P.old) + at + j);
+            for (int i = 0; i < 8; ++i)
+                if ((P.f32 ? 4 : 8) * i < min(left, 32)) {
+                    const uint4 q = gemm::load_c(reinterpret_cast<const __nv_bfloat16 *>(old + 16 * i));
+                    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+                    if (P.f32) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            v[4 * i + j] += __uint_as_float(w[j]);
+                    } else if (i < 4) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            v[(8 * i + 2 * j) & 31] += __uint_as_float(w[j] << 16);
+                            v[(8 * i + 2 * j + 1) & 31] += __uint_as_float(w[j] & 0xFFFF0000u);
+                        }
+                    }
+                }
         }
         if (P.f32)
             st.f32(&P.d0, v, col0, row0);
@@ -607,16 +657,21 @@ struct Exchange {
 };
 
 // The first n of 32 values of a row, n a multiple of 8, rows 16-byte aligned.
-__device__ __forceinline__ void store_row(__nv_bfloat16 *p, const float (&v)[32], int n)
+__device__ __forceinline__ void store_row(__nv_bfloat16 *p, const uint32_t (&w)[16], int n)
 {
 #pragma unroll
     for (int g = 0; g < 4; ++g)
         if (g * 8 < n)
             *reinterpret_cast<uint4 *>(p + g * 8) =
-                make_uint4(gemm::pack_bf16(v[g * 8], v[g * 8 + 1]),
-                           gemm::pack_bf16(v[g * 8 + 2], v[g * 8 + 3]),
-                           gemm::pack_bf16(v[g * 8 + 4], v[g * 8 + 5]),
-                           gemm::pack_bf16(v[g * 8 + 6], v[g * 8 + 7]));
+                make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
+}
+__device__ __forceinline__ void store_row(__nv_bfloat16 *p, const float (&v)[32], int n)
+{
+    uint32_t w[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        w[i] = gemm::pack_bf16(v[2 * i], v[2 * i + 1]);
+    store_row(p, w, n);
 }
 
 __device__ __forceinline__ void store_codes(uint8_t *p, uint8_t *scale, const float (&v)[32], int n)
@@ -696,17 +751,14 @@ __device__ __forceinline__ bool drain_split(const Product &P, Exchange &ex, uint
             ex.total(c, v);
             if (!mine)
                 continue;
-            if constexpr (EPI == kGateBack) {
-                float g[32], u[32];
-                load_kept(P, P.kept_g, P.scale_g, row, col0 + c * 32, g);
-                load_kept(P, P.kept_u, P.scale_u, row, col0 + c * 32, u);
-                if (P.act == kGelu)
-                    gate_back<kGelu>(g, u, v);
-                else
-                    gate_back<kSilu>(g, u, v);
-                store_row(P.o0 + at, g, n);
-                store_row(P.o1 + at, u, n);
-                store_row(P.o2 + at, v, n);
+            if constexpr (gate_back(EPI)) {
+                Kept<EPI == kGateBack8> kept;
+                uint32_t dg[16], du[16], a[16];
+                kept.load(P, row, col0 + c * 32, true);
+                kept.back(P, v, col0 + c * 32, dg, du, a);
+                store_row(P.o0 + at, dg, n);
+                store_row(P.o1 + at, du, n);
+                store_row(P.o2 + at, a, n);
             } else {
                 store_row(P.o0 + at, v, n);
             }
@@ -921,6 +973,8 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
             const Tile tile = tile_at(L, t);
             const Product &P = L.p[tile.p];
             const int a = lt & 1;
+            const int row0 = tile.m * T + (int)rank * BM + q * 32;
+            Kept<EPI == kGateBack8> kept;
             bool seen = mbar_wait(acc_full(a), (uint32_t)(lt >> 1) & 1u);
             if (!seen)
                 atomicOr(L.err, kErrWaitDone);
@@ -928,7 +982,6 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
             seen = __all_sync(0xFFFFFFFFu, seen && !*(volatile int *)&aborted);
             if (!seen)
                 break;
-            const int row0 = tile.m * T + (int)rank * BM + q * 32;
             const uint32_t acc =
                 tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * T + half * (kCols / 2));
 #pragma unroll 1
@@ -938,7 +991,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                 if constexpr (SPLIT)
                     seen = drain_split<EPI>(P, ex, at, kCols, row0, col0, acc_empty(a));
                 else
-                    drain<EPI>(P, st, at, kCols, row0, col0);
+                    drain<EPI>(P, st, kept, at, kCols, row0, col0, ch == 0);
             }
             if (SPLIT) {
                 if (seen)

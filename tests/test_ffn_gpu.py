@@ -308,6 +308,20 @@ def test_ffn_by_cta_pairs():
     assert ffn.status() == 0
 
 
+@pytest.mark.parametrize("keep", ["8bit", "bf16"])
+def test_ffn_by_cta_pairs_in_whole_chunks(keep):
+    """hidden a multiple of 128: what is kept is read in aligned 32-byte pieces."""
+    t, d, f = 2500, 520, 4096
+    g, x, *w = ffn_case(t, d, f, seed=2)
+    dout = randn(g, t, d, scale=1e-2)
+    out, kept = ffn.gated_ffn(x, *w, activation="gelu", keep=keep)
+    dw = [torch.zeros_like(v) for v in w]
+    dx = ffn.gated_ffn_backward(dout, kept, *w, *dw, x=x)
+    check_forward(x, w, "gelu", out, kept)
+    check_backward(dout, np64(x), kept, w, [dx, *dw])
+    assert ffn.status() == 0
+
+
 def test_ffn_non_finite_tokens_stay_in_their_rows():
     _, x, *w = ffn_case(200, 136, 264)
     clean, _ = ffn.gated_ffn(x, *w)
