@@ -2,6 +2,9 @@
 
 * ``_build/libdpo.so``       -- the product: C ABI of include/dpo.h and its
                                 kernels (csrc/).
+* ``_build/dpo_tensors.so``   -- the feed-forward calls on PyTorch tensors, a
+                                Python module (ffn.py's other half), compiled
+                                against PyTorch's headers by the host compiler.
 * ``_build/libdpo_synth.so`` -- seeded synthetic inputs (include/dpo_synth.h),
                                 used by the tests and the benchmark.
 
@@ -13,6 +16,7 @@ from __future__ import annotations
 
 import glob
 import os
+import shutil
 import subprocess
 import sys
 from concurrent.futures import ThreadPoolExecutor
@@ -22,6 +26,7 @@ ROOT = os.path.dirname(PKG)
 INCLUDE = os.path.join(ROOT, "include")
 OUT = os.path.join(PKG, "_build")
 NVCC = os.environ.get("NVCC", "nvcc")
+CXX = os.environ.get("CXX", "g++")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 COMMON = ARCH + ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC,-O3,-fopenmp",
@@ -40,6 +45,13 @@ LIBS = {
         "includes": ["csrc"],
         "ptxas_v": ["csrc/dpo_step_adamw.cu", "csrc/dpo_muon.cu", "csrc/dpo_ffn.cu"],
     },
+    "dpo_tensors.so": {
+        "sources": ["csrc/dpo_tensors.cpp"],
+        "headers": ["../include/dpo.h"],
+        "includes": [],
+        "ptxas_v": [],
+        "torch": True,
+    },
     "libdpo_synth.so": {
         "sources": ["synth/synth.cu"],
         "headers": ["synth/philox.h", "../include/dpo_synth.h"],
@@ -53,17 +65,40 @@ def _mtime(p):
     return os.path.getmtime(p) if os.path.exists(p) else -1.0
 
 
-def _compile(src, obj, includes, verbose_ptxas):
+def _torch_flags():
+    """(compile flags, link flags) of a Python module that uses PyTorch's C++ interface."""
+    import sysconfig
+    import torch
+    root = os.path.dirname(torch.__file__)
+    inc = [os.path.join(root, "include"), sysconfig.get_paths()["include"],
+           os.path.join(os.path.dirname(os.path.dirname(shutil.which(NVCC) or "/usr/local/cuda/bin/nvcc")),
+                        "include")]
+    lib = os.path.join(root, "lib")
+    abi = int(torch._C._GLIBCXX_USE_CXX11_ABI)
+    return (["-O2", "-std=c++17", "-fPIC", "-w", f"-D_GLIBCXX_USE_CXX11_ABI={abi}", "-I", INCLUDE] +
+            sum((["-isystem", i] for i in inc), []),
+            ["-shared", "-L" + lib, "-Wl,-rpath," + lib, "-ltorch_python", "-ltorch_cpu", "-lc10",
+             "-lc10_cuda"])
+
+
+def _run(cmd, what):
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{what} failed:\n{r.stdout}\n{r.stderr}")
+    return r.stderr
+
+
+def _compile(src, obj, includes, verbose_ptxas, torch=False):
+    if torch:
+        return _run([CXX] + _torch_flags()[0] + ["-c", os.path.join(PKG, src), "-o", obj],
+                    f"{CXX} for {src}")
     cmd = [NVCC] + COMMON + sum((["-I", os.path.join(PKG, i)] for i in includes), [])
     if src.endswith(".cpp"):
         cmd += ["-x", "cu"]
     if verbose_ptxas:
         cmd += ["-Xptxas", "-v"]
     cmd += ["-c", os.path.join(PKG, src), "-o", obj]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"nvcc failed for {src}:\n{r.stdout}\n{r.stderr}")
-    return r.stderr
+    return _run(cmd, f"nvcc for {src}")
 
 
 def build(force: bool = False, quiet: bool = True) -> dict:
@@ -76,7 +111,8 @@ def build(force: bool = False, quiet: bool = True) -> dict:
         if force or any(_mtime(d) > _mtime(out) for d in deps):
             for src in spec["sources"]:
                 obj = os.path.join(OUT, os.path.basename(src) + ".o")
-                jobs.append((lib, src, obj, spec["includes"], src in spec["ptxas_v"]))
+                jobs.append((lib, src, obj, spec["includes"], src in spec["ptxas_v"],
+                             spec.get("torch", False)))
     if jobs:
         with ThreadPoolExecutor(max_workers=max(1, min(len(jobs), os.cpu_count() or 1))) as ex:
             logs = list(ex.map(lambda j: _compile(*j[1:]), jobs))
@@ -88,10 +124,11 @@ def build(force: bool = False, quiet: bool = True) -> dict:
             objs = [os.path.join(OUT, os.path.basename(s) + ".o") for s in LIBS[lib]["sources"]]
             out = os.path.join(OUT, lib)
             tmp = out + f".tmp{os.getpid()}"
-            cmd = [NVCC] + ARCH + ["-shared", "-Xcompiler", "-fopenmp", "-o", tmp] + objs
-            r = subprocess.run(cmd, capture_output=True, text=True)
-            if r.returncode != 0:
-                raise RuntimeError(f"link of {lib} failed:\n{r.stdout}\n{r.stderr}")
+            if LIBS[lib].get("torch", False):
+                cmd = [CXX, "-o", tmp] + objs + _torch_flags()[1]
+            else:
+                cmd = [NVCC] + ARCH + ["-shared", "-Xcompiler", "-fopenmp", "-o", tmp] + objs
+            _run(cmd, f"link of {lib}")
             os.replace(tmp, out)
     return {lib: os.path.join(OUT, lib) for lib in LIBS}
 
