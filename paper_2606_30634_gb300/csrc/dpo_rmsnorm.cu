@@ -205,11 +205,13 @@ __device__ __forceinline__ float warp_sum(float v)
 // input is read once. Thread i of the row takes the V-element pieces i, i + 32 W, ...:
 // a group of 32 is in 32 / V adjacent lanes.
 
-constexpr int kRowElems = 32;                 // elements of a row per thread
+// Elements of a row per thread: 32, or 8 in the narrow forms (pieces of one or two
+// elements, so that a thread's pieces are many and its row's time is their number) up to
+// 4096 columns.
+constexpr int kRowElems = 32, kNarrowElems = 8;
 constexpr int kMinWarps = 4;                  // warps of a CTA, at least
-// Threads of a CTA, at most: rows of up to 8192 elements, and wider ones. The bound
-// sets the registers a thread may have.
-constexpr int kCta = 256, kWideCta = 512;
+// Threads of a CTA, at most. The bound sets the registers a thread may have.
+constexpr int kCta = 512;
 
 struct NormForwardArgs {
     dpo_rmsnorm_args a;
@@ -233,11 +235,11 @@ __device__ __forceinline__ float row_sum(float v, int warps, float *red)
     return v;
 }
 
-template <class T, class WT, int V, int TB>
-__global__ void __launch_bounds__(TB)
+template <class T, class WT, int V, int E>
+__global__ void __launch_bounds__(kCta)
 rmsnorm_kernel(const NormForwardArgs args)
 {
-    constexpr int N = kRowElems / V;
+    constexpr int N = E / V;
     __shared__ float red[32];
     const dpo_rmsnorm_args &a = args.a;
     const int warps = args.warps, tpr = warps * 32;
@@ -329,7 +331,7 @@ struct NormBackArgs {
 
 // E elements of a row per thread: 16, or 32 where that would take more than 512 threads
 // (cols above 8192).
-constexpr int kBackElems = 16, kBackThreads = 512;
+constexpr int kBackElems = 16, kBackThreads = 512, kBackMinWarps = 8;
 constexpr int kDepth = 4;                     // rows of the ring
 
 // B bytes from global to shared memory, or zeros.
@@ -631,21 +633,21 @@ rmsnorm_backward_kernel(const NormBackArgs args)
     }
 }
 
-// dweight[c] = the sum of the n partial rows, in a fixed order: 32 columns per
-// CTA, 16 interleaved shares of the rows, eight loads of each in flight, added up
-// in order.
-constexpr int kSumShares = 16, kSumLoads = 8;
+// dweight[c] = the sum of the n partial rows, in a fixed order. A CTA takes 8 columns, a
+// sector of each row: 64 shares of the rows, four to a warp, ten loads of each in flight,
+// added up in order; more columns to a CTA are fewer CTAs and a longer chain of loads.
+constexpr int kSumCols = 8, kSumWarps = 16, kSumLoads = 10, kSumShares = kSumWarps * 4;
 template <class GT>
-__global__ void __launch_bounds__(32 * kSumShares)
+__global__ void __launch_bounds__(32 * kSumWarps)
 rmsnorm_dweight_kernel(const float *partials, int n, int cols, GT *dweight, int accumulate)
 {
-    __shared__ float share[kSumShares][33];
-    const int lane = threadIdx.x & 31, k = threadIdx.x >> 5;
-    const int c = blockIdx.x * 32 + lane;
+    __shared__ float share[kSumWarps][kSumCols];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c = blockIdx.x * kSumCols + (lane & 7);
     pdl_wait();
     float sum = 0.0f;
     if (c < cols)
-        for (int i = k; i < n; i += kSumShares * kSumLoads) {
+        for (int i = warp * 4 + (lane >> 3); i < n; i += kSumShares * kSumLoads) {
             float v[kSumLoads];
 #pragma unroll
             for (int u = 0; u < kSumLoads; ++u) {
@@ -656,13 +658,16 @@ rmsnorm_dweight_kernel(const float *partials, int n, int cols, GT *dweight, int 
             for (int u = 0; u < kSumLoads; ++u)
                 sum += v[u];
         }
-    share[k][lane] = sum;
+    sum += __shfl_down_sync(0xFFFFFFFFu, sum, 16);
+    sum += __shfl_down_sync(0xFFFFFFFFu, sum, 8);
+    if (lane < kSumCols)
+        share[warp][lane] = sum;
     __syncthreads();
-    if (k != 0 || c >= cols)
+    if (warp != 0 || lane >= kSumCols || c >= cols)
         return;
     sum = share[0][lane];
 #pragma unroll
-    for (int i = 1; i < kSumShares; ++i)
+    for (int i = 1; i < kSumWarps; ++i)
         sum += share[i][lane];
     if (accumulate)
         sum += ld1(dweight + c);
@@ -670,10 +675,11 @@ rmsnorm_dweight_kernel(const float *partials, int n, int cols, GT *dweight, int 
 }
 
 // ---------------------------------------------------------------- pack ----
-// A warp takes spans of kSpan elements of a row, V a lane at a time.
+// A warp takes spans of span_of_pieces(V) elements of a row, V a lane at a time: 1024, or in
+// the narrow forms eight pieces a lane, whose number is then the time of a small matrix.
 
-constexpr int kSpan = 1024;
 constexpr int kPackThreads = 256;
+__host__ __device__ constexpr int span_of_pieces(int v) { return v >= 4 ? 1024 : 8 * 32 * v; }
 
 struct PackArgs {
     const void *x;                            // pack: in; unpack: out
@@ -686,7 +692,7 @@ template <class T, int V, bool Unpack>
 __global__ void __launch_bounds__(kPackThreads)
 pack8_kernel(const PackArgs a)
 {
-    constexpr int N = kSpan / 32 / V;
+    constexpr int kSpan = span_of_pieces(V), N = kSpan / 32 / V;
     const int lane = threadIdx.x & 31;
     const int64_t first = (int64_t)blockIdx.x * (kPackThreads / 32) + (threadIdx.x >> 5);
     const int64_t step = (int64_t)gridDim.x * (kPackThreads / 32);
@@ -788,7 +794,7 @@ BackShape back_shape(int64_t rows, int64_t cols, int sms)
     BackShape b;
     b.elems = cols <= (int64_t)kBackThreads * kBackElems ? kBackElems : kRowElems;
     b.warps = row_warps(cols, b.elems);
-    b.cta = b.warps > kMinWarps ? b.warps : kMinWarps;
+    b.cta = b.warps > kBackMinWarps ? b.warps : kBackMinWarps;
     const int64_t want = (rows + b.cta / b.warps - 1) / (b.cta / b.warps);
     const int64_t most = (int64_t)sms * (16 / b.cta);   // 16 warps an SM
     b.grid = want < most ? want : most;
@@ -882,7 +888,7 @@ int pack_or_unpack(const char *what, const void *x, dpo_dtype dtype, int64_t row
     while (v > 1 && !(cols % v == 0 && whole(x, ld_x, size, v) && whole(p->codes, p->ld_codes, 1, v)))
         v = v == 8 ? 2 : 1;
     PackArgs a = {x, p->codes, p->scales, ld_x, p->ld_codes, p->ld_scales, cols, 0, 0};
-    a.spans = (cols + kSpan - 1) / kSpan;
+    a.spans = (cols + span_of_pieces(v) - 1) / span_of_pieces(v);
     a.items = rows * a.spans;
     const int64_t want = (a.items + kPackThreads / 32 - 1) / (kPackThreads / 32);
     const int64_t grid = want < (int64_t)sms * 8 ? want : (int64_t)sms * 8;
@@ -894,49 +900,75 @@ int pack_or_unpack(const char *what, const void *x, dpo_dtype dtype, int64_t row
     return launch(what, k, grid, kPackThreads, 0, stream, a);
 }
 
-// The instance for these types, V elements an access and CTA size.
-template <template <class, class, int, int> class K, int TB>
-auto pick_vec(int dtype, int wdtype, int v)
+// The kernels by types, elements an access and elements a thread.
+using FwdFn = void (*)(NormForwardArgs);
+using BackFn = void (*)(NormBackArgs);
+using B16 = __nv_bfloat16;
+
+template <int E> FwdFn forward_narrow(int dtype, int wdtype, int v)
 {
-    using B = __nv_bfloat16;
     if (dtype == DPO_F32)
-        return v >= 4 ? K<float, float, 4, TB>::fn() : K<float, float, 1, TB>::fn();
+        return rmsnorm_kernel<float, float, 1, E>;
     if (wdtype == DPO_F32)
-        return v == 8 ? K<B, float, 4, TB>::fn()
-                      : v >= 2 ? K<B, float, 2, TB>::fn() : K<B, float, 1, TB>::fn();
-    return v == 8 ? K<B, B, 8, TB>::fn() : v >= 2 ? K<B, B, 2, TB>::fn() : K<B, B, 1, TB>::fn();
+        return v == 2 ? rmsnorm_kernel<B16, float, 2, E> : rmsnorm_kernel<B16, float, 1, E>;
+    return v == 2 ? rmsnorm_kernel<B16, B16, 2, E> : rmsnorm_kernel<B16, B16, 1, E>;
 }
-template <template <class, class, int, int> class K>
-auto pick(int dtype, int wdtype, int v, int threads)
+FwdFn forward_of(int dtype, int wdtype, int v, int elems)
 {
-    return threads <= kCta ? pick_vec<K, kCta>(dtype, wdtype, v)
-                           : pick_vec<K, kWideCta>(dtype, wdtype, v);
-}
-template <class T, class WT, int V, int TB> struct Fwd {
-    static auto fn() { return &rmsnorm_kernel<T, WT, V, TB>; }
-};
-template <class T, class WT, int V, int E> struct BackH {
-    static auto fn() { return &rmsnorm_backward_kernel<T, WT, V, E, false, false>; }
-};
-template <class T, class WT, int V, int E> struct Back8 {
-    static auto fn() { return &rmsnorm_backward_kernel<T, WT, V, E, true, false>; }
-};
-template <template <class, class, int, int> class K>
-auto pick_back(int dtype, int wdtype, int v, int elems)
-{
-    return elems == kBackElems ? pick_vec<K, kBackElems>(dtype, wdtype, v)
-                               : pick_vec<K, kRowElems>(dtype, wdtype, v);
+    if (v <= 2)
+        return elems == kNarrowElems ? forward_narrow<kNarrowElems>(dtype, wdtype, v)
+                                     : forward_narrow<kRowElems>(dtype, wdtype, v);
+    if (dtype == DPO_F32)
+        return rmsnorm_kernel<float, float, 4, kRowElems>;
+    return wdtype == DPO_F32 ? rmsnorm_kernel<B16, float, 4, kRowElems>
+                             : rmsnorm_kernel<B16, B16, 8, kRowElems>;
 }
 
-// The ring's instance and its shared memory for CTAs of so many threads.
-using BackFn = void (*)(NormBackArgs);
-template <class T, class WT, int V> BackFn ring_of(bool x8, int threads, int *smem)
+template <class T, class WT, int V, int E> BackFn back_regs(bool x8)
+{
+    return x8 ? rmsnorm_backward_kernel<T, WT, V, E, true, false>
+              : rmsnorm_backward_kernel<T, WT, V, E, false, false>;
+}
+template <int E> BackFn back_narrow(int dtype, int wdtype, int v, bool x8)
+{
+    if (dtype == DPO_F32)
+        return back_regs<float, float, 1, E>(x8);
+    if (wdtype == DPO_F32)
+        return v == 2 ? back_regs<B16, float, 2, E>(x8) : back_regs<B16, float, 1, E>(x8);
+    return v == 2 ? back_regs<B16, B16, 2, E>(x8) : back_regs<B16, B16, 1, E>(x8);
+}
+// ... with the ring, and its shared memory for CTAs of so many threads
+template <class T, class WT, int V> BackFn back_ring(bool x8, int threads, int *smem)
 {
     constexpr int E = kBackElems;
     *smem = kDepth * (x8 ? RowSlot<T, V, E, true>::bytes(threads) : RowSlot<T, V, E, false>::bytes(threads));
     return x8 ? rmsnorm_backward_kernel<T, WT, V, E, true, true>
               : rmsnorm_backward_kernel<T, WT, V, E, false, true>;
 }
+// The ring where the pieces are the widest ones and it fits, which it does for bf16.
+BackFn back_of(int dtype, int wdtype, int v, int elems, bool x8, int threads, int *smem)
+{
+    *smem = 0;
+    if (v <= 2)
+        return elems == kBackElems ? back_narrow<kBackElems>(dtype, wdtype, v, x8)
+                                   : back_narrow<kRowElems>(dtype, wdtype, v, x8);
+    if (elems == kBackElems) {
+        const BackFn fn = dtype == DPO_F32    ? back_ring<float, float, 4>(x8, threads, smem)
+                          : wdtype == DPO_F32 ? back_ring<B16, float, 4>(x8, threads, smem)
+                                              : back_ring<B16, B16, 8>(x8, threads, smem);
+        if (*smem <= kMaxSmem)
+            return fn;
+        *smem = 0;
+        return back_regs<float, float, 4, kBackElems>(x8);
+    }
+    if (dtype == DPO_F32)
+        return back_regs<float, float, 4, kRowElems>(x8);
+    return wdtype == DPO_F32 ? back_regs<B16, float, 4, kRowElems>(x8)
+                             : back_regs<B16, B16, 8, kRowElems>(x8);
+}
+// bf16: pieces of 16 bytes, or 8 beside fp32 weights; at most 48 bytes of inputs per
+// 16-byte piece of dy, 16 elements a thread
+static_assert(kDepth * (kBackElems / 8) * 48 * kBackThreads <= kMaxSmem, "the ring fits for bf16");
 
 int check_norm(const char *what, int64_t rows, int64_t cols, int dtype, int wdtype,
                const void *weight)
@@ -1014,11 +1046,12 @@ extern "C" int dpo_rmsnorm(const dpo_rmsnorm_args *args, void *cuda_stream)
              aligned_to(a.weight, a.weight_dtype == DPO_F32 ? (v == 2 ? 8 : 16) : 2 * v) &&
              whole(a.x8.codes, a.x8.ld_codes, 1, v)))
         v = v == 8 ? 2 : 1;
-    const NormForwardArgs k = {a, row_warps(a.cols, kRowElems)};
+    const bool narrow = v <= 2 && a.cols <= (int64_t)kCta * kNarrowElems;
+    const NormForwardArgs k = {a, row_warps(a.cols, narrow ? kNarrowElems : kRowElems)};
     const int cta = k.warps > kMinWarps ? k.warps : kMinWarps;
     const int64_t grid = (a.rows + cta / k.warps - 1) / (cta / k.warps);
-    return launch(what, pick<Fwd>(a.dtype, a.weight_dtype, v, cta * 32), grid, cta * 32, 0,
-                  cuda_stream, k);
+    return launch(what, forward_of(a.dtype, a.weight_dtype, v, narrow ? kNarrowElems : kRowElems), grid,
+                  cta * 32, 0, cuda_stream, k);
 }
 
 extern "C" int dpo_rmsnorm_workspace(int64_t rows, int64_t cols, int64_t *bytes)
@@ -1110,35 +1143,25 @@ extern "C" int dpo_rmsnorm_backward(const dpo_rmsnorm_backward_args *args, void 
              whole(codes, a.x8.ld_codes, 1, v)))
         v = v == 8 ? 2 : 1;
     const NormBackArgs k = {a, shape.warps, static_cast<float *>(a.workspace)};
-    // the ring where the pieces are the widest ones and it fits
-    const bool x8 = a.h == nullptr;
-    int smem = shape.cta > shape.warps ? (int)a.cols * 4 : 0, ring = 0;
-    BackFn fn = x8 ? pick_back<Back8>(a.dtype, a.weight_dtype, v, shape.elems)
-                   : pick_back<BackH>(a.dtype, a.weight_dtype, v, shape.elems);
-    if (v >= 4 && shape.elems == kBackElems) {
-        using B = __nv_bfloat16;
-        const int threads = shape.cta * 32;
-        const BackFn with = a.dtype == DPO_F32 ? ring_of<float, float, 4>(x8, threads, &ring)
-                            : a.weight_dtype == DPO_F32 ? ring_of<B, float, 4>(x8, threads, &ring)
-                                                        : ring_of<B, B, 8>(x8, threads, &ring);
-        if (ring <= kMaxSmem) {
-            fn = with;
-            smem = ring > smem ? ring : smem;
-            const cudaError_t e = cudaFuncSetAttribute(
-                reinterpret_cast<const void *>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
-            if (e != cudaSuccess)
-                return call_fail(DPO_ECUDA, "%s: %s", what, cudaGetErrorString(e));
-        }
+    int smem = 0;
+    const BackFn fn = back_of(a.dtype, a.weight_dtype, v, shape.elems, a.h == nullptr, shape.cta * 32, &smem);
+    if (smem > 0) {
+        const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(fn),
+                                                   cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+        if (e != cudaSuccess)
+            return call_fail(DPO_ECUDA, "%s: %s", what, cudaGetErrorString(e));
     }
+    const int sums = shape.cta > shape.warps ? (int)a.cols * 4 : 0;   // of the CTA's rows
+    smem = smem > sums ? smem : sums;
     rc = launch(what, fn, grid, shape.cta * 32, (size_t)smem, cuda_stream, k);
     if (rc != DPO_OK || a.dweight == nullptr)
         return rc;
-    const int64_t sum_grid = (a.cols + 31) / 32;
+    const int64_t sum_grid = (a.cols + kSumCols - 1) / kSumCols;
     if (a.dweight_dtype == DPO_F32)
-        return launch(what, rmsnorm_dweight_kernel<float>, sum_grid, 32 * kSumShares, 0, cuda_stream,
+        return launch(what, rmsnorm_dweight_kernel<float>, sum_grid, 32 * kSumWarps, 0, cuda_stream,
                       static_cast<const float *>(k.partials), (int)grid, (int)a.cols,
                       static_cast<float *>(a.dweight), a.accumulate);
-    return launch(what, rmsnorm_dweight_kernel<__nv_bfloat16>, sum_grid, 32 * kSumShares, 0,
+    return launch(what, rmsnorm_dweight_kernel<__nv_bfloat16>, sum_grid, 32 * kSumWarps, 0,
                   cuda_stream, static_cast<const float *>(k.partials), (int)grid, (int)a.cols,
                   static_cast<__nv_bfloat16 *>(a.dweight), a.accumulate);
 }
