@@ -284,7 +284,7 @@ Form form_of(const Device &d, const Shape *s, int n, int epi)
 }
 
 int run(const char *what, const Device &d, Launch &L, const Shape *s, int n, int epi, Form f,
-        bool maps_ok, void *stream)
+        bool followed, bool maps_ok, void *stream)
 {
     const int cg = f.cg;
     if (!maps_ok)
@@ -307,6 +307,7 @@ int run(const char *what, const Device &d, Launch &L, const Shape *s, int n, int
     L.err = d.err;
     L.a_rows = f.a_rows;
     const int64_t slots = slots_of(d, f, epi);
+    L.early = followed;
     return launch_clusters(what, kernel_of(f, epi), (total < slots ? total : slots) * f.cluster(),
                            f.cluster(), kThreads, (size_t)f.smem(), stream, L);
 }
@@ -516,7 +517,7 @@ extern "C" int dpo_ffn_forward(const dpo_ffn_args *args, void *cuda_stream)
         }
         P.keep = a.keep;
         P.act = a.act;
-        if ((rc = run(what, *d, L, &s, 1, kGate, form, m.ok, cuda_stream)) != DPO_OK)
+        if ((rc = run(what, *d, L, &s, 1, kGate, form, true, m.ok, cuda_stream)) != DPO_OK)
             return rc;
     }
     const Shape s = {T, D, F, 1};
@@ -528,7 +529,7 @@ extern "C" int dpo_ffn_forward(const dpo_ffn_args *args, void *cuda_stream)
     m.bf16(&L.p[0].d0, a.out, T, D, a.ld_out);
     L.p[0].o0 = static_cast<__nv_bfloat16 *>(a.out);
     L.p[0].ld_o = a.ld_out;
-    return run(what, *d, L, &s, 1, kStore, form, m.ok, cuda_stream);
+    return run(what, *d, L, &s, 1, kStore, form, false, m.ok, cuda_stream);
 }
 
 extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_stream)
@@ -648,7 +649,7 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
                  (a.keep != DPO_KEEP_8BIT ||
                   (reinterpret_cast<uintptr_t>(P.scale_g) % 4 == 0 &&
                    reinterpret_cast<uintptr_t>(P.scale_u) % 4 == 0 && P.ld_scale % 4 == 0));
-        if ((rc = run(what, *d, L, &s, 1, epi, form, m.ok, cuda_stream)) != DPO_OK)
+        if ((rc = run(what, *d, L, &s, 1, epi, form, true, m.ok, cuda_stream)) != DPO_OK)
             return rc;
     }
     Launch L{};
@@ -692,7 +693,7 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
             P.gain_f32 = a.gain_dtype == DPO_F32;
         }
     }
-    return run(what, *d, L, s, n, kStore, form_of(*d, s, n, kStore), m.ok, cuda_stream);
+    return run(what, *d, L, s, n, kStore, form_of(*d, s, n, kStore), false, m.ok, cuda_stream);
 }
 
 extern "C" int dpo_ffn_get_status(uint32_t *bits)

@@ -81,7 +81,12 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(const FewArgs a)
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
     const int col0 = (int)(blockIdx.x / ranks) * kOut;
-    pdl_wait();
+    if (EPI == kGate) {
+        pdl_wait();
+        // The second product's CTAs may take the places that this one's leave: they start
+        // once all of these are here, behind all earlier work of the stream.
+        launch_dependents();
+    }
 
     // this lane's rows g and g + 8 and its token; past the end they read the last ones
     const __nv_bfloat16 *w[2];
@@ -108,6 +113,10 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(const FewArgs a)
             }
     };
     load_w(k0);
+    // The second product follows the first one in the same call, which has waited for all
+    // that came before it and writes no weights: its first weights are read ahead.
+    if (EPI != kGate)
+        pdl_wait();
     for (; k0 - t * 8 < a.k; k0 += step) {
         uint4 cur[2][U];
 #pragma unroll

@@ -129,8 +129,14 @@ struct Launch {
     Product p[kMaxProducts];
     int n_products, n_tiles;
     int a_rows;                   // rows of A in a stage (BM but where K is split)
+    int early;                    // another launch of this kernel follows in the same call
     unsigned int *err;
 };
+
+__device__ __forceinline__ void launch_dependents()
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
 
 // 2-D TMA load and store (see the 3-D ones in dpo_gemm.cuh).
 template <int CG>
@@ -191,6 +197,23 @@ __device__ __forceinline__ Tile tile_at(const Launch &L, int t)
     return {p, b * kBandRows + r - n * rows, n};
 }
 
+// 2^x and 1 / x by the hardware's approximations (relative errors of about 2^-22 and 2^-23),
+// without the steps that keep subnormal results: 1 + 2^x does not see them, and its
+// reciprocal, of a number from 1 to infinity, is 0 where it would be one. The epilogues are
+// bound by their instructions: with __expf and __fdividef 36 a value for the gate.
+__device__ __forceinline__ float exp2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // act(z) = z s(q(z)) with s the logistic function: SiLU with q = z, GELU's tanh form
 // with q = 2 sqrt(2/pi) (z + 0.044715 z^3), since (1 + tanh(q / 2)) / 2 = s(q).
 // act' = s + z q' s (1 - s).
@@ -204,7 +227,7 @@ __device__ __forceinline__ float logistic(float z, float &dq)
         q = z * fmaf(k, z2, c);
         dq = fmaf(3.0f * k, z2, c);
     }
-    return __fdividef(1.0f, 1.0f + __expf(-q));
+    return rcp(1.0f + exp2(-1.4426950408889634f * q));
 }
 
 // Scale byte of the first n of 32 values that one lane holds; infinities become NaN (rare:
@@ -842,6 +865,12 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
         }
     }
     pdl_wait();
+    // The next launch's CTAs, one to an SM like these, may set themselves up wherever one
+    // of these has ended; they wait at the same place until all of them have. Only where
+    // the next launch is this kernel's: others spread unevenly (dpo_device.cuh). Forward of
+    // 768 x 2048 widths, 17 to 200 tokens: 16.4 -> 15.1 us.
+    if (L.early)
+        launch_dependents();
 
     if (warp == 0) {
         if (lane == 0) {
@@ -1005,7 +1034,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                 mbar_arrive<CG>(acc_empty(a));
         }
         if (lane == 0)
-            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
         __syncwarp();
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     }
