@@ -606,12 +606,6 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
     void *dg = ws, *du = ws + hb, *act = ws + 2 * hb;
     const void *x = a.x;
     int64_t ld_x = a.ld_x;
-    if (from_x8) {
-        if ((rc = dpo_unpack8(&a.x8, T, D, ws + 3 * hb, DPO_BF16, D, cuda_stream)) != DPO_OK)
-            return rc;
-        x = ws + 3 * hb;
-        ld_x = D;
-    }
     {
         const Shape s = {T, F, D, 1};
         const int epi = a.keep == DPO_KEEP_8BIT ? kGateBack8 : kGateBack16;
@@ -650,6 +644,12 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
                   (reinterpret_cast<uintptr_t>(P.scale_g) % 4 == 0 &&
                    reinterpret_cast<uintptr_t>(P.scale_u) % 4 == 0 && P.ld_scale % 4 == 0));
         if ((rc = run(what, *d, L, &s, 1, epi, form, true, m.ok, cuda_stream)) != DPO_OK)
+            return rc;
+    }
+    if (from_x8) {   // needed by the next launch only: beside the one just made
+        x = ws + 3 * hb;
+        ld_x = D;
+        if ((rc = unpack8_beside(a.x8, T, D, ws + 3 * hb, cuda_stream)) != DPO_OK)
             return rc;
     }
     Launch L{};

@@ -686,6 +686,7 @@ struct PackArgs {
     uint8_t *codes, *scales;
     int64_t ld_x, ld_codes, ld_scales;
     int64_t cols, spans, items;               // spans per row, rows * spans
+    int beside;                               // see unpack8_beside
 };
 
 template <class T, int V, bool Unpack>
@@ -696,7 +697,10 @@ pack8_kernel(const PackArgs a)
     const int lane = threadIdx.x & 31;
     const int64_t first = (int64_t)blockIdx.x * (kPackThreads / 32) + (threadIdx.x >> 5);
     const int64_t step = (int64_t)gridDim.x * (kPackThreads / 32);
-    pdl_wait();
+    if (a.beside)
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    else
+        pdl_wait();
     for (int64_t item = first; item < a.items; item += step) {
         const int64_t row = item / a.spans, c0 = (item - row * a.spans) * kSpan;
         T *const xp = const_cast<T *>(static_cast<const T *>(a.x)) + row * a.ld_x;
@@ -751,6 +755,8 @@ pack8_kernel(const PackArgs a)
             }
         }
     }
+    if (a.beside)
+        pdl_wait();
 }
 
 // ---------------------------------------------------------------- host ----
@@ -860,7 +866,7 @@ auto pack_kernel(int v) -> void (*)(PackArgs)
 }
 
 int pack_or_unpack(const char *what, const void *x, dpo_dtype dtype, int64_t rows, int64_t cols,
-                   int64_t ld_x, const dpo_packed8 *p, bool unpack, void *stream)
+                   int64_t ld_x, const dpo_packed8 *p, bool unpack, void *stream, bool beside = false)
 {
     if (!known(dtype))
         return call_fail(DPO_EDTYPE, "%s: dtype %d", what, (int)dtype);
@@ -887,7 +893,7 @@ int pack_or_unpack(const char *what, const void *x, dpo_dtype dtype, int64_t row
     int v = dtype == DPO_BF16 ? 8 : 4;
     while (v > 1 && !(cols % v == 0 && whole(x, ld_x, size, v) && whole(p->codes, p->ld_codes, 1, v)))
         v = v == 8 ? 2 : 1;
-    PackArgs a = {x, p->codes, p->scales, ld_x, p->ld_codes, p->ld_scales, cols, 0, 0};
+    PackArgs a = {x, p->codes, p->scales, ld_x, p->ld_codes, p->ld_scales, cols, 0, 0, beside};
     a.spans = (cols + span_of_pieces(v) - 1) / span_of_pieces(v);
     a.items = rows * a.spans;
     const int64_t want = (a.items + kPackThreads / 32 - 1) / (kPackThreads / 32);
@@ -981,6 +987,13 @@ int check_norm(const char *what, int64_t rows, int64_t cols, int dtype, int wdty
 }
 
 }  // namespace
+
+int unpack8_beside(const dpo_packed8 &in, int64_t rows, int64_t cols, void *out, void *cuda_stream)
+{
+    return pack_or_unpack("dpo_ffn_backward", out, DPO_BF16, rows, cols, cols, &in, true, cuda_stream,
+                          true);
+}
+
 }  // namespace dpo
 
 using namespace dpo;

@@ -11,6 +11,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <ATen/ops/empty_strided.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -209,11 +210,11 @@ Packed make_packed(int64_t rows, int64_t cols, at::Device device, int64_t pitch)
 {
     Packed q;
     const int64_t ld = (cols + pitch - 1) / pitch * pitch, ng = groups(cols);
-    q.codes = make({rows, ld}, at::kByte, device);
+    q.codes = ld == cols ? make({rows, cols}, at::kByte, device)
+                         : at::empty_strided({rows, cols}, {ld, 1},
+                                             at::TensorOptions().dtype(at::kByte).device(device));
     q.scales = make({rows, ng}, at::kByte, device);
     q.p = {(uint8_t *)q.codes.data_ptr(), (uint8_t *)q.scales.data_ptr(), ld, ng};
-    if (ld != cols)
-        q.codes = q.codes.slice(1, 0, cols);
     return q;
 }
 
