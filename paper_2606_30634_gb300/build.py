@@ -41,7 +41,8 @@ LIBS = {
         "headers": ["csrc/dpo_internal.h", "csrc/dpo_device.cuh", "csrc/dpo_reduce.cuh",
                     "csrc/dpo_step.cuh",
                     "csrc/dpo_gemm.cuh", "csrc/dpo_call.h", "csrc/dpo_pack8.cuh",
-                    "csrc/dpo_ffn_gemm.cuh", "csrc/dpo_ffn_few.cuh", "../include/dpo.h", "../include/dpo_muon.h"],
+                    "csrc/dpo_ffn_gemm.cuh", "csrc/dpo_ffn_few.cuh", "../include/dpo.h",
+                    "../include/dpo_muon.h"],
         "includes": ["csrc"],
         "ptxas_v": ["csrc/dpo_step_adamw.cu", "csrc/dpo_muon.cu", "csrc/dpo_ffn.cu"],
     },
@@ -70,9 +71,9 @@ def _torch_flags():
     import sysconfig
     import torch
     root = os.path.dirname(torch.__file__)
+    nvcc = shutil.which(NVCC) or "/usr/local/cuda/bin/nvcc"
     inc = [os.path.join(root, "include"), sysconfig.get_paths()["include"],
-           os.path.join(os.path.dirname(os.path.dirname(shutil.which(NVCC) or "/usr/local/cuda/bin/nvcc")),
-                        "include")]
+           os.path.join(os.path.dirname(os.path.dirname(nvcc)), "include")]
     lib = os.path.join(root, "lib")
     abi = int(torch._C._GLIBCXX_USE_CXX11_ABI)
     return (["-O2", "-std=c++17", "-fPIC", "-w", f"-D_GLIBCXX_USE_CXX11_ABI={abi}", "-I", INCLUDE] +

@@ -323,7 +323,8 @@ int run_few(const char *what, const FewArgs &a, int epi, int sms, void *stream)
     int split = 1;
     while (split < 8 && units * split < (int64_t)sms * kFewCtas && a.k > split * kFewWarps * 64)
         split *= 2;
-    return launch_clusters(what, epi == kGate ? few_kernel<kGate> : few_kernel<kStore>, units * split, split, kFewThreads, 0, stream, a);
+    return launch_clusters(what, epi == kGate ? few_kernel<kGate> : few_kernel<kStore>,
+                           units * split, split, kFewThreads, 0, stream, a);
 }
 
 int64_t align_up(int64_t v) { return (v + 255) / 256 * 256; }

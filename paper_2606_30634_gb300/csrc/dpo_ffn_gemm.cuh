@@ -24,7 +24,8 @@
 //   kGate      the tile's columns are T / 2 of G beside the same T / 2 of U (the B
 //              operand is half w_gate rows, half w_up rows), so act(G) U is formed
 //              where both are in registers; writes A and what is kept of G and U
-//   kGateBack8, kGateBack16  the tile is of dA; reads what was kept of G and U, writes dG, dU, A
+//   kGateBack8, kGateBack16  the tile is of dA; reads what was kept of G and U (8 bits, or
+//              bf16), writes dG, dU and A
 //   kStore     writes D in bf16 or fp32, with factors along the columns and the old
 //              contents added where asked for
 #pragma once
@@ -377,9 +378,9 @@ __device__ __forceinline__ void back_pair(float2 g, float2 u, float2 da, uint32_
 // warp touches 32 lines whatever its width, and their number is what the loads cost (1B
 // layer, the whole launch: 8-byte pieces 142 us, 16-byte ones 125, no loads at all 112):
 // Product::wide says that all rows are 32-byte aligned and whole chunks of 128 columns, so
-// a row's chunk of codes is one load (past L1: 134 -> 124 us) and four chunks' scales another. Otherwise rows and
-// pitches are 16-byte aligned and hidden is a multiple of 8: pieces of 8 elements.
-// Rows past the end read the last one.
+// a row's chunk of codes is one load (past L1: 134 -> 124 us) and four chunks' scales
+// another. Otherwise rows and pitches are 16-byte aligned and hidden is a multiple of 8:
+// pieces of 8 elements. Rows past the end read the last one.
 template <bool CODES> struct Kept {
     static constexpr int W = CODES ? 2 : 4;   // words of 8 elements
     uint32_t g[4 * W], u[4 * W];

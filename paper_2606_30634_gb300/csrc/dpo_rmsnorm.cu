@@ -322,7 +322,8 @@ rmsnorm_kernel(const NormForwardArgs args)
 // once, since HBM answers after about 2 us under load and a row is 12 to 24 bytes a
 // column. With 16-byte pieces (RING) each thread copies its own pieces of the next three
 // rows to shared memory with cp.async, in places that only it reads, so no barrier
-// guards them. GB300, 8192 x 4096 from 8-bit rows: one row ahead in registers 65 us.
+// guards them. GB300, 8192 x 4096 from 8-bit rows: one row ahead in registers 65 us, the
+// ring 46 with the sum of the partial rows (5.1 TB/s of the 236 MB).
 struct NormBackArgs {
     dpo_rmsnorm_backward_args a;
     int warps;

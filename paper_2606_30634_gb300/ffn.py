@@ -14,9 +14,8 @@ gradients into ``opt.grads(i)``, which the next ``opt.step`` reads:
     dx, _ = ffn.add_rms_norm_backward(dy, w_norm, n.rstd, x8=n.x8, dh=dout, dweight=dw_norm)
 
 Every step of it runs in libdpo.so's kernels; PyTorch provides memory and streams, and
-dpo_tensors (csrc/dpo_tensors.cpp) checks the tensors and makes the calls. Tensors are on the
-current CUDA device; their last dimension is contiguous and the
-others flatten to rows. Outputs are allocated unless given. Calls go to PyTorch's
+dpo_tensors (csrc/dpo_tensors.cpp) checks the tensors and makes the calls. Tensors are on
+the current CUDA device; their last dimension is contiguous and the others flatten to rows. Outputs are allocated unless given. Calls go to PyTorch's
 current stream, or to ``stream=`` (a torch.cuda.Stream), on which the outputs and
 workspaces are then allocated too; tensors last used on another stream need the usual
 event or ``wait_stream`` before the call. ValueError and TypeError for tensors that do
@@ -24,17 +23,16 @@ not fit, DpoError for what the library refuses.
 """
 from __future__ import annotations
 
+import ctypes
 import importlib.util
 import os
 from typing import NamedTuple, Optional, Tuple
 
-import ctypes
 import torch
 
 from . import build as _build
 from . import dpo as _dpo
-from .dpo import (DPO_ACT_GELU, DPO_ACT_SILU, DPO_KEEP_8BIT, DPO_KEEP_BF16, DPO_KEEP_NONE,
-                  DPO_PACK8_GROUP as GROUP)
+from .dpo import DPO_ACT_GELU, DPO_ACT_SILU, DPO_KEEP_8BIT, DPO_KEEP_BF16, DPO_KEEP_NONE
 
 ACTIVATIONS = {"silu": DPO_ACT_SILU, "gelu": DPO_ACT_GELU}
 KEEP = {"none": DPO_KEEP_NONE, "8bit": DPO_KEEP_8BIT, "bf16": DPO_KEEP_BF16}
