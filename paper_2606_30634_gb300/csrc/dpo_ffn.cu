@@ -56,13 +56,14 @@ EncodeTiled g_encode = nullptr;
 struct Form {
     int cg;
     bool thin;
-    int ways, a_rows;
+    int ways, a_rows, cols;       // rows of A a stage loads, a tile's columns
     int cluster() const { return cg * ways; }
     int bk() const { return thin ? Ring<true>::BK : Ring<false>::BK; }
-    int smem() const { return thin ? Ring<true>::smem(a_rows) : Ring<false>::smem(BM); }
+    int smem() const { return thin ? Ring<true>::smem(a_rows, cols) : Ring<false>::smem(BM, BH); }
 };
-constexpr Form kPairs = {2, false, 1, BM}, kSingles = {1, false, 1, BM};
-Form thin(int ways, int a_rows) { return {1, true, ways, a_rows}; }
+constexpr Form kPairs = {2, false, 1, BM, kTile(2)};
+Form single(int a_rows) { return {1, false, 1, a_rows, kTile(1)}; }
+Form thin(int ways, int a_rows, int cols) { return {1, true, ways, a_rows, cols}; }
 
 int slots_of(const Device &d, Form f, int epi)
 {
@@ -126,11 +127,13 @@ cudaError_t prepare(Device &d)
             return cudaErrorNotSupported;
         g_encode = reinterpret_cast<EncodeTiled>(p);
     }
-    for (const Form f : {kPairs, kSingles, thin(1, BM), thin(2, BM), thin(4, BM), thin(8, BM)})
+    // (every form of a kernel has an SM to itself)
+    for (const Form f : {kPairs, single(BM), thin(1, BM, BH), thin(2, BM, BH), thin(4, BM, BH),
+                         thin(8, BM, BH)})
         for (int epi = 0; epi < kForms; ++epi) {
             const void *k = reinterpret_cast<const void *>(kernel_of(f, epi));
             cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                 f.smem());
+                                                 kMaxSmem);
             if (e != cudaSuccess)
                 return e;
             cudaLaunchAttribute attr = cluster_of(f.cluster());
@@ -230,11 +233,13 @@ struct Shape {
     int segments;
 };
 
-int64_t tiles_of(const Shape &s, int cg, int epi)
+int64_t m_tiles(const Shape &s, const Form &f) { return (s.m + kTile(f.cg) - 1) / kTile(f.cg); }
+int64_t n_tiles(const Shape &s, const Form &f, int epi)
 {
-    const int64_t t = kTile(cg), tn = epi == kGate ? t / 2 : t;
-    return (s.m + t - 1) / t * ((s.n + tn - 1) / tn);
+    const int64_t tn = epi == kGate ? f.cols / 2 : f.cols;
+    return (s.n + tn - 1) / tn;
 }
+int64_t tiles_of(const Shape &s, const Form &f, int epi) { return m_tiles(s, f) * n_tiles(s, f, epi); }
 
 // The form of a launch: the one with the smallest estimate of its time in ns, tiles dealt
 // round-robin. A K block costs what its stage of the ring waits for, about 2 us over the
@@ -247,18 +252,20 @@ int64_t tiles_of(const Shape &s, int cg, int epi)
 Form form_of(const Device &d, const Shape *s, int n, int epi)
 {
     const int a_rows = s[0].m <= 32 ? 32 : s[0].m <= 64 ? 64 : BM;
-    const Form forms[] = {kSingles, thin(1, a_rows), thin(2, a_rows), thin(4, a_rows),
-                          thin(8, a_rows), kPairs};
+    const Form forms[] = {single(n == 1 ? a_rows : BM), thin(1, a_rows, BH), thin(2, a_rows, BH),
+                          thin(4, a_rows, BH), thin(8, a_rows, BH), thin(1, a_rows, BH / 2),
+                          thin(2, a_rows, BH / 2), thin(4, a_rows, BH / 2),
+                          thin(8, a_rows, BH / 2), kPairs};
     Form best = kPairs;
     double least = 1e30;
     for (const Form &f : forms) {
-        const double block = f.cg == 2 ? 700.0 : 2000.0 / (f.thin ? Ring<true>::stages(f.a_rows) : 3);
+        const double block = f.cg == 2 ? 700.0 : 2000.0 / (f.thin ? Ring<true>::stages(f.a_rows, f.cols) : 3);
         const double epilogue = f.cg == 2 ? 3000.0 : f.thin ? 3000.0 : 1500.0;
         const int64_t slots = slots_of(d, f, epi);
         int64_t tiles = 0;
         double work = 0.0, longest = 0.0, weights = 0.0;
         for (int i = 0; i < n; ++i)
-            tiles += tiles_of(s[i], f.cg, epi);
+            tiles += tiles_of(s[i], f, epi);
         if (f.cg == 1 && !f.thin && tiles > 4 * slots)
             return kPairs;
         if (f.thin && (n > 1 || blocks_of(s[0].k, f.bk()) < 2 * f.ways))
@@ -267,7 +274,7 @@ Form form_of(const Device &d, const Shape *s, int n, int epi)
             const int64_t blocks = blocks_of(s[i].k, f.bk()) * s[i].segments;
             const double c = (double)((blocks + f.ways - 1) / f.ways) * block;
             const double each = f.thin ? c + 2500.0 : c > epilogue ? c : epilogue;
-            work += (double)tiles_of(s[i], f.cg, epi) * each;
+            work += (double)tiles_of(s[i], f, epi) * each;
             longest = longest > each ? longest : each;
             weights += (double)(s[i].n * s[i].k * s[i].segments) * (epi == kGate ? 4.0 : 2.0) / 6500.0;
         }
@@ -286,26 +293,25 @@ Form form_of(const Device &d, const Shape *s, int n, int epi)
 int run(const char *what, const Device &d, Launch &L, const Shape *s, int n, int epi, Form f,
         bool followed, bool maps_ok, void *stream)
 {
-    const int cg = f.cg;
     if (!maps_ok)
         return call_fail(DPO_ECUDA, "%s: a tensor map was refused", what);
     int64_t total = 0;
     for (int i = 0; i < n; ++i) {
-        const int64_t t = kTile(cg), tn = epi == kGate ? t / 2 : t;
         Product &P = L.p[i];
         P.m = (int)s[i].m;
         P.n = (int)s[i].n;
         P.k_blocks[0] = (int)blocks_of(s[i].k, f.bk());
         P.k_blocks[1] = s[i].segments == 2 ? P.k_blocks[0] : 0;
-        P.m_tiles = (int)((s[i].m + t - 1) / t);
-        P.n_tiles = (int)((s[i].n + tn - 1) / tn);
+        P.m_tiles = (int)m_tiles(s[i], f);
+        P.n_tiles = (int)n_tiles(s[i], f, epi);
         P.first = (int)total;
-        total += tiles_of(s[i], cg, epi);
+        total += tiles_of(s[i], f, epi);
     }
     L.n_products = n;
     L.n_tiles = (int)total;
     L.err = d.err;
     L.a_rows = f.a_rows;
+    L.cols = f.cols;
     const int64_t slots = slots_of(d, f, epi);
     L.early = followed;
     return launch_clusters(what, kernel_of(f, epi), (total < slots ? total : slots) * f.cluster(),
@@ -342,7 +348,7 @@ int check_sizes(const char *what, int64_t tokens, int64_t dim, int64_t hidden)
     const Shape s[] = {{tokens, hidden, dim, 1}, {tokens, dim, hidden, 1}, {hidden, dim, tokens, 1}};
     bool fits = tokens <= kMaxSide && dim <= kMaxSide && hidden <= kMaxSide;
     for (const Shape &q : s)
-        fits = fits && tiles_of(q, 2, kGate) < ((int64_t)1 << 28);
+        fits = fits && tiles_of(q, kPairs, kGate) < ((int64_t)1 << 28);
     if (!fits)
         return call_fail(DPO_EINVAL, "%s: %lld x %lld x %lld is too large", what, (long long)tokens,
                          (long long)dim, (long long)hidden);
@@ -488,13 +494,13 @@ extern "C" int dpo_ffn_forward(const dpo_ffn_args *args, void *cuda_stream)
     {
         const Shape s = {T, F, D, 1};
         const Form form = form_of(*d, &s, 1, kGate);
-        const int cg = form.cg;
+        const int rows_w = form.cg == 2 ? BH : form.cols / 2;   // a box of either projection
         Launch L{};
         Maps m;
         Product &P = L.p[0];
         m.operand(&P.a[0], a.x, T, D, a.ld_x, form.a_rows);
-        m.operand(&P.b[0], a.w_gate, F, D, D, cg == 2 ? BH : BH / 2);
-        m.operand(&P.b[1], a.w_up, F, D, D, cg == 2 ? BH : BH / 2);
+        m.operand(&P.b[0], a.w_gate, F, D, D, rows_w);
+        m.operand(&P.b[1], a.w_up, F, D, D, rows_w);
         m.bf16(&P.d0, a.workspace, T, F, F);
         P.o0 = static_cast<__nv_bfloat16 *>(a.workspace);
         P.ld_o = F;
@@ -526,7 +532,7 @@ extern "C" int dpo_ffn_forward(const dpo_ffn_args *args, void *cuda_stream)
     Maps m;
     const Form form = form_of(*d, &s, 1, kStore);
     m.operand(&L.p[0].a[0], a.workspace, T, F, F, form.a_rows);
-    m.operand(&L.p[0].b[0], a.w_down, D, F, F, BH);
+    m.operand(&L.p[0].b[0], a.w_down, D, F, F, form.cg == 2 ? BH : form.cols);
     m.bf16(&L.p[0].d0, a.out, T, D, a.ld_out);
     L.p[0].o0 = static_cast<__nv_bfloat16 *>(a.out);
     L.p[0].ld_o = a.ld_out;

@@ -72,27 +72,27 @@ constexpr int kThreads = 64 + 32 * kEpiWarps;
 // 32, 64 or 128 rows that a product of so few tokens has. The MMA reads 128 rows all the
 // same; what lies behind a short box ends up in accumulator rows that nothing reads.
 constexpr int kRowBytes = kBoxK * 2;                          // of a box: the swizzle span
-constexpr int kMaxStages = 10;
+constexpr int kMaxStages = 16;
+constexpr int kMaxSmem = 232448 - 1024;   // of a CTA, beside its static variables
 template <bool SPLIT> struct Ring {
     static constexpr int BK = SPLIT ? 64 : 128;
     static constexpr int box = BM * kRowBytes;                // of one box of 128 rows
     static constexpr int staging = SPLIT ? 8192 : 2 * kChunkBytes;   // per epilogue warp
-    static __host__ __device__ constexpr int a_bytes(int rows) { return rows * BK * 2; }
-    static constexpr int b_bytes = BH * BK * 2;
+    // of a stage: `rows` of A, `cols` of B
+    static __host__ __device__ constexpr int bytes(int n) { return n * BK * 2; }
     // epilogue warps of tiles with so many rows
     static __host__ __device__ constexpr int warps(int rows) { return kEpiWarps * rows / BM; }
-    static __host__ __device__ constexpr int stages(int rows)
+    static __host__ __device__ constexpr int stages(int rows, int cols)
     {
-        return !SPLIT ? 3 : rows == 32 ? 10 : rows == 64 ? 8 : 5;
+        const int fit = (kMaxSmem - 1024 - warps(rows) * staging) / (bytes(rows) + bytes(cols));
+        return fit < kMaxStages ? fit : kMaxStages;
     }
-    static __host__ __device__ constexpr int smem(int rows)
+    static __host__ __device__ constexpr int smem(int rows, int cols)
     {
-        return stages(rows) * (a_bytes(rows) + b_bytes) + 1024 + warps(rows) * staging;
+        return stages(rows, cols) * (bytes(rows) + bytes(cols)) + 1024 + warps(rows) * staging;
     }
 };
-static_assert(Ring<true>::smem(32) <= 232448 && Ring<true>::smem(64) <= 232448 &&
-                  Ring<true>::smem(128) <= 232448 && Ring<false>::smem(BM) <= 232448,
-              "shared memory of a CTA");
+static_assert(Ring<false>::stages(BM, BH) == 3, "stages");
 
 constexpr int kMaxProducts = 4;
 constexpr int kBandRows = 16;   // block rows per band, as in dpo_gemm.cuh
@@ -129,10 +129,43 @@ struct Product {
 struct Launch {
     Product p[kMaxProducts];
     int n_products, n_tiles;
-    int a_rows;                   // rows of A in a stage (BM but where K is split)
+    int a_rows;                   // rows of A that a stage loads, BM where A is M-contiguous
+    int cols;                     // single CTAs: the tile's columns, kTile(1), or half of them
+                                  // where K is split
     int early;                    // another launch of this kernel follows in the same call
     unsigned int *err;
 };
+
+// A value that every lane of the warp has, known to be so by the compiler: what the copies
+// and MMAs take from uniform registers then comes without a move to them each time.
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
+
+// True in one lane of the (whole) warp.
+__device__ __forceinline__ bool elect()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0u;
+}
+
+// By the whole warp: false when the wait gave up in any lane, or another role did (*aborted,
+// set here too); looked at only where the phase is not there yet.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *aborted)
+{
+    if (__all_sync(0xFFFFFFFFu, gemm::mbar_try(bar, parity)))
+        return true;
+    const unsigned long long t0 = gemm::globaltimer();
+    for (;;) {
+        const bool there = gemm::mbar_try(bar, parity);
+        if (__all_sync(0xFFFFFFFFu, there))
+            return true;
+        if (__any_sync(0xFFFFFFFFu, *aborted || gemm::globaltimer() - t0 > gemm::kWaitNs)) {
+            *aborted = 1;
+            return false;
+        }
+    }
+}
 
 __device__ __forceinline__ void launch_dependents()
 {
@@ -166,11 +199,11 @@ __device__ __forceinline__ void tma_store(const CUtensorMap *map, uint32_t src, 
                  : "memory");
 }
 
-// kind::f16 with fp32 accumulation and bf16 operands, M = N = kTile(cg), operands
+// kind::f16 with fp32 accumulation and bf16 operands, M = kTile(cg), operands
 // K-major, or MN-major with bits 15 (A) and 16 (B).
-__device__ __forceinline__ uint32_t idesc_of(int cg, int a_mn, int b_mn)
+__device__ __forceinline__ uint32_t idesc_of(int cg, int n, int a_mn, int b_mn)
 {
-    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTile(cg) >> 3) << 17) |
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) |
            ((uint32_t)(kTile(cg) >> 4) << 24) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16);
 }
 
@@ -642,31 +675,46 @@ struct Exchange {
     {
         return !give_up(mbar_wait_cluster(xfull, (uint32_t)turn & 1u));
     }
-    // In lanes below 32 / ranks: the total of row 32 / ranks * rank + lane.
-    __device__ __forceinline__ void total(int chunk, float (&v)[32]) const
+    // Once landed, the warp's 32 / ranks rows are dealt to its lanes in pieces of 4 columns:
+    // `ranks` lanes to a row, pieces() of each chunk to a lane. Eight lanes read 128
+    // consecutive bytes of the buffer's banks at a time. A lane's values are few, so the code
+    // is short: run once in a launch, it costs its way to the instruction cache.
+    __device__ __forceinline__ int pieces() const { return 8 / (int)ranks; }
+    __device__ __forceinline__ int my_row() const   // of the 32
+    {
+        return (int)rank * (32 / (int)ranks) + lane / (int)ranks;
+    }
+    __device__ __forceinline__ int granule(int i) const   // where the buffer has piece i
+    {
+        return lane % (int)ranks + (int)ranks * ((i + lane / (int)ranks) & (pieces() - 1));
+    }
+    __device__ __forceinline__ int column(int i) const   // first of its four
+    {
+        return 4 * (granule(i) ^ (my_row() & 7));
+    }
+    __device__ __forceinline__ void total(int chunk, int i, float (&v)[4]) const
     {
         const int rows = 32 / (int)ranks;
-        if (lane >= rows)
-            return;
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-            v[j] = 0.0f;
-        const int key = ((int)rank * rows + lane) & 7;   // of the sending lane
-        for (int r = 0; r < (int)ranks; ++r) {
-            const uint32_t from = buf + (uint32_t)(chunk * kSendBytes + (r * rows + lane) * 128);
-#pragma unroll
-            for (int g = 0; g < 8; ++g) {
-                float4 f;
-                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
-                             : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w)
-                             : "r"(from + (uint32_t)((g ^ key) << 4))
-                             : "memory");
-                v[4 * g] += f.x;
-                v[4 * g + 1] += f.y;
-                v[4 * g + 2] += f.z;
-                v[4 * g + 3] += f.w;
-            }
+        uint32_t from = buf + (uint32_t)(chunk * kSendBytes + lane / (int)ranks * 128 + granule(i) * 16);
+        v[0] = v[1] = v[2] = v[3] = 0.0f;
+        for (int r = 0; r < (int)ranks; ++r, from += (uint32_t)rows * 128) {
+            float4 f;
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                         : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w)
+                         : "r"(from)
+                         : "memory");
+            v[0] += f.x;
+            v[1] += f.y;
+            v[2] += f.z;
+            v[3] += f.w;
         }
+    }
+    // Over the lanes of a row.
+    __device__ __forceinline__ float row_max(float v) const
+    {
+        for (int o = 1; o < (int)ranks; o <<= 1)
+            v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+        return v;
     }
     // The buffer has been read: tell every rank.
     __device__ __forceinline__ void end()
@@ -680,55 +728,80 @@ struct Exchange {
     }
 };
 
-// The first n of 32 values of a row, n a multiple of 8, rows 16-byte aligned.
-__device__ __forceinline__ void store_row(__nv_bfloat16 *p, const uint32_t (&w)[16], int n)
+__device__ __forceinline__ void store4(__nv_bfloat16 *p, const float (&v)[4])
 {
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-        if (g * 8 < n)
-            *reinterpret_cast<uint4 *>(p + g * 8) =
-                make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
+    *reinterpret_cast<uint2 *>(p) = make_uint2(gemm::pack_bf16(v[0], v[1]), gemm::pack_bf16(v[2], v[3]));
 }
-__device__ __forceinline__ void store_row(__nv_bfloat16 *p, const float (&v)[32], int n)
+__device__ __forceinline__ void store4(uint8_t *p, const float (&v)[4], float inv)
 {
-    uint32_t w[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-        w[i] = gemm::pack_bf16(v[2 * i], v[2 * i + 1]);
-    store_row(p, w, n);
+    *reinterpret_cast<uint32_t *>(p) =
+        encode4(inf_to_nan(v[0]) * inv, inf_to_nan(v[1]) * inv, inf_to_nan(v[2]) * inv,
+                inf_to_nan(v[3]) * inv);
+}
+__device__ __forceinline__ float finite_max(const float (&v)[4])
+{
+    return fmaxf(fmaxf(finite_abs(v[0]), finite_abs(v[1])),
+                 fmaxf(finite_abs(v[2]), finite_abs(v[3])));
 }
 
-__device__ __forceinline__ void store_codes(uint8_t *p, uint8_t *scale, const float (&v)[32], int n)
-{
-    float q[32];
-#pragma unroll
-    for (int j = 0; j < 32; ++j)
-        q[j] = v[j];
-    const uint32_t s = row_scale(q, n);
-    const float inv = inv_scale_of(s);
-    *scale = (uint8_t)s;
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-        if (g * 8 < n) {
-            const float *w = q + g * 8;
-            *reinterpret_cast<uint2 *>(p + g * 8) =
-                make_uint2(encode4(w[0] * inv, w[1] * inv, w[2] * inv, w[3] * inv),
-                           encode4(w[4] * inv, w[5] * inv, w[6] * inv, w[7] * inv));
+// Four kept values, 4- (codes) or 8-byte (bf16) aligned.
+template <bool CODES> struct Kept4 {
+    uint32_t w[CODES ? 1 : 2];
+    __device__ __forceinline__ void load(const void *base, int64_t at)
+    {
+        if constexpr (CODES)
+            asm volatile("ld.global.b32 %0, [%1];"
+                         : "=r"(w[0])
+                         : "l"(static_cast<const uint8_t *>(base) + at));
+        else
+            asm volatile("ld.global.v2.b32 {%0, %1}, [%2];"
+                         : "=r"(w[0]), "=r"(w[1])
+                         : "l"(static_cast<const __nv_bfloat16 *>(base) + at));
+    }
+    __device__ __forceinline__ float2 pair(int i, float scale) const
+    {
+        return Kept<CODES>::pair(w, i, scale);
+    }
+};
+
+// What a lane needs of one chunk's kept values, all loads under way at once.
+template <bool CODES> struct KeptPieces {
+    Kept4<CODES> g[8], u[8];
+    uint32_t sg, su;
+    __device__ __forceinline__ void load(const Product &P, const Exchange &ex, int row, int col0)
+    {
+        row = min(row, P.m - 1);
+        if (CODES) {
+            const int64_t sat = row * P.ld_scale + col0 / kGroup;
+            asm volatile("ld.global.u8 %0, [%1];" : "=r"(sg) : "l"(P.scale_g + sat));
+            asm volatile("ld.global.u8 %0, [%1];" : "=r"(su) : "l"(P.scale_u + sat));
         }
-}
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < ex.pieces() && col0 + ex.column(i) < P.n) {
+                const int64_t at = row * P.ld_kept + col0 + ex.column(i);
+                g[i].load(P.kept_g, at);
+                u[i].load(P.kept_u, at);
+            }
+    }
+};
 
 // A warp's part of a tile split along K: 32 rows of kGate: 32 columns of G and of U,
-// otherwise of 64 columns, from row0 and col0 on. bf16 outputs o0, o1, o2 (as d0, d1, d2),
-// written row by row. acc_empty is arrived on as soon as the accumulator is read.
-// False when a wait gave up.
+// otherwise of up to 64 columns, from row0 and col0 on, in `chunks` chunks (0: none are in
+// the matrix, the same on every rank). bf16 outputs o0, o1, o2 (as d0, d1, d2).
+// acc_empty is arrived on as soon as the accumulator is read. False when a wait gave up.
 template <int EPI>
 __device__ __forceinline__ bool drain_split(const Product &P, Exchange &ex, uint32_t acc,
-                                            int half_cols, int row0, int col0, uint32_t acc_empty)
+                                            int half_cols, int row0, int col0, int chunks,
+                                            uint32_t acc_empty)
 {
-    const bool any = row0 < P.m && col0 < P.n;   // the same on every rank
-    const int chunks = !any ? 0 : EPI == kGate || col0 + 32 < P.n ? 2 : 1;
-    if (any && !ex.begin(chunks))
+    const int row = row0 + ex.my_row();
+    KeptPieces<EPI == kGateBack8> kept;
+    if (gate_back(EPI) && chunks > 0)
+        kept.load(P, ex, row, col0);
+    if (chunks > 0 && !ex.begin(chunks))
         return false;
+#pragma unroll 1
     for (int c = 0; c < chunks; ++c) {
         float v[32];
         load_acc(acc + (uint32_t)(c * (EPI == kGate ? half_cols : 32)), v);
@@ -738,55 +811,101 @@ __device__ __forceinline__ bool drain_split(const Product &P, Exchange &ex, uint
     __syncwarp();
     if (ex.lane == 0)
         mbar_arrive<1>(acc_empty);
-    if (!any)
+    if (chunks == 0)
         return true;
     if (!ex.landed())
         return false;
-    const int rows = 32 / (int)ex.ranks;
-    const int row = row0 + (int)ex.rank * rows + ex.lane;
-    const bool mine = ex.lane < rows && row < P.m;
+    const bool in = row < P.m;
     if constexpr (EPI == kGate) {
-        const int n = min(32, P.n - col0);
-        const int64_t at = row * P.ld_o + col0;
-        float g[32], u[32];
-        ex.total(0, g);
-        ex.total(1, u);
-        ex.end();
-        if (!mine)
-            return true;
-        if (P.keep == kKeep16) {
-            store_row(P.o1 + at, g, n);
-            store_row(P.o2 + at, u, n);
-        } else if (P.keep == kKeep8) {
-            const int64_t sat = row * P.ld_scale + col0 / kGroup;
-            store_codes(P.codes_g + row * P.ld_codes_g + col0, P.scale_g + sat, g, n);
-            store_codes(P.codes_u + row * P.ld_codes_u + col0, P.scale_u + sat, u, n);
-        }
-        if (P.act == kGelu)
-            gate<kGelu>(g, u);
-        else
-            gate<kSilu>(g, u);
-        store_row(P.o0 + at, u, n);
-    } else {
-        for (int c = 0; c < chunks; ++c) {
-            const int n = min(32, P.n - col0 - c * 32);
-            const int64_t at = row * P.ld_o + col0 + c * 32;
-            float v[32];
-            ex.total(c, v);
-            if (!mine)
-                continue;
-            if constexpr (gate_back(EPI)) {
-                Kept<EPI == kGateBack8> kept;
-                uint32_t dg[16], du[16], a[16];
-                kept.load(P, row, col0 + c * 32, true);
-                kept.back(P, v, col0 + c * 32, dg, du, a);
-                store_row(P.o0 + at, dg, n);
-                store_row(P.o1 + at, du, n);
-                store_row(P.o2 + at, a, n);
-            } else {
-                store_row(P.o0 + at, v, n);
+        float inv_g = 0.0f, inv_u = 0.0f;
+        if (P.keep == kKeep8) {
+            float ag = 0.0f, au = 0.0f;
+#pragma unroll 1
+            for (int i = 0; i < ex.pieces(); ++i) {
+                float g[4], u[4];
+                ex.total(0, i, g);
+                ex.total(1, i, u);
+                if (col0 + ex.column(i) < P.n) {
+                    ag = fmaxf(ag, finite_max(g));
+                    au = fmaxf(au, finite_max(u));
+                }
+            }
+            const uint32_t sg = scale_byte(ex.row_max(ag)), su = scale_byte(ex.row_max(au));
+            inv_g = inv_scale_of(sg);
+            inv_u = inv_scale_of(su);
+            if (in && ex.lane % (int)ex.ranks == 0) {
+                const int64_t sat = row * P.ld_scale + col0 / kGroup;
+                P.scale_g[sat] = (uint8_t)sg;
+                P.scale_u[sat] = (uint8_t)su;
             }
         }
+#pragma unroll 1
+        for (int i = 0; i < ex.pieces(); ++i) {
+            const int col = col0 + ex.column(i);
+            float g[4], u[4];
+            ex.total(0, i, g);
+            ex.total(1, i, u);
+            if (!in || col >= P.n)
+                continue;
+            const int64_t at = row * P.ld_o + col;
+            if (P.keep == kKeep16) {
+                store4(P.o1 + at, g);
+                store4(P.o2 + at, u);
+            } else if (P.keep == kKeep8) {
+                store4(P.codes_g + row * P.ld_codes_g + col, g, inv_g);
+                store4(P.codes_u + row * P.ld_codes_u + col, u, inv_u);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float dq;
+                u[j] *= g[j] * (P.act == kGelu ? logistic<kGelu>(g[j], dq) : logistic<kSilu>(g[j], dq));
+            }
+            store4(P.o0 + at, u);
+        }
+        ex.end();
+    } else if constexpr (gate_back(EPI)) {
+#pragma unroll 1
+        for (int c = 0; c < chunks; ++c, col0 += 32) {
+            if (c > 0)
+                kept.load(P, ex, row, col0);
+            const float fg = scale_of(kept.sg), fu = scale_of(kept.su);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (i >= ex.pieces())
+                    break;
+                const int col = col0 + ex.column(i);
+                float v[4];
+                ex.total(c, i, v);
+                if (!in || col >= P.n)
+                    continue;
+                uint32_t dg[2], du[2], a[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float2 g = kept.g[i].pair(j, fg), u = kept.u[i].pair(j, fu);
+                    const float2 da = make_float2(v[2 * j], v[2 * j + 1]);
+                    if (P.act == kGelu)
+                        back_pair<kGelu>(g, u, da, dg[j], du[j], a[j]);
+                    else
+                        back_pair<kSilu>(g, u, da, dg[j], du[j], a[j]);
+                }
+                const int64_t at = row * P.ld_o + col;
+                *reinterpret_cast<uint2 *>(P.o0 + at) = make_uint2(dg[0], dg[1]);
+                *reinterpret_cast<uint2 *>(P.o1 + at) = make_uint2(du[0], du[1]);
+                *reinterpret_cast<uint2 *>(P.o2 + at) = make_uint2(a[0], a[1]);
+            }
+        }
+        ex.end();
+    } else {
+#pragma unroll 1
+        for (int c = 0; c < chunks; ++c, col0 += 32)
+#pragma unroll 1
+            for (int i = 0; i < ex.pieces(); ++i) {
+                const int col = col0 + ex.column(i);
+                float v[4];
+                ex.total(c, i, v);
+                if (in && col < P.n)
+                    store4(P.o0 + row * P.ld_o + col, v);
+            }
         ex.end();
     }
     return true;
@@ -803,22 +922,25 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
 {
     static_assert(CG == 1 || !SPLIT, "pairs do not split K");
     using R = Ring<SPLIT>;
-    constexpr int T = kTile(CG), BK = R::BK, kBBytes = R::b_bytes;
-    const int a_rows = SPLIT ? L.a_rows : BM;
-    const int n_stages = R::stages(a_rows), a_bytes = R::a_bytes(a_rows);
+    constexpr int T = kTile(CG), BK = R::BK;
+    const int a_rows = CG == 1 ? L.a_rows : BM, cols = SPLIT ? L.cols : T;
+    // of a stage; where K is not split its layout is that of whole boxes
+    const int a_bytes = R::bytes(SPLIT ? a_rows : BM), b_bytes = R::bytes(SPLIT ? cols : BH);
+    const int n_stages = SPLIT ? R::stages(a_rows, cols) : R::stages(BM, BH);
     extern __shared__ uint8_t smem_raw[];
-    constexpr int kStages = SPLIT ? kMaxStages : R::stages(BM);   // barriers laid out for
+    constexpr int kStages = SPLIT ? kMaxStages : R::stages(BM, BH);   // barriers laid out for
     __shared__ uint64_t bars[2 * kStages + 4 + (SPLIT ? 2 * kEpiWarps : 0)];
     __shared__ uint32_t tmem_slot;
     __shared__ int aborted;
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = CG == 2 ? gemm::cluster_rank() : 0u;
+    const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? (uint32_t)uniform((int)gemm::cluster_rank()) : 0u;
     const bool leader = rank == 0;
     uint32_t split = 1, share = 0;   // CTAs on a tile's K blocks, and which this is
     if (SPLIT) {
         asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(split));
-        share = gemm::cluster_rank();
+        split = (uint32_t)uniform((int)split);
+        share = (uint32_t)uniform((int)gemm::cluster_rank());
     }
     const int group = SPLIT ? (int)split : CG;
     const int pair = blockIdx.x / group, n_pairs = gridDim.x / group;
@@ -855,7 +977,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
     if (SPLIT)
         __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = (uint32_t)uniform((int)tmem_slot);
     const int n_tiles = L.n_tiles;
     if (warp == 0 && lane < L.n_products) {   // the maps are parameters: read before the wait
         for (int i = 0; i < 2; ++i) {
@@ -873,28 +995,34 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
     if (L.early)
         launch_dependents();
 
+    // Loading and MMA warps run as a whole, with one lane for the copies, the MMAs and the
+    // error bits: in a branch of one lane the compiler takes no operand for uniform and moves
+    // each to where the instruction wants it (7B step 4.13 -> 3.93 ms, 1B 0.83 -> 0.79; a
+    // 64-K stage of single CTAs took 570 clocks of issue for MMAs of 256).
     if (warp == 0) {
-        if (lane == 0) {
-            int it = 0, s = 0;   // K blocks issued by this CTA, the ring's next stage
-            uint32_t ph = 1;     // parity of the stage's release
-            const uint32_t bytes = (uint32_t)(CG * (a_bytes + kBBytes));
-            for (int t = pair; t < n_tiles && !*(volatile int *)&aborted; t += n_pairs) {
-                const Tile tile = tile_at(L, t);
-                const Product &P = L.p[tile.p];
-                const bool a_mn = P.a_mn, b_mn = P.b_mn;
-                const int ma = tile.m * T + (int)rank * BM;
-                // B rows of this CTA: T / CG of the tile's columns; kGate: a pair's CTAs
-                // hold one projection each, a single CTA half a box of either
-                const int nb = EPI == kGate ? tile.n * (T / 2) : tile.n * T + (int)rank * BH;
-                const int kb0 = P.k_blocks[0], kb_all = kb0 + P.k_blocks[1];
-                const int kb_n = SPLIT ? share_end(kb_all, share, split) : kb_all;
-                for (int kb = SPLIT ? share_end(kb_all, share - 1, split) : 0; kb < kb_n;
-                     ++kb, ++it) {
-                    if (!mbar_wait(empty(s), ph) || *(volatile int *)&aborted) {
+        const bool one = elect();
+        int it = 0, s = 0;   // K blocks issued by this CTA, the ring's next stage
+        uint32_t ph = 1;     // parity of the stage's release
+        const uint32_t bytes = (uint32_t)(CG * (R::bytes(a_rows) + b_bytes));
+        bool ok = true;
+        for (int t = pair; ok && t < n_tiles; t += n_pairs) {
+            const Tile tile = tile_at(L, t);
+            const Product &P = L.p[tile.p];
+            const bool a_mn = P.a_mn, b_mn = P.b_mn;
+            const int ma = tile.m * T + (int)rank * BM;
+            // B rows of this CTA: T / CG of the tile's columns; kGate: a pair's CTAs
+            // hold one projection each, a single CTA half a box of either
+            const int nb = EPI == kGate ? tile.n * (cols / 2) : tile.n * cols + (int)rank * BH;
+            const int kb0 = P.k_blocks[0], kb_all = kb0 + P.k_blocks[1];
+            const int kb_n = SPLIT ? share_end(kb_all, share, split) : kb_all;
+            for (int kb = SPLIT ? share_end(kb_all, share - 1, split) : 0; kb < kb_n; ++kb, ++it) {
+                ok = warp_wait(empty(s), ph, &aborted);
+                if (!ok) {
+                    if (one)
                         atomicOr(L.err, kErrWaitEmpty);
-                        aborted = 1;
-                        break;
-                    }
+                    break;
+                }
+                if (one) {
                     const uint32_t fbar = CG == 2 ? map_to_rank(full(s), 0) : full(s);
                     if (leader)
                         mbar_arrive_expect_tx(full(s), bytes);
@@ -905,87 +1033,94 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                     for (int h = 0; h < BK / kBoxK; ++h) {
                         const int k0 = k + h * kBoxK;
                         const uint32_t ah = sa + (uint32_t)(s * a_bytes + h * R::box);
-                        const uint32_t bh = sb + (uint32_t)(s * kBBytes + h * R::box);
+                        const uint32_t bh = sb + (uint32_t)(s * b_bytes + h * R::box);
                         if (!SPLIT && a_mn) {
                             tma_load<CG>(ah, ta, ma, k0, fbar);
                             tma_load<CG>(ah + R::box / 2, ta, ma + 64, k0, fbar);
                         } else {
                             tma_load<CG>(ah, ta, k0, ma, fbar);
                         }
-                        if (EPI == kGate && CG == 1) {   // 64 rows of each projection
+                        if (EPI == kGate && CG == 1) {   // half of the rows of each projection
                             tma_load<CG>(bh, &P.b[0], k0, nb, fbar);
-                            tma_load<CG>(bh + R::box / 2, &P.b[1], k0, nb, fbar);
+                            tma_load<CG>(bh + (uint32_t)(cols / 2 * kRowBytes), &P.b[1], k0, nb, fbar);
                         } else if (b_mn) {
                             tma_load<CG>(bh, tb, nb, k0, fbar);
-                            tma_load<CG>(bh + R::box / 2, tb, nb + 64, k0, fbar);
+                            if (cols > 64)
+                                tma_load<CG>(bh + R::box / 2, tb, nb + 64, k0, fbar);
                         } else {
                             tma_load<CG>(bh, tb, k0, nb, fbar);
                         }
                     }
-                    if (++s == n_stages) {
-                        s = 0;
-                        ph ^= 1u;
-                    }
+                }
+                __syncwarp();
+                if (++s == n_stages) {
+                    s = 0;
+                    ph ^= 1u;
                 }
             }
-            if (leader)   // no CTA leaves before the loads in flight have landed
-                for (int q = it - n_stages < 0 ? 0 : it - n_stages; q < it; ++q)
-                    if (!mbar_wait(full(q % n_stages), (uint32_t)(q / n_stages) & 1u))
-                        atomicOr(L.err, kErrDrain);
         }
+        if (leader && one)   // no CTA leaves before the loads in flight have landed
+            for (int q = it - n_stages < 0 ? 0 : it - n_stages; q < it; ++q)
+                if (!mbar_wait(full(q % n_stages), (uint32_t)(q / n_stages) & 1u))
+                    atomicOr(L.err, kErrDrain);
+        __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0 && leader) {
+        if (leader) {
+            const bool one = elect();
             int lt = 0, s = 0;
             uint32_t ph = 0;
-            for (int t = pair; t < n_tiles && !*(volatile int *)&aborted; t += n_pairs, ++lt) {
+            bool ok = true;
+            for (int t = pair; ok && t < n_tiles; t += n_pairs, ++lt) {
                 const Product &P = L.p[tile_at(L, t).p];
                 const int kb_all = P.k_blocks[0] + P.k_blocks[1];
                 const int kb_n = SPLIT ? share_end(kb_all, share, split) -
                                              share_end(kb_all, share - 1, split)
                                        : kb_all;
                 const bool a_mn = P.a_mn, b_mn = P.b_mn;
-                const uint32_t idesc = idesc_of(CG, a_mn, b_mn);
+                const uint32_t idesc = idesc_of(CG, cols, a_mn, b_mn);
                 const int a = lt & 1;
                 const uint32_t aph = (uint32_t)(lt >> 1) & 1u;
-                if (!mbar_wait(acc_empty(a), aph ^ 1u)) {
-                    atomicOr(L.err, kErrWaitDone);
-                    aborted = 1;
+                ok = warp_wait(acc_empty(a), aph ^ 1u, &aborted);
+                if (!ok) {
+                    if (one)
+                        atomicOr(L.err, kErrWaitDone);
                     break;
                 }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t d = tmem + (uint32_t)(a * T);
-                bool ok = true;
                 for (int kb = 0; kb < kb_n; ++kb) {
-                    if (!mbar_wait(full(s), ph) || *(volatile int *)&aborted) {
-                        atomicOr(L.err, kErrWaitFull);
-                        aborted = 1;
-                        ok = false;
+                    ok = warp_wait(full(s), ph, &aborted);
+                    if (!ok) {
+                        if (one)
+                            atomicOr(L.err, kErrWaitFull);
                         break;
                     }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    if (one) {
 #pragma unroll
-                    for (int k = 0; k < BK / 16; ++k) {
-                        const int h = k / (kBoxK / 16), kk = k % (kBoxK / 16);
-                        const uint32_t ah = sa + (uint32_t)(s * a_bytes + h * R::box);
-                        const uint32_t bh = sb + (uint32_t)(s * kBBytes + h * R::box);
-                        const uint64_t ad = a_mn ? smem_desc_mn(ah + (uint32_t)(kk * 16 * 128))
-                                                 : smem_desc(ah + (uint32_t)(kk * 32));
-                        const uint64_t bd = b_mn ? smem_desc_mn(bh + (uint32_t)(kk * 16 * 128))
-                                                 : smem_desc(bh + (uint32_t)(kk * 32));
-                        mma_bf16<CG>(d, ad, bd, idesc, (kb | k) != 0 ? 1u : 0u);
+                        for (int k = 0; k < BK / 16; ++k) {
+                            const int h = k / (kBoxK / 16), kk = k % (kBoxK / 16);
+                            const uint32_t ah = sa + (uint32_t)(s * a_bytes + h * R::box);
+                            const uint32_t bh = sb + (uint32_t)(s * b_bytes + h * R::box);
+                            const uint64_t ad = a_mn ? smem_desc_mn(ah + (uint32_t)(kk * 16 * 128))
+                                                     : smem_desc(ah + (uint32_t)(kk * 32));
+                            const uint64_t bd = b_mn ? smem_desc_mn(bh + (uint32_t)(kk * 16 * 128))
+                                                     : smem_desc(bh + (uint32_t)(kk * 32));
+                            mma_bf16<CG>(d, ad, bd, idesc, (kb | k) != 0 ? 1u : 0u);
+                        }
+                        mma_commit<CG>(empty(s));
                     }
-                    mma_commit<CG>(empty(s));
+                    __syncwarp();
                     if (++s == n_stages) {
                         s = 0;
                         ph ^= 1u;
                     }
                 }
-                mma_commit<CG>(acc_full(a));
-                if (!ok) {
-                    if (!mbar_wait(acc_full(a), aph))
-                        atomicOr(L.err, kErrDrain);
-                    break;
-                }
+                if (one)
+                    mma_commit<CG>(acc_full(a));
+                __syncwarp();
+                if (!ok && !mbar_wait(acc_full(a), aph) && one)
+                    atomicOr(L.err, kErrDrain);
             }
         }
     } else {
@@ -994,10 +1129,13 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
         const int q = warp & 3, half = (warp - 2) >> 2;
         // staging of the warps that have rows
         const int slot = SPLIT ? half * (a_rows / 32) + q : warp - 2;
-        Stager st = {ring + (uint32_t)(n_stages * (a_bytes + kBBytes) + slot * R::staging), lane, 0};
+        Stager st = {ring + (uint32_t)(n_stages * (a_bytes + b_bytes) + slot * R::staging), lane, 0};
         const uint32_t xbar = bar0 + 8u * (uint32_t)(2 * kStages + 4 + (warp - 2) * 2);
         Exchange ex = {st.buf, xbar, xbar + 8u, share, split, lane, 0, L.err};
-        constexpr int kCols = EPI == kGate ? T / 2 : T;   // output columns of a tile
+        // Output columns of a tile, and where its second half of the warps begins; 32 columns
+        // of kGate (a scale's group) are the first half's alone.
+        const int out_cols = EPI == kGate ? cols / 2 : cols;
+        const int half0 = half * (SPLIT && EPI == kGate ? 32 : out_cols / 2);
         int lt = 0;
         for (int t = pair; t < n_tiles; t += n_pairs, ++lt) {
             const Tile tile = tile_at(L, t);
@@ -1013,15 +1151,19 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
             if (!seen)
                 break;
             const uint32_t acc =
-                tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * T + half * (kCols / 2));
+                tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * T + half0);
 #pragma unroll 1
-            for (int ch = 0; ch < (SPLIT ? 1 : kCols / 64); ++ch) {
+            for (int ch = 0; ch < (SPLIT ? 1 : out_cols / 64); ++ch) {
                 const uint32_t at = acc + (uint32_t)(ch * 32);
-                const int col0 = tile.n * kCols + half * (kCols / 2) + ch * 32;
-                if constexpr (SPLIT)
-                    seen = drain_split<EPI>(P, ex, at, kCols, row0, col0, acc_empty(a));
-                else
-                    drain<EPI>(P, st, kept, at, kCols, row0, col0, ch == 0);
+                const int col0 = tile.n * out_cols + half0 + ch * 32;
+                if constexpr (SPLIT) {
+                    const bool any = row0 < P.m && col0 < P.n && half0 < out_cols;
+                    const bool two = EPI == kGate || (cols > 64 && col0 + 32 < P.n);
+                    seen = drain_split<EPI>(P, ex, at, out_cols, row0, col0, any ? 1 + two : 0,
+                                            acc_empty(a));
+                } else {
+                    drain<EPI>(P, st, kept, at, out_cols, row0, col0, ch == 0);
+                }
             }
             if (SPLIT) {
                 if (seen)
