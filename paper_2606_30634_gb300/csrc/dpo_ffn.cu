@@ -621,7 +621,7 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
         Maps m;
         Product &P = L.p[0];
         m.operand(&P.a[0], a.dout, T, D, a.ld_dout, form.a_rows);
-        m.operand(&P.b[0], a.w_down, D, F, F, kBoxK);
+        m.operand(&P.b[0], a.w_down, D, F, F, form.bk());
         P.b_mn = 1;
         m.bf16(&P.d0, dg, T, F, F);
         m.bf16(&P.d1, du, T, F, F);
@@ -668,8 +668,8 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
         s[n++] = {T, D, F, 2};
         m.operand(&P.a[0], dg, T, F, F, BM);
         m.operand(&P.a[1], du, T, F, F, BM);
-        m.operand(&P.b[0], a.w_gate, F, D, D, kBoxK);
-        m.operand(&P.b[1], a.w_up, F, D, D, kBoxK);
+        m.operand(&P.b[0], a.w_gate, F, D, D, kPairs.bk());
+        m.operand(&P.b[1], a.w_up, F, D, D, kPairs.bk());
         P.b_mn = 1;
         m.bf16(&P.d0, a.dx, T, D, a.ld_dx);
     }
@@ -684,8 +684,8 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
     for (const auto &w : dw) {
         Product &P = L.p[n];
         s[n++] = {w.rows, w.cols, T, 1};
-        m.operand(&P.a[0], w.left, T, w.rows, w.ld_left, kBoxK);
-        m.operand(&P.b[0], w.right, T, w.cols, w.ld_right, kBoxK);
+        m.operand(&P.a[0], w.left, T, w.rows, w.ld_left, kPairs.bk());
+        m.operand(&P.b[0], w.right, T, w.cols, w.ld_right, kPairs.bk());
         P.a_mn = P.b_mn = 1;
         if (a.grad_dtype == DPO_F32)
             m.f32(&P.d0, w.dw, w.rows, w.cols, w.cols);

@@ -54,7 +54,6 @@ using gemm::mbar_wait;
 using gemm::mma_bf16;
 using gemm::mma_commit;
 using gemm::smem_desc;
-using gemm::smem_desc_mn;
 using gemm::swz64;
 using gemm::tmem_ld32;
 
@@ -77,6 +76,7 @@ constexpr int kMaxSmem = 232448 - 1024;   // of a CTA, beside its static variabl
 template <bool SPLIT> struct Ring {
     static constexpr int BK = SPLIT ? 64 : 128;
     static constexpr int box = BM * kRowBytes;                // of one box of 128 rows
+    static constexpr int mn_box = BK * kRowBytes;             // of a box of 64 columns, BK of K
     static constexpr int staging = SPLIT ? 8192 : 2 * kChunkBytes;   // per epilogue warp
     // of a stage: `rows` of A, `cols` of B
     static __host__ __device__ constexpr int bytes(int n) { return n * BK * 2; }
@@ -205,6 +205,31 @@ __device__ __forceinline__ uint32_t idesc_of(int cg, int n, int a_mn, int b_mn)
 {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) |
            ((uint32_t)(kTile(cg) >> 4) << 24) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16);
+}
+
+// The descriptors of an operand stage's steps of 16 of K: 32 bytes apart in a K-major box
+// of 64, 16 rows apart where the operand is M- or N-contiguous. The address is the low
+// word's, in 16 bytes, so a step is one addition.
+struct Steps {
+    uint32_t lo, hi, step, four;
+    __device__ __forceinline__ Steps stage(int bytes) const
+    {
+        return {lo + ((uint32_t)bytes >> 4), hi, step, four};
+    }
+    __device__ __forceinline__ uint64_t at(int k) const
+    {
+        return (uint64_t)hi << 32 | (lo + (uint32_t)(k % 4) * step + (uint32_t)(k / 4) * four);
+    }
+};
+template <int BK> __device__ __forceinline__ Steps steps_of(uint32_t addr, bool mn)
+{
+    // M- or N-contiguous: smem_desc_mn of dpo_gemm.cuh but for the distance between boxes of
+    // 64 columns (there 8 KiB, here BK rows): bits 16 to 29, in 16 bytes
+    const uint64_t d = mn ? gemm::smem_desc_mn(addr) ^
+                                ((uint64_t)((8192 >> 4) ^ (BK * kRowBytes >> 4)) << 16)
+                          : smem_desc(addr);
+    const uint32_t step = mn ? 16 * kRowBytes : 32, four = mn ? 64 * kRowBytes : BM * kRowBytes;
+    return {(uint32_t)d, (uint32_t)(d >> 32), step >> 4, four >> 4};
 }
 
 // K blocks of shares 0 .. share of `split` (share -1: none); with split <= all, none is
@@ -1029,26 +1054,28 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                     const int seg = kb >= kb0, k = (kb - (seg ? kb0 : 0)) * BK;
                     const CUtensorMap *ta = &P.a[seg];
                     const CUtensorMap *tb = EPI == kGate ? &P.b[CG == 2 ? rank : 0] : &P.b[seg];
+                    const uint32_t as = sa + (uint32_t)(s * a_bytes);
+                    const uint32_t bs = sb + (uint32_t)(s * b_bytes);
+                    if (!SPLIT && a_mn) {
+                        tma_load<CG>(as, ta, ma, k, fbar);
+                        tma_load<CG>(as + R::mn_box, ta, ma + 64, k, fbar);
+                    } else {
 #pragma unroll
-                    for (int h = 0; h < BK / kBoxK; ++h) {
-                        const int k0 = k + h * kBoxK;
-                        const uint32_t ah = sa + (uint32_t)(s * a_bytes + h * R::box);
-                        const uint32_t bh = sb + (uint32_t)(s * b_bytes + h * R::box);
-                        if (!SPLIT && a_mn) {
-                            tma_load<CG>(ah, ta, ma, k0, fbar);
-                            tma_load<CG>(ah + R::box / 2, ta, ma + 64, k0, fbar);
-                        } else {
-                            tma_load<CG>(ah, ta, k0, ma, fbar);
-                        }
-                        if (EPI == kGate && CG == 1) {   // half of the rows of each projection
-                            tma_load<CG>(bh, &P.b[0], k0, nb, fbar);
-                            tma_load<CG>(bh + (uint32_t)(cols / 2 * kRowBytes), &P.b[1], k0, nb, fbar);
-                        } else if (b_mn) {
-                            tma_load<CG>(bh, tb, nb, k0, fbar);
-                            if (cols > 64)
-                                tma_load<CG>(bh + R::box / 2, tb, nb + 64, k0, fbar);
-                        } else {
-                            tma_load<CG>(bh, tb, k0, nb, fbar);
+                        for (int h = 0; h < BK / kBoxK; ++h)
+                            tma_load<CG>(as + (uint32_t)(h * R::box), ta, k + h * kBoxK, ma, fbar);
+                    }
+                    if (EPI != kGate && b_mn) {
+                        tma_load<CG>(bs, tb, nb, k, fbar);
+                        if (cols > 64)
+                            tma_load<CG>(bs + R::mn_box, tb, nb + 64, k, fbar);
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < BK / kBoxK; ++h) {
+                            const uint32_t bh = bs + (uint32_t)(h * R::box);
+                            tma_load<CG>(bh, tb, k + h * kBoxK, nb, fbar);
+                            if (EPI == kGate && CG == 1)   // half of the rows of each projection
+                                tma_load<CG>(bh + (uint32_t)(cols / 2 * kRowBytes), &P.b[1],
+                                             k + h * kBoxK, nb, fbar);
                         }
                     }
                 }
@@ -1078,6 +1105,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                                        : kb_all;
                 const bool a_mn = P.a_mn, b_mn = P.b_mn;
                 const uint32_t idesc = idesc_of(CG, cols, a_mn, b_mn);
+                const Steps a0 = steps_of<BK>(sa, a_mn), b0 = steps_of<BK>(sb, b_mn);
                 const int a = lt & 1;
                 const uint32_t aph = (uint32_t)(lt >> 1) & 1u;
                 ok = warp_wait(acc_empty(a), aph ^ 1u, &aborted);
@@ -1097,17 +1125,10 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                     }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     if (one) {
+                        const Steps da = a0.stage(s * a_bytes), db = b0.stage(s * b_bytes);
 #pragma unroll
-                        for (int k = 0; k < BK / 16; ++k) {
-                            const int h = k / (kBoxK / 16), kk = k % (kBoxK / 16);
-                            const uint32_t ah = sa + (uint32_t)(s * a_bytes + h * R::box);
-                            const uint32_t bh = sb + (uint32_t)(s * b_bytes + h * R::box);
-                            const uint64_t ad = a_mn ? smem_desc_mn(ah + (uint32_t)(kk * 16 * 128))
-                                                     : smem_desc(ah + (uint32_t)(kk * 32));
-                            const uint64_t bd = b_mn ? smem_desc_mn(bh + (uint32_t)(kk * 16 * 128))
-                                                     : smem_desc(bh + (uint32_t)(kk * 32));
-                            mma_bf16<CG>(d, ad, bd, idesc, (kb | k) != 0 ? 1u : 0u);
-                        }
+                        for (int k = 0; k < BK / 16; ++k)
+                            mma_bf16<CG>(d, da.at(k), db.at(k), idesc, (kb | k) != 0 ? 1u : 0u);
                         mma_commit<CG>(empty(s));
                     }
                     __syncwarp();
