@@ -242,50 +242,48 @@ int64_t n_tiles(const Shape &s, const Form &f, int epi)
 int64_t tiles_of(const Shape &s, const Form &f, int epi) { return m_tiles(s, f) * n_tiles(s, f, epi); }
 
 // The form of a launch: the one with the smallest estimate of its time in ns, tiles dealt
-// round-robin. A K block costs what its stage of the ring waits for, about 2 us over the
-// stages, or on a pair the tensor core's 700 ns; all of them, the weights' way from HBM at
-// least. The exchange of a split tile's sums adds 2.5 us to each round, since the next
-// tile's MMAs hide only part of it. K is split only where a launch is one product, and more
-// than four rounds of single CTAs go to the pairs unweighed. Forward of GB300's measured
-// alternatives (all forms forced in turn, 17 to 1536 tokens, four pairs of widths): within
-// 3 us of the best form of either product but for a 7B gate at 17 and 128 tokens (4 and 1).
-Form form_of(const Device &d, const Shape *s, int n, int epi)
+// in rounds. A K block costs a single CTA the stage's bytes at 140 a ns, or 350 for 128 of K,
+// and a pair 640; the exchange of a split tile's sums adds 1.15 us to each round and 2.6 us
+// at the end. (The weights' way from HBM is the same for all forms.) K is split only where a
+// launch is one product. The numbers are fitted to GB300's measured alternatives, all forms
+// forced in turn, 9 to 1001 tokens, four pairs of widths: within 2 us of the best one but for
+// 128 tokens of 520 x 1560 widths, gate backward (3).
+struct Choice {
+    Form form;
+    double time;
+};
+Choice form_of(const Device &d, const Shape *s, int n, int epi)
 {
     const int a_rows = s[0].m <= 32 ? 32 : s[0].m <= 64 ? 64 : BM;
     const Form forms[] = {single(n == 1 ? a_rows : BM), thin(1, a_rows, BH), thin(2, a_rows, BH),
                           thin(4, a_rows, BH), thin(8, a_rows, BH), thin(1, a_rows, BH / 2),
                           thin(2, a_rows, BH / 2), thin(4, a_rows, BH / 2),
                           thin(8, a_rows, BH / 2), kPairs};
-    Form best = kPairs;
-    double least = 1e30;
+    Choice best = {kPairs, 1e30};
     for (const Form &f : forms) {
-        const double block = f.cg == 2 ? 700.0 : 2000.0 / (f.thin ? Ring<true>::stages(f.a_rows, f.cols) : 3);
-        const double epilogue = f.cg == 2 ? 3000.0 : f.thin ? 3000.0 : 1500.0;
+        const double bytes = (double)(f.a_rows + f.cols) * f.bk() * 2;
+        const double block = f.cg == 2 ? 640.0
+                             : f.thin  ? bytes / 140.0 : bytes > 49000.0 ? bytes / 140.0 : 350.0;
+        const double epilogue = f.cg == 2 ? 1850.0 : f.thin ? 3600.0 : 1000.0;
         const int64_t slots = slots_of(d, f, epi);
         int64_t tiles = 0;
-        double work = 0.0, longest = 0.0, weights = 0.0;
+        double work = 0.0, longest = 0.0;
         for (int i = 0; i < n; ++i)
             tiles += tiles_of(s[i], f, epi);
-        if (f.cg == 1 && !f.thin && tiles > 4 * slots)
-            return kPairs;
         if (f.thin && (n > 1 || blocks_of(s[0].k, f.bk()) < 2 * f.ways))
             continue;
         for (int i = 0; i < n; ++i) {
             const int64_t blocks = blocks_of(s[i].k, f.bk()) * s[i].segments;
             const double c = (double)((blocks + f.ways - 1) / f.ways) * block;
-            const double each = f.thin ? c + 2500.0 : c > epilogue ? c : epilogue;
+            const double each = f.thin ? c + 1150.0 : c > epilogue ? c : epilogue;
             work += (double)tiles_of(s[i], f, epi) * each;
             longest = longest > each ? longest : each;
-            weights += (double)(s[i].n * s[i].k * s[i].segments) * (epi == kGate ? 4.0 : 2.0) / 6500.0;
         }
         // whole rounds of equal tiles, or the longest one's end
         double time = n == 1 ? (double)((tiles + slots - 1) / slots) * longest : work / (double)slots;
-        time = time > longest ? time : longest;
-        time = (time > weights ? time : weights) + epilogue + 0.1 * time;   // ties: the shorter
-        if (time < least) {
-            least = time;
-            best = f;
-        }
+        time = (time > longest ? time : longest) * 1.02 + epilogue;
+        if (time < best.time)
+            best = {f, time};
     }
     return best;
 }
@@ -493,7 +491,7 @@ extern "C" int dpo_ffn_forward(const dpo_ffn_args *args, void *cuda_stream)
     }
     {
         const Shape s = {T, F, D, 1};
-        const Form form = form_of(*d, &s, 1, kGate);
+        const Form form = form_of(*d, &s, 1, kGate).form;
         const int rows_w = form.cg == 2 ? BH : form.cols / 2;   // a box of either projection
         Launch L{};
         Maps m;
@@ -530,7 +528,7 @@ extern "C" int dpo_ffn_forward(const dpo_ffn_args *args, void *cuda_stream)
     const Shape s = {T, D, F, 1};
     Launch L{};
     Maps m;
-    const Form form = form_of(*d, &s, 1, kStore);
+    const Form form = form_of(*d, &s, 1, kStore).form;
     m.operand(&L.p[0].a[0], a.workspace, T, F, F, form.a_rows);
     m.operand(&L.p[0].b[0], a.w_down, D, F, F, form.cg == 2 ? BH : form.cols);
     m.bf16(&L.p[0].d0, a.out, T, D, a.ld_out);
@@ -616,7 +614,7 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
     {
         const Shape s = {T, F, D, 1};
         const int epi = a.keep == DPO_KEEP_8BIT ? kGateBack8 : kGateBack16;
-        const Form form = form_of(*d, &s, 1, epi);
+        const Form form = form_of(*d, &s, 1, epi).form;
         Launch L{};
         Maps m;
         Product &P = L.p[0];
@@ -660,18 +658,32 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
             return rc;
     }
     Launch L{};
-    Shape s[kMaxProducts];
+    const Shape s[kMaxProducts] = {{T, D, F, 2}, {F, D, T, 1}, {F, D, T, 1}, {D, F, T, 1}};
     Maps m;
-    int n = 0;
+    int n = 0, first = 1;   // products of L, of s
     if (a.dx != nullptr) {
-        Product &P = L.p[n];
-        s[n++] = {T, D, F, 2};
-        m.operand(&P.a[0], dg, T, F, F, BM);
-        m.operand(&P.a[1], du, T, F, F, BM);
-        m.operand(&P.b[0], a.w_gate, F, D, D, kPairs.bk());
-        m.operand(&P.b[1], a.w_up, F, D, D, kPairs.bk());
+        // dx with the weights' gradients in one list, or, where its few long tiles would be
+        // what the list waits for, before them with K split (1B widths, 9 tokens: its tiles
+        // have 128 blocks, the gradients' one)
+        const Choice all = form_of(*d, s, 4, kStore), dx = form_of(*d, s, 1, kStore);
+        const bool alone = dx.form.thin &&
+                           dx.time + form_of(*d, s + 1, 3, kStore).time + 2000.0 < all.time;
+        const Form f = alone ? dx.form : kPairs;
+        Product &P = L.p[0];
+        m.operand(&P.a[0], dg, T, F, F, f.a_rows);
+        m.operand(&P.a[1], du, T, F, F, f.a_rows);
+        m.operand(&P.b[0], a.w_gate, F, D, D, f.bk());
+        m.operand(&P.b[1], a.w_up, F, D, D, f.bk());
         P.b_mn = 1;
         m.bf16(&P.d0, a.dx, T, D, a.ld_dx);
+        P.o0 = static_cast<__nv_bfloat16 *>(a.dx);
+        P.ld_o = a.ld_dx;
+        if (!alone) {
+            n = 1;
+            first = 0;
+        } else if ((rc = run(what, *d, L, s, 1, kStore, f, true, m.ok, cuda_stream)) != DPO_OK) {
+            return rc;
+        }
     }
     struct {
         const void *left, *right;
@@ -682,8 +694,8 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
                      {du, x, F, ld_x, F, D, a.dw_up, true},
                      {a.dout, act, a.ld_dout, F, D, F, a.dw_down, false}};
     for (const auto &w : dw) {
-        Product &P = L.p[n];
-        s[n++] = {w.rows, w.cols, T, 1};
+        Product &P = L.p[n++];
+        P = Product{};
         m.operand(&P.a[0], w.left, T, w.rows, w.ld_left, kPairs.bk());
         m.operand(&P.b[0], w.right, T, w.cols, w.ld_right, kPairs.bk());
         P.a_mn = P.b_mn = 1;
@@ -700,7 +712,8 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
             P.gain_f32 = a.gain_dtype == DPO_F32;
         }
     }
-    return run(what, *d, L, s, n, kStore, form_of(*d, s, n, kStore), false, m.ok, cuda_stream);
+    return run(what, *d, L, s + first, n, kStore, form_of(*d, s + first, n, kStore).form, false, m.ok,
+               cuda_stream);
 }
 
 extern "C" int dpo_ffn_get_status(uint32_t *bits)

@@ -256,6 +256,14 @@ __device__ __forceinline__ Tile tile_at(const Launch &L, int t)
     return {p, b * kBandRows + r - n * rows, n};
 }
 
+// Tile of round r: back and forth, so that whoever has one of a list's first tiles, the
+// longest, is the last one to get another (1001 tokens of 520 x 1560 widths, the gradients'
+// launch: 40 CTAs had a tile of dx, 25 K blocks, and one of 8).
+__device__ __forceinline__ int turn_of(int r, int pair, int n)
+{
+    return r * n + (r & 1 ? n - 1 - pair : pair);
+}
+
 // 2^x and 1 / x by the hardware's approximations (relative errors of about 2^-22 and 2^-23),
 // without the steps that keep subnormal results: 1 + 2^x does not see them, and its
 // reciprocal, of a number from 1 to infinity, is 0 where it would be one. The epilogues are
@@ -1030,7 +1038,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
         uint32_t ph = 1;     // parity of the stage's release
         const uint32_t bytes = (uint32_t)(CG * (R::bytes(a_rows) + b_bytes));
         bool ok = true;
-        for (int t = pair; ok && t < n_tiles; t += n_pairs) {
+        for (int t, r = 0; ok && (t = turn_of(r, pair, n_pairs)) < n_tiles; ++r) {
             const Tile tile = tile_at(L, t);
             const Product &P = L.p[tile.p];
             const bool a_mn = P.a_mn, b_mn = P.b_mn;
@@ -1097,7 +1105,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
             int lt = 0, s = 0;
             uint32_t ph = 0;
             bool ok = true;
-            for (int t = pair; ok && t < n_tiles; t += n_pairs, ++lt) {
+            for (int t; ok && (t = turn_of(lt, pair, n_pairs)) < n_tiles; ++lt) {
                 const Product &P = L.p[tile_at(L, t).p];
                 const int kb_all = P.k_blocks[0] + P.k_blocks[1];
                 const int kb_n = SPLIT ? share_end(kb_all, share, split) -
@@ -1158,7 +1166,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
         const int out_cols = EPI == kGate ? cols / 2 : cols;
         const int half0 = half * (SPLIT && EPI == kGate ? 32 : out_cols / 2);
         int lt = 0;
-        for (int t = pair; t < n_tiles; t += n_pairs, ++lt) {
+        for (int t; (t = turn_of(lt, pair, n_pairs)) < n_tiles; ++lt) {
             const Tile tile = tile_at(L, t);
             const Product &P = L.p[tile.p];
             const int a = lt & 1;
