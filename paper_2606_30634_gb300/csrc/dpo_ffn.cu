@@ -242,12 +242,13 @@ int64_t n_tiles(const Shape &s, const Form &f, int epi)
 int64_t tiles_of(const Shape &s, const Form &f, int epi) { return m_tiles(s, f) * n_tiles(s, f, epi); }
 
 // The form of a launch: the one with the smallest estimate of its time in ns, tiles dealt
-// in rounds. A K block costs a single CTA the stage's bytes at 140 a ns, or 350 for 128 of K,
-// and a pair 640; the exchange of a split tile's sums adds 1.15 us to each round and 2.6 us
-// at the end. (The weights' way from HBM is the same for all forms.) K is split only where a
-// launch is one product. The numbers are fitted to GB300's measured alternatives, all forms
-// forced in turn, 9 to 1001 tokens, four pairs of widths: within 2 us of the best one but for
-// 128 tokens of 520 x 1560 widths, gate backward (3).
+// in rounds. A K block costs a single CTA the stage's bytes at 154 a ns, or its instructions,
+// and a pair 500; the exchange of a split tile's sums adds to each round, with the CTAs that
+// take part, and 3.2 us at the end. (The weights' way from HBM is the same for all forms.) In
+// a list of products the tiles' stores may take longer than few K blocks. K is split only
+// where a launch is one product. The numbers are fitted to GB300's measured alternatives, all
+// forms forced in turn, 9 to 1001 tokens, four pairs of widths, each product of forward and
+// backward: within 2.3 us of the best one, or 2 % of the block.
 struct Choice {
     Form form;
     double time;
@@ -262,9 +263,11 @@ Choice form_of(const Device &d, const Shape *s, int n, int epi)
     Choice best = {kPairs, 1e30};
     for (const Form &f : forms) {
         const double bytes = (double)(f.a_rows + f.cols) * f.bk() * 2;
-        const double block = f.cg == 2 ? 640.0
-                             : f.thin  ? bytes / 140.0 : bytes > 49000.0 ? bytes / 140.0 : 350.0;
-        const double epilogue = f.cg == 2 ? 1850.0 : f.thin ? 3600.0 : 1000.0;
+        const double copy = bytes / 154.0, issue = f.thin ? 110.0 : 365.0;
+        const double block = f.cg == 2 ? 500.0 : copy > issue ? copy : issue;
+        const double epilogue = f.cg == 2 ? 370.0 : f.thin ? 3200.0 : 240.0;
+        const double store = n == 1 ? 0.0 : f.cg == 2 ? 1850.0 : 1000.0;
+        const double exchange = 400.0 + 73.0 * f.ways;
         const int64_t slots = slots_of(d, f, epi);
         int64_t tiles = 0;
         double work = 0.0, longest = 0.0;
@@ -275,7 +278,7 @@ Choice form_of(const Device &d, const Shape *s, int n, int epi)
         for (int i = 0; i < n; ++i) {
             const int64_t blocks = blocks_of(s[i].k, f.bk()) * s[i].segments;
             const double c = (double)((blocks + f.ways - 1) / f.ways) * block;
-            const double each = f.thin ? c + 1150.0 : c > epilogue ? c : epilogue;
+            const double each = f.thin ? c + exchange : c > store ? c : store;
             work += (double)tiles_of(s[i], f, epi) * each;
             longest = longest > each ? longest : each;
         }
