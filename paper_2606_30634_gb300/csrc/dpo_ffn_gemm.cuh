@@ -586,7 +586,6 @@ __device__ __forceinline__ void drain(const Product &P, Stager &st, Kept<EPI == 
     } else if constexpr (gate_back(EPI)) {
         float d[32];
         uint32_t dg[16], du[16], a[16];
-        kept.load(P, row, col0, first);
         load_acc(acc, d);
         kept.back(P, d, col0, dg, du, a);
         st.bf16(&P.d0, dg, col0, row0);
@@ -1171,7 +1170,15 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
             const Product &P = L.p[tile.p];
             const int a = lt & 1;
             const int row0 = tile.m * T + (int)rank * BM + q * 32;
+            const int col_0 = tile.n * out_cols + half0;
             Kept<EPI == kGateBack8> kept;
+            auto load_kept = [&](int ch) {   // a chunk ahead of its use
+                const int col0 = col_0 + ch * 32;
+                if (row0 < P.m && col0 < P.n)
+                    kept.load(P, min(row0 + lane, P.m - 1), col0, ch == 0);
+            };
+            if constexpr (gate_back(EPI) && !SPLIT)
+                load_kept(0);
             bool seen = mbar_wait(acc_full(a), (uint32_t)(lt >> 1) & 1u);
             if (!seen)
                 atomicOr(L.err, kErrWaitDone);
@@ -1184,12 +1191,17 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
 #pragma unroll 1
             for (int ch = 0; ch < (SPLIT ? 1 : out_cols / 64); ++ch) {
                 const uint32_t at = acc + (uint32_t)(ch * 32);
-                const int col0 = tile.n * out_cols + half0 + ch * 32;
+                const int col0 = col_0 + ch * 32;
                 if constexpr (SPLIT) {
                     const bool any = row0 < P.m && col0 < P.n && half0 < out_cols;
                     const bool two = EPI == kGate || (cols > 64 && col0 + 32 < P.n);
                     seen = drain_split<EPI>(P, ex, at, out_cols, row0, col0, any ? 1 + two : 0,
                                             acc_empty(a));
+                } else if constexpr (gate_back(EPI)) {
+                    Kept<EPI == kGateBack8> now = kept;
+                    if (ch + 1 < out_cols / 64)
+                        load_kept(ch + 1);
+                    drain<EPI>(P, st, now, at, out_cols, row0, col0, ch == 0);
                 } else {
                     drain<EPI>(P, st, kept, at, out_cols, row0, col0, ch == 0);
                 }
