@@ -323,7 +323,9 @@ rmsnorm_kernel(const NormForwardArgs args)
 // column. With 16-byte pieces (RING) each thread copies its own pieces of the next three
 // rows to shared memory with cp.async, in places that only it reads, so no barrier
 // guards them. GB300, 8192 x 4096 from 8-bit rows: one row ahead in registers 65 us, the
-// ring 46 with the sum of the partial rows (5.1 TB/s of the 236 MB).
+// ring 45.6 with the sum of the partial rows (5.2 TB/s of the 236 MB; this kernel alone
+// 42.7). Slower: dy and the normalised row taken from the ring once more instead of kept
+// (48.9), and with the 80 registers that this leaves three CTAs an SM (55.3).
 struct NormBackArgs {
     dpo_rmsnorm_backward_args a;
     int warps;
@@ -406,18 +408,18 @@ template <class T, int V, int E, bool X8> struct RowRegs {
 
 // The same from a slot of the ring: pieces of dy, dh, and h or the codes, each [n][thread].
 // rstd and the scales, single bytes, wait in registers.
-template <class T, int V, int E, bool X8> struct RowSlot {
+// TH threads a CTA, so that a place in the ring is a constant behind the thread's own.
+template <class T, int V, int E, bool X8, int TH> struct RowSlot {
     static constexpr int N = E / V, B = V * (int)sizeof(T), BH = X8 ? V : B;
-    static __host__ __device__ constexpr int bytes(int threads) { return N * (2 * B + BH) * threads; }
-    uint8_t *slot;             // of this thread's first piece of dy
-    int threads;
+    static constexpr int bytes = N * (2 * B + BH) * TH;
+    uint8_t *slot;
     float rstd;
     uint32_t scale[X8 ? N : 1];   // as loaded: converting it here would wait for it
 
     __device__ __forceinline__ const uint8_t *piece(int kind, int n) const
     {
         const uint8_t *base = slot + (int)threadIdx.x * (kind == 2 ? BH : B);
-        return base + threads * ((kind == 2 ? 2 * N * B + n * BH : (kind * N + n) * B));
+        return base + TH * ((kind == 2 ? 2 * N * B + n * BH : (kind * N + n) * B));
     }
     __device__ __forceinline__ void load(const dpo_rmsnorm_backward_args &a, int64_t row, int i0,
                                          int tpr)
@@ -490,8 +492,9 @@ template <class T, int V, int E, bool X8> struct RowSlot {
     }
 };
 
-template <class T, class WT, int V, int E, bool X8, bool RING>
-__global__ void __launch_bounds__(kBackThreads)
+// RING: the CTA's threads where rows come through the ring, or 0
+template <class T, class WT, int V, int E, bool X8, int RING>
+__global__ void __launch_bounds__(RING ? RING : kBackThreads)
 rmsnorm_backward_kernel(const NormBackArgs args)
 {
     constexpr int N = E / V;
@@ -566,8 +569,8 @@ rmsnorm_backward_kernel(const NormBackArgs args)
         }
     };
     int64_t base = (int64_t)blockIdx.x * rows_cta;
-    if constexpr (RING) {
-        using Slot = RowSlot<T, V, E, X8>;
+    if constexpr (RING != 0) {
+        using Slot = RowSlot<T, V, E, X8, RING>;
         Slot ring[kDepth];
         auto fetch = [&](Slot &s, int64_t b) {
             if (b < a.rows)
@@ -576,8 +579,7 @@ rmsnorm_backward_kernel(const NormBackArgs args)
         };
 #pragma unroll
         for (int d = 0; d < kDepth; ++d) {
-            ring[d].slot = smem + d * Slot::bytes((int)blockDim.x);
-            ring[d].threads = (int)blockDim.x;
+            ring[d].slot = smem + d * Slot::bytes;
             if (d < kDepth - 1)
                 fetch(ring[d], base + d * stride);
         }
@@ -946,8 +948,8 @@ FwdFn forward_of(int dtype, int wdtype, int v, int elems)
 
 template <class T, class WT, int V, int E> BackFn back_regs(bool x8)
 {
-    return x8 ? rmsnorm_backward_kernel<T, WT, V, E, true, false>
-              : rmsnorm_backward_kernel<T, WT, V, E, false, false>;
+    return x8 ? rmsnorm_backward_kernel<T, WT, V, E, true, 0>
+              : rmsnorm_backward_kernel<T, WT, V, E, false, 0>;
 }
 template <int E> BackFn back_narrow(int dtype, int wdtype, int v, bool x8)
 {
@@ -958,12 +960,20 @@ template <int E> BackFn back_narrow(int dtype, int wdtype, int v, bool x8)
     return v == 2 ? back_regs<B16, B16, 2, E>(x8) : back_regs<B16, B16, 1, E>(x8);
 }
 // ... with the ring, and its shared memory for CTAs of so many threads
+template <class T, class WT, int V, bool X8, int TH> BackFn back_ring(int *smem)
+{
+    *smem = kDepth * RowSlot<T, V, kBackElems, X8, TH>::bytes;
+    if constexpr (kDepth * RowSlot<T, V, kBackElems, X8, TH>::bytes <= kMaxSmem)
+        return rmsnorm_backward_kernel<T, WT, V, kBackElems, X8, TH>;
+    return nullptr;
+}
 template <class T, class WT, int V> BackFn back_ring(bool x8, int threads, int *smem)
 {
-    constexpr int E = kBackElems;
-    *smem = kDepth * (x8 ? RowSlot<T, V, E, true>::bytes(threads) : RowSlot<T, V, E, false>::bytes(threads));
-    return x8 ? rmsnorm_backward_kernel<T, WT, V, E, true, true>
-              : rmsnorm_backward_kernel<T, WT, V, E, false, true>;
+    static_assert(kBackThreads == 64 * kBackMinWarps, "two sizes of CTAs");
+    constexpr int TH = kBackThreads;   // or half of them
+    if (threads == TH)
+        return x8 ? back_ring<T, WT, V, true, TH>(smem) : back_ring<T, WT, V, false, TH>(smem);
+    return x8 ? back_ring<T, WT, V, true, TH / 2>(smem) : back_ring<T, WT, V, false, TH / 2>(smem);
 }
 // The ring where the pieces are the widest ones and it fits, which it does for bf16.
 BackFn back_of(int dtype, int wdtype, int v, int elems, bool x8, int threads, int *smem)
@@ -976,7 +986,7 @@ BackFn back_of(int dtype, int wdtype, int v, int elems, bool x8, int threads, in
         const BackFn fn = dtype == DPO_F32    ? back_ring<float, float, 4>(x8, threads, smem)
                           : wdtype == DPO_F32 ? back_ring<B16, float, 4>(x8, threads, smem)
                                               : back_ring<B16, B16, 8>(x8, threads, smem);
-        if (*smem <= kMaxSmem)
+        if (fn != nullptr)
             return fn;
         *smem = 0;
         return back_regs<float, float, 4, kBackElems>(x8);
