@@ -321,17 +321,31 @@ int run(const char *what, const Device &d, Launch &L, const Shape *s, int n, int
 
 // ---- few tokens ----
 
-// One product of the forward for at most kFewTokens tokens. K is split over a cluster
-// while the units alone do not fill the SMs and every warp keeps 64 of k.
-int run_few(const char *what, const FewArgs &a, int epi, int sms, void *stream)
+// One product of the forward for at most kFewTokens tokens. K is split over a cluster as far
+// as all CTAs are resident at once (one more doubling, 1 token: 7B 49.3 -> 51.4 us, 1B
+// 20.6 -> 23.3; one less: 52.7, 22.7) and every warp keeps 64 of k.
+int run_few(const char *what, FewArgs a, int epi, int sms, void *stream)
 {
     const int rows = epi == kGate ? 8 : 16;
     const int64_t units = (a.rows + rows - 1) / rows;
     int split = 1;
-    while (split < 8 && units * split < (int64_t)sms * kFewCtas && a.k > split * kFewWarps * 64)
+    while (split < 8 && units * split * 2 <= (int64_t)sms * kFewCtas && a.k > split * kFewWarps * 64)
         split *= 2;
+    const int64_t ctas = units * split, resident = (int64_t)sms * kFewCtas;
+    a.ahead.ctas = (int)(ctas < resident ? ctas : resident);
     return launch_clusters(what, epi == kGate ? few_kernel<kGate> : few_kernel<kStore>,
-                           units * split, split, kFewThreads, 0, stream, a);
+                           ctas, split, kFewThreads, 0, stream, a);
+}
+
+// What the first product reads ahead of a weight matrix: up to 24 MB, evenly over its rows
+// (1 and 8 tokens: 7B 49.4 -> 48.5 us, 53.5 -> 52.5; 1B 21.1 -> 20.5, 23.6 -> 22.5; 8 and 48 MB
+// less of it. Before the split tiles of dpo_ffn_gemm.cuh it delays the first product by as
+// much as the second one gains).
+Ahead ahead_of(const void *w, int64_t rows, int64_t cols)
+{
+    constexpr int64_t kBytes = (int64_t)24 << 20;
+    const int64_t share = kBytes / rows / 128 * 128, bytes = cols * 2 < share ? cols * 2 : share;
+    return {static_cast<const uint8_t *>(w), cols * 2, bytes > 0 ? (int)rows : 0, (int)bytes, 0};
 }
 
 int64_t align_up(int64_t v) { return (v + 255) / 256 * 256; }
@@ -479,6 +493,7 @@ extern "C" int dpo_ffn_forward(const dpo_ffn_args *args, void *cuda_stream)
         f.rows = (int)F;
         f.k = (int)D;
         f.act = a.act;
+        f.ahead = ahead_of(a.w_down, D, F);
         if ((rc = run_few(what, f, kGate, d->sms, cuda_stream)) != DPO_OK)
             return rc;
         FewArgs o{};

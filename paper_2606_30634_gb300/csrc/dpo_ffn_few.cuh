@@ -13,9 +13,8 @@
 // k inside an MMA is free as long as both operands agree, so a lane takes 16 bytes of a
 // row at once (8 consecutive k, the four lanes of a row 32 of them), which is two MMAs'
 // worth, and the tokens' fragments come the same way, from L1.
-// GB300, whole forward, this against the split tiles: 7B widths, 1 token 52.8 / 65.1 us,
-// 8 tokens 58.9 / 65.8 (floor 39.9); 1B 24.7 / 41.7 (14.8); 768 x 2048 8.2 / 16.7. Two steps
-// of eight tokens in one kernel: 16 tokens 77.5 / 65.7 (7B), 36.9 / 41.1 (1B).
+// GB300, whole forward, this against the split tiles: 7B widths, 1 token 48.5 / 59.5 us,
+// 8 tokens 52.5 / 59.6 (floor 39.9); 1B 20.5 / 27.5, 22.5 / 27.5 (14.8); 768 x 2048 8.2 / 11.0.
 #pragma once
 
 #include "dpo_ffn_gemm.cuh"
@@ -29,6 +28,16 @@ constexpr int kFewRows = 16;       // weight rows of a unit
 constexpr int kFewChunk = 4;       // blocks of 32 k a warp takes at a time
 constexpr int kFewCtas = 4;        // resident on an SM
 
+// The start of the second product's weight rows, read into L2 by the first one's last CTAs
+// once their own loads are done, so that HBM is not idle from there until the second
+// product's CTAs, most of which wait for places, have theirs under way.
+struct Ahead {
+    const uint8_t *base;
+    int64_t pitch;
+    int rows, bytes;               // of each; a multiple of 16, as are base and pitch
+    int ctas;                      // that share the rows
+};
+
 struct FewArgs {
     const __nv_bfloat16 *x;        // tokens x k
     const __nv_bfloat16 *w0, *w1;  // rows x k; kGate: w_gate, w_up
@@ -37,6 +46,7 @@ struct FewArgs {
     int64_t ld_x, ld_out;
     int tokens, rows, k;           // kGate: rows of one projection
     int act;
+    Ahead ahead;                   // kGate
 };
 
 __device__ __forceinline__ uint4 ld_weights(const __nv_bfloat16 *p)
@@ -69,7 +79,7 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr)
 // w_gate's and the others the same rows of w_up, so one lane holds G and U of one
 // element; kStore: sixteen rows of w0. One unit per CTA, or per cluster: walking several
 // from CTAs that stay, the next one's weights requested before the sums of the last,
-// takes longer (7B layer, one token: 52.7 -> 62.4 us, 80 registers instead of 64).
+// takes longer (7B layer, one token: 9.7 us, with 80 registers instead of 64).
 template <int EPI>
 __global__ void __launch_bounds__(kFewThreads) few_kernel(const FewArgs a)
 {
@@ -135,6 +145,13 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(const FewArgs a)
             mma_16816(acc, p.x, q.x, p.y, q.y, xq.x, xq.y);
             mma_16816(acc, p.z, q.z, p.w, q.w, xq.z, xq.w);
         }
+    }
+
+    if (EPI == kGate && threadIdx.x == 0) {
+        const int first = (int)gridDim.x - a.ahead.ctas;
+        for (int r = (int)blockIdx.x - first; r >= 0 && r < a.ahead.rows; r += a.ahead.ctas)
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;"
+                         ::"l"(a.ahead.base + r * a.ahead.pitch), "r"(a.ahead.bytes) : "memory");
     }
 
     float *s = sums + warp * kSums + g * kTok + t * 2;
