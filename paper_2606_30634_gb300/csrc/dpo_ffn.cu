@@ -6,7 +6,8 @@
 //                          out = A w_down^T
 // Backward, two launches:  dG, dU, A from dA = dout w_down and what was kept;
 //                          dx, dw_gate, dw_up, dw_down, one list of tiles
-// (and one more to widen the 8-bit rows when the block's input was kept so).
+// (one more where dx is better off alone, and one to widen the 8-bit rows when the block's
+// input was kept so).
 #include "dpo.h"
 #include "dpo_call.h"
 #include "dpo_ffn_few.cuh"

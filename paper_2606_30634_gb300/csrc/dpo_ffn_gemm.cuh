@@ -58,18 +58,22 @@ using gemm::swz64;
 using gemm::tmem_ld32;
 
 enum Epilogue { kGate = 0, kGateBack8 = 1, kGateBack16 = 2, kStore = 3 };
-__host__ __device__ constexpr bool gate_back(int epi) { return epi == kGateBack8 || epi == kGateBack16; }
+__host__ __device__ constexpr bool gate_back(int epi)
+{
+    return epi == kGateBack8 || epi == kGateBack16;
+}
 enum Keep { kKeepNone = 0, kKeep8 = 1, kKeep16 = 2 };
 enum Act { kSilu = 0, kGelu = 1 };
 
 constexpr int kEpiWarps = 8;
 constexpr int kThreads = 64 + 32 * kEpiWarps;
 // The ring of operand stages and the epilogue warps' staging behind it. Three stages of
-// 128 of K (six of 64 are slower, see dpo_gemm.cuh). Where K is split the time is the
-// operands' latency, about 2 us from request to MMA with the ring full, so the bytes in
-// flight count: stages of 64 of K, which leave room for more of them, and of A only the
-// 32, 64 or 128 rows that a product of so few tokens has. The MMA reads 128 rows all the
-// same; what lies behind a short box ends up in accumulator rows that nothing reads.
+// 128 of K (six of 64 are slower, see dpo_gemm.cuh). Where K is split, a CTA has few blocks
+// and waits for the first ones to arrive, so the bytes in flight count: stages of 64 of K,
+// which leave room for more of them, and of A only the 32, 64 or 128 rows that a product of
+// so few tokens has (so too single CTAs without a split: boxes of 128 rows for 17 to 24
+// tokens of a 1B layer 38 us, of 32 rows 31). The MMA reads 128 rows all the same; what lies
+// behind a short box ends up in accumulator rows that nothing reads.
 constexpr int kRowBytes = kBoxK * 2;                          // of a box: the swizzle span
 constexpr int kMaxStages = 16;
 constexpr int kMaxSmem = 232448 - 1024;   // of a CTA, beside its static variables
@@ -297,21 +301,19 @@ __device__ __forceinline__ float logistic(float z, float &dq)
     return rcp(1.0f + exp2(-1.4426950408889634f * q));
 }
 
-// Scale byte of the first n of 32 values that one lane holds; infinities become NaN (rare:
+// Scale byte of 32 values that one lane holds; infinities become NaN (rare:
 // looked for only where the maximum, which passes over NaN, found one).
-__device__ __forceinline__ uint32_t row_scale(float (&v)[32], int n)
+__device__ __forceinline__ uint32_t row_scale(float (&v)[32])
 {
     float a = 0.0f;
 #pragma unroll
     for (int j = 0; j < 32; ++j)
-        if (j < n)
-            a = fmaxf(a, fabsf(v[j]));
+        a = fmaxf(a, fabsf(v[j]));
     if (a > kMaxFinite) {
         a = 0.0f;
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
-            if (j < n)
-                a = fmaxf(a, finite_abs(v[j]));
+            a = fmaxf(a, finite_abs(v[j]));
             v[j] = inf_to_nan(v[j]);
         }
     }
@@ -385,7 +387,7 @@ struct Stager {
     // 32 rows of 32 codes; returns this row's scale byte. v is taken over.
     __device__ __forceinline__ uint32_t codes(const CUtensorMap *map, float (&v)[32], int x, int y)
     {
-        const uint32_t s = row_scale(v, 32);
+        const uint32_t s = row_scale(v);
         const float inv = inv_scale_of(s);
         const uint32_t b = begin();
 #pragma unroll
@@ -442,7 +444,8 @@ __device__ __forceinline__ void back_pair(float2 g, float2 u, float2 da, uint32_
 // 32 columns of one row of what was kept of G and U, as loaded: codes with their scale
 // bytes (CODES), or bf16, zeros past the matrix. A lane holds a row, so every load of the
 // warp touches 32 lines whatever its width, and their number is what the loads cost (1B
-// layer, the whole launch: 8-byte pieces 142 us, 16-byte ones 125, no loads at all 112):
+// layer, the whole launch, each chunk's loads just before their use: 8-byte pieces 142 us,
+// 16-byte ones 125, none at all 112; loaded a chunk ahead they are hidden):
 // Product::wide says that all rows are 32-byte aligned and whole chunks of 128 columns, so
 // a row's chunk of codes is one load (past L1: 134 -> 124 us) and four chunks' scales
 // another. Otherwise rows and pitches are 16-byte aligned and hidden is a multiple of 8:
@@ -1080,7 +1083,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                         for (int h = 0; h < BK / kBoxK; ++h) {
                             const uint32_t bh = bs + (uint32_t)(h * R::box);
                             tma_load<CG>(bh, tb, k + h * kBoxK, nb, fbar);
-                            if (EPI == kGate && CG == 1)   // half of the rows of each projection
+                            if (EPI == kGate && CG == 1)   // half the rows of each projection
                                 tma_load<CG>(bh + (uint32_t)(cols / 2 * kRowBytes), &P.b[1],
                                              k + h * kBoxK, nb, fbar);
                         }
