@@ -102,11 +102,15 @@ def _compile(src, obj, includes, verbose_ptxas, torch=False):
     return _run(cmd, f"nvcc for {src}")
 
 
-def build(force: bool = False, quiet: bool = True) -> dict:
-    """Compile every library whose sources changed; returns {name: path}."""
+def build(force: bool = False, quiet: bool = True, only=None) -> dict:
+    """Compile every library whose sources changed, or those of ``only``; returns
+    {name: path}. A library's user builds that one alone: the optimizers need no Python
+    headers, which dpo_tensors.so does."""
     os.makedirs(OUT, exist_ok=True)
+    names = list(LIBS if only is None else only)
     jobs = []
-    for lib, spec in LIBS.items():
+    for lib in names:
+        spec = LIBS[lib]
         out = os.path.join(OUT, lib)
         deps = [os.path.join(PKG, p) for p in spec["sources"] + spec["headers"]]
         if force or any(_mtime(d) > _mtime(out) for d in deps):
@@ -131,7 +135,7 @@ def build(force: bool = False, quiet: bool = True) -> dict:
                 cmd = [NVCC] + ARCH + ["-shared", "-Xcompiler", "-fopenmp", "-o", tmp] + objs
             _run(cmd, f"link of {lib}")
             os.replace(tmp, out)
-    return {lib: os.path.join(OUT, lib) for lib in LIBS}
+    return {lib: os.path.join(OUT, lib) for lib in names}
 
 
 if __name__ == "__main__":

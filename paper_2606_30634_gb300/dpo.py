@@ -124,7 +124,7 @@ def load() -> ctypes.CDLL:
     global _lib
     if _lib is not None:
         return _lib
-    path = os.environ.get("DPO_LIBRARY") or _build.build()["libdpo.so"]
+    path = os.environ.get("DPO_LIBRARY") or _build.build(only=["libdpo.so"])["libdpo.so"]
     if not os.path.exists(path):
         raise RuntimeError(f"libdpo.so is missing at {path}")
     L = ctypes.CDLL(path)

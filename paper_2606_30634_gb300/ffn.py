@@ -25,7 +25,6 @@ from __future__ import annotations
 
 import ctypes
 import importlib.util
-import os
 from typing import NamedTuple, Optional, Tuple
 
 import torch
@@ -49,9 +48,7 @@ class _Tensors:
 
     def __getattr__(self, name):
         lib = _dpo.load()
-        path = os.path.join(_build.OUT, "dpo_tensors.so")
-        if not os.path.exists(path):
-            _build.build()
+        path = _build.build(only=["dpo_tensors.so"])["dpo_tensors.so"]
         spec = importlib.util.spec_from_file_location("dpo_tensors", path)
         mod = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(mod)

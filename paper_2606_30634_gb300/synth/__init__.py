@@ -32,7 +32,7 @@ def load():
     if _lib is not None:
         return _lib
     from .. import build as _build
-    path = _build.build()["libdpo_synth.so"]
+    path = _build.build(only=["libdpo_synth.so"])["libdpo_synth.so"]
     L = ctypes.CDLL(path)
     u64, u32, i64, P = ctypes.c_uint64, ctypes.c_uint32, ctypes.c_int64, ctypes.c_void_p
     L.synth_philox.restype = None
