@@ -82,6 +82,19 @@ def _torch_flags():
              "-lc10_cuda"])
 
 
+def _torch_tag() -> str:
+    """What a module built against PyTorch depends on beside its sources."""
+    import torch
+    return f"python {sys.version}\ntorch {torch.__version__} in {os.path.dirname(torch.__file__)}\n"
+
+
+def _read(path):
+    if not os.path.exists(path):
+        return None
+    with open(path) as f:
+        return f.read()
+
+
 def _run(cmd, what):
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
@@ -113,7 +126,8 @@ def build(force: bool = False, quiet: bool = True, only=None) -> dict:
         spec = LIBS[lib]
         out = os.path.join(OUT, lib)
         deps = [os.path.join(PKG, p) for p in spec["sources"] + spec["headers"]]
-        if force or any(_mtime(d) > _mtime(out) for d in deps):
+        other = spec.get("torch", False) and _read(out + ".tag") != _torch_tag()
+        if force or other or any(_mtime(d) > _mtime(out) for d in deps):
             for src in spec["sources"]:
                 obj = os.path.join(OUT, os.path.basename(src) + ".o")
                 jobs.append((lib, src, obj, spec["includes"], src in spec["ptxas_v"],
@@ -135,6 +149,9 @@ def build(force: bool = False, quiet: bool = True, only=None) -> dict:
                 cmd = [NVCC] + ARCH + ["-shared", "-Xcompiler", "-fopenmp", "-o", tmp] + objs
             _run(cmd, f"link of {lib}")
             os.replace(tmp, out)
+            if LIBS[lib].get("torch", False):
+                with open(out + ".tag", "w") as f:
+                    f.write(_torch_tag())
     return {lib: os.path.join(OUT, lib) for lib in names}
 
 

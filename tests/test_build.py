@@ -30,3 +30,22 @@ def test_the_optimizers_do_not_need_the_tensor_module(out):
     assert sorted(os.listdir(out)) == ["libdpo.so", "libdpo_synth.so"]
     with pytest.raises((RuntimeError, OSError)):   # and it fails loudly where it is needed
         ffn._t.pack8
+
+
+def test_a_module_of_another_pytorch_is_built_again(tmp_path, monkeypatch):
+    path = build.build()["dpo_tensors.so"]
+    monkeypatch.setattr(build, "OUT", str(tmp_path))
+    for f in os.listdir(os.path.dirname(path)):
+        if f.startswith("dpo_tensors.so"):   # newer than its sources
+            shutil.copy(os.path.join(os.path.dirname(path), f), tmp_path / f)
+    built = []
+    monkeypatch.setattr(build, "_compile", lambda src, *a: built.append(src) or "")
+    monkeypatch.setattr(build, "_run", lambda cmd, what: open(cmd[cmd.index("-o") + 1], "w").close())
+    build.build(only=["dpo_tensors.so"])
+    assert built == []
+    import torch
+    monkeypatch.setattr(torch, "__version__", "0.0")
+    build.build(only=["dpo_tensors.so"])
+    assert built == ["csrc/dpo_tensors.cpp"]
+    build.build(only=["dpo_tensors.so"])
+    assert len(built) == 1
