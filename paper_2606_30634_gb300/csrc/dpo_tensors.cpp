@@ -14,6 +14,7 @@
 #include <ATen/ops/empty_strided.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+#include <c10/util/DimVector.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -206,15 +207,30 @@ struct Packed {
     Tensor codes, scales;
     dpo_packed8 p;
 };
-Packed make_packed(int64_t rows, int64_t cols, at::Device device, int64_t pitch)
+// What stands for a tensor of this shape: codes of the same shape, and scales that differ
+// in the last dimension.
+Packed make_packed(at::IntArrayRef size, at::Device device)
 {
     Packed q;
-    const int64_t ld = (cols + pitch - 1) / pitch * pitch, ng = groups(cols);
-    q.codes = ld == cols ? make({rows, cols}, at::kByte, device)
-                         : at::empty_strided({rows, cols}, {ld, 1},
-                                             at::TensorOptions().dtype(at::kByte).device(device));
-    q.scales = make({rows, ng}, at::kByte, device);
-    q.p = {(uint8_t *)q.codes.data_ptr(), (uint8_t *)q.scales.data_ptr(), ld, ng};
+    c10::DimVector groups_of(size.begin(), size.end());
+    const int64_t cols = size.back(), ng = groups(cols);
+    groups_of.back() = ng;
+    q.codes = make(size, at::kByte, device);
+    q.scales = make(groups_of, at::kByte, device);
+    q.p = {(uint8_t *)q.codes.data_ptr(), (uint8_t *)q.scales.data_ptr(), cols, ng};
+    return q;
+}
+// A matrix whose codes have a pitch of whole 32 bytes.
+Packed make_kept(int64_t rows, int64_t cols, at::Device device)
+{
+    const int64_t ld = (cols + 31) / 32 * 32;
+    if (ld == cols)
+        return make_packed({rows, cols}, device);
+    Packed q;
+    q.codes = at::empty_strided({rows, cols}, {ld, 1},
+                                at::TensorOptions().dtype(at::kByte).device(device));
+    q.scales = make({rows, groups(cols)}, at::kByte, device);
+    q.p = {(uint8_t *)q.codes.data_ptr(), (uint8_t *)q.scales.data_ptr(), ld, groups(cols)};
     return q;
 }
 
@@ -284,7 +300,7 @@ PyObject *pack8(PyObject *, PyObject *const *a, Py_ssize_t n)
         const Mat m = rows_of(x, "x");
         const int dt = dtype_of(x, "x");
         void *const s = stream_of(x, "x");
-        const Packed q = make_packed(m.rows, m.cols, x.device(), 1);
+        const Packed q = make_packed(x.sizes(), x.device());
         check(g_lib.pack8(m.p, (dpo_dtype)dt, m.rows, m.cols, m.ld, &q.p, s));
         return tuple(q.codes, q.scales);
     });
@@ -344,7 +360,7 @@ PyObject *add_rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
         const Tensor rstd = make({m.rows}, at::kFloat, device);
         Packed q;
         if (integer(a[4])) {
-            q = make_packed(m.rows, m.cols, device, 1);
+            q = make_packed(x.sizes(), device);
             k.x8 = q.p;
         }
         k.x = m.p;
@@ -449,8 +465,8 @@ PyObject *gated_ffn(PyObject *, PyObject *const *a, Py_ssize_t n)
         Packed g, u;
         Tensor g16, u16;
         if (k.keep == DPO_KEEP_8BIT) {
-            g = make_packed(k.tokens, k.hidden, device, 32);
-            u = make_packed(k.tokens, k.hidden, device, 32);
+            g = make_kept(k.tokens, k.hidden, device);
+            u = make_kept(k.tokens, k.hidden, device);
             k.gate8 = g.p;
             k.up8 = u.p;
         } else if (k.keep == DPO_KEEP_BF16) {

@@ -63,8 +63,8 @@ _t = _Tensors()
 
 
 class Packed8(NamedTuple):
-    """A matrix in 8 bits: E4M3 ``codes`` (uint8, rows x cols) and the scale bytes of
-    each row's groups of 32 (uint8, rows x ceil(cols / 32))."""
+    """A tensor in 8 bits: E4M3 ``codes`` (uint8, its shape) and the scale bytes of the
+    groups of 32 along its last dimension (uint8, ceil(n / 32) of them)."""
     codes: torch.Tensor
     scales: torch.Tensor
 
@@ -85,8 +85,8 @@ class NormOut(NamedTuple):
 
 
 class Kept(NamedTuple):
-    """What ``gated_ffn`` keeps of its projections for the backward: each a Packed8, or a
-    bf16 tensor."""
+    """What ``gated_ffn`` keeps of its projections for the backward: each a matrix of all
+    tokens, a Packed8 or a bf16 tensor."""
     gate: object
     up: object
     activation: str
@@ -102,7 +102,7 @@ class Kept(NamedTuple):
 # ----------------------------------------------------- activations, 8 bits --
 
 def pack8(x, *, stream=None) -> Packed8:
-    """x (fp32 or bf16, any leading dimensions) in 8 bits."""
+    """x (fp32 or bf16, any leading dimensions, which the result keeps) in 8 bits."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return pack8(x)
