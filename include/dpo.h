@@ -529,7 +529,8 @@ int dpo_rmsnorm_workspace(int64_t rows, int64_t cols, int64_t *bytes);
  * A is rounded once to bf16, the second product's operand type. keep says what
  * is stored of G and U: their 8-bit form or bf16. dim and hidden are multiples
  * of 8; pointers are 16-byte aligned, pitches of bf16 matrices multiples of 8,
- * of codes of 16.
+ * of codes of 16. (What the backward reads of codes may be 8-byte aligned with a
+ * pitch of a multiple of 8, as a copy without the forward's pitch is.)
  */
 typedef struct {
     const void *x;              /* bf16, tokens x dim */

@@ -610,8 +610,9 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
             b.rc = call_fail(DPO_EINVAL, "%s: a gain goes with x8, not with x", what);
     }
     if (a.keep == DPO_KEEP_8BIT) {
-        b.packed("gate8", a.gate8, T, F, 16, false);
-        b.packed("up8", a.up8, T, F, 16, false);
+        // read in pieces of 8 codes; the forward's TMA stores want 16 bytes
+        b.packed("gate8", a.gate8, T, F, 8, false);
+        b.packed("up8", a.up8, T, F, 8, false);
         if (b.rc == DPO_OK && (a.gate8.ld_scales != a.up8.ld_scales || a.gate8.ld_codes != a.up8.ld_codes))
             b.rc = call_fail(DPO_EINVAL, "%s: gate8 and up8 have different pitches", what);
     } else {

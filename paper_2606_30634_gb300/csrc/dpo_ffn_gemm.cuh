@@ -448,8 +448,8 @@ __device__ __forceinline__ void back_pair(float2 g, float2 u, float2 da, uint32_
 // 16-byte ones 125, none at all 112; loaded a chunk ahead they are hidden):
 // Product::wide says that all rows are 32-byte aligned and whole chunks of 128 columns, so
 // a row's chunk of codes is one load (past L1: 134 -> 124 us) and four chunks' scales
-// another. Otherwise rows and pitches are 16-byte aligned and hidden is a multiple of 8:
-// pieces of 8 elements. Rows past the end read the last one.
+// another. Otherwise rows and pitches are 8-byte (codes) or 16-byte (bf16) aligned and hidden
+// is a multiple of 8: pieces of 8 elements. Rows past the end read the last one.
 template <bool CODES> struct Kept {
     static constexpr int W = CODES ? 2 : 4;   // words of 8 elements
     uint32_t g[4 * W], u[4 * W];

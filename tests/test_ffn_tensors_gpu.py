@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from paper_2606_30634_gb300 import ffn
-from test_ffn_gpu import DEV, gen, randn
+from test_ffn_gpu import DEV, ffn_case, gen, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +37,24 @@ def test_the_norms_8_bit_rows_keep_the_shape():
     dx, dw = ffn.add_rms_norm_backward(dy, w, o.rstd, x8=o.x8)
     dx2, dw2 = ffn.add_rms_norm_backward(dy.view(10, 72), w, o.rstd, x8=flat.x8)
     assert dx.shape == x.shape and torch.equal(dx.view(10, 72), dx2) and torch.equal(dw, dw2)
+
+
+def away(p):
+    """A Packed8 moved to the host and back: contiguous, without the pitch it had."""
+    return ffn.Packed8(p.codes.cpu().to(DEV), p.scales.cpu().to(DEV))
+
+
+@pytest.mark.parametrize("t,d,f", [(1, 64, 72), (7, 328, 136), (300, 200, 328), (1001, 520, 1560),
+                                   (23, 2400, 1096)])
+def test_what_was_kept_may_have_been_on_the_host(t, d, f):
+    g, x, *w = ffn_case(t, d, f)
+    _, kept = ffn.gated_ffn(x, *w)
+    back = ffn.Kept(away(kept.gate), away(kept.up), kept.activation, kept.keep)
+    assert t == 1 or f % 32 == 0 or back.gate.codes.stride() != kept.gate.codes.stride()
+    dout = randn(g, t, d, scale=1e-2)
+    res = []
+    for k in (kept, back):
+        dw = [torch.empty_like(v) for v in w]
+        res.append([ffn.gated_ffn_backward(dout, k, *w, *dw, x=x), *dw])
+    assert all(torch.equal(a, b) for a, b in zip(*res))
+    assert ffn.status() == 0
