@@ -420,7 +420,8 @@ int dpo_grad_norm_noalloc(const void *grad, int64_t numel, dpo_dtype grad_dtype,
  * These calls have no context. The caller owns every buffer, workspace included;
  * all are device memory of the current device. Matrices are row-major with
  * contiguous rows; ld is the pitch in elements between rows (>= the columns).
- * No output may overlap an input or another output. Nothing is allocated and
+ * No output may overlap an input or another output; blocks of columns of one
+ * buffer, with its pitch, may lie side by side. Nothing is allocated and
  * the host is never synchronized: the launches go to the stream passed in, and
  * the buffers stay alive and in place until they are done. Two calls
  * may share a workspace only on one stream. A call of zero rows launches

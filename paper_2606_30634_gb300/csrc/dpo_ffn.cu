@@ -375,7 +375,7 @@ int check_sizes(const char *what, int64_t tokens, int64_t dim, int64_t hidden)
 struct Buffers {
     struct Entry {
         const char *name;
-        uintptr_t lo, hi;
+        Extent at;
         bool out;
     };
     const char *what;
@@ -400,8 +400,7 @@ struct Buffers {
                            (long long)align);
         if (rc != DPO_OK)
             return;
-        const uintptr_t b = reinterpret_cast<uintptr_t>(p);
-        e[n++] = {name, b, b + (uintptr_t)(((rows - 1) * ld + cols) * size), out};
+        e[n++] = {name, extent_of(p, rows, cols, ld, size), out};
     }
     void packed(const char *name, const dpo_packed8 &p, int64_t rows, int64_t cols, int64_t align,
                 bool out)
@@ -413,7 +412,7 @@ struct Buffers {
     {
         for (int i = 0; i < n && rc == DPO_OK; ++i)
             for (int j = 0; j < i && rc == DPO_OK; ++j)
-                if ((e[i].out || e[j].out) && e[i].lo < e[j].hi && e[j].lo < e[i].hi)
+                if ((e[i].out || e[j].out) && overlap(e[i].at, e[j].at))
                     rc = call_fail(DPO_EINVAL, "%s: %s overlaps %s", what, e[i].name, e[j].name);
         return rc;
     }

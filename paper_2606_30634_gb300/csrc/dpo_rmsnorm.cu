@@ -819,18 +819,6 @@ BackShape back_shape(int64_t rows, int64_t cols, int sms)
     return b;
 }
 
-struct Span {
-    uintptr_t lo, hi;
-};
-Span span_of(const void *p, int64_t rows, int64_t cols, int64_t ld, int64_t size)
-{
-    const uintptr_t b = reinterpret_cast<uintptr_t>(p);
-    if (p == nullptr || rows <= 0 || cols <= 0)
-        return {0, 0};
-    return {b, b + (uintptr_t)(((rows - 1) * ld + cols) * size)};
-}
-bool meet(Span a, Span b) { return a.lo < b.hi && b.lo < a.hi; }
-
 template <class... P, class... A>
 int launch(const char *what, void (*kernel)(P...), int64_t grid, int threads, size_t smem,
            void *stream, A &&...args)
@@ -894,10 +882,10 @@ int pack_or_unpack(const char *what, const void *x, dpo_dtype dtype, int64_t row
         rc = check_packed(what, *p, cols);
     if (rc != DPO_OK)
         return rc;
-    const Span sx = span_of(x, rows, cols, ld_x, size),
-               sc = span_of(p->codes, rows, cols, p->ld_codes, 1),
-               ss = span_of(p->scales, rows, groups_of(cols), p->ld_scales, 1);
-    if (meet(sx, sc) || meet(sx, ss) || (!unpack && meet(sc, ss)))
+    const Extent sx = extent_of(x, rows, cols, ld_x, size),
+               sc = extent_of(p->codes, rows, cols, p->ld_codes, 1),
+               ss = extent_of(p->scales, rows, groups_of(cols), p->ld_scales, 1);
+    if (overlap(sx, sc) || overlap(sx, ss) || (!unpack && overlap(sc, ss)))
         return call_fail(DPO_EINVAL, "%s: buffers overlap", what);
     const int sms = sm_count();
     if (sms == 0)
@@ -1060,20 +1048,20 @@ extern "C" int dpo_rmsnorm(const dpo_rmsnorm_args *args, void *cuda_stream)
     if (a.x8.codes != nullptr && (rc = check_packed(what, a.x8, a.cols)) != DPO_OK)
         return rc;
     const int64_t ng = groups_of(a.cols);
-    const Span in[] = {span_of(a.x, a.rows, a.cols, a.ld_x, size),
-                       span_of(a.residual, a.rows, a.cols, a.ld_residual, size),
-                       span_of(a.weight, 1, a.cols, a.cols, elem_size(a.weight_dtype))};
-    const Span out[] = {span_of(a.h, a.rows, a.cols, a.ld_h, size),
-                        span_of(a.y, a.rows, a.cols, a.ld_y, size),
-                        span_of(a.rstd, 1, a.rows, a.rows, 4),
-                        span_of(a.x8.codes, a.rows, a.cols, a.x8.ld_codes, 1),
-                        span_of(a.x8.codes ? a.x8.scales : nullptr, a.rows, ng, a.x8.ld_scales, 1)};
+    const Extent in[] = {extent_of(a.x, a.rows, a.cols, a.ld_x, size),
+                       extent_of(a.residual, a.rows, a.cols, a.ld_residual, size),
+                       extent_of(a.weight, 1, a.cols, a.cols, elem_size(a.weight_dtype))};
+    const Extent out[] = {extent_of(a.h, a.rows, a.cols, a.ld_h, size),
+                        extent_of(a.y, a.rows, a.cols, a.ld_y, size),
+                        extent_of(a.rstd, 1, a.rows, a.rows, 4),
+                        extent_of(a.x8.codes, a.rows, a.cols, a.x8.ld_codes, 1),
+                        extent_of(a.x8.codes ? a.x8.scales : nullptr, a.rows, ng, a.x8.ld_scales, 1)};
     for (int i = 0; i < 5; ++i) {
-        for (const Span &s : in)
-            if (meet(out[i], s))
+        for (const Extent &s : in)
+            if (overlap(out[i], s))
                 return call_fail(DPO_EINVAL, "%s: an output overlaps an input", what);
         for (int j = 0; j < i; ++j)
-            if (meet(out[i], out[j]))
+            if (overlap(out[i], out[j]))
                 return call_fail(DPO_EINVAL, "%s: outputs overlap", what);
     }
     int v = a.dtype == DPO_BF16 ? 8 : 4;
@@ -1153,23 +1141,23 @@ extern "C" int dpo_rmsnorm_backward(const dpo_rmsnorm_backward_args *args, void 
             return call_fail(DPO_EALIGN, "%s: workspace", what);
     }
     const uint8_t *codes = a.h == nullptr ? a.x8.codes : nullptr;
-    const Span in[] = {span_of(a.dy, a.rows, a.cols, a.ld_dy, size),
-                       span_of(a.h, a.rows, a.cols, a.ld_h, size),
-                       span_of(a.dh, a.rows, a.cols, a.ld_dh, size),
-                       span_of(a.rstd, 1, a.rows, a.rows, 4),
-                       span_of(a.weight, 1, a.cols, a.cols, elem_size(a.weight_dtype)),
-                       span_of(codes, a.rows, a.cols, a.x8.ld_codes, 1),
-                       span_of(codes ? a.x8.scales : nullptr, a.rows, groups_of(a.cols),
+    const Extent in[] = {extent_of(a.dy, a.rows, a.cols, a.ld_dy, size),
+                       extent_of(a.h, a.rows, a.cols, a.ld_h, size),
+                       extent_of(a.dh, a.rows, a.cols, a.ld_dh, size),
+                       extent_of(a.rstd, 1, a.rows, a.rows, 4),
+                       extent_of(a.weight, 1, a.cols, a.cols, elem_size(a.weight_dtype)),
+                       extent_of(codes, a.rows, a.cols, a.x8.ld_codes, 1),
+                       extent_of(codes ? a.x8.scales : nullptr, a.rows, groups_of(a.cols),
                                a.x8.ld_scales, 1)};
-    const Span out[] = {span_of(a.dx, a.rows, a.cols, a.ld_dx, size),
-                        span_of(a.dweight, 1, a.cols, a.cols, elem_size(a.dweight_dtype)),
-                        span_of(a.dweight ? a.workspace : nullptr, 1, grid * a.cols, grid * a.cols, 4)};
+    const Extent out[] = {extent_of(a.dx, a.rows, a.cols, a.ld_dx, size),
+                        extent_of(a.dweight, 1, a.cols, a.cols, elem_size(a.dweight_dtype)),
+                        extent_of(a.dweight ? a.workspace : nullptr, 1, grid * a.cols, grid * a.cols, 4)};
     for (int i = 0; i < 3; ++i) {
-        for (const Span &s : in)
-            if (meet(out[i], s))
+        for (const Extent &s : in)
+            if (overlap(out[i], s))
                 return call_fail(DPO_EINVAL, "%s: an output overlaps an input", what);
         for (int j = 0; j < i; ++j)
-            if (meet(out[i], out[j]))
+            if (overlap(out[i], out[j]))
                 return call_fail(DPO_EINVAL, "%s: outputs overlap", what);
     }
     int v = a.dtype == DPO_BF16 ? 8 : 4;

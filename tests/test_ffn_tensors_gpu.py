@@ -7,7 +7,7 @@ from __future__ import annotations
 import pytest
 import torch
 
-from paper_2606_30634_gb300 import ffn
+from paper_2606_30634_gb300 import dpo, ffn
 from test_ffn_gpu import DEV, ffn_case, gen, randn
 
 pytestmark = pytest.mark.gpu
@@ -58,3 +58,54 @@ def test_what_was_kept_may_have_been_on_the_host(t, d, f):
         res.append([ffn.gated_ffn_backward(dout, k, *w, *dw, x=x), *dw])
     assert all(torch.equal(a, b) for a, b in zip(*res))
     assert ffn.status() == 0
+
+
+def beside(g, rows, cols):
+    """A random matrix and an empty one in the columns to its right, in one buffer."""
+    buf = randn(g, rows, 2 * cols)
+    return buf[:, :cols], buf[:, cols:], buf
+
+
+@pytest.mark.parametrize("t,d,f", [(5, 64, 72), (40, 264, 520), (300, 200, 328), (2600, 136, 264),
+                                   (23, 2056, 1096)])
+@pytest.mark.parametrize("side", [0, 1])
+def test_outputs_beside_inputs(t, d, f, side):
+    """out and dx in the columns beside x and dout: nothing but their own columns changes."""
+    g, _, *w = ffn_case(t, d, f)
+    x, out, buf = beside(g, t, d)
+    dout, dx, dbuf = beside(g, t, d)
+    if side:
+        x, out, dout, dx = out, x, dx, dout
+    x0, dout0 = x.clone(), dout.clone()
+    want, kept = ffn.gated_ffn(x0, *w, keep="bf16")
+    dw = [torch.empty_like(v) for v in w]
+    wdx = ffn.gated_ffn_backward(dout0, kept, *w, *dw, x=x0)
+    got, _ = ffn.gated_ffn(x, *w, keep="bf16", out=out)
+    gdx = ffn.gated_ffn_backward(dout, kept, *w, *dw, x=x, dx=dx)
+    assert got is out and gdx is dx
+    assert torch.equal(out, want) and torch.equal(dx, wdx)
+    assert torch.equal(x, x0) and torch.equal(dout, dout0)
+    assert ffn.status() == 0
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 64), (7, 72), (300, 1000), (2003, 33)])
+def test_norm_outputs_beside_its_inputs(rows, cols):
+    g = gen(rows)
+    x, y, _ = beside(g, rows, cols)
+    r, h, _ = beside(g, rows, cols)
+    dy, dx, _ = beside(g, rows, cols)
+    w = 1 + randn(g, cols, scale=0.1)
+    x0, r0, dy0 = x.clone(), r.clone(), dy.clone()
+    want = ffn.add_rms_norm(x0, w, r0)
+    rstd = torch.empty_like(want.rstd)
+    p, ld = (lambda v: v.data_ptr()), 2 * cols
+    dpo.dpo_rmsnorm(dpo.dpo_rmsnorm_args(
+        x=p(x), residual=p(r), weight=p(w), h=p(h), y=p(y), rstd=p(rstd), rows=rows, cols=cols,
+        ld_x=ld, ld_residual=ld, ld_h=ld, ld_y=ld, eps=1e-5, dtype=dpo.DPO_BF16,
+        weight_dtype=dpo.DPO_BF16))
+    wdx, _ = ffn.add_rms_norm_backward(dy0, w, rstd, h=want.h)
+    dpo.dpo_rmsnorm_backward(dpo.dpo_rmsnorm_backward_args(
+        dy=p(dy), h=p(h), rstd=p(rstd), weight=p(w), dx=p(dx), rows=rows, cols=cols, ld_dy=ld,
+        ld_h=ld, ld_dx=ld, dtype=dpo.DPO_BF16, weight_dtype=dpo.DPO_BF16))
+    for a, b in ((y, want.y), (h, want.h), (rstd, want.rstd), (dx, wdx), (x, x0), (r, r0), (dy, dy0)):
+        assert torch.equal(a, b)
