@@ -287,7 +287,8 @@ __device__ __forceinline__ float rcp(float x)
 
 // act(z) = z s(q(z)) with s the logistic function: SiLU with q = z, GELU's tanh form
 // with q = 2 sqrt(2/pi) (z + 0.044715 z^3), since (1 + tanh(q / 2)) / 2 = s(q).
-// act' = s + z q' s (1 - s).
+// act' = s + z q' s (1 - s), taken as ((1 - s) q') (z s) + s: past |z| = 10^19 q' would be
+// infinite, where 1 - s or z s is 0, so dq ends at the largest finite number.
 template <int ACT>
 __device__ __forceinline__ float logistic(float z, float &dq)
 {
@@ -296,7 +297,7 @@ __device__ __forceinline__ float logistic(float z, float &dq)
     if (ACT == kGelu) {
         const float c = 1.5957691216057308f, k = 0.044715f * c, z2 = z * z;
         q = z * fmaf(k, z2, c);
-        dq = fmaf(3.0f * k, z2, c);
+        dq = fminf(fmaf(3.0f * k, z2, c), kMaxFinite);
     }
     return rcp(1.0f + exp2(-1.4426950408889634f * q));
 }
@@ -437,8 +438,8 @@ __device__ __forceinline__ void back_pair(float2 g, float2 u, float2 da, uint32_
     const float a0 = g.x * s0, a1 = g.y * s1;
     a = gemm::pack_bf16(a0 * u.x, a1 * u.y);
     du = gemm::pack_bf16(da.x * a0, da.y * a1);
-    dg = gemm::pack_bf16(da.x * u.x * fmaf(a0 * q0, 1.0f - s0, s0),
-                         da.y * u.y * fmaf(a1 * q1, 1.0f - s1, s1));
+    dg = gemm::pack_bf16(da.x * u.x * fmaf((1.0f - s0) * q0, a0, s0),
+                         da.y * u.y * fmaf((1.0f - s1) * q1, a1, s1));
 }
 
 // 32 columns of one row of what was kept of G and U, as loaded: codes with their scale
