@@ -177,6 +177,15 @@ void *matrix_of(const Tensor &t, int64_t rows, int64_t cols, at::ScalarType type
     return t.data_ptr();
 }
 
+// A weight of the block, whose products take bf16.
+void *weight_of(const Tensor &t, int64_t rows, int64_t cols, at::Device device, const char *name)
+{
+    if (t.scalar_type() == at::kFloat)
+        type_error(std::string(name) + ": Float, expected BFloat16 (an optimizer's stale weights are "
+                   "with stash_dtype=DPO_BF16)");
+    return matrix_of(t, rows, cols, at::kBFloat16, device, name);
+}
+
 constexpr int64_t groups(int64_t cols) { return (cols + DPO_PACK8_GROUP - 1) / DPO_PACK8_GROUP; }
 
 dpo_packed8 packed_of(PyObject *codes, PyObject *scales, int64_t rows, int64_t cols,
@@ -448,9 +457,9 @@ PyObject *gated_ffn(PyObject *, PyObject *const *a, Py_ssize_t n)
         k.tokens = m.rows;
         k.dim = m.cols;
         k.hidden = wg.size(0);
-        k.w_gate = matrix_of(wg, k.hidden, k.dim, at::kBFloat16, device, "w_gate");
-        k.w_up = matrix_of(tensor(a[2], "w_up"), k.hidden, k.dim, at::kBFloat16, device, "w_up");
-        k.w_down = matrix_of(tensor(a[3], "w_down"), k.dim, k.hidden, at::kBFloat16, device, "w_down");
+        k.w_gate = weight_of(wg, k.hidden, k.dim, device, "w_gate");
+        k.w_up = weight_of(tensor(a[2], "w_up"), k.hidden, k.dim, device, "w_up");
+        k.w_down = weight_of(tensor(a[3], "w_down"), k.dim, k.hidden, device, "w_down");
         check(g_lib.ffn_workspace(k.tokens, k.dim, k.hidden, 0, &k.workspace_bytes, nullptr));
         Tensor out;
         if (a[6] == Py_None) {
@@ -507,9 +516,9 @@ PyObject *gated_ffn_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         k.tokens = m.rows;
         k.dim = m.cols;
         k.hidden = wg.size(0);
-        k.w_gate = matrix_of(wg, k.hidden, k.dim, at::kBFloat16, device, "w_gate");
-        k.w_up = matrix_of(tensor(a[8], "w_up"), k.hidden, k.dim, at::kBFloat16, device, "w_up");
-        k.w_down = matrix_of(tensor(a[9], "w_down"), k.dim, k.hidden, at::kBFloat16, device, "w_down");
+        k.w_gate = weight_of(wg, k.hidden, k.dim, device, "w_gate");
+        k.w_up = weight_of(tensor(a[8], "w_up"), k.hidden, k.dim, device, "w_up");
+        k.w_down = weight_of(tensor(a[9], "w_down"), k.dim, k.hidden, device, "w_down");
         const Tensor &dwg = tensor(a[10], "dw_gate");
         const at::ScalarType gt = dwg.scalar_type();
         k.grad_dtype = dtype_of(dwg, "dw_gate");

@@ -4,7 +4,9 @@ activations kept in 8 bits (include/dpo.h, "The feed-forward half of a pipeline
 stage").
 
 A stage runs its forward and backward at ``opt.stale(i)`` and writes the weights'
-gradients into ``opt.grads(i)``, which the next ``opt.step`` reads:
+gradients into ``opt.grads(i)``, which the next ``opt.step`` reads. The block takes its
+weights in bf16, so their optimizer is made with ``stash_dtype=DPO_BF16`` (DelayedMuon's
+default; DelayedAdamW's is fp32, which the norm's weight may have):
 
     n = ffn.add_rms_norm(x, w_norm, residual=r, save8=True)
     out, kept = ffn.gated_ffn(n.y, w_gate, w_up, w_down)

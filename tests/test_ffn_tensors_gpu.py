@@ -7,7 +7,7 @@ from __future__ import annotations
 import pytest
 import torch
 
-from paper_2606_30634_gb300 import dpo, ffn
+from paper_2606_30634_gb300 import dpo, ffn, muon
 from test_ffn_gpu import DEV, ffn_case, gen, randn
 
 pytestmark = pytest.mark.gpu
@@ -109,3 +109,33 @@ def test_norm_outputs_beside_its_inputs(rows, cols):
         ld_h=ld, ld_dx=ld, dtype=dpo.DPO_BF16, weight_dtype=dpo.DPO_BF16))
     for a, b in ((y, want.y), (h, want.h), (rstd, want.rstd), (dx, wdx), (x, x0), (r, r0), (dy, dy0)):
         assert torch.equal(a, b)
+
+
+def test_weights_of_an_optimizer(cuda_device):
+    """The stale weights of both optimizers: in bf16 they are what the block takes; the fp32
+    ones of a default DelayedAdamW are refused with what to do, and are fine in the norm."""
+    t, d, f = 9, 64, 72
+    g, x, *w = ffn_case(t, d, f)
+    want, _ = ffn.gated_ffn(x, *w)
+    shapes = [v.shape for v in w]
+    start = [v.float().flatten() for v in w]
+    sets = [dpo.DelayedAdamW([v.numel() for v in w], stash_dtype=dpo.DPO_BF16, x0=start),
+            muon.DelayedMuon([tuple(s) for s in shapes], x0=[v.float() for v in w]),
+            dpo.DelayedAdamW([v.numel() for v in w] + [d], x0=start + [torch.ones(d, device=DEV)])]
+    try:
+        for o in sets[:2]:
+            stale = [o.stale(i).view(s) for i, s in enumerate(shapes)]
+            out, kept = ffn.gated_ffn(x, *stale)
+            assert torch.equal(out, want)
+        wide = [sets[2].stale(i).view(s) for i, s in enumerate(shapes)]
+        with pytest.raises(TypeError, match="stash_dtype=DPO_BF16"):
+            ffn.gated_ffn(x, *wide)
+        dw = [torch.empty_like(v) for v in w]
+        for k in range(3):
+            with pytest.raises(TypeError, match=("w_gate", "w_up", "w_down")[k] + ".*stash_dtype"):
+                ffn.gated_ffn_backward(x, kept, *w[:k], wide[k], *w[k + 1:], *dw, x=x)
+        o = ffn.add_rms_norm(x, sets[2].stale(3))
+        assert torch.equal(o.y, ffn.add_rms_norm(x, torch.ones(d, device=DEV)).y)
+    finally:
+        for o in sets:
+            o.close()
