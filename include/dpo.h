@@ -587,6 +587,33 @@ int dpo_ffn_workspace(int64_t tokens, int64_t dim, int64_t hidden, int from_x8,
                       int64_t *forward_bytes, int64_t *backward_bytes);
 
 /*
+ * Test hook for the choice of forms: how the products of a forward that keeps
+ * `keep`, and of a backward with dx from it (for DPO_KEEP_NONE as from bf16),
+ * are launched where slots[0] CTA pairs, slots[1] single CTAs and slots[2 .. 5]
+ * clusters that split a tile's K by 1, 2, 4, 8 are resident at once; slots NULL:
+ * what the current device holds. forms receives five: the gate's product, the
+ * down product, the gate's backward, dx in a launch of its own, and the list of
+ * the weights' gradients, with dx where it has no launch. Returns DPO_OK,
+ * DPO_EINVAL (also for no tokens) or DPO_ECUDA.
+ */
+#define DPO_FFN_NO_LAUNCH 0
+#define DPO_FFN_STREAM 1    /* weights streamed, for few tokens */
+#define DPO_FFN_PAIRS 2     /* CTA pairs */
+#define DPO_FFN_SINGLE 3    /* single CTAs */
+#define DPO_FFN_SPLIT 4     /* clusters that split K */
+
+typedef struct {
+    int kind;                   /* DPO_FFN_* */
+    int split;                  /* shares of K */
+    int cols;                   /* a tile's columns (the gate's product: of both together) */
+    int64_t tiles;
+    int slots;                  /* tiles at once */
+} dpo_ffn_form;
+
+int dpo_ffn_test_forms(int64_t tokens, int64_t dim, int64_t hidden, int keep, const int *slots,
+                       dpo_ffn_form *forms);
+
+/*
  * Error bits of the feed-forward kernels on the current device since the last
  * clear (a wait inside a kernel that gave up after one second; 0 when healthy).
  * Waits for the device. dpo_ffn_clear_status clears them on the stream.

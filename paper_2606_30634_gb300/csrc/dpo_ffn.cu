@@ -292,6 +292,31 @@ Choice form_of(const Device &d, const Shape *s, int n, int epi)
     return best;
 }
 
+// The products of a call of T tokens, D dim and F hidden.
+Shape gate_shape(int64_t T, int64_t D, int64_t F) { return {T, F, D, 1}; }   // its backward too
+Shape down_shape(int64_t T, int64_t D, int64_t F) { return {T, D, F, 1}; }
+struct Gradients {   // dx, then the weights'
+    Shape s[kMaxProducts];
+};
+Gradients gradient_shapes(int64_t T, int64_t D, int64_t F)
+{
+    return {{{T, D, F, 2}, {F, D, T, 1}, {F, D, T, 1}, {D, F, T, 1}}};
+}
+// dx with the weights' gradients in one list, or, where its few long tiles would be what the
+// list waits for, before them with K split (1B widths, 9 tokens: its tiles have 128 blocks,
+// the gradients' one).
+struct DxChoice {
+    bool alone;
+    Form form;      // of its own launch
+};
+DxChoice dx_form(const Device &d, const Gradients &g)
+{
+    const Choice all = form_of(d, g.s, 4, kStore), dx = form_of(d, g.s, 1, kStore);
+    return {dx.form.thin && dx.time + form_of(d, g.s + 1, 3, kStore).time + 2000.0 < all.time, dx.form};
+}
+// The forward's products by streaming the weights (dpo_ffn_few.cuh), which has no 8-bit form.
+bool streamed(int64_t tokens, int keep) { return tokens <= kFewTokens && keep != DPO_KEEP_8BIT; }
+
 int run(const char *what, const Device &d, Launch &L, const Shape *s, int n, int epi, Form f,
         bool followed, bool maps_ok, void *stream)
 {
@@ -476,7 +501,7 @@ extern "C" int dpo_ffn_forward(const dpo_ffn_args *args, void *cuda_stream)
     if ((rc = device_info(what, &d)) != DPO_OK)
         return rc;
 
-    if (T <= kFewTokens && a.keep != DPO_KEEP_8BIT) {
+    if (streamed(T, a.keep)) {
         using E = __nv_bfloat16;
         FewArgs f{};
         f.x = static_cast<const E *>(a.x);
@@ -508,7 +533,7 @@ extern "C" int dpo_ffn_forward(const dpo_ffn_args *args, void *cuda_stream)
         return run_few(what, o, kStore, d->sms, cuda_stream);
     }
     {
-        const Shape s = {T, F, D, 1};
+        const Shape s = gate_shape(T, D, F);
         const Form form = form_of(*d, &s, 1, kGate).form;
         const int rows_w = form.cg == 2 ? BH : form.cols / 2;   // a box of either projection
         Launch L{};
@@ -543,7 +568,7 @@ extern "C" int dpo_ffn_forward(const dpo_ffn_args *args, void *cuda_stream)
         if ((rc = run(what, *d, L, &s, 1, kGate, form, true, m.ok, cuda_stream)) != DPO_OK)
             return rc;
     }
-    const Shape s = {T, D, F, 1};
+    const Shape s = down_shape(T, D, F);
     Launch L{};
     Maps m;
     const Form form = form_of(*d, &s, 1, kStore).form;
@@ -631,7 +656,7 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
     const void *x = a.x;
     int64_t ld_x = a.ld_x;
     {
-        const Shape s = {T, F, D, 1};
+        const Shape s = gate_shape(T, D, F);
         const int epi = a.keep == DPO_KEEP_8BIT ? kGateBack8 : kGateBack16;
         const Form form = form_of(*d, &s, 1, epi).form;
         Launch L{};
@@ -677,16 +702,13 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
             return rc;
     }
     Launch L{};
-    const Shape s[kMaxProducts] = {{T, D, F, 2}, {F, D, T, 1}, {F, D, T, 1}, {D, F, T, 1}};
+    const Gradients g = gradient_shapes(T, D, F);
+    const Shape *const s = g.s;
     Maps m;
     int n = 0, first = 1;   // products of L, of s
     if (a.dx != nullptr) {
-        // dx with the weights' gradients in one list, or, where its few long tiles would be
-        // what the list waits for, before them with K split (1B widths, 9 tokens: its tiles
-        // have 128 blocks, the gradients' one)
-        const Choice all = form_of(*d, s, 4, kStore), dx = form_of(*d, s, 1, kStore);
-        const bool alone = dx.form.thin &&
-                           dx.time + form_of(*d, s + 1, 3, kStore).time + 2000.0 < all.time;
+        const DxChoice dx = dx_form(*d, g);
+        const bool alone = dx.alone;
         const Form f = alone ? dx.form : kPairs;
         Product &P = L.p[0];
         m.operand(&P.a[0], dg, T, F, F, f.a_rows);
@@ -733,6 +755,58 @@ extern "C" int dpo_ffn_backward(const dpo_ffn_backward_args *args, void *cuda_st
     }
     return run(what, *d, L, s + first, n, kStore, form_of(*d, s + first, n, kStore).form, false, m.ok,
                cuda_stream);
+}
+
+extern "C" int dpo_ffn_test_forms(int64_t tokens, int64_t dim, int64_t hidden, int keep,
+                                  const int *slots, dpo_ffn_form *forms)
+{
+    const char *what = "dpo_ffn_test_forms";
+    int rc = check_sizes(what, tokens, dim, hidden);
+    if (rc != DPO_OK)
+        return rc;
+    if (tokens == 0 || forms == nullptr ||
+        (keep != DPO_KEEP_NONE && keep != DPO_KEEP_8BIT && keep != DPO_KEEP_BF16))
+        return call_fail(DPO_EINVAL, "%s: tokens %lld, keep %d", what, (long long)tokens, keep);
+    Device given;
+    const Device *d = &given;
+    if (slots == nullptr) {
+        if ((rc = device_info(what, &d)) != DPO_OK)
+            return rc;
+    } else {
+        for (int i = 0; i < 6; ++i)
+            if (slots[i] < 1)
+                return call_fail(DPO_EINVAL, "%s: %d slots", what, slots[i]);
+        for (int e = 0; e < kForms; ++e) {
+            given.pairs[e] = slots[0];
+            given.singles[e] = slots[1];
+            for (int i = 0; i < 4; ++i)
+                given.clusters[i][e] = slots[2 + i];
+        }
+    }
+    auto fill = [&](dpo_ffn_form &out, const Shape *s, int n, int epi, const Form &f) {
+        int64_t tiles = 0;
+        for (int i = 0; i < n; ++i)
+            tiles += tiles_of(s[i], f, epi);
+        out = {f.cg == 2 ? DPO_FFN_PAIRS : f.thin ? DPO_FFN_SPLIT : DPO_FFN_SINGLE, f.ways, f.cols, tiles,
+               slots_of(*d, f, epi)};
+    };
+    const Shape gate = gate_shape(tokens, dim, hidden), down = down_shape(tokens, dim, hidden);
+    if (streamed(tokens, keep)) {
+        forms[0] = forms[1] = {DPO_FFN_STREAM, 0, 0, 0, 0};
+    } else {
+        fill(forms[0], &gate, 1, kGate, form_of(*d, &gate, 1, kGate).form);
+        fill(forms[1], &down, 1, kStore, form_of(*d, &down, 1, kStore).form);
+    }
+    const int back = keep == DPO_KEEP_8BIT ? kGateBack8 : kGateBack16;
+    fill(forms[2], &gate, 1, back, form_of(*d, &gate, 1, back).form);
+    const Gradients g = gradient_shapes(tokens, dim, hidden);
+    const DxChoice dx = dx_form(*d, g);
+    forms[3] = {DPO_FFN_NO_LAUNCH, 0, 0, 0, 0};
+    if (dx.alone)
+        fill(forms[3], g.s, 1, kStore, dx.form);
+    const int first = dx.alone ? 1 : 0, n = kMaxProducts - first;
+    fill(forms[4], g.s + first, n, kStore, form_of(*d, g.s + first, n, kStore).form);
+    return DPO_OK;
 }
 
 extern "C" int dpo_ffn_get_status(uint32_t *bits)

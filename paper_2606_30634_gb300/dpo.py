@@ -31,6 +31,7 @@ DPO_OPT_ADAMW, DPO_OPT_NADAM, DPO_OPT_LION, DPO_OPT_ADAN = 0, 1, 2, 3
 DPO_STASH_COPY, DPO_STASH_PINGPONG = 0, 1
 DPO_ACT_SILU, DPO_ACT_GELU = 0, 1
 DPO_KEEP_NONE, DPO_KEEP_8BIT, DPO_KEEP_BF16 = 0, 1, 2
+DPO_FFN_NO_LAUNCH, DPO_FFN_STREAM, DPO_FFN_PAIRS, DPO_FFN_SINGLE, DPO_FFN_SPLIT = range(5)
 DPO_PACK8_GROUP = 32
 DPO_RMSNORM_MAX_COLS = 16384
 
@@ -42,7 +43,7 @@ EXPORTS = ("dpo_init", "dpo_stash", "dpo_step", "dpo_read_weights", "dpo_get_ste
            "dpo_set_timing", "dpo_get_timing", "dpo_pack8", "dpo_unpack8", "dpo_rmsnorm",
            "dpo_rmsnorm_backward", "dpo_rmsnorm_workspace", "dpo_ffn_forward",
            "dpo_ffn_backward", "dpo_ffn_workspace", "dpo_ffn_get_status",
-           "dpo_ffn_clear_status")
+           "dpo_ffn_clear_status", "dpo_ffn_test_forms")
 
 DPO_NOALLOC_CHUNK_ELEMS = 1 << 20
 DPO_NOALLOC_MAX_CHUNKS = 16384
@@ -110,6 +111,10 @@ class dpo_ffn_backward_args(ctypes.Structure):
                 ("workspace_bytes", _L)]
 
 
+class dpo_ffn_form(ctypes.Structure):
+    _fields_ = [("kind", _I), ("split", _I), ("cols", _I), ("tiles", _L), ("slots", _I)]
+
+
 _lib = None
 
 
@@ -165,6 +170,7 @@ def load() -> ctypes.CDLL:
         "dpo_ffn_workspace": (I, [_L, _L, _L, I, P, P]),
         "dpo_ffn_get_status": (I, [P]),
         "dpo_ffn_clear_status": (I, [P]),
+        "dpo_ffn_test_forms": (I, [_L, _L, _L, I, P, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -352,7 +358,8 @@ def dpo_grad_norm_noalloc(grad, numel: int, grad_dtype: int, max_grad_norm: floa
 
 
 # ------------------------------------- the feed-forward half of a stage --
-# Argument structures as in include/dpo.h; ``ffn`` fills them from tensors.
+# The calls as they are in include/dpo.h, with its argument structures; ``ffn`` makes the
+# same ones from tensors through dpo_tensors.
 
 def dpo_pack8(x, dtype: int, rows: int, cols: int, ld_x: int, out: dpo_packed8,
               stream=None) -> None:
@@ -405,6 +412,14 @@ def dpo_ffn_get_status() -> int:
 
 def dpo_ffn_clear_status(stream=None) -> None:
     _check(load().dpo_ffn_clear_status(_stream(stream)), None)
+
+
+def dpo_ffn_test_forms(tokens: int, dim: int, hidden: int, keep: int, slots=None):
+    """The five forms (include/dpo.h): gate, down, gate backward, dx alone, gradients."""
+    out = (dpo_ffn_form * 5)()
+    given = None if slots is None else (ctypes.c_int * 6)(*slots)
+    _check(load().dpo_ffn_test_forms(tokens, dim, hidden, keep, given, out), None)
+    return list(out)
 
 
 # ------------------------------------------------------------------ owner --
