@@ -4,6 +4,8 @@ call on plain tensors, bit for bit, which test_ffn_gpu.py compares with the defi
 """
 from __future__ import annotations
 
+import threading
+
 import pytest
 import torch
 
@@ -139,3 +141,47 @@ def test_weights_of_an_optimizer(cuda_device):
     finally:
         for o in sets:
             o.close()
+
+
+def test_threads_and_streams_at_once():
+    """Four host threads, each with a stream and sizes of its own, step at once; each gets what
+    it gets alone, and an error of one is not another's."""
+    sizes = [(5, 264, 520), (77, 136, 264), (900, 520, 1560), (20, 512, 4096)]
+    jobs = []
+    for i, (t, d, f) in enumerate(sizes):
+        g, x, *w = ffn_case(t, d, f, seed=70 + i)
+        jobs.append((x, w, 1 + randn(g, d, scale=0.1), randn(g, t, d, scale=1e-2)))
+
+    def step(x, w, wn, dout):
+        n = ffn.add_rms_norm(x, wn, x, save8=True)
+        out, kept = ffn.gated_ffn(n.y, *w)
+        dw = [torch.empty_like(v) for v in w]
+        dy = ffn.gated_ffn_backward(dout, kept, *w, *dw, x8=n.x8, gain=wn)
+        dx, dwn = ffn.add_rms_norm_backward(dy, wn, n.rstd, x8=n.x8, dh=dout)
+        return [out, dx, dwn, *dw]
+
+    want = [step(*j) for j in jobs]
+    torch.cuda.synchronize()
+    got, wrong = [None] * len(jobs), []
+
+    def work(i):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for k in range(20):
+                    got[i] = step(*jobs[i])
+                    with pytest.raises(dpo.DpoError, match="dpo_ffn_forward: out"):
+                        ffn.gated_ffn(jobs[i][0], *jobs[i][1], out=jobs[i][0])
+            stream.synchronize()
+        except BaseException as e:
+            wrong.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(jobs))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong
+    for a, b in zip(want, got):
+        assert all(torch.equal(u, v) for u, v in zip(a, b))
+    assert ffn.status() == 0
