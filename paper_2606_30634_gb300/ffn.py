@@ -17,11 +17,14 @@ default; DelayedAdamW's is fp32, which the norm's weight may have):
 
 Every step of it runs in libdpo.so's kernels; PyTorch provides memory and streams, and
 dpo_tensors (csrc/dpo_tensors.cpp) checks the tensors and makes the calls. Tensors are on
-the current CUDA device; their last dimension is contiguous and the others flatten to rows. Outputs are allocated unless given. Calls go to PyTorch's
-current stream, or to ``stream=`` (a torch.cuda.Stream), on which the outputs and
-workspaces are then allocated too; tensors last used on another stream need the usual
-event or ``wait_stream`` before the call. ValueError and TypeError for tensors that do
-not fit, DpoError for what the library refuses.
+the current CUDA device; their last dimension is contiguous and the others flatten to
+rows. Outputs are allocated unless given. Calls go to PyTorch's current stream, or to
+``stream=`` (a torch.cuda.Stream), on which the outputs and workspaces are then allocated
+too; tensors last used on another stream need the usual event or ``wait_stream`` before
+the call, and ``record_stream`` if they are freed before it has run. Autograd does not see
+these calls: outputs require no gradient, and the backward passes are the calls here.
+ValueError and TypeError for tensors that do not fit, DpoError for what the library
+refuses.
 """
 from __future__ import annotations
 
@@ -197,5 +200,6 @@ def gated_ffn_backward(dout, kept: Kept, w_gate, w_up, w_down, dw_gate, dw_up, d
 
 
 def status() -> int:
-    """Error bits of the tensor-core kernels (0: healthy); waits for the device."""
+    """Error bits of the tensor-core kernels (0: healthy), until dpo.dpo_ffn_clear_status
+    clears them; waits for the device."""
     return _dpo.dpo_ffn_get_status()
