@@ -5,7 +5,7 @@ from __future__ import annotations
 
 import pytest
 
-from ffn_forms import BACK, DOWN, DX, GATE, GB300, KEEP, LIST, ROUNDS, SPLIT, WHOLE, forms, rounds
+from ffn_forms import BACK, DOWN, DX, GATE, GB300, KEEP, LIST, NEAR, ROUNDS, SPLIT, WHOLE, forms, rounds
 from paper_2606_30634_gb300 import dpo
 from test_ffn_forms_gpu import SIZES
 
@@ -22,6 +22,22 @@ def test_sizes_of_the_split_tests(size, keep):
         f = got[product]
         assert (f.kind, f.split, f.cols) == (dpo.DPO_FFN_SPLIT, split, cols), product
         assert (rounds(f) > 1) == (size in ROUNDS)
+
+
+@pytest.mark.parametrize("slots", NEAR)
+def test_the_gpu_tests_split_on_a_chip_with_other_clusters(slots):
+    for sizes in (SPLIT, ROUNDS, WHOLE):
+        for size, products in sizes.items():
+            for keep in ("8bit", "bf16"):
+                got = forms(size, keep, slots)
+                for p in set(products) - {DX}:
+                    if keep == "bf16" and size[0] <= 8 and p in (GATE, DOWN):
+                        continue
+                    assert got[p].kind == dpo.DPO_FFN_SPLIT and (rounds(got[p]) > 1) >= (sizes is ROUNDS)
+    got = forms((20, 512, 4096), "8bit", slots)   # test_ffn_abi_gpu.py
+    assert got[DOWN].kind == got[DX].kind == dpo.DPO_FFN_SPLIT
+    for size in ((70, 1032, 264), (300, 200, 328), (2600, 136, 264)):
+        assert forms(size, "8bit", slots)[DX].kind == dpo.DPO_FFN_NO_LAUNCH
 
 
 def test_the_split_tests_reach_every_split():

@@ -8,7 +8,7 @@ import numpy as np
 import pytest
 import torch
 
-from ffn_forms import BACK, DOWN, GATE, ROUNDS, SPLIT, WHOLE, forms, rounds
+from ffn_forms import DOWN, DX, GATE, ROUNDS, SPLIT, WHOLE, forms, rounds
 from paper_2606_30634_gb300 import dpo, ffn
 from test_ffn_gpu import check_backward, check_forward, ffn_case, np64, randn
 
@@ -16,10 +16,10 @@ pytestmark = pytest.mark.gpu
 
 
 def takes(size, keep, products, several=False):
-    """The forms on this device, which need not be GB300's table to the last cluster."""
+    """The products are split on this device, whatever its number of clusters."""
     got = forms(size, keep, None)
     for p in products:
-        if keep == "bf16" and size[0] <= 8 and p in (GATE, DOWN):
+        if p == DX or (keep == "bf16" and size[0] <= 8 and p in (GATE, DOWN)):
             continue
         assert got[p].kind == dpo.DPO_FFN_SPLIT, (size, p)
         assert not several or rounds(got[p]) > 1
@@ -99,7 +99,7 @@ def test_non_finite_tokens_stay_in_their_rows(size, keep):
     assert ffn.status() == 0
 
 
-@pytest.mark.parametrize("size", [(39, 2560, 528), (397, 1560, 584), (19, 1808, 976)])
+@pytest.mark.parametrize("size", [(39, 2560, 528), (572, 2056, 456), (135, 1408, 256)])
 def test_a_group_with_an_infinity_keeps_its_finite_scale(size):
     """One gate column overflows to infinity: its code is NaN, and its group's scale is that
     of the other 31 columns. The 8-bit values of the other columns are those without it."""
