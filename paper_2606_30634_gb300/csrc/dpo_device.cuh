@@ -26,12 +26,10 @@ namespace {
 // (ld_table; ld.global.nc) is for the tables of init alone. Everything else is
 // read by an ordinary load: a plain one, which the wait's memory clobber keeps
 // behind it, or a volatile asm, which keeps its place among volatile asms.
-// No kernel of the optimizers asks for its successor earlier than that
+// No kernel asks for its successor earlier than that
 // (griddepcontrol.launch_dependents at its start): CTAs that arrive while
 // others still run are spread unevenly over the SMs, and the persistent
-// kernels lose more than the launch costs. (The launches inside one feed-forward
-// call do, behind their own wait: dpo_ffn_gemm.cuh, dpo_ffn_few.cuh, and the
-// widening of 8-bit rows, dpo_call.h.) GB300, with against without it: the
+// kernels lose more than the launch costs. GB300, with against without it: the
 // GPT-2 AdamW step 768 / 741 us, the clipped 1B step 8006 / 7876, GPT-2's
 // Newton-Schulz step 1679 / 1565; only a clipped step on 74 thousand elements
 // gained (9.5 / 10.0).

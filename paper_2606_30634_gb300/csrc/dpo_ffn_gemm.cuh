@@ -171,6 +171,9 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
     }
 }
 
+// Between the launches of one feed-forward call: the kernels here, the streaming one and the
+// widening of 8-bit rows (dpo_call.h) let their successor start early. What dpo_device.cuh says of
+// "no kernel" is of the optimizers', whose figures it gives.
 __device__ __forceinline__ void launch_dependents()
 {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
