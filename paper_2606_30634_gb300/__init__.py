@@ -5,4 +5,4 @@ hand-written CUDA kernels, with a thin Python binding in ``dpo``.
 Submodules load their native libraries on first use; importing the package
 itself loads nothing.
 """
-__all__ = ["dpo", "muon", "ffn", "synth", "build"]
+__all__ = ["dpo", "muon", "ffn", "ends", "synth", "build"]

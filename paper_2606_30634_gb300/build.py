@@ -2,9 +2,11 @@
 
 * ``_build/libdpo.so``       -- the product: C ABI of include/dpo.h and its
                                 kernels (csrc/).
-* ``_build/dpo_tensors.so``   -- the feed-forward calls on PyTorch tensors, a
-                                Python module (ffn.py's other half), compiled
-                                against PyTorch's headers by the host compiler.
+* ``_build/dpo_tensors.so``   -- the feed-forward calls and those of the
+                                pipeline's ends on PyTorch tensors, a Python
+                                module (ffn.py's and ends.py's other half),
+                                compiled against PyTorch's headers by the
+                                host compiler.
 * ``_build/libdpo_synth.so`` -- seeded synthetic inputs (include/dpo_synth.h),
                                 used by the tests and the benchmark.
 
@@ -37,18 +39,20 @@ LIBS = {
         "sources": ["csrc/dpo_kernels.cu", "csrc/dpo_step_adamw.cu", "csrc/dpo_step_nadam.cu",
                     "csrc/dpo_step_lion.cu", "csrc/dpo_step_adan.cu", "csrc/dpo_abi.cpp",
                     "csrc/dpo_noalloc.cu", "csrc/dpo_muon.cu", "csrc/dpo_rmsnorm.cu",
-                    "csrc/dpo_ffn.cu"],
+                    "csrc/dpo_ffn.cu", "csrc/dpo_embed.cu", "csrc/dpo_dropout.cu",
+                    "csrc/dpo_logprobs.cu", "csrc/dpo_head.cu"],
         "headers": ["csrc/dpo_internal.h", "csrc/dpo_device.cuh", "csrc/dpo_reduce.cuh",
                     "csrc/dpo_step.cuh",
                     "csrc/dpo_gemm.cuh", "csrc/dpo_call.h", "csrc/dpo_pack8.cuh",
-                    "csrc/dpo_ffn_gemm.cuh", "csrc/dpo_ffn_few.cuh", "../include/dpo.h",
-                    "../include/dpo_muon.h"],
+                    "csrc/dpo_ffn_gemm.cuh", "csrc/dpo_ffn_few.cuh", "csrc/dpo_check.h",
+                    "csrc/dpo_vec.cuh", "csrc/dpo_ends.cuh", "csrc/dpo_logprobs.cuh", "csrc/dpo_products.h",
+                    "../include/dpo.h", "../include/dpo_muon.h", "../include/dpo_ends.h"],
         "includes": ["csrc"],
         "ptxas_v": ["csrc/dpo_step_adamw.cu", "csrc/dpo_muon.cu", "csrc/dpo_ffn.cu"],
     },
     "dpo_tensors.so": {
         "sources": ["csrc/dpo_tensors.cpp"],
-        "headers": ["../include/dpo.h"],
+        "headers": ["../include/dpo.h", "../include/dpo_ends.h"],
         "includes": [],
         "ptxas_v": [],
         "torch": True,

@@ -1,0 +1,584 @@
+// dpo_embed.cu -- the embedding of token ids and its gradient (dpo_embed, dpo_embed_backward in
+// include/dpo_ends.h).
+//
+// Forward: out[t] = scale table[id_t]; one pass, the rows' bytes in and out.
+// Backward: dtable[v] = scale sum over the t with id_t = v of dy[t]. The tokens are sorted by id
+// (stably, so each id's tokens stay in order), and the sorted list is cut into chunks of
+// equal length; a CTA adds up the rows of a chunk, id by id, in fp32. An id's run within one
+// chunk is finished there; of one that crosses chunks every chunk leaves a partial sum, and
+// the chunks' sums are added in order. So the work is even whatever the ids are, and its
+// order depends on the ids alone.
+#include "dpo_ends.cuh"
+#include "dpo_vec.cuh"
+
+#include <math.h>
+
+namespace dpo {
+namespace {
+
+// ------------------------------------------------------------- forward ----
+// A warp takes kPieces accesses a lane of one row: 2 KB of a bf16 row of 16-byte accesses, so
+// that a single token's row is shared by several warps and its latency is one access's.
+constexpr int kPieces = 4, kEmbedWarps = 8;
+
+struct EmbedArgs {
+    Ids ids;
+    const void *table;
+    void *out;
+    int64_t tokens, vocab, dim, ld_table, ld_out, segs;
+    float scale;
+};
+
+template <class TT, class OT, int V>
+__global__ void __launch_bounds__(32 * kEmbedWarps) embed_kernel(const EmbedArgs a)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t unit = (int64_t)blockIdx.x * kEmbedWarps + (threadIdx.x >> 5);
+    const int64_t t = unit / a.segs;
+    pdl_wait();
+    if (t >= a.tokens)
+        return;
+    const int64_t c0 = (unit - t * a.segs) * (32 * kPieces * V) + lane * V;
+    const int id = a.ids.at(t, a.vocab);
+    const TT *const row = static_cast<const TT *>(a.table) + (int64_t)max(id, 0) * a.ld_table;
+    OT *const out = static_cast<OT *>(a.out) + t * a.ld_out;
+    Vec<TT, V> v[kPieces];
+#pragma unroll
+    for (int n = 0; n < kPieces; ++n) {
+        v[n].zero();
+        if (id >= 0 && c0 + n * 32 * V < a.dim)
+            v[n].load(row + c0 + n * 32 * V);
+    }
+#pragma unroll
+    for (int n = 0; n < kPieces; ++n) {
+        float x[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            x[j] = v[n].get(j) * (id >= 0 ? a.scale : 0.0f);
+        Vec<OT, V> o;
+        o.set(x);
+        if (c0 + n * 32 * V < a.dim)
+            o.store(out + c0 + n * 32 * V);
+    }
+}
+
+// ---------------------------------------------------------------- sort ----
+// (id, token) pairs of up to DPO_EMBED_SPAN tokens by id, least significant digit first, in the
+// shared memory of one cluster: a launch, with the cluster's barrier between its steps. In a
+// pass every warp ranks its own 256 pairs, in their order, among those with the same digit
+// (match.any), the counts are added up over warps and CTAs, and the pairs are sent to their
+// places, wherever in the cluster these are. Padding sorts behind the last id.
+constexpr int kSortItems = 8, kSortThreads = 1024, kSortMinThreads = 128, kSortCtas = 8;
+constexpr int kDigitBits = 9;   // of a pass, at most
+static_assert(kSortItems * kSortThreads * kSortCtas == DPO_EMBED_SPAN, "a span is a cluster's");
+
+struct SortArgs {
+    Ids ids;
+    int64_t first, count;      // tokens of this span
+    int64_t vocab;
+    int passes, bits;          // of a pass
+    uint2 *sorted;             // (id, token of the span)
+    int *n_valid;              // how many are no padding
+    uint32_t *met;             // a bit for each id that is met
+};
+
+__host__ __device__ constexpr int sort_smem(int threads, int bits)
+{
+    return threads * kSortItems * 8 + (threads / 32 + 2) * (1 << bits) * 4;
+}
+
+__global__ void __launch_bounds__(kSortThreads) sort_ids_kernel(const SortArgs a)
+{
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ uint32_t warp_sums[32];
+    const int nt = blockDim.x, warps = nt >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cta_of_cluster(), ranks = ctas_of_cluster();
+    const int per = nt * kSortItems, digits = 1 << a.bits;
+    uint2 *const items = reinterpret_cast<uint2 *>(smem);
+    uint32_t *const count = reinterpret_cast<uint32_t *>(items + per);   // [warp][digit]
+    uint32_t *const total = count + warps * digits;                      // of this CTA
+    uint32_t *const base = total + digits;                               // first place, in all
+    uint32_t *const mine = count + warp * digits;
+    const uint32_t pad = (uint32_t)a.vocab;
+    const int at0 = warp * 32 * kSortItems + lane;
+    pdl_wait();
+    for (int64_t i = (int64_t)rank * nt + threadIdx.x; i < (a.vocab + 31) / 32; i += ranks * nt)
+        a.met[i] = 0u;
+    uint32_t key[kSortItems], pos[kSortItems], place[kSortItems];
+#pragma unroll
+    for (int i = 0; i < kSortItems; ++i) {
+        const int64_t t = (int64_t)rank * per + at0 + i * 32;
+        key[i] = pad;
+        pos[i] = (uint32_t)t;
+        if (t < a.count) {
+            const int id = a.ids.at(a.first + t, a.vocab);
+            key[i] = id < 0 ? pad : (uint32_t)id;
+        }
+    }
+    for (int p = 0; p < a.passes; ++p) {
+        const int shift = p * a.bits;
+        auto digit = [&](int i) { return key[i] >> shift & (uint32_t)(digits - 1); };
+        for (int d = lane; d < digits; d += 32)
+            mine[d] = 0u;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kSortItems; ++i) {
+            const uint32_t d = digit(i), peers = __match_any_sync(0xFFFFFFFFu, d);
+            const uint32_t before = __popc(peers & ((1u << lane) - 1u)), old = mine[d];
+            __syncwarp();
+            if (before == 0)
+                mine[d] = old + __popc(peers);
+            __syncwarp();
+            place[i] = old + before;
+        }
+        __syncthreads();
+        for (int d = threadIdx.x; d < digits; d += nt) {   // counts of earlier warps
+            uint32_t sum = 0;
+            for (int w = 0; w < warps; ++w) {
+                const uint32_t c = count[w * digits + d];
+                count[w * digits + d] = sum;
+                sum += c;
+            }
+            total[d] = sum;
+        }
+        cluster_barrier();
+        // first places: digits below, then the same digit in earlier CTAs
+        const int each = digits > nt ? digits / nt : 1;   // consecutive digits of a thread
+        uint32_t sum = 0;
+        for (int j = 0; j < each; ++j) {
+            const int d = threadIdx.x * each + j;
+            if (d < digits) {
+                uint32_t all = 0, earlier = 0;
+                for (uint32_t r = 0; r < ranks; ++r) {
+                    const uint32_t c = ld_cluster(in_cta(total + d, r));
+                    earlier += r < rank ? c : 0u;
+                    all += c;
+                }
+                base[d] = sum + earlier;
+                sum += all;
+            }
+        }
+        uint32_t scan = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, scan, o);
+            scan += lane >= o ? v : 0u;
+        }
+        if (lane == 31)
+            warp_sums[warp] = scan;
+        __syncthreads();
+        uint32_t below = scan - sum;
+        for (int w = 0; w < warp; ++w)
+            below += warp_sums[w];
+        for (int j = 0; j < each; ++j) {
+            const int d = threadIdx.x * each + j;
+            if (d < digits)
+                base[d] += below;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kSortItems; ++i) {
+            const uint32_t d = digit(i), to = base[d] + mine[d] + place[i];
+            st_cluster(in_cta(items + to % (uint32_t)per, to / (uint32_t)per), key[i], pos[i]);
+        }
+        cluster_barrier();
+#pragma unroll
+        for (int i = 0; i < kSortItems; ++i) {
+            key[i] = items[at0 + i * 32].x;
+            pos[i] = items[at0 + i * 32].y;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kSortItems; ++i) {
+        const int at = at0 + i * 32;
+        const int64_t g = (int64_t)rank * per + at;
+        const uint32_t prev = at > 0     ? items[at - 1].x
+                              : rank > 0 ? ld_cluster(in_cta(items + per - 1, rank - 1))
+                                         : ~0u;
+        if (key[i] != pad) {
+            a.sorted[g] = make_uint2(key[i], pos[i]);
+            if (prev != key[i])
+                atomicOr(a.met + key[i] / 32, 1u << key[i] % 32);
+            if (g + 1 == (int64_t)ranks * per)
+                *a.n_valid = (int)(g + 1);
+        } else if (prev != pad) {
+            *a.n_valid = (int)g;   // the first of the padding
+        }
+    }
+    cluster_barrier();   // no CTA leaves while its neighbour may read its last pair
+}
+
+// ------------------------------------------------------------ backward ----
+constexpr int kSumThreads = 128, kSumRows = 8;   // rows requested at a time
+constexpr int kSpan = 32;                        // pairs of a chunk, at least
+constexpr int kMaxChunk = DPO_EMBED_SPAN / 256;
+constexpr int kZeroRows = 16;                    // rows that a CTA looks at for clearing
+
+struct SumArgs {
+    const void *dy;
+    void *dtable;
+    const uint2 *sorted;
+    const int *n_valid;
+    const uint32_t *met;
+    float *partial;            // [chunk][begun here, not here][dim]
+    int64_t vocab, dim, ld_dy, ld_dtable;
+    int64_t sums;              // CTAs that add; the others clear the rows that no id has
+    int chunk, segs;
+    float scale;
+    int accumulate;
+};
+
+__device__ __forceinline__ uint2 ld_pair(const uint2 *p)
+{
+    uint2 q;
+    asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(q.x), "=r"(q.y) : "l"(p));
+    return q;
+}
+__device__ __forceinline__ int ld_int(const int *p)
+{
+    int v;
+    asm volatile("ld.global.b32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+
+// dtable[id, c ..] (+)= scale sum.
+template <class GT, int V>
+__device__ __forceinline__ void finish(const SumArgs &a, uint32_t id, int64_t c, const float (&sum)[V])
+{
+    GT *const p = static_cast<GT *>(a.dtable) + (int64_t)id * a.ld_dtable + c;
+    float y[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        y[j] = sum[j] * a.scale;
+    Vec<GT, V> o;
+    if (a.accumulate) {
+        o.load(p);
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            y[j] += o.get(j);
+    }
+    o.set(y);
+    o.store(p);
+}
+
+// CTAs [0, sums): a chunk of the sorted pairs and 128 V columns, a thread V of them. The
+// others: rows of dtable that no id has, set to zero.
+template <class T, class GT, int V>
+__global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const SumArgs a)
+{
+    __shared__ uint2 pair_[kMaxChunk + 2];
+    uint2 *const pair = pair_ + 1;
+    pdl_wait();
+    if (blockIdx.x >= a.sums) {
+        const int64_t r0 = ((int64_t)blockIdx.x - a.sums) * kZeroRows;
+        Vec<GT, V> o;
+        o.zero();
+        for (int i = threadIdx.x >> 5; i < kZeroRows && r0 + i < a.vocab; i += kSumThreads / 32) {
+            const int64_t r = r0 + i;
+            if (a.met[r / 32] >> (r % 32) & 1u)
+                continue;
+            GT *const p = static_cast<GT *>(a.dtable) + r * a.ld_dtable;
+            for (int64_t c = (int64_t)(threadIdx.x & 31) * V; c < a.dim; c += 32 * V)
+                o.store(p + c);
+        }
+        return;
+    }
+    const int chunk = (int)blockIdx.x / a.segs, seg = (int)blockIdx.x - chunk * a.segs;
+    const int n = ld_int(a.n_valid), i0 = chunk * a.chunk;
+    const int len = min(a.chunk, n - i0);
+    if (len <= 0)
+        return;
+    for (int i = threadIdx.x - 1; i <= len; i += kSumThreads)
+        pair[i] = i0 + i < 0 || i0 + i >= n ? make_uint2(~0u, 0u) : ld_pair(a.sorted + i0 + i);
+    __syncthreads();
+    const int64_t c = ((int64_t)seg * kSumThreads + threadIdx.x) * V;
+    if (c >= a.dim)
+        return;
+    const T *const dy = static_cast<const T *>(a.dy) + c;
+    float sum[V] = {};
+    bool here = pair[-1].x != pair[0].x;   // the run began in this chunk
+    for (int i = 0; i < len; i += kSumRows) {
+        Vec<T, V> v[kSumRows];
+#pragma unroll
+        for (int u = 0; u < kSumRows; ++u)
+            if (i + u < len)
+                v[u].load(dy + (int64_t)pair[i + u].y * a.ld_dy);
+#pragma unroll
+        for (int u = 0; u < kSumRows; ++u) {
+            if (i + u >= len)
+                break;
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                sum[j] += v[u].get(j);
+            const uint32_t id = pair[i + u].x;
+            const bool ends = pair[i + u + 1].x != id;
+            if (!ends && i + u + 1 < len)
+                continue;
+            if (here && ends) {
+                finish<GT, V>(a, id, c, sum);
+            } else {
+                float *const p = a.partial + ((int64_t)chunk * 2 + !here) * a.dim + c;
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    p[j] = sum[j];
+            }
+            here = true;
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                sum[j] = 0.0f;
+        }
+    }
+}
+
+// The runs that cross chunks: the CTA of the chunk where one begins adds its chunks' sums.
+template <class GT, int V>
+__global__ void __launch_bounds__(kSumThreads) embed_join_kernel(const SumArgs a)
+{
+    pdl_wait();
+    const int chunk = (int)blockIdx.x / a.segs, seg = (int)blockIdx.x - chunk * a.segs;
+    const int n = ld_int(a.n_valid), i0 = chunk * a.chunk, i1 = i0 + a.chunk, lane = threadIdx.x & 31;
+    if (i1 >= n)
+        return;
+    const uint32_t id = ld_pair(a.sorted + i1 - 1).x;
+    if (ld_pair(a.sorted + i1).x != id)
+        return;
+    if (i0 > 0 && ld_pair(a.sorted + i0 - 1).x == id)
+        return;   // begun before this chunk
+    int last = chunk + 1;   // the chunk where it ends: the next one does not begin with it
+    for (;; last += 32) {
+        const int64_t next = (int64_t)(last + lane + 1) * a.chunk;
+        const unsigned ends =
+            __ballot_sync(0xFFFFFFFFu, next >= n || ld_pair(a.sorted + next).x != id);
+        if (ends != 0u) {
+            last += __ffs(ends) - 1;
+            break;
+        }
+    }
+    const int64_t c = ((int64_t)seg * kSumThreads + threadIdx.x) * V;
+    if (c >= a.dim)
+        return;
+    float sum[V];
+    const float *p = a.partial + (int64_t)chunk * 2 * a.dim + c;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        sum[j] = p[j];
+    p += 3 * a.dim;   // the next chunk's run that did not begin there
+#pragma unroll 8
+    for (int k = chunk + 1; k <= last; ++k, p += 2 * a.dim)
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            sum[j] += p[j];
+    finish<GT, V>(a, id, c, sum);
+}
+
+// ---------------------------------------------------------------- host ----
+
+using EmbedFn = void (*)(EmbedArgs);
+using SumFn = void (*)(SumArgs);
+using B16 = __nv_bfloat16;
+
+template <class A, class B> constexpr int wide() { return sizeof(A) == 4 && sizeof(B) == 4 ? 4 : 8; }
+int wide_of(int a, int b) { return a == DPO_F32 && b == DPO_F32 ? 4 : 8; }
+
+template <class TT, class OT> EmbedFn embed_fn(int v)
+{
+    return v > 2 ? embed_kernel<TT, OT, wide<TT, OT>()> : v == 2 ? embed_kernel<TT, OT, 2> : embed_kernel<TT, OT, 1>;
+}
+EmbedFn embed_fn(int tt, int ot, int v)
+{
+    if (tt == DPO_F32)
+        return ot == DPO_F32 ? embed_fn<float, float>(v) : embed_fn<float, B16>(v);
+    return ot == DPO_F32 ? embed_fn<B16, float>(v) : embed_fn<B16, B16>(v);
+}
+template <class T, class GT> SumFn sum_fn(int v, bool join)
+{
+    constexpr int W = wide<T, GT>();
+    if (join)
+        return v > 2 ? embed_join_kernel<GT, W> : v == 2 ? embed_join_kernel<GT, 2> : embed_join_kernel<GT, 1>;
+    return v > 2 ? embed_sum_kernel<T, GT, W> : v == 2 ? embed_sum_kernel<T, GT, 2> : embed_sum_kernel<T, GT, 1>;
+}
+SumFn sum_fn(int t, int gt, int v, bool join)
+{
+    if (t == DPO_F32)
+        return gt == DPO_F32 ? sum_fn<float, float>(v, join) : sum_fn<float, B16>(v, join);
+    return gt == DPO_F32 ? sum_fn<B16, float>(v, join) : sum_fn<B16, B16>(v, join);
+}
+
+int check_table(const char *what, int64_t vocab, int64_t dim, float scale)
+{
+    if (vocab < 1 || dim < 1 || vocab >= kMaxCount - 1 || dim >= kMaxCount)
+        return call_fail(DPO_EINVAL, "%s: vocab %lld, dim %lld", what, (long long)vocab, (long long)dim);
+    if (!isfinite(scale))
+        return call_fail(DPO_EINVAL, "%s: scale", what);
+    return DPO_OK;
+}
+
+// The workspace of a span, and how its sorted pairs are cut.
+struct Plan {
+    int chunk, chunks;
+    int64_t sorted, met, partial, bytes;   // where each begins; n_valid is at 0
+};
+Plan plan_of(int64_t tokens, int64_t vocab, int64_t dim)
+{
+    auto up = [](int64_t v) { return (v + 255) / 256 * 256; };
+    const int64_t n = tokens < DPO_EMBED_SPAN ? tokens : DPO_EMBED_SPAN;
+    Plan p;
+    p.chunk = kSpan;
+    while ((int64_t)p.chunk * 256 < n)   // at most 256 chunks
+        p.chunk *= 2;
+    p.chunks = (int)((n + p.chunk - 1) / p.chunk);
+    p.sorted = 256;
+    p.met = p.sorted + up(n * 8);
+    p.partial = p.met + up((vocab + 31) / 32 * 4);
+    p.bytes = p.partial + (p.chunks > 1 ? up((int64_t)p.chunks * 2 * dim * 4) : 0);
+    return p;
+}
+
+}  // namespace
+}  // namespace dpo
+
+using namespace dpo;
+
+extern "C" int dpo_embed(const dpo_embed_args *args, void *cuda_stream)
+{
+    const char *what = "dpo_embed";
+    if (args == nullptr)
+        return call_fail(DPO_EINVAL, "%s: no arguments", what);
+    const dpo_embed_args &a = *args;
+    if (!known(a.table_dtype) || !known(a.out_dtype))
+        return call_fail(DPO_EDTYPE, "%s: table dtype %d, out dtype %d", what, a.table_dtype, a.out_dtype);
+    EmbedArgs k{};
+    int rc = check_table(what, a.vocab, a.dim, a.scale);
+    if (rc != DPO_OK || (rc = check_ids(what, a.ids, &k.ids, &k.tokens)) != DPO_OK || k.tokens == 0)
+        return rc;
+    const int64_t ts = elem_size(a.table_dtype), os = elem_size(a.out_dtype);
+    Buffers b(what);
+    add_ids(b, a.ids);
+    b.add("table", a.table, a.vocab, a.dim, a.ld_table, ts, ts, false);
+    b.add("out", a.out, k.tokens, a.dim, a.ld_out, os, os, true);
+    if ((rc = b.done()) != DPO_OK)
+        return rc;
+    Width w(wide_of(a.table_dtype, a.out_dtype));
+    w.fit(a.table, a.dim, a.ld_table, ts);
+    w.fit(a.out, a.dim, a.ld_out, os);
+    k.table = a.table;
+    k.out = a.out;
+    k.vocab = a.vocab;
+    k.dim = a.dim;
+    k.ld_table = a.ld_table;
+    k.ld_out = a.ld_out;
+    k.scale = a.scale;
+    const int64_t seg = 32 * kPieces * w.v;
+    k.segs = (a.dim + seg - 1) / seg;
+    const int64_t grid = (k.tokens * k.segs + kEmbedWarps - 1) / kEmbedWarps;
+    if (grid >= kMaxCount)
+        return call_fail(DPO_EINVAL, "%s: %lld tokens of %lld are too many", what, (long long)k.tokens,
+                         (long long)a.dim);
+    return launch(what, embed_fn(a.table_dtype, a.out_dtype, w.v), grid, 32 * kEmbedWarps, 0, cuda_stream, k);
+}
+
+extern "C" int dpo_embed_workspace(int64_t tokens, int64_t vocab, int64_t dim, int64_t *bytes)
+{
+    const char *what = "dpo_embed_workspace";
+    const int rc = check_table(what, vocab, dim, 1.0f);
+    if (rc != DPO_OK)
+        return rc;
+    if (bytes == nullptr || tokens < 0 || tokens >= kMaxCount)
+        return call_fail(DPO_EINVAL, "%s: %lld tokens", what, (long long)tokens);
+    *bytes = plan_of(tokens, vocab, dim).bytes;
+    return DPO_OK;
+}
+
+extern "C" int dpo_embed_backward(const dpo_embed_backward_args *args, void *cuda_stream)
+{
+    const char *what = "dpo_embed_backward";
+    if (args == nullptr)
+        return call_fail(DPO_EINVAL, "%s: no arguments", what);
+    const dpo_embed_backward_args &a = *args;
+    if (!known(a.dtype) || !known(a.grad_dtype))
+        return call_fail(DPO_EDTYPE, "%s: dtype %d, grad dtype %d", what, a.dtype, a.grad_dtype);
+    SortArgs so{};
+    int64_t tokens = 0;
+    int rc = check_table(what, a.vocab, a.dim, a.scale);
+    if (rc != DPO_OK || (rc = check_ids(what, a.ids, &so.ids, &tokens)) != DPO_OK)
+        return rc;
+    const int64_t size = elem_size(a.dtype), gsize = elem_size(a.grad_dtype);
+    const Plan plan = plan_of(tokens, a.vocab, a.dim);
+    Buffers b(what);
+    b.add("dtable", a.dtable, a.vocab, a.dim, a.ld_dtable, gsize, gsize, true);
+    if (tokens == 0) {
+        if ((rc = b.done()) != DPO_OK || a.accumulate)
+            return rc;
+        const cudaError_t e =
+            cudaMemset2DAsync(a.dtable, (size_t)(a.ld_dtable * gsize), 0, (size_t)(a.dim * gsize),
+                              (size_t)a.vocab, static_cast<cudaStream_t>(cuda_stream));
+        return e == cudaSuccess ? DPO_OK : call_fail(DPO_ECUDA, "%s: %s", what, cudaGetErrorString(e));
+    }
+    if (a.workspace != nullptr && a.workspace_bytes < plan.bytes)
+        return call_fail(DPO_EINVAL, "%s: workspace of %lld bytes, %lld needed", what,
+                         (long long)a.workspace_bytes, (long long)plan.bytes);
+    add_ids(b, a.ids);
+    b.add("dy", a.dy, tokens, a.dim, a.ld_dy, size, size, false);
+    b.add("workspace", a.workspace, 1, plan.bytes, plan.bytes, 1, 256, true);
+    if ((rc = b.done()) != DPO_OK)
+        return rc;
+    Width w(wide_of(a.dtype, a.grad_dtype));
+    w.fit(a.dy, a.dim, a.ld_dy, size);
+    w.fit(a.dtable, a.dim, a.ld_dtable, gsize);
+
+    uint8_t *const ws = static_cast<uint8_t *>(a.workspace);
+    SumArgs su{};
+    su.dtable = a.dtable;
+    su.n_valid = so.n_valid = reinterpret_cast<int *>(ws);
+    su.sorted = so.sorted = reinterpret_cast<uint2 *>(ws + plan.sorted);
+    su.met = so.met = reinterpret_cast<uint32_t *>(ws + plan.met);
+    su.partial = reinterpret_cast<float *>(ws + plan.partial);
+    su.vocab = so.vocab = a.vocab;
+    su.dim = a.dim;
+    su.ld_dy = a.ld_dy;
+    su.ld_dtable = a.ld_dtable;
+    su.scale = a.scale;
+    su.chunk = plan.chunk;
+    const int64_t seg = (int64_t)kSumThreads * w.v;
+    su.segs = (int)((a.dim + seg - 1) / seg);
+    int bits = 1;   // of the ids and of the padding's key
+    while ((a.vocab >> bits) != 0)
+        ++bits;
+    so.passes = (bits + kDigitBits - 1) / kDigitBits;
+    so.bits = (bits + so.passes - 1) / so.passes;
+    const int64_t clears = (a.vocab + kZeroRows - 1) / kZeroRows;
+    if ((int64_t)plan.chunks * su.segs + clears >= kMaxCount)
+        return call_fail(DPO_EINVAL, "%s: %lld x %lld is too large", what, (long long)a.vocab, (long long)a.dim);
+    const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(sort_ids_kernel),
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               sort_smem(kSortThreads, kDigitBits));
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return call_fail(DPO_ECUDA, "%s: %s", what, cudaGetErrorString(e));
+    }
+    for (int64_t first = 0; first < tokens; first += DPO_EMBED_SPAN) {
+        so.first = first;
+        so.count = tokens - first < DPO_EMBED_SPAN ? tokens - first : DPO_EMBED_SPAN;
+        int threads = kSortMinThreads, ctas = 1;
+        while (threads < kSortThreads && (int64_t)threads * kSortItems < so.count)
+            threads *= 2;
+        while ((int64_t)ctas * threads * kSortItems < so.count)
+            ctas *= 2;
+        rc = launch_in_clusters(what, sort_ids_kernel, ctas, ctas, threads, (size_t)sort_smem(threads, so.bits),
+                                cuda_stream, so);
+        if (rc != DPO_OK)
+            return rc;
+        su.dy = static_cast<const uint8_t *>(a.dy) + first * a.ld_dy * size;
+        su.accumulate = a.accumulate || first > 0;
+        const int chunks = (int)((so.count + su.chunk - 1) / su.chunk);
+        su.sums = (int64_t)chunks * su.segs;
+        rc = launch(what, sum_fn(a.dtype, a.grad_dtype, w.v, false), su.sums + (su.accumulate ? 0 : clears),
+                    kSumThreads, 0, cuda_stream, su);
+        if (rc == DPO_OK && chunks > 1)
+            rc = launch(what, sum_fn(a.dtype, a.grad_dtype, w.v, true), (int64_t)(chunks - 1) * su.segs,
+                        kSumThreads, 0, cuda_stream, su);
+        if (rc != DPO_OK)
+            return rc;
+    }
+    return DPO_OK;
+}

@@ -1,0 +1,119 @@
+// dpo_ends.cuh -- what the kernels of dpo_ends.h share: token ids as they lie in memory,
+// and the cluster's shared memory.
+#pragma once
+
+#include "dpo_check.h"
+#include "dpo_device.cuh"
+#include "dpo_ends.h"
+
+namespace dpo {
+namespace {
+
+// Ids of a block of tokens; a vector has cols = ld.
+struct Ids {
+    const void *p;
+    int64_t cols, ld;
+    int bytes;
+    // The id of token t, -1 for one outside 0 .. vocab - 1.
+    __device__ __forceinline__ int at(int64_t t, int64_t vocab) const
+    {
+        if (ld != cols) {
+            const int64_t r = t / cols;
+            t += r * (ld - cols);
+        }
+        int64_t id;
+        if (bytes == 8) {
+            asm volatile("ld.global.b64 %0, [%1];" : "=l"(id) : "l"(static_cast<const int64_t *>(p) + t));
+        } else {
+            int v;
+            asm volatile("ld.global.b32 %0, [%1];" : "=r"(v) : "l"(static_cast<const int *>(p) + t));
+            id = v;
+        }
+        return id >= 0 && id < vocab ? (int)id : -1;
+    }
+};
+
+__device__ __forceinline__ uint32_t cta_of_cluster()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t ctas_of_cluster()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+// By all threads of the cluster; orders their accesses to its shared and to global memory.
+__device__ __forceinline__ void cluster_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The address of p, in this CTA's shared memory, in that of another CTA of the cluster.
+__device__ __forceinline__ uint32_t in_cta(const void *p, uint32_t rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                 : "=r"(r)
+                 : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ uint32_t ld_cluster(uint32_t addr)
+{
+    uint32_t v;
+    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) { return __uint_as_float(ld_cluster(addr)); }
+__device__ __forceinline__ void st_cluster(uint32_t addr, uint32_t a, uint32_t b)
+{
+    asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+}
+
+// ---------------------------------------------------------------- host ----
+
+constexpr int64_t kMaxCount = (int64_t)1 << 31;
+
+// Ids as the kernels take them, checked, and their number.
+inline int check_ids(const char *what, const dpo_ids &s, Ids *out, int64_t *count)
+{
+    if (s.rows < 0 || s.cols < 0 || (s.cols > 0 && s.rows >= (kMaxCount + s.cols - 1) / s.cols))
+        return call_fail(DPO_EINVAL, "%s: %lld x %lld ids", what, (long long)s.rows, (long long)s.cols);
+    *count = s.rows * s.cols;
+    if (s.bytes != 4 && s.bytes != 8)
+        return call_fail(DPO_EDTYPE, "%s: ids of %d bytes", what, s.bytes);
+    if (*count == 0)
+        return DPO_OK;
+    const int64_t ld = s.rows == 1 ? s.cols : s.ld;
+    const int rc = check_matrix(what, "ids", s.p, s.cols, ld, s.bytes);
+    *out = ld == s.cols ? Ids{s.p, *count, *count, s.bytes} : Ids{s.p, s.cols, ld, s.bytes};
+    return rc;
+}
+inline void add_ids(Buffers &b, const dpo_ids &s)
+{
+    b.add("ids", s.p, s.rows, s.cols, s.rows == 1 ? s.cols : s.ld, s.bytes, s.bytes, false);
+}
+
+// Elements of an access: `wide`, or 2 or 1 where sizes, pitches or addresses are not multiples.
+struct Width {
+    int v;
+    explicit Width(int wide) : v(wide) {}
+    void fit(const void *p, int64_t cols, int64_t ld, int64_t size)
+    {
+        if (p == nullptr)
+            return;
+        auto ok = [&](int n) {
+            const int64_t bytes = n * size < 16 ? n * size : 16;
+            return cols % n == 0 && ld % n == 0 && reinterpret_cast<uintptr_t>(p) % bytes == 0;
+        };
+        if (v > 2 && !ok(v))
+            v = 2;
+        if (v == 2 && !ok(2))
+            v = 1;
+    }
+};
+
+}  // namespace
+}  // namespace dpo

@@ -13,8 +13,9 @@
 // rounding alone leaves 0.0017. As pairs of bf16 numbers they would hold 16 bits, for twice
 // the MMAs and bytes of the down product, of dx and of the weights' gradients.
 #include "dpo.h"
-#include "dpo_call.h"
+#include "dpo_check.h"
 #include "dpo_ffn_few.cuh"
+#include "dpo_products.h"
 
 #include <cuda_runtime.h>
 
@@ -258,9 +259,10 @@ struct Choice {
     Form form;
     double time;
 };
-Choice form_of(const Device &d, const Shape *s, int n, int epi)
+// whole: no split of K (outputs in fp32 or added, A M-contiguous); a_mn: A is M-contiguous, its boxes whole.
+Choice form_of(const Device &d, const Shape *s, int n, int epi, bool whole = false, bool a_mn = false)
 {
-    const int a_rows = s[0].m <= 32 ? 32 : s[0].m <= 64 ? 64 : BM;
+    const int a_rows = a_mn ? BM : s[0].m <= 32 ? 32 : s[0].m <= 64 ? 64 : BM;
     const Form forms[] = {single(n == 1 ? a_rows : BM), thin(1, a_rows, BH), thin(2, a_rows, BH),
                           thin(4, a_rows, BH), thin(8, a_rows, BH), thin(1, a_rows, BH / 2),
                           thin(2, a_rows, BH / 2), thin(4, a_rows, BH / 2),
@@ -278,7 +280,7 @@ Choice form_of(const Device &d, const Shape *s, int n, int epi)
         double work = 0.0, longest = 0.0;
         for (int i = 0; i < n; ++i)
             tiles += tiles_of(s[i], f, epi);
-        if (f.thin && (n > 1 || blocks_of(s[0].k, f.bk()) < 2 * f.ways))
+        if (f.thin && (whole || n > 1 || blocks_of(s[0].k, f.bk()) < 2 * f.ways))
             continue;
         for (int i = 0; i < n; ++i) {
             const int64_t blocks = blocks_of(s[i].k, f.bk()) * s[i].segments;
@@ -402,54 +404,49 @@ int check_sizes(const char *what, int64_t tokens, int64_t dim, int64_t hidden)
     return DPO_OK;
 }
 
-// The buffers of a call, for the checks of pointers, pitches and overlaps.
-struct Buffers {
-    struct Entry {
-        const char *name;
-        Extent at;
-        bool out;
-    };
-    const char *what;
-    Entry e[20];
-    int n = 0, rc = DPO_OK;
-    explicit Buffers(const char *w) : what(w) {}
-    // rows x cols of `size`-byte elements, `align`-byte aligned, its pitch too
-    void add(const char *name, const void *p, int64_t rows, int64_t cols, int64_t ld, int64_t size,
-             int64_t align, bool out)
-    {
-        if (rc != DPO_OK)
-            return;
-        if (p == nullptr)
-            rc = call_fail(DPO_EINVAL, "%s: %s is NULL", what, name);
-        else if (ld < cols)
-            rc = call_fail(DPO_EINVAL, "%s: pitch %lld of %s is below its %lld columns", what,
-                           (long long)ld, name, (long long)cols);
-        else if (ld > ((int64_t)1 << 36))
-            rc = call_fail(DPO_EINVAL, "%s: pitch of %s", what, name);
-        else if (reinterpret_cast<uintptr_t>(p) % align != 0 || ld * size % align != 0)
-            rc = call_fail(DPO_EALIGN, "%s: %s or its pitch is not %lld-byte aligned", what, name,
-                           (long long)align);
-        if (rc != DPO_OK)
-            return;
-        e[n++] = {name, extent_of(p, rows, cols, ld, size), out};
-    }
-    void packed(const char *name, const dpo_packed8 &p, int64_t rows, int64_t cols, int64_t align,
-                bool out)
-    {
-        add(name, p.codes, rows, cols, p.ld_codes, 1, align, out);
-        add("its scales", p.scales, rows, (cols + kGroup - 1) / kGroup, p.ld_scales, 1, 1, out);
-    }
-    int done()
-    {
-        for (int i = 0; i < n && rc == DPO_OK; ++i)
-            for (int j = 0; j < i && rc == DPO_OK; ++j)
-                if ((e[i].out || e[j].out) && overlap(e[i].at, e[j].at))
-                    rc = call_fail(DPO_EINVAL, "%s: %s overlaps %s", what, e[i].name, e[j].name);
-        return rc;
-    }
-};
-
 }  // namespace
+
+int dpo::store_products(const char *what, const StoreProduct *p, int n, void *stream)
+{
+    const Device *d = nullptr;
+    int rc = device_info(what, &d);
+    if (rc != DPO_OK)
+        return rc;
+    Shape s[kMaxProducts];
+    bool whole = n > 1, a_mn = false;
+    for (int i = 0; i < n; ++i) {
+        s[i] = {p[i].m, p[i].n, p[i].k, 1};
+        whole = whole || p[i].f32 || p[i].accumulate || p[i].a_mn;
+        a_mn = a_mn || p[i].a_mn;
+    }
+    const Form f = form_of(*d, s, n, kStore, whole, a_mn).form;
+    Launch L{};
+    Maps m;
+    for (int i = 0; i < n; ++i) {
+        const StoreProduct &q = p[i];
+        Product &P = L.p[i];
+        P.a_mn = q.a_mn;
+        P.b_mn = q.b_mn;
+        if (q.a_mn)
+            m.operand(&P.a[0], q.a, q.k, q.m, q.ld_a, f.bk());
+        else
+            m.operand(&P.a[0], q.a, q.m, q.k, q.ld_a, f.a_rows);
+        if (q.b_mn)
+            m.operand(&P.b[0], q.b, q.k, q.n, q.ld_b, f.bk());
+        else
+            m.operand(&P.b[0], q.b, q.n, q.k, q.ld_b, f.cg == 2 ? BH : f.cols);
+        if (q.f32)
+            m.f32(&P.d0, q.out, q.m, q.n, q.ld_out);
+        else
+            m.bf16(&P.d0, q.out, q.m, q.n, q.ld_out);
+        P.f32 = q.f32;
+        P.accumulate = q.accumulate;
+        P.old = q.out;
+        P.ld_old = P.ld_o = q.ld_out;
+        P.o0 = static_cast<__nv_bfloat16 *>(q.out);
+    }
+    return run(what, *d, L, s, n, kStore, f, false, m.ok, stream);
+}
 
 extern "C" int dpo_ffn_workspace(int64_t tokens, int64_t dim, int64_t hidden, int from_x8,
                                  int64_t *forward_bytes, int64_t *backward_bytes)

@@ -1,0 +1,26 @@
+// dpo_products.h -- products on the tensor cores (dpo_ffn_gemm.cuh) for other calls than the
+// feed-forward block's.
+#pragma once
+
+#include <stdint.h>
+
+namespace dpo {
+
+// out = A B (m x n), or out += A B: bf16 operands, fp32 accumulation. A is m x k row-major, or
+// with a_mn k x m; B is n x k, or with b_mn k x n. Pointers 16-byte aligned, pitches of whole 16
+// bytes, an added out with n a multiple of 8.
+struct StoreProduct {
+    const void *a, *b;
+    void *out;
+    int64_t m, n, k;
+    int64_t ld_a, ld_b, ld_out;
+    int a_mn, b_mn;
+    int f32, accumulate;
+};
+
+constexpr int kMaxStoreProducts = 4;
+
+// Up to four of them in one launch, in whose order their tiles are begun (longest first).
+int store_products(const char *what, const StoreProduct *p, int n, void *stream);
+
+}  // namespace dpo

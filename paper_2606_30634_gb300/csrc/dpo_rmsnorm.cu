@@ -5,8 +5,9 @@
 // All four move bytes: a few operations per element against 2 to 9 bytes of it,
 // so HBM bounds them, and launch latency where there are few rows.
 #include "dpo.h"
-#include "dpo_call.h"
+#include "dpo_check.h"
 #include "dpo_pack8.cuh"
+#include "dpo_vec.cuh"
 
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -15,117 +16,6 @@
 
 namespace dpo {
 namespace {
-
-// ------------------------------------------------------------- vectors ----
-// V elements as one access of at most 16 bytes (codes: V bytes).
-
-template <int B> struct Bytes;
-template <> struct Bytes<1> {
-    static __device__ __forceinline__ void ld(const void *p, uint32_t (&w)[1])
-    {
-        uint16_t v;
-        asm volatile("ld.global.u8 %0, [%1];" : "=h"(v) : "l"(p));
-        w[0] = v;
-    }
-    static __device__ __forceinline__ void st(void *p, const uint32_t (&w)[1])
-    {
-        *static_cast<uint8_t *>(p) = (uint8_t)w[0];
-    }
-};
-template <> struct Bytes<2> {
-    static __device__ __forceinline__ void ld(const void *p, uint32_t (&w)[1])
-    {
-        uint16_t v;
-        asm volatile("ld.global.b16 %0, [%1];" : "=h"(v) : "l"(p));
-        w[0] = v;
-    }
-    static __device__ __forceinline__ void st(void *p, const uint32_t (&w)[1])
-    {
-        *static_cast<uint16_t *>(p) = (uint16_t)w[0];
-    }
-};
-template <> struct Bytes<4> {
-    static __device__ __forceinline__ void ld(const void *p, uint32_t (&w)[1])
-    {
-        asm volatile("ld.global.b32 %0, [%1];" : "=r"(w[0]) : "l"(p));
-    }
-    static __device__ __forceinline__ void st(void *p, const uint32_t (&w)[1])
-    {
-        *static_cast<uint32_t *>(p) = w[0];
-    }
-};
-template <> struct Bytes<8> {
-    static __device__ __forceinline__ void ld(const void *p, uint32_t (&w)[2])
-    {
-        asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
-    }
-    static __device__ __forceinline__ void st(void *p, const uint32_t (&w)[2])
-    {
-        *static_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
-    }
-};
-template <> struct Bytes<16> {
-    static __device__ __forceinline__ void ld(const void *p, uint32_t (&w)[4])
-    {
-        asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                     : "l"(p));
-    }
-    static __device__ __forceinline__ void st(void *p, const uint32_t (&w)[4])
-    {
-        *static_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-};
-
-__host__ __device__ constexpr int words(int bytes) { return bytes < 4 ? 1 : bytes / 4; }
-
-// V elements of T as loaded.
-template <class T, int V> struct Vec;
-template <int V> struct Vec<float, V> {
-    static constexpr int B = 4 * V;
-    uint32_t w[V];
-    __device__ __forceinline__ void load(const float *p) { Bytes<B>::ld(p, w); }
-    __device__ __forceinline__ float get(int i) const { return __uint_as_float(w[i]); }
-    __device__ __forceinline__ void zero()
-    {
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            w[i] = 0u;
-    }
-    __device__ __forceinline__ void set(const float (&v)[V])
-    {
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            w[i] = __float_as_uint(v[i]);
-    }
-    __device__ __forceinline__ void store(float *p) const { Bytes<B>::st(p, w); }
-};
-template <int V> struct Vec<__nv_bfloat16, V> {
-    static constexpr int B = 2 * V;
-    uint32_t w[words(B)];
-    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { Bytes<B>::ld(p, w); }
-    __device__ __forceinline__ float get(int i) const
-    {
-        return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
-    }
-    __device__ __forceinline__ void zero()
-    {
-#pragma unroll
-        for (int i = 0; i < words(B); ++i)
-            w[i] = 0u;
-    }
-    __device__ __forceinline__ void set(const float (&v)[V])
-    {
-        if (V == 1) {
-            w[0] = pack_bf16x2(v[0], 0.0f);
-        } else {
-#pragma unroll
-            for (int i = 0; i < V / 2; ++i)
-                w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
-        }
-    }
-    __device__ __forceinline__ void store(__nv_bfloat16 *p) const { Bytes<B>::st(p, w); }
-};
 
 // V codes.
 template <int V> struct Codes {
@@ -775,26 +665,6 @@ pack8_kernel(const PackArgs a)
 
 // ---------------------------------------------------------------- host ----
 
-int64_t elem_size(int dt) { return dt == DPO_BF16 ? 2 : 4; }
-bool known(int dt) { return dt == DPO_F32 || dt == DPO_BF16; }
-
-// Whether a matrix can be accessed V elements of `size` bytes at a time.
-bool whole(const void *p, int64_t ld, int64_t size, int v)
-{
-    return p == nullptr || (reinterpret_cast<uintptr_t>(p) % (size * v) == 0 && ld % v == 0);
-}
-
-bool aligned_to(const void *p, int64_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
-
-int sm_count()
-{
-    int device = 0, sms = 0;
-    if (cudaGetDevice(&device) != cudaSuccess ||
-        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)
-        return 0;
-    return sms;
-}
-
 // Warps of a row with so many elements a thread.
 int row_warps(int64_t cols, int elems)
 {
@@ -824,15 +694,6 @@ BackShape back_shape(int64_t rows, int64_t cols, int sms)
     return b;
 }
 
-template <class... P, class... A>
-int launch(const char *what, void (*kernel)(P...), int64_t grid, int threads, size_t smem,
-           void *stream, A &&...args)
-{
-    const cudaError_t e = launch_pdl(kernel, dim3((unsigned)grid), threads, smem,
-                                     static_cast<cudaStream_t>(stream), static_cast<A &&>(args)...);
-    return e == cudaSuccess ? DPO_OK : call_fail(DPO_ECUDA, "%s: %s", what, cudaGetErrorString(e));
-}
-
 int check_packed(const char *what, const dpo_packed8 &p, int64_t cols)
 {
     if (p.codes == nullptr || p.scales == nullptr)
@@ -844,19 +705,6 @@ int check_packed(const char *what, const dpo_packed8 &p, int64_t cols)
 
 constexpr int64_t kMaxRows = (int64_t)1 << 31;
 constexpr int kMaxSmem = 226 * 1024;   // dynamic, beside the kernel's own 256 bytes
-
-int check_matrix(const char *what, const char *name, const void *p, int64_t cols, int64_t ld,
-                 int64_t size)
-{
-    if (p == nullptr)
-        return call_fail(DPO_EINVAL, "%s: %s is NULL", what, name);
-    if (ld < cols)
-        return call_fail(DPO_EINVAL, "%s: pitch %lld of %s is below its %lld columns", what,
-                         (long long)ld, name, (long long)cols);
-    if (!aligned_to(p, size))
-        return call_fail(DPO_EALIGN, "%s: %s is not aligned to its elements", what, name);
-    return DPO_OK;
-}
 
 template <class T, bool Unpack>
 auto pack_kernel(int v) -> void (*)(PackArgs)

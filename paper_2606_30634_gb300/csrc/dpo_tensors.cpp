@@ -1,6 +1,7 @@
-// dpo_tensors.cpp -- the feed-forward calls of include/dpo.h on PyTorch tensors: the
-// part of ffn.py between its signatures and the C ABI (checks, pitches, outputs and
-// workspaces from PyTorch's allocator, the current stream), as a Python module.
+// dpo_tensors.cpp -- the feed-forward calls of include/dpo.h and those of
+// include/dpo_ends.h on PyTorch tensors: the part of ffn.py and ends.py between their
+// signatures and the C ABI (checks, pitches, outputs and workspaces from PyTorch's
+// allocator, the current stream), as a Python module.
 //
 // A small call is as long as its host side: the norm of one row takes 4 us on the GPU, and
 // the same checks, three allocations and a ctypes call took 17 us in Python.
@@ -21,6 +22,7 @@
 #include <string>
 
 #include "dpo.h"
+#include "dpo_ends.h"
 
 namespace {
 
@@ -37,6 +39,15 @@ struct Library {
     decltype(&dpo_ffn_forward) ffn_forward = nullptr;
     decltype(&dpo_ffn_backward) ffn_backward = nullptr;
     decltype(&dpo_ffn_workspace) ffn_workspace = nullptr;
+    decltype(&dpo_embed) embed = nullptr;
+    decltype(&dpo_embed_backward) embed_backward = nullptr;
+    decltype(&dpo_embed_workspace) embed_workspace = nullptr;
+    decltype(&dpo_dropout) dropout = nullptr;
+    decltype(&dpo_logprobs) logprobs = nullptr;
+    decltype(&dpo_logprobs_backward) logprobs_backward = nullptr;
+    decltype(&dpo_head) head = nullptr;
+    decltype(&dpo_head_backward) head_backward = nullptr;
+    decltype(&dpo_head_workspace) head_workspace = nullptr;
     decltype(&dpo_last_error) last_error = nullptr;
     PyObject *error = nullptr;   // DpoError
 };
@@ -570,13 +581,408 @@ PyObject *gated_ffn_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// Ids of the leading dimensions of a tensor: int32 or int64, rows as rows_of's.
+dpo_ids ids_of(const Tensor &t, at::Device device)
+{
+    if (t.scalar_type() != at::kLong && t.scalar_type() != at::kInt)
+        type_error(std::string("ids: ") + toString(t.scalar_type()) + " (int32 or int64)");
+    on_device(t, device, "ids");
+    if (t.dim() == 0)
+        return {t.data_ptr(), 1, 1, 1, t.scalar_type() == at::kLong ? 8 : 4};
+    const Mat m = rows_of(t, "ids");
+    return {m.p, m.rows, m.cols, m.ld, t.scalar_type() == at::kLong ? 8 : 4};
+}
+
+c10::DimVector with_last(at::IntArrayRef lead, int64_t last)
+{
+    c10::DimVector s(lead.begin(), lead.end());
+    s.push_back(last);
+    return s;
+}
+c10::IntArrayRef lead_of(const Tensor &t) { return t.sizes().slice(0, t.dim() - 1); }
+
+void same_lead(const Tensor &ids, const Tensor &x, const char *name)
+{
+    if (x.dim() < 1 || ids.sizes() != lead_of(x))
+        value_error("ids: shape " + shape(ids.sizes()) + ", expected the leading dimensions of " + name + " " +
+                    shape(x.sizes()));
+}
+
+double number(PyObject *o)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) {
+        PyErr_Clear();
+        type_error("a number is needed");
+    }
+    return v;
+}
+
+// A float32 value for each row of x, contiguous.
+const float *per_row(PyObject *o, const Tensor &x, at::Device device, const char *name)
+{
+    const Tensor &t = tensor(o, name);
+    fits(t, at::kFloat, lead_of(x), device, name);
+    if (!t.is_contiguous())
+        value_error(std::string(name) + " is not contiguous");
+    return static_cast<const float *>(t.data_ptr());
+}
+
+// embed(ids, table, scale, bf16 (-1: the table's type), out or None) -> out
+PyObject *embed(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!expect(n, 5))
+        return nullptr;
+    return guarded([&] {
+        const Tensor &ids = tensor(a[0], "ids"), &table = tensor(a[1], "table");
+        if (table.dim() != 2)
+            value_error("table: expected a matrix");
+        const Mat m = rows_of(table, "table");
+        const at::Device device = table.device();
+        void *const s = stream_of(table, "table");
+        dpo_embed_args k{};
+        k.ids = ids_of(ids, device);
+        k.table = m.p;
+        k.vocab = m.rows;
+        k.dim = m.cols;
+        k.ld_table = m.ld;
+        k.table_dtype = dtype_of(table, "table");
+        k.scale = (float)number(a[2]);
+        const int bf16 = integer(a[3]);
+        const c10::DimVector size = with_last(ids.sizes(), m.cols);
+        Tensor out;
+        if (a[4] == Py_None) {
+            out = make(size, bf16 < 0 ? table.scalar_type() : bf16 ? at::kBFloat16 : at::kFloat, device);
+        } else {
+            out = tensor(a[4], "out");
+            fits(out, out.scalar_type(), size, device, "out");
+        }
+        const Mat o = rows_of(out, "out");
+        k.out = o.p;
+        k.ld_out = o.ld;
+        k.out_dtype = dtype_of(out, "out");
+        check(g_lib.embed(&k, s));
+        return wrap(out);
+    });
+}
+
+// embed_backward(dy, ids, dtable, scale, accumulate) -> dtable
+PyObject *embed_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!expect(n, 5))
+        return nullptr;
+    return guarded([&] {
+        const Tensor &dy = tensor(a[0], "dy"), &ids = tensor(a[1], "ids"), &dt = tensor(a[2], "dtable");
+        const Mat m = rows_of(dy, "dy");
+        const at::Device device = dy.device();
+        void *const s = stream_of(dy, "dy");
+        same_lead(ids, dy, "dy");
+        if (dt.dim() != 2 || dt.size(1) != m.cols)
+            value_error("dtable: expected a matrix with " + std::to_string(m.cols) + " columns, got " +
+                        shape(dt.sizes()));
+        on_device(dt, device, "dtable");
+        const Mat t = rows_of(dt, "dtable");
+        dpo_embed_backward_args k{};
+        k.dy = m.p;
+        k.ld_dy = m.ld;
+        k.dtype = dtype_of(dy, "dy");
+        k.ids = ids_of(ids, device);
+        k.dtable = t.p;
+        k.vocab = t.rows;
+        k.dim = m.cols;
+        k.ld_dtable = t.ld;
+        k.grad_dtype = dtype_of(dt, "dtable");
+        k.scale = (float)number(a[3]);
+        k.accumulate = integer(a[4]);
+        check(g_lib.embed_workspace(m.rows, k.vocab, k.dim, &k.workspace_bytes));
+        const Tensor ws = make({k.workspace_bytes}, at::kByte, device);
+        k.workspace = ws.data_ptr();
+        check(g_lib.embed_backward(&k, s));
+        return wrap(dt);
+    });
+}
+
+// dropout(x, residual or None, p, seed (int or tensor), site, out or None) -> y
+PyObject *dropout(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!expect(n, 6))
+        return nullptr;
+    return guarded([&] {
+        const Tensor &x = tensor(a[0], "x");
+        const Mat m = rows_of(x, "x");
+        const at::Device device = x.device();
+        void *const s = stream_of(x, "x");
+        dpo_dropout_args k{};
+        k.x = m.p;
+        k.rows = m.rows;
+        k.cols = m.cols;
+        k.ld_x = m.ld;
+        k.dtype = dtype_of(x, "x");
+        if (a[1] != Py_None) {
+            const Tensor &r = tensor(a[1], "residual");
+            fits(r, x.scalar_type(), x.sizes(), device, "residual");
+            const Mat rm = rows_of(r, "residual");
+            k.residual = rm.p;
+            k.ld_residual = rm.ld;
+        }
+        k.p = number(a[2]);
+        if (THPVariable_Check(a[3])) {
+            const Tensor &seed = tensor(a[3], "seed");
+            if (seed.scalar_type() != at::kLong || seed.numel() != 1)
+                type_error("seed: an integer or an int64 tensor of one element is needed");
+            on_device(seed, device, "seed");
+            k.seed_source = static_cast<const uint64_t *>(seed.data_ptr());
+        } else {
+            k.seed = PyLong_AsUnsignedLongLongMask(a[3]);
+            if (k.seed == (uint64_t)-1 && PyErr_Occurred()) {
+                PyErr_Clear();
+                type_error("seed: an integer or an int64 tensor of one element is needed");
+            }
+        }
+        const unsigned long long site = PyLong_AsUnsignedLongLong(a[4]);
+        if (PyErr_Occurred() || site > 0xFFFFFFFFull) {
+            PyErr_Clear();
+            value_error("site: an integer from 0 to 2^32 - 1 is needed");
+        }
+        k.site = (uint32_t)site;
+        Tensor y;
+        if (a[5] == Py_None) {
+            y = make(x.sizes(), x.scalar_type(), device);
+        } else {
+            y = tensor(a[5], "out");
+            fits(y, x.scalar_type(), x.sizes(), device, "out");
+        }
+        const Mat o = rows_of(y, "out");
+        k.y = o.p;
+        k.ld_y = o.ld;
+        check(g_lib.dropout(&k, s));
+        return wrap(y);
+    });
+}
+
+// What the log probabilities of rows come in.
+struct LogOut {
+    Tensor logp, entropy, stats, top_logp, top_ids;
+    LogOut(at::IntArrayRef lead, bool ids, int top, at::Device device)
+    {
+        if (ids)
+            logp = make(lead, at::kFloat, device);
+        entropy = make(lead, at::kFloat, device);
+        stats = make(with_last(lead, 2), at::kFloat, device);
+        if (top > 0) {
+            top_logp = make(with_last(lead, top), at::kFloat, device);
+            top_ids = make(with_last(lead, top), at::kLong, device);
+        }
+    }
+    template <class A> void into(A &k) const
+    {
+        auto p = [](const Tensor &t) { return t.defined() ? static_cast<float *>(t.data_ptr()) : nullptr; };
+        k.logp = p(logp);
+        k.entropy = p(entropy);
+        k.stats = p(stats);
+        k.top_logp = p(top_logp);
+        k.top_ids = top_ids.defined() ? static_cast<int64_t *>(top_ids.data_ptr()) : nullptr;
+    }
+};
+
+int top_of(PyObject *o)
+{
+    const int top = integer(o);
+    if (top < 0 || top > DPO_MAX_TOP)
+        value_error("top: 0 to " + std::to_string(DPO_MAX_TOP));
+    return top;
+}
+
+// token_logprobs(logits, ids or None, scale, top) -> logp, entropy, stats, top_logp, top_ids
+PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!expect(n, 4))
+        return nullptr;
+    return guarded([&] {
+        const Tensor &x = tensor(a[0], "logits");
+        const Mat m = rows_of(x, "logits");
+        const at::Device device = x.device();
+        void *const s = stream_of(x, "logits");
+        dpo_logprobs_args k{};
+        if (a[1] != Py_None) {
+            const Tensor &ids = tensor(a[1], "ids");
+            same_lead(ids, x, "logits");
+            k.ids = ids_of(ids, device);
+        }
+        k.logits = m.p;
+        k.rows = m.rows;
+        k.vocab = m.cols;
+        k.ld_logits = m.ld;
+        k.dtype = dtype_of(x, "logits");
+        k.scale = (float)number(a[2]);
+        k.top = top_of(a[3]);
+        const LogOut out(lead_of(x), a[1] != Py_None, k.top, device);
+        out.into(k);
+        check(g_lib.logprobs(&k, s));
+        return tuple(out.logp, out.entropy, out.stats, out.top_logp, out.top_ids);
+    });
+}
+
+// token_logprobs_backward(dlogp, logits, ids, stats, entropy, dentropy or None, scale,
+//                         dlogits or None) -> dlogits
+PyObject *token_logprobs_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!expect(n, 8))
+        return nullptr;
+    return guarded([&] {
+        const Tensor &x = tensor(a[1], "logits"), &ids = tensor(a[2], "ids"), &st = tensor(a[3], "stats");
+        const Mat m = rows_of(x, "logits");
+        const at::Device device = x.device();
+        void *const s = stream_of(x, "logits");
+        same_lead(ids, x, "logits");
+        dpo_logprobs_backward_args k{};
+        k.ids = ids_of(ids, device);
+        fits(st, at::kFloat, with_last(lead_of(x), 2), device, "stats");
+        if (!st.is_contiguous())
+            value_error("stats is not contiguous");
+        k.stats = static_cast<const float *>(st.data_ptr());
+        k.dlogp = per_row(a[0], x, device, "dlogp");
+        if (a[5] != Py_None) {
+            k.entropy = per_row(a[4], x, device, "entropy");
+            k.dentropy = per_row(a[5], x, device, "dentropy");
+        }
+        k.scale = (float)number(a[6]);
+        Tensor d;
+        if (a[7] == Py_None) {
+            d = make(x.sizes(), x.scalar_type(), device);
+        } else {
+            d = tensor(a[7], "dlogits");
+            fits(d, x.scalar_type(), x.sizes(), device, "dlogits");
+        }
+        const Mat o = rows_of(d, "dlogits");
+        k.logits = m.p;
+        k.rows = m.rows;
+        k.vocab = m.cols;
+        k.ld_logits = m.ld;
+        k.dtype = dtype_of(x, "logits");
+        k.dlogits = o.p;
+        k.ld_dlogits = o.ld;
+        check(g_lib.logprobs_backward(&k, s));
+        return wrap(d);
+    });
+}
+
+// head_logprobs(x, w, ids or None, scale, top, keep)
+//     -> logp, entropy, stats, top_logp, top_ids, kept
+PyObject *head_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!expect(n, 6))
+        return nullptr;
+    return guarded([&] {
+        const Tensor &x = tensor(a[0], "x"), &w = tensor(a[1], "w");
+        const Mat m = rows_of(x, "x");
+        if (x.scalar_type() != at::kBFloat16)
+            type_error(std::string("x: ") + toString(x.scalar_type()) + " (bfloat16)");
+        const at::Device device = x.device();
+        void *const s = stream_of(x, "x");
+        if (w.dim() != 2)
+            value_error("w: expected a matrix");
+        dpo_head_args k{};
+        k.tokens = m.rows;
+        k.dim = m.cols;
+        k.vocab = w.size(0);
+        k.w = weight_of(w, k.vocab, k.dim, device, "w");
+        if (a[2] != Py_None) {
+            const Tensor &ids = tensor(a[2], "ids");
+            same_lead(ids, x, "x");
+            k.ids = ids_of(ids, device);
+        }
+        k.x = m.p;
+        k.ld_x = m.ld;
+        k.scale = (float)number(a[3]);
+        k.top = top_of(a[4]);
+        const int keep = integer(a[5]);
+        int64_t kept_bytes = 0;
+        check(g_lib.head_workspace(k.tokens, k.dim, k.vocab, keep, k.top, &k.workspace_bytes, &kept_bytes,
+                                   nullptr));
+        const LogOut out(lead_of(x), a[2] != Py_None, k.top, device);
+        out.into(k);
+        Tensor kept, ws;
+        if (keep) {
+            kept = make({kept_bytes}, at::kByte, device);
+            k.kept = kept.data_ptr();
+        }
+        if (k.workspace_bytes > 0) {
+            ws = make({k.workspace_bytes}, at::kByte, device);
+            k.workspace = ws.data_ptr();
+        }
+        check(g_lib.head(&k, s));
+        return tuple(out.logp, out.entropy, out.stats, out.top_logp, out.top_ids, kept);
+    });
+}
+
+// head_logprobs_backward(dlogp, kept, x, w, ids, logp, entropy, stats, dw, dentropy or None,
+//                        scale, accumulate, dx or None) -> dx
+PyObject *head_logprobs_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!expect(n, 13))
+        return nullptr;
+    return guarded([&] {
+        const Tensor &x = tensor(a[2], "x"), &w = tensor(a[3], "w"), &ids = tensor(a[4], "ids"),
+                     &kept = tensor(a[1], "kept"), &st = tensor(a[7], "stats"), &dw = tensor(a[8], "dw");
+        const Mat m = rows_of(x, "x");
+        if (x.scalar_type() != at::kBFloat16)
+            type_error(std::string("x: ") + toString(x.scalar_type()) + " (bfloat16)");
+        const at::Device device = x.device();
+        void *const s = stream_of(x, "x");
+        if (w.dim() != 2)
+            value_error("w: expected a matrix");
+        dpo_head_backward_args k{};
+        k.tokens = m.rows;
+        k.dim = m.cols;
+        k.vocab = w.size(0);
+        k.w = weight_of(w, k.vocab, k.dim, device, "w");
+        k.grad_dtype = dtype_of(dw, "dw");
+        k.dw = matrix_of(dw, k.vocab, k.dim, dw.scalar_type(), device, "dw");
+        same_lead(ids, x, "x");
+        k.ids = ids_of(ids, device);
+        k.dlogp = per_row(a[0], x, device, "dlogp");
+        k.logp = per_row(a[5], x, device, "logp");
+        k.entropy = per_row(a[6], x, device, "entropy");
+        fits(st, at::kFloat, with_last(lead_of(x), 2), device, "stats");
+        if (!st.is_contiguous())
+            value_error("stats is not contiguous");
+        k.stats = static_cast<const float *>(st.data_ptr());
+        if (a[9] != Py_None)
+            k.dentropy = per_row(a[9], x, device, "dentropy");
+        k.scale = (float)number(a[10]);
+        k.accumulate = integer(a[11]);
+        int64_t kept_bytes = 0;
+        check(g_lib.head_workspace(k.tokens, k.dim, k.vocab, 1, 0, nullptr, &kept_bytes, &k.workspace_bytes));
+        fits(kept, at::kByte, {kept_bytes}, device, "kept");
+        k.kept = kept.data_ptr();
+        Tensor dx;
+        if (a[12] == Py_None) {
+            dx = make(x.sizes(), at::kBFloat16, device);
+        } else {
+            dx = tensor(a[12], "dx");
+            fits(dx, at::kBFloat16, x.sizes(), device, "dx");
+        }
+        const Mat xo = rows_of(dx, "dx");
+        const Tensor ws = make({k.workspace_bytes}, at::kByte, device);
+        k.workspace = ws.data_ptr();
+        k.x = m.p;
+        k.ld_x = m.ld;
+        k.dx = xo.p;
+        k.ld_dx = xo.ld;
+        check(g_lib.head_backward(&k, s));
+        return wrap(dx);
+    });
+}
+
 // bind(DpoError, addresses in the order of Library)
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    if (!expect(n, 10))
+    constexpr int kCalls = 18;
+    if (!expect(n, kCalls + 1))
         return nullptr;
-    void *p[9];
-    for (int i = 0; i < 9; ++i) {
+    void *p[kCalls];
+    for (int i = 0; i < kCalls; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i + 1]);
         if (p[i] == nullptr) {
             if (!PyErr_Occurred())
@@ -593,7 +999,16 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
     l.ffn_forward = (decltype(l.ffn_forward))p[5];
     l.ffn_backward = (decltype(l.ffn_backward))p[6];
     l.ffn_workspace = (decltype(l.ffn_workspace))p[7];
-    l.last_error = (decltype(l.last_error))p[8];
+    l.embed = (decltype(l.embed))p[8];
+    l.embed_backward = (decltype(l.embed_backward))p[9];
+    l.embed_workspace = (decltype(l.embed_workspace))p[10];
+    l.dropout = (decltype(l.dropout))p[11];
+    l.logprobs = (decltype(l.logprobs))p[12];
+    l.logprobs_backward = (decltype(l.logprobs_backward))p[13];
+    l.head = (decltype(l.head))p[14];
+    l.head_backward = (decltype(l.head_backward))p[15];
+    l.head_workspace = (decltype(l.head_workspace))p[16];
+    l.last_error = (decltype(l.last_error))p[17];
     Py_INCREF(a[0]);
     Py_XDECREF(g_lib.error);
     l.error = a[0];
@@ -605,6 +1020,10 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 PyMethodDef g_methods[] = {FAST(bind),        FAST(pack8),     FAST(unpack8),
                            FAST(add_rms_norm), FAST(add_rms_norm_backward),
                            FAST(gated_ffn),   FAST(gated_ffn_backward),
+                           FAST(embed),       FAST(embed_backward),
+                           FAST(dropout),     FAST(token_logprobs),
+                           FAST(token_logprobs_backward),
+                           FAST(head_logprobs), FAST(head_logprobs_backward),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "dpo_tensors", nullptr, -1, g_methods,
                         nullptr, nullptr, nullptr, nullptr};

@@ -44,6 +44,8 @@ KEEP = {"none": DPO_KEEP_NONE, "8bit": DPO_KEEP_8BIT, "bf16": DPO_KEEP_BF16}
 # What dpo_tensors calls, in the order of its bind().
 _CALLS = ("dpo_pack8", "dpo_unpack8", "dpo_rmsnorm", "dpo_rmsnorm_backward",
           "dpo_rmsnorm_workspace", "dpo_ffn_forward", "dpo_ffn_backward", "dpo_ffn_workspace",
+          "dpo_embed", "dpo_embed_backward", "dpo_embed_workspace", "dpo_dropout", "dpo_logprobs",
+          "dpo_logprobs_backward", "dpo_head", "dpo_head_backward", "dpo_head_workspace",
           "dpo_last_error")
 
 
