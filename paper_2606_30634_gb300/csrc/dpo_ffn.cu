@@ -41,7 +41,7 @@ using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t,
                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 using KernelFn = void (*)(const Launch);
-constexpr int kForms = 4;   // epilogues
+constexpr int kForms = 5;   // epilogues
 
 // What the launches need to know of a device, found by its first call.
 struct Device {
@@ -79,6 +79,9 @@ int slots_of(const Device &d, Form f, int epi)
 
 template <int CG, bool SPLIT> KernelFn kernel_of(int epi)
 {
+    if constexpr (!SPLIT)
+        if (epi == kHead)
+            return ffn_gemm_kernel<CG, kHead, SPLIT>;
     return epi == kGate         ? ffn_gemm_kernel<CG, kGate, SPLIT>
            : epi == kGateBack8  ? ffn_gemm_kernel<CG, kGateBack8, SPLIT>
            : epi == kGateBack16 ? ffn_gemm_kernel<CG, kGateBack16, SPLIT>
@@ -137,6 +140,8 @@ cudaError_t prepare(Device &d)
     for (const Form f : {kPairs, single(BM), thin(1, BM, BH), thin(2, BM, BH), thin(4, BM, BH),
                          thin(8, BM, BH)})
         for (int epi = 0; epi < kForms; ++epi) {
+            if (f.thin && epi == kHead)   // K is not split there
+                continue;
             const void *k = reinterpret_cast<const void *>(kernel_of(f, epi));
             cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                  kMaxSmem);
@@ -446,6 +451,28 @@ int dpo::store_products(const char *what, const StoreProduct *p, int n, void *st
         P.o0 = static_cast<__nv_bfloat16 *>(q.out);
     }
     return run(what, *d, L, s, n, kStore, f, false, m.ok, stream);
+}
+
+int dpo::head_product(const char *what, const HeadProduct &h, void *stream)
+{
+    const Device *d = nullptr;
+    int rc = device_info(what, &d);
+    if (rc != DPO_OK)
+        return rc;
+    const Shape s = {h.tokens, h.vocab, h.dim, 1};
+    const Form f = form_of(*d, &s, 1, kHead, true).form;
+    Launch L{};
+    Maps m;
+    Product &P = L.p[0];
+    m.operand(&P.a[0], h.x, h.tokens, h.dim, h.ld_x, f.a_rows);
+    m.operand(&P.b[0], h.w, h.vocab, h.dim, h.dim, f.cg == 2 ? BH : f.cols);
+    if (h.kept != nullptr)
+        m.bf16(&P.d0, h.kept, h.tokens, h.vocab, h.ld);
+    if (h.logits != nullptr)
+        m.f32(&P.d1, h.logits, h.tokens, h.vocab, h.ld);
+    P.head = {h.ids, h.scale, h.target, h.maxima, h.sums, h.tokens, h.maxima != nullptr, h.kept != nullptr,
+              h.logits != nullptr};
+    return run(what, *d, L, &s, 1, kHead, f, false, m.ok, stream);
 }
 
 extern "C" int dpo_ffn_workspace(int64_t tokens, int64_t dim, int64_t hidden, int from_x8,

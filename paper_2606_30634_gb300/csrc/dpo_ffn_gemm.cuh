@@ -28,10 +28,15 @@
 //              bf16), writes dG, dU and A
 //   kStore     writes D in bf16 or fp32, with factors along the columns and the old
 //              contents added where asked for
+//   kHead      the tile is of a head's logits; leaves each row's maximum, sum and entropy sum
+//              over 128 columns, and what the backward keeps (dpo_head.cu)
 #pragma once
 
 #include "dpo_gemm.cuh"
+#include "dpo_ids.cuh"
 #include "dpo_pack8.cuh"
+
+#include <cuda_fp16.h>
 
 namespace dpo {
 namespace ffn {
@@ -57,7 +62,7 @@ using gemm::smem_desc;
 using gemm::swz64;
 using gemm::tmem_ld32;
 
-enum Epilogue { kGate = 0, kGateBack8 = 1, kGateBack16 = 2, kStore = 3 };
+enum Epilogue { kGate = 0, kGateBack8 = 1, kGateBack16 = 2, kStore = 3, kHead = 4 };
 __host__ __device__ constexpr bool gate_back(int epi)
 {
     return epi == kGateBack8 || epi == kGateBack16;
@@ -101,6 +106,24 @@ static_assert(Ring<false>::stages(BM, BH) == 3, "stages");
 constexpr int kMaxProducts = 4;
 constexpr int kBandRows = 16;   // block rows per band, as in dpo_gemm.cuh
 
+// kHead: columns of which a row's sums are formed, and K blocks of an accumulation. The tensor
+// cores cut a sum to the accumulator's bits at each of their steps, toward zero, so its error grows with K:
+// over 4096 it is 9e-6 of logits of size 2 and 1.4e-6 of log probabilities. The epilogue adds up
+// accumulations of 1024 in registers, rounding to nearest: 2e-6 and 3.3e-7.
+constexpr int kHeadCols = 128, kHeadPart = 8;
+// What is kept of e^(z - m), in fp16: times 2^15, so that values down to 2^-29 keep 11 bits.
+constexpr float kHeadUnit = 32768.0f;
+
+struct HeadOut {
+    Ids ids;                      // p nullptr: none
+    float scale;                  // of the accumulator: z
+    float *target;                // z of each row's id
+    float *maxima;                // [kHeadCols columns][row]
+    float2 *sums;                 // likewise: sum of e^(z - m), of e^(z - m) (z - m)
+    int64_t rows;                 // pitch of the two
+    int stats, keep, logits;      // sums are wanted; d0 of the kept values; d1 of z / scale in fp32
+};
+
 // One product of a launch.
 struct Product {
     CUtensorMap a[2], b[2];       // operands per segment (kGate: b[0] w_gate, b[1] w_up)
@@ -128,6 +151,7 @@ struct Product {
     int64_t ld_o;
     uint8_t *codes_g, *codes_u;
     int64_t ld_codes_g, ld_codes_u;
+    HeadOut head;
 };
 
 struct Launch {
@@ -637,6 +661,75 @@ __device__ __forceinline__ void drain(const Product &P, Stager &st, Kept<EPI == 
     }
 }
 
+// 32 rows, one a lane, and 128 columns of a head's logits.
+__device__ __forceinline__ void head_rows(const Product &P, Stager &st, float (&v)[kHeadCols], int id,
+                                          int row0, int col0)
+{
+    const HeadOut &H = P.head;
+    const int row = row0 + st.lane;
+    const bool in = row < P.m;
+    if (H.logits)
+#pragma unroll
+        for (int c = 0; c < kHeadCols; c += 32) {
+            float w[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                w[j] = v[c + j];
+            if (col0 + c < P.n)
+                st.f32(&P.d1, w, col0 + c, row0);
+        }
+    if (!H.stats)
+        return;
+#pragma unroll
+    for (int j = 0; j < kHeadCols; ++j)
+        v[j] = __fmul_rn(v[j], H.scale);
+    if (col0 + kHeadCols > P.n)
+#pragma unroll
+        for (int j = 0; j < kHeadCols; ++j)
+            v[j] = col0 + j < P.n ? v[j] : -INFINITY;
+    const int at = id - col0;
+    const bool mine = in && id >= 0 && at >= 0 && at < kHeadCols;
+    if (__any_sync(0xFFFFFFFFu, mine)) {
+        float z = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kHeadCols; ++j)
+            z = at == j ? v[j] : z;
+        if (mine)
+            H.target[row] = z;
+    }
+    float m[2] = {v[0], v[1]};   // fmaxf passes over NaN, which then reaches the sum
+#pragma unroll
+    for (int j = 2; j < kHeadCols; ++j)
+        m[j & 1] = fmaxf(m[j & 1], v[j]);
+    const float top = fmaxf(m[0], m[1]);
+    const float from = top == -INFINITY ? 0.0f : top;
+    float s[2] = {}, w[2] = {};
+#pragma unroll
+    for (int c = 0; c < kHeadCols; c += 32) {
+        uint32_t e2[16];
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+            float e[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float d = v[c + j + k] - from;
+                e[k] = exp2(d * 1.4426950408889634f);
+                s[k] += e[k];
+                w[k] = fmaf(fmaxf(d, -1e30f), e[k], w[k]);   // no infinity times 0
+            }
+            const __half2 h = __floats2half2_rn(e[0] * kHeadUnit, e[1] * kHeadUnit);
+            e2[j / 2] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+        if (H.keep && col0 + c < P.n)
+            st.bf16(&P.d0, e2, col0 + c, row0);   // two bytes an element, whatever they mean
+    }
+    if (in) {
+        const int64_t i = col0 / kHeadCols * H.rows + row;
+        H.maxima[i] = top;
+        H.sums[i] = make_float2(s[0] + s[1], w[0] + w[1]);
+    }
+}
+
 // ---- split K ----
 // Warp w of each of the S CTAs holds its K share's sums of the same 32 rows, in two
 // chunks of 32 columns. Rank j finishes rows 32/S j .. of them: each lane sends its row
@@ -999,7 +1092,8 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(acc_full(a), 1);
-            mbar_init(acc_empty(a), CG * kEpiWarps);
+            // kHead on single CTAs: four warps, each 128 columns, take every tile
+            mbar_init(acc_empty(a), EPI == kHead && CG == 1 ? kEpiWarps / 2 : CG * kEpiWarps);
         }
         if (SPLIT)
             for (int w = 0; w < kEpiWarps; ++w) {
@@ -1108,7 +1202,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
     } else if (warp == 1) {
         if (leader) {
             const bool one = elect();
-            int lt = 0, s = 0;
+            int lt = 0, s = 0, visit = 0;
             uint32_t ph = 0;
             bool ok = true;
             for (int t; ok && (t = turn_of(lt, pair, n_pairs)) < n_tiles; ++lt) {
@@ -1120,42 +1214,47 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                 const bool a_mn = P.a_mn, b_mn = P.b_mn;
                 const uint32_t idesc = idesc_of(CG, cols, a_mn, b_mn);
                 const Steps a0 = steps_of<BK>(sa, a_mn), b0 = steps_of<BK>(sb, b_mn);
-                const int a = lt & 1;
-                const uint32_t aph = (uint32_t)(lt >> 1) & 1u;
-                ok = warp_wait(acc_empty(a), aph ^ 1u, &aborted);
-                if (!ok) {
-                    if (one)
-                        atomicOr(L.err, kErrWaitDone);
-                    break;
-                }
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t d = tmem + (uint32_t)(a * T);
-                for (int kb = 0; kb < kb_n; ++kb) {
-                    ok = warp_wait(full(s), ph, &aborted);
+                // accumulations of a tile: one, or of kHead its parts of K
+                for (int kb0 = 0; ok && kb0 < kb_n; ++visit) {
+                    const int kb1 = EPI == kHead ? min(kb0 + kHeadPart, kb_n) : kb_n;
+                    const int a = visit & 1;
+                    const uint32_t aph = (uint32_t)(visit >> 1) & 1u;
+                    ok = warp_wait(acc_empty(a), aph ^ 1u, &aborted);
                     if (!ok) {
                         if (one)
-                            atomicOr(L.err, kErrWaitFull);
+                            atomicOr(L.err, kErrWaitDone);
                         break;
                     }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    if (one) {
-                        const Steps da = a0.stage(s * a_bytes), db = b0.stage(s * b_bytes);
+                    const uint32_t d = tmem + (uint32_t)(a * T);
+                    for (int kb = kb0; kb < kb1; ++kb) {
+                        ok = warp_wait(full(s), ph, &aborted);
+                        if (!ok) {
+                            if (one)
+                                atomicOr(L.err, kErrWaitFull);
+                            break;
+                        }
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        if (one) {
+                            const Steps da = a0.stage(s * a_bytes), db = b0.stage(s * b_bytes);
 #pragma unroll
-                        for (int k = 0; k < BK / 16; ++k)
-                            mma_bf16<CG>(d, da.at(k), db.at(k), idesc, (kb | k) != 0 ? 1u : 0u);
-                        mma_commit<CG>(empty(s));
+                            for (int k = 0; k < BK / 16; ++k)
+                                mma_bf16<CG>(d, da.at(k), db.at(k), idesc, ((kb - kb0) | k) != 0 ? 1u : 0u);
+                            mma_commit<CG>(empty(s));
+                        }
+                        __syncwarp();
+                        if (++s == n_stages) {
+                            s = 0;
+                            ph ^= 1u;
+                        }
                     }
+                    if (one)
+                        mma_commit<CG>(acc_full(a));
                     __syncwarp();
-                    if (++s == n_stages) {
-                        s = 0;
-                        ph ^= 1u;
-                    }
+                    if (!ok && !mbar_wait(acc_full(a), aph) && one)
+                        atomicOr(L.err, kErrDrain);
+                    kb0 = kb1;
                 }
-                if (one)
-                    mma_commit<CG>(acc_full(a));
-                __syncwarp();
-                if (!ok && !mbar_wait(acc_full(a), aph) && one)
-                    atomicOr(L.err, kErrDrain);
             }
         }
     } else {
@@ -1172,7 +1271,54 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
         const int out_cols = EPI == kGate ? cols / 2 : cols;
         const int half0 = half * (SPLIT && EPI == kGate ? 32 : out_cols / 2);
         int lt = 0;
-        for (int t; (t = turn_of(lt, pair, n_pairs)) < n_tiles; ++lt) {
+        if constexpr (EPI == kHead) {
+            static_assert(T == CG * kHeadCols, "columns of a warp");
+            bool seen = true;
+            int visit = 0;
+            if (CG == 1 && half == 1)
+                seen = false;
+            for (int t; seen && (t = turn_of(lt, pair, n_pairs)) < n_tiles; ++lt) {
+                const Tile tile = tile_at(L, t);
+                const Product &P = L.p[tile.p];
+                const int parts = (P.k_blocks[0] + kHeadPart - 1) / kHeadPart;
+                const int row0 = tile.m * T + (int)rank * BM + q * 32;
+                const int col0 = tile.n * T + half * kHeadCols;
+                const bool any = row0 < P.m && col0 < P.n;
+                const int id = any && P.head.ids.p != nullptr && row0 + lane < P.m
+                                   ? P.head.ids.at(row0 + lane, P.n) : -1;
+                float v[kHeadCols];
+#pragma unroll
+                for (int j = 0; j < kHeadCols; ++j)
+                    v[j] = 0.0f;
+                for (const int end = visit + parts; seen && visit < end; ++visit) {
+                    const int a = visit & 1;
+                    seen = mbar_wait(acc_full(a), (uint32_t)(visit >> 1) & 1u);
+                    if (!seen)
+                        atomicOr(L.err, kErrWaitDone);
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    seen = __all_sync(0xFFFFFFFFu, seen && !*(volatile int *)&aborted);
+                    if (!seen)
+                        break;
+                    const uint32_t acc =
+                        tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * T + half * kHeadCols);
+#pragma unroll
+                    for (int c = 0; c < kHeadCols; c += 32) {
+                        float x[32];
+                        load_acc(acc + (uint32_t)c, x);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            v[c + j] += x[j];
+                    }
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0)
+                        mbar_arrive<CG>(acc_empty(a));
+                }
+                if (seen && any)
+                    head_rows(P, st, v, id, row0, col0);
+            }
+        }
+        for (int t; EPI != kHead && (t = turn_of(lt, pair, n_pairs)) < n_tiles; ++lt) {
             const Tile tile = tile_at(L, t);
             const Product &P = L.p[tile.p];
             const int a = lt & 1;

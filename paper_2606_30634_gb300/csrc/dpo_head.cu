@@ -1,13 +1,154 @@
 // dpo_head.cu -- the head: log probabilities from the stream and the head's weights, and the
 // gradients of both (dpo_head, dpo_head_backward in include/dpo_ends.h).
 //
-// Forward, two launches: logits = x w^T in fp32; the rows' distributions (dpo_logprobs.cu).
-// Backward, two launches: G from the kept logits; dx = G w and dw = G^T x, one list of tiles.
+// Forward, two launches: the product x w^T, whose epilogue reduces 128 columns of a row to
+// (maximum m, sum of e^(z - m), entropy sum), so that no logits are written; and the join of a
+// row's parts. For `top` the logits are written and read once more (dpo_logprobs.cu).
+// Kept for the backward: e^(z - m) in fp16, and m. Forming the logits again would cost a third
+// of the backward's two products; reading this costs 2 bytes a logit.
+// Backward, two launches: G from what was kept; dx = G w and dw = G^T x, one list of tiles.
 #include "dpo_logprobs.cuh"
 #include "dpo_products.h"
 
+#include <cuda_fp16.h>
+
 namespace dpo {
 namespace {
+
+constexpr float kKeptUnit = 1.0f / 32768.0f;   // of the kept fp16 values
+
+// ---------------------------------------------------------------- join ----
+// A CTA joins 32 rows, one a lane; its warps take the rows' parts in turn.
+constexpr int kJoinMaxWarps = 32, kJoinAhead = 4;
+
+struct JoinArgs {
+    const float *maxima, *target;
+    const float2 *sums;
+    Ids ids;
+    float *logp, *entropy, *stats;
+    int64_t rows, vocab;
+    int parts;
+};
+
+__global__ void __launch_bounds__(32 * kJoinMaxWarps) head_join_kernel(const JoinArgs a)
+{
+    __shared__ Part part_[kJoinMaxWarps][32];
+    const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t row = (int64_t)blockIdx.x * 32 + lane, r = min(row, a.rows - 1);
+    pdl_wait();
+    Part part;
+    for (int i = warp; i < a.parts; i += warps * kJoinAhead) {
+        Part p[kJoinAhead];
+#pragma unroll
+        for (int u = 0; u < kJoinAhead; ++u)
+            if (i + u * warps < a.parts) {
+                const int64_t at = (int64_t)(i + u * warps) * a.rows + r;
+                const float2 sw = a.sums[at];
+                p[u].m = a.maxima[at];
+                p[u].s = sw.x;
+                p[u].w = sw.y;
+            }
+#pragma unroll
+        for (int u = 0; u < kJoinAhead; ++u)
+            if (i + u * warps < a.parts)
+                part.join(p[u]);
+    }
+    part_[warp][lane] = part;
+    __syncthreads();
+    if (warp != 0 || row >= a.rows)
+        return;
+    for (int w = 1; w < warps; ++w)
+        part.join(part_[w][lane]);
+    const float logs = part.log_sum();
+    a.stats[2 * row] = part.m;
+    a.stats[2 * row + 1] = logs;
+    a.entropy[row] = part.entropy();
+    if (a.logp != nullptr)
+        a.logp[row] = a.ids.at(row, a.vocab) < 0 ? 0.0f : a.target[row] - part.m - logs;
+}
+
+// ------------------------------------------------------------- dlogits ----
+// G in bf16 from the kept values: p = e^(z - m_part) e^(m_part - m - log S). The id's own
+// element is a (1 - p) from the log probability itself: a kept p near 1 would leave little of it.
+constexpr int kGradWarps = 8, kGradPieces = 4;   // rows of a CTA; accesses of 8 columns a lane
+
+struct GradArgs {
+    const __half *kept;
+    const float *maxima;
+    Ids ids;
+    const float *logp, *entropy, *stats, *dlogp, *dentropy;
+    __nv_bfloat16 *g;
+    int64_t rows, vocab, ld;
+    int spans;
+    float scale;
+};
+
+__global__ void __launch_bounds__(32 * kGradWarps) head_gradient_kernel(const GradArgs a)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t group = blockIdx.x / a.spans;
+    const int span = (int)(blockIdx.x - group * a.spans);
+    const int64_t row = group * kGradWarps + (threadIdx.x >> 5);
+    pdl_wait();
+    if (row >= a.rows)
+        return;
+    const int id = a.ids.at(row, a.vocab);
+    const float ga = id >= 0 ? ld1(a.dlogp + row) : 0.0f;
+    const float gb = a.dentropy != nullptr ? ld1(a.dentropy + row) : 0.0f;
+    const float m = ld1(a.stats + 2 * row), logs = ld1(a.stats + 2 * row + 1), h = ld1(a.entropy + row);
+    const bool none = ga == 0.0f && gb == 0.0f;
+    const int64_t c0 = ((int64_t)span * kGradPieces * 32 + lane) * 8;
+    const __half *const e = a.kept + row * a.ld;
+    __nv_bfloat16 *const g = a.g + row * a.ld;
+    uint4 q[kGradPieces];
+    float top[kGradPieces];
+#pragma unroll
+    for (int u = 0; u < kGradPieces; ++u) {
+        const int64_t c = c0 + u * 256;
+        q[u] = make_uint4(0u, 0u, 0u, 0u);
+        top[u] = 0.0f;
+        if (c < a.vocab && !none) {   // whole pieces: the pitch is a multiple of 8
+            asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(q[u].x), "=r"(q[u].y), "=r"(q[u].z), "=r"(q[u].w)
+                         : "l"(e + c));
+            top[u] = ld1(a.maxima + c / kHeadStatCols * a.rows + row);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kGradPieces; ++u) {
+        const int64_t c = c0 + u * 256;
+        if (c >= a.vocab)
+            break;
+        const float part = none ? 0.0f : exp2_fast((top[u] - m - logs) * kLog2e) * kKeptUnit;
+        const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+        uint32_t o[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(w + j));
+            float p[2] = {v.x * part, v.y * part}, y[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                float lp = 0.0f;
+                y[k] = -ga * p[k];
+                if (id == c + 2 * j + k) {
+                    lp = ld1(a.logp + row);
+                    p[k] = exp2_fast(lp * kLog2e);
+                    y[k] = -ga * expm1f(lp);
+                } else if (gb != 0.0f) {
+                    lp = __logf(p[k]);
+                }
+                if (gb != 0.0f && p[k] != 0.0f)
+                    y[k] = fmaf(-gb * p[k], lp + h, y[k]);
+                y[k] = none ? 0.0f : y[k] * a.scale;
+            }
+            o[j] = pack_bf16x2(y[0], y[1]);
+        }
+        // columns past the vocabulary, up to the pitch, are not read by the products
+        *reinterpret_cast<uint4 *>(g + c) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+}
+
+// ---------------------------------------------------------------- host ----
 
 int64_t align_up(int64_t v) { return (v + 255) / 256 * 256; }
 int64_t pitch_of(int64_t vocab) { return (vocab + 7) / 8 * 8; }
@@ -28,16 +169,27 @@ int check_head(const char *what, int64_t tokens, int64_t dim, int64_t vocab, flo
     return DPO_OK;
 }
 
+// What is kept, and the workspaces: where each part begins.
 struct Sizes {
-    int64_t ld, forward, kept, backward;
+    int64_t ld, parts;
+    int64_t kept, maxima;              // kept: the values, their maxima
+    int64_t target, sums, own, logits; // forward: without kept its maxima, for `top` logits
+    int64_t forward, backward;
 };
-Sizes sizes_of(int64_t tokens, int64_t vocab, bool keep)
+Sizes sizes_of(int64_t tokens, int64_t vocab, bool keep, int top)
 {
     Sizes s;
     s.ld = pitch_of(vocab);
-    const int64_t logits = align_up(tokens * s.ld * 4);
-    s.forward = keep ? 0 : logits;
-    s.kept = logits;
+    s.parts = (vocab + kHeadStatCols - 1) / kHeadStatCols;
+    s.maxima = align_up(tokens * s.ld * 2);
+    s.kept = s.maxima + align_up(s.parts * tokens * 4);
+    s.target = 0;
+    s.sums = align_up(tokens * 4);
+    s.own = s.sums + align_up(s.parts * tokens * 8);
+    s.logits = s.own + (keep ? 0 : align_up(s.parts * tokens * 4));
+    if (top > 0 && !keep)
+        s.logits = 0;
+    s.forward = s.logits + (top > 0 ? align_up(tokens * s.ld * 4) : 0);
     s.backward = align_up(tokens * s.ld * 2);
     return s;
 }
@@ -76,7 +228,7 @@ extern "C" int dpo_head_workspace(int64_t tokens, int64_t dim, int64_t vocab, in
         return rc;
     if (top < 0 || top > DPO_MAX_TOP || top > vocab)
         return call_fail(DPO_EINVAL, "%s: top %d of %lld", what, top, (long long)vocab);
-    const Sizes s = sizes_of(tokens, vocab, keep != 0);
+    const Sizes s = sizes_of(tokens, vocab, keep != 0, top);
     if (forward_bytes != nullptr)
         *forward_bytes = s.forward;
     if (kept_bytes != nullptr)
@@ -103,7 +255,7 @@ extern "C" int dpo_head(const dpo_head_args *args, void *cuda_stream)
     if (a.tokens == 0)
         return DPO_OK;
     const int64_t T = a.tokens;
-    const Sizes s = sizes_of(T, a.vocab, a.kept != nullptr);
+    const Sizes s = sizes_of(T, a.vocab, a.kept != nullptr, a.top);
     Buffers b(what);
     b.add("x", a.x, T, a.dim, a.ld_x, 2, 16, false);
     b.add("w", a.w, a.vocab, a.dim, a.dim, 2, 16, false);
@@ -122,12 +274,37 @@ extern "C" int dpo_head(const dpo_head_args *args, void *cuda_stream)
     if ((rc = check_workspace(what, b, a.workspace, a.workspace_bytes, s.forward)) != DPO_OK ||
         (rc = b.done()) != DPO_OK)
         return rc;
-    void *const logits = a.kept != nullptr ? a.kept : a.workspace;
-    const StoreProduct p = {a.x, a.w, logits, T, a.vocab, a.dim, a.ld_x, a.dim, s.ld, 0, 0, 1, 0};
-    if ((rc = store_products(what, &p, 1, cuda_stream)) != DPO_OK)
+    uint8_t *const ws = static_cast<uint8_t *>(a.workspace), *const kept = static_cast<uint8_t *>(a.kept);
+    HeadProduct p{};
+    p.x = a.x;
+    p.w = a.w;
+    p.tokens = T;
+    p.dim = a.dim;
+    p.vocab = a.vocab;
+    p.ld_x = a.ld_x;
+    p.ids = ids;
+    p.scale = a.scale;
+    p.ld = s.ld;
+    if (a.top == 0 || kept != nullptr) {
+        p.target = reinterpret_cast<float *>(ws + s.target);
+        p.sums = reinterpret_cast<float2 *>(ws + s.sums);
+        p.maxima = reinterpret_cast<float *>(kept != nullptr ? kept + s.maxima : ws + s.own);
+        p.kept = kept;
+    }
+    if (a.top > 0)
+        p.logits = ws + s.logits;
+    if ((rc = head_product(what, p, cuda_stream)) != DPO_OK)
         return rc;
+    if (a.top == 0) {
+        JoinArgs j{p.maxima, p.target, p.sums, ids, a.ids.p != nullptr ? a.logp : nullptr, a.entropy, a.stats,
+                   T, a.vocab, (int)s.parts};
+        int warps = 4;
+        while (warps < kJoinMaxWarps && warps * kJoinAhead < s.parts)
+            warps *= 2;
+        return launch(what, head_join_kernel, (T + 31) / 32, 32 * warps, 0, cuda_stream, j);
+    }
     dpo_logprobs_args l{};
-    l.logits = logits;
+    l.logits = p.logits;
     l.ids = a.ids;
     l.logp = a.logp;
     l.entropy = a.entropy;
@@ -167,7 +344,7 @@ extern "C" int dpo_head_backward(const dpo_head_backward_args *args, void *cuda_
             cudaMemsetAsync(a.dw, 0, (size_t)(V * D * gsize), static_cast<cudaStream_t>(cuda_stream));
         return e == cudaSuccess ? DPO_OK : call_fail(DPO_ECUDA, "%s: %s", what, cudaGetErrorString(e));
     }
-    const Sizes s = sizes_of(T, V, true);
+    const Sizes s = sizes_of(T, V, true, 0);
     b.add("x", a.x, T, D, a.ld_x, 2, 16, false);
     b.add("w", a.w, V, D, D, 2, 16, false);
     add_ids(b, a.ids);
@@ -183,21 +360,27 @@ extern "C" int dpo_head_backward(const dpo_head_backward_args *args, void *cuda_
     if ((rc = check_workspace(what, b, a.workspace, a.workspace_bytes, s.backward)) != DPO_OK ||
         (rc = b.done()) != DPO_OK)
         return rc;
+    const uint8_t *const kept = static_cast<const uint8_t *>(a.kept);
     void *const G = a.workspace;
-    dpo_logprobs_backward_args l{};
-    l.logits = a.kept;
-    l.ids = a.ids;
-    l.stats = a.stats;
-    l.entropy = a.entropy;
-    l.dlogp = a.dlogp;
-    l.dentropy = a.dentropy;
-    l.dlogits = G;
-    l.rows = T;
-    l.vocab = V;
-    l.ld_logits = l.ld_dlogits = s.ld;
-    l.scale = a.scale;
-    l.dtype = DPO_F32;
-    if ((rc = logits_gradient(what, l, cuda_stream)) != DPO_OK)
+    GradArgs g{};
+    g.kept = reinterpret_cast<const __half *>(kept);
+    g.maxima = reinterpret_cast<const float *>(kept + s.maxima);
+    g.ids = ids;
+    g.logp = a.logp;
+    g.entropy = a.entropy;
+    g.stats = a.stats;
+    g.dlogp = a.dlogp;
+    g.dentropy = a.dentropy;
+    g.g = static_cast<__nv_bfloat16 *>(G);
+    g.rows = T;
+    g.vocab = V;
+    g.ld = s.ld;
+    g.scale = a.scale;
+    g.spans = (int)((V + kGradPieces * 256 - 1) / (kGradPieces * 256));
+    const int64_t grid = (T + kGradWarps - 1) / kGradWarps * g.spans;
+    if (grid >= kMaxCount)
+        return call_fail(DPO_EINVAL, "%s: %lld x %lld is too large", what, (long long)T, (long long)V);
+    if ((rc = launch(what, head_gradient_kernel, grid, 32 * kGradWarps, 0, cuda_stream, g)) != DPO_OK)
         return rc;
     StoreProduct p[2];
     int n = 0;

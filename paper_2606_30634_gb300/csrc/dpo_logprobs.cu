@@ -184,14 +184,14 @@ template <bool ACCURATE> struct RowGradient {
 
 // CTAs of a row take spans of kBackThreads * kBackPieces accesses; V elements an access, the
 // same alignment on both sides, or 1.
-template <class T, class G, int V>
+template <class T, int V>
 __global__ void __launch_bounds__(kBackThreads) logprobs_backward_kernel(const LogBackArgs a)
 {
     const int64_t row = blockIdx.x / a.spans, span = blockIdx.x - row * a.spans;
     pdl_wait();
     const T *const p = static_cast<const T *>(a.logits) + row * a.ld;
-    G *const d = static_cast<G *>(a.dlogits) + row * a.ld_d;
-    RowGradient<sizeof(G) == 4> f;
+    T *const d = static_cast<T *>(a.dlogits) + row * a.ld_d;
+    RowGradient<sizeof(T) == 4> f;
     f.id = a.ids.at(row, a.vocab);
     f.a = f.id >= 0 ? ld1(a.dlogp + row) : 0.0f;
     f.b = a.dentropy != nullptr ? ld1(a.dentropy + row) : 0.0f;
@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(kBackThreads) logprobs_backward_kernel(const L
 #pragma unroll
         for (int j = 0; j < V; ++j)
             g[j] = none ? 0.0f : f(v[u].get(j), i + j);
-        Vec<G, V> o;
+        Vec<T, V> o;
         o.set(g);
         if (i0 + u * kBackThreads < body)
             o.store(d + i);
@@ -251,9 +251,9 @@ int check_row_ids(const char *what, const dpo_ids &ids, int64_t rows, Ids *out)
     return rc;
 }
 
-template <class T, class G> auto back_fn(bool wide) -> void (*)(LogBackArgs)
+template <class T> auto back_fn(bool wide) -> void (*)(LogBackArgs)
 {
-    return wide ? logprobs_backward_kernel<T, G, 16 / (int)sizeof(T)> : logprobs_backward_kernel<T, G, 1>;
+    return wide ? logprobs_backward_kernel<T, 16 / (int)sizeof(T)> : logprobs_backward_kernel<T, 1>;
 }
 
 }  // namespace
@@ -321,20 +321,22 @@ extern "C" int dpo_logprobs(const dpo_logprobs_args *args, void *cuda_stream)
     return launch_in_clusters(what, fn, a.rows * ctas, ctas, threads, 0, cuda_stream, k);
 }
 
-namespace {
-
-int backward(const char *what, const dpo_logprobs_backward_args &a, bool to_bf16, void *cuda_stream)
+extern "C" int dpo_logprobs_backward(const dpo_logprobs_backward_args *args, void *cuda_stream)
 {
+    const char *what = "dpo_logprobs_backward";
+    if (args == nullptr)
+        return call_fail(DPO_EINVAL, "%s: no arguments", what);
+    const dpo_logprobs_backward_args &a = *args;
     int rc = check_rows(what, a.rows, a.vocab, a.dtype, a.scale);
     LogBackArgs k{};
     if (rc != DPO_OK || (rc = check_row_ids(what, a.ids, a.rows, &k.ids)) != DPO_OK || a.rows == 0)
         return rc;
-    const int64_t size = elem_size(a.dtype), dsize = to_bf16 ? 2 : size;
-    const bool in_place = a.dlogits == a.logits && a.ld_dlogits == a.ld_logits && !to_bf16;
+    const int64_t size = elem_size(a.dtype);
+    const bool in_place = a.dlogits == a.logits && a.ld_dlogits == a.ld_logits;
     Buffers b(what);
     b.add("logits", a.logits, a.rows, a.vocab, a.ld_logits, size, size, in_place);
     if (!in_place)
-        b.add("dlogits", a.dlogits, a.rows, a.vocab, a.ld_dlogits, dsize, dsize, true);
+        b.add("dlogits", a.dlogits, a.rows, a.vocab, a.ld_dlogits, size, size, true);
     add_ids(b, a.ids);
     b.add("stats", a.stats, 1, 2 * a.rows, 2 * a.rows, 4, 4, false);
     b.add("dlogp", a.dlogp, 1, a.rows, a.rows, 4, 4, false);
@@ -344,11 +346,9 @@ int backward(const char *what, const dpo_logprobs_backward_args &a, bool to_bf16
     }
     if ((rc = b.done()) != DPO_OK)
         return rc;
-    // in accesses of 16 bytes of logits, where dlogits' boundaries come with theirs
     const int64_t wide = 16 / size;
-    const int64_t at = (int64_t)(reinterpret_cast<uintptr_t>(a.logits) / (uintptr_t)size % 8),
-                  at_d = (int64_t)(reinterpret_cast<uintptr_t>(a.dlogits) / (uintptr_t)dsize % 8);
-    const bool aligned = (at - at_d) % wide == 0 && (a.ld_logits - a.ld_dlogits) % wide == 0;
+    const bool aligned = (reinterpret_cast<uintptr_t>(a.logits) - reinterpret_cast<uintptr_t>(a.dlogits)) % 16 == 0 &&
+                         (a.ld_logits - a.ld_dlogits) % wide == 0;
     k.logits = a.logits;
     k.stats = a.stats;
     k.entropy = a.entropy;
@@ -365,24 +365,6 @@ int backward(const char *what, const dpo_logprobs_backward_args &a, bool to_bf16
     if (k.spans * a.rows >= kMaxCount)
         return call_fail(DPO_EINVAL, "%s: %lld rows of %lld are too many", what, (long long)a.rows,
                          (long long)a.vocab);
-    using B16 = __nv_bfloat16;
-    return launch(what, to_bf16                ? back_fn<float, B16>(aligned)
-                        : a.dtype == DPO_F32   ? back_fn<float, float>(aligned)
-                                               : back_fn<B16, B16>(aligned),
+    return launch(what, a.dtype == DPO_F32 ? back_fn<float>(aligned) : back_fn<__nv_bfloat16>(aligned),
                   k.spans * a.rows, kBackThreads, 0, cuda_stream, k);
-}
-
-}  // namespace
-
-int dpo::logits_gradient(const char *what, const dpo_logprobs_backward_args &a, void *cuda_stream)
-{
-    return backward(what, a, true, cuda_stream);
-}
-
-extern "C" int dpo_logprobs_backward(const dpo_logprobs_backward_args *args, void *cuda_stream)
-{
-    const char *what = "dpo_logprobs_backward";
-    if (args == nullptr)
-        return call_fail(DPO_EINVAL, "%s: no arguments", what);
-    return backward(what, *args, false, cuda_stream);
 }

@@ -8,10 +8,6 @@
 #include <math.h>
 
 namespace dpo {
-
-// dpo_logprobs_backward from fp32 logits to dlogits in bf16, both at pitch ld.
-int logits_gradient(const char *what, const dpo_logprobs_backward_args &a, void *cuda_stream);
-
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;

@@ -2,6 +2,8 @@
 // feed-forward block's.
 #pragma once
 
+#include "dpo_ids.cuh"
+
 #include <stdint.h>
 
 namespace dpo {
@@ -22,5 +24,22 @@ constexpr int kMaxStoreProducts = 4;
 
 // Up to four of them in one launch, in whose order their tiles are begun (longest first).
 int store_products(const char *what, const StoreProduct *p, int n, void *stream);
+
+// A head's logits x w^T: what their distributions need, by kHeadStatCols columns, or the logits
+// themselves, or both.
+constexpr int kHeadStatCols = 128;
+struct HeadProduct {
+    const void *x, *w;            // bf16, tokens x dim at pitch ld_x, vocab x dim
+    int64_t tokens, dim, vocab, ld_x;
+    Ids ids;                      // p nullptr: none
+    float scale;
+    float *target;                // z of each token's id
+    float *maxima;                // [columns / kHeadStatCols][token], or nullptr: no statistics
+    float2 *sums;                 // likewise
+    void *kept;                   // fp16 e^(z - maximum) times 2^15, or nullptr (with statistics)
+    void *logits;                 // fp32, before the scale, or nullptr
+    int64_t ld;                   // of both
+};
+int head_product(const char *what, const HeadProduct &h, void *stream);
 
 }  // namespace dpo

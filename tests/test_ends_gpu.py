@@ -492,7 +492,8 @@ def test_logprobs_gradient_by_differences():
 # ------------------------------------------------------------------ head ----
 
 HEAD = [(1, 64, 100), (1, 8, 1), (3, 72, 33), (9, 264, 1003), (33, 520, 300), (130, 768, 2051), (257, 64, 5003), (8, 2048, 700),
-        (700, 136, 129), (300, 1096, 4100), (64, 2400, 257)]
+        (700, 136, 129), (300, 1096, 4100), (64, 2400, 257),
+        (20, 1104, 50001), (600, 1104, 30001)]   # several tiles, each in parts of K, to a CTA and to a pair
 
 
 def head_case(t, d, v, seed=0, pitch=0, spread=2.0):
@@ -576,6 +577,19 @@ def test_head_backward(t, d, v, gd, scale, entropy):
         dx = ends.head_logprobs_backward(a, kept, x, w, ids, o, dw, dentropy=b, accumulate=accumulate)
         check_head_backward(x, w, ids, scale, a, b, o, kept, *rest, (dx, dw), gd, np64(old) if accumulate else None)
     assert ends.status() == 0
+
+
+def test_head_is_precise():
+    """K is added up in parts, so truncation does not grow with it: 64 steps of at most one step
+    2^-23 of a partial sum of size about one, 8e-6 where all add up, in each of four parts, of
+    log probabilities near 10: 4e-6, and random signs halve it."""
+    _, x, w, ids = head_case(64, 4096, 8000, seed=2)
+    ids = ids.clamp(0, 7999)
+    o, _ = ends.head_logprobs(x, w, ids)
+    z = np64(x) @ np64(w).T
+    logp, h = ref.logprobs(z, ids.cpu().numpy())
+    assert np.linalg.norm(np64(o.logp) - logp) <= 2e-6 * np.linalg.norm(logp)
+    assert np.linalg.norm(np64(o.entropy) - h) <= 2e-6 * np.linalg.norm(h)
 
 
 @pytest.mark.parametrize("t,d,v", [(40, 136, 1003), (3, 64, 300)])
