@@ -124,7 +124,7 @@ typedef struct {
     int64_t *top_ids;           /* rows x top */
     int64_t rows, vocab;        /* vocab in [1, 2^31) */
     int64_t ld_logits;
-    float scale;                /* finite, > 0 */
+    float scale;                /* 1e-20 to 1e6 */
     int dtype;
     int top;                    /* 0 .. min(DPO_MAX_TOP, vocab) */
 } dpo_logprobs_args;
@@ -174,7 +174,7 @@ typedef struct {
     void *kept;                 /* what the backward needs, or NULL: 256-byte aligned */
     int64_t tokens, dim, vocab;
     int64_t ld_x;
-    float scale;                /* finite, > 0 */
+    float scale;                /* 1e-20 to 1e6 */
     int top;
     void *workspace;            /* 256-byte aligned */
     int64_t workspace_bytes;

@@ -51,6 +51,9 @@ __device__ __forceinline__ void st_cluster(uint32_t addr, uint32_t a, uint32_t b
 
 // ---------------------------------------------------------------- host ----
 
+// Of logits.
+inline bool good_scale(float s) { return s >= 1e-20f && s <= 1e6f; }
+
 constexpr int64_t kMaxCount = (int64_t)1 << 31;
 
 // Ids as the kernels take them, checked, and their number.

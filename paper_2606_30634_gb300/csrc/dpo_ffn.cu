@@ -418,18 +418,34 @@ int dpo::store_products(const char *what, const StoreProduct *p, int n, void *st
     if (rc != DPO_OK)
         return rc;
     Shape s[kMaxProducts];
-    bool whole = n > 1, a_mn = false;
-    for (int i = 0; i < n; ++i) {
+    auto whole = [&](int i) { return p[i].f32 || p[i].accumulate || p[i].a_mn; };
+    for (int i = 0; i < n; ++i)
         s[i] = {p[i].m, p[i].n, p[i].k, 1};
-        whole = whole || p[i].f32 || p[i].accumulate || p[i].a_mn;
-        a_mn = a_mn || p[i].a_mn;
+    auto choose = [&](int i, int count) {
+        bool a_mn = false;
+        for (int j = i; j < i + count; ++j)
+            a_mn = a_mn || p[j].a_mn;
+        return form_of(*d, s + i, count, kStore, count > 1 || whole(i), a_mn);
+    };
+    const Choice all = choose(0, n);
+    Form f = all.form;
+    // the first product on its own with its K split, where its few long tiles would be what the
+    // list waits for (dx_form)
+    int first = 0;
+    if (n > 1) {
+        const Choice one = choose(0, 1);
+        if (one.form.thin && one.time + choose(1, n - 1).time + 2000.0 < all.time) {
+            if ((rc = store_products(what, p, 1, stream)) != DPO_OK)
+                return rc;
+            first = 1;
+            f = choose(1, n - 1).form;
+        }
     }
-    const Form f = form_of(*d, s, n, kStore, whole, a_mn).form;
     Launch L{};
     Maps m;
-    for (int i = 0; i < n; ++i) {
+    for (int i = first; i < n; ++i) {
         const StoreProduct &q = p[i];
-        Product &P = L.p[i];
+        Product &P = L.p[i - first];
         P.a_mn = q.a_mn;
         P.b_mn = q.b_mn;
         if (q.a_mn)
@@ -450,7 +466,17 @@ int dpo::store_products(const char *what, const StoreProduct *p, int n, void *st
         P.ld_old = P.ld_o = q.ld_out;
         P.o0 = static_cast<__nv_bfloat16 *>(q.out);
     }
-    return run(what, *d, L, s, n, kStore, f, false, m.ok, stream);
+    if (n - first == 2) {   // deal by length
+        const int64_t slots = slots_of(*d, f, kStore), longs = tiles_of(s[first], f, kStore),
+                      shorts = tiles_of(s[first + 1], f, kStore), fewer = longs % slots;
+        const int64_t a = blocks_of(s[first].k, f.bk()), b = blocks_of(s[first + 1].k, f.bk());
+        if (fewer > 0 && longs + shorts > slots && a >= 2 * b) {
+            const int64_t most = shorts / (slots - fewer), want = a / (b > 4 ? b : 4);   // 4: its store
+            L.longs = (int)longs;
+            L.extra = (int)(want < most ? want : most);
+        }
+    }
+    return run(what, *d, L, s + first, n - first, kStore, f, false, m.ok, stream);
 }
 
 int dpo::head_product(const char *what, const HeadProduct &h, void *stream)

@@ -161,6 +161,7 @@ struct Launch {
     int cols;                     // single CTAs: the tile's columns, kTile(1), or half of them
                                   // where K is split
     int early;                    // another launch of this kernel follows in the same call
+    int longs, extra;             // extra > 0: how unequal tiles are dealt, see tile_of_round
     unsigned int *err;
 };
 
@@ -293,6 +294,26 @@ __device__ __forceinline__ Tile tile_at(const Launch &L, int t)
 __device__ __forceinline__ int turn_of(int r, int pair, int n)
 {
     return r * n + (r & 1 ? n - 1 - pair : pair);
+}
+
+// The same where the first `longs` tiles are several times the others' length and do not come
+// out even: whoever has one less of them gets `extra` short ones before the rest are dealt. (4096
+// tokens, 768 x 50257: 48 tiles of 393 K blocks and 591 of 32 for 76 pairs, 649 blocks for
+// the busiest by turn_of, 521 so.)
+__device__ __forceinline__ int tile_of_round(const Launch &L, int r, int pair, int n)
+{
+    if (L.extra == 0)
+        return turn_of(r, pair, n);
+    const int mine = (L.longs - pair + n - 1) / n, fewer = L.longs % n;   // pairs from `fewer` on
+    if (r < mine)
+        return pair + r * n;
+    r -= mine;
+    if (pair >= fewer) {
+        if (r < L.extra)
+            return L.longs + r * (n - fewer) + pair - fewer;
+        r -= L.extra;
+    }
+    return L.longs + L.extra * (n - fewer) + turn_of(r, pair, n);
 }
 
 // 2^x and 1 / x by the hardware's approximations (relative errors of about 2^-22 and 2^-23),
@@ -1138,7 +1159,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
         uint32_t ph = 1;     // parity of the stage's release
         const uint32_t bytes = (uint32_t)(CG * (R::bytes(a_rows) + b_bytes));
         bool ok = true;
-        for (int t, r = 0; ok && (t = turn_of(r, pair, n_pairs)) < n_tiles; ++r) {
+        for (int t, r = 0; ok && (t = tile_of_round(L, r, pair, n_pairs)) < n_tiles; ++r) {
             const Tile tile = tile_at(L, t);
             const Product &P = L.p[tile.p];
             const bool a_mn = P.a_mn, b_mn = P.b_mn;
@@ -1205,7 +1226,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
             int lt = 0, s = 0, visit = 0;
             uint32_t ph = 0;
             bool ok = true;
-            for (int t; ok && (t = turn_of(lt, pair, n_pairs)) < n_tiles; ++lt) {
+            for (int t; ok && (t = tile_of_round(L, lt, pair, n_pairs)) < n_tiles; ++lt) {
                 const Product &P = L.p[tile_at(L, t).p];
                 const int kb_all = P.k_blocks[0] + P.k_blocks[1];
                 const int kb_n = SPLIT ? share_end(kb_all, share, split) -
@@ -1277,7 +1298,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
             int visit = 0;
             if (CG == 1 && half == 1)
                 seen = false;
-            for (int t; seen && (t = turn_of(lt, pair, n_pairs)) < n_tiles; ++lt) {
+            for (int t; seen && (t = tile_of_round(L, lt, pair, n_pairs)) < n_tiles; ++lt) {
                 const Tile tile = tile_at(L, t);
                 const Product &P = L.p[tile.p];
                 const int parts = (P.k_blocks[0] + kHeadPart - 1) / kHeadPart;
@@ -1318,7 +1339,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                     head_rows(P, st, v, id, row0, col0);
             }
         }
-        for (int t; EPI != kHead && (t = turn_of(lt, pair, n_pairs)) < n_tiles; ++lt) {
+        for (int t; EPI != kHead && (t = tile_of_round(L, lt, pair, n_pairs)) < n_tiles; ++lt) {
             const Tile tile = tile_at(L, t);
             const Product &P = L.p[tile.p];
             const int a = lt & 1;

@@ -164,8 +164,8 @@ int check_head(const char *what, int64_t tokens, int64_t dim, int64_t vocab, flo
         (dim + 127) / 128 * ((vocab + 127) / 128) >= ((int64_t)1 << 28))
         return call_fail(DPO_EINVAL, "%s: %lld x %lld x %lld is too large", what, (long long)tokens,
                          (long long)dim, (long long)vocab);
-    if (!isfinite(scale) || !(scale > 0.0f))
-        return call_fail(DPO_EINVAL, "%s: scale %g", what, (double)scale);
+    if (!good_scale(scale))
+        return call_fail(DPO_EINVAL, "%s: scale %g (1e-20 to 1e6)", what, (double)scale);
     return DPO_OK;
 }
 

@@ -28,15 +28,31 @@ template <class T> __device__ __forceinline__ int64_t to_boundary(const T *p, in
     return k < n ? k : n;
 }
 
+// The warps' lists, in shared memory, merged into the first one's p.
+__device__ __forceinline__ void merge_warps(Pair &p, Pair (*lists)[32], int warps, int warp, int lane)
+{
+    lists[warp][lane] = p;
+    for (int step = 1; step < warps; step *= 2) {
+        __syncthreads();
+        if (warp % (2 * step) == 0) {   // the number of warps is a power of two
+            merge_pairs(p, lists[warp + step][31 - lane], lane);
+            lists[warp][lane] = p;
+        }
+    }
+    __syncthreads();
+}
+
 // A cluster's CTAs share a row, in equal spans; accesses of 16 bytes from the span's first
 // boundary on, so rows of odd pitches cost two short ends.
+// The `top` largest: each thread knows the largest of its own values, and the top-th of these
+// bounds the top-th of all from below. So only the threads that hold one of the first `top`
+// of them, `top` threads at most, can hold others, and their values alone are read again.
 template <class T, bool TOP>
 __global__ void __launch_bounds__(kMaxThreads) logprobs_kernel(const LogArgs a)
 {
     constexpr int V = 16 / (int)sizeof(T), U = 4;
     __shared__ Part parts[kMaxWarps];
-    __shared__ float tops_v[TOP ? kMaxWarps * 32 : 1];
-    __shared__ int tops_id[TOP ? kMaxWarps * 32 : 1];
+    __shared__ Pair lists[TOP ? kMaxWarps : 1][32];
     const int nt = blockDim.x, warps = nt >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cta_of_cluster(), ranks = ctas_of_cluster();
     const int64_t row = blockIdx.x / ranks;
@@ -44,76 +60,113 @@ __global__ void __launch_bounds__(kMaxThreads) logprobs_kernel(const LogArgs a)
     const int64_t n = min(share, a.vocab - begin);
     pdl_wait();
     const T *const p = static_cast<const T *>(a.logits) + row * a.ld + begin;
-    Part part;
-    TopList list(TOP ? a.top : 1, lane);
-
-    const int64_t head = to_boundary(p, n), body = (n - head) / V, tail = head + body * V;
-    auto one = [&](int64_t i, bool in) {   // one element a lane, by whole warps
-        float z[1] = {-INFINITY};
-        if (in) {
-            z[0] = __fmul_rn(ld1(p + i), a.scale);
-            part.add(z);
-        }
-        if (TOP && list.wanted(in ? z[0] : -INFINITY))
-            list.offer(z[0], in ? (int)(begin + i) : 0x7FFFFFFF);
-    };
-    if (warp == 0)
-        one(lane, lane < head);
-    if (warp == warps - 1)
-        one(tail + lane, tail + lane < n);
-    for (int64_t i0 = (int64_t)warp * 32; i0 < body; i0 += (int64_t)nt * U) {
+    const int head = (int)to_boundary(p, n);
+    const int64_t body = (n - head) / V, tail = head + body * V;
+    const T *const vectors = p + head;
+    // where ids are wanted the values are the products z, else the logits themselves
+    const float pre = TOP ? a.scale : 1.0f, c = TOP ? kLog2e : a.scale * kLog2e;
+    const float low = -Run::kLow / 10 * pre;
+    Run run;
+    int64_t best = threadIdx.x;   // the access with this thread's largest value
+    for (int64_t i0 = threadIdx.x; i0 < body; i0 += (int64_t)nt * U) {
         Vec<T, V> v[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (i0 + lane + (int64_t)u * nt < body)
-                v[u].load(p + head + (i0 + lane + (int64_t)u * nt) * V);
+            if (i0 + (int64_t)u * nt < body)
+                v[u].load(vectors + (i0 + (int64_t)u * nt) * V);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t i = i0 + lane + (int64_t)u * nt;
-            const bool in = i < body;
-            float z[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                z[j] = in ? __fmul_rn(v[u].get(j), a.scale) : -INFINITY;
-            if (in)
-                part.add(z);
+            if (i0 + (int64_t)u * nt >= body)
+                break;
+            float l[V], k[V];
+            float top = open_row(v[u], l, k);
             if (TOP) {
-                float largest = z[0];
 #pragma unroll
-                for (int j = 1; j < V; ++j)
-                    largest = fmaxf(largest, z[j]);
-                if (list.wanted(in ? largest : -INFINITY))
-#pragma unroll
-                    for (int j = 0; j < V; ++j)
-                        list.offer(z[j], in ? (int)(begin + head + i * V + j) : 0x7FFFFFFF);
+                for (int j = 0; j < V; ++j) {
+                    l[j] = __fmul_rn(l[j], pre);
+                    k[j] = __fmul_rn(k[j], pre);
+                }
+                top = __fmul_rn(top, pre);
+                if (top > run.m)
+                    best = i0 + (int64_t)u * nt;
             }
+            run.add(l, k, top, c, low);
         }
     }
+    Pair mine;
+    if (TOP && threadIdx.x < body) {
+        Vec<T, V> v;
+        v.load(vectors + best * V);
+        mine.v = run.m;
+#pragma unroll
+        for (int j = V - 1; j >= 0; --j) {
+            const float z = __fmul_rn(v.get(j), pre);
+            if ((z == z ? z : -INFINITY) == run.m)
+                mine.id = (int)(begin + head + best * V + j);
+        }
+    }
+    // the short ends: the first warp's lanes, one element each (V <= 8 of either)
+    const int64_t end = lane < 16 ? (lane < head ? lane : -1) : tail + lane - 16 < n ? tail + lane - 16 : -1;
+    float end_z = -INFINITY;
+    if (warp == 0 && end >= 0) {
+        const float l[1] = {__fmul_rn(ld1(p + end), pre)};
+        const float k[1] = {l[0] == l[0] ? fmaxf(l[0], -Run::kLow * pre) : l[0]};
+        end_z = l[0];
+        run.add(l, k, l[0], c, low);
+    }
 
+    Part part = run.part(TOP ? 1.0f : a.scale);
     part.warp_join();
     if (lane == 0)
         parts[warp] = part;
     if (TOP) {
-        tops_v[warp * 32 + lane] = list.v;
-        tops_id[warp * 32 + lane] = list.id;
-    }
-    __syncthreads();
-    if (warp == 0) {
-        for (int w = 1; w < warps; ++w) {
-            part.join(parts[w]);
-            if (TOP && list.wanted(tops_v[w * 32]))
-                list.offer(lane < a.top ? tops_v[w * 32 + lane] : -INFINITY,
-                           lane < a.top ? tops_id[w * 32 + lane] : 0x7FFFFFFF);
+        sort_pairs(mine, lane);
+        merge_warps(mine, lists, warps, warp, lane);
+        TopList more;   // what the others left out
+        more.top = a.top;
+        more.lane = lane;
+        more.last = lists[0][a.top - 1];
+        for (int i = warp; i < a.top; i += warps) {
+            const int id = lists[0][i].id;
+            if (id == 0x7FFFFFFF)
+                break;
+            const int64_t own = (id - begin - head) / V % nt;
+            for (int64_t q0 = own; q0 < body; q0 += 32 * (int64_t)nt) {
+                const int64_t q = q0 + lane * (int64_t)nt;
+                Vec<T, V> v;
+                v.zero();
+                if (q < body)
+                    v.load(vectors + q * V);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const int at = (int)(begin + head + q * V + j);
+                    const bool in = q < body && at != id;
+                    more.offer(in ? __fmul_rn(v.get(j), pre) : -INFINITY, in ? at : 0x7FFFFFFF);
+                }
+            }
         }
+        if (warp == 0)
+            more.offer(end_z, end >= 0 ? (int)(begin + end) : 0x7FFFFFFF);
+        if (__syncthreads_or(more.p.id != 0x7FFFFFFF)) {
+            Pair base = mine;   // the first warp's
+            merge_warps(more.p, lists, warps, warp, lane);
+            if (warp == 0) {
+                merge_pairs(base, shfl(more.p, 31 - lane), lane);
+                mine = base;
+            }
+        }
+    } else {
+        __syncthreads();
     }
+    if (warp == 0)
+        for (int w = 1; w < warps; ++w)
+            part.join(parts[w]);
     if (ranks > 1) {
         if (warp == 0) {
             if (lane == 0)
                 parts[0] = part;
-            if (TOP) {
-                tops_v[lane] = list.v;
-                tops_id[lane] = list.id;
-            }
+            if (TOP)
+                lists[0][lane] = mine;
         }
         cluster_barrier();
         if (rank == 0 && warp == 0) {
@@ -124,9 +177,13 @@ __global__ void __launch_bounds__(kMaxThreads) logprobs_kernel(const LogArgs a)
                 o.s = ld_cluster_f32(at + 4);
                 o.w = ld_cluster_f32(at + 8);
                 part.join(o);
-                if (TOP)
-                    list.offer(lane < a.top ? ld_cluster_f32(in_cta(tops_v + lane, r)) : -INFINITY,
-                               lane < a.top ? (int)ld_cluster(in_cta(tops_id + lane, r)) : 0x7FFFFFFF);
+                if (TOP) {
+                    const uint32_t q = in_cta(&lists[0][31 - lane], r);
+                    Pair other;
+                    other.v = ld_cluster_f32(q);
+                    other.id = (int)ld_cluster(q + 4);
+                    merge_pairs(mine, other, lane);
+                }
             }
         }
         cluster_barrier();   // no CTA leaves while the first may read its part
@@ -148,8 +205,8 @@ __global__ void __launch_bounds__(kMaxThreads) logprobs_kernel(const LogArgs a)
         }
     }
     if (TOP && lane < a.top) {
-        a.top_logp[row * a.top + lane] = list.v - part.m - logs;
-        a.top_ids[row * a.top + lane] = list.id;
+        a.top_logp[row * a.top + lane] = mine.v - part.m - logs;
+        a.top_ids[row * a.top + lane] = mine.id;
     }
 }
 
@@ -166,19 +223,49 @@ struct LogBackArgs {
     float scale;
 };
 
-// A row's scalars and its gradient's elements. p = e^(z - m - log S) by the accurate
-// exponential where fp32 is stored, by the approximation (2^-20 here) where bf16 is.
-template <bool ACCURATE> struct RowGradient {
-    float m, logs, h, a, b, scale;
+// A row's scalars and its gradient's elements,
+//   dlogit = -scale p (a + b (log p + h)) = p (k0 + k1 log p),
+// the id's own apart. fp32 results: log p = (z - m) - log S and the accurate exponential. bf16
+// results: t = log2 p by two multiply-adds and the approximation, 2^-20 with t's rounding.
+template <class T> struct RowGradient {
+    static constexpr bool kAccurate = sizeof(T) == 4;
+    float m, logs, h, a, b, scale, k0, k1, t0;
     int id;
-    __device__ __forceinline__ float operator()(float logit, int64_t col) const
+    bool none;
+    __device__ __forceinline__ RowGradient(const LogBackArgs &s, int64_t row)
     {
-        const float lp = __fmul_rn(logit, scale) - m - logs;
-        const float p = ACCURATE ? expf(lp) : exp2_fast(lp * kLog2e);
-        float g = col == id ? a * -expm1f(lp) : -a * p;
+        id = s.ids.at(row, s.vocab);
+        a = id >= 0 ? ld1(s.dlogp + row) : 0.0f;
+        b = s.dentropy != nullptr ? ld1(s.dentropy + row) : 0.0f;
+        h = s.dentropy != nullptr ? ld1(s.entropy + row) : 0.0f;
+        m = ld1(s.stats + 2 * row);
+        logs = ld1(s.stats + 2 * row + 1);
+        scale = s.scale;
+        none = a == 0.0f && b == 0.0f;
+        if (b == 0.0f)
+            h = 0.0f;
+        k0 = -scale * fmaf(b, h, a);
+        k1 = -scale * b * (kAccurate ? 1.0f : 0.6931471805599453f);
+        t0 = -logs * kLog2e;
+    }
+    __device__ __forceinline__ float other(float logit) const
+    {
+        const float t = kAccurate ? __fmul_rn(logit, scale) - m - logs
+                                  : fmaf(fmaf(logit, scale, -m), kLog2e, t0);
+        const float p = kAccurate ? expf(t) : exp2_fast(t);
+        return p * fmaf(k1, fmaxf(t, -1e30f), k0);   // no infinity times 0
+    }
+    __device__ __forceinline__ float own(float logit) const   // col == id
+    {
+        const float lp = __fmul_rn(logit, scale) - m - logs, p = expf(lp);
+        float g = a * -expm1f(lp);
         if (b != 0.0f && p != 0.0f)
             g = fmaf(-b * p, lp + h, g);
         return g * scale;
+    }
+    __device__ __forceinline__ float operator()(float logit, int64_t col) const
+    {
+        return none ? 0.0f : col == id ? own(logit) : other(logit);
     }
 };
 
@@ -191,41 +278,37 @@ __global__ void __launch_bounds__(kBackThreads) logprobs_backward_kernel(const L
     pdl_wait();
     const T *const p = static_cast<const T *>(a.logits) + row * a.ld;
     T *const d = static_cast<T *>(a.dlogits) + row * a.ld_d;
-    RowGradient<sizeof(T) == 4> f;
-    f.id = a.ids.at(row, a.vocab);
-    f.a = f.id >= 0 ? ld1(a.dlogp + row) : 0.0f;
-    f.b = a.dentropy != nullptr ? ld1(a.dentropy + row) : 0.0f;
-    f.h = a.dentropy != nullptr ? ld1(a.entropy + row) : 0.0f;
-    f.m = ld1(a.stats + 2 * row);
-    f.logs = ld1(a.stats + 2 * row + 1);
-    f.scale = a.scale;
-    const bool none = f.a == 0.0f && f.b == 0.0f;
     const int64_t head = V == 1 ? 0 : to_boundary(p, a.vocab), body = (a.vocab - head) / V;
-    auto one = [&](int64_t i) { st1(d + i, none ? 0.0f : f(ld1(p + i), i)); };
-    if (span == 0) {
-        if ((int64_t)threadIdx.x < head)
-            one(threadIdx.x);
-        const int64_t i = head + body * V + threadIdx.x;
-        if (i < a.vocab)
-            one(i);
-    }
     const int64_t i0 = span * (kBackThreads * kBackPieces) + threadIdx.x;
     Vec<T, V> v[kBackPieces];
 #pragma unroll
     for (int u = 0; u < kBackPieces; ++u)
-        if (!none && i0 + u * kBackThreads < body)
+        if (i0 + u * kBackThreads < body)
             v[u].load(p + head + (i0 + u * kBackThreads) * V);
+    const RowGradient<T> f(a, row);
+    if (V > 1 && span == 0) {
+        const int64_t end = threadIdx.x < 16 ? (threadIdx.x < head ? threadIdx.x : a.vocab)
+                                             : head + body * V + threadIdx.x - 16;
+        if (end < a.vocab)
+            st1(d + end, f(ld1(p + end), end));
+    }
 #pragma unroll
     for (int u = 0; u < kBackPieces; ++u) {
+        if (i0 + u * kBackThreads >= body)
+            break;
         const int64_t i = head + (i0 + u * kBackThreads) * V;
         float g[V];
 #pragma unroll
         for (int j = 0; j < V; ++j)
-            g[j] = none ? 0.0f : f(v[u].get(j), i + j);
+            g[j] = f.none ? 0.0f : f.other(v[u].get(j));
+        const int64_t at = f.id - i;
+        if (at >= 0 && at < V && !f.none)
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                g[j] = at == j ? f.own(v[u].get(j)) : g[j];
         Vec<T, V> o;
         o.set(g);
-        if (i0 + u * kBackThreads < body)
-            o.store(d + i);
+        o.store(d + i);
     }
 }
 
@@ -237,8 +320,8 @@ int check_rows(const char *what, int64_t rows, int64_t vocab, int dtype, float s
         return call_fail(DPO_EDTYPE, "%s: dtype %d", what, dtype);
     if (rows < 0 || rows >= kMaxCount / kMaxCtas || vocab < 1 || vocab >= kMaxCount - 1)
         return call_fail(DPO_EINVAL, "%s: %lld rows of %lld", what, (long long)rows, (long long)vocab);
-    if (!isfinite(scale) || !(scale > 0.0f))
-        return call_fail(DPO_EINVAL, "%s: scale %g", what, (double)scale);
+    if (!good_scale(scale))
+        return call_fail(DPO_EINVAL, "%s: scale %g (1e-20 to 1e6)", what, (double)scale);
     return DPO_OK;
 }
 

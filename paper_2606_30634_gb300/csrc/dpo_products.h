@@ -22,7 +22,8 @@ struct StoreProduct {
 
 constexpr int kMaxStoreProducts = 4;
 
-// Up to four of them in one launch, in whose order their tiles are begun (longest first).
+// Up to four of them, in one launch in whose order their tiles are begun (longest first), or the
+// first one before the others where its K is better split.
 int store_products(const char *what, const StoreProduct *p, int n, void *stream);
 
 // A head's logits x w^T: what their distributions need, by kHeadStatCols columns, or the logits

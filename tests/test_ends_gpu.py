@@ -267,9 +267,10 @@ def test_dropout_refusals(kw):
 # ------------------------------------------------------ log probabilities ----
 
 def scaled(logits, scale):
-    """z as the kernels form it, and in 64 bits."""
+    """z as the kernels form it, and in 64 bits but for what is infinite in fp32."""
     with np.errstate(over="ignore"):
-        return (np64(logits).astype(f32) * f32(scale)), np64(logits) * float(f32(scale))
+        z = np64(logits).astype(f32) * f32(scale)
+    return z, np.where(np.isinf(z), z, np64(logits) * float(f32(scale)))
 
 
 def bars_of(z, ids, vocab, zerr=0.0):
@@ -277,14 +278,17 @@ def bars_of(z, ids, vocab, zerr=0.0):
     logs, p, h = ref.distribution(z)
     with np.errstate(invalid="ignore"):
         m = z.max(1, keepdims=True)
-        d = np.where(p > 0, z - m, 0.0)
+        # of all numbers, those whose p is 0 in 64 bits too: z - m is rounded, u of its size,
+        # before log S is taken from it, u of the result (-4e16 of logits of 1e38 and a scale of
+        # 1e-20: 5e9)
+        d = np.where(np.isfinite(z), z - m, 0.0)
         az = np.where(np.isfinite(z), np.abs(z), 0.0)
     dz = U * (az + np.abs(m) + np.abs(d)) + zerr
     eps = dz + 1.5 * U * np.abs(d) + 2.0 ** -22
     n = max(64, vocab // 512 + 32)
     tot = (p * eps).sum(1) + (n + 64) * U + 16 * 2.0 ** -22
     logsum = np.abs(h) + (p * np.abs(d)).sum(1)
-    each = dz + tot[:, None] + 3 * U * (logsum[:, None] + np.where(p > 0, np.abs(logs), 0.0))
+    each = dz + tot[:, None] + 3 * U * (logsum[:, None] + np.where(np.isfinite(logs), np.abs(logs), 0.0))
     ent = tot + (p * np.abs(d) * (eps + tot[:, None])).sum(1) + (p * dz).sum(1) + 4 * U * (logsum + np.abs(h))
     r = np.arange(len(ids))
     real = (ids >= 0) & (ids < vocab)
@@ -313,17 +317,19 @@ def check_logprobs(x, ids, scale, top):
     bl, bh, each = bars_of(z, i, vocab)
     finite = np.isfinite(logp)
     got = np64(o.logp)
-    assert np.array_equal(got[~finite], logp[~finite])    # a masked id's -infinity
+    assert np.array_equal(got[~finite], logp[~finite], equal_nan=True)   # a masked id, no distribution
     within(got[finite], logp[finite], bl[finite], "logp")
     assert (got[(i < 0) | (i >= vocab)] == 0).all()
-    within(o.entropy, h, bh, "entropy")
+    got, some = np64(o.entropy), ~np.isnan(h)
+    assert np.isnan(got[~some]).all()
+    within(got[some], h[some], bh[some], "entropy")
     if top:
         want = ref.top(z32, top)
         assert np.array_equal(o.top_ids.cpu().numpy(), want)
         logs = ref.distribution(z)[0]
         wl = np.take_along_axis(logs, want, 1)
         gl, f = np64(o.top_logp), np.isfinite(wl)
-        assert np.array_equal(gl[~f], wl[~f])
+        assert np.array_equal(gl[~f], wl[~f], equal_nan=True)
         within(gl[f], wl[f], np.take_along_axis(each, want, 1)[f], "top logp")
     else:
         assert o.top_logp is None and o.top_ids is None
@@ -431,6 +437,21 @@ def test_rows_of_odd_values(dtype, vocab):
     assert torch.isfinite(d).all() and (d[[0, 2, 3, 5, 6, 7]] == 0).all()
     want = np.where(np.arange(vocab) == 2, 1.0, 0.0) - 1 / vocab
     assert np.allclose(np64(d[1]), want, atol=2.0 ** -8 + 1e-5)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale,size", [(1e-20, 1e38), (1e-20, 1e20), (1e6, 1e-6), (1e6, 1e30), (1.0, 1e37)])
+@pytest.mark.parametrize("top", [0, 7])
+def test_extreme_scales(dtype, scale, size, top):
+    """Logits of any size: their exponentials are 0 or 1 where they are far apart."""
+    x = randn(gen(9), 6, 2003, scale=1.0, dtype=torch.float32)
+    x[2] = -x[2].abs()
+    x[3, 5:] = -math.inf
+    x = (x * size).to(DT[dtype])
+    x[4] = torch.finfo(DT[dtype]).min
+    x[4, ::3] = -math.inf
+    x[5, 1:] = torch.finfo(DT[dtype]).min
+    check_logprobs(x, torch.tensor([0, 5, 2002, 1, 4, 0], device=DEV), scale, top)
 
 
 def test_ties_go_to_the_lowest_id():
