@@ -3,11 +3,13 @@
 //
 // Forward: out[t] = scale table[id_t]; one pass, the rows' bytes in and out.
 // Backward: dtable[v] = scale sum over the t with id_t = v of dy[t]. The tokens are sorted by id
-// (stably, so each id's tokens stay in order), and the sorted list is cut into chunks of
-// equal length; a CTA adds up the rows of a chunk, id by id, in fp32. An id's run within one
-// chunk is finished there; of one that crosses chunks every chunk leaves a partial sum, and
-// the chunks' sums are added in order. So the work is even whatever the ids are, and its
-// order depends on the ids alone.
+// (each id's tokens in order), and the sorted list is cut into chunks of equal length; a CTA adds
+// up the rows of a chunk, id by id, in fp32. An id's run within one chunk is finished there; of
+// one that crosses chunks every chunk leaves a partial sum, and the chunks' sums are added in a
+// fixed order. So the work is even whatever the ids are, and its order depends on the ids alone.
+// A gradient that is written is first cleared as a whole by CTAs beside the sort's, which leaves
+// HBM idle; the rows that ids have are written twice (8192 tokens of a 32000 x 4096 buffer: 75 us
+// when the sums' launch cleared the other rows, by a bit for each).
 #include "dpo_ends.cuh"
 #include "dpo_vec.cuh"
 
@@ -62,16 +64,44 @@ __global__ void __launch_bounds__(32 * kEmbedWarps) embed_kernel(const EmbedArgs
     }
 }
 
-// ---------------------------------------------------------------- sort ----
-// (id, token) pairs of up to DPO_EMBED_SPAN tokens by id, least significant digit first, in the
-// shared memory of one cluster: a launch, with the cluster's barrier between its steps. In a
-// pass every warp ranks its own 256 pairs, in their order, among those with the same digit
-// (match.any), the counts are added up over warps and CTAs, and the pairs are sent to their
-// places, wherever in the cluster these are. Padding sorts behind the last id.
-constexpr int kSortItems = 8, kSortThreads = 1024, kSortMinThreads = 128, kSortCtas = 8;
-constexpr int kDigitBits = 9;   // of a pass, at most
-static_assert(kSortItems * kSortThreads * kSortCtas == DPO_EMBED_SPAN, "a span is a cluster's");
+// ------------------------------------------------------------- clearing ----
+// dtable's rows as bytes, set to zero 4 KB a warp; contiguous rows are one.
+struct ClearArgs {
+    uint8_t *p;                // nullptr: nothing to clear
+    int64_t rows, bytes, pitch;
+    int size;                  // of an element, to whose multiple p is aligned
+};
+constexpr int kClearBytes = 4096;
 
+// By the CTAs from number `first` of the grid on.
+__device__ __forceinline__ void clear_rows(const ClearArgs &a, int first)
+{
+    const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+    const int64_t pieces = (a.bytes + kClearBytes - 1) / kClearBytes, all = a.rows * pieces;
+    const int64_t step = (int64_t)((int)gridDim.x - first) * warps;
+    for (int64_t u = (int64_t)((int)blockIdx.x - first) * warps + (threadIdx.x >> 5); u < all; u += step) {
+        const int64_t row = u / pieces, at = (u - row * pieces) * kClearBytes;
+        const int n = (int)min((int64_t)kClearBytes, a.bytes - at);
+        uint8_t *const p = a.p + row * a.pitch + at;
+        const int head = min((int)((16u - (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u)) & 15u), n);
+        const int body = (n - head) / 16 * 16;
+        auto ends = [&](uint8_t *q, int bytes) {   // less than 16 bytes
+            if (lane * a.size < bytes) {
+                if (a.size == 4)
+                    *reinterpret_cast<uint32_t *>(q + lane * 4) = 0u;
+                else
+                    *reinterpret_cast<uint16_t *>(q + lane * 2) = 0u;
+            }
+        };
+        ends(p, head);
+        for (int i = lane * 16; i < body; i += 512)
+            *reinterpret_cast<uint4 *>(p + head + i) = make_uint4(0u, 0u, 0u, 0u);
+        ends(p + head + body, n - head - body);
+    }
+}
+
+// ---------------------------------------------------------------- sort ----
+// (id, token) pairs by id, and then by token, padding behind the last id.
 struct SortArgs {
     Ids ids;
     int64_t first, count;      // tokens of this span
@@ -79,12 +109,93 @@ struct SortArgs {
     int passes, bits;          // of a pass
     uint2 *sorted;             // (id, token of the span)
     int *n_valid;              // how many are no padding
-    uint32_t *met;             // a bit for each id that is met
+    int ctas;                  // that sort; the others clear
+    ClearArgs clear;
 };
+
+// Up to 8192 tokens: a pair's place is the number of pairs before it, counted by comparing it
+// with all of them. 67 million comparisons of two instructions each are 4 us on all SMs, with
+// no step that waits for another (the cluster's sort below, two passes: 12).
+constexpr int kRankTokens = 8192, kRankBits = 13, kRankWarps = 8, kRankKeys = 7;   // keys of a warp
+constexpr int64_t kRankVocab = (int64_t)1 << (32 - kRankBits);
+
+__global__ void __launch_bounds__(32 * kRankWarps) rank_ids_kernel(const SortArgs a)
+{
+    __shared__ uint4 keys_[kRankTokens / 4];
+    pdl_wait();
+    if ((int)blockIdx.x >= a.ctas) {
+        clear_rows(a.clear, a.ctas);
+        return;
+    }
+    uint32_t *const keys = reinterpret_cast<uint32_t *>(keys_);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = (int)a.count;
+    const int padded = (n + 127) / 128 * 128;
+    bool valid = false;
+    int some = 0;
+    for (int i0 = 0; i0 < padded; i0 += 32 * kRankWarps * 4) {
+        uint32_t k[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = i0 + u * 32 * kRankWarps + (int)threadIdx.x;
+            const int id = i < n ? a.ids.at(a.first + i, a.vocab) : -1;
+            valid = id >= 0;
+            some += valid;
+            k[u] = valid ? (uint32_t)id << kRankBits | (uint32_t)i : ~0u;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = i0 + u * 32 * kRankWarps + (int)threadIdx.x;
+            if (i < padded)
+                keys[i] = k[u];
+        }
+    }
+    __shared__ int counts[kRankWarps];
+    some = __reduce_add_sync(0xFFFFFFFFu, some);
+    if (lane == 0)
+        counts[warp] = some;
+    __syncthreads();
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        int sum = 0;
+        for (int w = 0; w < kRankWarps; ++w)
+            sum += counts[w];
+        *a.n_valid = sum;
+    }
+    const int t0 = ((int)blockIdx.x * kRankWarps + warp) * kRankKeys;
+    if (t0 >= n)
+        return;
+    uint32_t mine[kRankKeys], before[kRankKeys];
+#pragma unroll
+    for (int j = 0; j < kRankKeys; ++j) {
+        mine[j] = t0 + j < n ? keys[t0 + j] : ~0u;
+        before[j] = 0u;
+    }
+#pragma unroll 2
+    for (int i = lane; i < padded / 4; i += 32) {
+        const uint4 q = keys_[i];
+#pragma unroll
+        for (int j = 0; j < kRankKeys; ++j)
+            before[j] += (uint32_t)(q.x < mine[j]) + (uint32_t)(q.y < mine[j]) + (uint32_t)(q.z < mine[j]) +
+                         (uint32_t)(q.w < mine[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < kRankKeys; ++j) {
+        const uint32_t place = __reduce_add_sync(0xFFFFFFFFu, before[j]);
+        if (lane == j && mine[j] != ~0u)
+            a.sorted[place] = make_uint2(mine[j] >> kRankBits, (uint32_t)(t0 + j));
+    }
+}
+
+// Others, up to DPO_EMBED_SPAN: least significant digit first, in the shared memory of one
+// cluster. In a pass every warp ranks its own 256 pairs, in their order, among those with the
+// same digit (match.any), the counts are added up over warps and CTAs, and the pairs are sent
+// to their places, wherever in the cluster these are.
+constexpr int kSortItems = 8, kSortThreads = 1024, kSortMinThreads = 128, kSortCtas = 8;
+constexpr int kDigitBits = 9;   // of a pass, at most
+static_assert(kSortItems * kSortThreads * kSortCtas == DPO_EMBED_SPAN, "a span is a cluster's");
 
 __host__ __device__ constexpr int sort_smem(int threads, int bits)
 {
-    return threads * kSortItems * 8 + (threads / 32 + 2) * (1 << bits) * 4;
+    return threads * kSortItems * 8 + (threads / 32 + kSortCtas + 1) * (1 << bits) * 4;
 }
 
 __global__ void __launch_bounds__(kSortThreads) sort_ids_kernel(const SortArgs a)
@@ -96,14 +207,17 @@ __global__ void __launch_bounds__(kSortThreads) sort_ids_kernel(const SortArgs a
     const int per = nt * kSortItems, digits = 1 << a.bits;
     uint2 *const items = reinterpret_cast<uint2 *>(smem);
     uint32_t *const count = reinterpret_cast<uint32_t *>(items + per);   // [warp][digit]
-    uint32_t *const total = count + warps * digits;                      // of this CTA
-    uint32_t *const base = total + digits;                               // first place, in all
+    uint32_t *const total = count + warps * digits;                      // [CTA][digit]
+    uint32_t *const base = total + kSortCtas * digits;                   // first place, in all
     uint32_t *const mine = count + warp * digits;
     const uint32_t pad = (uint32_t)a.vocab;
     const int at0 = warp * 32 * kSortItems + lane;
     pdl_wait();
-    for (int64_t i = (int64_t)rank * nt + threadIdx.x; i < (a.vocab + 31) / 32; i += ranks * nt)
-        a.met[i] = 0u;
+    if ((int)blockIdx.x >= a.ctas) {   // whole clusters
+        clear_rows(a.clear, a.ctas);
+        return;
+    }
+    cluster_barrier();   // the others' shared memory is written before the next one
     uint32_t key[kSortItems], pos[kSortItems], place[kSortItems];
 #pragma unroll
     for (int i = 0; i < kSortItems; ++i) {
@@ -134,12 +248,16 @@ __global__ void __launch_bounds__(kSortThreads) sort_ids_kernel(const SortArgs a
         __syncthreads();
         for (int d = threadIdx.x; d < digits; d += nt) {   // counts of earlier warps
             uint32_t sum = 0;
+#pragma unroll 4
             for (int w = 0; w < warps; ++w) {
                 const uint32_t c = count[w * digits + d];
                 count[w * digits + d] = sum;
                 sum += c;
             }
-            total[d] = sum;
+            // to every CTA: a store is not waited for, and what was fetched from eight others
+            // one after the other took 4 of a pass's 8 us
+            for (uint32_t r = 0; r < ranks; ++r)
+                st_cluster(in_cta(total + rank * digits + d, r), sum);
         }
         cluster_barrier();
         // first places: digits below, then the same digit in earlier CTAs
@@ -149,8 +267,9 @@ __global__ void __launch_bounds__(kSortThreads) sort_ids_kernel(const SortArgs a
             const int d = threadIdx.x * each + j;
             if (d < digits) {
                 uint32_t all = 0, earlier = 0;
-                for (uint32_t r = 0; r < ranks; ++r) {
-                    const uint32_t c = ld_cluster(in_cta(total + d, r));
+#pragma unroll
+                for (uint32_t r = 0; r < kSortCtas; ++r) {
+                    const uint32_t c = r < ranks ? total[r * digits + d] : 0u;
                     earlier += r < rank ? c : 0u;
                     all += c;
                 }
@@ -197,8 +316,6 @@ __global__ void __launch_bounds__(kSortThreads) sort_ids_kernel(const SortArgs a
                                          : ~0u;
         if (key[i] != pad) {
             a.sorted[g] = make_uint2(key[i], pos[i]);
-            if (prev != key[i])
-                atomicOr(a.met + key[i] / 32, 1u << key[i] % 32);
             if (g + 1 == (int64_t)ranks * per)
                 *a.n_valid = (int)(g + 1);
         } else if (prev != pad) {
@@ -212,17 +329,14 @@ __global__ void __launch_bounds__(kSortThreads) sort_ids_kernel(const SortArgs a
 constexpr int kSumThreads = 128, kSumRows = 8;   // rows requested at a time
 constexpr int kSpan = 32;                        // pairs of a chunk, at least
 constexpr int kMaxChunk = DPO_EMBED_SPAN / 256;
-constexpr int kZeroRows = 16;                    // rows that a CTA looks at for clearing
 
 struct SumArgs {
     const void *dy;
     void *dtable;
     const uint2 *sorted;
     const int *n_valid;
-    const uint32_t *met;
     float *partial;            // [chunk][begun here, not here][dim]
-    int64_t vocab, dim, ld_dy, ld_dtable;
-    int64_t sums;              // CTAs that add; the others clear the rows that no id has
+    int64_t dim, ld_dy, ld_dtable;
     int chunk, segs;
     float scale;
     int accumulate;
@@ -261,28 +375,13 @@ __device__ __forceinline__ void finish(const SumArgs &a, uint32_t id, int64_t c,
     o.store(p);
 }
 
-// CTAs [0, sums): a chunk of the sorted pairs and 128 V columns, a thread V of them. The
-// others: rows of dtable that no id has, set to zero.
+// A CTA: a chunk of the sorted pairs and 128 V columns, a thread V of them.
 template <class T, class GT, int V>
 __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const SumArgs a)
 {
     __shared__ uint2 pair_[kMaxChunk + 2];
     uint2 *const pair = pair_ + 1;
     pdl_wait();
-    if (blockIdx.x >= a.sums) {
-        const int64_t r0 = ((int64_t)blockIdx.x - a.sums) * kZeroRows;
-        Vec<GT, V> o;
-        o.zero();
-        for (int i = threadIdx.x >> 5; i < kZeroRows && r0 + i < a.vocab; i += kSumThreads / 32) {
-            const int64_t r = r0 + i;
-            if (a.met[r / 32] >> (r % 32) & 1u)
-                continue;
-            GT *const p = static_cast<GT *>(a.dtable) + r * a.ld_dtable;
-            for (int64_t c = (int64_t)(threadIdx.x & 31) * V; c < a.dim; c += 32 * V)
-                o.store(p + c);
-        }
-        return;
-    }
     const int chunk = (int)blockIdx.x / a.segs, seg = (int)blockIdx.x - chunk * a.segs;
     const int n = ld_int(a.n_valid), i0 = chunk * a.chunk;
     const int len = min(a.chunk, n - i0);
@@ -330,44 +429,58 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const SumArgs a)
     }
 }
 
-// The runs that cross chunks: the CTA of the chunk where one begins adds its chunks' sums.
+// The runs that cross chunks: the CTA of the chunk where one begins adds its chunks' sums, its four
+// warps every fourth of them, 32 V columns a CTA.
+constexpr int kJoinWarps = kSumThreads / 32;
+
 template <class GT, int V>
 __global__ void __launch_bounds__(kSumThreads) embed_join_kernel(const SumArgs a)
 {
+    __shared__ float sums[kJoinWarps - 1][32 * V];
     pdl_wait();
-    const int chunk = (int)blockIdx.x / a.segs, seg = (int)blockIdx.x - chunk * a.segs;
-    const int n = ld_int(a.n_valid), i0 = chunk * a.chunk, i1 = i0 + a.chunk, lane = threadIdx.x & 31;
-    if (i1 >= n)
-        return;
-    const uint32_t id = ld_pair(a.sorted + i1 - 1).x;
-    if (ld_pair(a.sorted + i1).x != id)
-        return;
-    if (i0 > 0 && ld_pair(a.sorted + i0 - 1).x == id)
-        return;   // begun before this chunk
+    const int segs = (int)((a.dim + 32 * V - 1) / (32 * V));
+    const int chunk = (int)blockIdx.x / segs, seg = (int)blockIdx.x - chunk * segs;
+    const int i0 = chunk * a.chunk, i1 = i0 + a.chunk, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    // all at once: the list has room for the pair after this chunk, which is not the last one
+    const uint32_t id = ld_pair(a.sorted + i1 - 1).x, after = ld_pair(a.sorted + i1).x,
+                   before = i0 > 0 ? ld_pair(a.sorted + i0 - 1).x : ~id;
+    const int n = ld_int(a.n_valid);
+    if (i1 >= n || after != id || before == id)
+        return;   // ends here, or was begun before this chunk
     int last = chunk + 1;   // the chunk where it ends: the next one does not begin with it
     for (;; last += 32) {
         const int64_t next = (int64_t)(last + lane + 1) * a.chunk;
-        const unsigned ends =
-            __ballot_sync(0xFFFFFFFFu, next >= n || ld_pair(a.sorted + next).x != id);
+        const uint32_t key = ld_pair(a.sorted + (next < n ? next : i1)).x;
+        const unsigned ends = __ballot_sync(0xFFFFFFFFu, next >= n || key != id);
         if (ends != 0u) {
             last += __ffs(ends) - 1;
             break;
         }
     }
-    const int64_t c = ((int64_t)seg * kSumThreads + threadIdx.x) * V;
-    if (c >= a.dim)
-        return;
-    float sum[V];
-    const float *p = a.partial + (int64_t)chunk * 2 * a.dim + c;
+    const int64_t c = ((int64_t)seg * 32 + lane) * V;
+    const bool in = c < a.dim;
+    float sum[V] = {};
+    // the chunk's own sum, then those of runs that did not begin where they lie
+#pragma unroll 4
+    for (int k = chunk + warp; k <= last; k += kJoinWarps) {
+        const float *const p = a.partial + ((int64_t)k * 2 + (k != chunk)) * a.dim + c;
+        if (in)
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-        sum[j] = p[j];
-    p += 3 * a.dim;   // the next chunk's run that did not begin there
-#pragma unroll 8
-    for (int k = chunk + 1; k <= last; ++k, p += 2 * a.dim)
+            for (int j = 0; j < V; ++j)
+                sum[j] += p[j];
+    }
+    if (warp > 0)
 #pragma unroll
         for (int j = 0; j < V; ++j)
-            sum[j] += p[j];
+            sums[warp - 1][lane * V + j] = sum[j];
+    __syncthreads();
+    if (warp > 0 || !in)
+        return;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps - 1; ++w)
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            sum[j] += sums[w][lane * V + j];
     finish<GT, V>(a, id, c, sum);
 }
 
@@ -416,9 +529,9 @@ int check_table(const char *what, int64_t vocab, int64_t dim, float scale)
 // The workspace of a span, and how its sorted pairs are cut.
 struct Plan {
     int chunk, chunks;
-    int64_t sorted, met, partial, bytes;   // where each begins; n_valid is at 0
+    int64_t sorted, partial, bytes;   // where each begins; n_valid is at 0
 };
-Plan plan_of(int64_t tokens, int64_t vocab, int64_t dim)
+Plan plan_of(int64_t tokens, int64_t dim)
 {
     auto up = [](int64_t v) { return (v + 255) / 256 * 256; };
     const int64_t n = tokens < DPO_EMBED_SPAN ? tokens : DPO_EMBED_SPAN;
@@ -428,8 +541,7 @@ Plan plan_of(int64_t tokens, int64_t vocab, int64_t dim)
         p.chunk *= 2;
     p.chunks = (int)((n + p.chunk - 1) / p.chunk);
     p.sorted = 256;
-    p.met = p.sorted + up(n * 8);
-    p.partial = p.met + up((vocab + 31) / 32 * 4);
+    p.partial = p.sorted + up(n * 8);
     p.bytes = p.partial + (p.chunks > 1 ? up((int64_t)p.chunks * 2 * dim * 4) : 0);
     return p;
 }
@@ -485,7 +597,7 @@ extern "C" int dpo_embed_workspace(int64_t tokens, int64_t vocab, int64_t dim, i
         return rc;
     if (bytes == nullptr || tokens < 0 || tokens >= kMaxCount)
         return call_fail(DPO_EINVAL, "%s: %lld tokens", what, (long long)tokens);
-    *bytes = plan_of(tokens, vocab, dim).bytes;
+    *bytes = plan_of(tokens, dim).bytes;
     return DPO_OK;
 }
 
@@ -503,7 +615,7 @@ extern "C" int dpo_embed_backward(const dpo_embed_backward_args *args, void *cud
     if (rc != DPO_OK || (rc = check_ids(what, a.ids, &so.ids, &tokens)) != DPO_OK)
         return rc;
     const int64_t size = elem_size(a.dtype), gsize = elem_size(a.grad_dtype);
-    const Plan plan = plan_of(tokens, a.vocab, a.dim);
+    const Plan plan = plan_of(tokens, a.dim);
     Buffers b(what);
     b.add("dtable", a.dtable, a.vocab, a.dim, a.ld_dtable, gsize, gsize, true);
     if (tokens == 0) {
@@ -531,9 +643,8 @@ extern "C" int dpo_embed_backward(const dpo_embed_backward_args *args, void *cud
     su.dtable = a.dtable;
     su.n_valid = so.n_valid = reinterpret_cast<int *>(ws);
     su.sorted = so.sorted = reinterpret_cast<uint2 *>(ws + plan.sorted);
-    su.met = so.met = reinterpret_cast<uint32_t *>(ws + plan.met);
     su.partial = reinterpret_cast<float *>(ws + plan.partial);
-    su.vocab = so.vocab = a.vocab;
+    so.vocab = a.vocab;
     su.dim = a.dim;
     su.ld_dy = a.ld_dy;
     su.ld_dtable = a.ld_dtable;
@@ -546,9 +657,12 @@ extern "C" int dpo_embed_backward(const dpo_embed_backward_args *args, void *cud
         ++bits;
     so.passes = (bits + kDigitBits - 1) / kDigitBits;
     so.bits = (bits + so.passes - 1) / so.passes;
-    const int64_t clears = (a.vocab + kZeroRows - 1) / kZeroRows;
-    if ((int64_t)plan.chunks * su.segs + clears >= kMaxCount)
-        return call_fail(DPO_EINVAL, "%s: %lld x %lld is too large", what, (long long)a.vocab, (long long)a.dim);
+    const int64_t joins = (a.dim + 32 * w.v - 1) / (32 * w.v);
+    if ((int64_t)plan.chunks * joins >= kMaxCount)
+        return call_fail(DPO_EINVAL, "%s: %lld columns are too many", what, (long long)a.dim);
+    const int sms = sm_count();
+    if (sms == 0)
+        return call_fail(DPO_ECUDA, "%s: no device", what);
     const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(sort_ids_kernel),
                                                cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                sort_smem(kSortThreads, kDigitBits));
@@ -559,24 +673,38 @@ extern "C" int dpo_embed_backward(const dpo_embed_backward_args *args, void *cud
     for (int64_t first = 0; first < tokens; first += DPO_EMBED_SPAN) {
         so.first = first;
         so.count = tokens - first < DPO_EMBED_SPAN ? tokens - first : DPO_EMBED_SPAN;
-        int threads = kSortMinThreads, ctas = 1;
-        while (threads < kSortThreads && (int64_t)threads * kSortItems < so.count)
-            threads *= 2;
-        while ((int64_t)ctas * threads * kSortItems < so.count)
-            ctas *= 2;
-        rc = launch_in_clusters(what, sort_ids_kernel, ctas, ctas, threads, (size_t)sort_smem(threads, so.bits),
-                                cuda_stream, so);
+        int64_t clears = 0;
+        so.clear = {};
+        if (!a.accumulate && first == 0) {
+            const bool whole = a.ld_dtable == a.dim;
+            so.clear = {static_cast<uint8_t *>(a.dtable), whole ? 1 : a.vocab,
+                        (whole ? a.vocab : 1) * a.dim * gsize, a.ld_dtable * gsize, (int)gsize};
+            clears = (so.clear.rows * ((so.clear.bytes + kClearBytes - 1) / kClearBytes) + 31) / 32;
+            clears = clears < (int64_t)sms * 4 ? clears : (int64_t)sms * 4;
+        }
+        if (so.count <= kRankTokens && a.vocab < kRankVocab) {
+            so.ctas = (int)((so.count + kRankWarps * kRankKeys - 1) / (kRankWarps * kRankKeys));
+            rc = launch(what, rank_ids_kernel, so.ctas + clears, 32 * kRankWarps, 0, cuda_stream, so);
+        } else {   // small CTAs first: the ranking's votes and the counts' sums on as many SMs
+            int threads = kSortMinThreads, ctas = 1;
+            while (ctas < kSortCtas && (int64_t)ctas * threads * kSortItems < so.count)
+                ctas *= 2;
+            while ((int64_t)ctas * threads * kSortItems < so.count)
+                threads *= 2;
+            so.ctas = ctas;
+            rc = launch_in_clusters(what, sort_ids_kernel, ctas + (clears + ctas - 1) / ctas * ctas, ctas,
+                                    threads, (size_t)sort_smem(threads, so.bits), cuda_stream, so);
+        }
         if (rc != DPO_OK)
             return rc;
         su.dy = static_cast<const uint8_t *>(a.dy) + first * a.ld_dy * size;
         su.accumulate = a.accumulate || first > 0;
         const int chunks = (int)((so.count + su.chunk - 1) / su.chunk);
-        su.sums = (int64_t)chunks * su.segs;
-        rc = launch(what, sum_fn(a.dtype, a.grad_dtype, w.v, false), su.sums + (su.accumulate ? 0 : clears),
-                    kSumThreads, 0, cuda_stream, su);
+        rc = launch(what, sum_fn(a.dtype, a.grad_dtype, w.v, false), (int64_t)chunks * su.segs, kSumThreads, 0,
+                    cuda_stream, su);
         if (rc == DPO_OK && chunks > 1)
-            rc = launch(what, sum_fn(a.dtype, a.grad_dtype, w.v, true), (int64_t)(chunks - 1) * su.segs,
-                        kSumThreads, 0, cuda_stream, su);
+            rc = launch(what, sum_fn(a.dtype, a.grad_dtype, w.v, true), (chunks - 1) * joins, kSumThreads, 0,
+                        cuda_stream, su);
         if (rc != DPO_OK)
             return rc;
     }

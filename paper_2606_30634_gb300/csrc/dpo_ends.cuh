@@ -44,6 +44,10 @@ __device__ __forceinline__ uint32_t ld_cluster(uint32_t addr)
     return v;
 }
 __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) { return __uint_as_float(ld_cluster(addr)); }
+__device__ __forceinline__ void st_cluster(uint32_t addr, uint32_t a)
+{
+    asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(addr), "r"(a) : "memory");
+}
 __device__ __forceinline__ void st_cluster(uint32_t addr, uint32_t a, uint32_t b)
 {
     asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
