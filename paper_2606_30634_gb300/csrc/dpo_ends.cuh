@@ -22,11 +22,20 @@ __device__ __forceinline__ uint32_t ctas_of_cluster()
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
     return r;
 }
+// The two halves of the cluster's barrier.
+__device__ __forceinline__ void cluster_arrive()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait()
+{
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 // By all threads of the cluster; orders their accesses to its shared and to global memory.
 __device__ __forceinline__ void cluster_barrier()
 {
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    cluster_arrive();
+    cluster_wait();
 }
 // The address of p, in this CTA's shared memory, in that of another CTA of the cluster.
 __device__ __forceinline__ uint32_t in_cta(const void *p, uint32_t rank)

@@ -3,7 +3,9 @@
 //
 // Forward: every logit is read once; a thread keeps the running maximum m, sum S and entropy
 // sum W of its own, and the threads' are joined. Backward: every logit once more, dlogits
-// written. Both are bound by HBM; few rows by latency, where a cluster shares a row.
+// written. Both are bound by HBM (4096 x 50257 bf16: 71 and 132 us, 5.8 and 6.2 TB/s); few rows
+// by latency, where a cluster shares a row. What instructions they take is seen: with 15 an
+// element instead of 6 the forward took 107 us, with 20 instead of 7 the backward 180.
 #include "dpo_logprobs.cuh"
 
 namespace dpo {
@@ -19,6 +21,7 @@ struct LogArgs {
     int64_t rows, vocab, ld;
     float scale;
     int top;
+    int warps;                   // of a row: all of the CTA's, or one
 };
 
 // Elements before the first 16-byte boundary, at most n.
@@ -28,167 +31,223 @@ template <class T> __device__ __forceinline__ int64_t to_boundary(const T *p, in
     return k < n ? k : n;
 }
 
-// The warps' lists, in shared memory, merged into the first one's p.
-__device__ __forceinline__ void merge_warps(Pair &p, Pair (*lists)[32], int warps, int warp, int lane)
+// By all threads that have a row.
+__device__ __forceinline__ void row_sync(int warps)
+{
+    if (warps == 1)
+        __syncwarp();
+    else
+        __syncthreads();
+}
+
+// The warps' sorted lists, in shared memory, merged into the first one's p.
+template <class K>
+__device__ __forceinline__ void merge_warps(K &p, K (*lists)[32], int warps, int warp, int lane)
 {
     lists[warp][lane] = p;
     for (int step = 1; step < warps; step *= 2) {
         __syncthreads();
         if (warp % (2 * step) == 0) {   // the number of warps is a power of two
-            merge_pairs(p, lists[warp + step][31 - lane], lane);
+            merge_lanes(p, lists[warp + step][31 - lane], lane);
             lists[warp][lane] = p;
         }
     }
-    __syncthreads();
+    row_sync(warps);
 }
 
-// A cluster's CTAs share a row, in equal spans; accesses of 16 bytes from the span's first
-// boundary on, so rows of odd pitches cost two short ends.
+// A warp, a CTA or a cluster has a row, a cluster's CTAs in equal spans; accesses of 16 bytes from the span's first
+// boundary on, so rows of odd pitches cost two short ends. A thread takes kBatch logits at a time,
+// their largest first.
 // The `top` largest: each thread knows the largest of its own values, and the top-th of these
-// bounds the top-th of all from below. So only the threads that hold one of the first `top`
-// of them, `top` threads at most, can hold others, and their values alone are read again.
+// bounds the top-th of all from below. So only the threads whose largest reaches the bound, `top`
+// and what is equal, can hold one of them; their values are read again, and what reaches the
+// bound is sorted, or offered to lists where it is much (equal values, masked rows).
+// us by the threads of a row, 32 / 128 / 512: 4096 rows of 50257 bf16 71 / 77 / 104, 300 of 32000
+// fp32 - / 12.4 / 9.4; with 5 of 1000 rows of 32000 fp32 64 / 128 / 256: 25.7 / 25.6 / 27.2, 4000
+// rows 117 / 92 / 92 (a bound from few threads lets more values be read again). 4000 rows of
+// 32000 fp32: 76 us, 6.7 TB/s, 0.99 of the measured copy.
+constexpr int kBatch = 32, kSmThreads = 800, kTopThreads = 128;
+
 template <class T, bool TOP>
-__global__ void __launch_bounds__(kMaxThreads) logprobs_kernel(const LogArgs a)
+__global__ void __launch_bounds__(kMaxThreads, 2) logprobs_kernel(const LogArgs a)
 {
-    constexpr int V = 16 / (int)sizeof(T), U = 4;
-    __shared__ Part parts[kMaxWarps];
-    __shared__ Pair lists[TOP ? kMaxWarps : 1][32];
-    const int nt = blockDim.x, warps = nt >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    using Access = RowAccess<T>;
+    constexpr int V = Access::V, U = kBatch / V;
+    __shared__ Part parts[kMaxWarps], from_cta[kMaxCtas];
+    constexpr int kLists = TOP ? kMaxWarps : 1;
+    __shared__ Key lists_[kLists][32], list_from[TOP ? kMaxCtas : 1][32];
+    __shared__ float largest_[kLists][32];
+    __shared__ uint16_t chosen_[TOP ? kMaxThreads : 1];
+    __shared__ int counts_[kLists][2];
+    const int warps = a.warps, nt = 32 * warps, lane = threadIdx.x & 31;
+    const int first_warp = warps == 1 ? (int)threadIdx.x >> 5 : 0;   // of this row
+    const int warp = ((int)threadIdx.x >> 5) - first_warp, thread = 32 * warp + lane;
     const uint32_t rank = cta_of_cluster(), ranks = ctas_of_cluster();
-    const int64_t row = blockIdx.x / ranks;
-    const int64_t share = (a.vocab + ranks - 1) / ranks, begin = min(share * rank, a.vocab);
-    const int64_t n = min(share, a.vocab - begin);
+    const int64_t its = ranks > 1 ? blockIdx.x / ranks : (int64_t)blockIdx.x * (blockDim.x / nt) + first_warp;
+    const int64_t row = min(its, a.rows - 1);
+    Key (*const lists)[32] = lists_ + (TOP ? first_warp : 0);
+    const int vocab = (int)a.vocab, share = (int)((a.vocab + ranks - 1) / ranks);
+    const int begin = (int)min((int64_t)share * rank, a.vocab), n = min(share, vocab - begin);
+    if (ranks > 1)
+        cluster_arrive();   // its shared memory may be written from now on
     pdl_wait();
+    const bool last = rank == 0 && warp == 0 && its < a.rows;   // the warp that ends the row
+    int id = -1;
+    if (last && a.logp != nullptr)
+        id = a.ids.at(row, a.vocab);
     const T *const p = static_cast<const T *>(a.logits) + row * a.ld + begin;
     const int head = (int)to_boundary(p, n);
-    const int64_t body = (n - head) / V, tail = head + body * V;
+    const int body = (n - head) / V, tail = head + body * V;
     const T *const vectors = p + head;
-    // where ids are wanted the values are the products z, else the logits themselves
-    const float pre = TOP ? a.scale : 1.0f, c = TOP ? kLog2e : a.scale * kLog2e;
-    const float low = -Run::kLow / 10 * pre;
+    const float c = a.scale * kLog2e;
+    const Two cc = two(c, c);
     Run run;
-    int64_t best = threadIdx.x;   // the access with this thread's largest value
-    for (int64_t i0 = threadIdx.x; i0 < body; i0 += (int64_t)nt * U) {
-        Vec<T, V> v[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (i0 + (int64_t)u * nt < body)
-                v[u].load(vectors + (i0 + (int64_t)u * nt) * V);
+    for (int i0 = thread; i0 < body; i0 += nt * U) {
+        Access v[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (i0 + (int64_t)u * nt >= body)
-                break;
-            float l[V], k[V];
-            float top = open_row(v[u], l, k);
-            if (TOP) {
+            if (i0 + u * nt < body)
+                v[u].v.load(vectors + (int64_t)(i0 + u * nt) * V);
+            else
+                v[u].none();
+        }
+        float top = v[0].largest();
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    l[j] = __fmul_rn(l[j], pre);
-                    k[j] = __fmul_rn(k[j], pre);
-                }
-                top = __fmul_rn(top, pre);
-                if (top > run.m)
-                    best = i0 + (int64_t)u * nt;
+        for (int u = 1; u < U; ++u)
+            top = fmaxf(top, v[u].largest());
+        if (top > run.m)
+            run.raise(top, c);
+        if (run.near()) {
+            const Two minus_r = two(-run.r, -run.r);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (i0 + u * nt >= body)
+                    break;
+#pragma unroll
+                for (int j = 0; j < V / 2; ++j)
+                    run.add_near(v[u].pair(j, Access::kLow), cc, minus_r);
             }
-            run.add(l, k, top, c, low);
-        }
-    }
-    Pair mine;
-    if (TOP && threadIdx.x < body) {
-        Vec<T, V> v;
-        v.load(vectors + best * V);
-        mine.v = run.m;
+        } else {
 #pragma unroll
-        for (int j = V - 1; j >= 0; --j) {
-            const float z = __fmul_rn(v.get(j), pre);
-            if ((z == z ? z : -INFINITY) == run.m)
-                mine.id = (int)(begin + head + best * V + j);
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    run.add_far(v[u].v.get(j), c);
         }
     }
-    // the short ends: the first warp's lanes, one element each (V <= 8 of either)
-    const int64_t end = lane < 16 ? (lane < head ? lane : -1) : tail + lane - 16 < n ? tail + lane - 16 : -1;
-    float end_z = -INFINITY;
-    if (warp == 0 && end >= 0) {
-        const float l[1] = {__fmul_rn(ld1(p + end), pre)};
-        const float k[1] = {l[0] == l[0] ? fmaxf(l[0], -Run::kLow * pre) : l[0]};
-        end_z = l[0];
-        run.add(l, k, l[0], c, low);
+    float bound = TOP ? __fmul_rn(run.m, a.scale) : 0.0f;
+    // the short ends: a row's first warp's lanes, one element each (V <= 8 of either)
+    const int at_end = lane < 16 ? lane : tail + lane - 16;
+    const int end = warp == 0 && at_end < (lane < 16 ? head : n) ? at_end : -1;
+    float end_z = -INFINITY, own = 0.0f;
+    if (end >= 0) {
+        const float l = ld1(p + end);
+        end_z = __fmul_rn(l, a.scale);
+        run.add(l, c);
     }
+    if (id >= 0)
+        own = ld1(static_cast<const T *>(a.logits) + row * a.ld + id);
 
-    Part part = run.part(TOP ? 1.0f : a.scale);
+    Part part = run.part(a.scale);
     part.warp_join();
-    if (lane == 0)
+    if (lane == 0 && warps > 1)
         parts[warp] = part;
+    Key mine = 0;
     if (TOP) {
-        sort_pairs(mine, lane);
-        merge_warps(mine, lists, warps, warp, lane);
-        TopList more;   // what the others left out
-        more.top = a.top;
-        more.lane = lane;
-        more.last = lists[0][a.top - 1];
-        for (int i = warp; i < a.top; i += warps) {
-            const int id = lists[0][i].id;
-            if (id == 0x7FFFFFFF)
-                break;
-            const int64_t own = (id - begin - head) / V % nt;
-            for (int64_t q0 = own; q0 < body; q0 += 32 * (int64_t)nt) {
-                const int64_t q = q0 + lane * (int64_t)nt;
-                Vec<T, V> v;
-                v.zero();
-                if (q < body)
-                    v.load(vectors + q * V);
+        uint16_t *const chosen = chosen_ + 32 * first_warp;
+        int *const counts = counts_[first_warp];   // of threads, of values
+        const float own_largest = bound;
+        if (thread < 2)
+            counts[thread] = 0;
+        sort_lanes(bound, lane);
+        merge_warps(bound, largest_ + first_warp, warps, warp, lane);
+        bound = largest_[first_warp][a.top - 1];
+        if (thread < body && own_largest >= bound)
+            chosen[atomicAdd(counts, 1)] = (uint16_t)thread;
+        row_sync(warps);
+        // 32 of a thread's accesses are a block; the warps take the blocks in turn
+        const int blocks = (body + 32 * nt - 1) / (32 * nt), all = counts[0] * blocks;
+        auto scan = [&](auto &&use) {   // by whole warps
+            constexpr int kAhead = 2;
+            for (int k0 = warp; k0 < all; k0 += warps * kAhead) {
+                Access v[kAhead];
+                int q[kAhead];
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const int at = (int)(begin + head + q * V + j);
-                    const bool in = q < body && at != id;
-                    more.offer(in ? __fmul_rn(v.get(j), pre) : -INFINITY, in ? at : 0x7FFFFFFF);
+                for (int u = 0; u < kAhead; ++u) {
+                    const int k = k0 + u * warps, i = k / blocks;
+                    v[u].none();
+                    q[u] = k < all ? chosen[i] + ((k - i * blocks) * 32 + lane) * nt : body;
+                    if (q[u] < body)
+                        v[u].v.load(vectors + (int64_t)q[u] * V);
+                }
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    const bool in = q[u] < body && !(__fmul_rn(v[u].largest(), a.scale) < bound);
+                    if (__any_sync(0xFFFFFFFFu, in))
+#pragma unroll
+                        for (int j = 0; j < V; ++j)
+                            use(in, __fmul_rn(v[u].v.get(j), a.scale), begin + head + q[u] * V + j);
                 }
             }
-        }
-        if (warp == 0)
-            more.offer(end_z, end >= 0 ? (int)(begin + end) : 0x7FFFFFFF);
-        if (__syncthreads_or(more.p.id != 0x7FFFFFFF)) {
-            Pair base = mine;   // the first warp's
-            merge_warps(more.p, lists, warps, warp, lane);
-            if (warp == 0) {
-                merge_pairs(base, shfl(more.p, 31 - lane), lane);
-                mine = base;
+            if (warp == 0)
+                use(end >= 0, end_z, begin + end);
+        };
+        scan([&](bool in, float z, int at) {
+            if (in && !(z < bound) && (z == z || bound == -INFINITY)) {
+                const int slot = atomicAdd(counts + 1, 1);
+                if (slot < nt)
+                    lists[0][slot] = key_of(z, at);
             }
+        });
+        row_sync(warps);
+        const int found = counts[1];
+        if (found <= nt) {
+            mine = thread < found ? lists[warp][lane] : 0;
+            if (32 * warp < found)
+                sort_lanes(mine, lane);
+            if (found > 32)
+                merge_warps(mine, lists, warps, warp, lane);
+        } else {
+            TopList list{0, key_of(bound, 0x7FFFFFFF), a.top, lane};
+            row_sync(warps);
+            scan([&](bool in, float z, int at) { list.offer(in ? key_of(z, at) : 0); });
+            mine = list.p;
+            merge_warps(mine, lists, warps, warp, lane);
         }
-    } else {
+    } else if (warps > 1) {
         __syncthreads();
     }
-    if (warp == 0)
-        for (int w = 1; w < warps; ++w)
-            part.join(parts[w]);
-    if (ranks > 1) {
-        if (warp == 0) {
-            if (lane == 0)
-                parts[0] = part;
+    if (warp == 0 && warps > 1) {
+        part = lane < warps ? parts[lane] : Part();
+        part.warp_join();
+    }
+    if (ranks > 1) {   // the first CTA gets the others' parts; all of its warps are there (ranks <= warps)
+        cluster_wait();
+        if (warp == 0 && rank > 0) {
+            if (lane == 0) {
+                const uint32_t at = in_cta(&from_cta[rank], 0);
+                st_cluster(at, __float_as_uint(part.m));
+                st_cluster(at + 4, __float_as_uint(part.s));
+                st_cluster(at + 8, __float_as_uint(part.w));
+            }
             if (TOP)
-                lists[0][lane] = mine;
+                st_cluster(in_cta(&list_from[rank][lane], 0), (uint32_t)mine, (uint32_t)(mine >> 32));
         }
         cluster_barrier();
-        if (rank == 0 && warp == 0) {
-            for (uint32_t r = 1; r < ranks; ++r) {
-                Part o;
-                const uint32_t at = in_cta(&parts[0], r);
-                o.m = ld_cluster_f32(at);
-                o.s = ld_cluster_f32(at + 4);
-                o.w = ld_cluster_f32(at + 8);
-                part.join(o);
-                if (TOP) {
-                    const uint32_t q = in_cta(&lists[0][31 - lane], r);
-                    Pair other;
-                    other.v = ld_cluster_f32(q);
-                    other.id = (int)ld_cluster(q + 4);
-                    merge_pairs(mine, other, lane);
-                }
-            }
+        if (rank != 0)
+            return;
+        if (TOP) {
+            if (warp > 0)
+                mine = warp < (int)ranks ? list_from[warp][lane] : 0;
+            merge_warps(mine, lists, (int)ranks, warp, lane);
         }
-        cluster_barrier();   // no CTA leaves while the first may read its part
+        if (warp == 0) {
+            const Part o = lane > 0 && lane < (int)ranks ? from_cta[lane] : Part();
+            part = lane == 0 ? part : o;
+            part.warp_join();
+        }
     }
-    if (rank != 0 || warp != 0)
+    if (!last)
         return;
     const float logs = part.log_sum();
     if (lane == 0) {
@@ -196,17 +255,12 @@ __global__ void __launch_bounds__(kMaxThreads) logprobs_kernel(const LogArgs a)
         a.stats[2 * row + 1] = logs;
         if (a.entropy != nullptr)
             a.entropy[row] = part.entropy();
-        if (a.logp != nullptr) {
-            const int id = a.ids.at(row, a.vocab);
-            float logp = 0.0f;
-            if (id >= 0)
-                logp = __fmul_rn(ld1(static_cast<const T *>(a.logits) + row * a.ld + id), a.scale) - part.m - logs;
-            a.logp[row] = logp;
-        }
+        if (a.logp != nullptr)
+            a.logp[row] = id >= 0 ? __fmul_rn(own, a.scale) - part.m - logs : 0.0f;
     }
     if (TOP && lane < a.top) {
-        a.top_logp[row * a.top + lane] = mine.v - part.m - logs;
-        a.top_ids[row * a.top + lane] = mine.id;
+        a.top_logp[row * a.top + lane] = value_of(mine) - part.m - logs;
+        a.top_ids[row * a.top + lane] = id_of(mine);
     }
 }
 
@@ -226,10 +280,12 @@ struct LogBackArgs {
 // A row's scalars and its gradient's elements,
 //   dlogit = -scale p (a + b (log p + h)) = p (k0 + k1 log p),
 // the id's own apart. fp32 results: log p = (z - m) - log S and the accurate exponential. bf16
-// results: t = log2 p by two multiply-adds and the approximation, 2^-20 with t's rounding.
+// results: t = log2 p = l c - r by one multiply-add and the approximation, 2^-20 with t's
+// rounding; logits so low that p is 0 come as one of these, so that t times 0 is 0.
 template <class T> struct RowGradient {
     static constexpr bool kAccurate = sizeof(T) == 4;
-    float m, logs, h, a, b, scale, k0, k1, t0;
+    float m, logs, h, a, b, scale, k0, k1, c, r;
+    typename RowAccess<T>::Low low;
     int id;
     bool none;
     __device__ __forceinline__ RowGradient(const LogBackArgs &s, int64_t row)
@@ -246,12 +302,19 @@ template <class T> struct RowGradient {
             h = 0.0f;
         k0 = -scale * fmaf(b, h, a);
         k1 = -scale * b * (kAccurate ? 1.0f : 0.6931471805599453f);
-        t0 = -logs * kLog2e;
+        c = scale * kLog2e;
+        r = (m + logs) * kLog2e;
+        set_low(&low);
+    }
+    __device__ __forceinline__ void set_low(float *v) const { *v = -INFINITY; }
+    __device__ __forceinline__ void set_low(uint32_t *v) const   // t at most -1000, about
+    {
+        const __nv_bfloat162 q = __float2bfloat162_rn(fmaxf((r - 1000.0f) / c, -1e30f));
+        *v = *reinterpret_cast<const uint32_t *>(&q);
     }
     __device__ __forceinline__ float other(float logit) const
     {
-        const float t = kAccurate ? __fmul_rn(logit, scale) - m - logs
-                                  : fmaf(fmaf(logit, scale, -m), kLog2e, t0);
+        const float t = kAccurate ? __fmul_rn(logit, scale) - m - logs : fmaf(logit, c, -r);
         const float p = kAccurate ? expf(t) : exp2_fast(t);
         return p * fmaf(k1, fmaxf(t, -1e30f), k0);   // no infinity times 0
     }
@@ -269,12 +332,34 @@ template <class T> struct RowGradient {
     }
 };
 
+template <class T, int V>
+__device__ __forceinline__ void row_gradient(const RowGradient<T> &f, const Vec<T, V> &v, float (&g)[V])
+{
+    if constexpr (sizeof(T) == 4 || V == 1) {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            g[j] = f.other(v.get(j));
+    } else {
+        RowAccess<T> x;
+        x.v = v;
+        const Two cc = two(f.c, f.c), rr = two(-f.r, -f.r), k0 = two(f.k0, f.k0), k1 = two(f.k1, f.k1);
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) {
+            const Two t = fma_two(x.pair(j, f.low), cc, rr);
+            const float2 u = of_two(t);
+            const float2 y = of_two(mul_two(two(exp2_fast(u.x), exp2_fast(u.y)), fma_two(k1, t, k0)));
+            g[2 * j] = y.x;
+            g[2 * j + 1] = y.y;
+        }
+    }
+}
+
 // CTAs of a row take spans of kBackThreads * kBackPieces accesses; V elements an access, the
 // same alignment on both sides, or 1.
 template <class T, int V>
 __global__ void __launch_bounds__(kBackThreads) logprobs_backward_kernel(const LogBackArgs a)
 {
-    const int64_t row = blockIdx.x / a.spans, span = blockIdx.x - row * a.spans;
+    const int64_t row = blockIdx.x / (unsigned)a.spans, span = blockIdx.x - row * a.spans;
     pdl_wait();
     const T *const p = static_cast<const T *>(a.logits) + row * a.ld;
     T *const d = static_cast<T *>(a.dlogits) + row * a.ld_d;
@@ -287,7 +372,7 @@ __global__ void __launch_bounds__(kBackThreads) logprobs_backward_kernel(const L
             v[u].load(p + head + (i0 + u * kBackThreads) * V);
     const RowGradient<T> f(a, row);
     if (V > 1 && span == 0) {
-        const int64_t end = threadIdx.x < 16 ? (threadIdx.x < head ? threadIdx.x : a.vocab)
+        const int64_t end = threadIdx.x < 16 ? ((int)threadIdx.x < head ? threadIdx.x : a.vocab)
                                              : head + body * V + threadIdx.x - 16;
         if (end < a.vocab)
             st1(d + end, f(ld1(p + end), end));
@@ -297,17 +382,18 @@ __global__ void __launch_bounds__(kBackThreads) logprobs_backward_kernel(const L
         if (i0 + u * kBackThreads >= body)
             break;
         const int64_t i = head + (i0 + u * kBackThreads) * V;
-        float g[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-            g[j] = f.none ? 0.0f : f.other(v[u].get(j));
-        const int64_t at = f.id - i;
-        if (at >= 0 && at < V && !f.none)
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                g[j] = at == j ? f.own(v[u].get(j)) : g[j];
         Vec<T, V> o;
-        o.set(g);
+        o.zero();
+        if (!f.none) {
+            float g[V];
+            row_gradient<T, V>(f, v[u], g);
+            const int64_t at = f.id - i;
+            if (at >= 0 && at < V)
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    g[j] = at == j ? f.own(v[u].get(j)) : g[j];
+            o.set(g);
+        }
         o.store(d + i);
     }
 }
@@ -390,18 +476,23 @@ extern "C" int dpo_logprobs(const dpo_logprobs_args *args, void *cuda_stream)
     k.ld = a.ld_logits;
     k.scale = a.scale;
     k.top = a.top;
-    // a thread has some 16 elements at least; CTAs share a row while there are few rows
+    // As few threads of a row as give every SM kSmThreads, so that little is joined; where there
+    // are too few rows for that, as many as find a batch, and then the CTAs of a cluster.
     int threads = 32, ctas = 1;
-    while (threads < kMaxThreads && (int64_t)threads * 32 < a.vocab)
+    while (threads < kMaxThreads && (int64_t)threads * kBatch < a.vocab &&
+           (a.rows * threads < (int64_t)sms * kSmThreads || (a.top > 0 && threads < kTopThreads)))
         threads *= 2;
-    while (ctas < kMaxCtas && a.rows * ctas * 2 <= sms && (int64_t)ctas * threads * 32 < a.vocab)
+    k.warps = threads / 32;
+    const int per = k.warps == 1 ? 4 : 1;   // rows of a CTA
+    while (threads == kMaxThreads && ctas < kMaxCtas && a.rows * ctas * 2 <= sms &&
+           (int64_t)ctas * threads * 32 < a.vocab)
         ctas *= 2;
     void (*fn)(LogArgs);
     if (a.dtype == DPO_F32)
         fn = a.top > 0 ? logprobs_kernel<float, true> : logprobs_kernel<float, false>;
     else
         fn = a.top > 0 ? logprobs_kernel<__nv_bfloat16, true> : logprobs_kernel<__nv_bfloat16, false>;
-    return launch_in_clusters(what, fn, a.rows * ctas, ctas, threads, 0, cuda_stream, k);
+    return launch_in_clusters(what, fn, (a.rows + per - 1) / per * ctas, ctas, threads * per, 0, cuda_stream, k);
 }
 
 extern "C" int dpo_logprobs_backward(const dpo_logprobs_backward_args *args, void *cuda_stream)
