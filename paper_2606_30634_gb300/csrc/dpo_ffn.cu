@@ -242,6 +242,7 @@ int64_t blocks_of(int64_t k, int bk) { return (k + bk - 1) / bk; }
 struct Shape {
     int64_t m, n, k;    // kGate: n of one projection
     int segments;
+    int ways = 1;       // shares of K, each a tile of its own (Product::ways)
 };
 
 int64_t m_tiles(const Shape &s, const Form &f) { return (s.m + kTile(f.cg) - 1) / kTile(f.cg); }
@@ -250,7 +251,7 @@ int64_t n_tiles(const Shape &s, const Form &f, int epi)
     const int64_t tn = epi == kGate ? f.cols / 2 : f.cols;
     return (s.n + tn - 1) / tn;
 }
-int64_t tiles_of(const Shape &s, const Form &f, int epi) { return m_tiles(s, f) * n_tiles(s, f, epi); }
+int64_t tiles_of(const Shape &s, const Form &f, int epi) { return m_tiles(s, f) * n_tiles(s, f, epi) * s.ways; }
 
 // The form of a launch: the one with the smallest estimate of its time in ns, tiles dealt
 // in rounds. A K block costs a single CTA the stage's bytes at 154 a ns, or its instructions,
@@ -288,7 +289,7 @@ Choice form_of(const Device &d, const Shape *s, int n, int epi, bool whole = fal
         if (f.thin && (whole || n > 1 || blocks_of(s[0].k, f.bk()) < 2 * f.ways))
             continue;
         for (int i = 0; i < n; ++i) {
-            const int64_t blocks = blocks_of(s[i].k, f.bk()) * s[i].segments;
+            const int64_t blocks = (blocks_of(s[i].k, f.bk()) * s[i].segments + s[i].ways - 1) / s[i].ways;
             const double c = (double)((blocks + f.ways - 1) / f.ways) * block;
             const double each = f.thin ? c + exchange : c > store ? c : store;
             work += (double)tiles_of(s[i], f, epi) * each;
@@ -345,6 +346,7 @@ int run(const char *what, const Device &d, Launch &L, const Shape *s, int n, int
         P.m_tiles = (int)m_tiles(s[i], f);
         P.n_tiles = (int)n_tiles(s[i], f, epi);
         P.first = (int)total;
+        P.ways = s[i].ways;
         total += tiles_of(s[i], f, epi);
     }
     L.n_products = n;
@@ -411,6 +413,28 @@ int check_sizes(const char *what, int64_t tokens, int64_t dim, int64_t hidden)
 
 }  // namespace
 
+namespace {
+
+int64_t slab_rows(int64_t m) { return (m + kTile(2) - 1) / kTile(2) * kTile(2); }
+
+}  // namespace
+
+int dpo::product_ways(int64_t m, int64_t n, int64_t k)
+{
+    constexpr int64_t kPlanned = 76;
+    const int64_t tiles = (m + 255) / 256 * ((n + 255) / 256), blocks = (k + 127) / 128;
+    const int64_t other = (k + 255) / 256 * ((n + 255) / 256), each = (m + 127) / 128;
+    const double all = (double)(tiles * blocks + other * (each > 4 ? each : 4)) / kPlanned;
+    const int64_t ways = (int64_t)((double)blocks / (0.6 * all) + 0.999);
+    const int64_t most = blocks / 8 < 16 ? blocks / 8 : 16;
+    return ways < 1 || most < 2 ? 1 : (int)(ways < most ? ways : most);
+}
+int64_t dpo::product_share_bytes(int64_t m, int64_t n, int64_t k)
+{
+    const int ways = product_ways(m, n, k);
+    return ways > 1 ? ways * slab_rows(m) * n * 4 : 0;
+}
+
 int dpo::store_products(const char *what, const StoreProduct *p, int n, void *stream)
 {
     const Device *d = nullptr;
@@ -427,20 +451,32 @@ int dpo::store_products(const char *what, const StoreProduct *p, int n, void *st
             a_mn = a_mn || p[j].a_mn;
         return form_of(*d, s + i, count, kStore, count > 1 || whole(i), a_mn);
     };
-    const Choice all = choose(0, n);
-    Form f = all.form;
-    // the first product on its own with its K split, where its few long tiles would be what the
-    // list waits for (dx_form)
+    Choice all = choose(0, n);
+    // the first product, where its few long tiles would be what the list waits for, on its own with its
+    // K split over clusters (dx_form), or in shares that are tiles of the list
     int first = 0;
     if (n > 1) {
-        const Choice one = choose(0, 1);
-        if (one.form.thin && one.time + choose(1, n - 1).time + 2000.0 < all.time) {
+        const Choice one = choose(0, 1), rest = choose(1, n - 1);
+        const bool alone = one.form.thin && one.time + rest.time + 2000.0 < all.time;
+        if (alone)
+            all.time = one.time + rest.time + 2000.0;
+        if (p[0].shares != nullptr) {
+            s[0].ways = product_ways(p[0].m, p[0].n, p[0].k);
+            const Choice shared = choose(0, n);
+            const double sums = 4000.0 + (double)product_share_bytes(p[0].m, p[0].n, p[0].k) / 2500.0;
+            if (s[0].ways > 1 && shared.time + sums < all.time)
+                all = shared;
+            else
+                s[0].ways = 1;
+        }
+        if (alone && s[0].ways == 1) {
             if ((rc = store_products(what, p, 1, stream)) != DPO_OK)
                 return rc;
             first = 1;
-            f = choose(1, n - 1).form;
+            all = rest;
         }
     }
+    const Form f = all.form;
     Launch L{};
     Maps m;
     for (int i = first; i < n; ++i) {
@@ -456,11 +492,15 @@ int dpo::store_products(const char *what, const StoreProduct *p, int n, void *st
             m.operand(&P.b[0], q.b, q.k, q.n, q.ld_b, f.bk());
         else
             m.operand(&P.b[0], q.b, q.n, q.k, q.ld_b, f.cg == 2 ? BH : f.cols);
-        if (q.f32)
+        const bool shared = s[i].ways > 1;
+        if (shared)
+            m.f32(&P.d0, q.shares, s[i].ways * slab_rows(q.m), q.n, q.n);
+        else if (q.f32)
             m.f32(&P.d0, q.out, q.m, q.n, q.ld_out);
         else
             m.bf16(&P.d0, q.out, q.m, q.n, q.ld_out);
-        P.f32 = q.f32;
+        P.slab = shared ? (int)slab_rows(q.m) : 0;
+        P.f32 = shared || q.f32;
         P.accumulate = q.accumulate;
         P.old = q.out;
         P.ld_old = P.ld_o = q.ld_out;
@@ -469,14 +509,20 @@ int dpo::store_products(const char *what, const StoreProduct *p, int n, void *st
     if (n - first == 2) {   // deal by length
         const int64_t slots = slots_of(*d, f, kStore), longs = tiles_of(s[first], f, kStore),
                       shorts = tiles_of(s[first + 1], f, kStore), fewer = longs % slots;
-        const int64_t a = blocks_of(s[first].k, f.bk()), b = blocks_of(s[first + 1].k, f.bk());
+        const int64_t a = blocks_of(s[first].k, f.bk()) / s[first].ways, b = blocks_of(s[first + 1].k, f.bk());
         if (fewer > 0 && longs + shorts > slots && a >= 2 * b) {
             const int64_t most = shorts / (slots - fewer), want = a / (b > 4 ? b : 4);   // 4: its store
             L.longs = (int)longs;
             L.extra = (int)(want < most ? want : most);
         }
     }
-    return run(what, *d, L, s + first, n - first, kStore, f, false, m.ok, stream);
+    if ((rc = run(what, *d, L, s + first, n - first, kStore, f, false, m.ok, stream)) != DPO_OK ||
+        s[0].ways == 1)
+        return rc;
+    const StoreProduct &q = p[0];
+    return launch(what, sum_shares_kernel, (q.m * (q.n / 8) + kSumThreads - 1) / kSumThreads, kSumThreads, 0,
+                  stream, static_cast<const float *>(q.shares), static_cast<__nv_bfloat16 *>(q.out), q.m, q.n,
+                  q.ld_out, slab_rows(q.m) * q.n, s[0].ways);
 }
 
 int dpo::head_product(const char *what, const HeadProduct &h, void *stream)

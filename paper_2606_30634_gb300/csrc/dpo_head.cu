@@ -18,8 +18,9 @@ namespace {
 constexpr float kKeptUnit = 1.0f / 32768.0f;   // of the kept fp16 values
 
 // ---------------------------------------------------------------- join ----
-// A CTA joins 32 rows, one a lane; its warps take the rows' parts in turn.
-constexpr int kJoinMaxWarps = 32, kJoinAhead = 4;
+// A CTA joins 32 rows, one a lane; its warps take the rows' parts in turn, several at a time, and
+// then a row each, its warps' parts in the lanes.
+constexpr int kJoinMaxWarps = 32, kJoinAhead = 8;
 
 struct JoinArgs {
     const float *maxima, *target;
@@ -32,13 +33,14 @@ struct JoinArgs {
 
 __global__ void __launch_bounds__(32 * kJoinMaxWarps) head_join_kernel(const JoinArgs a)
 {
-    __shared__ Part part_[kJoinMaxWarps][32];
+    __shared__ Part part_[kJoinMaxWarps][33];
     const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t row = (int64_t)blockIdx.x * 32 + lane, r = min(row, a.rows - 1);
+    const int64_t row0 = (int64_t)blockIdx.x * 32, r = min(row0 + lane, a.rows - 1);
     pdl_wait();
     Part part;
     for (int i = warp; i < a.parts; i += warps * kJoinAhead) {
         Part p[kJoinAhead];
+        float top = part.m;
 #pragma unroll
         for (int u = 0; u < kJoinAhead; ++u)
             if (i + u * warps < a.parts) {
@@ -50,26 +52,41 @@ __global__ void __launch_bounds__(32 * kJoinMaxWarps) head_join_kernel(const Joi
             }
 #pragma unroll
         for (int u = 0; u < kJoinAhead; ++u)
-            if (i + u * warps < a.parts)
-                part.join(p[u]);
+            top = fmaxf(top, p[u].m);
+        part.raise(top);
+#pragma unroll
+        for (int u = 0; u < kJoinAhead; ++u) {
+            p[u].raise(top);
+            part.s += p[u].s;
+            part.w += p[u].w;
+        }
     }
     part_[warp][lane] = part;
     __syncthreads();
-    if (warp != 0 || row >= a.rows)
-        return;
-    for (int w = 1; w < warps; ++w)
-        part.join(part_[w][lane]);
-    const float logs = part.log_sum();
-    a.stats[2 * row] = part.m;
-    a.stats[2 * row + 1] = logs;
-    a.entropy[row] = part.entropy();
-    if (a.logp != nullptr)
-        a.logp[row] = a.ids.at(row, a.vocab) < 0 ? 0.0f : a.target[row] - part.m - logs;
+    for (int i = warp; i < 32; i += warps) {
+        const int64_t row = row0 + i;
+        if (row >= a.rows)
+            break;
+        Part p;
+        if (lane < warps)
+            p = part_[lane][i];
+        p.warp_join();
+        if (lane != 0)
+            continue;
+        const float logs = p.log_sum();
+        a.stats[2 * row] = p.m;
+        a.stats[2 * row + 1] = logs;
+        a.entropy[row] = p.entropy();
+        if (a.logp != nullptr)
+            a.logp[row] = a.ids.at(row, a.vocab) < 0 ? 0.0f : a.target[row] - p.m - logs;
+    }
 }
 
 // ------------------------------------------------------------- dlogits ----
-// G in bf16 from the kept values: p = e^(z - m_part) e^(m_part - m - log S). The id's own
-// element is a (1 - p) from the log probability itself: a kept p near 1 would leave little of it.
+// G in bf16 from the kept values x = 2^15 e^(z - m_part): with q = m_part - m - log S,
+//   g = -scale p (a + b (log p + h)),   p = x 2^-15 e^q,   log2 p = log2 x + q log2(e) - 15,
+// so g = x (k0 + k1 log2 x) with two factors of 128 columns of a row. The id's own element is
+// a (1 - p) from the log probability itself: a kept p near 1 would leave little of it.
 constexpr int kGradWarps = 8, kGradPieces = 4;   // rows of a CTA; accesses of 8 columns a lane
 
 struct GradArgs {
@@ -79,72 +96,90 @@ struct GradArgs {
     const float *logp, *entropy, *stats, *dlogp, *dentropy;
     __nv_bfloat16 *g;
     int64_t rows, vocab, ld;
-    int spans;
+    int spans, batches;          // of a row; of kGradPieces accesses in a span
     float scale;
 };
+
+// log2 by the hardware's approximation (2^-22); of 0 a number too, so that 0 times it is 0.
+__device__ __forceinline__ float log2_fast(float x)
+{
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return fmaxf(y, -100.0f);
+}
 
 __global__ void __launch_bounds__(32 * kGradWarps) head_gradient_kernel(const GradArgs a)
 {
     const int lane = threadIdx.x & 31;
-    const int64_t group = blockIdx.x / a.spans;
-    const int span = (int)(blockIdx.x - group * a.spans);
-    const int64_t row = group * kGradWarps + (threadIdx.x >> 5);
+    const uint32_t group = blockIdx.x / (uint32_t)a.spans, span = blockIdx.x - group * (uint32_t)a.spans;
+    const int64_t row = (int64_t)group * kGradWarps + (threadIdx.x >> 5);
     pdl_wait();
     if (row >= a.rows)
         return;
     const int id = a.ids.at(row, a.vocab);
     const float ga = id >= 0 ? ld1(a.dlogp + row) : 0.0f;
     const float gb = a.dentropy != nullptr ? ld1(a.dentropy + row) : 0.0f;
-    const float m = ld1(a.stats + 2 * row), logs = ld1(a.stats + 2 * row + 1), h = ld1(a.entropy + row);
+    const float m = ld1(a.stats + 2 * row), logs = ld1(a.stats + 2 * row + 1);
+    const float h = gb != 0.0f ? ld1(a.entropy + row) : 0.0f;
     const bool none = ga == 0.0f && gb == 0.0f;
-    const int64_t c0 = ((int64_t)span * kGradPieces * 32 + lane) * 8;
+    const float k0 = -a.scale * fmaf(gb, h, ga), k1 = -a.scale * gb * 0.6931471805599453f;
     const __half *const e = a.kept + row * a.ld;
     __nv_bfloat16 *const g = a.g + row * a.ld;
-    uint4 q[kGradPieces];
-    float top[kGradPieces];
+    const int vocab = (int)a.vocab;
+    int c0 = ((int)span * a.batches * kGradPieces * 32 + lane) * 8;
+    for (int n = 0; n < a.batches && c0 < vocab; ++n, c0 += kGradPieces * 256) {
+        uint4 q[kGradPieces];
+        float top[kGradPieces];
 #pragma unroll
-    for (int u = 0; u < kGradPieces; ++u) {
-        const int64_t c = c0 + u * 256;
-        q[u] = make_uint4(0u, 0u, 0u, 0u);
-        top[u] = 0.0f;
-        if (c < a.vocab && !none) {   // whole pieces: the pitch is a multiple of 8
-            asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(q[u].x), "=r"(q[u].y), "=r"(q[u].z), "=r"(q[u].w)
-                         : "l"(e + c));
-            top[u] = ld1(a.maxima + c / kHeadStatCols * a.rows + row);
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < kGradPieces; ++u) {
-        const int64_t c = c0 + u * 256;
-        if (c >= a.vocab)
-            break;
-        const float part = none ? 0.0f : exp2_fast((top[u] - m - logs) * kLog2e) * kKeptUnit;
-        const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
-        uint32_t o[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(w + j));
-            float p[2] = {v.x * part, v.y * part}, y[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                float lp = 0.0f;
-                y[k] = -ga * p[k];
-                if (id == c + 2 * j + k) {
-                    lp = ld1(a.logp + row);
-                    p[k] = exp2_fast(lp * kLog2e);
-                    y[k] = -ga * expm1f(lp);
-                } else if (gb != 0.0f) {
-                    lp = __logf(p[k]);
-                }
-                if (gb != 0.0f && p[k] != 0.0f)
-                    y[k] = fmaf(-gb * p[k], lp + h, y[k]);
-                y[k] = none ? 0.0f : y[k] * a.scale;
+        for (int u = 0; u < kGradPieces; ++u) {
+            const int c = c0 + u * 256;
+            q[u] = make_uint4(0u, 0u, 0u, 0u);
+            top[u] = 0.0f;
+            if (c < vocab && !none) {   // whole pieces: the pitch is a multiple of 8
+                asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(q[u].x), "=r"(q[u].y), "=r"(q[u].z), "=r"(q[u].w)
+                             : "l"(e + c));
+                top[u] = ld1(a.maxima + (int64_t)(c / kHeadStatCols) * a.rows + row);
             }
-            o[j] = pack_bf16x2(y[0], y[1]);
         }
-        // columns past the vocabulary, up to the pitch, are not read by the products
-        *reinterpret_cast<uint4 *>(g + c) = make_uint4(o[0], o[1], o[2], o[3]);
+#pragma unroll
+        for (int u = 0; u < kGradPieces; ++u) {
+            const int c = c0 + u * 256;
+            if (c >= vocab)
+                break;
+            const float t = (top[u] - m - logs) * kLog2e, part = exp2_fast(t) * kKeptUnit;
+            const float f0 = part * fmaf(k1, fmaxf(t, -1000.0f) - 15.0f, k0), f1 = part * k1;
+            const Two f00 = two(f0, f0), f11 = two(f1, f1);
+            const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+            uint32_t o[4];
+            if (none) {
+                o[0] = o[1] = o[2] = o[3] = 0u;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(w + j));
+                    Two f = f00;
+                    if (gb != 0.0f)
+                        f = fma_two(f11, two(log2_fast(v.x), log2_fast(v.y)), f00);
+                    const float2 y = of_two(mul_two(two(v.x, v.y), f));
+                    o[j] = pack_bf16x2(y.x, y.y);
+                }
+                const int at = id - c;
+                if (at >= 0 && at < 8) {
+                    const float lp = ld1(a.logp + row), p = expf(lp);
+                    float y = -ga * expm1f(lp);
+                    if (gb != 0.0f && p != 0.0f)
+                        y = fmaf(-gb * p, lp + h, y);
+                    const uint32_t own = pack_bf16x2(y * a.scale, y * a.scale);
+                    const uint32_t mask = at & 1 ? 0xFFFF0000u : 0x0000FFFFu;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        o[j] = at / 2 == j ? (o[j] & ~mask) | (own & mask) : o[j];
+                }
+            }
+            // columns past the vocabulary, up to the pitch, are not read by the products
+            *reinterpret_cast<uint4 *>(g + c) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
     }
 }
 
@@ -174,9 +209,10 @@ struct Sizes {
     int64_t ld, parts;
     int64_t kept, maxima;              // kept: the values, their maxima
     int64_t target, sums, own, logits; // forward: without kept its maxima, for `top` logits
+    int64_t shares;                    // backward: G, the shares of dx
     int64_t forward, backward;
 };
-Sizes sizes_of(int64_t tokens, int64_t vocab, bool keep, int top)
+Sizes sizes_of(int64_t tokens, int64_t dim, int64_t vocab, bool keep, int top)
 {
     Sizes s;
     s.ld = pitch_of(vocab);
@@ -190,7 +226,8 @@ Sizes sizes_of(int64_t tokens, int64_t vocab, bool keep, int top)
     if (top > 0 && !keep)
         s.logits = 0;
     s.forward = s.logits + (top > 0 ? align_up(tokens * s.ld * 4) : 0);
-    s.backward = align_up(tokens * s.ld * 2);
+    s.shares = align_up(tokens * s.ld * 2);
+    s.backward = s.shares + align_up(product_share_bytes(tokens, dim, vocab));
     return s;
 }
 
@@ -228,7 +265,7 @@ extern "C" int dpo_head_workspace(int64_t tokens, int64_t dim, int64_t vocab, in
         return rc;
     if (top < 0 || top > DPO_MAX_TOP || top > vocab)
         return call_fail(DPO_EINVAL, "%s: top %d of %lld", what, top, (long long)vocab);
-    const Sizes s = sizes_of(tokens, vocab, keep != 0, top);
+    const Sizes s = sizes_of(tokens, dim, vocab, keep != 0, top);
     if (forward_bytes != nullptr)
         *forward_bytes = s.forward;
     if (kept_bytes != nullptr)
@@ -255,7 +292,7 @@ extern "C" int dpo_head(const dpo_head_args *args, void *cuda_stream)
     if (a.tokens == 0)
         return DPO_OK;
     const int64_t T = a.tokens;
-    const Sizes s = sizes_of(T, a.vocab, a.kept != nullptr, a.top);
+    const Sizes s = sizes_of(T, a.dim, a.vocab, a.kept != nullptr, a.top);
     Buffers b(what);
     b.add("x", a.x, T, a.dim, a.ld_x, 2, 16, false);
     b.add("w", a.w, a.vocab, a.dim, a.dim, 2, 16, false);
@@ -344,7 +381,7 @@ extern "C" int dpo_head_backward(const dpo_head_backward_args *args, void *cuda_
             cudaMemsetAsync(a.dw, 0, (size_t)(V * D * gsize), static_cast<cudaStream_t>(cuda_stream));
         return e == cudaSuccess ? DPO_OK : call_fail(DPO_ECUDA, "%s: %s", what, cudaGetErrorString(e));
     }
-    const Sizes s = sizes_of(T, V, true, 0);
+    const Sizes s = sizes_of(T, D, V, true, 0);
     b.add("x", a.x, T, D, a.ld_x, 2, 16, false);
     b.add("w", a.w, V, D, D, 2, 16, false);
     add_ids(b, a.ids);
@@ -376,8 +413,11 @@ extern "C" int dpo_head_backward(const dpo_head_backward_args *args, void *cuda_
     g.vocab = V;
     g.ld = s.ld;
     g.scale = a.scale;
-    g.spans = (int)((V + kGradPieces * 256 - 1) / (kGradPieces * 256));
-    const int64_t grid = (T + kGradWarps - 1) / kGradWarps * g.spans;
+    // up to four batches a span, where that leaves CTAs enough for all SMs
+    const int64_t groups = (T + kGradWarps - 1) / kGradWarps, batches = (V + kGradPieces * 256 - 1) / (kGradPieces * 256);
+    g.batches = groups * batches >= 4 * 2048 ? 4 : 1;
+    g.spans = (int)((batches + g.batches - 1) / g.batches);
+    const int64_t grid = groups * g.spans;
     if (grid >= kMaxCount)
         return call_fail(DPO_EINVAL, "%s: %lld x %lld is too large", what, (long long)T, (long long)V);
     if ((rc = launch(what, head_gradient_kernel, grid, 32 * kGradWarps, 0, cuda_stream, g)) != DPO_OK)
@@ -385,7 +425,8 @@ extern "C" int dpo_head_backward(const dpo_head_backward_args *args, void *cuda_
     StoreProduct p[2];
     int n = 0;
     if (a.dx != nullptr)
-        p[n++] = {G, a.w, a.dx, T, D, V, s.ld, D, a.ld_dx, 0, 1, 0, 0};
-    p[n++] = {G, a.x, a.dw, V, D, T, s.ld, a.ld_x, D, 1, 1, a.grad_dtype == DPO_F32, a.accumulate != 0};
+        p[n++] = {G, a.w, a.dx, T, D, V, s.ld, D, a.ld_dx, 0, 1, 0, 0,
+                  s.backward > s.shares ? static_cast<uint8_t *>(G) + s.shares : nullptr};
+    p[n++] = {G, a.x, a.dw, V, D, T, s.ld, a.ld_x, D, 1, 1, a.grad_dtype == DPO_F32, a.accumulate != 0, nullptr};
     return store_products(what, p, n, cuda_stream);
 }

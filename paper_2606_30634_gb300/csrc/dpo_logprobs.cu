@@ -281,7 +281,8 @@ struct LogBackArgs {
 //   dlogit = -scale p (a + b (log p + h)) = p (k0 + k1 log p),
 // the id's own apart. fp32 results: log p = (z - m) - log S and the accurate exponential. bf16
 // results: t = log2 p = l c - r by one multiply-add and the approximation, 2^-20 with t's
-// rounding; logits so low that p is 0 come as one of these, so that t times 0 is 0.
+// rounding; logits so low that p is 0 come as one of these, so that t times 0 is 0. Rows whose r
+// is far out take the differences instead.
 template <class T> struct RowGradient {
     static constexpr bool kAccurate = sizeof(T) == 4;
     float m, logs, h, a, b, scale, k0, k1, c, r;
@@ -314,7 +315,8 @@ template <class T> struct RowGradient {
     }
     __device__ __forceinline__ float other(float logit) const
     {
-        const float t = kAccurate ? __fmul_rn(logit, scale) - m - logs : fmaf(logit, c, -r);
+        const float t = kAccurate ? __fmul_rn(logit, scale) - m - logs
+                                  : fmaf(fmaf(logit, scale, -m), kLog2e, -logs * kLog2e);
         const float p = kAccurate ? expf(t) : exp2_fast(t);
         return p * fmaf(k1, fmaxf(t, -1e30f), k0);   // no infinity times 0
     }
@@ -335,11 +337,11 @@ template <class T> struct RowGradient {
 template <class T, int V>
 __device__ __forceinline__ void row_gradient(const RowGradient<T> &f, const Vec<T, V> &v, float (&g)[V])
 {
-    if constexpr (sizeof(T) == 4 || V == 1) {
+    if (sizeof(T) == 4 || V == 1 || !(fabsf(f.r) < 16384.0f)) {
 #pragma unroll
         for (int j = 0; j < V; ++j)
             g[j] = f.other(v.get(j));
-    } else {
+    } else if constexpr (sizeof(T) == 2 && V > 1) {
         RowAccess<T> x;
         x.v = v;
         const Two cc = two(f.c, f.c), rr = two(-f.r, -f.r), k0 = two(f.k0, f.k0), k1 = two(f.k1, f.k1);

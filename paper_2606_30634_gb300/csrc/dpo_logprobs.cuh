@@ -3,6 +3,7 @@
 #pragma once
 
 #include "dpo_ends.cuh"
+#include "dpo_two.cuh"
 #include "dpo_vec.cuh"
 
 #include <math.h>
@@ -64,39 +65,6 @@ struct Part {
     __device__ __forceinline__ float log_sum() const { return logf(s); }
     __device__ __forceinline__ float entropy() const { return logf(s) - w / s; }
 };
-
-// Two fp32 values as an operand of the instructions that work on pairs.
-using Two = unsigned long long;
-__device__ __forceinline__ Two two(float a, float b)
-{
-    Two r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ float2 of_two(Two v)
-{
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
-__device__ __forceinline__ Two fma_two(Two a, Two b, Two c)
-{
-    Two r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ Two add_two(Two a, Two b)
-{
-    Two r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ Two mul_two(Two a, Two b)
-{
-    Two r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 
 // A thread's share of a row, added up in units of 2 and as pairs: with the largest logit l so far
 // at m and c = scale log2(e), sums of 2^t and 2^t t, t = l c - r by one multiply-add, r = m c rounded.

@@ -18,9 +18,16 @@ struct StoreProduct {
     int64_t ld_a, ld_b, ld_out;
     int a_mn, b_mn;
     int f32, accumulate;
+    void *shares;                 // the first of a list, bf16: product_share_bytes, or nullptr
 };
 
 constexpr int kMaxStoreProducts = 4;
+
+// How far the K of the first of two products whose list is out = G w (m x n, k) and G^T x (k x n, m) is
+// divided so that no tile takes longer than some six tenths of the list, by 76 pairs' shares of
+// it, and the bytes that the shares' sums take (0: not divided).
+int product_ways(int64_t m, int64_t n, int64_t k);
+int64_t product_share_bytes(int64_t m, int64_t n, int64_t k);
 
 // Up to four of them, in one launch in whose order their tiles are begun (longest first), or the
 // first one before the others where its K is better split.
