@@ -414,12 +414,39 @@ struct Stager {
                                          int y)
     {
         const uint32_t b = begin();
+        put(b, w);
+        end(map, b, x, y);
+    }
+    __device__ __forceinline__ void put(uint32_t b, const uint32_t (&w)[16])
+    {
 #pragma unroll
         for (int g = 0; g < 4; ++g)
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(b + swz64(lane, g)),
                          "r"(w[4 * g]), "r"(w[4 * g + 1]), "r"(w[4 * g + 2]), "r"(w[4 * g + 3])
                          : "memory");
-        end(map, b, x, y);
+    }
+    // Chunk k of a row of them, two by two, one in each buffer: a wait and a fence for both.
+    __device__ __forceinline__ void bf16_of_two(const CUtensorMap *map, const uint32_t (&w)[16], int k, int x,
+                                                int y, int cols)
+    {
+        if (k % 2 == 0) {
+            if (lane == 0)
+                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            __syncwarp();
+        }
+        put(buf + (uint32_t)(k % 2 * kChunkBytes), w);
+        if (k % 2 == 0)
+            return;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            if (x - 32 < cols)
+                tma_store(map, buf, x - 32, y);
+            if (x < cols)
+                tma_store(map, buf + (uint32_t)kChunkBytes, x, y);
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+        turn = 0;
     }
     // one 4 KiB chunk in the 128-byte swizzle (granule index XOR row mod 8), in both
     // buffers
@@ -469,6 +496,19 @@ __device__ __forceinline__ void load_acc(uint32_t acc, float (&v)[32])
 #pragma unroll
     for (int j = 0; j < 32; ++j)
         v[j] = __uint_as_float(r[j]);
+}
+
+// 128 columns with one wait.
+__device__ __forceinline__ void load_acc_ahead(uint32_t acc, float (&v)[kHeadCols])
+{
+    uint32_t r[4][32];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        gemm::tmem_ld32_ahead(acc + (uint32_t)(32 * c), r[c]);
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < kHeadCols; ++j)
+        v[j] = __uint_as_float(r[j / 32][j % 32]);
 }
 
 // u := act(g) u
@@ -751,8 +791,9 @@ __device__ __forceinline__ void head_rows(const Product &P, Stager &st, float (&
                 const __half2 h = __floats2half2_rn(q.x, q.y);
                 e2[j] = *reinterpret_cast<const uint32_t *>(&h);
             }
-            if (H.keep && col0 + k < P.n)
-                st.bf16(&P.d0, e2, col0 + k, row0);   // two bytes an element, whatever they mean
+            if (H.keep)
+                // two bytes an element, whatever they mean
+                st.bf16_of_two(&P.d0, e2, k / 32, col0 + k, row0, P.n);
         }
         const float2 s2 = of_two(add_two(ss[0], ss[1])), w2 = of_two(add_two(ww[0], ww[1]));
         const float f = exp2(-off);
@@ -778,8 +819,8 @@ __device__ __forceinline__ void head_rows(const Product &P, Stager &st, float (&
                 const __half2 h = __floats2half2_rn(e[0] * kHeadUnit, e[1] * kHeadUnit);
                 e2[j / 2] = *reinterpret_cast<const uint32_t *>(&h);
             }
-            if (H.keep && col0 + k < P.n)
-                st.bf16(&P.d0, e2, col0 + k, row0);
+            if (H.keep)
+                st.bf16_of_two(&P.d0, e2, k / 32, col0 + k, row0, P.n);
         }
     }
     if (in) {
@@ -1362,18 +1403,17 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                         break;
                     const uint32_t acc =
                         tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * T + half * kHeadCols);
+                    if (visit == begin) {
+                        load_acc_ahead(acc, v);
+                    } else {
 #pragma unroll
-                    for (int c = 0; c < kHeadCols; c += 32) {
-                        float x[32];
-                        load_acc(acc + (uint32_t)c, x);
-                        if (visit == begin)
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                v[c + j] = x[j];
-                        else
+                        for (int c = 0; c < kHeadCols; c += 32) {
+                            float x[32];
+                            load_acc(acc + (uint32_t)c, x);
 #pragma unroll
                             for (int j = 0; j < 32; ++j)
                                 v[c + j] += x[j];
+                        }
                     }
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();

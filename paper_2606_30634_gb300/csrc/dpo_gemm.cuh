@@ -316,7 +316,8 @@ template <int CG> __device__ __forceinline__ void tmem_free(uint32_t tmem)
                      : "memory");
 }
 
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32])
+// To be waited for (tcgen05.wait::ld) before its results are used.
+__device__ __forceinline__ void tmem_ld32_ahead(uint32_t taddr, uint32_t (&r)[32])
 {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
@@ -329,6 +330,10 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32])
           "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
           "=r"(r[31])
         : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32])
+{
+    tmem_ld32_ahead(taddr, r);
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
