@@ -116,8 +116,9 @@ struct SortArgs {
 // Up to 8192 tokens: a pair's place is the number of pairs before it, counted by comparing it
 // with all of them. 67 million comparisons of two instructions each are 4 us on all SMs, with
 // no step that waits for another (the cluster's sort below, two passes: 12).
-constexpr int kRankTokens = 8192, kRankBits = 13, kRankWarps = 8, kRankKeys = 7;   // keys of a warp
-constexpr int64_t kRankVocab = (int64_t)1 << (32 - kRankBits);
+constexpr int kRankTokens = 8192, kRankBits = 13, kRankWarps = 16, kRankKeys = 4;   // keys of a warp
+constexpr uint32_t kRankNone = 0x7FFFFFFFu;
+constexpr int64_t kRankVocab = (int64_t)1 << (31 - kRankBits);
 
 __global__ void __launch_bounds__(32 * kRankWarps) rank_ids_kernel(const SortArgs a)
 {
@@ -130,24 +131,14 @@ __global__ void __launch_bounds__(32 * kRankWarps) rank_ids_kernel(const SortArg
     uint32_t *const keys = reinterpret_cast<uint32_t *>(keys_);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = (int)a.count;
     const int padded = (n + 127) / 128 * 128;
-    bool valid = false;
-    int some = 0;
-    for (int i0 = 0; i0 < padded; i0 += 32 * kRankWarps * 4) {
-        uint32_t k[4];
+    int id[kRankTokens / (32 * kRankWarps)], some = 0;
+    a.ids.at(a.first + threadIdx.x, 32 * kRankWarps, a.first + n, a.vocab, id);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = i0 + u * 32 * kRankWarps + (int)threadIdx.x;
-            const int id = i < n ? a.ids.at(a.first + i, a.vocab) : -1;
-            valid = id >= 0;
-            some += valid;
-            k[u] = valid ? (uint32_t)id << kRankBits | (uint32_t)i : ~0u;
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = i0 + u * 32 * kRankWarps + (int)threadIdx.x;
-            if (i < padded)
-                keys[i] = k[u];
-        }
+    for (int u = 0; u < kRankTokens / (32 * kRankWarps); ++u) {
+        const int i = u * 32 * kRankWarps + (int)threadIdx.x;
+        some += id[u] >= 0;
+        if (i < padded)
+            keys[i] = id[u] >= 0 ? (uint32_t)id[u] << kRankBits | (uint32_t)i : kRankNone;
     }
     __shared__ int counts[kRankWarps];
     some = __reduce_add_sync(0xFFFFFFFFu, some);
@@ -166,7 +157,7 @@ __global__ void __launch_bounds__(32 * kRankWarps) rank_ids_kernel(const SortArg
     uint32_t mine[kRankKeys], before[kRankKeys];
 #pragma unroll
     for (int j = 0; j < kRankKeys; ++j) {
-        mine[j] = t0 + j < n ? keys[t0 + j] : ~0u;
+        mine[j] = t0 + j < n ? keys[t0 + j] : kRankNone;
         before[j] = 0u;
     }
 #pragma unroll 2
@@ -174,13 +165,13 @@ __global__ void __launch_bounds__(32 * kRankWarps) rank_ids_kernel(const SortArg
         const uint4 q = keys_[i];
 #pragma unroll
         for (int j = 0; j < kRankKeys; ++j)
-            before[j] += (uint32_t)(q.x < mine[j]) + (uint32_t)(q.y < mine[j]) + (uint32_t)(q.z < mine[j]) +
-                         (uint32_t)(q.w < mine[j]);
+            for (const uint32_t other : {q.x, q.y, q.z, q.w})
+                before[j] += (other - mine[j]) >> 31;   // keys are below 2^31: a sign, shifted and added in one
     }
 #pragma unroll
     for (int j = 0; j < kRankKeys; ++j) {
         const uint32_t place = __reduce_add_sync(0xFFFFFFFFu, before[j]);
-        if (lane == j && mine[j] != ~0u)
+        if (lane == j && mine[j] != kRankNone)
             a.sorted[place] = make_uint2(mine[j] >> kRankBits, (uint32_t)(t0 + j));
     }
 }
@@ -219,15 +210,12 @@ __global__ void __launch_bounds__(kSortThreads) sort_ids_kernel(const SortArgs a
     }
     cluster_barrier();   // the others' shared memory is written before the next one
     uint32_t key[kSortItems], pos[kSortItems], place[kSortItems];
+    int id[kSortItems];
+    a.ids.at(a.first + (int64_t)rank * per + at0, 32, a.first + a.count, a.vocab, id);
 #pragma unroll
     for (int i = 0; i < kSortItems; ++i) {
-        const int64_t t = (int64_t)rank * per + at0 + i * 32;
-        key[i] = pad;
-        pos[i] = (uint32_t)t;
-        if (t < a.count) {
-            const int id = a.ids.at(a.first + t, a.vocab);
-            key[i] = id < 0 ? pad : (uint32_t)id;
-        }
+        key[i] = id[i] < 0 ? pad : (uint32_t)id[i];
+        pos[i] = rank * (uint32_t)per + (uint32_t)(at0 + i * 32);
     }
     for (int p = 0; p < a.passes; ++p) {
         const int shift = p * a.bits;
@@ -326,7 +314,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_ids_kernel(const SortArgs a
 }
 
 // ------------------------------------------------------------ backward ----
-constexpr int kSumThreads = 128, kSumRows = 8;   // rows requested at a time
+constexpr int kSumThreads = 128;
 constexpr int kSpan = 32;                        // pairs of a chunk, at least
 constexpr int kMaxChunk = DPO_EMBED_SPAN / 256;
 
@@ -355,22 +343,19 @@ __device__ __forceinline__ int ld_int(const int *p)
     return v;
 }
 
-// dtable[id, c ..] (+)= scale sum.
+// dtable[id, c ..] (+)= scale sum; one rounding of the product and the sum.
 template <class GT, int V>
 __device__ __forceinline__ void finish(const SumArgs &a, uint32_t id, int64_t c, const float (&sum)[V])
 {
     GT *const p = static_cast<GT *>(a.dtable) + (int64_t)id * a.ld_dtable + c;
     float y[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-        y[j] = sum[j] * a.scale;
     Vec<GT, V> o;
-    if (a.accumulate) {
+    o.zero();
+    if (a.accumulate)
         o.load(p);
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            y[j] += o.get(j);
-    }
+    for (int j = 0; j < V; ++j)
+        y[j] = a.accumulate ? fmaf(sum[j], a.scale, o.get(j)) : sum[j] * a.scale;
     o.set(y);
     o.store(p);
 }
@@ -394,14 +379,24 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const SumArgs a)
     if (c >= a.dim)
         return;
     const T *const dy = static_cast<const T *>(a.dy) + c;
+    const uint32_t begun = pair[-1].x;   // this id's run began before this chunk
+    // the last of its run, which is all in this chunk: what dtable's row takes
+    auto whole = [&](int i) { return pair[i + 1].x != pair[i].x && pair[i].x != begun; };
+    GT *const table = static_cast<GT *>(a.dtable) + c;
+    constexpr int kSumRows = V <= 2 ? 16 : 8;   // requested at a time
     float sum[V] = {};
-    bool here = pair[-1].x != pair[0].x;   // the run began in this chunk
     for (int i = 0; i < len; i += kSumRows) {
         Vec<T, V> v[kSumRows];
+        Vec<GT, V> old[kSumRows];
 #pragma unroll
         for (int u = 0; u < kSumRows; ++u)
             if (i + u < len)
                 v[u].load(dy + (int64_t)pair[i + u].y * a.ld_dy);
+        if (a.accumulate)   // with them, not one after the other at the ends of the runs
+#pragma unroll
+            for (int u = 0; u < kSumRows; ++u)
+                if (i + u < len && whole(i + u))
+                    old[u].load(table + (int64_t)pair[i + u].x * a.ld_dtable);
 #pragma unroll
         for (int u = 0; u < kSumRows; ++u) {
             if (i + u >= len)
@@ -409,19 +404,22 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const SumArgs a)
 #pragma unroll
             for (int j = 0; j < V; ++j)
                 sum[j] += v[u].get(j);
-            const uint32_t id = pair[i + u].x;
-            const bool ends = pair[i + u + 1].x != id;
-            if (!ends && i + u + 1 < len)
-                continue;
-            if (here && ends) {
-                finish<GT, V>(a, id, c, sum);
-            } else {
-                float *const p = a.partial + ((int64_t)chunk * 2 + !here) * a.dim + c;
+            if (whole(i + u)) {
+                float y[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    y[j] = a.accumulate ? fmaf(sum[j], a.scale, old[u].get(j)) : sum[j] * a.scale;
+                Vec<GT, V> o;
+                o.set(y);
+                o.store(table + (int64_t)pair[i + u].x * a.ld_dtable);
+            } else if (i + u + 1 == len || pair[i + u + 1].x != pair[i + u].x) {
+                float *const p = a.partial + ((int64_t)chunk * 2 + (pair[i + u].x == begun)) * a.dim + c;
 #pragma unroll
                 for (int j = 0; j < V; ++j)
                     p[j] = sum[j];
+            } else {
+                continue;
             }
-            here = true;
 #pragma unroll
             for (int j = 0; j < V; ++j)
                 sum[j] = 0.0f;
