@@ -19,9 +19,11 @@ namespace dpo {
 namespace {
 
 // ------------------------------------------------------------- forward ----
-// A warp takes kPieces accesses a lane of one row: 2 KB of a bf16 row of 16-byte accesses, so
-// that a single token's row is shared by several warps and its latency is one access's.
-constexpr int kPieces = 4, kEmbedWarps = 8;
+// A warp takes some accesses a lane of one row: 2 KB of a bf16 row of 16-byte accesses, so
+// that a single token's row is shared by several warps and its latency is one access's. (us of 8192
+// tokens by 4 / 8 / 16 of them: 4094 bf16, 4 bytes an access, 27 / 21 / -; 4095 49 / - / 67.)
+__host__ __device__ constexpr int pieces(int v) { return v == 2 ? 8 : 4; }
+constexpr int kEmbedWarps = 8;
 
 struct EmbedArgs {
     Ids ids;
@@ -40,19 +42,19 @@ __global__ void __launch_bounds__(32 * kEmbedWarps) embed_kernel(const EmbedArgs
     pdl_wait();
     if (t >= a.tokens)
         return;
-    const int64_t c0 = (unit - t * a.segs) * (32 * kPieces * V) + lane * V;
+    const int64_t c0 = (unit - t * a.segs) * (32 * pieces(V) * V) + lane * V;
     const int id = a.ids.at(t, a.vocab);
     const TT *const row = static_cast<const TT *>(a.table) + (int64_t)max(id, 0) * a.ld_table;
     OT *const out = static_cast<OT *>(a.out) + t * a.ld_out;
-    Vec<TT, V> v[kPieces];
+    Vec<TT, V> v[pieces(V)];
 #pragma unroll
-    for (int n = 0; n < kPieces; ++n) {
+    for (int n = 0; n < pieces(V); ++n) {
         v[n].zero();
         if (id >= 0 && c0 + n * 32 * V < a.dim)
             v[n].load(row + c0 + n * 32 * V);
     }
 #pragma unroll
-    for (int n = 0; n < kPieces; ++n) {
+    for (int n = 0; n < pieces(V); ++n) {
         float x[V];
 #pragma unroll
         for (int j = 0; j < V; ++j)
@@ -535,7 +537,9 @@ Plan plan_of(int64_t tokens, int64_t dim)
     const int64_t n = tokens < DPO_EMBED_SPAN ? tokens : DPO_EMBED_SPAN;
     Plan p;
     p.chunk = kSpan;
-    while ((int64_t)p.chunk * 256 < n)   // at most 256 chunks
+    // at most 256 chunks of wide rows, more of those that few CTAs share
+    const int64_t segs = (dim + 8 * kSumThreads - 1) / (8 * kSumThreads), most = 1024 / segs;
+    while ((int64_t)p.chunk * (most > 256 ? most : 256) < n)
         p.chunk *= 2;
     p.chunks = (int)((n + p.chunk - 1) / p.chunk);
     p.sorted = 256;
@@ -578,7 +582,7 @@ extern "C" int dpo_embed(const dpo_embed_args *args, void *cuda_stream)
     k.ld_table = a.ld_table;
     k.ld_out = a.ld_out;
     k.scale = a.scale;
-    const int64_t seg = 32 * kPieces * w.v;
+    const int64_t seg = 32 * pieces(w.v) * w.v;
     k.segs = (a.dim + seg - 1) / seg;
     const int64_t grid = (k.tokens * k.segs + kEmbedWarps - 1) / kEmbedWarps;
     if (grid >= kMaxCount)
