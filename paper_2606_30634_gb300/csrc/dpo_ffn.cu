@@ -425,7 +425,7 @@ int dpo::product_ways(int64_t m, int64_t n, int64_t k)
     const int64_t tiles = (m + 255) / 256 * ((n + 255) / 256), blocks = (k + 127) / 128;
     const int64_t other = (k + 255) / 256 * ((n + 255) / 256), each = (m + 127) / 128;
     const double all = (double)(tiles * blocks + other * (each > 4 ? each : 4)) / kPlanned;
-    const int64_t ways = (int64_t)((double)blocks / (0.6 * all) + 0.999);
+    const int64_t ways = (int64_t)((double)blocks / (0.8 * all) + 0.999);
     const int64_t most = blocks / 8 < 16 ? blocks / 8 : 16;
     return ways < 1 || most < 2 ? 1 : (int)(ways < most ? ways : most);
 }

@@ -24,7 +24,7 @@ struct StoreProduct {
 constexpr int kMaxStoreProducts = 4;
 
 // How far the K of the first of two products whose list is out = G w (m x n, k) and G^T x (k x n, m) is
-// divided so that no tile takes longer than some six tenths of the list, by 76 pairs' shares of
+// divided so that no tile takes longer than some eight tenths of the list, by 76 pairs' shares of
 // it, and the bytes that the shares' sums take (0: not divided).
 int product_ways(int64_t m, int64_t n, int64_t k);
 int64_t product_share_bytes(int64_t m, int64_t n, int64_t k);
