@@ -18,9 +18,9 @@ namespace {
 constexpr float kKeptUnit = 1.0f / 32768.0f;   // of the kept fp16 values
 
 // ---------------------------------------------------------------- join ----
-// A CTA joins 32 rows, one a lane; its warps take the rows' parts in turn, several at a time, and
-// then a row each, its warps' parts in the lanes.
-constexpr int kJoinMaxWarps = 32, kJoinAhead = 8;
+// A CTA joins kJoinRows rows, a lane one part of one of them, several at a time; then a warp has a
+// row, with its warps' sums in the lanes.
+constexpr int kJoinMaxWarps = 32, kJoinRows = 8, kJoinLanes = 32 / kJoinRows, kJoinAhead = 4;
 
 struct JoinArgs {
     const float *maxima, *target;
@@ -33,18 +33,19 @@ struct JoinArgs {
 
 __global__ void __launch_bounds__(32 * kJoinMaxWarps) head_join_kernel(const JoinArgs a)
 {
-    __shared__ Part part_[kJoinMaxWarps][33];
+    __shared__ Part part_[kJoinMaxWarps][kJoinRows + 1];
     const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t row0 = (int64_t)blockIdx.x * 32, r = min(row0 + lane, a.rows - 1);
+    const int64_t row0 = (int64_t)blockIdx.x * kJoinRows, r = min(row0 + lane % kJoinRows, a.rows - 1);
+    const int step = warps * kJoinLanes;
     pdl_wait();
     Part part;
-    for (int i = warp; i < a.parts; i += warps * kJoinAhead) {
+    for (int i = warp * kJoinLanes + lane / kJoinRows; i < a.parts; i += step * kJoinAhead) {
         Part p[kJoinAhead];
         float top = part.m;
 #pragma unroll
         for (int u = 0; u < kJoinAhead; ++u)
-            if (i + u * warps < a.parts) {
-                const int64_t at = (int64_t)(i + u * warps) * a.rows + r;
+            if (i + u * step < a.parts) {
+                const int64_t at = (int64_t)(i + u * step) * a.rows + r;
                 const float2 sw = a.sums[at];
                 p[u].m = a.maxima[at];
                 p[u].s = sw.x;
@@ -61,9 +62,11 @@ __global__ void __launch_bounds__(32 * kJoinMaxWarps) head_join_kernel(const Joi
             part.w += p[u].w;
         }
     }
-    part_[warp][lane] = part;
+    part.warp_join<kJoinRows>();
+    if (lane < kJoinRows)
+        part_[warp][lane] = part;
     __syncthreads();
-    for (int i = warp; i < 32; i += warps) {
+    for (int i = warp; i < kJoinRows; i += warps) {
         const int64_t row = row0 + i;
         if (row >= a.rows)
             break;
@@ -336,9 +339,9 @@ extern "C" int dpo_head(const dpo_head_args *args, void *cuda_stream)
         JoinArgs j{p.maxima, p.target, p.sums, ids, a.ids.p != nullptr ? a.logp : nullptr, a.entropy, a.stats,
                    T, a.vocab, (int)s.parts};
         int warps = 4;
-        while (warps < kJoinMaxWarps && warps * kJoinAhead < s.parts)
+        while (warps < kJoinMaxWarps && warps * kJoinLanes * kJoinAhead < s.parts)
             warps *= 2;
-        return launch(what, head_join_kernel, (T + 31) / 32, 32 * warps, 0, cuda_stream, j);
+        return launch(what, head_join_kernel, (T + kJoinRows - 1) / kJoinRows, 32 * warps, 0, cuda_stream, j);
     }
     dpo_logprobs_args l{};
     l.logits = p.logits;

@@ -48,16 +48,17 @@ struct Part {
         s += p.s;
         w += p.w;
     }
-    // over the lanes of the warp, in all of them: one exponential, to the largest maximum
-    __device__ __forceinline__ void warp_join()
+    // over the lanes of the warp, or every LOW-th of them, in all of these: one exponential, to the
+    // largest maximum
+    template <int LOW = 1> __device__ __forceinline__ void warp_join()
     {
         float top = m;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1)
+        for (int o = 16; o >= LOW; o >>= 1)
             top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
         raise(top);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
+        for (int o = 16; o >= LOW; o >>= 1) {
             s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
             w += __shfl_xor_sync(0xFFFFFFFFu, w, o);
         }
