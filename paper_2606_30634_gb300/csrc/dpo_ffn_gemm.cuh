@@ -1418,7 +1418,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
                     if (lane == 0)
-                        mbar_arrive<CG>(acc_empty(a));
+                        gemm::mbar_arrive_read<CG>(acc_empty(a));   // 1001 x 256 x 50257: 60 -> 44 us
                 }
                 if (seen && any)
                     head_rows(P, st, v, id, row0, col0);

@@ -208,6 +208,19 @@ template <int CG> __device__ __forceinline__ void mbar_arrive(uint32_t bar)
         asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// The same by a warp that has read TMEM, waited for it (tcgen05.wait::ld) and fenced its reads
+// (tcgen05.fence::before_thread_sync): nothing else of its is ordered, so that stores to global
+// memory that are under way are not waited for.
+template <int CG> __device__ __forceinline__ void mbar_arrive_read(uint32_t bar)
+{
+    if (CG == 2)
+        asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+                         map_to_rank(bar, 0))
+                     : "memory");
+    else
+        asm volatile("mbarrier.arrive.relaxed.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
 // All threads of the CTA, or of the pair.
 template <int CG> __device__ __forceinline__ void group_sync()
 {
