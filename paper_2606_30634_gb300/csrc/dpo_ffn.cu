@@ -539,11 +539,11 @@ int dpo::head_product(const char *what, const HeadProduct &h, void *stream)
     m.operand(&P.a[0], h.x, h.tokens, h.dim, h.ld_x, f.a_rows);
     m.operand(&P.b[0], h.w, h.vocab, h.dim, h.dim, f.cg == 2 ? BH : f.cols);
     if (h.kept != nullptr)
-        m.bf16(&P.d0, h.kept, h.tokens, h.vocab, h.ld);
+        m.bf16(&P.d0, h.kept, blocks_of(h.vocab, kHeadStatCols) * h.kept_rows, kHeadStatCols, kHeadStatCols);
     if (h.logits != nullptr)
         m.f32(&P.d1, h.logits, h.tokens, h.vocab, h.ld);
     P.head = {h.ids, h.scale, h.target, h.maxima, h.sums, h.tokens, h.maxima != nullptr, h.kept != nullptr,
-              h.logits != nullptr};
+              h.logits != nullptr, (int)h.kept_rows};
     return run(what, *d, L, &s, 1, kHead, f, false, m.ok, stream);
 }
 

@@ -123,6 +123,7 @@ struct HeadOut {
     float2 *sums;                 // likewise: sum of e^(z - m), of e^(z - m) (z - m)
     int64_t rows;                 // pitch of the two
     int stats, keep, logits;      // sums are wanted; d0 of the kept values; d1 of z / scale in fp32
+    int kept_rows;                // of a part of kHeadCols columns of the kept values
 };
 
 // One product of a launch.
@@ -772,6 +773,7 @@ __device__ __forceinline__ void head_rows(const Product &P, Stager &st, float (&
     // 50257 product's 65 us for all rows, 43 this way).
     const float top = fmaxf(high[0], high[1]), c = H.scale * 1.4426950408889634f, r = top * c;
     const bool near = fabsf(r) < 16384.0f && fminf(low[0], low[1]) > -1e30f;
+    const int part_row = col0 / kHeadCols * H.kept_rows + row0;
     float s, w;
     if (__all_sync(0xFFFFFFFFu, near || !in)) {
         const float off = fmaf(top, c, -r);
@@ -793,7 +795,7 @@ __device__ __forceinline__ void head_rows(const Product &P, Stager &st, float (&
             }
             if (H.keep)
                 // two bytes an element, whatever they mean
-                st.bf16_of_two(&P.d0, e2, k / 32, col0 + k, row0, P.n);
+                st.bf16_of_two(&P.d0, e2, k / 32, k, part_row, kHeadCols);
         }
         const float2 s2 = of_two(add_two(ss[0], ss[1])), w2 = of_two(add_two(ww[0], ww[1]));
         const float f = exp2(-off);
@@ -820,7 +822,7 @@ __device__ __forceinline__ void head_rows(const Product &P, Stager &st, float (&
                 e2[j / 2] = *reinterpret_cast<const uint32_t *>(&h);
             }
             if (H.keep)
-                st.bf16_of_two(&P.d0, e2, k / 32, col0 + k, row0, P.n);
+                st.bf16_of_two(&P.d0, e2, k / 32, k, part_row, kHeadCols);
         }
     }
     if (in) {

@@ -98,7 +98,7 @@ struct GradArgs {
     Ids ids;
     const float *logp, *entropy, *stats, *dlogp, *dentropy;
     __nv_bfloat16 *g;
-    int64_t rows, vocab, ld;
+    int64_t rows, vocab, ld, kept_rows;
     int spans, batches;          // of a row; of kGradPieces accesses in a span
     float scale;
 };
@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(32 * kGradWarps) head_gradient_kernel(const Gr
     const float h = gb != 0.0f ? ld1(a.entropy + row) : 0.0f;
     const bool none = ga == 0.0f && gb == 0.0f;
     const float k0 = -a.scale * fmaf(gb, h, ga), k1 = -a.scale * gb * 0.6931471805599453f;
-    const __half *const e = a.kept + row * a.ld;
+    const __half *const e = a.kept + row * kHeadStatCols;
     __nv_bfloat16 *const g = a.g + row * a.ld;
     const int vocab = (int)a.vocab;
     int c0 = ((int)span * a.batches * kGradPieces * 32 + lane) * 8;
@@ -138,10 +138,11 @@ __global__ void __launch_bounds__(32 * kGradWarps) head_gradient_kernel(const Gr
             const int c = c0 + u * 256;
             q[u] = make_uint4(0u, 0u, 0u, 0u);
             top[u] = 0.0f;
-            if (c < vocab && !none) {   // whole pieces: the pitch is a multiple of 8
+            if (c < vocab && !none) {
                 asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];"
                              : "=r"(q[u].x), "=r"(q[u].y), "=r"(q[u].z), "=r"(q[u].w)
-                             : "l"(e + c));
+                             : "l"(e + (int64_t)(c / kHeadStatCols) * a.kept_rows * kHeadStatCols +
+                                   c % kHeadStatCols));
                 top[u] = ld1(a.maxima + (int64_t)(c / kHeadStatCols) * a.rows + row);
             }
         }
@@ -209,7 +210,7 @@ int check_head(const char *what, int64_t tokens, int64_t dim, int64_t vocab, flo
 
 // What is kept, and the workspaces: where each part begins.
 struct Sizes {
-    int64_t ld, parts;
+    int64_t ld, parts, kept_rows;
     int64_t kept, maxima;              // kept: the values, their maxima
     int64_t target, sums, own, logits; // forward: without kept its maxima, for `top` logits
     int64_t shares;                    // backward: G, the shares of dx
@@ -220,7 +221,8 @@ Sizes sizes_of(int64_t tokens, int64_t dim, int64_t vocab, bool keep, int top)
     Sizes s;
     s.ld = pitch_of(vocab);
     s.parts = (vocab + kHeadStatCols - 1) / kHeadStatCols;
-    s.maxima = align_up(tokens * s.ld * 2);
+    s.kept_rows = (tokens + 31) / 32 * 32;
+    s.maxima = align_up(s.parts * s.kept_rows * kHeadStatCols * 2);
     s.kept = s.maxima + align_up(s.parts * tokens * 4);
     s.target = 0;
     s.sums = align_up(tokens * 4);
@@ -325,6 +327,7 @@ extern "C" int dpo_head(const dpo_head_args *args, void *cuda_stream)
     p.ids = ids;
     p.scale = a.scale;
     p.ld = s.ld;
+    p.kept_rows = s.kept_rows;
     if (a.top == 0 || kept != nullptr) {
         p.target = reinterpret_cast<float *>(ws + s.target);
         p.sums = reinterpret_cast<float2 *>(ws + s.sums);
@@ -415,6 +418,7 @@ extern "C" int dpo_head_backward(const dpo_head_backward_args *args, void *cuda_
     g.rows = T;
     g.vocab = V;
     g.ld = s.ld;
+    g.kept_rows = s.kept_rows;
     g.scale = a.scale;
     // up to four batches a span, where that leaves CTAs enough for all SMs
     const int64_t groups = (T + kGradWarps - 1) / kGradWarps, batches = (V + kGradPieces * 256 - 1) / (kGradPieces * 256);

@@ -44,9 +44,11 @@ struct HeadProduct {
     float *target;                // z of each token's id
     float *maxima;                // [columns / kHeadStatCols][token], or nullptr: no statistics
     float2 *sums;                 // likewise
-    void *kept;                   // fp16 e^(z - maximum) times 2^15, or nullptr (with statistics)
+    void *kept;                   // fp16 e^(z - maximum) times 2^15, or nullptr (with statistics):
+    int64_t kept_rows;            // [columns / kHeadStatCols][kept_rows][kHeadStatCols], kept_rows the
+                                  // tokens to a multiple of 32
     void *logits;                 // fp32, before the scale, or nullptr
-    int64_t ld;                   // of both
+    int64_t ld;                   // its pitch
 };
 int head_product(const char *what, const HeadProduct &h, void *stream);
 
