@@ -90,7 +90,9 @@ __global__ void __launch_bounds__(32 * kJoinMaxWarps) head_join_kernel(const Joi
 //   g = -scale p (a + b (log p + h)),   p = x 2^-15 e^q,   log2 p = log2 x + q log2(e) - 15,
 // so g = x (k0 + k1 log2 x) with two factors of 128 columns of a row. The id's own element is
 // a (1 - p) from the log probability itself: a kept p near 1 would leave little of it.
-constexpr int kGradWarps = 8, kGradPieces = 4;   // rows of a CTA; accesses of 8 columns a lane
+// rows of a CTA; accesses of 8 columns a lane (by 4, 8 and 16 rows a backward of 1001 x 768 x 50257 is
+// 147, 151 and 154 us)
+constexpr int kGradWarps = 4, kGradPieces = 4;
 
 struct GradArgs {
     const __half *kept;
@@ -126,10 +128,13 @@ __global__ void __launch_bounds__(32 * kGradWarps) head_gradient_kernel(const Gr
     const float h = gb != 0.0f ? ld1(a.entropy + row) : 0.0f;
     const bool none = ga == 0.0f && gb == 0.0f;
     const float k0 = -a.scale * fmaf(gb, h, ga), k1 = -a.scale * gb * 0.6931471805599453f;
-    const __half *const e = a.kept + row * kHeadStatCols;
     __nv_bfloat16 *const g = a.g + row * a.ld;
     const int vocab = (int)a.vocab;
     int c0 = ((int)span * a.batches * kGradPieces * 32 + lane) * 8;
+    // this lane's columns in their part; the next ones are two parts on
+    const __half *e = a.kept + ((int64_t)(c0 / kHeadStatCols) * a.kept_rows + row) * kHeadStatCols + c0 % kHeadStatCols;
+    const float *largest = a.maxima + (int64_t)(c0 / kHeadStatCols) * a.rows + row;
+    const int64_t next_e = 256 * a.kept_rows, next_largest = 256 / kHeadStatCols * a.rows;
     for (int n = 0; n < a.batches && c0 < vocab; ++n, c0 += kGradPieces * 256) {
         uint4 q[kGradPieces];
         float top[kGradPieces];
@@ -141,10 +146,11 @@ __global__ void __launch_bounds__(32 * kGradWarps) head_gradient_kernel(const Gr
             if (c < vocab && !none) {
                 asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];"
                              : "=r"(q[u].x), "=r"(q[u].y), "=r"(q[u].z), "=r"(q[u].w)
-                             : "l"(e + (int64_t)(c / kHeadStatCols) * a.kept_rows * kHeadStatCols +
-                                   c % kHeadStatCols));
-                top[u] = ld1(a.maxima + (int64_t)(c / kHeadStatCols) * a.rows + row);
+                             : "l"(e));
+                top[u] = ld1(largest);
             }
+            e += next_e;
+            largest += next_largest;
         }
 #pragma unroll
         for (int u = 0; u < kGradPieces; ++u) {
