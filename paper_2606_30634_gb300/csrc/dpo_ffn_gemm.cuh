@@ -39,6 +39,8 @@
 
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 namespace dpo {
 namespace ffn {
 
@@ -770,22 +772,28 @@ __device__ __forceinline__ void head_rows(const Product &P, Stager &st, float (&
     // t = v c - r by one multiply-add, in units of 2; `off`, its value for the largest, comes
     // out at the end. For infinities and largest values whose `off` would be past 2^-11 the
     // differences of the products, in the epilogue's instructions twice as many (of the 1001 x 768 x
-    // 50257 product's 65 us for all rows, 43 this way).
+    // 50257 product's 65 us for all rows, 43 this way); by row, so that none depends on another.
     const float top = fmaxf(high[0], high[1]), c = H.scale * 1.4426950408889634f, r = top * c;
+    const float z = __fmul_rn(top, H.scale), from = z == -INFINITY ? 0.0f : z;
     const bool near = fabsf(r) < 16384.0f && fminf(low[0], low[1]) > -1e30f;
+    const float off = near ? fmaf(top, c, -r) : 0.0f;
     const int part_row = col0 / kHeadCols * H.kept_rows + row0;
-    float s, w;
-    if (__all_sync(0xFFFFFFFFu, near || !in)) {
-        const float off = fmaf(top, c, -r);
-        const Two cc = two(c, c), rr = two(-r, -r), unit = two(kHeadUnit, kHeadUnit);
-        Two ss[2] = {0, 0}, ww[2] = {0, 0};
+    const Two cc = two(c, c), rr = two(-r, -r), unit = two(kHeadUnit, kHeadUnit);
+    Two ss[2] = {0, 0}, ww[2] = {0, 0};
+    auto sums = [&](auto mixed) {
 #pragma unroll
         for (int k = 0; k < kHeadCols; k += 32) {
             uint32_t e2[16];
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                const Two t = fma_two(two(v[k + 2 * j], v[k + 2 * j + 1]), cc, rr);
-                const float2 u = of_two(t);
+                const float v0 = v[k + 2 * j], v1 = v[k + 2 * j + 1];
+                Two t = fma_two(two(v0, v1), cc, rr);
+                float2 u = of_two(t);
+                if (decltype(mixed)::value && !near) {
+                    u = make_float2((__fmul_rn(v0, H.scale) - from) * 1.4426950408889634f,
+                                    (__fmul_rn(v1, H.scale) - from) * 1.4426950408889634f);
+                    t = two(fmaxf(u.x, -1e30f), fmaxf(u.y, -1e30f));   // no infinity times 0
+                }
                 const Two e = two(exp2(u.x), exp2(u.y));
                 ss[j & 1] = add_two(ss[j & 1], e);
                 ww[j & 1] = fma_two(t, e, ww[j & 1]);
@@ -793,41 +801,20 @@ __device__ __forceinline__ void head_rows(const Product &P, Stager &st, float (&
                 const __half2 h = __floats2half2_rn(q.x, q.y);
                 e2[j] = *reinterpret_cast<const uint32_t *>(&h);
             }
-            if (H.keep)
-                // two bytes an element, whatever they mean
+            if (H.keep)   // two bytes an element, whatever they mean
                 st.bf16_of_two(&P.d0, e2, k / 32, k, part_row, kHeadCols);
         }
-        const float2 s2 = of_two(add_two(ss[0], ss[1])), w2 = of_two(add_two(ww[0], ww[1]));
-        const float f = exp2(-off);
-        s = s2.x + s2.y;
-        w = fmaf(-off, s, w2.x + w2.y) * f * 0.6931471805599453f;
-        s *= f;
-    } else {
-        const float z = __fmul_rn(top, H.scale), from = z == -INFINITY ? 0.0f : z;
-        s = w = 0.0f;
-#pragma unroll
-        for (int k = 0; k < kHeadCols; k += 32) {
-            uint32_t e2[16];
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-                float e[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const float d = __fmul_rn(v[k + j + i], H.scale) - from;
-                    e[i] = exp2(d * 1.4426950408889634f);
-                    s += e[i];
-                    w = fmaf(fmaxf(d, -1e30f), e[i], w);   // no infinity times 0
-                }
-                const __half2 h = __floats2half2_rn(e[0] * kHeadUnit, e[1] * kHeadUnit);
-                e2[j / 2] = *reinterpret_cast<const uint32_t *>(&h);
-            }
-            if (H.keep)
-                st.bf16_of_two(&P.d0, e2, k / 32, k, part_row, kHeadCols);
-        }
-    }
+    };
+    if (__all_sync(0xFFFFFFFFu, near || !in))
+        sums(std::false_type());
+    else
+        sums(std::true_type());
+    const float2 s2 = of_two(add_two(ss[0], ss[1])), w2 = of_two(add_two(ww[0], ww[1]));
+    const float f = exp2(-off), s = (s2.x + s2.y) * f;
+    const float w = fmaf(-off, s2.x + s2.y, w2.x + w2.y) * f * 0.6931471805599453f;
     if (in) {
         const int64_t i = col0 / kHeadCols * H.rows + row;
-        H.maxima[i] = __fmul_rn(top, H.scale);
+        H.maxima[i] = z;
         H.sums[i] = make_float2(s, w);
     }
 }

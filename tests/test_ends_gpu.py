@@ -186,6 +186,29 @@ def test_embed_takes_infinities_as_they_are():
     assert (d == 0).all()   # padding's gradient is not looked at
 
 
+@pytest.mark.parametrize("tokens", [1, 200, 8192])
+@pytest.mark.parametrize("vocab", [2 ** 18 - 1, 2 ** 18, 300001])
+def test_embed_backward_of_large_vocabularies(tokens, vocab):
+    """Ids on both sides of what the comparing sort packs beside a token's number."""
+    g = gen(tokens + vocab)
+    ids = torch.randint(0, vocab, (tokens,), generator=g, device=DEV)
+    ids[-1] = vocab - 1
+    if tokens > 1:
+        ids[0], ids[1] = vocab - 1, vocab
+    check_embed_backward(randn(g, tokens, 2), ids, vocab, 1.0, "f32")
+
+
+@pytest.mark.parametrize("dim,pitch", [(8, 8), (33, 33), (40, 50), (2100, 2100), (5, 5000)])
+@pytest.mark.parametrize("gd", ["f32", "bf16"])
+def test_embed_gradient_is_cleared_to_its_edges(dim, pitch, gd):
+    """Rows that begin and end anywhere: all of dtable is zero where no id is, nothing beside it."""
+    for shift in (0, 1, 3):
+        buf = torch.full((70, pitch + 4), 5.0, dtype=DT[gd], device=DEV)
+        d = buf[:, shift:shift + dim]
+        ends.embed_backward(randn(gen(1), 2, dim), torch.tensor([-1, 100], device=DEV), d)
+        assert (d == 0).all() and (buf[:, :shift] == 5).all() and (buf[:, shift + dim:] == 5).all()
+
+
 # --------------------------------------------------------------- dropout ----
 
 @pytest.mark.parametrize("rows,cols,pitch", [(1, 1, 1), (3, 7, 7), (2, 8, 8), (5, 33, 40), (4, 100, 101), (64, 256, 256),
@@ -218,6 +241,19 @@ def test_dropout_masks_do_not_depend_on_types_or_strides():
     for y in (torch.ones(300, 800, device=DEV)[:, 9:786], x.bfloat16(), x.view(3, 100, 777)):
         assert torch.equal((ends.dropout_add(y, None, 0.3, 7, site=2) != 0).view(300, 777), want)
     assert torch.equal(ends.dropout_add(x[:100, :40], None, 0.3, 7, site=2) != 0, want[:100, :40])
+
+
+@pytest.mark.parametrize("rows,cols", [(9, 255), (9, 257), (5, 1001), (5, 1002), (3, 4100), (1000, 12), (2, 70001)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_dropout_of_odd_rows(rows, cols, dtype):
+    """Rows that a warp's span, a draw or an access does not divide."""
+    g = gen(rows + cols)
+    x, r = (randn(g, rows, cols, dtype=DT[dtype]) for _ in range(2))
+    mask, share = ref.kept_mask(rows, cols, 0.3, 99, 4)
+    kept, want = ref.dropout(np64(x), None, mask, share), ref.dropout(np64(x), np64(r), mask, share)
+    within(ends.dropout_add(x, r, 0.3, 99, site=4), want, 3 * U * np.abs(kept) + (RND[dtype] + U) * np.abs(want) + TINY,
+           "y")
+    within(ends.dropout_backward(x, 0.3, 99, site=4, out=x), kept, (RND[dtype] + 3 * U) * np.abs(kept) + TINY, "dx")
 
 
 def test_dropped_elements_do_not_read_as_numbers():
@@ -440,6 +476,58 @@ def test_rows_of_odd_values(dtype, vocab):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(4000, 2050), (3999, 40), (2, 128256), (9, 40000)])
+def test_rows_by_warps_and_by_clusters(dtype, rows, vocab):
+    """So many rows that a warp has one of many batches, so few that CTAs share one."""
+    g, x, ids = logits_case(rows, vocab, dtype, seed=7)
+    check_logprobs(x, ids, 0.9, 0)
+    check_logprobs(x[:40], ids[:40], 0.9, 6)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("top", [1, 32])
+def test_shared_rows_of_odd_values(dtype, top):
+    """Rows shared by CTAs: masked but for one value, all masked, of equal values, with NaN."""
+    vocab = 100003
+    x = torch.full((5, vocab), -math.inf, device=DEV)
+    x[0, 77777] = 1.0
+    x[2] = 0.5
+    x[3] = randn(gen(1), vocab, dtype=torch.float32)
+    x[3, 50000:] = math.nan
+    x[4, ::1000] = torch.arange(0, vocab, 1000, device=DEV).float().neg()
+    x = x.to(DT[dtype])
+    o = ends.token_logprobs(x, torch.tensor([77777, 0, 5, 1, 0], device=DEV), top=top)
+    assert np.array_equal(o.top_ids.cpu().numpy(), ref.top(scaled(x, 1.0)[0], top))
+    logp, h = np64(o.logp), np64(o.entropy)
+    assert logp[0] == 0 and h[0] == 0 and np.isnan(logp[[1, 3]]).all() and np.isnan(h[[1, 3]]).all()
+    assert abs(logp[2] + math.log(vocab)) < 1e-5 and abs(h[2] - math.log(vocab)) < 1e-5
+    assert logp[4] == 0 and np64(o.top_logp)[0, 0] == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [1.0, 300.0])
+def test_logits_that_pass_the_near_range(dtype, scale):
+    """Rows whose largest value so far grows, or shrinks, past 16384 units of log 2, where sums and
+    gradients go another way, and rows altogether beyond."""
+    n = torch.arange(3001, device=DEV).float()
+    rows = [n * 13.0, 39000 - n * 13.0, n * 0.001 + 11300, n * 0.05 + 11300, n * -0.01 - 12000, n * 0.01 + 40000,
+            (n % 7) * 3000]
+    x = (torch.stack(rows) / scale).to(DT[dtype])
+    ids = torch.tensor([3000, 0, 3000, 2999, 0, 3000, 6], device=DEV)
+    o, z, i, (bl, bh, each) = check_logprobs(x, ids, scale, 3)
+    a = torch.ones(7, device=DEV)
+    d = ends.token_logprobs_backward(a, x, ids, o)
+    logs, p, _ = ref.distribution(z)
+    want = float(f32(scale)) * ref.logits_gradient(z, i, np64(a), None)
+    one = np.zeros_like(p)
+    one[np.arange(7), i] = 1
+    # one multiply-add takes m + log S, times log2(e), from the logit times a rounded factor: u of each
+    m = np.abs(z).max(1, keepdims=True)
+    pe = p * (each + 1.5 * U * np.abs(np.where(p > 0, logs, 0.0)) + 2 * U * (np.abs(z) + m) + 2.0 ** -20)
+    within(d, want, scale * (pe + 4 * U * (p + one)) + (RND[dtype] + 2 * U) * np.abs(want) + TINY, "dlogits")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("scale,size", [(1e-20, 1e38), (1e-20, 1e20), (1e6, 1e-6), (1e6, 1e30), (1.0, 1e37)])
 @pytest.mark.parametrize("top", [0, 7])
 def test_extreme_scales(dtype, scale, size, top):
@@ -514,7 +602,8 @@ def test_logprobs_gradient_by_differences():
 
 HEAD = [(1, 64, 100), (1, 8, 1), (3, 72, 33), (9, 264, 1003), (33, 520, 300), (130, 768, 2051), (257, 64, 5003), (8, 2048, 700),
         (700, 136, 129), (300, 1096, 4100), (64, 2400, 257),
-        (20, 1104, 50001), (600, 1104, 30001)]   # several tiles, each in parts of K, to a CTA and to a pair
+        (20, 1104, 50001), (600, 1104, 30001),   # several tiles, each in parts of K, to a CTA and to a pair
+        (520, 72, 20001), (64, 136, 30001), (1100, 264, 9001)]   # dx's K shared out
 
 
 def head_case(t, d, v, seed=0, pitch=0, spread=2.0):
@@ -627,6 +716,29 @@ def test_head_confident_and_padded_rows(t, d, v):
     dx = ends.head_logprobs_backward(a, kept, x, w, ids, o, dw)
     check_head_backward(x, w, ids, 1.0, a, None, o, kept, *rest, (dx, dw), "bf16")
     assert (dx[1] == 0).all() and o.logp[1] == 0
+
+
+def test_head_of_large_and_infinite_logits():
+    """Logits past 16384 units of log 2 go another way; infinite ones leave their rows no
+    distribution and the other rows theirs."""
+    g, x, w, ids = head_case(40, 64, 1003, seed=8)
+    check_head(x, w, ids, 2e4, 0, True)
+    check_head(x, w, ids, 2e4, 4, True)
+    want, _ = ends.head_logprobs(x, w, ids)
+    x = x.clone()
+    x[3] = 3e38
+    x[7, 5] = math.nan
+    o, kept = ends.head_logprobs(x, w, ids, keep=True)
+    rest = torch.ones(40, dtype=torch.bool, device=DEV)
+    rest[[3, 7]] = False
+    assert o.entropy[~rest].isnan().all()
+    assert torch.equal(o.logp[rest], want.logp[rest]) and torch.equal(o.entropy[rest], want.entropy[rest])
+    a = torch.ones(40, device=DEV)
+    a[[3, 7]] = 0      # a masked loss: their gradient is nothing, and so is their part of dw's G
+    x[3], x[7] = 0, 0  # (dw itself multiplies G with x)
+    dw = torch.empty_like(w)
+    dx = ends.head_logprobs_backward(a, kept, x, w, ids, o, dw)
+    assert (dx[~rest] == 0).all() and torch.isfinite(dx).all() and torch.isfinite(dw).all()
 
 
 def test_head_of_no_tokens_and_shapes():
