@@ -363,7 +363,7 @@ __device__ __forceinline__ void finish(const SumArgs &a, uint32_t id, int64_t c,
 }
 
 // A CTA: a chunk of the sorted pairs and 128 V columns, a thread V of them.
-template <class T, class GT, int V>
+template <class T, class GT, int V, bool ADD>
 __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const SumArgs a)
 {
     __shared__ uint2 pair_[kMaxChunk + 2];
@@ -389,12 +389,12 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const SumArgs a)
     float sum[V] = {};
     for (int i = 0; i < len; i += kSumRows) {
         Vec<T, V> v[kSumRows];
-        Vec<GT, V> old[kSumRows];
+        Vec<GT, V> old[ADD ? kSumRows : 1];
 #pragma unroll
         for (int u = 0; u < kSumRows; ++u)
             if (i + u < len)
                 v[u].load(dy + (int64_t)pair[i + u].y * a.ld_dy);
-        if (a.accumulate)   // with them, not one after the other at the ends of the runs
+        if constexpr (ADD)   // with them, not one after the other at the ends of the runs
 #pragma unroll
             for (int u = 0; u < kSumRows; ++u)
                 if (i + u < len && whole(i + u))
@@ -410,7 +410,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const SumArgs a)
                 float y[V];
 #pragma unroll
                 for (int j = 0; j < V; ++j)
-                    y[j] = a.accumulate ? fmaf(sum[j], a.scale, old[u].get(j)) : sum[j] * a.scale;
+                    y[j] = ADD ? fmaf(sum[j], a.scale, old[ADD ? u : 0].get(j)) : sum[j] * a.scale;
                 Vec<GT, V> o;
                 o.set(y);
                 o.store(table + (int64_t)pair[i + u].x * a.ld_dtable);
@@ -503,18 +503,23 @@ EmbedFn embed_fn(int tt, int ot, int v)
         return ot == DPO_F32 ? embed_fn<float, float>(v) : embed_fn<float, B16>(v);
     return ot == DPO_F32 ? embed_fn<B16, float>(v) : embed_fn<B16, B16>(v);
 }
-template <class T, class GT> SumFn sum_fn(int v, bool join)
+template <class T, class GT, bool ADD> SumFn sum_fn(int v)
+{
+    return v > 2    ? embed_sum_kernel<T, GT, wide<T, GT>(), ADD>
+           : v == 2 ? embed_sum_kernel<T, GT, 2, ADD> : embed_sum_kernel<T, GT, 1, ADD>;
+}
+template <class T, class GT> SumFn sum_fn(int v, bool join, bool add)
 {
     constexpr int W = wide<T, GT>();
     if (join)
         return v > 2 ? embed_join_kernel<GT, W> : v == 2 ? embed_join_kernel<GT, 2> : embed_join_kernel<GT, 1>;
-    return v > 2 ? embed_sum_kernel<T, GT, W> : v == 2 ? embed_sum_kernel<T, GT, 2> : embed_sum_kernel<T, GT, 1>;
+    return add ? sum_fn<T, GT, true>(v) : sum_fn<T, GT, false>(v);
 }
-SumFn sum_fn(int t, int gt, int v, bool join)
+SumFn sum_fn(int t, int gt, int v, bool join, bool add)
 {
     if (t == DPO_F32)
-        return gt == DPO_F32 ? sum_fn<float, float>(v, join) : sum_fn<float, B16>(v, join);
-    return gt == DPO_F32 ? sum_fn<B16, float>(v, join) : sum_fn<B16, B16>(v, join);
+        return gt == DPO_F32 ? sum_fn<float, float>(v, join, add) : sum_fn<float, B16>(v, join, add);
+    return gt == DPO_F32 ? sum_fn<B16, float>(v, join, add) : sum_fn<B16, B16>(v, join, add);
 }
 
 int check_table(const char *what, int64_t vocab, int64_t dim, float scale)
@@ -702,10 +707,10 @@ extern "C" int dpo_embed_backward(const dpo_embed_backward_args *args, void *cud
         su.dy = static_cast<const uint8_t *>(a.dy) + first * a.ld_dy * size;
         su.accumulate = a.accumulate || first > 0;
         const int chunks = (int)((so.count + su.chunk - 1) / su.chunk);
-        rc = launch(what, sum_fn(a.dtype, a.grad_dtype, w.v, false), (int64_t)chunks * su.segs, kSumThreads, 0,
+        rc = launch(what, sum_fn(a.dtype, a.grad_dtype, w.v, false, su.accumulate), (int64_t)chunks * su.segs, kSumThreads, 0,
                     cuda_stream, su);
         if (rc == DPO_OK && chunks > 1)
-            rc = launch(what, sum_fn(a.dtype, a.grad_dtype, w.v, true), (chunks - 1) * joins, kSumThreads, 0,
+            rc = launch(what, sum_fn(a.dtype, a.grad_dtype, w.v, true, false), (chunks - 1) * joins, kSumThreads, 0,
                         cuda_stream, su);
         if (rc != DPO_OK)
             return rc;
