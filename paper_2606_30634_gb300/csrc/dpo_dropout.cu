@@ -32,37 +32,17 @@ __device__ __forceinline__ uint4 philox(uint4 c, uint32_t k0, uint32_t k1)
 constexpr int kDraw = 8;          // elements of a draw
 constexpr int kThreads = 256;
 
-// n / d for n below 2^31 by a product and a shift: q = floor(n m / 2^(32 + s)) with
-// m = ceil(2^(32 + s) / d), 2^s the power of two below d, whose error n / 2^(32 + s) is below 1 / d.
-struct Divide {
-    uint32_t m, s;
-    __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return __umulhi(n, m) >> s; }
-};
-Divide divide_by(uint64_t d)
-{
-    uint32_t s = 0;
-    while (((uint64_t)2 << s) < d)
-        ++s;
-    return {(uint32_t)((((uint64_t)1 << (32 + s)) + d - 1) / d), s};   // d > 1
-}
-
 struct DropArgs {
     const void *x, *residual;
     void *y;
     int64_t rows, cols, ld_x, ld_residual, ld_y;
-    int64_t per_row, units;       // draws, or spans of a warp, of a row and in all
-    Divide by;                    // per_row, where units are below 2^31 and per_row above 1
+    Units units;                  // draws, or spans of a warp
     uint64_t seed;
     const uint64_t *seed_source;
     uint32_t site, cut;
     float scale;
 };
 
-__device__ __forceinline__ void row_of(const DropArgs &a, int64_t unit, int64_t &row, int64_t &at)
-{
-    row = a.per_row == 1 ? unit : a.units >> 31 ? unit / a.per_row : (int64_t)a.by((uint32_t)unit);
-    at = unit - row * a.per_row;
-}
 __device__ __forceinline__ uint64_t seed_of(const DropArgs &a)
 {
     uint64_t seed = a.seed;
@@ -83,10 +63,10 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const DropArgs a)
     const int64_t unit = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     pdl_wait();
     int64_t row, g;
-    row_of(a, min(unit, a.units - 1), row, g);
+    a.units.at(min(unit, a.units.all - 1), row, g);
     const int64_t c0 = g * kDraw;
     const uint64_t seed = seed_of(a);
-    if (unit >= a.units)
+    if (unit >= a.units.all)
         return;
     const T *const x = static_cast<const T *>(a.x) + row * a.ld_x + c0;
     const T *const r = static_cast<const T *>(a.residual) + row * a.ld_residual + c0;
@@ -132,10 +112,10 @@ __global__ void __launch_bounds__(kThreads) dropout_odd_kernel(const DropArgs a)
     const int lane = threadIdx.x & 31;
     const int64_t unit = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     pdl_wait();
-    if (unit >= a.units)
+    if (unit >= a.units.all)
         return;
     int64_t row, g;
-    row_of(a, unit, row, g);
+    a.units.at(unit, row, g);
     const uint64_t seed = seed_of(a);
     const int64_t c0 = g * 32 * kDraw + lane * V;
     const T *const x = static_cast<const T *>(a.x) + row * a.ld_x + c0;
@@ -231,15 +211,13 @@ extern "C" int dpo_dropout(const dpo_dropout_args *args, void *cuda_stream)
     k.ld_y = a.ld_y;
     // an access's elements are a draw's, or a warp's span is 32 draws'
     const int64_t span = w.v > 2 ? kDraw : 32 * kDraw, of_cta = w.v > 2 ? kThreads : kThreads / 32;
-    k.per_row = (a.cols + span - 1) / span;
-    k.units = a.rows * k.per_row;
-    k.by = k.per_row > 1 ? divide_by((uint64_t)k.per_row) : Divide{};
+    k.units = units_of(a.rows, (a.cols + span - 1) / span);
     k.seed = a.seed;
     k.seed_source = a.seed_source;
     k.site = a.site;
     k.cut = (uint32_t)cut;
     k.scale = (float)(65536.0 / (65536.0 - cut));
-    const int64_t grid = (k.units + of_cta - 1) / of_cta;
+    const int64_t grid = (k.units.all + of_cta - 1) / of_cta;
     if (grid >= kMaxCount)
         return call_fail(DPO_EINVAL, "%s: %lld x %lld is too large", what, (long long)a.rows, (long long)a.cols);
     const bool res = a.residual != nullptr;

@@ -19,42 +19,45 @@ namespace dpo {
 namespace {
 
 // ------------------------------------------------------------- forward ----
-// A warp takes some accesses a lane of one row: 2 KB of a bf16 row of 16-byte accesses, so
-// that a single token's row is shared by several warps and its latency is one access's. (us of 8192
-// tokens by 4 / 8 / 16 of them: 4094 bf16, 4 bytes an access, 27 / 21 / -; 4095 49 / - / 67.)
-__host__ __device__ constexpr int pieces(int v) { return v == 2 ? 8 : 4; }
+// A warp takes four accesses a lane of one row: 2 KB of a bf16 row of 16-byte accesses, so
+// that a single token's row is shared by several warps and its latency is one access's. Of accesses
+// of one or two elements eight, where the row has so many (us by 4 / 8 of them: 8192 tokens of
+// 4094 bf16, two an access, 27 / 21; of 4095 47 / 41; 60000 of 77 8.3 / 11).
+__host__ __device__ constexpr int pieces(int v, bool many) { return v <= 2 && many ? 8 : 4; }
 constexpr int kEmbedWarps = 8;
 
 struct EmbedArgs {
     Ids ids;
     const void *table;
     void *out;
-    int64_t tokens, vocab, dim, ld_table, ld_out, segs;
+    int64_t vocab, dim, ld_table, ld_out;
+    Units units;               // spans of a warp
     float scale;
 };
 
-template <class TT, class OT, int V>
+template <class TT, class OT, int V, bool MANY>
 __global__ void __launch_bounds__(32 * kEmbedWarps) embed_kernel(const EmbedArgs a)
 {
     const int lane = threadIdx.x & 31;
     const int64_t unit = (int64_t)blockIdx.x * kEmbedWarps + (threadIdx.x >> 5);
-    const int64_t t = unit / a.segs;
     pdl_wait();
-    if (t >= a.tokens)
+    if (unit >= a.units.all)
         return;
-    const int64_t c0 = (unit - t * a.segs) * (32 * pieces(V) * V) + lane * V;
+    int64_t t, span;
+    a.units.at(unit, t, span);
+    const int64_t c0 = span * (32 * pieces(V, MANY) * V) + lane * V;
     const int id = a.ids.at(t, a.vocab);
     const TT *const row = static_cast<const TT *>(a.table) + (int64_t)max(id, 0) * a.ld_table;
     OT *const out = static_cast<OT *>(a.out) + t * a.ld_out;
-    Vec<TT, V> v[pieces(V)];
+    Vec<TT, V> v[pieces(V, MANY)];
 #pragma unroll
-    for (int n = 0; n < pieces(V); ++n) {
+    for (int n = 0; n < pieces(V, MANY); ++n) {
         v[n].zero();
         if (id >= 0 && c0 + n * 32 * V < a.dim)
             v[n].load(row + c0 + n * 32 * V);
     }
 #pragma unroll
-    for (int n = 0; n < pieces(V); ++n) {
+    for (int n = 0; n < pieces(V, MANY); ++n) {
         float x[V];
 #pragma unroll
         for (int j = 0; j < V; ++j)
@@ -493,15 +496,19 @@ using B16 = __nv_bfloat16;
 template <class A, class B> constexpr int wide() { return sizeof(A) == 4 && sizeof(B) == 4 ? 4 : 8; }
 int wide_of(int a, int b) { return a == DPO_F32 && b == DPO_F32 ? 4 : 8; }
 
-template <class TT, class OT> EmbedFn embed_fn(int v)
+template <class TT, class OT> EmbedFn embed_fn(int v, bool many)
 {
-    return v > 2 ? embed_kernel<TT, OT, wide<TT, OT>()> : v == 2 ? embed_kernel<TT, OT, 2> : embed_kernel<TT, OT, 1>;
+    if (v > 2)
+        return embed_kernel<TT, OT, wide<TT, OT>(), false>;
+    if (v == 2)
+        return many ? embed_kernel<TT, OT, 2, true> : embed_kernel<TT, OT, 2, false>;
+    return many ? embed_kernel<TT, OT, 1, true> : embed_kernel<TT, OT, 1, false>;
 }
-EmbedFn embed_fn(int tt, int ot, int v)
+EmbedFn embed_fn(int tt, int ot, int v, bool many)
 {
     if (tt == DPO_F32)
-        return ot == DPO_F32 ? embed_fn<float, float>(v) : embed_fn<float, B16>(v);
-    return ot == DPO_F32 ? embed_fn<B16, float>(v) : embed_fn<B16, B16>(v);
+        return ot == DPO_F32 ? embed_fn<float, float>(v, many) : embed_fn<float, B16>(v, many);
+    return ot == DPO_F32 ? embed_fn<B16, float>(v, many) : embed_fn<B16, B16>(v, many);
 }
 template <class T, class GT, bool ADD> SumFn sum_fn(int v)
 {
@@ -567,14 +574,15 @@ extern "C" int dpo_embed(const dpo_embed_args *args, void *cuda_stream)
     if (!known(a.table_dtype) || !known(a.out_dtype))
         return call_fail(DPO_EDTYPE, "%s: table dtype %d, out dtype %d", what, a.table_dtype, a.out_dtype);
     EmbedArgs k{};
+    int64_t tokens = 0;
     int rc = check_table(what, a.vocab, a.dim, a.scale);
-    if (rc != DPO_OK || (rc = check_ids(what, a.ids, &k.ids, &k.tokens)) != DPO_OK || k.tokens == 0)
+    if (rc != DPO_OK || (rc = check_ids(what, a.ids, &k.ids, &tokens)) != DPO_OK || tokens == 0)
         return rc;
     const int64_t ts = elem_size(a.table_dtype), os = elem_size(a.out_dtype);
     Buffers b(what);
     add_ids(b, a.ids);
     b.add("table", a.table, a.vocab, a.dim, a.ld_table, ts, ts, false);
-    b.add("out", a.out, k.tokens, a.dim, a.ld_out, os, os, true);
+    b.add("out", a.out, tokens, a.dim, a.ld_out, os, os, true);
     if ((rc = b.done()) != DPO_OK)
         return rc;
     Width w(wide_of(a.table_dtype, a.out_dtype));
@@ -587,13 +595,14 @@ extern "C" int dpo_embed(const dpo_embed_args *args, void *cuda_stream)
     k.ld_table = a.ld_table;
     k.ld_out = a.ld_out;
     k.scale = a.scale;
-    const int64_t seg = 32 * pieces(w.v) * w.v;
-    k.segs = (a.dim + seg - 1) / seg;
-    const int64_t grid = (k.tokens * k.segs + kEmbedWarps - 1) / kEmbedWarps;
+    const bool many = a.dim > 32 * 4 * w.v;
+    const int64_t seg = 32 * pieces(w.v, many) * w.v;
+    k.units = units_of(tokens, (a.dim + seg - 1) / seg);
+    const int64_t grid = (k.units.all + kEmbedWarps - 1) / kEmbedWarps;
     if (grid >= kMaxCount)
-        return call_fail(DPO_EINVAL, "%s: %lld tokens of %lld are too many", what, (long long)k.tokens,
+        return call_fail(DPO_EINVAL, "%s: %lld tokens of %lld are too many", what, (long long)tokens,
                          (long long)a.dim);
-    return launch(what, embed_fn(a.table_dtype, a.out_dtype, w.v), grid, 32 * kEmbedWarps, 0, cuda_stream, k);
+    return launch(what, embed_fn(a.table_dtype, a.out_dtype, w.v, many), grid, 32 * kEmbedWarps, 0, cuda_stream, k);
 }
 
 extern "C" int dpo_embed_workspace(int64_t tokens, int64_t vocab, int64_t dim, int64_t *bytes)

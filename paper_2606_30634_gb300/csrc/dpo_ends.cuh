@@ -62,6 +62,36 @@ __device__ __forceinline__ void st_cluster(uint32_t addr, uint32_t a, uint32_t b
     asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
 }
 
+// n / d for n below 2^31 by a product and a shift: q = floor(n m / 2^(32 + s)) with
+// m = ceil(2^(32 + s) / d), 2^s the power of two below d, whose error n / 2^(32 + s) is below 1 / d.
+struct Divide {
+    uint32_t m, s;
+    __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return __umulhi(n, m) >> s; }
+};
+inline Divide divide_by(uint64_t d)
+{
+    uint32_t s = 0;
+    while (((uint64_t)2 << s) < d)
+        ++s;
+    return {(uint32_t)((((uint64_t)1 << (32 + s)) + d - 1) / d), s};   // d > 1
+}
+
+// Units of work that rows are made of, `per` a row; a division of 64 bits takes as many instructions
+// as a short unit's work.
+struct Units {
+    int64_t per, all;
+    Divide by;                 // per, where it is above 1 and all below 2^31
+    __device__ __forceinline__ void at(int64_t unit, int64_t &row, int64_t &place) const
+    {
+        row = per == 1 ? unit : all >> 31 ? unit / per : (int64_t)by((uint32_t)unit);
+        place = unit - row * per;
+    }
+};
+inline Units units_of(int64_t rows, int64_t per)
+{
+    return {per, rows * per, per > 1 ? divide_by((uint64_t)per) : Divide{}};
+}
+
 // ---------------------------------------------------------------- host ----
 
 // Of logits.
