@@ -7,9 +7,12 @@
 // up the rows of a chunk, id by id, in fp32. An id's run within one chunk is finished there; of
 // one that crosses chunks every chunk leaves a partial sum, and the chunks' sums are added in a
 // fixed order. So the work is even whatever the ids are, and its order depends on the ids alone.
+// (Joined by the last CTA to leave a sum, behind a fence and a counter, instead of a third launch:
+// 1.3 us more.)
 // A gradient that is written is first cleared as a whole by CTAs beside the sort's, which leaves
-// HBM idle; the rows that ids have are written twice (8192 tokens of a 32000 x 4096 buffer: 75 us
-// when the sums' launch cleared the other rows, by a bit for each).
+// HBM idle; the rows that ids have are written twice. 8192 tokens of a 32000 x 4096 bf16 buffer:
+// sort and clearing 41 us, 6.3 TB/s; sums 17; joins 6. 5003 of 50257 x 777 fp32, added: 8, 10 and 5, by
+// latency.
 #include "dpo_ends.cuh"
 #include "dpo_vec.cuh"
 
@@ -120,7 +123,7 @@ struct SortArgs {
 
 // Up to 8192 tokens: a pair's place is the number of pairs before it, counted by comparing it
 // with all of them. 67 million comparisons of two instructions each are 4 us on all SMs, with
-// no step that waits for another (the cluster's sort below, two passes: 12).
+// no step that waits for another (5003 tokens: 8 us; the cluster's sort below, two passes: 12).
 constexpr int kRankTokens = 8192, kRankBits = 13, kRankWarps = 16, kRankKeys = 4;   // keys of a warp
 constexpr uint32_t kRankNone = 0x7FFFFFFFu;
 constexpr int64_t kRankVocab = (int64_t)1 << (31 - kRankBits);

@@ -771,8 +771,10 @@ __device__ __forceinline__ void head_rows(const Product &P, Stager &st, float (&
     }
     // t = v c - r by one multiply-add, in units of 2; `off`, its value for the largest, comes
     // out at the end. For infinities and largest values whose `off` would be past 2^-11 the
-    // differences of the products, in the epilogue's instructions twice as many (of the 1001 x 768 x
-    // 50257 product's 65 us for all rows, 43 this way); by row, so that none depends on another.
+    // differences of the products, in twice as many instructions; by row, so that none depends on
+    // what lies beside it. (With values below 1024 of K this epilogue is as long as a tile's MMAs, by
+    // its latencies, not its instructions: 4 us a tile of 8 warps, a quarter of the issue slots.
+    // 16 warps of 64 columns spill: 1001 x 768 x 50257 61 -> 78 us.)
     const float top = fmaxf(high[0], high[1]), c = H.scale * 1.4426950408889634f, r = top * c;
     const float z = __fmul_rn(top, H.scale), from = z == -INFINITY ? 0.0f : z;
     const bool near = fabsf(r) < 16384.0f && fminf(low[0], low[1]) > -1e30f;
@@ -1407,7 +1409,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
                     if (lane == 0)
-                        gemm::mbar_arrive_read<CG>(acc_empty(a));   // 1001 x 256 x 50257: 60 -> 44 us
+                        gemm::mbar_arrive_read<CG>(acc_empty(a));   // 16 us less of 1001 x 256 x 50257
                 }
                 if (seen && any)
                     head_rows(P, st, v, id, row0, col0);

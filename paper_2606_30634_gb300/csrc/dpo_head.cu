@@ -6,7 +6,12 @@
 // row's parts. For `top` the logits are written and read once more (dpo_logprobs.cu).
 // Kept for the backward: e^(z - m) in fp16, and m. Forming the logits again would cost a third
 // of the backward's two products; reading this costs 2 bytes a logit.
-// Backward, two launches: G from what was kept; dx = G w and dw = G^T x, one list of tiles.
+// Backward, two launches: G from what was kept; dx = G w and dw = G^T x, one list of tiles. Where few
+// tokens leave dx a few tiles of the whole vocabulary's K, these are shared out among more tiles of
+// the list, and a third launch adds the shares up (1001 x 768 x 50257: 205 -> 147 us, the products 82
+// at the burst rate).
+// 8192 x 4096 x 32000, both: 3.6 to 3.9 ms by box and power, 0.9 to 1.0 of the sustained rate; its
+// products 1.07 and 2.24, G 0.17 (6.1 TB/s), the join 0.01.
 #include "dpo_logprobs.cuh"
 #include "dpo_products.h"
 
