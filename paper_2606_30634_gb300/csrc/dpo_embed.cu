@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(32 * kRankWarps) rank_ids_kernel(const SortArg
 // cluster. In a pass every warp ranks its own 256 pairs, in their order, among those with the
 // same digit (match.any), the counts are added up over warps and CTAs, and the pairs are sent
 // to their places, wherever in the cluster these are.
-constexpr int kSortItems = 8, kSortThreads = 1024, kSortMinThreads = 128, kSortCtas = 8;
+constexpr int kSortItems = 8, kSortThreads = 512, kSortMinThreads = 128, kSortCtas = 16;
 constexpr int kDigitBits = 9;   // of a pass, at most
 static_assert(kSortItems * kSortThreads * kSortCtas == DPO_EMBED_SPAN, "a span is a cluster's");
 
@@ -682,9 +682,11 @@ extern "C" int dpo_embed_backward(const dpo_embed_backward_args *args, void *cud
     const int sms = sm_count();
     if (sms == 0)
         return call_fail(DPO_ECUDA, "%s: no device", what);
-    const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(sort_ids_kernel),
-                                               cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               sort_smem(kSortThreads, kDigitBits));
+    const void *const sort = reinterpret_cast<const void *>(sort_ids_kernel);
+    cudaError_t e = cudaFuncSetAttribute(sort, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         sort_smem(kSortThreads, kDigitBits));
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(sort, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return call_fail(DPO_ECUDA, "%s: %s", what, cudaGetErrorString(e));
