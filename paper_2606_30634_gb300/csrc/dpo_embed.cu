@@ -368,8 +368,10 @@ __device__ __forceinline__ void finish(const SumArgs &a, uint32_t id, int64_t c,
     o.store(p);
 }
 
-// A CTA: a chunk of the sorted pairs and 128 V columns, a thread V of them.
-template <class T, class GT, int V, bool ADD>
+// A CTA: a chunk of the sorted pairs and 128 N V columns, a thread N accesses of V of them. (With
+// one access of one bf16 a row's bookkeeping is most of the instructions: 60000 tokens of 777 72 us, with
+// four 54.)
+template <class T, class GT, int V, int N, bool ADD>
 __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const SumArgs a)
 {
     __shared__ uint2 pair_[kMaxChunk + 2];
@@ -383,68 +385,88 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const SumArgs a)
     for (int i = threadIdx.x - 1; i <= len; i += kSumThreads)
         pair[i] = i0 + i < 0 || i0 + i >= n ? make_uint2(~0u, 0u) : ld_pair(a.sorted + i0 + i);
     __syncthreads();
-    const int64_t c = ((int64_t)seg * kSumThreads + threadIdx.x) * V;
+    constexpr int kStep = kSumThreads * V;   // from one access to the next
+    const int64_t c = (int64_t)seg * kStep * N + threadIdx.x * V;
     if (c >= a.dim)
         return;
+    const int own = N == 1 ? 1 : (int)min((int64_t)N, (a.dim - c + kStep - 1) / kStep);   // accesses
     const T *const dy = static_cast<const T *>(a.dy) + c;
     const uint32_t begun = pair[-1].x;   // this id's run began before this chunk
     // the last of its run, which is all in this chunk: what dtable's row takes
     auto whole = [&](int i) { return pair[i + 1].x != pair[i].x && pair[i].x != begun; };
     GT *const table = static_cast<GT *>(a.dtable) + c;
-    constexpr int kSumRows = V <= 2 ? 16 : 8;   // requested at a time
-    float sum[V] = {};
+    constexpr int kSumRows = N * V == 1 ? 16 : 8;   // requested at a time
+    float sum[N][V] = {};
     for (int i = 0; i < len; i += kSumRows) {
-        Vec<T, V> v[kSumRows];
-        Vec<GT, V> old[ADD ? kSumRows : 1];
+        Vec<T, V> v[kSumRows][N];
+        Vec<GT, V> old[ADD ? kSumRows : 1][N];
 #pragma unroll
         for (int u = 0; u < kSumRows; ++u)
             if (i + u < len)
-                v[u].load(dy + (int64_t)pair[i + u].y * a.ld_dy);
+#pragma unroll
+                for (int q = 0; q < N; ++q)
+                    if (q < own)
+                        v[u][q].load(dy + (int64_t)pair[i + u].y * a.ld_dy + q * kStep);
         if constexpr (ADD)   // with them, not one after the other at the ends of the runs
 #pragma unroll
             for (int u = 0; u < kSumRows; ++u)
                 if (i + u < len && whole(i + u))
-                    old[u].load(table + (int64_t)pair[i + u].x * a.ld_dtable);
+#pragma unroll
+                    for (int q = 0; q < N; ++q)
+                        if (q < own)
+                            old[u][q].load(table + (int64_t)pair[i + u].x * a.ld_dtable + q * kStep);
 #pragma unroll
         for (int u = 0; u < kSumRows; ++u) {
             if (i + u >= len)
                 break;
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                sum[j] += v[u].get(j);
-            if (whole(i + u)) {
-                float y[V];
+            for (int q = 0; q < N; ++q)
 #pragma unroll
                 for (int j = 0; j < V; ++j)
-                    y[j] = ADD ? fmaf(sum[j], a.scale, old[ADD ? u : 0].get(j)) : sum[j] * a.scale;
-                Vec<GT, V> o;
-                o.set(y);
-                o.store(table + (int64_t)pair[i + u].x * a.ld_dtable);
+                    sum[q][j] += v[u][q].get(j);
+            if (whole(i + u)) {
+#pragma unroll
+                for (int q = 0; q < N; ++q) {
+                    float y[V];
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        y[j] = ADD ? fmaf(sum[q][j], a.scale, old[ADD ? u : 0][q].get(j)) : sum[q][j] * a.scale;
+                    Vec<GT, V> o;
+                    o.set(y);
+                    if (q < own)
+                        o.store(table + (int64_t)pair[i + u].x * a.ld_dtable + q * kStep);
+                }
             } else if (i + u + 1 == len || pair[i + u + 1].x != pair[i + u].x) {
                 float *const p = a.partial + ((int64_t)chunk * 2 + (pair[i + u].x == begun)) * a.dim + c;
 #pragma unroll
-                for (int j = 0; j < V; ++j)
-                    p[j] = sum[j];
+                for (int q = 0; q < N; ++q)
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        if (q < own)
+                            p[q * kStep + j] = sum[q][j];
             } else {
                 continue;
             }
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                sum[j] = 0.0f;
+            for (int q = 0; q < N; ++q)
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    sum[q][j] = 0.0f;
         }
     }
 }
 
 // The runs that cross chunks: the CTA of the chunk where one begins adds its chunks' sums, its four
-// warps every fourth of them, 32 V columns a CTA.
+// warps every fourth of them, 32 N V columns a CTA.
 constexpr int kJoinWarps = kSumThreads / 32;
 
-template <class GT, int V>
+template <class GT, int V, int N>
 __global__ void __launch_bounds__(kSumThreads) embed_join_kernel(const SumArgs a)
 {
-    __shared__ float sums[kJoinWarps - 1][32 * V];
+    constexpr int kCols = 32 * N * V;
+    __shared__ float sums[kJoinWarps - 1][kCols];
     pdl_wait();
-    const int segs = (int)((a.dim + 32 * V - 1) / (32 * V));
+    const int segs = (int)((a.dim + kCols - 1) / kCols);
     const int chunk = (int)blockIdx.x / segs, seg = (int)blockIdx.x - chunk * segs;
     const int i0 = chunk * a.chunk, i1 = i0 + a.chunk, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // all at once: the list has room for the pair after this chunk, which is not the last one
@@ -463,31 +485,39 @@ __global__ void __launch_bounds__(kSumThreads) embed_join_kernel(const SumArgs a
             break;
         }
     }
-    const int64_t c = ((int64_t)seg * 32 + lane) * V;
-    const bool in = c < a.dim;
-    float sum[V] = {};
+    const int64_t c = (int64_t)seg * kCols + lane * V;
+    float sum[N][V] = {};
     // the chunk's own sum, then those of runs that did not begin where they lie
 #pragma unroll 4
     for (int k = chunk + warp; k <= last; k += kJoinWarps) {
         const float *const p = a.partial + ((int64_t)k * 2 + (k != chunk)) * a.dim + c;
-        if (in)
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                sum[j] += p[j];
+        for (int q = 0; q < N; ++q)
+            if (c + q * 32 * V < a.dim)
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    sum[q][j] += p[q * 32 * V + j];
     }
     if (warp > 0)
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            sums[warp - 1][lane * V + j] = sum[j];
+        for (int q = 0; q < N; ++q)
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                sums[warp - 1][(q * 32 + lane) * V + j] = sum[q][j];
     __syncthreads();
-    if (warp > 0 || !in)
+    if (warp > 0)
         return;
 #pragma unroll
-    for (int w = 0; w < kJoinWarps - 1; ++w)
+    for (int q = 0; q < N; ++q) {
+        if (c + q * 32 * V >= a.dim)
+            break;
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            sum[j] += sums[w][lane * V + j];
-    finish<GT, V>(a, id, c, sum);
+        for (int w = 0; w < kJoinWarps - 1; ++w)
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                sum[q][j] += sums[w][(q * 32 + lane) * V + j];
+        finish<GT, V>(a, id, c + q * 32 * V, sum[q]);
+    }
 }
 
 // ---------------------------------------------------------------- host ----
@@ -513,23 +543,44 @@ EmbedFn embed_fn(int tt, int ot, int v, bool many)
         return ot == DPO_F32 ? embed_fn<float, float>(v, many) : embed_fn<float, B16>(v, many);
     return ot == DPO_F32 ? embed_fn<B16, float>(v, many) : embed_fn<B16, B16>(v, many);
 }
-template <class T, class GT, bool ADD> SumFn sum_fn(int v)
+// The accesses of a thread: several of few elements, where that leaves each SM so many CTAs.
+int accesses(int v, int64_t chunks, int64_t dim, int threads, int64_t ctas)
 {
-    return v > 2    ? embed_sum_kernel<T, GT, wide<T, GT>(), ADD>
-           : v == 2 ? embed_sum_kernel<T, GT, 2, ADD> : embed_sum_kernel<T, GT, 1, ADD>;
+    const int n = v == 1 ? 4 : v == 2 ? 2 : 1;
+    const int64_t cols = (int64_t)n * threads * v;
+    return chunks * ((dim + cols - 1) / cols) >= ctas ? n : 1;
 }
-template <class T, class GT> SumFn sum_fn(int v, bool join, bool add)
+template <class T, class GT, bool ADD> SumFn sum_fn(int v, int n)
 {
-    constexpr int W = wide<T, GT>();
-    if (join)
-        return v > 2 ? embed_join_kernel<GT, W> : v == 2 ? embed_join_kernel<GT, 2> : embed_join_kernel<GT, 1>;
-    return add ? sum_fn<T, GT, true>(v) : sum_fn<T, GT, false>(v);
+    if (v > 2)
+        return embed_sum_kernel<T, GT, wide<T, GT>(), 1, ADD>;
+    if (v == 2)
+        return n > 1 ? embed_sum_kernel<T, GT, 2, 2, ADD> : embed_sum_kernel<T, GT, 2, 1, ADD>;
+    return n > 1 ? embed_sum_kernel<T, GT, 1, 4, ADD> : embed_sum_kernel<T, GT, 1, 1, ADD>;
 }
-SumFn sum_fn(int t, int gt, int v, bool join, bool add)
+template <class T, class GT> SumFn sum_fn(int v, int n, bool add)
+{
+    return add ? sum_fn<T, GT, true>(v, n) : sum_fn<T, GT, false>(v, n);
+}
+SumFn sum_fn(int t, int gt, int v, int n, bool add)
 {
     if (t == DPO_F32)
-        return gt == DPO_F32 ? sum_fn<float, float>(v, join, add) : sum_fn<float, B16>(v, join, add);
-    return gt == DPO_F32 ? sum_fn<B16, float>(v, join, add) : sum_fn<B16, B16>(v, join, add);
+        return gt == DPO_F32 ? sum_fn<float, float>(v, n, add) : sum_fn<float, B16>(v, n, add);
+    return gt == DPO_F32 ? sum_fn<B16, float>(v, n, add) : sum_fn<B16, B16>(v, n, add);
+}
+template <class GT, int W> SumFn join_fn(int v, int n)
+{
+    if (v > 2)
+        return embed_join_kernel<GT, W, 1>;
+    if (v == 2)
+        return n > 1 ? embed_join_kernel<GT, 2, 2> : embed_join_kernel<GT, 2, 1>;
+    return n > 1 ? embed_join_kernel<GT, 1, 4> : embed_join_kernel<GT, 1, 1>;
+}
+SumFn join_fn(int t, int gt, int v, int n)
+{
+    if (gt == DPO_F32)
+        return t == DPO_F32 ? join_fn<float, 4>(v, n) : join_fn<float, 8>(v, n);
+    return join_fn<B16, 8>(v, n);
 }
 
 int check_table(const char *what, int64_t vocab, int64_t dim, float scale)
@@ -669,19 +720,21 @@ extern "C" int dpo_embed_backward(const dpo_embed_backward_args *args, void *cud
     su.ld_dtable = a.ld_dtable;
     su.scale = a.scale;
     su.chunk = plan.chunk;
-    const int64_t seg = (int64_t)kSumThreads * w.v;
+    const int sms = sm_count();
+    if (sms == 0)
+        return call_fail(DPO_ECUDA, "%s: no device", what);
+    const int each = accesses(w.v, plan.chunks, a.dim, kSumThreads, (int64_t)8 * sms);
+    const int join_each = accesses(w.v, plan.chunks, a.dim, 32, (int64_t)16 * sms);
+    const int64_t seg = (int64_t)kSumThreads * w.v * each;
     su.segs = (int)((a.dim + seg - 1) / seg);
     int bits = 1;   // of the ids and of the padding's key
     while ((a.vocab >> bits) != 0)
         ++bits;
     so.passes = (bits + kDigitBits - 1) / kDigitBits;
     so.bits = (bits + so.passes - 1) / so.passes;
-    const int64_t joins = (a.dim + 32 * w.v - 1) / (32 * w.v);
+    const int64_t joins = (a.dim + 32 * join_each * w.v - 1) / (32 * join_each * w.v);
     if ((int64_t)plan.chunks * joins >= kMaxCount)
         return call_fail(DPO_EINVAL, "%s: %lld columns are too many", what, (long long)a.dim);
-    const int sms = sm_count();
-    if (sms == 0)
-        return call_fail(DPO_ECUDA, "%s: no device", what);
     const void *const sort = reinterpret_cast<const void *>(sort_ids_kernel);
     cudaError_t e = cudaFuncSetAttribute(sort, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          sort_smem(kSortThreads, kDigitBits));
@@ -721,10 +774,10 @@ extern "C" int dpo_embed_backward(const dpo_embed_backward_args *args, void *cud
         su.dy = static_cast<const uint8_t *>(a.dy) + first * a.ld_dy * size;
         su.accumulate = a.accumulate || first > 0;
         const int chunks = (int)((so.count + su.chunk - 1) / su.chunk);
-        rc = launch(what, sum_fn(a.dtype, a.grad_dtype, w.v, false, su.accumulate), (int64_t)chunks * su.segs, kSumThreads, 0,
+        rc = launch(what, sum_fn(a.dtype, a.grad_dtype, w.v, each, su.accumulate), (int64_t)chunks * su.segs, kSumThreads, 0,
                     cuda_stream, su);
         if (rc == DPO_OK && chunks > 1)
-            rc = launch(what, sum_fn(a.dtype, a.grad_dtype, w.v, true, false), (chunks - 1) * joins, kSumThreads, 0,
+            rc = launch(what, join_fn(a.dtype, a.grad_dtype, w.v, join_each), (chunks - 1) * joins, kSumThreads, 0,
                         cuda_stream, su);
         if (rc != DPO_OK)
             return rc;
