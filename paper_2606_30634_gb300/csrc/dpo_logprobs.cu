@@ -55,9 +55,9 @@ __device__ __forceinline__ void merge_warps(K &p, K (*lists)[32], int warps, int
     row_sync(warps);
 }
 
-// A warp, a CTA or a cluster has a row, a cluster's CTAs in equal spans; accesses of 16 bytes from the span's first
-// boundary on, so rows of odd pitches cost two short ends. A thread takes kBatch logits at a time,
-// their largest first.
+// A warp, a CTA or a cluster has a row, a cluster's CTAs in equal spans; accesses of 16 bytes from
+// the span's first boundary on, so rows of odd pitches cost two short ends. A thread takes kBatch
+// logits at a time, their largest first.
 // The `top` largest: each thread knows the largest of its own values, and the top-th of these
 // bounds the top-th of all from below. So only the threads whose largest reaches the bound, `top`
 // and what is equal, can hold one of them; their values are read again, and what reaches the
@@ -313,10 +313,16 @@ template <class T> struct RowGradient {
         const __nv_bfloat162 q = __float2bfloat162_rn(fmaxf((r - 1000.0f) / c, -1e30f));
         *v = *reinterpret_cast<const uint32_t *>(&q);
     }
-    __device__ __forceinline__ float other(float logit) const
+    __device__ __forceinline__ bool near() const { return fabsf(r) < 16384.0f; }
+    __device__ __forceinline__ float other(float logit) const   // row_gradient's, one at a time
     {
-        const float t = kAccurate ? __fmul_rn(logit, scale) - m - logs
-                                  : fmaf(fmaf(logit, scale, -m), kLog2e, -logs * kLog2e);
+        float t;
+        if constexpr (kAccurate)
+            t = __fmul_rn(logit, scale) - m - logs;
+        else if (near())
+            t = fmaf(logit == logit ? fmaxf(logit, __uint_as_float(low << 16)) : logit, c, -r);
+        else
+            t = fmaf(fmaf(logit, scale, -m), kLog2e, -logs * kLog2e);
         const float p = kAccurate ? expf(t) : exp2_fast(t);
         return p * fmaf(k1, fmaxf(t, -1e30f), k0);   // no infinity times 0
     }
@@ -337,7 +343,7 @@ template <class T> struct RowGradient {
 template <class T, int V>
 __device__ __forceinline__ void row_gradient(const RowGradient<T> &f, const Vec<T, V> &v, float (&g)[V])
 {
-    if (sizeof(T) == 4 || V == 1 || !(fabsf(f.r) < 16384.0f)) {
+    if (sizeof(T) == 4 || V == 1 || !f.near()) {
 #pragma unroll
         for (int j = 0; j < V; ++j)
             g[j] = f.other(v.get(j));
