@@ -3,7 +3,7 @@
 //
 // Forward: every logit is read once; a thread keeps the running maximum m, sum S and entropy
 // sum W of its own, and the threads' are joined. Backward: every logit once more, dlogits
-// written. Both are bound by HBM (4096 x 50257 bf16: 71 and 132 us, 5.8 and 6.2 TB/s); few rows
+// written. Both are bound by HBM (4096 x 50257 bf16: 66 and 132 us, 6.2 TB/s both); few rows
 // by latency, where a cluster shares a row. What instructions they take is seen: with 15 an
 // element instead of 6 the forward took 107 us, with 20 instead of 7 the backward 180.
 #include "dpo_logprobs.cuh"
@@ -56,8 +56,8 @@ __device__ __forceinline__ void merge_warps(K &p, K (*lists)[32], int warps, int
 }
 
 // A warp, a CTA or a cluster has a row, a cluster's CTAs in equal spans; accesses of 16 bytes from
-// the span's first boundary on, so rows of odd pitches cost two short ends. A thread takes kBatch
-// logits at a time, their largest first.
+// the span's first boundary on, so rows of odd pitches cost two short ends. A thread takes kAhead
+// accesses at a time, their largest first (4096 x 50257 bf16: 71 us by four, 66 by eight).
 // The `top` largest: each thread knows the largest of its own values, and the top-th of these
 // bounds the top-th of all from below. So only the threads whose largest reaches the bound, `top`
 // and what is equal, can hold one of them; their values are read again, and what reaches the
@@ -66,13 +66,13 @@ __device__ __forceinline__ void merge_warps(K &p, K (*lists)[32], int warps, int
 // fp32 - / 12.4 / 9.4; with 5 of 1000 rows of 32000 fp32 64 / 128 / 256: 25.7 / 25.6 / 27.2, 4000
 // rows 117 / 92 / 92 (a bound from few threads lets more values be read again). 4000 rows of
 // 32000 fp32: 76 us, 6.7 TB/s, 0.99 of the measured copy.
-constexpr int kBatch = 32, kSmThreads = 800, kTopThreads = 128;
+constexpr int kAhead = 8, kBatch = 32, kSmThreads = 800, kTopThreads = 128;
 
 template <class T, bool TOP>
 __global__ void __launch_bounds__(kMaxThreads, 2) logprobs_kernel(const LogArgs a)
 {
     using Access = RowAccess<T>;
-    constexpr int V = Access::V, U = kBatch / V;
+    constexpr int V = Access::V, U = kAhead;
     __shared__ Part parts[kMaxWarps], from_cta[kMaxCtas];
     constexpr int kLists = TOP ? kMaxWarps : 1;
     __shared__ Key lists_[kLists][32], list_from[TOP ? kMaxCtas : 1][32];
@@ -168,12 +168,12 @@ __global__ void __launch_bounds__(kMaxThreads, 2) logprobs_kernel(const LogArgs 
         // 32 of a thread's accesses are a block; the warps take the blocks in turn
         const int blocks = (body + 32 * nt - 1) / (32 * nt), all = counts[0] * blocks;
         auto scan = [&](auto &&use) {   // by whole warps
-            constexpr int kAhead = 2;
-            for (int k0 = warp; k0 < all; k0 += warps * kAhead) {
-                Access v[kAhead];
-                int q[kAhead];
+            constexpr int kBoth = 2;
+            for (int k0 = warp; k0 < all; k0 += warps * kBoth) {
+                Access v[kBoth];
+                int q[kBoth];
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
+                for (int u = 0; u < kBoth; ++u) {
                     const int k = k0 + u * warps, i = k / blocks;
                     v[u].none();
                     q[u] = k < all ? chosen[i] + ((k - i * blocks) * 32 + lane) * nt : body;
@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(kMaxThreads, 2) logprobs_kernel(const LogArgs 
                         v[u].v.load(vectors + (int64_t)q[u] * V);
                 }
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
+                for (int u = 0; u < kBoth; ++u) {
                     const bool in = q[u] < body && !(__fmul_rn(v[u].largest(), a.scale) < bound);
                     if (__any_sync(0xFFFFFFFFu, in))
 #pragma unroll
@@ -485,7 +485,7 @@ extern "C" int dpo_logprobs(const dpo_logprobs_args *args, void *cuda_stream)
     k.scale = a.scale;
     k.top = a.top;
     // As few threads of a row as give every SM kSmThreads, so that little is joined; where there
-    // are too few rows for that, as many as find a batch, and then the CTAs of a cluster.
+    // are too few rows for that, as many as find kBatch logits each, and then the CTAs of a cluster.
     int threads = 32, ctas = 1;
     while (threads < kMaxThreads && (int64_t)threads * kBatch < a.vocab &&
            (a.rows * threads < (int64_t)sms * kSmThreads || (a.top > 0 && threads < kTopThreads)))
