@@ -61,7 +61,8 @@ __device__ __forceinline__ void merge_warps(K &p, K (*lists)[32], int warps, int
 // The `top` largest: each thread knows the largest of its own values, and the top-th of these
 // bounds the top-th of all from below. So only the threads whose largest reaches the bound, `top`
 // and what is equal, can hold one of them; their values are read again, and what reaches the
-// bound is sorted, or offered to lists where it is much (equal values, masked rows).
+// bound is sorted, or offered to lists where it is much (equal values, masked rows): more than 32
+// values a warp, or 128 (7 rows of 199 bf16 with 20: 31 us by lists, for more than 32).
 // us by the threads of a row, 32 / 128 / 512: 4096 rows of 50257 bf16 71 / 77 / 104, 300 of 32000
 // fp32 - / 12.4 / 9.4; with 5 of 1000 rows of 32000 fp32 64 / 128 / 256: 25.7 / 25.6 / 27.2, 4000
 // rows 117 / 92 / 92 (a bound from few threads lets more values be read again). 4000 rows of
@@ -85,7 +86,9 @@ __global__ void __launch_bounds__(kMaxThreads, 2) logprobs_kernel(const LogArgs 
     const uint32_t rank = cta_of_cluster(), ranks = ctas_of_cluster();
     const int64_t its = ranks > 1 ? blockIdx.x / ranks : (int64_t)blockIdx.x * (blockDim.x / nt) + first_warp;
     const int64_t row = min(its, a.rows - 1);
-    Key (*const lists)[32] = lists_ + (TOP ? first_warp : 0);
+    constexpr int kRowLists = 4;   // of a row, at least; a CTA has four rows at most
+    Key (*const lists)[32] = lists_ + (TOP ? kRowLists * first_warp : 0);
+    const int room = 32 * max(warps, kRowLists);
     const int vocab = (int)a.vocab, share = (int)((a.vocab + ranks - 1) / ranks);
     const int begin = (int)min((int64_t)share * rank, a.vocab), n = min(share, vocab - begin);
     if (ranks > 1)
@@ -195,18 +198,25 @@ __global__ void __launch_bounds__(kMaxThreads, 2) logprobs_kernel(const LogArgs 
         scan([&](bool in, float z, int at) {
             if (in && !(z < bound) && (z == z || bound == -INFINITY)) {
                 const int slot = atomicAdd(counts + 1, 1);
-                if (slot < nt)
+                if (slot < room)
                     lists[0][slot] = key_of(z, at);
             }
         });
         row_sync(warps);
         const int found = counts[1];
-        if (found <= nt) {
-            mine = thread < found ? lists[warp][lane] : 0;
-            if (32 * warp < found)
-                sort_lanes(mine, lane);
-            if (found > 32)
+        if (found <= room) {
+            for (int l = warp; 32 * l < found; l += warps) {
+                Key more = 32 * l + lane < found ? lists[l][lane] : 0;
+                sort_lanes(more, lane);
+                if (l == warp)
+                    mine = more;
+                else
+                    merge_lanes(mine, __shfl_sync(0xFFFFFFFFu, more, 31 - lane), lane);
+            }
+            if (found > 32 && warps > 1) {
+                row_sync(warps);
                 merge_warps(mine, lists, warps, warp, lane);
+            }
         } else {
             TopList list{0, key_of(bound, 0x7FFFFFFF), a.top, lane};
             row_sync(warps);
@@ -489,6 +499,11 @@ extern "C" int dpo_logprobs(const dpo_logprobs_args *args, void *cuda_stream)
     int threads = 32, ctas = 1;
     while (threads < kMaxThreads && (int64_t)threads * kBatch < a.vocab &&
            (a.rows * threads < (int64_t)sms * kSmThreads || (a.top > 0 && threads < kTopThreads)))
+        threads *= 2;
+    // The bound by few of many threads, where a first access each leaves some to others: 500 rows of
+    // 300 fp32 with 32: 41 us by 32 threads, 9 by 128; but 5000 of 900 bf16 with 20: 31 and 38.
+    while (threads < kTopThreads && threads * (16 / size) < a.vocab &&
+           (a.top > 24 || (2 * a.top > threads && a.rows * threads < (int64_t)sms * kSmThreads)))
         threads *= 2;
     k.warps = threads / 32;
     const int per = k.warps == 1 ? 4 : 1;   // rows of a CTA

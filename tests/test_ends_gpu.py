@@ -485,6 +485,16 @@ def test_rows_by_warps_and_by_clusters(dtype, rows, vocab):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [33, 64, 100, 199, 300, 1000, 1500, 4000])
+@pytest.mark.parametrize("rows", [1, 7, 400])
+def test_many_alternatives_of_few(dtype, vocab, rows):
+    """More of a row reaches the threads' bound than a warp sorts at once."""
+    g, x, ids = logits_case(rows, vocab, dtype, seed=11)
+    for top in (20, 31, 32):
+        check_logprobs(x, ids, 1.0, top)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("top", [1, 32])
 def test_shared_rows_of_odd_values(dtype, top):
     """Rows shared by CTAs: masked but for one value, all masked, of equal values, with NaN."""
