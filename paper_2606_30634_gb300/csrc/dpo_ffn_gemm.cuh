@@ -1482,7 +1482,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
 }
 
 // out = the sum of a split product's shares, in their order.
-constexpr int kSumThreads = 256;
+constexpr int kSumThreads = 128;
 __global__ void __launch_bounds__(kSumThreads) sum_shares_kernel(const float *shares, __nv_bfloat16 *out,
                                                                  int64_t rows, int64_t cols, int64_t ld_out,
                                                                  int64_t share, int ways)
@@ -1494,7 +1494,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_shares_kernel(const float *sh
         return;
     const float *p = shares + row * cols + col;
     float sum[8] = {};
-#pragma unroll 4
+#pragma unroll 8
     for (int w = 0; w < ways; ++w, p += share) {
         float v[8];
         ld8(p, v);
