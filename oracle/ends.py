@@ -1,4 +1,4 @@
-"""The two ends of a pipeline in 64 bits (numpy): the definitions that include/dpo_ends.h
+"""The two ends of a pipeline in 64 bits (numpy): the definitions that include/dpo.h
 states for dpo_embed, dpo_dropout, dpo_logprobs, dpo_head and their backward passes, written
 from the formulas. Test infrastructure; shares no code with the package.
 """

@@ -47,13 +47,13 @@ LIBS = {
                     "csrc/dpo_ffn_gemm.cuh", "csrc/dpo_ffn_few.cuh", "csrc/dpo_check.h",
                     "csrc/dpo_vec.cuh", "csrc/dpo_two.cuh", "csrc/dpo_ends.cuh", "csrc/dpo_ids.cuh",
                     "csrc/dpo_logprobs.cuh", "csrc/dpo_products.h",
-                    "../include/dpo.h", "../include/dpo_muon.h", "../include/dpo_ends.h"],
+                    "../include/dpo.h", "../include/dpo_muon.h"],
         "includes": ["csrc"],
         "ptxas_v": ["csrc/dpo_step_adamw.cu", "csrc/dpo_muon.cu", "csrc/dpo_ffn.cu"],
     },
     "dpo_tensors.so": {
         "sources": ["csrc/dpo_tensors.cpp"],
-        "headers": ["../include/dpo.h", "../include/dpo_ends.h"],
+        "headers": ["../include/dpo.h"],
         "includes": [],
         "ptxas_v": [],
         "torch": True,

@@ -1,5 +1,5 @@
 // dpo_dropout.cu -- residual + dropout(x) with a mask that is drawn and not stored
-// (dpo_dropout in include/dpo_ends.h).
+// (dpo_dropout in include/dpo.h).
 //
 // The mask's bits are a function of the element's place, so the backward pass draws the same
 // ones and nothing is kept. One draw of the generator is 128 bits, 16 for each of eight

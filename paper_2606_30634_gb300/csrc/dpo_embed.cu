@@ -1,5 +1,5 @@
 // dpo_embed.cu -- the embedding of token ids and its gradient (dpo_embed, dpo_embed_backward in
-// include/dpo_ends.h).
+// include/dpo.h).
 //
 // Forward: out[t] = scale table[id_t]; one pass, the rows' bytes in and out.
 // Backward: dtable[v] = scale sum over the t with id_t = v of dy[t]. The tokens are sorted by id

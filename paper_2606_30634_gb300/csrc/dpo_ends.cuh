@@ -1,10 +1,9 @@
-// dpo_ends.cuh -- what the kernels of dpo_ends.h share: the cluster's shared memory, and checks
+// dpo_ends.cuh -- what the kernels of the pipeline's ends share: the cluster's shared memory, and checks
 // of ids.
 #pragma once
 
 #include "dpo_check.h"
 #include "dpo_device.cuh"
-#include "dpo_ends.h"
 #include "dpo_ids.cuh"
 
 namespace dpo {

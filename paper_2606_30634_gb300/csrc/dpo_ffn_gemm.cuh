@@ -210,6 +210,19 @@ __device__ __forceinline__ void launch_dependents()
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+// mbar_arrive by a warp that has read TMEM, waited for it (tcgen05.wait::ld) and fenced its reads
+// (tcgen05.fence::before_thread_sync): nothing else of its is ordered, so that stores to global
+// memory that are under way are not waited for.
+template <int CG> __device__ __forceinline__ void mbar_arrive_read(uint32_t bar)
+{
+    if (CG == 2)
+        asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+                         map_to_rank(bar, 0))
+                     : "memory");
+    else
+        asm volatile("mbarrier.arrive.relaxed.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
 // 2-D TMA load and store (see the 3-D ones in dpo_gemm.cuh).
 template <int CG>
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int x, int y,
@@ -492,6 +505,22 @@ struct Stager {
     }
 };
 
+// tmem_ld32 without its wait (tcgen05.wait::ld), which comes before its results are used.
+__device__ __forceinline__ void tmem_ld32_ahead(uint32_t taddr, uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+          "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+          "=r"(r[31])
+        : "r"(taddr));
+}
+
 __device__ __forceinline__ void load_acc(uint32_t acc, float (&v)[32])
 {
     uint32_t r[32];
@@ -507,7 +536,7 @@ __device__ __forceinline__ void load_acc_ahead(uint32_t acc, float (&v)[kHeadCol
     uint32_t r[4][32];
 #pragma unroll
     for (int c = 0; c < 4; ++c)
-        gemm::tmem_ld32_ahead(acc + (uint32_t)(32 * c), r[c]);
+        tmem_ld32_ahead(acc + (uint32_t)(32 * c), r[c]);
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
     for (int j = 0; j < kHeadCols; ++j)
@@ -1409,7 +1438,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
                     if (lane == 0)
-                        gemm::mbar_arrive_read<CG>(acc_empty(a));   // 16 us less of 1001 x 256 x 50257
+                        mbar_arrive_read<CG>(acc_empty(a));   // 16 us less of 1001 x 256 x 50257
                 }
                 if (seen && any)
                     head_rows(P, st, v, id, row0, col0);

@@ -208,19 +208,6 @@ template <int CG> __device__ __forceinline__ void mbar_arrive(uint32_t bar)
         asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// The same by a warp that has read TMEM, waited for it (tcgen05.wait::ld) and fenced its reads
-// (tcgen05.fence::before_thread_sync): nothing else of its is ordered, so that stores to global
-// memory that are under way are not waited for.
-template <int CG> __device__ __forceinline__ void mbar_arrive_read(uint32_t bar)
-{
-    if (CG == 2)
-        asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(
-                         map_to_rank(bar, 0))
-                     : "memory");
-    else
-        asm volatile("mbarrier.arrive.relaxed.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-
 // All threads of the CTA, or of the pair.
 template <int CG> __device__ __forceinline__ void group_sync()
 {
@@ -329,8 +316,7 @@ template <int CG> __device__ __forceinline__ void tmem_free(uint32_t tmem)
                      : "memory");
 }
 
-// To be waited for (tcgen05.wait::ld) before its results are used.
-__device__ __forceinline__ void tmem_ld32_ahead(uint32_t taddr, uint32_t (&r)[32])
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32])
 {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
@@ -343,10 +329,6 @@ __device__ __forceinline__ void tmem_ld32_ahead(uint32_t taddr, uint32_t (&r)[32
           "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
           "=r"(r[31])
         : "r"(taddr));
-}
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32])
-{
-    tmem_ld32_ahead(taddr, r);
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 

@@ -1,5 +1,5 @@
 // dpo_head.cu -- the head: log probabilities from the stream and the head's weights, and the
-// gradients of both (dpo_head, dpo_head_backward in include/dpo_ends.h).
+// gradients of both (dpo_head, dpo_head_backward in include/dpo.h).
 //
 // Forward, two launches: the product x w^T, whose epilogue reduces 128 columns of a row to
 // (maximum m, sum of e^(z - m), entropy sum), so that no logits are written; and the join of a

@@ -1,5 +1,5 @@
 // dpo_logprobs.cu -- log probabilities of given tokens, entropy and most likely ids from logits,
-// and their gradient (dpo_logprobs, dpo_logprobs_backward in include/dpo_ends.h).
+// and their gradient (dpo_logprobs, dpo_logprobs_backward in include/dpo.h).
 //
 // Forward: every logit is read once; a thread keeps the running maximum m, sum S and entropy
 // sum W of its own, and the threads' are joined. Backward: every logit once more, dlogits

@@ -1,5 +1,5 @@
 // dpo_tensors.cpp -- the feed-forward calls of include/dpo.h and those of
-// include/dpo_ends.h on PyTorch tensors: the part of ffn.py and ends.py between their
+// include/dpo.h on PyTorch tensors: the part of ffn.py and ends.py between their
 // signatures and the C ABI (checks, pitches, outputs and workspaces from PyTorch's
 // allocator, the current stream), as a Python module.
 //
@@ -24,7 +24,6 @@
 #include <string>
 
 #include "dpo.h"
-#include "dpo_ends.h"
 
 namespace {
 

@@ -43,7 +43,12 @@ EXPORTS = ("dpo_init", "dpo_stash", "dpo_step", "dpo_read_weights", "dpo_get_ste
            "dpo_set_timing", "dpo_get_timing", "dpo_pack8", "dpo_unpack8", "dpo_rmsnorm",
            "dpo_rmsnorm_backward", "dpo_rmsnorm_workspace", "dpo_ffn_forward",
            "dpo_ffn_backward", "dpo_ffn_workspace", "dpo_ffn_get_status",
-           "dpo_ffn_clear_status", "dpo_ffn_test_forms")
+           "dpo_ffn_clear_status", "dpo_ffn_test_forms", "dpo_embed", "dpo_embed_backward",
+           "dpo_embed_workspace", "dpo_dropout", "dpo_logprobs", "dpo_logprobs_backward",
+           "dpo_head", "dpo_head_backward", "dpo_head_workspace")
+
+DPO_EMBED_SPAN = 65536
+DPO_MAX_TOP = 32
 
 DPO_NOALLOC_CHUNK_ELEMS = 1 << 20
 DPO_NOALLOC_MAX_CHUNKS = 16384
@@ -115,6 +120,56 @@ class dpo_ffn_form(ctypes.Structure):
     _fields_ = [("kind", _I), ("split", _I), ("cols", _I), ("tiles", _L), ("slots", _I)]
 
 
+class dpo_ids(ctypes.Structure):
+    _fields_ = [("p", _P), ("rows", _L), ("cols", _L), ("ld", _L), ("bytes", _I)]
+
+
+class dpo_embed_args(ctypes.Structure):
+    _fields_ = [("ids", dpo_ids), ("table", _P), ("out", _P), ("vocab", _L), ("dim", _L),
+                ("ld_table", _L), ("ld_out", _L), ("scale", _F), ("table_dtype", _I),
+                ("out_dtype", _I)]
+
+
+class dpo_embed_backward_args(ctypes.Structure):
+    _fields_ = [("dy", _P), ("ids", dpo_ids), ("dtable", _P), ("vocab", _L), ("dim", _L),
+                ("ld_dy", _L), ("ld_dtable", _L), ("scale", _F), ("dtype", _I),
+                ("grad_dtype", _I), ("accumulate", _I), ("workspace", _P),
+                ("workspace_bytes", _L)]
+
+
+class dpo_dropout_args(ctypes.Structure):
+    _fields_ = [("x", _P), ("residual", _P), ("y", _P), ("rows", _L), ("cols", _L), ("ld_x", _L),
+                ("ld_residual", _L), ("ld_y", _L), ("dtype", _I), ("site", ctypes.c_uint32),
+                ("seed", ctypes.c_uint64), ("seed_source", _P), ("p", ctypes.c_double)]
+
+
+class dpo_logprobs_args(ctypes.Structure):
+    _fields_ = [("logits", _P), ("ids", dpo_ids), ("logp", _P), ("entropy", _P), ("stats", _P),
+                ("top_logp", _P), ("top_ids", _P), ("rows", _L), ("vocab", _L),
+                ("ld_logits", _L), ("scale", _F), ("dtype", _I), ("top", _I)]
+
+
+class dpo_logprobs_backward_args(ctypes.Structure):
+    _fields_ = [("logits", _P), ("ids", dpo_ids), ("stats", _P), ("entropy", _P), ("dlogp", _P),
+                ("dentropy", _P), ("dlogits", _P), ("rows", _L), ("vocab", _L),
+                ("ld_logits", _L), ("ld_dlogits", _L), ("scale", _F), ("dtype", _I)]
+
+
+class dpo_head_args(ctypes.Structure):
+    _fields_ = [("x", _P), ("w", _P), ("ids", dpo_ids), ("logp", _P), ("entropy", _P),
+                ("stats", _P), ("top_logp", _P), ("top_ids", _P), ("kept", _P), ("tokens", _L),
+                ("dim", _L), ("vocab", _L), ("ld_x", _L), ("scale", _F), ("top", _I),
+                ("workspace", _P), ("workspace_bytes", _L)]
+
+
+class dpo_head_backward_args(ctypes.Structure):
+    _fields_ = [("x", _P), ("w", _P), ("ids", dpo_ids), ("kept", _P), ("logp", _P),
+                ("entropy", _P), ("stats", _P), ("dlogp", _P), ("dentropy", _P), ("dx", _P),
+                ("dw", _P), ("tokens", _L), ("dim", _L), ("vocab", _L), ("ld_x", _L),
+                ("ld_dx", _L), ("scale", _F), ("grad_dtype", _I), ("accumulate", _I),
+                ("workspace", _P), ("workspace_bytes", _L)]
+
+
 _lib = None
 
 
@@ -171,6 +226,15 @@ def load() -> ctypes.CDLL:
         "dpo_ffn_get_status": (I, [P]),
         "dpo_ffn_clear_status": (I, [P]),
         "dpo_ffn_test_forms": (I, [_L, _L, _L, I, P, P]),
+        "dpo_embed": (I, [P, P]),
+        "dpo_embed_backward": (I, [P, P]),
+        "dpo_embed_workspace": (I, [_L, _L, _L, P]),
+        "dpo_dropout": (I, [P, P]),
+        "dpo_logprobs": (I, [P, P]),
+        "dpo_logprobs_backward": (I, [P, P]),
+        "dpo_head": (I, [P, P]),
+        "dpo_head_backward": (I, [P, P]),
+        "dpo_head_workspace": (I, [_L, _L, _L, I, I, P, P, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -420,6 +484,51 @@ def dpo_ffn_test_forms(tokens: int, dim: int, hidden: int, keep: int, slots=None
     given = None if slots is None else (ctypes.c_int * 6)(*slots)
     _check(load().dpo_ffn_test_forms(tokens, dim, hidden, keep, given, out), None)
     return list(out)
+
+
+# ------------------------------------------------- the two ends of a pipeline --
+# As above; ``ends`` makes the same calls from tensors.
+
+def dpo_embed(args: dpo_embed_args, stream=None) -> None:
+    _check(load().dpo_embed(ctypes.byref(args), _stream(stream)), None)
+
+
+def dpo_embed_backward(args: dpo_embed_backward_args, stream=None) -> None:
+    _check(load().dpo_embed_backward(ctypes.byref(args), _stream(stream)), None)
+
+
+def dpo_embed_workspace(tokens: int, vocab: int, dim: int) -> int:
+    n = ctypes.c_int64()
+    _check(load().dpo_embed_workspace(tokens, vocab, dim, ctypes.byref(n)), None)
+    return n.value
+
+
+def dpo_dropout(args: dpo_dropout_args, stream=None) -> None:
+    _check(load().dpo_dropout(ctypes.byref(args), _stream(stream)), None)
+
+
+def dpo_logprobs(args: dpo_logprobs_args, stream=None) -> None:
+    _check(load().dpo_logprobs(ctypes.byref(args), _stream(stream)), None)
+
+
+def dpo_logprobs_backward(args: dpo_logprobs_backward_args, stream=None) -> None:
+    _check(load().dpo_logprobs_backward(ctypes.byref(args), _stream(stream)), None)
+
+
+def dpo_head(args: dpo_head_args, stream=None) -> None:
+    _check(load().dpo_head(ctypes.byref(args), _stream(stream)), None)
+
+
+def dpo_head_backward(args: dpo_head_backward_args, stream=None) -> None:
+    _check(load().dpo_head_backward(ctypes.byref(args), _stream(stream)), None)
+
+
+def dpo_head_workspace(tokens: int, dim: int, vocab: int, keep: bool = False, top: int = 0):
+    """(forward, kept, backward) bytes."""
+    n = [ctypes.c_int64() for _ in range(3)]
+    _check(load().dpo_head_workspace(tokens, dim, vocab, 1 if keep else 0, top,
+                                     *(ctypes.byref(v) for v in n)), None)
+    return tuple(v.value for v in n)
 
 
 # ------------------------------------------------------------------ owner --

@@ -1,6 +1,6 @@
 """The two ends of a pipeline and its residual stream on tensors: the first stage's
 embedding, the last stage's log probabilities, and dropout where a branch joins the
-stream (include/dpo_ends.h).
+stream (include/dpo.h).
 
 They run around the blocks of ``ffn`` and follow its rules: weights are ``opt.stale(i)``,
 gradients of weights go into ``opt.grads(i)`` (written, or with ``accumulate`` added);
@@ -23,13 +23,15 @@ zeros, its log probability 0, and neither has a gradient.
 """
 from __future__ import annotations
 
-import ctypes
 from typing import NamedTuple, Optional
 
 import torch
 
+from . import dpo as _dpo
 from . import ffn as _ffn
-from .dpo import _check, _stream, load
+from .dpo import (DPO_EMBED_SPAN, DPO_MAX_TOP, dpo_dropout_args, dpo_embed_args, dpo_embed_backward_args,
+                  dpo_embed_workspace, dpo_head_args, dpo_head_backward_args, dpo_head_workspace, dpo_ids,
+                  dpo_logprobs_args, dpo_logprobs_backward_args, load)
 
 
 def embed(ids, table, *, scale: float = 1.0, dtype=None, out=None, stream=None):
@@ -140,101 +142,14 @@ def status() -> int:
     return _ffn.status()
 
 
-# The calls as they are in include/dpo_ends.h, with its argument structures; the functions above
-# make them through dpo_tensors.
-
-_P, _L, _I, _F = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_float
-
-
-class dpo_ids(ctypes.Structure):
-    _fields_ = [("p", _P), ("rows", _L), ("cols", _L), ("ld", _L), ("bytes", _I)]
-
-
-class dpo_embed_args(ctypes.Structure):
-    _fields_ = [("ids", dpo_ids), ("table", _P), ("out", _P), ("vocab", _L), ("dim", _L),
-                ("ld_table", _L), ("ld_out", _L), ("scale", _F), ("table_dtype", _I),
-                ("out_dtype", _I)]
-
-
-class dpo_embed_backward_args(ctypes.Structure):
-    _fields_ = [("dy", _P), ("ids", dpo_ids), ("dtable", _P), ("vocab", _L), ("dim", _L),
-                ("ld_dy", _L), ("ld_dtable", _L), ("scale", _F), ("dtype", _I),
-                ("grad_dtype", _I), ("accumulate", _I), ("workspace", _P),
-                ("workspace_bytes", _L)]
-
-
-class dpo_dropout_args(ctypes.Structure):
-    _fields_ = [("x", _P), ("residual", _P), ("y", _P), ("rows", _L), ("cols", _L), ("ld_x", _L),
-                ("ld_residual", _L), ("ld_y", _L), ("dtype", _I), ("site", ctypes.c_uint32),
-                ("seed", ctypes.c_uint64), ("seed_source", _P), ("p", ctypes.c_double)]
-
-
-class dpo_logprobs_args(ctypes.Structure):
-    _fields_ = [("logits", _P), ("ids", dpo_ids), ("logp", _P), ("entropy", _P), ("stats", _P),
-                ("top_logp", _P), ("top_ids", _P), ("rows", _L), ("vocab", _L),
-                ("ld_logits", _L), ("scale", _F), ("dtype", _I), ("top", _I)]
-
-
-class dpo_logprobs_backward_args(ctypes.Structure):
-    _fields_ = [("logits", _P), ("ids", dpo_ids), ("stats", _P), ("entropy", _P), ("dlogp", _P),
-                ("dentropy", _P), ("dlogits", _P), ("rows", _L), ("vocab", _L),
-                ("ld_logits", _L), ("ld_dlogits", _L), ("scale", _F), ("dtype", _I)]
-
-
-class dpo_head_args(ctypes.Structure):
-    _fields_ = [("x", _P), ("w", _P), ("ids", dpo_ids), ("logp", _P), ("entropy", _P),
-                ("stats", _P), ("top_logp", _P), ("top_ids", _P), ("kept", _P), ("tokens", _L),
-                ("dim", _L), ("vocab", _L), ("ld_x", _L), ("scale", _F), ("top", _I),
-                ("workspace", _P), ("workspace_bytes", _L)]
-
-
-class dpo_head_backward_args(ctypes.Structure):
-    _fields_ = [("x", _P), ("w", _P), ("ids", dpo_ids), ("kept", _P), ("logp", _P),
-                ("entropy", _P), ("stats", _P), ("dlogp", _P), ("dentropy", _P), ("dx", _P),
-                ("dw", _P), ("tokens", _L), ("dim", _L), ("vocab", _L), ("ld_x", _L),
-                ("ld_dx", _L), ("scale", _F), ("grad_dtype", _I), ("accumulate", _I),
-                ("workspace", _P), ("workspace_bytes", _L)]
-
+# The calls as they are in include/dpo.h; the functions above make them through dpo_tensors.
 
 EXPORTS = ("dpo_embed", "dpo_embed_backward", "dpo_embed_workspace", "dpo_dropout", "dpo_logprobs",
            "dpo_logprobs_backward", "dpo_head", "dpo_head_backward", "dpo_head_workspace")
 
-DPO_EMBED_SPAN = 65536
-DPO_MAX_TOP = 32
-
-_typed = False
-
-
-def lib() -> ctypes.CDLL:
-    """The library with these calls' types."""
-    global _typed
-    L = load()
-    if not _typed:
-        sig = {name: [_P, _P] for name in EXPORTS}
-        sig["dpo_embed_workspace"] = [_L, _L, _L, _P]
-        sig["dpo_head_workspace"] = [_L, _L, _L, _I, _I, _P, _P, _P]
-        for name, args in sig.items():
-            fn = getattr(L, name)
-            fn.restype = _I
-            fn.argtypes = args
-        _typed = True
-    return L
+lib = load
 
 
 def call(name: str, args, stream=None) -> None:
     """One of the calls that take a structure and a stream."""
-    _check(getattr(lib(), name)(ctypes.byref(args), _stream(stream)), None)
-
-
-def dpo_embed_workspace(tokens: int, vocab: int, dim: int) -> int:
-    n = _L()
-    _check(lib().dpo_embed_workspace(tokens, vocab, dim, ctypes.byref(n)), None)
-    return n.value
-
-
-def dpo_head_workspace(tokens: int, dim: int, vocab: int, keep: bool = False, top: int = 0):
-    """(forward, kept, backward) bytes."""
-    n = [_L(), _L(), _L()]
-    _check(lib().dpo_head_workspace(tokens, dim, vocab, 1 if keep else 0, top,
-                                    *(ctypes.byref(v) for v in n)), None)
-    return tuple(v.value for v in n)
+    getattr(_dpo, name)(args, stream)

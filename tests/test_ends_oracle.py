@@ -219,7 +219,7 @@ def test_workspace_sizes():
 
 
 def test_binding_types_every_entry_point():
-    names = declared_functions(os.path.join(ROOT, "include", "dpo_ends.h"))
-    assert set(names) == set(ends.EXPORTS)
-    for n in names:
+    names = declared_functions(os.path.join(ROOT, "include", "dpo.h"))
+    assert set(ends.EXPORTS) <= set(names)
+    for n in ends.EXPORTS:
         assert getattr(ends.lib(), n).argtypes is not None
