@@ -63,8 +63,8 @@ __device__ __forceinline__ void merge_warps(K &p, K (*lists)[32], int warps, int
 // and what is equal, can hold one of them; their values are read again, and what reaches the
 // bound is sorted, or offered to lists where it is much (equal values, masked rows): more than 32
 // values a warp, or 128 (7 rows of 199 bf16 with 20: 31 us by lists, for more than 32).
-// us by the threads of a row, 32 / 128 / 512: 4096 rows of 50257 bf16 71 / 77 / 104, 300 of 32000
-// fp32 - / 12.4 / 9.4; with 5 of 1000 rows of 32000 fp32 64 / 128 / 256: 25.7 / 25.6 / 27.2, 4000
+// us by the threads of a row, 32 / 128 / 512: 4096 rows of 50257 bf16 by four accesses 71 / 77 / 104,
+// 300 of 32000 fp32 - / 12.4 / 9.4; with 5 of 1000 rows of 32000 fp32 64 / 128 / 256: 25.7 / 25.6 / 27.2, 4000
 // rows 117 / 92 / 92 (a bound from few threads lets more values be read again). 4000 rows of
 // 32000 fp32: 76 us, 6.7 TB/s, 0.99 of the measured copy.
 constexpr int kAhead = 8, kBatch = 32, kSmThreads = 800, kTopThreads = 128;
