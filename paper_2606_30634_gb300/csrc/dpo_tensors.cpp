@@ -1,5 +1,5 @@
-// dpo_tensors.cpp -- the feed-forward calls of include/dpo.h and those of
-// include/dpo.h on PyTorch tensors: the part of ffn.py and ends.py between their
+// dpo_tensors.cpp -- the feed-forward calls of include/dpo.h and those of a pipeline's
+// ends on PyTorch tensors: the part of ffn.py and ends.py between their
 // signatures and the C ABI (checks, pitches, outputs and workspaces from PyTorch's
 // allocator, the current stream), as a Python module.
 //
