@@ -284,18 +284,22 @@ struct LogBackArgs {
     void *dlogits;
     int64_t rows, vocab, ld, ld_d;
     int64_t spans;               // of a row
-    float scale;
+    float scale, inverse;        // 1 / scale
 };
 
 // A row's scalars and its gradient's elements,
 //   dlogit = -scale p (a + b (log p + h)) = p (k0 + k1 log p),
 // the id's own apart. fp32 results: log p = (z - m) - log S and the accurate exponential. bf16
-// results: t = log2 p = l c - r by one multiply-add and the approximation, 2^-20 with t's
-// rounding; logits so low that p is 0 come as one of these, so that t times 0 is 0. Rows whose r
-// is far out take the differences instead.
+// results: log p from the differences to the largest logit l0, which a bf16 number is and m, its
+// rounded product, gives back: t = l c - r by one multiply-add, c = scale log2(e), r = l0 c + log2 S
+// rounded. What t of l0 itself is off by then is the same for the whole row and comes out of k0 and
+// k1; left are 2^-22 of the exponential and 2^-22 of log p, wherever the row lies (with m c rounded in
+// r: 2^-13 of p for logits of 1000). Logits so low that p is 0 come as one of these, so that t times 0 is 0.
+// Rows whose r is far out take the differences themselves.
 template <class T> struct RowGradient {
     static constexpr bool kAccurate = sizeof(T) == 4;
     float m, logs, h, a, b, scale, k0, k1, c, r;
+    float top, logs2;            // bf16: l0, log2 S
     typename RowAccess<T>::Low low;
     int id;
     bool none;
@@ -314,7 +318,19 @@ template <class T> struct RowGradient {
         k0 = -scale * fmaf(b, h, a);
         k1 = -scale * b * (kAccurate ? 1.0f : 0.6931471805599453f);
         c = scale * kLog2e;
-        r = (m + logs) * kLog2e;
+        if constexpr (!kAccurate) {
+            const float q = m * s.inverse;   // l0 but for 2^-22, less than half a step of bf16
+            top = __bfloat162float(__float2bfloat16_rn(q));
+            if (__fmul_rn(top, scale) != m)
+                top = q;                     // a maximum from elsewhere
+            logs2 = logs * kLog2e;
+            r = fmaf(top, c, logs2);
+            if (near()) {
+                const float off = fmaf(top, c, -r) + logs2, f = exp2_fast(-off);
+                k0 = fmaf(-k1, off, k0) * f;
+                k1 *= f;
+            }
+        }
         set_low(&low);
     }
     __device__ __forceinline__ void set_low(float *v) const { *v = -INFINITY; }
@@ -332,13 +348,14 @@ template <class T> struct RowGradient {
         else if (near())
             t = fmaf(logit == logit ? fmaxf(logit, __uint_as_float(low << 16)) : logit, c, -r);
         else
-            t = fmaf(fmaf(logit, scale, -m), kLog2e, -logs * kLog2e);
+            t = fmaf(logit - top, c, -logs2);
         const float p = kAccurate ? expf(t) : exp2_fast(t);
         return p * fmaf(k1, fmaxf(t, -1e30f), k0);   // no infinity times 0
     }
     __device__ __forceinline__ float own(float logit) const   // col == id
     {
-        const float lp = __fmul_rn(logit, scale) - m - logs, p = expf(lp);
+        const float lp = kAccurate ? __fmul_rn(logit, scale) - m - logs : fmaf(logit - top, scale, -logs);
+        const float p = expf(lp);
         float g = a * -expm1f(lp);
         if (b != 0.0f && p != 0.0f)
             g = fmaf(-b * p, lp + h, g);
@@ -557,6 +574,7 @@ extern "C" int dpo_logprobs_backward(const dpo_logprobs_backward_args *args, voi
     k.ld = a.ld_logits;
     k.ld_d = a.ld_dlogits;
     k.scale = a.scale;
+    k.inverse = 1.0f / a.scale;
     const int64_t span = (int64_t)kBackThreads * kBackPieces * (aligned ? wide : 1);
     k.spans = (a.vocab + span - 1) / span;
     if (k.spans * a.rows >= kMaxCount)

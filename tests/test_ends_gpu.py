@@ -537,6 +537,44 @@ def test_logits_that_pass_the_near_range(dtype, scale):
     within(d, want, scale * (pe + 4 * U * (p + one)) + (RND[dtype] + 2 * U) * np.abs(want) + TINY, "dlogits")
 
 
+def rounds_to(got, want, bar, dtype, what):
+    """Each element is what some number within bar of want rounds to (fp32's half step on the way to
+    bf16 is in the bar)."""
+    low, high = (torch.from_numpy(want + s * (bar + U * np.abs(want))).to(dtype).double().numpy() for s in (-1, 1))
+    got = np64(got)
+    off = (got < low) | (got > high)
+    assert not off.any(), f"{what}: {off.sum()} of {off.size}, {got[off][:3]} for {want[off][:3]}"
+
+
+@pytest.mark.parametrize("scale", [1.0, 0.7, 1.9])
+@pytest.mark.parametrize("offset", [30.0, -1000.0, 5e3, 11000.0, 3e5])
+@pytest.mark.parametrize("entropy", [False, True])
+def test_gradients_of_rows_far_from_zero(scale, offset, entropy):
+    """What a row's logits have in common leaves no error in its probabilities: bf16 gradients are the
+    roundings of numbers within 2^-17 of p's terms, which takes the sum's 64 u and the two
+    exponentials' 2^-22, and 2^-22 of log p for the multiply-add that forms it."""
+    rows, vocab = 800, 40
+    g = gen(int(abs(offset)) + entropy)
+    top = torch.tensor(offset / scale, device=DEV).bfloat16()
+    below = torch.nextafter(top, torch.tensor(-math.inf, device=DEV, dtype=torch.bfloat16))
+    x = torch.where(torch.rand(rows, vocab, generator=g, device=DEV) < 0.3, below, top)
+    x[:, 0] = top
+    ids = torch.randint(0, vocab, (rows,), generator=g, device=DEV)
+    a = torch.randn(rows, generator=g, device=DEV)
+    b = torch.randn(rows, generator=g, device=DEV) if entropy else None
+    o = ends.token_logprobs(x, ids, scale=scale)
+    d = ends.token_logprobs_backward(a, x, ids, o, dentropy=b)
+    s = float(f32(scale))
+    z, i = np64(x) * s, ids.cpu().numpy()
+    want = s * ref.logits_gradient(z, i, np64(a), None if b is None else np64(b))
+    logs, p, h = ref.distribution(z)
+    av, bv = np.abs(np64(a))[:, None], np.abs(np64(b))[:, None] if entropy else 0.0
+    own = np.zeros_like(p)
+    own[np.arange(rows), i] = 1
+    bar = s * (p * (av + bv * (np.abs(logs + h[:, None]) + 1)) * (2.0 ** -17 + 2.0 ** -22 * np.abs(logs)) + own * av * 8 * U)
+    rounds_to(d, want, bar + TINY, torch.bfloat16, "dlogits")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("scale,size", [(1e-20, 1e38), (1e-20, 1e20), (1e6, 1e-6), (1e6, 1e30), (1.0, 1e37)])
 @pytest.mark.parametrize("top", [0, 7])
