@@ -798,18 +798,18 @@ __device__ __forceinline__ void head_rows(const Product &P, Stager &st, float (&
         high[j & 1] = fmaxf(high[j & 1], v[j]);
         low[j & 1] = fminf(low[j & 1], v[j]);
     }
-    // t = v c - r by one multiply-add, in units of 2; `off`, its value for the largest, comes
-    // out at the end. For infinities and largest values whose `off` would be past 2^-11 the
-    // differences of the products, in twice as many instructions; by row, so that none depends on
-    // what lies beside it. (With values below 1024 of K this epilogue is as long as a tile's MMAs, by
+    // t = v c - r by one multiply-add, in units of 2; `off`, its value for the largest, comes out of
+    // the sums at the end, and out of what is kept by its unit. For infinities and largest values
+    // whose `off` would be past 2^-11 the differences of the products, in twice as many instructions; by
+    // row, so that none depends on what lies beside it. (With values below 1024 of K this epilogue is as long as a tile's MMAs, by
     // its latencies, not its instructions: 4 us a tile of 8 warps, a quarter of the issue slots.
     // 16 warps of 64 columns spill: 1001 x 768 x 50257 61 -> 78 us.)
     const float top = fmaxf(high[0], high[1]), c = H.scale * 1.4426950408889634f, r = top * c;
     const float z = __fmul_rn(top, H.scale), from = z == -INFINITY ? 0.0f : z;
     const bool near = fabsf(r) < 16384.0f && fminf(low[0], low[1]) > -1e30f;
-    const float off = near ? fmaf(top, c, -r) : 0.0f;
+    const float off = near ? fmaf(top, c, -r) : 0.0f, unit = kHeadUnit * exp2(-off);
     const int part_row = col0 / kHeadCols * H.kept_rows + row0;
-    const Two cc = two(c, c), rr = two(-r, -r), unit = two(kHeadUnit, kHeadUnit);
+    const Two cc = two(c, c), rr = two(-r, -r), units = two(unit, unit);
     Two ss[2] = {0, 0}, ww[2] = {0, 0};
     auto sums = [&](auto mixed) {
 #pragma unroll
@@ -828,7 +828,7 @@ __device__ __forceinline__ void head_rows(const Product &P, Stager &st, float (&
                 const Two e = two(exp2(u.x), exp2(u.y));
                 ss[j & 1] = add_two(ss[j & 1], e);
                 ww[j & 1] = fma_two(t, e, ww[j & 1]);
-                const float2 q = of_two(mul_two(e, unit));
+                const float2 q = of_two(mul_two(e, units));
                 const __half2 h = __floats2half2_rn(q.x, q.y);
                 e2[j] = *reinterpret_cast<const uint32_t *>(&h);
             }
@@ -841,7 +841,7 @@ __device__ __forceinline__ void head_rows(const Product &P, Stager &st, float (&
     else
         sums(std::true_type());
     const float2 s2 = of_two(add_two(ss[0], ss[1])), w2 = of_two(add_two(ww[0], ww[1]));
-    const float f = exp2(-off), s = (s2.x + s2.y) * f;
+    const float f = unit / kHeadUnit, s = (s2.x + s2.y) * f;
     const float w = fmaf(-off, s2.x + s2.y, w2.x + w2.y) * f * 0.6931471805599453f;
     if (in) {
         const int64_t i = col0 / kHeadCols * H.rows + row;

@@ -789,6 +789,34 @@ def test_head_of_large_and_infinite_logits():
     assert (dx[~rest] == 0).all() and torch.isfinite(dx).all() and torch.isfinite(dw).all()
 
 
+def test_head_gradients_of_rows_far_from_zero():
+    """Rows that differ by a constant of their logits, which fp32 holds exactly, have one gradient but
+    for the roundings of e^(z - m) before it is kept: 2^-22 and 2^-24 of a log2 below 16, under 2^-19,
+    which moves the mean of the kept values' and G's roundings by as much."""
+    tokens, vocab, dim = 32, 5000, 64
+    g = gen(17)
+    x, w = (torch.zeros(n, dim, device=DEV) for n in (tokens, vocab))
+    x[1:, 0] = torch.randint(64, 88, (tokens - 1,), generator=g, device=DEV).float() / -64   # 128 of them: -11000 to -8192
+    x[1::2, 0] *= -1
+    w[:, 0] = 8192
+    x[:, 1] = 1
+    w[:, 1] = torch.randint(-128, 128, (vocab,), generator=g, device=DEV).float() / 32
+    x[:, 2] = 2.0 ** -8
+    w[:, 2] = torch.randint(0, 8, (vocab,), generator=g, device=DEV).float()
+    x[:, 8:8 + tokens] = torch.eye(tokens, device=DEV)   # dw's columns: G of each token
+    x, w = x.bfloat16(), w.bfloat16()
+    ids = torch.zeros(tokens, dtype=torch.long, device=DEV)
+    o, kept = ends.head_logprobs(x, w, ids, keep=True)
+    dw = torch.empty(vocab, dim, device=DEV)
+    ends.head_logprobs_backward(torch.full((tokens,), 1.3, device=DEV), kept, x, w, ids, o, dw)
+    G = np64(dw)[1:, 8:8 + tokens].T
+    z = np64(x) @ np64(w).T
+    want = ref.logits_gradient(z, ids.cpu().numpy(), np.full(tokens, float(f32(1.3))))[:, 1:]
+    assert np.abs(G / want - 1).max() <= B + 2.0 ** -11 + 2.0 ** -18
+    mean = np.abs((G / G[0] - 1).mean(1))
+    assert mean.max() <= 2.0 ** -17, mean
+
+
 def test_head_of_no_tokens_and_shapes():
     g, x, w, ids = head_case(24, 64, 100)
     want, kept = ends.head_logprobs(x, w, ids, top=3, keep=True)
