@@ -722,7 +722,7 @@ int dpo_dropout(const dpo_dropout_args *args, void *cuda_stream);
  *   logp = z_id - m - log S,  entropy = log S - sum e^(z - m) (z - m) / S,
  *   stats = (m, log S),
  *   top ids: those of the `top` largest z, descending, ties to the lowest id, NaN below
- *   all numbers; top logp: theirs.
+ *   all numbers and -infinity; top logp: theirs.
  * Logits of -infinity are masked: probability 0, no part in sums. A row of nothing else,
  * or with a NaN or +infinity, has no distribution: logp, entropy and top logp are NaN.
  */

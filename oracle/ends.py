@@ -83,8 +83,9 @@ def logprobs(z, ids):
 
 
 def top(z, k):
-    """Ids of the k largest, ties to the lowest id, NaN last."""
-    return np.argsort(np.where(np.isnan(z), np.inf, -z), axis=1, kind="stable")[:, :k]
+    """Ids of the k largest, ties to the lowest id, NaN last, behind -inf."""
+    nan = np.isnan(z)
+    return np.lexsort((np.where(nan, 0.0, -z), nan), axis=1)[:, :k]
 
 
 def logits_gradient(z, ids, dlogp, dentropy=None):

@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(kMaxThreads, 2) logprobs_kernel(const LogArgs 
                 merge_warps(mine, lists, warps, warp, lane);
             }
         } else {
-            TopList list{0, key_of(bound, 0x7FFFFFFF), a.top, lane};
+            TopList list{0, bound == -INFINITY ? 0 : key_of(bound, 0x7FFFFFFF), a.top, lane};   // 0: NaN too
             row_sync(warps);
             scan([&](bool in, float z, int at) { list.offer(in ? key_of(z, at) : 0); });
             mine = list.p;

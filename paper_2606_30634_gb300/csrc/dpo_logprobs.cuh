@@ -203,13 +203,14 @@ template <> struct RowAccess<float> {
 };
 
 // ---------------------------------------------------------- the largest ----
-// A value and its id as one number: the larger value first, of equal ones the lower id; NaN counts
-// as -infinity. 0 is behind all.
+// A value and its id as one number: the larger value first, of equal ones the lower id; NaN behind
+// -infinity, whose first word is 0x007FFFFF. 0 is behind all.
 using Key = unsigned long long;
 __device__ __forceinline__ Key key_of(float v, int id)
 {
-    const uint32_t u = __float_as_uint(v == v ? v + 0.0f : -INFINITY);   // -0 is 0
-    return (Key)(u ^ ((uint32_t)((int)u >> 31) | 0x80000000u)) << 32 | (uint32_t)(0x7FFFFFFF - id);
+    const uint32_t u = __float_as_uint(v + 0.0f);   // -0 is 0
+    const uint32_t high = v == v ? u ^ ((uint32_t)((int)u >> 31) | 0x80000000u) : 1u;
+    return (Key)high << 32 | (uint32_t)(0x7FFFFFFF - id);
 }
 __device__ __forceinline__ float value_of(Key k)
 {

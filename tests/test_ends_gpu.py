@@ -476,6 +476,31 @@ def test_rows_of_odd_values(dtype, vocab):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(6, 5), (6, 40), (6, 3000), (6, 100003), (4000, 300)])
+@pytest.mark.parametrize("top", [1, 5, 32])
+def test_nan_comes_after_masked_logits(dtype, rows, vocab, top):
+    """Alternatives: numbers, then -infinity, then NaN, each of equal ones by their ids."""
+    top = min(top, vocab)
+    x = torch.full((rows, vocab), -math.inf, device=DEV)
+    x[0, 0] = math.nan
+    x[1, ::2] = math.nan
+    x[2, :] = math.nan
+    x[2, vocab - 1] = -math.inf
+    x[3, 1:] = math.nan
+    x[3, 0] = -3.0
+    x[4:, vocab // 2] = 7.0
+    x[4:, vocab // 2 + 1] = torch.finfo(DT[dtype]).min
+    x[4:, :2] = math.nan
+    x = x.to(DT[dtype])
+    o = ends.token_logprobs(x, top=top)
+    z = np64(x[:6])
+    want = [sorted(range(vocab), key=lambda j: (math.isnan(r[j]), 0.0 if math.isnan(r[j]) else -r[j], j))[:top] for r in z]
+    assert o.top_ids[:6].tolist() == want
+    assert (o.top_ids[4:] == o.top_ids[4]).all()
+    assert np.array_equal(ref.top(z, top), want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,vocab", [(4000, 2050), (3999, 40), (2, 128256), (9, 40000)])
 def test_rows_by_warps_and_by_clusters(dtype, rows, vocab):
     """So many rows that a warp has one of many batches, so few that CTAs share one."""

@@ -60,6 +60,11 @@ def test_distribution_closed_forms():
     assert ref.top(np.array([[1.0, 3, 3, np.nan, 2]]), 5).tolist() == [[1, 2, 4, 0, 3]]
 
 
+def test_nan_is_behind_masked_logits():
+    z = np.array([[np.nan, -np.inf, 1.0, np.nan, -np.inf], [np.inf, np.nan, np.inf, 0.0, -0.0]])
+    assert ref.top(z, 5).tolist() == [[2, 1, 4, 0, 3], [0, 2, 3, 4, 1]]
+
+
 def test_gradient_by_differences():
     """Step 1e-5: truncation 1e-10 and rounding 1e-11 of values near 1, under 1e-8."""
     r = np.random.RandomState(0)
