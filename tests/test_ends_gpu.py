@@ -900,6 +900,24 @@ def test_head_gradient_by_differences():
             assert abs(d - grad[i, j].item()) <= 2e-2 * scale[which] + h * h * 5, (which, k)
 
 
+def test_outputs_are_tensors_of_their_own():
+    """Each in a storage of its size: one that is kept holds no other's memory, and one that PyTorch
+    lets grow does not grow into another."""
+    _, x, ids = logits_case(24, 100, "f32")
+    _, h, w, _ = head_case(24, 64, 100)
+    for o in (ends.token_logprobs(x, ids, top=5), ends.head_logprobs(h, w, ids, top=5)[0]):
+        outs = [t for t in o[:5]]
+        assert len({t.untyped_storage().data_ptr() for t in outs}) == 5
+        for t in outs:
+            assert t.is_contiguous() and t.storage_offset() == 0
+            assert t.untyped_storage().nbytes() == t.numel() * t.element_size()
+        before = [t.clone() for t in outs]
+        o.entropy.resize_(1000).fill_(7.0)
+        o.stats.resize_(1000).fill_(7.0)
+        for t, b in zip((o.logp, o.top_logp, o.top_ids), (before[0], before[3], before[4])):
+            assert torch.equal(t, b)
+
+
 # ---------------------------------------------------------- used together ----
 
 def stage(tokens, table, w_head, dtable, dw, seed):
