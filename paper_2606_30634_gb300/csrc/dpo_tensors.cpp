@@ -10,10 +10,12 @@
 // is the one that is called. Nothing here throws past its entry points.
 #include <Python.h>
 
+#include <ATen/Context.h>
 #include <ATen/EmptyTensor.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_strided.h>
+#include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
@@ -219,14 +221,23 @@ dpo_packed8 packed_of(PyObject *codes, PyObject *scales, int64_t rows, int64_t c
     return {(uint8_t *)m[0].p, (uint8_t *)m[1].p, m[0].ld, m[1].ld};
 }
 
-// From PyTorch's allocator, on the current device without its dispatcher, which takes half as long
-// again (1.2 us).
-constexpr c10::DispatchKeySet kCuda(c10::DispatchKey::CUDA);
+// Whether an allocation passes PyTorch's dispatcher unseen: no mode watches or replaces operators
+// (TorchDispatchMode, FakeTensor, functorch, tracing; inference mode too), and uninitialised memory
+// is not to be filled.
+bool unseen()
+{
+    const at::Context &c = at::globalContext();
+    return c10::impl::tls_local_dispatch_key_set().included_ == c10::default_included_set &&
+           !(c.deterministicAlgorithms() && c.deterministicFillUninitializedMemory());
+}
+// From PyTorch's allocator: torch.empty, on the current device without its dispatcher where that
+// makes no difference (it takes half as long again, 1.2 us).
 Tensor make(at::IntArrayRef size, at::ScalarType type, at::Device device)
 {
-    if (device.index() != c10::cuda::current_device())
+    if (device.index() != c10::cuda::current_device() || !unseen())
         return at::empty(size, at::TensorOptions().dtype(type).device(device));
-    return at::detail::empty_generic(size, c10::cuda::CUDACachingAllocator::get(), kCuda, type, std::nullopt);
+    return at::detail::empty_generic(size, c10::cuda::CUDACachingAllocator::get(),
+                                     c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt);
 }
 
 struct Packed {

@@ -23,9 +23,10 @@ import threading
 import numpy as np
 import pytest
 import torch
+from torch.utils._python_dispatch import TorchDispatchMode
 
 from oracle import ends as ref
-from paper_2606_30634_gb300 import dpo, ends
+from paper_2606_30634_gb300 import dpo, ends, ffn
 from test_ffn_gpu import B, DEV, DT, RND, U, gen, np64, randn, within
 
 pytestmark = pytest.mark.gpu
@@ -916,6 +917,43 @@ def test_outputs_are_tensors_of_their_own():
         o.stats.resize_(1000).fill_(7.0)
         for t, b in zip((o.logp, o.top_logp, o.top_ids), (before[0], before[3], before[4])):
             assert torch.equal(t, b)
+
+
+class Allocations(TorchDispatchMode):
+    """Counts what is allocated."""
+
+    def __init__(self):
+        super().__init__()
+        self.count = 0
+
+    def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+        self.count += func.overloadpacket is torch.ops.aten.empty
+        return func(*args, **(kwargs or {}))
+
+
+def test_modes_of_pytorch_see_allocations():
+    """Outputs and workspaces are torch.empty's to a mode that watches operators, and are filled where
+    deterministic algorithms ask for it: the bytes of `kept` that no token has."""
+    _, x, ids = logits_case(24, 100, "f32")
+    _, h, w, _ = head_case(3, 64, 300)
+    table = randn(gen(1), 100, 16)
+    calls = [lambda: ends.embed(ids, table), lambda: ends.dropout_add(x, None, 0.1, 1),
+             lambda: ends.token_logprobs(x, ids, top=2), lambda: ends.head_logprobs(h, w, keep=True),
+             lambda: ffn.add_rms_norm(table.float(), torch.ones(16, device=DEV)), lambda: ffn.pack8(table)]
+    for call in calls:
+        want = call()
+        with Allocations() as seen:
+            got = call()
+        assert seen.count > 0
+        for a, b in zip(want if isinstance(want, tuple) else (want,), got if isinstance(got, tuple) else (got,)):
+            if torch.is_tensor(a) and a.dtype is not torch.uint8:
+                assert torch.equal(a, b)
+    torch.use_deterministic_algorithms(True)
+    try:
+        _, kept = ends.head_logprobs(h, w, keep=True)
+    finally:
+        torch.use_deterministic_algorithms(False)
+    assert (kept[-220:] == 255).all()   # the maxima of 3 parts of 3 tokens are 36 bytes of 256
 
 
 # ---------------------------------------------------------- used together ----
