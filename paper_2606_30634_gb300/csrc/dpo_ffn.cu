@@ -41,7 +41,7 @@ using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t,
                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 using KernelFn = void (*)(const Launch);
-constexpr int kForms = 5;   // epilogues
+constexpr int kForms = 6;   // epilogues
 
 // What the launches need to know of a device, found by its first call.
 struct Device {
@@ -79,9 +79,12 @@ int slots_of(const Device &d, Form f, int epi)
 
 template <int CG, bool SPLIT> KernelFn kernel_of(int epi)
 {
-    if constexpr (!SPLIT)
+    if constexpr (!SPLIT) {
+        if (epi == kShared)
+            return ffn_gemm_kernel<CG, kShared, SPLIT>;
         if (epi == kHead)
             return ffn_gemm_kernel<CG, kHead, SPLIT>;
+    }
     return epi == kGate         ? ffn_gemm_kernel<CG, kGate, SPLIT>
            : epi == kGateBack8  ? ffn_gemm_kernel<CG, kGateBack8, SPLIT>
            : epi == kGateBack16 ? ffn_gemm_kernel<CG, kGateBack16, SPLIT>
@@ -140,7 +143,7 @@ cudaError_t prepare(Device &d)
     for (const Form f : {kPairs, single(BM), thin(1, BM, BH), thin(2, BM, BH), thin(4, BM, BH),
                          thin(8, BM, BH)})
         for (int epi = 0; epi < kForms; ++epi) {
-            if (f.thin && epi == kHead)   // K is not split there
+            if (f.thin && epi >= kShared)   // K is not split there
                 continue;
             const void *k = reinterpret_cast<const void *>(kernel_of(f, epi));
             cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize,
@@ -506,17 +509,20 @@ int dpo::store_products(const char *what, const StoreProduct *p, int n, void *st
         P.ld_old = P.ld_o = q.ld_out;
         P.o0 = static_cast<__nv_bfloat16 *>(q.out);
     }
+    int epi = s[0].ways > 1 ? kShared : kStore;
     if (n - first == 2) {   // deal by length
-        const int64_t slots = slots_of(*d, f, kStore), longs = tiles_of(s[first], f, kStore),
-                      shorts = tiles_of(s[first + 1], f, kStore), fewer = longs % slots;
+        const int64_t slots = slots_of(*d, f, kShared), longs = tiles_of(s[first], f, kShared),
+                      shorts = tiles_of(s[first + 1], f, kShared), fewer = longs % slots;
         const int64_t a = blocks_of(s[first].k, f.bk()) / s[first].ways, b = blocks_of(s[first + 1].k, f.bk());
         if (fewer > 0 && longs + shorts > slots && a >= 2 * b) {
             const int64_t most = shorts / (slots - fewer), want = a / (b > 4 ? b : 4);   // 4: its store
             L.longs = (int)longs;
             L.extra = (int)(want < most ? want : most);
+            if (L.extra > 0)
+                epi = kShared;
         }
     }
-    if ((rc = run(what, *d, L, s + first, n - first, kStore, f, false, m.ok, stream)) != DPO_OK ||
+    if ((rc = run(what, *d, L, s + first, n - first, epi, f, false, m.ok, stream)) != DPO_OK ||
         s[0].ways == 1)
         return rc;
     const StoreProduct &q = p[0];

@@ -28,6 +28,7 @@
 //              bf16), writes dG, dU and A
 //   kStore     writes D in bf16 or fp32, with factors along the columns and the old
 //              contents added where asked for
+//   kShared    kStore where products may be divided into shares of K and tiles are dealt by length
 //   kHead      the tile is of a head's logits; leaves each row's maximum, sum and entropy sum
 //              over 128 columns, and what the backward keeps (dpo_head.cu)
 #pragma once
@@ -65,7 +66,7 @@ using gemm::smem_desc;
 using gemm::swz64;
 using gemm::tmem_ld32;
 
-enum Epilogue { kGate = 0, kGateBack8 = 1, kGateBack16 = 2, kStore = 3, kHead = 4 };
+enum Epilogue { kGate = 0, kGateBack8 = 1, kGateBack16 = 2, kStore = 3, kShared = 4, kHead = 5 };
 __host__ __device__ constexpr bool gate_back(int epi)
 {
     return epi == kGateBack8 || epi == kGateBack16;
@@ -136,9 +137,9 @@ struct Product {
     int k_blocks[2];              // K blocks of each segment (second 0: one segment)
     int a_mn, b_mn;               // the operand is M- or N-contiguous
     int m_tiles, n_tiles, first;  // tiles, and the launch's number of the first
-    int ways, slab;               // kStore: every tile is so many of the launch's, each with a share of
+    int ways, slab;               // kShared: every tile is so many of the launch's, each with a share of
                                   // the K blocks and rows of d0 `slab` further on; or 1, 0
-    // kStore
+    // kStore, kShared
     int f32, accumulate;
     const void *old;              // accumulate: D itself
     int64_t ld_old;
@@ -167,7 +168,7 @@ struct Launch {
     int cols;                     // single CTAs: the tile's columns, kTile(1), or half of them
                                   // where K is split
     int early;                    // another launch of this kernel follows in the same call
-    int longs, extra;             // extra > 0: how unequal tiles are dealt, see tile_of_round
+    int longs, extra;             // kShared: extra > 0: how unequal tiles are dealt, see tile_of_round
     unsigned int *err;
 };
 
@@ -290,18 +291,20 @@ __device__ __forceinline__ int share_end(int all, uint32_t share, uint32_t split
     return (int)((uint32_t)all * (share + 1u) / split);
 }
 
-// Product and position of tile t: bands of kBandRows block rows, column by column.
+// Product and position of tile t: bands of kBandRows block rows, column by column. SHARES: of
+// kShared, whose products may be divided (Product::ways) and dealt by length; the other epilogues have
+// no instruction of it (in all of them: 1001 tokens, 520 x 1560 widths 55.3 -> 56.7 us a step).
 struct Tile {
     int p, m, n;   // product, block row, block column
     int share;     // of its K blocks
 };
-__device__ __forceinline__ Tile tile_at(const Launch &L, int t)
+template <bool SHARES> __device__ __forceinline__ Tile tile_at(const Launch &L, int t)
 {
     int p = 0;
     while (p + 1 < L.n_products && t >= L.p[p + 1].first)
         ++p;
     const Product &P = L.p[p];
-    const int each = P.m_tiles * P.n_tiles, share = P.ways > 1 ? (t - P.first) / each : 0;
+    const int each = P.m_tiles * P.n_tiles, share = SHARES && P.ways > 1 ? (t - P.first) / each : 0;
     const int i = t - P.first - share * each, band = kBandRows * P.n_tiles;
     const int b = i / band, r = i - b * band;
     const int rows = min(kBandRows, P.m_tiles - b * kBandRows);
@@ -321,9 +324,9 @@ __device__ __forceinline__ int turn_of(int r, int pair, int n)
 // out even: whoever has one less of them gets `extra` short ones before the rest are dealt. (4096
 // tokens, 768 x 50257: 48 tiles of 393 K blocks and 591 of 32 for 76 pairs, 649 blocks for
 // the busiest by turn_of, 521 so.)
-__device__ __forceinline__ int tile_of_round(const Launch &L, int r, int pair, int n)
+template <bool SHARES> __device__ __forceinline__ int tile_of_round(const Launch &L, int r, int pair, int n)
 {
-    if (L.extra == 0)
+    if (!SHARES || L.extra == 0)
         return turn_of(r, pair, n);
     const int mine = (L.longs - pair + n - 1) / n, fewer = L.longs % n;   // pairs from `fewer` on
     if (r < mine)
@@ -1175,6 +1178,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
     static_assert(CG == 1 || !SPLIT, "pairs do not split K");
     using R = Ring<SPLIT>;
     constexpr int T = kTile(CG), BK = R::BK;
+    constexpr bool SHARES = EPI == kShared;
     const int a_rows = CG == 1 ? L.a_rows : BM, cols = SPLIT ? L.cols : T;
     // of a stage; where K is not split its layout is that of whole boxes
     const int a_bytes = R::bytes(SPLIT ? a_rows : BM), b_bytes = R::bytes(SPLIT ? cols : BH);
@@ -1258,8 +1262,8 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
         uint32_t ph = 1;     // parity of the stage's release
         const uint32_t bytes = (uint32_t)(CG * (R::bytes(a_rows) + b_bytes));
         bool ok = true;
-        for (int t, r = 0; ok && (t = tile_of_round(L, r, pair, n_pairs)) < n_tiles; ++r) {
-            const Tile tile = tile_at(L, t);
+        for (int t, r = 0; ok && (t = tile_of_round<SHARES>(L, r, pair, n_pairs)) < n_tiles; ++r) {
+            const Tile tile = tile_at<SHARES>(L, t);
             const Product &P = L.p[tile.p];
             const bool a_mn = P.a_mn, b_mn = P.b_mn;
             const int ma = tile.m * T + (int)rank * BM;
@@ -1268,7 +1272,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
             const int nb = EPI == kGate ? tile.n * (cols / 2) : tile.n * cols + (int)rank * BH;
             const int kb0 = P.k_blocks[0], kb_all = kb0 + P.k_blocks[1];
             const uint32_t part = SPLIT ? share : (uint32_t)tile.share, parts = SPLIT ? split : (uint32_t)P.ways;
-            const bool whole = !SPLIT && EPI != kStore;
+            const bool whole = !SPLIT && !(SHARES && P.ways > 1);
             const int kb_n = whole ? kb_all : share_end(kb_all, part, parts);
             for (int kb = whole ? 0 : share_end(kb_all, part - 1, parts); kb < kb_n; ++kb, ++it) {
                 ok = warp_wait(empty(s), ph, &aborted);
@@ -1327,15 +1331,14 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
             int lt = 0, s = 0, visit = 0;
             uint32_t ph = 0;
             bool ok = true;
-            for (int t; ok && (t = tile_of_round(L, lt, pair, n_pairs)) < n_tiles; ++lt) {
-                const Tile tile = tile_at(L, t);
+            for (int t; ok && (t = tile_of_round<SHARES>(L, lt, pair, n_pairs)) < n_tiles; ++lt) {
+                const Tile tile = tile_at<SHARES>(L, t);
                 const Product &P = L.p[tile.p];
                 const int kb_all = P.k_blocks[0] + P.k_blocks[1];
                 const uint32_t part = SPLIT ? share : (uint32_t)tile.share;
                 const uint32_t parts = SPLIT ? split : (uint32_t)P.ways;
-                const int kb_n = !SPLIT && EPI != kStore ? kb_all
-                                                         : share_end(kb_all, part, parts) -
-                                                               share_end(kb_all, part - 1, parts);
+                const bool whole = !SPLIT && !(SHARES && P.ways > 1);
+                const int kb_n = whole ? kb_all : share_end(kb_all, part, parts) - share_end(kb_all, part - 1, parts);
                 const bool a_mn = P.a_mn, b_mn = P.b_mn;
                 const uint32_t idesc = idesc_of(CG, cols, a_mn, b_mn);
                 const Steps a0 = steps_of<BK>(sa, a_mn), b0 = steps_of<BK>(sb, b_mn);
@@ -1402,8 +1405,8 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
             int visit = 0;
             if (CG == 1 && half == 1)
                 seen = false;
-            for (int t; seen && (t = tile_of_round(L, lt, pair, n_pairs)) < n_tiles; ++lt) {
-                const Tile tile = tile_at(L, t);
+            for (int t; seen && (t = tile_of_round<SHARES>(L, lt, pair, n_pairs)) < n_tiles; ++lt) {
+                const Tile tile = tile_at<SHARES>(L, t);
                 const Product &P = L.p[tile.p];
                 const int parts = (P.k_blocks[0] + kHeadPart - 1) / kHeadPart;
                 const int row0 = tile.m * T + (int)rank * BM + q * 32;
@@ -1444,8 +1447,8 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                     head_rows(P, st, v, id, row0, col0);
             }
         }
-        for (int t; EPI != kHead && (t = tile_of_round(L, lt, pair, n_pairs)) < n_tiles; ++lt) {
-            const Tile tile = tile_at(L, t);
+        for (int t; EPI != kHead && (t = tile_of_round<SHARES>(L, lt, pair, n_pairs)) < n_tiles; ++lt) {
+            const Tile tile = tile_at<SHARES>(L, t);
             const Product &P = L.p[tile.p];
             const int a = lt & 1;
             const int row0 = tile.m * T + (int)rank * BM + q * 32;
@@ -1482,7 +1485,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                         load_kept(ch + 1);
                     drain<EPI>(P, st, now, at, out_cols, row0, col0, ch == 0, 0);
                 } else {
-                    drain<EPI>(P, st, kept, at, out_cols, row0, col0, ch == 0, tile.share * P.slab);
+                    drain<EPI>(P, st, kept, at, out_cols, row0, col0, ch == 0, SHARES ? tile.share * P.slab : 0);
                 }
             }
             if (SPLIT) {
