@@ -444,6 +444,9 @@ int dpo::store_products(const char *what, const StoreProduct *p, int n, void *st
     int rc = device_info(what, &d);
     if (rc != DPO_OK)
         return rc;
+    static_assert(kMaxStoreProducts == kMaxProducts, "products of a launch");
+    if (n < 1 || n > kMaxStoreProducts || (p[0].shares != nullptr && (p[0].f32 || p[0].accumulate)))
+        return call_fail(DPO_EINVAL, "%s: %d products", what, n);
     Shape s[kMaxProducts];
     auto whole = [&](int i) { return p[i].f32 || p[i].accumulate || p[i].a_mn; };
     for (int i = 0; i < n; ++i)

@@ -36,6 +36,7 @@
 #include "dpo_gemm.cuh"
 #include "dpo_ids.cuh"
 #include "dpo_pack8.cuh"
+#include "dpo_products.h"
 #include "dpo_two.cuh"
 
 #include <cuda_fp16.h>
@@ -114,9 +115,7 @@ constexpr int kBandRows = 16;   // block rows per band, as in dpo_gemm.cuh
 // cores cut a sum to the accumulator's bits at each of their steps, toward zero, so its error grows with K:
 // over 4096 it is 9e-6 of logits of size 2 and 1.4e-6 of log probabilities. The epilogue adds up
 // accumulations of 1024 in registers, rounding to nearest: 2e-6 and 3.3e-7.
-constexpr int kHeadCols = 128, kHeadPart = 8;
-// What is kept of e^(z - m), in fp16: times 2^15, so that values down to 2^-29 keep 11 bits.
-constexpr float kHeadUnit = 32768.0f;
+constexpr int kHeadCols = kHeadStatCols, kHeadPart = 8;
 
 struct HeadOut {
     Ids ids;                      // p nullptr: none

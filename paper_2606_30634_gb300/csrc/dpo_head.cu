@@ -20,8 +20,6 @@
 namespace dpo {
 namespace {
 
-constexpr float kKeptUnit = 1.0f / 32768.0f;   // of the kept fp16 values
-
 // ---------------------------------------------------------------- join ----
 // A CTA joins kJoinRows rows, a lane one part of one of them, several at a time; then a warp has a
 // row, with its warps' sums in the lanes.
@@ -98,6 +96,10 @@ __global__ void __launch_bounds__(32 * kJoinMaxWarps) head_join_kernel(const Joi
 // rows of a CTA; accesses of 8 columns a lane (by 4, 8 and 16 rows a backward of 1001 x 768 x 50257 is
 // 147, 151 and 154 us)
 constexpr int kGradWarps = 4, kGradPieces = 4;
+constexpr int kGradCols = 32 * 8;        // of one access of a warp, whole parts
+static_assert(kGradCols % kHeadStatCols == 0, "parts of an access");
+constexpr float kUnitLog2 = 15.0f;       // of kHeadUnit
+static_assert(kHeadUnit == 32768.0f, "its logarithm");
 
 struct GradArgs {
     const __half *kept;
@@ -135,17 +137,17 @@ __global__ void __launch_bounds__(32 * kGradWarps) head_gradient_kernel(const Gr
     const float k0 = -a.scale * fmaf(gb, h, ga), k1 = -a.scale * gb * 0.6931471805599453f;
     __nv_bfloat16 *const g = a.g + row * a.ld;
     const int vocab = (int)a.vocab;
-    int c0 = ((int)span * a.batches * kGradPieces * 32 + lane) * 8;
-    // this lane's columns in their part; the next ones are two parts on
+    int c0 = (int)span * a.batches * kGradPieces * kGradCols + lane * 8;
+    // this lane's columns in their part, and how far the next ones' are
     const __half *e = a.kept + ((int64_t)(c0 / kHeadStatCols) * a.kept_rows + row) * kHeadStatCols + c0 % kHeadStatCols;
     const float *largest = a.maxima + (int64_t)(c0 / kHeadStatCols) * a.rows + row;
-    const int64_t next_e = 256 * a.kept_rows, next_largest = 256 / kHeadStatCols * a.rows;
-    for (int n = 0; n < a.batches && c0 < vocab; ++n, c0 += kGradPieces * 256) {
+    const int64_t next_e = kGradCols * a.kept_rows, next_largest = kGradCols / kHeadStatCols * a.rows;
+    for (int n = 0; n < a.batches && c0 < vocab; ++n, c0 += kGradPieces * kGradCols) {
         uint4 q[kGradPieces];
         float top[kGradPieces];
 #pragma unroll
         for (int u = 0; u < kGradPieces; ++u) {
-            const int c = c0 + u * 256;
+            const int c = c0 + u * kGradCols;
             q[u] = make_uint4(0u, 0u, 0u, 0u);
             top[u] = 0.0f;
             if (c < vocab && !none) {
@@ -159,11 +161,11 @@ __global__ void __launch_bounds__(32 * kGradWarps) head_gradient_kernel(const Gr
         }
 #pragma unroll
         for (int u = 0; u < kGradPieces; ++u) {
-            const int c = c0 + u * 256;
+            const int c = c0 + u * kGradCols;
             if (c >= vocab)
                 break;
-            const float t = (top[u] - m - logs) * kLog2e, part = exp2_fast(t) * kKeptUnit;
-            const float f0 = part * fmaf(k1, fmaxf(t, -1000.0f) - 15.0f, k0), f1 = part * k1;
+            const float t = (top[u] - m - logs) * kLog2e, part = exp2_fast(t) * (1.0f / kHeadUnit);
+            const float f0 = part * fmaf(k1, fmaxf(t, -1000.0f) - kUnitLog2, k0), f1 = part * k1;
             const Two f00 = two(f0, f0), f11 = two(f1, f1);
             const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
             uint32_t o[4];
@@ -432,7 +434,7 @@ extern "C" int dpo_head_backward(const dpo_head_backward_args *args, void *cuda_
     g.kept_rows = s.kept_rows;
     g.scale = a.scale;
     // up to four batches a span, where that leaves CTAs enough for all SMs
-    const int64_t groups = (T + kGradWarps - 1) / kGradWarps, batches = (V + kGradPieces * 256 - 1) / (kGradPieces * 256);
+    const int64_t groups = (T + kGradWarps - 1) / kGradWarps, batches = (V + kGradPieces * kGradCols - 1) / (kGradPieces * kGradCols);
     g.batches = groups * batches >= 4 * 2048 ? 4 : 1;
     g.spans = (int)((batches + g.batches - 1) / g.batches);
     const int64_t grid = groups * g.spans;

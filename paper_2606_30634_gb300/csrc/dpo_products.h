@@ -34,8 +34,10 @@ int64_t product_share_bytes(int64_t m, int64_t n, int64_t k);
 int store_products(const char *what, const StoreProduct *p, int n, void *stream);
 
 // A head's logits x w^T: what their distributions need, by kHeadStatCols columns, or the logits
-// themselves, or both.
+// themselves, or both. What is kept of e^(z - maximum), in fp16, comes times kHeadUnit, so that values
+// down to 2^-29 keep 11 bits.
 constexpr int kHeadStatCols = 128;
+constexpr float kHeadUnit = 32768.0f;
 struct HeadProduct {
     const void *x, *w;            // bf16, tokens x dim at pitch ld_x, vocab x dim
     int64_t tokens, dim, vocab, ld_x;
@@ -44,7 +46,7 @@ struct HeadProduct {
     float *target;                // z of each token's id
     float *maxima;                // [columns / kHeadStatCols][token], or nullptr: no statistics
     float2 *sums;                 // likewise
-    void *kept;                   // fp16 e^(z - maximum) times 2^15, or nullptr (with statistics):
+    void *kept;                   // fp16 e^(z - maximum) kHeadUnit, or nullptr (with statistics):
     int64_t kept_rows;            // [columns / kHeadStatCols][kept_rows][kHeadStatCols], kept_rows the
                                   // tokens to a multiple of 32
     void *logits;                 // fp32, before the scale, or nullptr
