@@ -51,7 +51,6 @@ __device__ __forceinline__ uint32_t ld_cluster(uint32_t addr)
     asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
     return v;
 }
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) { return __uint_as_float(ld_cluster(addr)); }
 __device__ __forceinline__ void st_cluster(uint32_t addr, uint32_t a)
 {
     asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(addr), "r"(a) : "memory");

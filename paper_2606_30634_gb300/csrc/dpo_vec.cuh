@@ -1,5 +1,5 @@
-// dpo_vec.cuh -- elements of a row as one access of up to 16 bytes, for the kernels that
-// move rows (dpo_rmsnorm.cu, dpo_embed.cu).
+// dpo_vec.cuh -- elements of a row as one access of up to 16 bytes, or two of them, for the kernels
+// that move rows.
 #pragma once
 
 #include "dpo_device.cuh"

@@ -27,7 +27,6 @@ from typing import NamedTuple, Optional
 
 import torch
 
-from . import dpo as _dpo
 from . import ffn as _ffn
 from .dpo import (DPO_EMBED_SPAN, DPO_MAX_TOP, dpo_dropout_args, dpo_embed_args, dpo_embed_backward_args,
                   dpo_embed_workspace, dpo_head_args, dpo_head_backward_args, dpo_head_workspace, dpo_ids,
@@ -148,8 +147,3 @@ EXPORTS = ("dpo_embed", "dpo_embed_backward", "dpo_embed_workspace", "dpo_dropou
            "dpo_logprobs_backward", "dpo_head", "dpo_head_backward", "dpo_head_workspace")
 
 lib = load
-
-
-def call(name: str, args, stream=None) -> None:
-    """One of the calls that take a structure and a stream."""
-    getattr(_dpo, name)(args, stream)
