@@ -792,6 +792,19 @@ def test_head_confident_and_padded_rows(t, d, v):
     assert (dx[1] == 0).all() and o.logp[1] == 0
 
 
+@pytest.mark.parametrize("t,d,v", [(9, 264, 1003), (130, 768, 2051), (600, 1104, 30001)])
+@pytest.mark.parametrize("gd", ["f32", "bf16"])
+def test_head_backward_after_alternatives(t, d, v, gd):
+    """The statistics that the backward takes come from the written logits there."""
+    g, x, w, ids = head_case(t, d, v, seed=4)
+    o, kept, *rest = check_head(x, w, ids, 0.8, 7, True)
+    a, b = (torch.randn(t, generator=g, device=DEV) for _ in range(2))
+    dw = torch.empty(v, d, dtype=DT[gd], device=DEV)
+    dx = ends.head_logprobs_backward(a, kept, x, w, ids, o, dw, dentropy=b)
+    check_head_backward(x, w, ids, 0.8, a, b, o, kept, *rest, (dx, dw), gd)
+    assert ends.status() == 0
+
+
 def test_head_of_large_and_infinite_logits():
     """Logits past 16384 units of log 2 go another way; infinite ones leave their rows no
     distribution and the other rows theirs."""
