@@ -969,6 +969,85 @@ def test_modes_of_pytorch_see_allocations():
     assert (kept[-220:] == 255).all()   # the maxima of 3 parts of 3 tokens are 36 bytes of 256
 
 
+# ------------------------------------------------- more than 2^31 elements ----
+
+def test_embedding_of_a_table_past_32_bits():
+    vocab, dim = 2 ** 20 + 7, 2056
+    g = gen(40)
+    table = torch.zeros(vocab, dim, dtype=torch.bfloat16, device=DEV)
+    ids = torch.tensor([vocab - 1, 0, vocab - 5, 2 ** 20, vocab - 1], device=DEV)
+    table[ids] = randn(g, 5, dim)
+    assert torch.equal(ends.embed(ids, table), table[ids])
+    dy = randn(g, 5, dim)
+    d = torch.full_like(table, 3.0)
+    ends.embed_backward(dy, ids, d)
+    sums = dy.float()
+    sums[0] += sums[4]
+    assert torch.equal(d[ids[:4]], sums[:4].bfloat16())
+    d[ids] = 0
+    assert not d.any()
+    ends.embed_backward(dy, ids, d, accumulate=True)
+    assert torch.equal(d[ids[:4]], sums[:4].bfloat16())
+    many = ids.repeat(vocab // 5 + 1)[:vocab].flip(0)     # as many tokens, so as large an output
+    assert torch.equal(ends.embed(many, table)[-5:], table[many[-5:]])
+
+
+@pytest.mark.parametrize("cols", [2056, 2055])
+def test_dropout_of_rows_past_32_bits(cols):
+    rows = 2 ** 20 + 5
+    x = torch.ones(rows, cols, dtype=torch.bfloat16, device=DEV)
+    y = ends.dropout_add(x, x, 0.25, 5, site=1)
+    for r in (0, 2 ** 20 - 3, rows - 1):
+        words = [ref.philox((c // 8, r, 0, 1), (5, 0))[c % 8 // 2] >> 16 * (c % 2) & 0xFFFF for c in range(cols)]
+        kept = torch.tensor([w >= 16384 for w in words], device=DEV)
+        assert torch.equal(y[r], torch.where(kept, 1 + 65536 / 49152, 1.0).bfloat16())
+
+
+def test_logits_past_32_bits():
+    rows, vocab = 70003, 32001
+    g = gen(41)
+    x = torch.randn(1000, vocab, generator=g, device=DEV).bfloat16().repeat(71, 1)[:rows]
+    ids = torch.randint(0, vocab, (1000,), generator=g, device=DEV).repeat(71)[:rows]
+    a = torch.randn(1000, generator=g, device=DEV).repeat(71)[:rows]
+    for top in (0, 3):
+        o = ends.token_logprobs(x, ids, top=top)
+        for v in o[:5]:
+            assert v is None or torch.equal(v[-1000:], v[rows - 2000:rows - 1000])
+        check_logprobs(x[-7:], ids[-7:], 1.0, top)
+        want, _ = ref.logprobs(np64(x[-7:]), ids[-7:].cpu().numpy())
+        within(o.logp[-7:], want, 1e-5 * np.abs(want), "logp")
+    d = ends.token_logprobs_backward(a, x, ids, o)
+    assert torch.equal(d[-1000:], d[rows - 2000:rows - 1000])
+    g64 = ref.logits_gradient(np64(x[-7:]), ids[-7:].cpu().numpy(), np64(a[-7:]))
+    within(d[-7:], g64, (B + 1e-5) * np.abs(g64) + TINY, "dlogits")
+
+
+def test_head_of_logits_past_32_bits():
+    """40003 x 60001 of them, kept and as G; every 1000 tokens are the first ones again."""
+    tokens, dim, vocab = 40003, 64, 60001
+    _, x, w, ids = head_case(1000, dim, vocab, seed=9)
+    x, ids = x.repeat(41, 1)[:tokens], ids.repeat(41)[:tokens]
+    a = torch.randn(1000, generator=gen(42), device=DEV)
+    o, kept = ends.head_logprobs(x, w, ids, keep=True)
+    assert torch.equal(o.logp[39000:40000], o.logp[:1000])
+    dw = torch.empty(vocab, dim, device=DEV)
+    dx = ends.head_logprobs_backward(a.repeat(41)[:tokens], kept, x, w, ids, o, dw)
+    assert torch.equal(dx[39000:40000], dx[:1000]) and torch.equal(dx[40000:], dx[:3])
+    one, k1, *rest = check_head(x[:1000], w, ids[:1000], 1.0, 0, True)
+    d1 = torch.empty_like(dw)
+    dx1 = ends.head_logprobs_backward(a, k1, x[:1000], w, ids[:1000], one, d1)
+    check_head_backward(x[:1000], w, ids[:1000], 1.0, a, None, one, k1, *rest, (dx1, d1), "f32")
+    assert torch.equal(one.logp, o.logp[:1000])
+    check_head_backward(x[:1000], w, ids[:1000], 1.0, a, None, one, k1, *rest, (dx[:1000], d1), "f32")
+    # dw: 40 times theirs and the first three tokens' again, whose G is rounded; both sums are off by what
+    # the bar of a product of so many terms says, of 41 and of 40 times the magnitudes
+    G, X = ref.logits_gradient(rest[0], rest[1], np64(a)), np64(x[:1000])
+    mag = (1 + B) * np.abs(G).T @ np.abs(X)
+    bar = (41 * (tokens / 4 + 16) + 40 * (1000 / 4 + 16)) * U * mag + 2 * B * np.abs(G[:3]).T @ np.abs(X[:3])
+    within(dw, 40 * np64(d1) + G[:3].T @ X[:3], bar, "dw")
+    assert ends.status() == 0
+
+
 # ---------------------------------------------------------- used together ----
 
 def stage(tokens, table, w_head, dtable, dw, seed):
