@@ -655,7 +655,7 @@ typedef struct {
     dpo_ids ids;                /* rows x cols = tokens */
     const void *table;          /* table_dtype, vocab x dim */
     void *out;                  /* out_dtype, tokens x dim */
-    int64_t vocab, dim;         /* both in [1, 2^31) */
+    int64_t vocab, dim;         /* vocab in [1, 2^31 - 2], dim in [1, 2^31) */
     int64_t ld_table, ld_out;
     float scale;                /* finite */
     int table_dtype, out_dtype; /* DPO_F32 or DPO_BF16 */
@@ -667,7 +667,9 @@ int dpo_embed(const dpo_embed_args *args, void *cuda_stream);
 
 /*
  * dtable[v] (+)= scale * sum over t with id_t = v of dy[t], in fp32, in an order that the
- * ids alone decide (ascending t in spans, then the spans' sums), rounded once for
+ * ids, their number and dim alone decide: the tokens, sorted by id and then by t, are cut into
+ * chunks of equal length (which dim decides too), an id's tokens of a chunk are added in
+ * ascending t, and its chunks' sums by fours: every fourth one, then the four. Rounded once for
  * DPO_EMBED_SPAN tokens; more tokens are added to dtable span after span. Written rows are all of
  * dtable's, or with accumulate those of the ids met.
  */
@@ -698,7 +700,7 @@ int dpo_embed_workspace(int64_t tokens, int64_t vocab, int64_t dim, int64_t *byt
  * (col / 8, row's low word, row's high word, site) under the key seed. The mask depends on
  * (seed, site, row, col) alone; the backward pass is the same call on dy without a
  * residual. Dropped elements do not read as numbers: an infinity or NaN among them is
- * gone. y may be x or residual itself (same pointer and pitch).
+ * gone. y may be x or residual itself (same pointer and pitch) where these are two buffers.
  */
 typedef struct {
     const void *x;              /* dtype, rows x cols */
@@ -736,7 +738,7 @@ typedef struct {
     float *stats;               /* rows x 2 */
     float *top_logp;            /* rows x top */
     int64_t *top_ids;           /* rows x top */
-    int64_t rows, vocab;        /* vocab in [1, 2^31) */
+    int64_t rows, vocab;        /* rows below 2^28, vocab in [1, 2^31 - 2] */
     int64_t ld_logits;
     float scale;                /* 1e-20 to 1e6 */
     int dtype;
@@ -773,8 +775,12 @@ int dpo_logprobs_backward(const dpo_logprobs_backward_args *args, void *cuda_str
  * and the gradients of both,
  *   G = dlogits in bf16 (the type of the products that read it),
  *   dx = G w,  dw (+)= G^T x.
- * Logits are never stored in full precision where `top` is 0. dim is a multiple of 8, vocab any;
- * pointers are 16-byte aligned and the pitches of x and dx multiples of 8.
+ * Where `top` is 0 logits are not stored; with `top` the workspace holds them in fp32, 4 bytes a
+ * logit. What is kept is e^(z - m) in fp16, 2 bytes a logit, with m the largest z of the same 128
+ * columns, and these m: probabilities to 2^-11 down to 2^-29 of the part's largest, less exactly below,
+ * and 0, as their gradients then are, below 2^-40. G takes 2 bytes a logit of the backward's
+ * workspace. dim is a multiple of 8, vocab any, all sides at most 2^26; pointers are 16-byte aligned
+ * and the pitches of x and dx multiples of 8.
  */
 typedef struct {
     const void *x;              /* bf16, tokens x dim */

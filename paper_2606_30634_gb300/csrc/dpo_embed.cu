@@ -6,7 +6,8 @@
 // (each id's tokens in order), and the sorted list is cut into chunks of equal length; a CTA adds
 // up the rows of a chunk, id by id, in fp32. An id's run within one chunk is finished there; of
 // one that crosses chunks every chunk leaves a partial sum, and the chunks' sums are added in a
-// fixed order. So the work is even whatever the ids are, and its order depends on the ids alone.
+// fixed order. So the work is even whatever the ids are, and its order depends on the ids, their
+// number and the rows' width alone.
 // (Joined by the last CTA to leave a sum, behind a fence and a counter, instead of a third launch:
 // 1.3 us more.)
 // A gradient that is written is first cleared as a whole by CTAs beside the sort's, which leaves

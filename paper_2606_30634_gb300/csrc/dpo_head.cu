@@ -5,12 +5,12 @@
 // (maximum m, sum of e^(z - m), entropy sum), so that no logits are written; and the join of a
 // row's parts. For `top` the logits are written and read once more (dpo_logprobs.cu).
 // Kept for the backward: e^(z - m) in fp16, and m. Forming the logits again would cost a third
-// of the backward's two products; reading this costs 2 bytes a logit.
+// of the backward's two products; reading this costs 2 bytes a logit, and holding it as many.
 // Backward, two launches: G from what was kept; dx = G w and dw = G^T x, one list of tiles. Where few
 // tokens leave dx a few tiles of the whole vocabulary's K, these are shared out among more tiles of
 // the list, and a third launch adds the shares up (1001 x 768 x 50257: 205 -> 147 us, the products 82
 // at the burst rate).
-// 8192 x 4096 x 32000, both: 3.6 to 3.9 ms by box and power, 0.9 to 1.0 of the sustained rate; its
+// 8192 x 4096 x 32000, both: 3.6 to 4.1 ms by box and power, 0.9 to 1.0 of the sustained rate; its
 // products 1.07 and 2.24, G 0.17 (6.1 TB/s), the join 0.01.
 #include "dpo_logprobs.cuh"
 #include "dpo_products.h"
@@ -93,6 +93,11 @@ __global__ void __launch_bounds__(32 * kJoinMaxWarps) head_join_kernel(const Joi
 //   g = -scale p (a + b (log p + h)),   p = x 2^-15 e^q,   log2 p = log2 x + q log2(e) - 15,
 // so g = x (k0 + k1 log2 x) with two factors of 128 columns of a row. The id's own element is
 // a (1 - p) from the log probability itself: a kept p near 1 would leave little of it.
+// bf16 because one MMA takes both operands in one type and w and x have that: dx and dw are 0.0023 off in
+// the norm for it, where their own rounding to bf16 is 0.0017 and fp32's nothing; G as two terms would
+// double both products' MMAs. What the tensor cores truncate with the vocabulary or the tokens as K in one
+// chain is less: dx and dw shrink by 1e-5 to 1.3e-4, for 1003 to 128256 of K, so these chains are not
+// cut as the forward's is.
 // rows of a CTA; accesses of 8 columns a lane (by 4, 8 and 16 rows a backward of 1001 x 768 x 50257 is
 // 147, 151 and 154 us)
 constexpr int kGradWarps = 4, kGradPieces = 4;

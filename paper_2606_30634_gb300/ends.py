@@ -49,7 +49,7 @@ def embed(ids, table, *, scale: float = 1.0, dtype=None, out=None, stream=None):
 def embed_backward(dy, ids, dtable, *, scale: float = 1.0, accumulate: bool = False, stream=None):
     """dtable, with the embedding's gradient written over all of it, or with ``accumulate``
     added to the rows of the ids met: the sum of scale * dy over each id's tokens, in fp32,
-    in an order that the ids alone decide."""
+    in an order that the ids, their number and dim alone decide."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return embed_backward(dy, ids, dtable, scale=scale, accumulate=accumulate)
@@ -62,7 +62,7 @@ def dropout_add(x, residual, p: float, seed, *, site: int = 0, out=None, stream=
     function of (seed, site, row, column), so it is not kept: give each step its seed and
     each dropout in it a site. ``seed``: an integer, of which 64 bits count, or an int64 CUDA
     tensor of one element that is read when the kernel runs, for calls captured in a CUDA
-    graph. ``out`` may be x or residual."""
+    graph. ``out`` may be x or residual where these are two tensors."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return dropout_add(x, residual, p, seed, site=site, out=out)
@@ -88,7 +88,8 @@ class LogProbs(NamedTuple):
 
 def token_logprobs(logits, ids=None, *, scale: float = 1.0, top: int = 0, stream=None) -> LogProbs:
     """The log probability of each row's id under softmax(scale * logits), the entropy, and
-    the ``top`` (at most 32) most likely ids. Logits are float32 or bfloat16; -inf masks."""
+    the ``top`` (at most 32) most likely ids, NaN after all others. Logits are float32 or bfloat16;
+    -inf masks."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return token_logprobs(logits, ids, scale=scale, top=top)
@@ -110,7 +111,9 @@ def token_logprobs_backward(dlogp, logits, ids, lp: LogProbs, *, dentropy=None, 
 def head_logprobs(x, w, ids=None, *, scale: float = 1.0, top: int = 0, keep: bool = False, stream=None):
     """(LogProbs, kept): ``token_logprobs`` of the logits x w^T, which are formed in fp32 from
     the bf16 stream and the bf16 weights of the head (vocab x dim). With ``keep`` what the
-    backward needs is kept, an opaque tensor; else it is None."""
+    backward needs is kept, an opaque tensor of 2 bytes a logit and a 64th more (0.53 GB of 8192
+    tokens and a vocabulary of 32000), which every microbatch in flight holds; else it is None. With
+    ``top`` a workspace of 4 bytes a logit is taken for the call."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return head_logprobs(x, w, ids, scale=scale, top=top, keep=keep)
@@ -122,7 +125,8 @@ def head_logprobs_backward(dlogp, kept, x, w, ids, lp: LogProbs, dw, *, dentropy
                            accumulate: bool = False, dx=None, stream=None):
     """dx, from the gradients of lp.logp and, where given, of lp.entropy (float32, one per
     token), and the head's gradient written into dw (fp32 or bf16, ``opt.grads(i)`` reshaped),
-    or with ``accumulate`` added to it. ``kept`` may be used again."""
+    or with ``accumulate`` added to it. ``kept`` may be used again. A workspace of 2 bytes a logit is
+    taken for the call."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return head_logprobs_backward(dlogp, kept, x, w, ids, lp, dw, dentropy=dentropy,
