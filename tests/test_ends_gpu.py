@@ -914,6 +914,45 @@ def test_head_gradient_by_differences():
             assert abs(d - grad[i, j].item()) <= 2e-2 * scale[which] + h * h * 5, (which, k)
 
 
+@pytest.mark.parametrize("t,d,v", [(1, 64, 100), (130, 768, 2051), (520, 72, 20001)])
+@pytest.mark.parametrize("gd", ["f32", "bf16"])
+def test_head_gradient_of_the_weights_alone(t, d, v, gd):
+    """The C call without dx; int32 ids."""
+    g, x, w, ids = head_case(t, d, v, seed=5)
+    ids = torch.where((ids < 0) | (ids >= v), -1, ids).int()
+    o, kept, *rest = check_head(x, w, ids, 0.9, 0, True)
+    a = torch.randn(t, generator=g, device=DEV)
+    for accumulate in (0, 1):
+        old = randn(g, v, d, dtype=DT[gd])
+        dw = old.clone()
+        need = ends.dpo_head_workspace(t, d, v, True)[2]
+        ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+        dpo.dpo_head_backward(ends.dpo_head_backward_args(
+            x=x.data_ptr(), w=w.data_ptr(), ids=ends.dpo_ids(ids.data_ptr(), 1, t, t, 4), kept=kept.data_ptr(),
+            logp=o.logp.data_ptr(), entropy=o.entropy.data_ptr(), stats=o.stats.data_ptr(), dlogp=a.data_ptr(),
+            dw=dw.data_ptr(), tokens=t, dim=d, vocab=v, ld_x=d, scale=0.9, grad_dtype=gd == "bf16",
+            accumulate=accumulate, workspace=ws.data_ptr(), workspace_bytes=need),
+            torch.cuda.current_stream().cuda_stream)
+        check_head_backward(x, w, ids, 0.9, a, None, o, kept, *rest, (None, dw), gd, np64(old) if accumulate else None)
+    assert ends.status() == 0
+
+
+def test_log_probabilities_without_the_entropy():
+    """The C call without entropy, and without ids."""
+    _, x, ids = logits_case(30, 513, "bf16")
+    want = ends.token_logprobs(x, ids, top=3)
+    stats, logp = torch.empty(30, 2, device=DEV), torch.full((30,), 9.0, device=DEV)
+    tl, ti = torch.empty(30, 3, device=DEV), torch.empty(30, 3, dtype=torch.long, device=DEV)
+    for given in (False, True):
+        dpo.dpo_logprobs(ends.dpo_logprobs_args(
+            logits=x.data_ptr(), ids=ends.dpo_ids(ids.data_ptr() if given else None, 1, 30, 30, 8),
+            logp=logp.data_ptr(), stats=stats.data_ptr(), top_logp=tl.data_ptr(), top_ids=ti.data_ptr(), rows=30,
+            vocab=513, ld_logits=x.stride(0), scale=1.0, dtype=dpo.DPO_BF16, top=3), torch.cuda.current_stream().cuda_stream)
+        assert torch.equal(logp, want.logp if given else torch.full_like(logp, 9.0))
+        for a, b in ((stats, want.stats), (tl, want.top_logp), (ti, want.top_ids)):
+            assert torch.equal(a.nan_to_num(), b.nan_to_num())
+
+
 def test_outputs_are_tensors_of_their_own():
     """Each in a storage of its size: one that is kept holds no other's memory, and one that PyTorch
     lets grow does not grow into another."""
